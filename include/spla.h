@@ -282,6 +282,149 @@ int spla_set_length_bound(spla_cache_t *cache, int32_t max_seq_len);
 /* Releases the descriptor only; caller buffers are untouched.  NULL is allowed. */
 int spla_destroy_cache(spla_cache_t *cache);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Around the SPLA cache: rotary positions, and a paged cache with dense attention over it.
+ *
+ * The SPLA calls take queries and keys that already carry their positions, and a model may have layers that attend
+ * densely.  These calls give it both: spla_rope_apply rotates queries and keys, spla_paged_append stores new tokens in
+ * pages (rotating them on the way), spla_paged_attend attends to all cached tokens that a mask leaves.
+ * spla_paged_attend also reads the K/V of an SPLA cache as it lies: page_size = B, page_stride = B,
+ * head_stride = max_blocks * B, and page numbers b * H_kv * max_blocks + block.
+ * The general rules at the top of this file hold.
+ * ------------------------------------------------------------------------------------------------------------------ */
+
+typedef enum {
+  SPLA_ROPE_PLAIN = 0,   /* f_i = base^(-2 i / rot_dim) */
+  SPLA_ROPE_LINEAR = 1,  /* f_i / factor: positions interpolated */
+  SPLA_ROPE_BASE = 2,    /* base * factor^(rot_dim / (rot_dim - 2)) in place of base: low frequencies stretched, high ones kept */
+  SPLA_ROPE_RAMP = 3     /* w f_i + (1 - w) f_i / factor, w = clamp((original_len f_i / 2 pi - ramp_low) / (ramp_high - ramp_low), 0, 1):
+                            kept where a channel turns often over the original length, interpolated where it hardly turns */
+} spla_rope_scaling_t;
+
+typedef struct {
+  int32_t head_dim;       /* channels of a head: a multiple of 8 in [8, 256] */
+  int32_t rot_dim;        /* R: the first R channels are rotated (even, 2..head_dim), the others copied; 0 -> head_dim */
+  int32_t interleaved;    /* 0: channel i turns with i + R/2; 1: 2 i with 2 i + 1 (i < R/2) */
+  int32_t scaling;        /* spla_rope_scaling_t */
+  double base;            /* 0 -> 10000 */
+  double factor;          /* >= 1; 0 -> 1 */
+  double original_len;    /* SPLA_ROPE_RAMP: the length trained on, > 0 */
+  double ramp_low, ramp_high; /* SPLA_ROPE_RAMP: turns over original_len below / above which a frequency is interpolated / kept; low < high */
+  double amplitude;       /* multiplies the rotated channels; 0 -> 1 */
+} spla_rope_config_t;
+
+typedef struct spla_rope spla_rope_t; /* opaque host-side table of frequencies */
+
+/* HOST pointers; no device memory is involved.  The frequencies are computed in double precision and kept as 64-bit
+ * fractions of a turn, so that the angle of a position is exact modulo whole turns up to 2^31 (to 2^-64 of a turn per position). */
+int spla_rope_create(const spla_rope_config_t *config, spla_rope_t **rope_out);
+int spla_rope_destroy(spla_rope_t *rope);   /* NULL is allowed */
+
+/* Heads of head_dim consecutive channels: element (b, t, h, c) of `in` lies at in[b * in_batch + t * in_token + h * in_head + c]. */
+typedef struct {
+  const void *in;                        /* DEVICE, aligned to its element */
+  void *out;                             /* DEVICE; equal to `in` with equal strides (in place), else not overlapping it */
+  int32_t n_heads;
+  int64_t in_batch, in_token, in_head;   /* strides in elements */
+  int64_t out_batch, out_token, out_head;
+} spla_rope_tensor_t;
+
+/*
+ * Rotates queries and keys: y_a = A (x_a cos t - x_b sin t), y_b = A (x_b cos t + x_a sin t), t = position * f_i, computed in
+ * fp32 and rounded once.  With transpose != 0 the sines change sign: the gradient of the rotation for a gradient of its output.
+ *   positions: DEVICE int32 [batch][n_tokens], of any sign.
+ *   q, k:      HOST descriptors; k may be NULL.  dtype: spla_dtype_t of both.  Strides and addresses that are multiples of
+ *              16 bytes (and R a multiple of 16) take wide accesses; any others work.
+ */
+int spla_rope_apply(const spla_rope_t *rope, const int32_t *positions, int32_t batch, int32_t n_tokens,
+                    const spla_rope_tensor_t *q, const spla_rope_tensor_t *k, int32_t dtype, int32_t transpose, void *stream);
+
+typedef struct {
+  int32_t n_q_heads;     /* H_q */
+  int32_t n_kv_heads;    /* H_kv; G = H_q / H_kv must be an integer in [1, 16] */
+  int32_t head_dim;      /* d: 64 or 128 */
+  int32_t page_size;     /* P: 16, 32, 64 or 128 tokens */
+  int32_t n_pages;       /* page numbers are in [0, n_pages) */
+  int32_t kv_dtype;      /* spla_dtype_t of k_pages, v_pages, k_new, v_new */
+  int32_t q_dtype;       /* spla_dtype_t of q and out */
+  int64_t page_stride;   /* rows (of d elements) from a page of a head to the same head's in the next page; 0 -> H_kv * P */
+  int64_t head_stride;   /* rows from a page of a head to the next head's; 0 -> P.  Rows of different (page, head) must not overlap */
+  float sm_scale;        /* multiplies q.k; 0 -> 1/sqrt(d) */
+  uint32_t flags;        /* SPLA_GENERAL_KERNELS or 0 */
+} spla_paged_config_t;
+
+typedef struct spla_paged spla_paged_t; /* opaque host-side descriptor */
+
+/*
+ * k_pages, v_pages: DEVICE, 256-byte aligned, rows of d elements: token t of page g and KV head h is row g * page_stride + h * head_stride + t
+ *                   ([n_pages][H_kv][P][d] with the default strides).
+ * status:           DEVICE int32 [1], set to 0 by the caller before the first call: what only the device sees is latched there.
+ */
+int spla_paged_create(const spla_paged_config_t *config, void *k_pages, void *v_pages, int32_t *status, spla_paged_t **paged_out);
+int spla_paged_destroy(spla_paged_t *paged);   /* NULL is allowed */
+
+/*
+ * The new tokens of a call: rows cu_new[b] .. cu_new[b + 1] - 1 belong to sequence b and are its last n_b tokens, at positions
+ * seq_lens[b] - n_b ..; seq_lens counts them.  Rows from cu_new[batch] on are not touched.  Position x of sequence b lies in page
+ * page_table[b * table_stride + x / P].  A sequence whose numbers are not consistent (cu_new not ascending inside [0, total_new],
+ * n_b > max_new, seq_lens[b] < n_b or > max_len) is skipped, its rows are not touched, and SPLA_ERR_BOUNDS is latched.  The
+ * tokens of a page number outside [0, n_pages) are not stored, read as zeros, and latch SPLA_ERR_BOUNDS.
+ */
+typedef struct {
+  const int32_t *cu_new;      /* DEVICE [batch + 1] */
+  const int32_t *seq_lens;    /* DEVICE [batch] */
+  const int32_t *page_table;  /* DEVICE [batch][table_stride] */
+  int32_t batch;              /* >= 1 */
+  int32_t total_new;          /* rows of the new tokens' tensors, >= 1 */
+  int32_t max_new;            /* HOST bound of n_b, >= 1 */
+  int32_t max_len;            /* HOST bound of seq_lens[b], in [max_new, 2^24] and at most table_stride * P */
+  int32_t table_stride;
+} spla_paged_batch_t;
+
+/*
+ * Stores new keys and values in their pages, the keys rotated by `rope` (NULL: as they are), and rotates the queries beside them.
+ *   k_new, v_new: DEVICE [total_new][H_kv][d] kv_dtype, rows k_stride / v_stride elements apart (0 -> H_kv * d).
+ *   positions:    DEVICE int32 [total_new], the rotation's positions; NULL: the positions in the sequence.
+ *   q, q_out:     DEVICE [total_new][H_q][d] q_dtype, rows q_stride / q_out_stride elements apart (0 -> H_q * d); both NULL: no
+ *                 queries.  q_out may be q (with the same stride).  Without `rope` they are copied.
+ * Addresses and strides: multiples of 16 bytes, or else of the element.
+ */
+int spla_paged_append(spla_paged_t *paged, const spla_paged_batch_t *batch, const spla_rope_t *rope, const int32_t *positions,
+                      const void *k_new, int64_t k_stride, const void *v_new, int64_t v_stride, const void *q, int64_t q_stride,
+                      void *q_out, int64_t q_out_stride, void *stream);
+
+/* What a query's scores go through.  Query at position p, key at position j:
+ *   s = sm_scale q.k;  softcap > 0: s = softcap tanh(s / softcap);  slopes: s -= slopes[head] |p - j|.
+ * Visible are the j with max(0, p - window + 1, first_key) <= j < min(seq_len, max(p + 1, prefix_len)). */
+typedef struct {
+  float softcap;               /* 0: none */
+  int32_t window;              /* 0: none; else the last `window` positions, the query's own among them */
+  const float *slopes;         /* DEVICE fp32 [H_q] or NULL */
+  const int32_t *first_key;    /* DEVICE int32 [total_new] or NULL: where the document of each new token starts */
+  const int32_t *prefix_lens;  /* DEVICE int32 [batch] or NULL: so many first tokens are visible from every position */
+} spla_paged_mask_t;
+
+/* Scratch that spla_paged_attend needs for these sizes (HOST; may be 0).  Only host values of `batch` are used. */
+int spla_paged_query_workspace(const spla_paged_t *paged, const spla_paged_batch_t *batch, size_t *bytes_out);
+
+/*
+ * Softmax attention of the new tokens over the cache, which holds them already.  Keys outside a query's mask do not touch its
+ * result, whatever they hold.  A query that sees no key yields out = 0 and lse = -infinity.
+ *   q:    DEVICE [total_new][H_q][d] q_dtype, rows q_stride elements apart (0 -> H_q * d), aligned to the element (to 16 bytes for
+ *         the tensor-core kernel).
+ *   mask: HOST or NULL (causal only).
+ *   out:  DEVICE [total_new][H_q][d] q_dtype.  lse: DEVICE fp32 [total_new][H_q] or NULL: ln of the sum of exp(s).
+ *   workspace: DEVICE, 256-byte aligned, as spla_paged_query_workspace says; NULL where that is 0.  Calls that may overlap need
+ *         one each.
+ * bf16 caches and queries run on the tensor cores (probabilities rounded to bf16, sums in fp32); the others, and
+ * SPLA_GENERAL_KERNELS, in fp32.  Results do not depend on max_new, max_len or the rows of other sequences beyond rounding.
+ */
+int spla_paged_attend(spla_paged_t *paged, const spla_paged_batch_t *batch, const void *q, int64_t q_stride,
+                      const spla_paged_mask_t *mask, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/* As spla_sync_status, for the status word of `paged`. */
+int spla_paged_sync_status(spla_paged_t *paged, void *stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char *spla_status_string(int status);
 

@@ -1,0 +1,267 @@
+// The paged cache and the rotary positions: parameters of their kernels and the division of the attention's work, shared by
+// the translation units (not part of the public ABI).
+#pragma once
+
+#include "spla_internal.h"
+
+namespace spla {
+
+constexpr int kRopeMaxPairs = 128;
+
+// Frequencies as 64-bit fractions of a turn: position x frequency wraps at whole turns by itself, so that what is left for
+// the sine and cosine is the exact angle modulo a turn, at any position.
+struct RopeTable {
+  unsigned long long freq[kRopeMaxPairs];
+  int dim, rot, interleaved;            // head channels, rotated ones (0: copy only), pairing
+  float amplitude;
+};
+
+// A group of heads that one launch rotates or copies.
+struct RopeGroup {
+  const void* in;
+  void* out;                            // null: the group goes to pages
+  int n_heads, rotate;
+  long long in_batch, in_token, in_head, out_batch, out_token, out_head;   // elements
+  int elem_f32;                         // element type: 1 = fp32, 0 = bf16
+};
+
+struct PagedBatch {
+  const int* cu;                        // [batch + 1] rows of the new tokens
+  const int* lens;                      // [batch] cached tokens, the new ones included
+  const int* table;                     // [batch][table_stride]
+  int batch, total_new, max_new, max_len, table_stride;
+};
+
+struct PagedLayout {
+  int Hq, Hkv, G, d, P, log_p, n_pages;
+  long long page_stride, head_stride;   // rows
+  int* status;
+};
+
+// One sequence's new tokens: first row, count, cached tokens; n = 0 where there is nothing to do or the numbers do not fit together.
+struct PagedSeq {
+  int row0, n, L;
+};
+__device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& pb, int* status, int b) {
+  const int r0 = __ldg(pb.cu + b), r1 = __ldg(pb.cu + b + 1), L = __ldg(pb.lens + b);
+  PagedSeq s{r0, r1 - r0, L};
+  const bool fits = r0 >= 0 && r1 >= r0 && r1 <= pb.total_new && r1 - r0 <= pb.max_new && L >= r1 - r0 && L <= pb.max_len;
+  if (!fits) {
+    atomicExch(status, kStatusBounds);
+    s.n = 0;
+  }
+  return s;
+}
+
+// ---- division of the attention's work --------------------------------------------------------------------------------
+// A unit is one KV head's query rows of neighbouring new tokens (`upos` positions x G heads; a sequence of at most `ppos` new tokens
+// is one unit of one row tile).  It walks the key tiles of TK tokens that any of its positions sees.  The tiles of all units, in the
+// order sequence, head, unit, are dealt out in equal contiguous shares to the CTAs of one resident wave: every CTA carries the
+// same number of tiles however ragged the lengths are.  A unit that a share's border cuts leaves partial results (maximum, sum,
+// unnormalised output per row) that a second kernel joins, in the order of the shares: no atomics, the same bits every time.
+// Short caches are dealt out by whole units instead, which needs no second kernel.
+constexpr int kPagedMaxBatch = 512;    // sequences per launch (the host cuts larger batches)
+
+struct PagedWork {
+  int ppos, upos, TK;
+  int by_unit;                          // dealt out by units instead of tiles
+  int n_cta, min_tiles;
+  int rows;                             // rows that a partial result holds
+  float* part_o;                        // [2 n_cta][rows][d]
+  float2* part_ml;                      // [2 n_cta][rows]  maximum (base 2), sum
+};
+
+struct PagedAttend {
+  PagedBatch pb;
+  PagedLayout pl;
+  PagedWork w;
+  const void* q;
+  long long q_stride;
+  void* out;
+  float* lse;
+  float sm_scale, softcap;
+  int window;
+  const float* slopes;
+  const int* first_key;
+  const int* prefix;
+  int wait_limit, dbg_tx_extra;         // as in Params
+};
+
+// Sequence table of a CTA, in shared memory.
+struct PagedSeqs {
+  long long pre[kPagedMaxBatch + 1];    // tiles (units) before a sequence, all heads
+  int row0[kPagedMaxBatch], n[kPagedMaxBatch], L[kPagedMaxBatch], prefix[kPagedMaxBatch];
+};
+
+__host__ __device__ __forceinline__ int paged_units(const PagedWork& w, int n) { return n <= w.ppos ? (n > 0) : (n + w.upos - 1) / w.upos; }
+
+// Key tiles [t0, t1) that unit u of a sequence walks (its documents' starts are left aside here).  Never empty: a position sees itself.
+struct PagedSpan {
+  int t0, t1;
+};
+__device__ __forceinline__ PagedSpan paged_span(const PagedWork& w, int window, int n, int L, int prefix, int u) {
+  const int p0 = L - n + u * w.upos, p1 = L - n + min(n, (u + 1) * w.upos) - 1;
+  const int lo = window > 0 ? max(0, p0 - window + 1) : 0, hi = min(L, max(p1 + 1, prefix));
+  return PagedSpan{lo / w.TK, (hi + w.TK - 1) / w.TK};
+}
+__device__ __forceinline__ int paged_unit_tiles(const PagedWork& w, int window, int n, int L, int prefix, int u) {
+  if (w.by_unit) return 1;
+  const PagedSpan s = paged_span(w, window, n, L, prefix, u);
+  return s.t1 - s.t0;
+}
+
+// Fills the table; all threads of the CTA (whole warps), ends with a barrier.  Returns the total.
+__device__ __forceinline__ long long paged_fill_seqs(const PagedAttend& a, PagedSeqs& t, int tid, int threads) {
+  const int batch = a.pb.batch;
+  for (int b = tid; b < batch; b += threads) {
+    const PagedSeq s = paged_seq(a.pb, a.pl.status, b);
+    const int pre = a.prefix ? __ldg(a.prefix + b) : 0;
+    t.row0[b] = s.row0; t.n[b] = s.n; t.L[b] = s.L; t.prefix[b] = pre;
+    const int nu = paged_units(a.w, s.n);
+    long long sum = 0;
+    if (nu <= 4)
+      for (int u = 0; u < nu; ++u) sum += paged_unit_tiles(a.w, a.window, s.n, s.L, pre, u);
+    t.pre[b + 1] = sum;
+  }
+  __syncthreads();
+  for (int b = tid >> 5; b < batch; b += threads >> 5) {
+    const int n = t.n[b], nu = paged_units(a.w, n);
+    if (nu <= 4) continue;
+    int sum = 0;
+    for (int u = tid & 31; u < nu; u += 32) sum += paged_unit_tiles(a.w, a.window, n, t.L[b], t.prefix[b], u);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if ((tid & 31) == 0) t.pre[b + 1] = sum;
+  }
+  __syncthreads();
+  if (tid < 32) {
+    long long carry = 0;
+    for (int b0 = 0; b0 < batch; b0 += 32) {
+      const int b = b0 + tid;
+      long long v = b < batch ? t.pre[b + 1] * a.pl.Hkv : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long x = __shfl_up_sync(0xffffffffu, v, o);
+        if (tid >= o) v += x;
+      }
+      v += carry;
+      carry = __shfl_sync(0xffffffffu, v, 31);
+      if (b < batch) t.pre[b + 1] = v;
+    }
+    if (tid == 0) t.pre[0] = 0;
+  }
+  __syncthreads();
+  return t.pre[batch];
+}
+
+// Tiles (units) per CTA.
+__device__ __forceinline__ long long paged_share(const PagedWork& w, long long total) {
+  const long long per = (total + w.n_cta - 1) / w.n_cta;
+  return per < w.min_tiles ? w.min_tiles : per;
+}
+
+// A CTA's walk over its share: one segment (a run of key tiles of one unit) after the other.  Every role keeps its own copy.
+struct PagedWalk {
+  long long left;                       // tiles (units) still to walk
+  int b, h, u, off;                     // off: tiles of the unit that earlier segments (other CTAs) have
+  int row0, n, L, prefix;
+  // the current segment
+  int t0, t1;                           // key tiles
+  bool head, tail;                      // it starts / ends the unit
+
+  __device__ __forceinline__ void load(const PagedSeqs& t) { row0 = t.row0[b]; n = t.n[b]; L = t.L[b]; prefix = t.prefix[b]; }
+  // Goes to tile `at` of all; false if there is none.
+  __device__ __forceinline__ bool seek(const PagedAttend& a, const PagedSeqs& t, long long at, long long count) {
+    const long long total = t.pre[a.pb.batch];
+    left = min(count, total - at);
+    if (left <= 0) { left = 0; return false; }
+    int lo = 0, hi = a.pb.batch;        // the last b with pre[b] <= at
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (t.pre[mid] <= at) lo = mid; else hi = mid;
+    }
+    b = lo;
+    load(t);
+    const long long per_head = (t.pre[b + 1] - t.pre[b]) / a.pl.Hkv, rem = at - t.pre[b];
+    h = (int)(rem / per_head);
+    int in_head = (int)(rem - h * per_head);
+    u = 0;
+    for (;;) {
+      const int c = paged_unit_tiles(a.w, a.window, n, L, prefix, u);
+      if (in_head < c) break;
+      in_head -= c;
+      ++u;
+    }
+    off = in_head;
+    return true;
+  }
+  __device__ __forceinline__ bool next(const PagedAttend& a, const PagedSeqs& t) {
+    if (left <= 0) return false;
+    if (u >= paged_units(a.w, n)) {                  // the unit before was its head's last
+      u = 0;
+      if (++h == a.pl.Hkv) {
+        h = 0;
+        do ++b; while (b < a.pb.batch - 1 && t.pre[b + 1] == t.pre[b]);
+        load(t);
+      }
+    }
+    const PagedSpan s = paged_span(a.w, a.window, n, L, prefix, u);
+    if (a.w.by_unit) {
+      t0 = s.t0; t1 = s.t1; head = tail = true;
+      left -= 1;
+    } else {
+      t0 = s.t0 + off;
+      t1 = (int)min((long long)s.t1, t0 + left);
+      head = off == 0; tail = t1 == s.t1;
+      left -= t1 - t0;
+    }
+    off = 0;
+    u_cur = u++;
+    return true;
+  }
+  int u_cur;                            // unit of the current segment
+  __device__ __forceinline__ int first_pos(const PagedWork& w) const { return u_cur * w.upos; }   // index of its first new token in the sequence
+  __device__ __forceinline__ int n_pos(const PagedWork& w) const { return min(n - u_cur * w.upos, n <= w.ppos ? w.ppos : w.upos); }
+};
+
+// Keys [lo, hi) that the new token with index i of a sequence sees.
+struct PagedSees {
+  int lo, hi;
+};
+__device__ __forceinline__ PagedSees paged_sees(const PagedAttend& a, int row0, int n, int L, int prefix, int i) {
+  const int pos = L - n + i;
+  PagedSees s;
+  s.lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+  if (a.first_key) s.lo = max(s.lo, __ldg(a.first_key + row0 + i));
+  s.hi = min(L, max(pos + 1, prefix));
+  return s;
+}
+
+// First row of page `index` of a sequence's head; -1 where the page number is outside the pool.
+__device__ __forceinline__ long long paged_row(const PagedBatch& pb, const PagedLayout& pl, int b, int h, int index) {
+  const int page = __ldg(pb.table + (long long)b * pb.table_stride + index);
+  if ((unsigned)page >= (unsigned)pl.n_pages) {
+    atomicExch(pl.status, kStatusBounds);
+    return -1;
+  }
+  return page * pl.page_stride + h * pl.head_stride;
+}
+
+struct PagedMaps {                      // TMA tensor maps (CUtensorMap), opaque to the host code
+  alignas(64) unsigned char k[128];
+  alignas(64) unsigned char v[128];
+  alignas(64) unsigned char q[128];
+};
+
+// rope.cu: rotates / copies up to three groups; with `pages` the groups with out == null go to k_pages (group 1) and v_pages (group 2)
+cudaError_t launch_rope(const RopeTable& rt, const int* positions, int batch, int tokens, const RopeGroup* groups, int n_groups,
+                        const PagedBatch* pb, const PagedLayout* pl, void* k_pages, void* v_pages, int transpose, cudaStream_t s);
+// paged_attend.cu: fp32 kernels for every type, and the join of cut units
+void paged_plan_general(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int window, int sm_count);
+cudaError_t launch_paged_general(const PagedAttend& a, const void* k_pages, const void* v_pages, int q_bf16, int kv_bf16, cudaStream_t s);
+cudaError_t launch_paged_join(const PagedAttend& a, int out_bf16, cudaStream_t s);
+// paged_mma.cu: bf16 on tcgen05
+void paged_plan_mma(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int window, int sm_count);
+cudaError_t launch_paged_mma(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s);
+
+}  // namespace spla

@@ -1,0 +1,413 @@
+// Attention of new tokens over a paged cache, in fp32 arithmetic for every type (fp32 caches or queries, addresses that TMA does not
+// take), and the kernel that joins the partial results of units cut between CTAs, whichever kernel made them.
+//
+//   s_ij = scale q_i.k_j;  s <- cap tanh(s / cap);  s <- s - slope |p_i - j|;  o_i = sum_j softmax(s)_ij v_j;  lse_i = ln sum_j exp(s_ij)
+//
+// One pass over the keys with the running maximum and sum of the softmax in base 2.  A CTA walks tiles of TK keys for R query
+// rows: scores from row pieces in shared memory (four rows x KT keys per thread, packed FMAs over two channels), then the
+// product with V (four rows x CW channels per thread, the tile's tokens shared by TS threads).  R = 4, 16 and 64 by the rows that a
+// unit has at most; a row tile's products cost the same however few of its rows are real.  4 and 16 rows are bound by reading K and V, 64 by the FMA pipe.
+#include "paged.h"
+
+namespace spla {
+
+namespace {
+
+constexpr int kPgThreads = 256;
+
+template <int R, int D>
+struct PgShape {
+  static constexpr int TK = R == 64 ? 32 : 64;
+  static constexpr int KT = R == 64 ? 2 : 1;                       // keys per thread
+  static constexpr int RG = R / 4;                                 // groups of four rows
+  static constexpr int CS = kPgThreads / (RG * (TK / KT));         // threads that share the channels of a score
+  static constexpr int CW = R == 64 ? D / 16 : 4;                  // channels per thread in the product with V
+  static constexpr int TS = kPgThreads / (RG * (D / CW));          // threads that share a tile's tokens there
+  static constexpr int LD = D + 4, LP = TK + 4;
+  static constexpr int kQ = 0, kK = kQ + R * LD * 4, kV = kK + TK * LD * 4, kP = kV + TK * D * 4, kFac = kP + R * LP * 4, kLo = kFac + R * 4,
+                       kHi = kLo + R * 4, kSum = kHi + R * 4, kMax = kSum + R * 4, kSeqs = (kMax + R * 4 + 15) / 16 * 16,
+                       kBytes = kSeqs + (int)sizeof(PagedSeqs);
+  static_assert(CS >= 1 && TS >= 1 && D % (4 * CS) == 0, "shape");
+  static_assert((TS - 1) * R * D * 4 <= TK * (LD + D) * 4, "the partial products of a unit fit the K and V tiles");
+};
+
+template <typename T>
+__device__ __forceinline__ float4 load4(const T* p) {
+  float v[4];
+  load_vec<4>(p, v);
+  return make_float4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) { *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)); }
+
+template <typename TQ, typename TKV, int R, int D>
+__global__ void __launch_bounds__(kPgThreads, 2)
+    paged_general_kernel(const PagedAttend a, const TKV* __restrict__ k_pages, const TKV* __restrict__ v_pages) {
+  using S = PgShape<R, D>;
+  constexpr int TK = S::TK, KT = S::KT, CS = S::CS, CW = S::CW, TS = S::TS, LD = S::LD, LP = S::LP, D4 = D / 4;
+  extern __shared__ __align__(16) unsigned char smem[];
+  float* qs = reinterpret_cast<float*>(smem + S::kQ);
+  float* ks = reinterpret_cast<float*>(smem + S::kK);
+  float* vs = reinterpret_cast<float*>(smem + S::kV);
+  float* ps = reinterpret_cast<float*>(smem + S::kP);
+  float* fac = reinterpret_cast<float*>(smem + S::kFac);
+  int* lo_s = reinterpret_cast<int*>(smem + S::kLo);
+  int* hi_s = reinterpret_cast<int*>(smem + S::kHi);
+  float* sum_s = reinterpret_cast<float*>(smem + S::kSum);
+  float* max_s = reinterpret_cast<float*>(smem + S::kMax);
+  PagedSeqs& seqs = *reinterpret_cast<PagedSeqs*>(smem + S::kSeqs);
+  pdl_wait();
+  pdl_launch_dependents();
+  const int tid = threadIdx.x, G = a.pl.G;
+  const long long share = paged_share(a.w, paged_fill_seqs(a, seqs, tid, kPgThreads));
+  PagedWalk wk;
+  if (!wk.seek(a, seqs, blockIdx.x * share, share)) return;
+  // scores: thread = (channel share, key, row group); product: (channel group, token share, row group)
+  const int cs = tid % CS, kg = tid / CS % (TK / KT), rg = tid / (CS * (TK / KT));
+  const int cg = tid % (D / CW), ts = tid / (D / CW) % TS, rp = tid / (D / CW * TS);
+  const float sc = a.sm_scale, inv_cap = a.softcap > 0.f ? 1.f / a.softcap : 0.f;
+  while (wk.next(a, seqs)) {
+    const int i0 = wk.first_pos(a.w), rows = wk.n_pos(a.w) > wk.n - i0 ? (wk.n - i0) * G : wk.n_pos(a.w) * G;
+    const int pos0 = wk.L - wk.n + i0;
+    __syncthreads();                                               // the segment before is done with shared memory
+    for (int x = tid; x < R * D4; x += kPgThreads) {
+      const int r = x / D4, c = x % D4;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r < rows) {
+        const TQ* q = reinterpret_cast<const TQ*>(a.q) + (wk.row0 + i0 + r / G) * a.q_stride + (long long)(wk.h * G + r % G) * D + c * 4;
+        if (((uintptr_t)a.q | (uintptr_t)(a.q_stride * sizeof(TQ))) % (4 * sizeof(TQ)) == 0) v = load4(q);
+        else v = make_float4(to_float(q[0]), to_float(q[1]), to_float(q[2]), to_float(q[3]));
+      }
+      *reinterpret_cast<float4*>(qs + r * LD + c * 4) = v;
+    }
+    if (tid < R) {
+      PagedSees s{0, 0};
+      if (tid < rows) s = paged_sees(a, wk.row0, wk.n, wk.L, wk.prefix, i0 + tid / G);
+      lo_s[tid] = s.lo;
+      hi_s[tid] = s.hi;
+    }
+    float slope[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) slope[i] = a.slopes && rg * 4 + i < rows ? __ldg(a.slopes + wk.h * G + (rg * 4 + i) % G) : 0.f;
+    float m[4], l[4], o[4][CW];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+#pragma unroll
+      for (int x = 0; x < CW; ++x) o[i][x] = 0.f;
+    }
+#pragma unroll 1
+    for (int t = wk.t0; t < wk.t1; ++t) {
+      const int tok0 = t * TK;
+      __syncthreads();                                             // rows' bounds; the tile before is used up
+      bool bad = false;                                            // a value that is not finite
+#pragma unroll
+      for (int x0 = 0; x0 < TK * D4; x0 += kPgThreads) {
+        const int x = x0 + tid, j = x / D4, c = x % D4, tok = tok0 + j;
+        float4 kv = make_float4(0.f, 0.f, 0.f, 0.f), vv = kv;
+        if (tok < wk.L) {
+          const long long first = paged_row(a.pb, a.pl, wk.b, wk.h, tok >> a.pl.log_p);
+          if (first >= 0) {
+            const long long at = (first + (tok & (a.pl.P - 1))) * D + c * 4;
+            kv = load4(k_pages + at);
+            vv = load4(v_pages + at);
+          }
+        }
+        *reinterpret_cast<float4*>(ks + j * LD + c * 4) = kv;
+        *reinterpret_cast<float4*>(vs + j * D + c * 4) = vv;
+        bad |= !(fabsf(vv.x) < INFINITY && fabsf(vv.y) < INFINITY && fabsf(vv.z) < INFINITY && fabsf(vv.w) < INFINITY);
+      }
+      bad = __syncthreads_or(bad);
+      // ---- scores of four rows x KT keys, this thread's share of the channels
+      float2 acc[4][KT];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int y = 0; y < KT; ++y) acc[i][y] = make_float2(0.f, 0.f);
+#pragma unroll 4
+      for (int c = cs * 4; c < D; c += 4 * CS) {
+        float4 kx[KT];
+#pragma unroll
+        for (int y = 0; y < KT; ++y) kx[y] = *reinterpret_cast<const float4*>(ks + (kg + y * (TK / KT)) * LD + c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 qx = *reinterpret_cast<const float4*>(qs + (rg * 4 + i) * LD + c);
+#pragma unroll
+          for (int y = 0; y < KT; ++y) {
+            acc[i][y] = __ffma2_rn(make_float2(qx.x, qx.y), make_float2(kx[y].x, kx[y].y), acc[i][y]);
+            acc[i][y] = __ffma2_rn(make_float2(qx.z, qx.w), make_float2(kx[y].z, kx[y].w), acc[i][y]);
+          }
+        }
+      }
+      // ---- running maximum and sum; every row belongs to CS x TK / KT neighbouring threads
+      float s[4][KT], mt[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = rg * 4 + i, lo = lo_s[r], hi = hi_s[r], pos = pos0 + r / G;
+        mt[i] = -INFINITY;
+#pragma unroll
+        for (int y = 0; y < KT; ++y) {
+          float v = acc[i][y].x + acc[i][y].y;
+#pragma unroll
+          for (int w = 1; w < CS; w <<= 1) v += __shfl_xor_sync(0xffffffffu, v, w);
+          v *= sc;
+          if (a.softcap > 0.f) v = a.softcap * tanhf(v * inv_cap);
+          const int j = tok0 + kg + y * (TK / KT);
+          if (slope[i] != 0.f) v -= slope[i] * (float)abs(pos - j);
+          s[i][y] = j >= lo && j < hi ? v * kLog2e : -INFINITY;
+          mt[i] = fmaxf(mt[i], s[i][y]);
+        }
+      }
+      constexpr int kRowThreads = CS * (TK / KT);                  // 16 (R = 64: half a warp), 64 (two warps) or 256
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int w = kRowThreads < 32 ? kRowThreads / 2 : 16; w >= CS; w >>= 1) mt[i] = fmaxf(mt[i], __shfl_xor_sync(0xffffffffu, mt[i], w));
+      if constexpr (kRowThreads > 32) {                            // across the warps of a row group, through the score tile
+        constexpr int W = kRowThreads / 32;
+        const int w = tid / 32 % W;
+        if (tid % 32 == 0)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) ps[(rg * 4 + i) * LP + w] = mt[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int x = 0; x < W; ++x) mt[i] = fmaxf(mt[i], ps[(rg * 4 + i) * LP + x]);
+        __syncthreads();
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float mn = fmaxf(m[i], mt[i]), f = m[i] == mn ? 1.f : ex2(m[i] - mn), nm = mn == -INFINITY ? 0.f : -mn;
+        m[i] = mn;
+        l[i] *= f;
+        if (tid % kRowThreads == 0) fac[rg * 4 + i] = f;
+#pragma unroll
+        for (int y = 0; y < KT; ++y) {
+          const float p = ex2(s[i][y] + nm);
+          l[i] += p;                                               // (this thread's keys only, until the segment's end)
+          if (cs == 0) ps[(rg * 4 + i) * LP + kg + y * (TK / KT)] = p;
+        }
+      }
+      __syncthreads();
+      // ---- product with V: four rows x CW channels, every TS-th group of four tokens
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float f = fac[rp * 4 + i];
+#pragma unroll
+        for (int x = 0; x < CW; ++x) o[i][x] *= f;
+      }
+      if (!bad) {
+#pragma unroll 2
+        for (int j = ts * 4; j < TK; j += 4 * TS) {
+          float4 p[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[i] = *reinterpret_cast<const float4*>(ps + (rp * 4 + i) * LP + j);
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            float4 v[CW / 4];
+#pragma unroll
+            for (int x = 0; x < CW / 4; ++x) v[x] = *reinterpret_cast<const float4*>(vs + (j + y) * D + x * (D * 4 / CW) + cg * 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float w = y == 0 ? p[i].x : y == 1 ? p[i].y : y == 2 ? p[i].z : p[i].w;
+#pragma unroll
+              for (int x = 0; x < CW / 4; ++x) {
+                float2* d = reinterpret_cast<float2*>(&o[i][x * 4]);
+                d[0] = __ffma2_rn(make_float2(w, w), make_float2(v[x].x, v[x].y), d[0]);
+                d[1] = __ffma2_rn(make_float2(w, w), make_float2(v[x].z, v[x].w), d[1]);
+              }
+            }
+          }
+        }
+      } else {                                                     // 0 x infinity is no 0: hidden keys stay out
+#pragma unroll 1
+        for (int j = ts; j < TK; j += TS)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = rp * 4 + i;
+            if (tok0 + j < lo_s[r] || tok0 + j >= hi_s[r]) continue;
+#pragma unroll
+            for (int x = 0; x < CW; ++x) o[i][x] = fmaf(ps[r * LP + j], vs[j * D + x / 4 * (D * 4 / CW) + cg * 4 + x % 4], o[i][x]);
+          }
+      }
+    }
+    // ---- end of the segment: sums over the threads of a row, then over the token shares
+    constexpr int kRowThreads = CS * (TK / KT);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int w = kRowThreads < 32 ? kRowThreads / 2 : 16; w >= CS; w >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
+    __syncthreads();
+    if constexpr (kRowThreads > 32) {
+      constexpr int W = kRowThreads / 32;
+      if (tid % 32 == 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ps[(rg * 4 + i) * LP + tid / 32 % W] = l[i];
+      __syncthreads();
+      if (tid < R) {
+        float sum = 0.f;
+        for (int x = 0; x < W; ++x) sum += ps[tid * LP + x];
+        sum_s[tid] = sum;
+      }
+    } else if (tid % kRowThreads == 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum_s[rg * 4 + i] = l[i];
+    }
+    if (tid % kRowThreads == 0)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) max_s[rg * 4 + i] = m[i];
+    if constexpr (TS > 1) {
+      float* part = ks;                                            // (K and V are used up)
+      if (ts > 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int x = 0; x < CW; x += 4)
+            *reinterpret_cast<float4*>(part + ((ts - 1) * R + rp * 4 + i) * D + x / 4 * (D * 4 / CW) + cg * 4) =
+                make_float4(o[i][x], o[i][x + 1], o[i][x + 2], o[i][x + 3]);
+      __syncthreads();
+      if (ts == 0)
+        for (int y = 0; y < TS - 1; ++y)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int x = 0; x < CW; ++x) o[i][x] += part[(y * R + rp * 4 + i) * D + x / 4 * (D * 4 / CW) + cg * 4 + x % 4];
+    } else {
+      __syncthreads();
+    }
+    const bool whole = wk.head && wk.tail;
+    const long long slot = 2LL * blockIdx.x + (wk.head ? 1 : 0);
+    if (ts == 0)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = rp * 4 + i;
+        if (r >= rows) continue;
+        const float sum = sum_s[r], mul = !whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+        const long long row = (long long)(wk.row0 + i0 + r / G) * a.pl.Hq + wk.h * G + r % G;
+#pragma unroll
+        for (int x = 0; x < CW; x += 4) {
+          const int c = x / 4 * (D * 4 / CW) + cg * 4;
+          float4 v = make_float4(o[i][x] * mul, o[i][x + 1] * mul, o[i][x + 2] * mul, o[i][x + 3] * mul);
+          if (whole) {
+            if (sum == 0.f) v = make_float4(0.f, 0.f, 0.f, 0.f);
+            store4(reinterpret_cast<TQ*>(a.out) + row * D + c, v);
+          } else {
+            *reinterpret_cast<float4*>(a.w.part_o + (slot * a.w.rows + r) * D + c) = v;
+          }
+        }
+        if (cg == 0) {
+          if (!whole) a.w.part_ml[slot * a.w.rows + r] = make_float2(max_s[r], sum);
+          else if (a.lse) a.lse[row] = sum == 0.f ? -INFINITY : (max_s[r] + log2f(sum)) * kLn2;
+        }
+      }
+  }
+}
+
+// Joins the partial results of a cut unit: the share before its first cut holds its head, the shares after hold the rest.
+// A CTA per cut, which finds nothing to do unless it is the first of its unit; a warp per row.
+constexpr int kJoinThreads = 256;
+template <typename TO, int D>
+__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedAttend a) {
+  __shared__ PagedSeqs seqs;
+  pdl_wait();
+  pdl_launch_dependents();
+  const int tid = threadIdx.x, lane = tid & 31, G = a.pl.G;
+  const long long total = paged_fill_seqs(a, seqs, tid, kJoinThreads), share = paged_share(a.w, total);
+  const int cut = blockIdx.x + 1;                                  // the border between shares cut - 1 and cut
+  const long long at = cut * share;
+  PagedWalk wk;
+  if (!wk.seek(a, seqs, at, 1) || wk.off == 0 || wk.off > share) return;   // no border inside a unit, or not the unit's first
+  const int off = wk.off;
+  wk.next(a, seqs);
+  const int tiles = paged_unit_tiles(a.w, a.window, wk.n, wk.L, wk.prefix, wk.u_cur);
+  const int parts = 1 + (int)((tiles - off + share - 1) / share);  // share cut - 1 (its second slot), then cut, cut + 1, ... (their first slots)
+  const int i0 = wk.first_pos(a.w), rows = min(wk.n - i0, wk.n_pos(a.w)) * G;
+  constexpr int V = D / 32;
+  for (int r = blockIdx.y * (kJoinThreads / 32) + (tid >> 5); r < rows; r += gridDim.y * (kJoinThreads / 32)) {
+    float M = -INFINITY;
+    for (int x = lane; x < parts; x += 32) {
+      const float2 ml = a.w.part_ml[(x == 0 ? 2LL * (cut - 1) + 1 : 2LL * (cut + x - 1)) * a.w.rows + r];
+      M = fmaxf(M, ml.x);
+    }
+    M = warp_max(M);
+    float o[V], sum = 0.f;
+#pragma unroll
+    for (int x = 0; x < V; ++x) o[x] = 0.f;
+#pragma unroll 4
+    for (int x = 0; x < parts; ++x) {
+      const long long slot = (x == 0 ? 2LL * (cut - 1) + 1 : 2LL * (cut + x - 1)) * a.w.rows + r;
+      const float2 ml = a.w.part_ml[slot];
+      float v[V];
+      load_vec<V>(a.w.part_o + slot * D + lane * V, v);
+      const float w = ex2(ml.x - M);                               // (only where the part has seen a key: its output is 0 otherwise)
+      if (ml.y != 0.f) {
+        sum = fmaf(ml.y, w, sum);
+#pragma unroll
+        for (int y = 0; y < V; ++y) o[y] = fmaf(v[y], w, o[y]);
+      }
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const long long row = (long long)(wk.row0 + i0 + r / G) * a.pl.Hq + wk.h * G + r % G;
+#pragma unroll
+    for (int y = 0; y < V; ++y) o[y] *= inv;
+    TO* out = reinterpret_cast<TO*>(a.out) + row * D + lane * V;
+    if constexpr (sizeof(TO) == 4) {
+#pragma unroll
+      for (int y = 0; y < V; y += 2) *reinterpret_cast<float2*>(out + y) = make_float2(o[y], o[y + 1]);
+    } else {
+#pragma unroll
+      for (int y = 0; y < V; y += 2) *reinterpret_cast<uint32_t*>(out + y) = pack_bf16(o[y], o[y + 1]);
+    }
+    if (lane == 0 && a.lse) a.lse[row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+  }
+}
+
+template <typename TQ, typename TKV, int R, int D>
+cudaError_t general_launch(const PagedAttend& a, const void* k, const void* v, cudaStream_t s) {
+  auto kern = paged_general_kernel<TQ, TKV, R, D>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, PgShape<R, D>::kBytes);
+  if (e != cudaSuccess) return e;
+  return launch_ex(kern, dim3(a.w.n_cta), dim3(kPgThreads), PgShape<R, D>::kBytes, s, 0, true, a, reinterpret_cast<const TKV*>(k), reinterpret_cast<const TKV*>(v));
+}
+template <typename TQ, typename TKV, int D>
+cudaError_t general_rows(const PagedAttend& a, const void* k, const void* v, cudaStream_t s) {
+  const int r = a.w.ppos * a.pl.G;
+  return r <= 4 ? general_launch<TQ, TKV, 4, D>(a, k, v, s) : r <= 16 ? general_launch<TQ, TKV, 16, D>(a, k, v, s) : general_launch<TQ, TKV, 64, D>(a, k, v, s);
+}
+template <typename TQ, typename TKV>
+cudaError_t general_dim(const PagedAttend& a, const void* k, const void* v, cudaStream_t s) {
+  return a.pl.d == 128 ? general_rows<TQ, TKV, 128>(a, k, v, s) : general_rows<TQ, TKV, 64>(a, k, v, s);
+}
+
+}  // namespace
+
+void paged_plan_general(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int window, int sm_count) {
+  const int most = pb.max_new * pl.G;                              // rows that a sequence has for one KV head, at most
+  const int R = most <= 4 ? 4 : most <= 16 ? 16 : 64;
+  w->ppos = w->upos = R / pl.G;
+  w->TK = R == 64 ? 32 : 64;
+  const long long tiles = (pb.max_len + w->TK - 1) / w->TK, units = (long long)pb.batch * pl.Hkv * paged_units(*w, pb.max_new);
+  constexpr int per_sm = 2;
+  w->by_unit = tiles <= 4;
+  w->min_tiles = w->by_unit ? 1 : 2;
+  const long long most_ctas = w->by_unit ? units : (units * tiles + w->min_tiles - 1) / w->min_tiles;
+  w->n_cta = (int)(most_ctas < (long long)per_sm * sm_count ? most_ctas : (long long)per_sm * sm_count);
+  w->rows = (pb.max_new < w->upos ? pb.max_new : w->upos) * pl.G;
+}
+
+cudaError_t launch_paged_general(const PagedAttend& a, const void* k, const void* v, int q_bf16, int kv_bf16, cudaStream_t s) {
+  if (q_bf16) return kv_bf16 ? general_dim<__nv_bfloat16, __nv_bfloat16>(a, k, v, s) : general_dim<__nv_bfloat16, float>(a, k, v, s);
+  return kv_bf16 ? general_dim<float, __nv_bfloat16>(a, k, v, s) : general_dim<float, float>(a, k, v, s);
+}
+
+cudaError_t launch_paged_join(const PagedAttend& a, int out_bf16, cudaStream_t s) {
+  if (a.w.by_unit || a.w.n_cta < 2) return cudaSuccess;
+  auto kern = a.pl.d == 128 ? (out_bf16 ? paged_join_kernel<__nv_bfloat16, 128> : paged_join_kernel<float, 128>)
+                            : (out_bf16 ? paged_join_kernel<__nv_bfloat16, 64> : paged_join_kernel<float, 64>);
+  const int ys = (a.w.rows + 7) / 8;
+  return launch_ex(kern, dim3(a.w.n_cta - 1, ys < 8 ? ys : 8), dim3(kJoinThreads), 0, s, 0, true, a);
+}
+
+}  // namespace spla

@@ -62,7 +62,7 @@ static TensorMapEncodeFn tensor_map_encoder() {
 }
 
 // A K or V cache as a bf16 matrix [rows][d] with boxes of B rows x 64 columns (128-byte swizzle).
-static bool make_kv_map(void* out128, void* base, int d, int B, unsigned long long rows) {
+bool spla::make_kv_map(void* out128, void* base, int d, int B, unsigned long long rows) {
   TensorMapEncodeFn encode = tensor_map_encoder();
   if (!encode) return false;
   const cuuint64_t dims[2] = {(cuuint64_t)d, (cuuint64_t)rows};

@@ -72,6 +72,8 @@ inline int max_active_clusters(void (*kern)(KArgs...), dim3 grid, dim3 block, si
 
 // spla_api.cu: records the text of a failed CUDA call for spla_last_cuda_error and returns SPLA_ERR_CUDA
 int cuda_fail(cudaError_t e, const char* where);
+// ... a bf16 matrix [rows][d] as a TMA tensor map with boxes of B rows x 64 columns (128-byte swizzle); false if the driver refuses
+bool make_kv_map(void* out128, void* base, int d, int B, unsigned long long rows);
 int device_sm_count();   // multiprocessors of the current device (148 if the query fails)
 // score_select.cu
 int score_chunk_for(long long units, long long max_seq_blocks, int sm_count);
