@@ -125,6 +125,10 @@ extern "C" int spla_paged_create(const spla_paged_config_t* c, void* k_pages, vo
   p->v_pages = v_pages;
   if (p->cfg.sm_scale == 0.f) p->cfg.sm_scale = 1.0f / sqrtf((float)c->head_dim);
   p->sm_count = 0;
+  // the tensor-core kernel: bf16, rows that a TMA coordinate can name
+  const int64_t rows = (c->n_pages - 1) * ps + (c->n_kv_heads - 1) * hs + P;
+  p->tensor = c->kv_dtype == SPLA_BF16 && c->q_dtype == SPLA_BF16 && !(c->flags & SPLA_GENERAL_KERNELS) && rows < (1ll << 31) - 256 &&
+              make_kv_map(p->maps.k, k_pages, c->head_dim, P, rows) && make_kv_map(p->maps.v, v_pages, c->head_dim, P, rows);
   *paged_out = p;
   return SPLA_OK;
 }
@@ -183,8 +187,8 @@ extern "C" int spla_paged_append(spla_paged_t* p, const spla_paged_batch_t* batc
 // The plan of one launch (a batch of at most kPagedMaxBatch sequences) and the bytes of its partial results.
 static size_t plan_attend(const spla_paged* p, const PagedBatch& pb, bool tensor, int window, PagedWork* w) {
   const int sms = p->sm_count ? p->sm_count : device_sm_count();
-  paged_plan_general(w, pb, p->pl, window, sms);
-  (void)tensor;
+  if (tensor) paged_plan_mma(w, pb, p->pl, window, sms);
+  else paged_plan_general(w, pb, p->pl, window, sms);
   if (w->by_unit || w->n_cta < 2) return 0;
   return align_up((size_t)2 * w->n_cta * w->rows * p->pl.d * 4, 256) + align_up((size_t)2 * w->n_cta * w->rows * 8, 256);
 }
@@ -193,6 +197,12 @@ static PagedBatch part_of(PagedBatch b, int first) {
   b.cu += first; b.lens += first; b.table += (long long)first * b.table_stride;
   b.batch = b.batch - first < kPagedMaxBatch ? b.batch - first : kPagedMaxBatch;
   return b;
+}
+
+// The queries as [token][head][half of 64 channels], boxes of G heads x 128 / G tokens: the rows of a row tile, in their order.
+static bool make_q_map(void* out128, const void* q, const PagedLayout& pl, int64_t q_stride, int64_t total) {
+  return make_tile_map_4d(out128, const_cast<void*>(q), 64u, (unsigned)(pl.d / 64), (unsigned)pl.Hq, (unsigned)total, 128ull, (unsigned long long)pl.d * 2,
+                          (unsigned long long)q_stride * 2, (unsigned)pl.G, (unsigned)(128 / pl.G));
 }
 
 extern "C" int spla_paged_query_workspace(const spla_paged_t* p, const spla_paged_batch_t* batch, size_t* bytes_out) {
@@ -204,7 +214,7 @@ extern "C" int spla_paged_query_workspace(const spla_paged_t* p, const spla_page
   for (int first = 0; first < batch->batch; first += kPagedMaxBatch) {
     PagedBatch part = pb;
     part.batch = pb.batch - first < kPagedMaxBatch ? pb.batch - first : kPagedMaxBatch;
-    for (int tensor = 0; tensor < 2; ++tensor) {
+    for (int tensor = 0; tensor <= (p->tensor ? 1 : 0); ++tensor) {   // (queries that TMA does not take go to the general kernel)
       PagedWork w = {};
       const size_t n = plan_attend(p, part, tensor != 0, 0, &w);
       if (n > most) most = n;
@@ -233,7 +243,6 @@ extern "C" int spla_paged_attend(spla_paged_t* p, const spla_paged_batch_t* batc
   size_t need = 0;
   spla_paged_query_workspace(p, batch, &need);
   if (need && (!workspace || workspace_bytes < need)) return SPLA_ERR_INVALID_ARG;
-  if (!p->sm_count) p->sm_count = device_sm_count();
 
   PagedAttend a = {};
   a.pl = p->pl;
@@ -252,13 +261,19 @@ extern "C" int spla_paged_attend(spla_paged_t* p, const spla_paged_batch_t* batc
   const int q16 = p->cfg.q_dtype == SPLA_BF16, kv16 = p->cfg.kv_dtype == SPLA_BF16;
   cudaStream_t s = (cudaStream_t)stream;
   cudaError_t e = cudaSuccess;
+  PagedMaps maps;
+  const bool tensor = p->tensor && aligned(q, 16) && q_stride % 8 == 0 && make_q_map(maps.q, q, p->pl, q_stride, batch->total_new);
+  if (tensor) {
+    memcpy(maps.k, p->maps.k, sizeof(maps.k));
+    memcpy(maps.v, p->maps.v, sizeof(maps.v));
+  }
   for (int first = 0; first < batch->batch && e == cudaSuccess; first += kPagedMaxBatch) {
     a.pb = part_of(pb, first);
     a.prefix = mask->prefix_lens ? mask->prefix_lens + first : nullptr;
-    plan_attend(p, a.pb, false, a.window, &a.w);
+    plan_attend(p, a.pb, tensor, a.window, &a.w);
     a.w.part_o = reinterpret_cast<float*>(workspace);
     a.w.part_ml = reinterpret_cast<float2*>((char*)workspace + align_up((size_t)2 * a.w.n_cta * a.w.rows * p->pl.d * 4, 256));
-    e = launch_paged_general(a, p->k_pages, p->v_pages, q16, kv16, s);
+    e = tensor ? launch_paged_mma(a, maps, s) : launch_paged_general(a, p->k_pages, p->v_pages, q16, kv16, s);
     if (e == cudaSuccess) e = launch_paged_join(a, q16, s);
   }
   return e == cudaSuccess ? SPLA_OK : cuda_fail(e, "spla_paged_attend");

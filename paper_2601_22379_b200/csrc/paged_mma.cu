@@ -1,0 +1,598 @@
+// Attention of new tokens over a paged cache on the 5th-generation tensor cores: bf16 cache and queries.
+//
+//   S = Q K^T,  P = 2^(S scale log2 e - m),  O += P V,  l += sum P    over tiles of 128 keys; lse = ln 2 (m + log2 l), out = O / l
+//
+// One CTA per SM, persistent, on an equal share of all key tiles (paged.h).  Two row tiles of 128 query rows (positions x the G heads
+// of one KV head) are in work at a time, each with its own softmax warps and its own S and O in tensor memory, so that the tensor cores
+// work on one while the other is in its exponentials:
+//   - a unit of more than one row tile: two row tiles against the same key tile, K and V are read once for both;
+//   - a unit of one row tile (single tokens, short chunks): the same rows against key tiles in turn, the two halves merged at the end.
+// P takes the place of S in tensor memory, as the left operand of O += P V, rounded to bf16 (its sum l is of the unrounded values).
+// The maximum is a stale one: O is rescaled only when it grows by more than 2^8.
+//
+// Warps: 0 TMA (pages of K, V, and the query rows as boxes of G heads x positions), 1 the MMA issuer, 4 to 7 and 8 to 11 softmax and
+// epilogue of either row tile, one row per thread.
+//
+// Keys outside a row's mask: their scores are replaced before the maximum, whatever they are.  Values are looked over in tiles that
+// some row sees only in part: behind the sequence's end they are zeroed, and where one that is not finite is inside, the tile's product with V is formed by
+// the softmax warps, visible keys only (0 x infinity is no 0).
+//
+// Every wait is bounded; on expiry the CTA's roles leave their loops, copies and products in flight are waited for, tensor memory is
+// released and the time-out status latched.  No multicast.
+#include "paged.h"
+#include "umma.cuh"
+
+namespace spla {
+
+namespace {
+
+constexpr int kPmThreads = 384;
+constexpr int kPmKeys = 128;                       // keys per tile
+constexpr uint32_t kPmTmemCols = 512;              // S0, S1, O0, O1: 128 columns each
+
+template <int D>
+struct PmSmem {
+  static constexpr int H = D / 64;                               // arrays of 128-byte rows per operand
+  static constexpr int kHalf = kPmKeys * 128;
+  static constexpr int kTile = H * kHalf;                        // one K or V tile, or the queries of a row tile
+  static constexpr int NS = D == 128 ? 2 : 4;                    // stages of K, and of V
+  static constexpr int kQ = 0, kK = kQ + 2 * kTile, kV = kK + NS * kTile, kSeqs = kV + NS * kTile;
+  static constexpr int kMl = kSeqs + (int)((sizeof(PagedSeqs) + 15) / 16 * 16);   // float2 [128]: maximum and sum of the second half
+  static constexpr int kBars = kMl + 128 * 8;
+  static constexpr int kNumBars = 4 * NS + 14;
+  static constexpr int kMisc = kBars + kNumBars * 8;             // tensor-memory base, abort flag, skip flags [2], look-over marks [2][2]
+  static constexpr int kBytes = kMisc + 48;
+  static_assert(kBytes <= 227 * 1024, "shared memory of the paged attention kernel");
+};
+
+// What the roles agree on for one segment: which key tiles either row tile walks.
+struct PmPlan {
+  bool single;                                     // one row tile, key tiles in turn
+  int a[2], e[2], A, E;
+  __device__ __forceinline__ bool act(int s, int t) const { return single ? ((t - A) & 1) == s : (t >= a[s] && t < e[s]); }
+  __device__ __forceinline__ int items(int s) const { return single ? (E - A + 1 - s) >> 1 : e[s] - a[s]; }
+};
+
+// (whole warps)
+__device__ __forceinline__ PmPlan pm_plan(const PagedAttend& a, const PagedWalk& wk, int lane) {
+  PmPlan p;
+  p.single = wk.n <= a.w.ppos;
+  const int i0 = wk.first_pos(a.w), end = min(wk.n, i0 + wk.n_pos(a.w));
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const int ia = i0 + s * a.w.ppos, ib = min(end, ia + a.w.ppos) - 1;
+    p.a[s] = p.e[s] = 0;
+    if (ib < ia || (p.single && s > 0)) continue;
+    int lo = a.window > 0 ? max(0, wk.L - wk.n + ia - a.window + 1) : 0;
+    if (a.first_key) {
+      int least = 0x7fffffff;
+      for (int i = ia + lane; i <= ib; i += 32) {
+        const PagedSees v = paged_sees(a, wk.row0, wk.n, wk.L, wk.prefix, i);
+        if (v.lo < v.hi) least = min(least, v.lo);
+      }
+      lo = __reduce_min_sync(0xffffffffu, least);
+    }
+    const int hi = min(wk.L, max(wk.L - wk.n + ib + 1, wk.prefix));
+    if (lo >= hi) continue;
+    p.a[s] = max(wk.t0, lo / kPmKeys);
+    p.e[s] = max(p.a[s], min(wk.t1, (hi + kPmKeys - 1) / kPmKeys));
+  }
+  const bool h0 = p.e[0] > p.a[0], h1 = p.e[1] > p.a[1];
+  p.A = h0 && h1 ? min(p.a[0], p.a[1]) : h0 ? p.a[0] : p.a[1];
+  p.E = h0 && h1 ? max(p.e[0], p.e[1]) : h0 ? p.e[0] : p.e[1];
+  return p;
+}
+
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void tma_load_q(uint32_t dst, const CUtensorMap* map, int half, int head, int tok, uint64_t* bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+               "l"(map), "r"(0), "r"(half), "r"(head), "r"(tok), "r"(smem_u32(bar))
+               : "memory");
+}
+// bits a .. e - 1 of a word (a, e in any range)
+__device__ __forceinline__ uint32_t bits_between(int a, int e) {
+  const uint32_t below_e = e >= 32 ? 0xffffffffu : e <= 0 ? 0u : (1u << e) - 1u;
+  const uint32_t below_a = a >= 32 ? 0xffffffffu : a <= 0 ? 0u : (1u << a) - 1u;
+  return below_e & ~below_a;
+}
+__device__ __forceinline__ uint32_t pair_not_finite(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+
+template <int D, bool MODS>
+__global__ void __launch_bounds__(kPmThreads, 1)
+    paged_mma_kernel(const PagedAttend a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                     const __grid_constant__ CUtensorMap map_q) {
+  using SM = PmSmem<D>;
+  constexpr int H = SM::H, NS = SM::NS;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + SM::kBars);
+  uint64_t *k_full = bars, *k_empty = k_full + NS, *v_full = k_empty + NS, *v_empty = v_full + NS, *q_full = v_empty + NS, *q_empty = q_full + 1,
+           *s_full = q_empty + 1, *p_ready = s_full + 2, *pv_done = p_ready + 2, *o_free = pv_done + 2, *scanned = o_free + 2, *halves = scanned + 2,
+           *done = halves + 1;
+  uint32_t* tmem_base_s = reinterpret_cast<uint32_t*>(smem + SM::kMisc);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SM::kMisc + 4);
+  volatile int* skip_pv = reinterpret_cast<volatile int*>(smem + SM::kMisc + 8);    // [2]: this product with V has been formed by the softmax warps
+  volatile int* found_bad = reinterpret_cast<volatile int*>(smem + SM::kMisc + 16); // [2][2]: the last look-over (of even, of odd number) that found such a value
+  float2* ml_s = reinterpret_cast<float2*>(smem + SM::kMl);
+  PagedSeqs& seqs = *reinterpret_cast<PagedSeqs*>(smem + SM::kSeqs);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wg = warp >> 2;
+
+  if (tid == 0) {
+    for (int s = 0; s < NS; ++s) {
+      mbar_init(&k_full[s], 1);  mbar_init(&k_empty[s], 1);
+      mbar_init(&v_full[s], 1);  mbar_init(&v_empty[s], 1);
+    }
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 1);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&s_full[s], 1);  mbar_init(&p_ready[s], 4);
+      mbar_init(&pv_done[s], 1);  mbar_init(&o_free[s], 4);
+      mbar_init(&scanned[s], 4);
+      skip_pv[s] = 0;
+      found_bad[2 * s] = found_bad[2 * s + 1] = 0;
+    }
+    mbar_init(halves, 4);
+    mbar_init(done, 1);
+    mbar_init_done();
+    *abort_flag = 0;
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
+  }
+  if (warp == 1) tmem_alloc(tmem_base_s, kPmTmemCols);
+  pdl_wait();
+  pdl_launch_dependents();
+  tc_fence_before();
+  const long long share = paged_share(a.w, paged_fill_seqs(a, seqs, tid, kPmThreads));   // (ends with a barrier)
+  tc_fence_after();
+  const uint32_t tmem = *tmem_base_s;
+  const uint32_t sbase = smem_u32(smem);
+  const int lim = a.wait_limit;
+  const int ppos = a.w.ppos, G = a.pl.G;
+  PagedWalk wk;
+  const bool any = wk.seek(a, seqs, blockIdx.x * share, share);
+
+  if (wg == 0) {
+    warpgroup_reg_dec<56>();
+    if (warp == 0 && any) {
+      // ------------------------------------------------------------ TMA ------------------------------------------------
+      const int P = a.pl.P, npg = kPmKeys / P, boxes = npg * H, pg = lane / H, hh = lane % H;
+      const uint32_t box_dst = hh * SM::kHalf + pg * P * 128;
+      const long long n_rows = (a.pl.n_pages - 1) * a.pl.page_stride + (a.pl.Hkv - 1) * a.pl.head_stride + P;   // (a box there reads zeros)
+      int kt = 0, seg = 0;
+      bool ok = true;
+      while (ok && wk.next(a, seqs)) {
+        const PmPlan pl = pm_plan(a, wk, lane);
+        if (pl.A >= pl.E) continue;
+        if (seg > 0 && !warp_waits(q_empty, (seg - 1) & 1, lim)) { ok = false; break; }
+        ++seg;
+        const int i0 = wk.first_pos(a.w);
+        if (lane == 0) {
+          const bool two = !pl.single && pl.items(1) > 0;
+          const uint32_t rows = (uint32_t)ppos * G * 128;
+          mbar_expect_tx(q_full, (two ? 2 : 1) * H * rows + (uint32_t)a.dbg_tx_extra);
+          for (int s = 0; s < (two ? 2 : 1); ++s)
+            for (int x = 0; x < H; ++x)
+              tma_load_q(sbase + SM::kQ + s * SM::kTile + x * SM::kHalf, &map_q, x, wk.h * G, wk.row0 + i0 + s * ppos, q_full);
+        }
+        for (int t = pl.A; t < pl.E; ++t) {
+          if (!pl.act(0, t) && !pl.act(1, t)) continue;
+          const int index = t * npg + pg, st = kt % NS, ph = ((kt / NS) - 1) & 1;
+          long long row = -1;
+          if (lane < boxes && index * P < wk.L) row = paged_row(a.pb, a.pl, wk.b, wk.h, index);
+          if (row < 0) row = n_rows;
+          if (warp_aborted(abort_flag)) { ok = false; break; }
+          if (kt >= NS && !warp_waits(&k_empty[st], ph, lim)) { ok = false; break; }
+          if (lane == 0) mbar_expect_tx(&k_full[st], SM::kTile + (uint32_t)a.dbg_tx_extra);
+          __syncwarp();
+          if (lane < boxes) tma_load_box(sbase + SM::kK + st * SM::kTile + box_dst, &map_k, hh * 64, (int)row, &k_full[st]);
+          if (kt >= NS && !warp_waits(&v_empty[st], ph, lim)) {    // (the K tile above is still waited for at the end)
+            warp_waits(&k_full[st], (kt / NS) & 1, lim);
+            ok = false;
+            break;
+          }
+          if (lane == 0) mbar_expect_tx(&v_full[st], SM::kTile + (uint32_t)a.dbg_tx_extra);
+          __syncwarp();
+          if (lane < boxes) tma_load_box(sbase + SM::kV + st * SM::kTile + box_dst, &map_v, hh * 64, (int)row, &v_full[st]);
+          ++kt;
+        }
+      }
+      if (!ok) *abort_flag = 1;
+      // every copy has landed before the CTA leaves, whatever the other roles do
+      for (int x = max(0, kt - NS); x < kt; ++x) {
+        warp_waits(&k_full[x % NS], (x / NS) & 1, lim);
+        warp_waits(&v_full[x % NS], (x / NS) & 1, lim);
+      }
+      if (seg > 0) warp_waits(q_full, (seg - 1) & 1, lim);
+    } else if (warp == 1 && any) {
+      // ------------------------------------------------------------ MMA issuer -----------------------------------------
+      constexpr uint32_t id_s = umma_idesc(true, false, false, 128, kPmKeys);
+      constexpr uint32_t id_o = umma_idesc(true, false, true, 128, D);
+      const uint32_t one = elect_one();                           // (the whole warp runs this loop: see umma_ss_one)
+      bool ok = true;
+      int kt = 0, seg = 0;
+      int n_p[2] = {0, 0}, n_o[2] = {0, 0};                       // items whose P was awaited, segments that used O
+      bool pending = false;
+      int p_slot = 0, p_stage = 0, p_phase = 0;
+      bool p_first = false, p_last_v = false;
+      auto product = [&]() {                                      // O (+)= P V of the pending item
+        const int s = p_slot;
+        pending = false;
+        if (!warp_waits(&p_ready[s], n_p[s] & 1, lim) || !warp_waits(&v_full[p_stage], p_phase, lim)) { ok = false; return; }
+        ++n_p[s];
+        if (p_first) {
+          if (n_o[s] > 0 && !warp_waits(&o_free[s], (n_o[s] - 1) & 1, lim)) { ok = false; return; }
+          ++n_o[s];
+        }
+        tc_fence_after();
+        if (!skip_pv[s]) {
+          const uint32_t pt = tmem + s * 128, o = tmem + 256 + s * 128, v = umma_desc_lo(sbase + SM::kV + p_stage * SM::kTile, SM::kHalf);
+          umma_ts4_one<8, 2048 / 16>(one, o, pt, v, id_o, p_first ? 0u : 1u);
+          umma_ts4_one<8, 2048 / 16>(one, o, pt + 32, v + 4 * (2048 / 16), id_o, 1u);
+        }
+        umma_commit_one(one, &pv_done[s]);
+        if (p_last_v) umma_commit_one(one, &v_empty[p_stage]);
+      };
+      while (ok && wk.next(a, seqs)) {
+        const PmPlan pl = pm_plan(a, wk, lane);
+        if (pl.A >= pl.E) continue;
+        if (!warp_waits(q_full, seg & 1, lim)) { ok = false; break; }
+        ++seg;
+        tc_fence_after();
+        bool first[2] = {true, true};
+        for (int t = pl.A; t < pl.E && ok; ++t) {
+          const bool a0 = pl.act(0, t), a1 = pl.act(1, t);
+          if (!a0 && !a1) continue;
+          if (warp_aborted(abort_flag)) { ok = false; break; }
+          const int st = kt % NS, ph = (kt / NS) & 1;
+          if (!warp_waits(&k_full[st], ph, lim)) { ok = false; break; }
+          tc_fence_after();
+#pragma unroll 1
+          for (int s = a0 ? 0 : 1; s < (a1 ? 2 : 1) && ok; ++s) {
+            if (pending && p_slot == s) product();
+            if (!ok) break;
+            const uint32_t q = umma_desc_lo(sbase + SM::kQ + (pl.single ? 0 : s * SM::kTile), 16), k = umma_desc_lo(sbase + SM::kK + st * SM::kTile, 16);
+#pragma unroll
+            for (int x = 0; x < H; ++x) umma_ss4_one<2, 2>(one, tmem + s * 128, q + x * (SM::kHalf / 16), k + x * (SM::kHalf / 16), id_s, x > 0);
+            umma_commit_one(one, &s_full[s]);
+            const bool last = s == 1 || !a1;
+            if (last) umma_commit_one(one, &k_empty[st]);
+            if (pending) product();
+            pending = true;
+            p_slot = s; p_stage = st; p_phase = ph;
+            p_first = first[s]; p_last_v = last;
+            first[s] = false;
+          }
+          ++kt;
+        }
+        if (!ok) break;
+        umma_commit_one(one, q_empty);
+        if (pending) product();
+      }
+      umma_commit_one(one, done);
+      if (!warp_waits(done, 0, lim)) ok = false;
+      if (!ok) *abort_flag = 1;
+    }
+  } else if (any) {
+    // -------------------------------------------------------------- softmax and epilogue: one row per thread -------------
+    warpgroup_reg_inc<224>();
+    const int slot = wg - 1, row = tid - 128 * wg, pi = row / G, g = row % G;
+    const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t tS = tmem + slot * 128 + lane_off, tO = tmem + 256 + slot * 128 + lane_off;
+    const float sc2 = a.sm_scale * kLog2e;
+    bool ok = true;
+    int kt = 0, n = 0, n_scan = 0, n_half = 0, n_used = 0;        // tiles of the CTA, items of this slot, look-overs, merged segments, segments that used O
+    while (ok && wk.next(a, seqs)) {
+      const PmPlan pl = pm_plan(a, wk, lane);
+      const int my = pl.items(slot);
+      const int i0 = wk.first_pos(a.w) + (pl.single ? 0 : slot * ppos), i = i0 + pi;
+      const bool valid = row < ppos * G && i < wk.n;
+      PagedSees see{0x7fffffff, 0};
+      if (valid) see = paged_sees(a, wk.row0, wk.n, wk.L, wk.prefix, i);
+      const bool live = __any_sync(0xffffffffu, valid);
+      const int lo_most = __reduce_max_sync(0xffffffffu, valid ? see.lo : 0), hi_least = __reduce_min_sync(0xffffffffu, valid ? see.hi : 0x7fffffff);
+      // a tile is looked over where any row of the row tile may see it in part: by closed forms, the same for all four warps
+      const int ia = i0, ib = min(wk.n, i0 + ppos) - 1;
+      const int all_lo = a.first_key ? 0x7fffffff : a.window > 0 ? max(0, wk.L - wk.n + ib - a.window + 1) : 0;
+      const int all_hi = min(wk.L, max(wk.L - wk.n + ia + 1, wk.prefix));
+      float slope2 = 0.f;
+      if (MODS && a.slopes && valid) slope2 = __ldg(a.slopes + wk.h * G + g) * kLog2e;
+      const int pos = wk.L - wk.n + i;
+      float m = -INFINITY, l = 0.f;
+      int done_items = 0;
+      for (int t = pl.A; t < pl.E; ++t) {
+        const bool mine = pl.act(slot, t);
+        if (!mine) { kt += pl.act(1 - slot, t); continue; }
+        if (warp_aborted(abort_flag)) { ok = false; break; }
+        const int tok0 = t * kPmKeys;
+        const bool look = tok0 < all_lo || tok0 + kPmKeys > all_hi;
+        bool simt = false;
+        if (look) {
+          // values of this tile: zeroed behind the end where they are not finite; elsewhere such a value makes the tile special
+          const int st = kt % NS;
+          if (!warp_waits(&v_full[st], (kt / NS) & 1, lim)) { ok = false; break; }
+          bool bad = false;
+          unsigned char* vt = smem + SM::kV + st * SM::kTile + row * 16;
+#pragma unroll 4
+          for (int x = 0; x < SM::kTile / 2048; ++x) {             // 16-byte pieces: rows row / 8 + 16 x of either array
+            const uint4 v = *reinterpret_cast<const uint4*>(vt + x * 2048);
+            if (pair_not_finite(v.x) | pair_not_finite(v.y) | pair_not_finite(v.z) | pair_not_finite(v.w)) {
+              if (tok0 + (row >> 3) + 16 * (x & 7) >= wk.L) *reinterpret_cast<uint4*>(vt + x * 2048) = make_uint4(0u, 0u, 0u, 0u);
+              else bad = true;
+            }
+          }
+          proxy_fence();                                          // (zeros written -> tensor core)
+          const int mark = 2 * slot + (n_scan & 1);              // (a warp is at most one look-over ahead of another)
+          if (__any_sync(0xffffffffu, bad) && lane == 0) found_bad[mark] = n_scan + 1;
+          __syncwarp();
+          if (lane == 0) mbar_arrive1(&scanned[slot]);
+          if (!warp_waits(&scanned[slot], n_scan & 1, lim)) { ok = false; break; }
+          simt = __any_sync(0xffffffffu, found_bad[mark] == n_scan + 1);
+          ++n_scan;
+        }
+        if (!warp_waits(&s_full[slot], n & 1, lim)) { ok = false; break; }
+        tc_fence_after();
+        if (live) {
+          float s[kPmKeys];
+          {
+            uint32_t r0[32], r1[32], r2[32], r3[32];
+            tmem_ld32_async(tS, r0);
+            tmem_ld32_async(tS + 32, r1);
+            tmem_ld32_async(tS + 64, r2);
+            tmem_ld32_async(tS + 96, r3);
+            tmem_ld_wait32(r0);
+            tmem_ld_wait32(r1);
+            tmem_ld_wait32(r2);
+            tmem_ld_wait32(r3);
+#pragma unroll
+            for (int x = 0; x < 32; ++x) {
+              s[x] = __uint_as_float(r0[x]); s[32 + x] = __uint_as_float(r1[x]);
+              s[64 + x] = __uint_as_float(r2[x]); s[96 + x] = __uint_as_float(r3[x]);
+            }
+          }
+          if constexpr (MODS) {
+            if (a.softcap > 0.f) {                                // cap tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap)), in base 2
+              const float k1 = 2.f * sc2 / a.softcap, c2 = a.softcap * kLog2e;
+#pragma unroll
+              for (int x = 0; x < kPmKeys; ++x) s[x] = fmaf(-2.f * c2, rcp_approx(1.f + ex2(s[x] * k1)), c2);
+            } else {
+#pragma unroll
+              for (int x = 0; x < kPmKeys; ++x) s[x] *= sc2;
+            }
+            if (a.slopes) {
+              const float d0 = (float)(tok0 - pos);
+#pragma unroll
+              for (int x = 0; x < kPmKeys; ++x) s[x] = fmaf(-slope2, fabsf(d0 + (float)x), s[x]);
+            }
+          }
+          const float mul = MODS ? 1.f : sc2;
+          if (tok0 < lo_most || tok0 + kPmKeys > hi_least) {      // (warp-uniform)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const uint32_t bits = bits_between(see.lo - tok0 - 32 * w, see.hi - tok0 - 32 * w);
+#pragma unroll
+              for (int x = 0; x < 32; ++x)
+                if (!(bits & (1u << x))) s[32 * w + x] = -INFINITY;
+            }
+          }
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int x = 0; x < kPmKeys; x += 4) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) mx[y] = fmaxf(mx[y], s[x + y]);
+          }
+          const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * mul;
+          // The first visible keys of a row set its maximum (its row of O is zero so far); later ones only move it when it would
+          // let a probability exceed 2^8.
+          const bool grow = mt > m + 8.f && m > -INFINITY;
+          if (m == -INFINITY) m = mt;
+          if (__any_sync(0xffffffffu, grow)) {
+            if (!warp_waits(&pv_done[slot], (n - 1) & 1, lim)) { ok = false; break; }   // every product with P so far
+            tc_fence_after();
+            const float m_new = grow ? mt : m, f = grow ? ex2(m - m_new) : 1.f;
+            m = m_new;
+            l *= f;
+#pragma unroll 1
+            for (int c = 0; c < D; c += 16) {
+              uint32_t o[16];
+              tmem_ld16_async(tO + c, o);
+              tmem_ld_wait16(o);
+#pragma unroll
+              for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+              tmem_st16(tO + c, o);
+            }
+          }
+          const float nm = m == -INFINITY ? 0.f : -m;
+          float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+              const float2 v = __ffma2_rn(make_float2(s[32 * c + 2 * x], s[32 * c + 2 * x + 1]), make_float2(mul, mul), make_float2(nm, nm));
+              const float2 p = make_float2(ex2(v.x), ex2(v.y));
+              if (x & 1) sum1 = __fadd2_rn(sum1, p); else sum0 = __fadd2_rn(sum0, p);
+              pk[x] = pack_bf16(p.x, p.y);
+            }
+            tmem_st16(tS + 16 * c, pk);
+          }
+          l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
+          tmem_st_wait();
+        }
+        if (simt) {
+          // the product with V here: O += sum over the row's visible keys of p v
+          if (done_items > 0 && !warp_waits(&pv_done[slot], (n - 1) & 1, lim)) { ok = false; break; }
+          if (done_items == 0 && n_used > 0 && !warp_waits(&o_free[slot], (n_used - 1) & 1, lim)) { ok = false; break; }
+          tc_fence_after();
+          const unsigned char* vt = smem + SM::kV + (kt % NS) * SM::kTile;
+#pragma unroll 1
+          for (int c = 0; c < D; c += 16) {
+            float acc[16];
+#pragma unroll
+            for (int x = 0; x < 16; ++x) acc[x] = 0.f;
+#pragma unroll 1
+            for (int w = 0; w < 4; ++w) {
+              uint32_t pw[16];
+              tmem_ld16_async(tS + 16 * w, pw);
+              tmem_ld_wait16(pw);
+              const uint32_t bits = valid ? bits_between(see.lo - tok0 - 32 * w, see.hi - tok0 - 32 * w) : 0u;
+#pragma unroll
+              for (int y = 0; y < 32; ++y) {
+                if (!(bits & (1u << y))) continue;
+                const float p = (y & 1) ? bf16_hi(pw[y >> 1]) : bf16_lo(pw[y >> 1]);
+                const int j = 32 * w + y;
+                const unsigned char* vr = vt + (c >> 6) * SM::kHalf + j * 128;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                  const uint4 v = *reinterpret_cast<const uint4*>(vr + (((((c & 63) >> 3) + x) ^ (j & 7)) << 4));
+                  const uint32_t q[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                  for (int z = 0; z < 4; ++z) {
+                    acc[8 * x + 2 * z] = fmaf(p, bf16_lo(q[z]), acc[8 * x + 2 * z]);
+                    acc[8 * x + 2 * z + 1] = fmaf(p, bf16_hi(q[z]), acc[8 * x + 2 * z + 1]);
+                  }
+                }
+              }
+              __syncwarp();
+            }
+            uint32_t o[16];
+            if (done_items > 0) {
+              tmem_ld16_async(tO + c, o);
+              tmem_ld_wait16(o);
+            }
+#pragma unroll
+            for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(done_items > 0 ? __uint_as_float(o[x]) + acc[x] : acc[x]);
+            tmem_st16(tO + c, o);
+          }
+          tmem_st_wait();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0 && (warp & 3) == 0) skip_pv[slot] = simt;
+        if (lane == 0) mbar_arrive1(&p_ready[slot]);
+        ++n;
+        ++kt;
+        ++done_items;
+      }
+      if (!ok) break;
+      // ------------------------------------------------------------ end of the segment ----------------------------------
+      const bool whole = wk.head && wk.tail;
+      if (my > 0) {
+        if (!warp_waits(&pv_done[slot], (n - 1) & 1, lim)) { ok = false; break; }
+        tc_fence_after();
+        ++n_used;
+      }
+      float m1 = -INFINITY, l1 = 0.f;
+      const bool second = pl.single && pl.items(1) > 0;
+      if (second) {
+        if (slot == 1) {                                          // the second half's maxima and sums go to the first's warps, O stays where it is
+          ml_s[row] = make_float2(m, l);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive1(halves);
+        } else {
+          if (!warp_waits(halves, n_half & 1, lim)) { ok = false; break; }
+          tc_fence_after();
+          const float2 o = ml_s[row];
+          m1 = o.x;
+          l1 = o.y;
+        }
+        ++n_half;
+      }
+      if (pl.single && slot == 1) continue;
+      // O of both halves relative to the larger maximum; an empty half (no key seen) takes no part
+      const float M = fmaxf(m, m1);
+      const float f0 = l == 0.f ? 0.f : ex2(m - M), f1 = l1 == 0.f ? 0.f : ex2(m1 - M);
+      const float sum = (l == 0.f ? 0.f : l * f0) + (l1 == 0.f ? 0.f : l1 * f1);
+      const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
+      const float w0 = f0 * inv, w1 = f1 * inv;
+      const long long out_row = (long long)(wk.row0 + i) * a.pl.Hq + wk.h * G + g;
+      const long long part_row = (2LL * blockIdx.x + (wk.head ? 1 : 0)) * a.w.rows + (pl.single ? 0 : slot * ppos * G) + row;
+      if (live) {
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          float o[32];
+          if (my > 0) {
+            tmem_ld32(tO + c, o);
+#pragma unroll
+            for (int x = 0; x < 32; ++x) o[x] = f0 == 0.f && l == 0.f ? 0.f : o[x] * w0;
+          } else {
+#pragma unroll
+            for (int x = 0; x < 32; ++x) o[x] = 0.f;
+          }
+          if (second) {
+            float o1[32];
+            tmem_ld32(tO + 128 + c, o1);
+            if (l1 != 0.f)
+#pragma unroll
+              for (int x = 0; x < 32; ++x) o[x] = fmaf(o1[x], w1, o[x]);
+          }
+          if (valid && whole) {
+            uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + out_row * D + c);
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              dst[x] = make_uint4(pack_bf16(o[8 * x], o[8 * x + 1]), pack_bf16(o[8 * x + 2], o[8 * x + 3]), pack_bf16(o[8 * x + 4], o[8 * x + 5]),
+                                  pack_bf16(o[8 * x + 6], o[8 * x + 7]));
+          } else if (valid) {
+            float4* dst = reinterpret_cast<float4*>(a.w.part_o + part_row * D + c);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) dst[x] = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+          }
+        }
+        if (valid && !whole) a.w.part_ml[part_row] = make_float2(M, sum);
+        if (valid && whole && a.lse) a.lse[out_row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (my > 0) mbar_arrive1(&o_free[slot]);
+        if (second) mbar_arrive1(&o_free[1]);
+      }
+    }
+    if (!ok) *abort_flag = 1;
+  } else {
+    warpgroup_reg_inc<224>();
+  }
+
+  // ---------------------------------------------------------------- end: tensor memory back -----------------------------
+  __syncwarp();
+  __syncthreads();
+  if (*abort_flag && tid == 0) atomicExch(a.pl.status, kStatusTimeout);
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_free(tmem, kPmTmemCols);
+  }
+}
+
+template <int D>
+cudaError_t mma_d(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
+  auto kern = a.softcap > 0.f || a.slopes ? paged_mma_kernel<D, true> : paged_mma_kernel<D, false>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, PmSmem<D>::kBytes);
+  if (e != cudaSuccess) return e;
+  return launch_ex(kern, dim3(a.w.n_cta), dim3(kPmThreads), PmSmem<D>::kBytes, s, 0, true, a, *reinterpret_cast<const CUtensorMap*>(maps.k),
+                   *reinterpret_cast<const CUtensorMap*>(maps.v), *reinterpret_cast<const CUtensorMap*>(maps.q));
+}
+
+}  // namespace
+
+void paged_plan_mma(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int window, int sm_count) {
+  w->ppos = 128 / pl.G;
+  w->upos = 2 * w->ppos;
+  w->TK = kPmKeys;
+  const long long tiles = (pb.max_len + w->TK - 1) / w->TK, units = (long long)pb.batch * pl.Hkv * paged_units(*w, pb.max_new);
+  w->by_unit = tiles <= 4;
+  w->min_tiles = w->by_unit ? 1 : 2;
+  const long long most = w->by_unit ? units : (units * tiles + w->min_tiles - 1) / w->min_tiles;
+  w->n_cta = (int)(most < sm_count ? most : sm_count);
+  w->rows = (pb.max_new < w->upos ? pb.max_new : w->upos) * pl.G;
+}
+
+cudaError_t launch_paged_mma(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
+  return a.pl.d == 128 ? mma_d<128>(a, maps, s) : mma_d<64>(a, maps, s);
+}
+
+}  // namespace spla

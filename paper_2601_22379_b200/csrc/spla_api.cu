@@ -74,6 +74,20 @@ bool spla::make_kv_map(void* out128, void* base, int d, int B, unsigned long lon
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// [n3][n2][n1][n0] bf16 elements with the given byte strides, boxes of [b3][b2][1][n0] (n0 x 2 = 128 bytes, 128-byte swizzle).
+bool spla::make_tile_map_4d(void* out128, void* base, unsigned n0, unsigned n1, unsigned n2, unsigned n3, unsigned long long s1, unsigned long long s2,
+                            unsigned long long s3, unsigned b2, unsigned b3) {
+  TensorMapEncodeFn encode = tensor_map_encoder();
+  if (!encode) return false;
+  const cuuint64_t dims[4] = {n0, n1, n2, n3};
+  const cuuint64_t strides[3] = {s1, s2, s3};
+  const cuuint32_t box[4] = {n0, 1u, b2, b3};
+  const cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
+  return encode(reinterpret_cast<CUtensorMap*>(out128), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides, box, estr,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // The same cache seen as [d / 64 column halves][rows][64 columns], so that ONE copy brings a whole tile of `tile_rows`
 // rows: its box is all halves x tile_rows x 64, which lands in shared memory half by half, each half [rows][128 bytes]
 // with the 128-byte swizzle - the layout the attend phase reads.  (An issue costs the issuing thread about 0.1 us.)

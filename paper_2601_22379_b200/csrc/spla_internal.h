@@ -74,6 +74,8 @@ inline int max_active_clusters(void (*kern)(KArgs...), dim3 grid, dim3 block, si
 int cuda_fail(cudaError_t e, const char* where);
 // ... a bf16 matrix [rows][d] as a TMA tensor map with boxes of B rows x 64 columns (128-byte swizzle); false if the driver refuses
 bool make_kv_map(void* out128, void* base, int d, int B, unsigned long long rows);
+bool make_tile_map_4d(void* out128, void* base, unsigned n0, unsigned n1, unsigned n2, unsigned n3, unsigned long long s1, unsigned long long s2,
+                      unsigned long long s3, unsigned b2, unsigned b3);
 int device_sm_count();   // multiprocessors of the current device (148 if the query fails)
 // score_select.cu
 int score_chunk_for(long long units, long long max_seq_blocks, int sm_count);
