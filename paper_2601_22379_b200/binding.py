@@ -374,26 +374,16 @@ class SplaCache:
 _TYPE_CODE = {torch.bfloat16: SPLA_BF16, torch.float32: SPLA_F32}
 
 
-class _On:
-    """Makes `device` the current one for a call; costs nothing where it is."""
-
-    def __init__(self, device: torch.device):
-        self.index = device.index if device.index is not None else 0
-
-    def __enter__(self):
-        self.before = torch.cuda.current_device()
-        if self.before != self.index:
-            torch.cuda.set_device(self.index)
-        return torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.before != self.index:
-            torch.cuda.set_device(self.before)
-
-
-def _need(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
+def _on(index: int, fn, *args) -> int:
+    """fn(*args, stream) with device `index` the current one and its current stream as the last argument."""
+    before = torch._C._cuda_getDevice()
+    if before == index:
+        return fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    torch.cuda.set_device(index)
+    try:
+        return fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    finally:
+        torch.cuda.set_device(before)
 
 
 class Rope:
@@ -406,7 +396,8 @@ class Rope:
 
     def __init__(self, head_dim: int, rot_dim: int = 0, base: float = 10000.0, interleaved: bool = False, scaling: str = "none",
                  factor: float = 1.0, original_len: float = 0.0, ramp=(1.0, 32.0), amplitude: float = 1.0):
-        _need(scaling in self.SCALING, f"scaling must be one of {sorted(self.SCALING)}")
+        if scaling not in self.SCALING:
+            raise ValueError(f"rope: scaling must be one of {sorted(self.SCALING)}")
         self.lib = load()
         self.head_dim = head_dim
         cfg = SplaRopeConfig(head_dim, rot_dim, int(interleaved), self.SCALING[scaling], base, factor, original_len, ramp[0], ramp[1], amplitude)
@@ -414,37 +405,40 @@ class Rope:
         _check(self.lib.spla_rope_create(C.byref(cfg), C.byref(self.handle)), "spla_rope_create")
 
     def _tensor(self, x: torch.Tensor, out: torch.Tensor | None, positions: torch.Tensor):
-        d = self.head_dim
-        _need(x.is_cuda and x.dtype in _TYPE_CODE and x.shape[-1] == d and x.stride(-1) == 1 and x.shape[:-2] == positions.shape
-              and x.device == positions.device,
-              "rope: tensors [batch, tokens, heads, head_dim] or [tokens, heads, head_dim] of the positions' batch and device, channels contiguous")
+        shape, xs = x.shape, x.stride()
+        if not (shape[:-2] == positions.shape and shape[-1] == self.head_dim and xs[-1] == 1 and x.dtype in _TYPE_CODE and x.is_cuda
+                and x.device == positions.device):
+            raise ValueError("rope: tensors [batch, tokens, heads, head_dim] or [tokens, heads, head_dim] of the positions' batch and device, "
+                             "bf16 or fp32, channels contiguous")
         if out is None:
-            out = torch.empty_like(x)
+            out = torch.empty_like(x)                                        # (the strides of x where they are dense)
             if out.stride(-1) != 1:
-                out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        else:
-            _need(out.shape == x.shape and out.dtype == x.dtype and out.device == x.device and out.stride(-1) == 1, "rope: an output like its input")
-        xs, os_ = x.stride(), out.stride()
-        if x.dim() == 3:
-            xs, os_ = (0, *xs), (0, *os_)
-        return out, SplaRopeTensor(x.data_ptr(), out.data_ptr(), x.shape[-2], xs[0], xs[1], xs[2], os_[0], os_[1], os_[2])
+                out = x.new_empty(shape)
+        elif not (out.shape == shape and out.dtype == x.dtype and out.device == x.device and out.stride(-1) == 1):
+            raise ValueError("rope: an output like its input, channels contiguous")
+        ys = out.stride()
+        if len(xs) == 3:
+            return out, SplaRopeTensor(x.data_ptr(), out.data_ptr(), shape[1], 0, xs[0], xs[1], 0, ys[0], ys[1])
+        return out, SplaRopeTensor(x.data_ptr(), out.data_ptr(), shape[2], xs[0], xs[1], xs[2], ys[0], ys[1], ys[2])
 
     def apply(self, positions: torch.Tensor, q: torch.Tensor, k: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
               k_out: torch.Tensor | None = None, transpose: bool = False):
         """Rotates q (and k) to `positions` (int32 [batch, tokens] or [tokens]); any strides, channels contiguous.  `q_out=q`
         works in place.  `transpose`: the gradient of the rotation.  Returns q_out, or (q_out, k_out)."""
-        _need(positions.dtype == torch.int32 and positions.is_contiguous() and positions.dim() in (1, 2), "rope: positions int32 [batch, tokens] or [tokens], contiguous")
+        shape = positions.shape
+        if not (positions.dtype == torch.int32 and positions.is_contiguous() and 1 <= len(shape) <= 2):
+            raise ValueError("rope: positions int32 [batch, tokens] or [tokens], contiguous")
         q_out, tq = self._tensor(q, q_out, positions)
         tk = None
         if k is not None:
-            _need(k.dtype == q.dtype, "rope: q and k of one type")
+            if k.dtype != q.dtype:
+                raise ValueError("rope: q and k of one type")
             k_out, tk = self._tensor(k, k_out, positions)
         if positions.numel():
-            batch = positions.shape[0] if positions.dim() == 2 else 1
-            with _On(q.device) as stream:
-                _check(self.lib.spla_rope_apply(self.handle, positions.data_ptr(), batch, positions.shape[-1], C.addressof(tq),
-                                                C.addressof(tk) if tk is not None else None, _TYPE_CODE[q.dtype], int(transpose), stream),
-                       "spla_rope_apply")
+            rc = _on(positions.get_device(), self.lib.spla_rope_apply, self.handle, positions.data_ptr(), shape[0] if len(shape) == 2 else 1, shape[-1],
+                     C.addressof(tq), None if tk is None else C.addressof(tk), _TYPE_CODE[q.dtype], int(transpose))
+            if rc != SPLA_OK:
+                raise SplaError(rc, "spla_rope_apply")
         return q_out if k is None else (q_out, k_out)
 
     def close(self):
@@ -466,9 +460,9 @@ class PagedCache:
     how many tokens a sequence has with them, page_table int32 [batch, columns] where they lie."""
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, n_q_heads: int, q_dtype: str | None = None, sm_scale: float = 0.0, flags: int = 0):
-        _need(k_pages.is_cuda and k_pages.dim() == 4 and k_pages.is_contiguous() and v_pages.is_contiguous() and k_pages.dtype in _TYPE_CODE
-              and v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype and v_pages.device == k_pages.device,
-              "paged cache: contiguous k_pages, v_pages [n_pages, H_kv, P, d] of one type and device")
+        if not (k_pages.is_cuda and k_pages.dim() == 4 and k_pages.is_contiguous() and v_pages.is_contiguous() and k_pages.dtype in _TYPE_CODE
+                and v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype and v_pages.device == k_pages.device):
+            raise ValueError("paged cache: contiguous k_pages, v_pages [n_pages, H_kv, P, d] of one type and device")
         n_pages, hkv, P, d = k_pages.shape
         self._create(k_pages, v_pages, n_pages, hkv, P, d, 0, 0, n_q_heads, q_dtype, sm_scale, flags)
 
@@ -495,53 +489,55 @@ class PagedCache:
         self.q_torch_dtype = {"bf16": torch.bfloat16, "f32": torch.float32, None: k.dtype}[q_dtype]
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         cfg = SplaPagedConfig(n_q_heads, hkv, d, P, n_pages, _TYPE_CODE[k.dtype], _TYPE_CODE[self.q_torch_dtype], page_stride, head_stride, sm_scale, flags)
+        self.index = k.get_device()
         self.handle = C.c_void_p()
-        with _On(self.device):
-            _check(self.lib.spla_paged_create(C.byref(cfg), k.data_ptr(), v.data_ptr(), self.status.data_ptr(), C.byref(self.handle)),
-                   "spla_paged_create")
+        _check(_on(self.index, lambda *a: self.lib.spla_paged_create(*a[:-1]), C.byref(cfg), k.data_ptr(), v.data_ptr(), self.status.data_ptr(),
+                   C.byref(self.handle)), "spla_paged_create")
 
     def _batch(self, total, cu_new, seq_lens, page_table, max_new, max_len):
-        _need(cu_new.dtype == seq_lens.dtype == page_table.dtype == torch.int32 and cu_new.is_contiguous() and seq_lens.is_contiguous()
-              and page_table.dim() == 2 and page_table.stride(1) == 1
-              and cu_new.device == seq_lens.device == page_table.device == self.device
-              and cu_new.numel() == seq_lens.numel() + 1 and page_table.shape[0] == seq_lens.numel(),
-              "paged cache: int32 cu_new [batch + 1], seq_lens [batch], page_table [batch, columns] on the cache's device")
-        # (the table's columns as the stride: max_len may not reach past them)
-        _need(max_len <= page_table.shape[1] * self.page_size, "paged cache: max_len is more than the page table's columns hold")
-        return SplaPagedBatch(cu_new.data_ptr(), seq_lens.data_ptr(), page_table.data_ptr(), seq_lens.numel(), total, max_new, max_len,
-                              page_table.stride(0) if seq_lens.numel() > 1 else page_table.shape[1])
+        shape, n, dev = page_table.shape, seq_lens.shape[0], self.device
+        if not (cu_new.dtype == seq_lens.dtype == page_table.dtype == torch.int32 and cu_new.device == seq_lens.device == page_table.device == dev
+                and cu_new.is_contiguous() and seq_lens.is_contiguous() and len(shape) == 2 and page_table.stride(1) == 1
+                and cu_new.shape[0] == n + 1 and shape[0] == n):
+            raise ValueError("paged cache: int32 cu_new [batch + 1], seq_lens [batch], page_table [batch, columns] on the cache's device")
+        # (the table's columns bound max_len; its rows may be further apart)
+        if max_len > shape[1] * self.page_size:
+            raise ValueError("paged cache: max_len is more than the page table's columns hold")
+        return SplaPagedBatch(cu_new.data_ptr(), seq_lens.data_ptr(), page_table.data_ptr(), n, total, max_new, max_len, page_table.stride(0) if n > 1 else shape[1])
 
-    def _rows(self, x, heads, dtype, what):
-        _need(x.is_cuda and x.device == self.device and x.dtype == dtype and x.dim() == 3 and x.shape[1:] == (heads, self.head_dim)
-              and x.stride(2) == 1 and x.stride(1) == self.head_dim, f"paged cache: {what} [tokens, {heads}, {self.head_dim}] of its type, heads contiguous")
-        return x.stride(0) if x.shape[0] > 1 else heads * self.head_dim
+    def _rows(self, x, total, heads, dtype, what):
+        """Elements between the tokens of x [total, heads, d]."""
+        d, xs = self.head_dim, x.stride()
+        if not (x.shape == (total, heads, d) and x.dtype == dtype and x.device == self.device and xs[2] == 1 and xs[1] == d):
+            raise ValueError(f"paged cache: {what} [tokens, {heads}, {d}] of its type, heads contiguous")
+        return xs[0] if total > 1 else heads * d
 
     def append(self, k: torch.Tensor, v: torch.Tensor, cu_new: torch.Tensor, seq_lens: torch.Tensor, page_table: torch.Tensor,
                q: torch.Tensor | None = None, rope: Rope | None = None, positions: torch.Tensor | None = None, q_out: torch.Tensor | None = None):
         """Stores k, v [total, H_kv, d] at the last n_b positions of every sequence, keys rotated by `rope`; rotates q [total, H_q, d]
         beside them and returns it (None without q).  Tokens may be any stride apart; `q_out=q` works in place."""
-        total = k.shape[0]
-        ks = self._rows(k, self.n_kv_heads, self.k_pages.dtype, "k")
-        vs = self._rows(v, self.n_kv_heads, self.k_pages.dtype, "v")
-        _need(v.shape[0] == total, "paged cache: k and v of as many tokens")
+        total, hkv, kt = k.shape[0], self.n_kv_heads, self.k_pages.dtype
+        ks = self._rows(k, total, hkv, kt, "k")
+        vs = self._rows(v, total, hkv, kt, "v")
         qs = os_ = 0
+        qp = op = None
         if q is not None:
-            qs = self._rows(q, self.n_q_heads, self.q_torch_dtype, "q")
+            qs = self._rows(q, total, self.n_q_heads, self.q_torch_dtype, "q")
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            os_ = self._rows(q_out, self.n_q_heads, self.q_torch_dtype, "q_out")
-            _need(q.shape[0] == total and q_out.shape[0] == total, "paged cache: q of as many tokens as k")
-        if positions is not None:
-            _need(positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == total and positions.device == self.device, "paged cache: positions int32 [total]")
-        if total == 0:
-            return q_out
-        # the store needs no bounds of its own: a sequence may be as long as the table has columns
-        most = min(page_table.shape[1] * self.page_size, 1 << 24)
-        b = self._batch(total, cu_new, seq_lens, page_table, min(total, most), most)
-        with _On(self.device) as stream:
-            _check(self.lib.spla_paged_append(self.handle, C.addressof(b), rope.handle if rope is not None else None, _ptr(positions),
-                                              k.data_ptr(), ks, v.data_ptr(), vs, _ptr(q), qs, _ptr(q_out) if q is not None else None, os_, stream),
-                   "spla_paged_append")
+                q_out = q.new_empty(q.shape)
+            os_ = self._rows(q_out, total, self.n_q_heads, self.q_torch_dtype, "q_out")
+            qp, op = q.data_ptr(), q_out.data_ptr()
+        if positions is not None and not (positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == total
+                                          and positions.device == self.device):
+            raise ValueError("paged cache: positions int32 [total]")
+        if total:
+            # the store needs no bounds of its own: a sequence may be as long as the table has columns
+            most = min(page_table.shape[1] * self.page_size, 1 << 24)
+            b = self._batch(total, cu_new, seq_lens, page_table, min(total, most), most)
+            rc = _on(self.index, self.lib.spla_paged_append, self.handle, C.addressof(b), None if rope is None else rope.handle, _ptr(positions),
+                     k.data_ptr(), ks, v.data_ptr(), vs, qp, qs, op, os_)
+            if rc != SPLA_OK:
+                raise SplaError(rc, "spla_paged_append")
         return q_out
 
     def attend(self, q: torch.Tensor, cu_new: torch.Tensor, seq_lens: torch.Tensor, page_table: torch.Tensor, max_new: int, max_len: int,
@@ -550,36 +546,36 @@ class PagedCache:
         """Attention of the new tokens' queries q [total, H_q, d] over the cache, which holds their keys already; max_new and max_len
         bound the new tokens and the length of any sequence.  Returns out [total, H_q, d] and lse fp32 [total, H_q].  See
         spla_paged_mask_t for the mask."""
-        total = q.shape[0]
-        qs = self._rows(q, self.n_q_heads, self.q_torch_dtype, "q")
-        dev = self.device
+        total, hq, dev = q.shape[0], self.n_q_heads, self.device
+        qs = self._rows(q, total, hq, self.q_torch_dtype, "q")
         if out is None:
-            out = torch.empty(total, self.n_q_heads, self.head_dim, dtype=q.dtype, device=dev)
-        else:
-            _need(out.shape == q.shape and out.dtype == q.dtype and out.device == dev and out.is_contiguous(), "paged cache: a contiguous out like q")
+            out = q.new_empty(q.shape)
+        elif not (out.shape == q.shape and out.dtype == q.dtype and out.device == dev and out.is_contiguous()):
+            raise ValueError("paged cache: a contiguous out like q")
         if lse is None:
-            lse = torch.empty(total, self.n_q_heads, dtype=torch.float32, device=dev)
-        else:
-            _need(tuple(lse.shape) == (total, self.n_q_heads) and lse.dtype == torch.float32 and lse.device == dev and lse.is_contiguous(), "paged cache: lse fp32 [total, H_q]")
-        for x, n, t, what in ((slopes, self.n_q_heads, torch.float32, "slopes fp32 [H_q]"), (first_key, total, torch.int32, "first_key int32 [total]"),
-                              (prefix_lens, seq_lens.numel(), torch.int32, "prefix_lens int32 [batch]")):
-            _need(x is None or (x.dtype == t and x.numel() == n and x.is_contiguous() and x.device == dev), f"paged cache: {what}")
-        if total == 0:
-            return out, lse
-        b = self._batch(total, cu_new, seq_lens, page_table, max_new, max_len)
-        mask = SplaPagedMask(softcap, window, _ptr(slopes), _ptr(first_key), _ptr(prefix_lens))
-        with _On(dev) as stream:
+            lse = torch.empty((total, hq), dtype=torch.float32, device=dev)
+        elif not (lse.shape == (total, hq) and lse.dtype == torch.float32 and lse.device == dev and lse.is_contiguous()):
+            raise ValueError("paged cache: lse fp32 [total, H_q]")
+        for x, n, t, what in ((slopes, hq, torch.float32, "slopes fp32 [H_q]"), (first_key, total, torch.int32, "first_key int32 [total]"),
+                              (prefix_lens, seq_lens.shape[0], torch.int32, "prefix_lens int32 [batch]")):
+            if x is not None and not (x.dtype == t and x.numel() == n and x.is_contiguous() and x.device == dev):
+                raise ValueError(f"paged cache: {what}")
+        if total:
+            b = self._batch(total, cu_new, seq_lens, page_table, max_new, max_len)
+            mask = SplaPagedMask(softcap, window, _ptr(slopes), _ptr(first_key), _ptr(prefix_lens))
             nbytes = C.c_size_t()
-            _check(self.lib.spla_paged_query_workspace(self.handle, C.addressof(b), C.byref(nbytes)), "spla_paged_query_workspace")
+            # (what the call refuses it refuses below too, with its name)
+            self.lib.spla_paged_query_workspace(self.handle, C.addressof(b), C.byref(nbytes))
             # a scratch of the call's own, from the stream's pool: calls on other streams and captured graphs share nothing
             ws = torch.empty(nbytes.value, dtype=torch.uint8, device=dev) if nbytes.value else None
-            _check(self.lib.spla_paged_attend(self.handle, C.addressof(b), q.data_ptr(), qs, C.addressof(mask), out.data_ptr(), lse.data_ptr(),
-                                              _ptr(ws), nbytes.value, stream), "spla_paged_attend")
+            rc = _on(self.index, self.lib.spla_paged_attend, self.handle, C.addressof(b), q.data_ptr(), qs, C.addressof(mask), out.data_ptr(),
+                     lse.data_ptr(), _ptr(ws), nbytes.value)
+            if rc != SPLA_OK:
+                raise SplaError(rc, "spla_paged_attend")
         return out, lse
 
     def sync_status(self) -> int:
-        with _On(self.device) as stream:
-            return self.lib.spla_paged_sync_status(self.handle, stream)
+        return _on(self.index, self.lib.spla_paged_sync_status, self.handle)
 
     def close(self):
         if getattr(self, "handle", None) is not None and self.handle.value:
