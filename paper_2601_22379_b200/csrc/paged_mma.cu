@@ -10,7 +10,7 @@
 // P takes the place of S in tensor memory, as the left operand of O += P V, rounded to bf16 (its sum l is of the unrounded values).
 // The maximum is a stale one: O is rescaled only when it grows by more than 2^8.
 //
-// Warps: 0 TMA (pages of K, V, and the query rows as boxes of G heads x positions), 1 the MMA issuer, 4 to 7 and 8 to 11 softmax and
+// Warps: 0 and 2 TMA (pages of K and the query rows as boxes of G heads x positions; pages of V), 1 the MMA issuer, 4 to 7 and 8 to 11 softmax and
 // epilogue of either row tile, one row per thread.
 //
 // Keys outside a row's mask: their scores are replaced before the maximum, whatever they are.  Values are looked over in tiles that
@@ -19,6 +19,8 @@
 //
 // Every wait is bounded; on expiry the CTA's roles leave their loops, copies and products in flight are waited for, tensor memory is
 // released and the time-out status latched.  No multicast.
+#include <type_traits>
+
 #include "paged.h"
 #include "umma.cuh"
 
@@ -45,42 +47,67 @@ struct PmSmem {
   static_assert(kBytes <= 227 * 1024, "shared memory of the paged attention kernel");
 };
 
-// What the roles agree on for one segment: which key tiles either row tile walks.
+// What the roles agree on for one segment: which key tiles either row tile walks, and which of them every row sees whole.
 struct PmPlan {
   bool single;                                     // one row tile, key tiles in turn
-  int a[2], e[2], A, E;
-  __device__ __forceinline__ bool act(int s, int t) const { return single ? ((t - A) & 1) == s : (t >= a[s] && t < e[s]); }
-  __device__ __forceinline__ int items(int s) const { return single ? (E - A + 1 - s) >> 1 : e[s] - a[s]; }
+  int a0, e0, a1, e1;                              // key tiles of row tile 0, of row tile 1
+  int A, E;                                        // of either
+  int la0, le0, la1, le1;                          // seen whole by all rows (the values of the others are looked over)
+  template <int S>
+  __device__ __forceinline__ bool act(int t) const { return single ? ((t - A) & 1) == S : S == 0 ? t >= a0 && t < e0 : t >= a1 && t < e1; }
+  template <int S>
+  __device__ __forceinline__ bool look(int t) const { return single || S == 0 ? t < la0 || t >= le0 : t < la1 || t >= le1; }
+  __device__ __forceinline__ int items(int s) const { return single ? (E - A + 1 - s) >> 1 : s == 0 ? e0 - a0 : e1 - a1; }
 };
 
 // (whole warps)
+__device__ __forceinline__ void pm_row_tile(const PagedAttend& a, const PagedWalk& wk, int lane, int ia, int ib, int& ta, int& te, int& la, int& le) {
+  ta = te = la = le = 0;
+  if (ib < ia) return;
+  const int first = wk.L - wk.n;
+  int lo = a.window > 0 ? max(0, first + ia - a.window + 1) : 0;
+  int all_lo = a.window > 0 ? max(0, first + ib - a.window + 1) : 0;
+  const int hi = min(wk.L, max(first + ib + 1, wk.prefix)), all_hi = min(wk.L, max(first + ia + 1, wk.prefix));
+  if (a.first_key) {
+    int least = 0x7fffffff, most = 0;
+    for (int i = ia + lane; i <= ib; i += 32) {
+      const PagedSees v = paged_sees(a, wk.row0, wk.n, wk.L, wk.prefix, i);
+      if (v.lo < v.hi) least = min(least, v.lo);
+      most = max(most, v.lo);
+    }
+    lo = __reduce_min_sync(0xffffffffu, least);
+    all_lo = __reduce_max_sync(0xffffffffu, most);
+  }
+  if (lo >= hi) return;
+  ta = max(wk.t0, lo / kPmKeys);
+  te = max(ta, min(wk.t1, (hi + kPmKeys - 1) / kPmKeys));
+  la = all_lo / kPmKeys + (all_lo % kPmKeys != 0);
+  le = all_hi / kPmKeys;
+}
 __device__ __forceinline__ PmPlan pm_plan(const PagedAttend& a, const PagedWalk& wk, int lane) {
   PmPlan p;
   p.single = wk.n <= a.w.ppos;
   const int i0 = wk.first_pos(a.w), end = min(wk.n, i0 + wk.n_pos(a.w));
-#pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const int ia = i0 + s * a.w.ppos, ib = min(end, ia + a.w.ppos) - 1;
-    p.a[s] = p.e[s] = 0;
-    if (ib < ia || (p.single && s > 0)) continue;
-    int lo = a.window > 0 ? max(0, wk.L - wk.n + ia - a.window + 1) : 0;
-    if (a.first_key) {
-      int least = 0x7fffffff;
-      for (int i = ia + lane; i <= ib; i += 32) {
-        const PagedSees v = paged_sees(a, wk.row0, wk.n, wk.L, wk.prefix, i);
-        if (v.lo < v.hi) least = min(least, v.lo);
-      }
-      lo = __reduce_min_sync(0xffffffffu, least);
-    }
-    const int hi = min(wk.L, max(wk.L - wk.n + ib + 1, wk.prefix));
-    if (lo >= hi) continue;
-    p.a[s] = max(wk.t0, lo / kPmKeys);
-    p.e[s] = max(p.a[s], min(wk.t1, (hi + kPmKeys - 1) / kPmKeys));
-  }
-  const bool h0 = p.e[0] > p.a[0], h1 = p.e[1] > p.a[1];
-  p.A = h0 && h1 ? min(p.a[0], p.a[1]) : h0 ? p.a[0] : p.a[1];
-  p.E = h0 && h1 ? max(p.e[0], p.e[1]) : h0 ? p.e[0] : p.e[1];
+  pm_row_tile(a, wk, lane, i0, min(end, i0 + a.w.ppos) - 1, p.a0, p.e0, p.la0, p.le0);
+  pm_row_tile(a, wk, lane, i0 + a.w.ppos, (p.single ? 0 : min(end, i0 + 2 * a.w.ppos)) - 1, p.a1, p.e1, p.la1, p.le1);
+  const bool h0 = p.e0 > p.a0, h1 = p.e1 > p.a1;
+  p.A = h0 && h1 ? min(p.a0, p.a1) : h0 ? p.a0 : p.a1;
+  p.E = h0 && h1 ? max(p.e0, p.e1) : h0 ? p.e0 : p.e1;
   return p;
+}
+
+// Warp-uniform bounded wait that also ends when another role has given up.
+__device__ __noinline__ bool pm_wait_slow(uint64_t* bar, uint32_t parity, int limit, volatile int* abort_flag) {
+  if (limit <= 0) limit = kWaitLimitDefault;
+  for (int it = 0; it < limit; ++it) {
+    if (__all_sync(0xffffffffu, mbar_wait(bar, parity, 1))) return true;
+    if (it > 64) __nanosleep(64);
+    if ((it & 63) == 63 && warp_aborted(abort_flag)) return false;
+  }
+  return false;
+}
+__device__ __forceinline__ bool pm_wait(uint64_t* bar, uint32_t parity, int limit, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, 1)) || pm_wait_slow(bar, parity, limit, abort_flag);
 }
 
 __device__ __forceinline__ float rcp_approx(float x) {
@@ -156,121 +183,137 @@ __global__ void __launch_bounds__(kPmThreads, 1)
   const bool any = wk.seek(a, seqs, blockIdx.x * share, share);
 
   if (wg == 0) {
-    warpgroup_reg_dec<56>();
-    if (warp == 0 && any) {
-      // ------------------------------------------------------------ TMA ------------------------------------------------
+    if ((warp == 0 || warp == 2) && any) {
+      // ------------------------------------------------------------ TMA: queries and K, or V ----------------------------
+      const bool is_k = warp == 0;
       const int P = a.pl.P, npg = kPmKeys / P, boxes = npg * H, pg = lane / H, hh = lane % H;
-      const uint32_t box_dst = hh * SM::kHalf + pg * P * 128;
-      const long long n_rows = (a.pl.n_pages - 1) * a.pl.page_stride + (a.pl.Hkv - 1) * a.pl.head_stride + P;   // (a box there reads zeros)
+      const uint32_t dst = sbase + (is_k ? SM::kK : SM::kV) + hh * SM::kHalf + pg * P * 128;
+      const CUtensorMap* map = is_k ? &map_k : &map_v;
+      uint64_t *full = is_k ? k_full : v_full, *empty = is_k ? k_empty : v_empty;
+      const int n_rows = (int)((a.pl.n_pages - 1) * a.pl.page_stride + (a.pl.Hkv - 1) * a.pl.head_stride + P);   // (a box there reads zeros)
       int kt = 0, seg = 0;
       bool ok = true;
       while (ok && wk.next(a, seqs)) {
         const PmPlan pl = pm_plan(a, wk, lane);
         if (pl.A >= pl.E) continue;
-        if (seg > 0 && !warp_waits(q_empty, (seg - 1) & 1, lim)) { ok = false; break; }
-        ++seg;
-        const int i0 = wk.first_pos(a.w);
-        if (lane == 0) {
-          const bool two = !pl.single && pl.items(1) > 0;
-          const uint32_t rows = (uint32_t)ppos * G * 128;
-          mbar_expect_tx(q_full, (two ? 2 : 1) * H * rows + (uint32_t)a.dbg_tx_extra);
-          for (int s = 0; s < (two ? 2 : 1); ++s)
-            for (int x = 0; x < H; ++x)
-              tma_load_q(sbase + SM::kQ + s * SM::kTile + x * SM::kHalf, &map_q, x, wk.h * G, wk.row0 + i0 + s * ppos, q_full);
-        }
-        for (int t = pl.A; t < pl.E; ++t) {
-          if (!pl.act(0, t) && !pl.act(1, t)) continue;
-          const int index = t * npg + pg, st = kt % NS, ph = ((kt / NS) - 1) & 1;
-          long long row = -1;
-          if (lane < boxes && index * P < wk.L) row = paged_row(a.pb, a.pl, wk.b, wk.h, index);
-          if (row < 0) row = n_rows;
-          if (warp_aborted(abort_flag)) { ok = false; break; }
-          if (kt >= NS && !warp_waits(&k_empty[st], ph, lim)) { ok = false; break; }
-          if (lane == 0) mbar_expect_tx(&k_full[st], SM::kTile + (uint32_t)a.dbg_tx_extra);
-          __syncwarp();
-          if (lane < boxes) tma_load_box(sbase + SM::kK + st * SM::kTile + box_dst, &map_k, hh * 64, (int)row, &k_full[st]);
-          if (kt >= NS && !warp_waits(&v_empty[st], ph, lim)) {    // (the K tile above is still waited for at the end)
-            warp_waits(&k_full[st], (kt / NS) & 1, lim);
-            ok = false;
-            break;
+        // row of this lane's box in tile t; loaded a tile ahead
+        auto box_row = [&](int t) {
+          const int index = t * npg + pg;
+          long long r = -1;
+          if (lane < boxes && t < pl.E && index * P < wk.L) r = paged_row(a.pb, a.pl, wk.b, wk.h, index);
+          return r < 0 ? n_rows : (int)r;
+        };
+        int row = box_row(pl.A);
+        if (is_k) {
+          if (seg > 0 && !pm_wait(q_empty, (seg - 1) & 1, lim, abort_flag)) { ok = false; break; }
+          if (lane == 0) {
+            const bool two = !pl.single && pl.items(1) > 0;
+            mbar_expect_tx(q_full, (two ? 2 : 1) * H * ppos * G * 128 + (uint32_t)a.dbg_tx_extra);
+            for (int s = 0; s < (two ? 2 : 1); ++s)
+              for (int x = 0; x < H; ++x)
+                tma_load_q(sbase + SM::kQ + s * SM::kTile + x * SM::kHalf, &map_q, x, wk.h * G, wk.row0 + wk.first_pos(a.w) + s * ppos, q_full);
           }
-          if (lane == 0) mbar_expect_tx(&v_full[st], SM::kTile + (uint32_t)a.dbg_tx_extra);
-          __syncwarp();
-          if (lane < boxes) tma_load_box(sbase + SM::kV + st * SM::kTile + box_dst, &map_v, hh * 64, (int)row, &v_full[st]);
-          ++kt;
+        }
+        ++seg;
+        for (int t = pl.A; t < pl.E; ++t) {
+          const int row_next = box_row(t + 1);
+          if (pl.act<0>(t) || pl.act<1>(t)) {
+            const int st = kt % NS;
+            if (kt >= NS && !pm_wait(&empty[st], ((kt / NS) - 1) & 1, lim, abort_flag)) { ok = false; break; }
+            if (lane == 0) mbar_expect_tx(&full[st], SM::kTile + (uint32_t)a.dbg_tx_extra);
+            __syncwarp();
+            if (lane < boxes) tma_load_box(dst + st * SM::kTile, map, hh * 64, row, &full[st]);
+            ++kt;
+          }
+          row = row_next;
         }
       }
       if (!ok) *abort_flag = 1;
       // every copy has landed before the CTA leaves, whatever the other roles do
-      for (int x = max(0, kt - NS); x < kt; ++x) {
-        warp_waits(&k_full[x % NS], (x / NS) & 1, lim);
-        warp_waits(&v_full[x % NS], (x / NS) & 1, lim);
-      }
-      if (seg > 0) warp_waits(q_full, (seg - 1) & 1, lim);
+      for (int x = max(0, kt - NS); x < kt; ++x) warp_waits(&full[x % NS], (x / NS) & 1, lim);
+      if (is_k && seg > 0) warp_waits(q_full, (seg - 1) & 1, lim);
     } else if (warp == 1 && any) {
       // ------------------------------------------------------------ MMA issuer -----------------------------------------
       constexpr uint32_t id_s = umma_idesc(true, false, false, 128, kPmKeys);
       constexpr uint32_t id_o = umma_idesc(true, false, true, 128, D);
+      constexpr uint32_t kStep = 2048 / 16;                       // 16 keys of V
       const uint32_t one = elect_one();                           // (the whole warp runs this loop: see umma_ss_one)
+      const uint32_t q_lo = umma_desc_lo(sbase + SM::kQ, 16), k_lo = umma_desc_lo(sbase + SM::kK, 16), v_lo = umma_desc_lo(sbase + SM::kV, SM::kHalf);
       bool ok = true;
       int kt = 0, seg = 0;
-      int n_p[2] = {0, 0}, n_o[2] = {0, 0};                       // items whose P was awaited, segments that used O
-      bool pending = false;
-      int p_slot = 0, p_stage = 0, p_phase = 0;
-      bool p_first = false, p_last_v = false;
-      auto product = [&]() {                                      // O (+)= P V of the pending item
-        const int s = p_slot;
-        pending = false;
-        if (!warp_waits(&p_ready[s], n_p[s] & 1, lim) || !warp_waits(&v_full[p_stage], p_phase, lim)) { ok = false; return; }
-        ++n_p[s];
-        if (p_first) {
-          if (n_o[s] > 0 && !warp_waits(&o_free[s], (n_o[s] - 1) & 1, lim)) { ok = false; return; }
-          ++n_o[s];
+      uint32_t n_p0 = 0, n_p1 = 0, n_o0 = 0, n_o1 = 0;            // items whose P was awaited, segments that used O
+      // the item of either row tile whose product with V is to come: its stage and phase, whether it is the segment's first, whether
+      // V is free after it, whether the softmax warps may have formed it
+      bool pend0 = false, pend1 = false, first0 = true, first1 = true, free0 = false, free1 = false, look0 = false, look1 = false;
+      int st0 = 0, st1 = 0;
+      uint32_t ph0 = 0, ph1 = 0;
+      auto product = [&](auto slot_c) {                           // O (+)= P V
+        constexpr int S = decltype(slot_c)::value;
+        bool &pend = S ? pend1 : pend0, &first = S ? first1 : first0;
+        uint32_t &n_p = S ? n_p1 : n_p0, &n_o = S ? n_o1 : n_o0;
+        const int st = S ? st1 : st0;
+        pend = false;
+        if (!pm_wait(&v_full[st], S ? ph1 : ph0, lim, abort_flag) || !pm_wait(&p_ready[S], n_p & 1, lim, abort_flag)) { ok = false; return; }
+        ++n_p;
+        if (first) {
+          if (n_o > 0 && !pm_wait(&o_free[S], (n_o - 1) & 1, lim, abort_flag)) { ok = false; return; }
+          ++n_o;
         }
         tc_fence_after();
-        if (!skip_pv[s]) {
-          const uint32_t pt = tmem + s * 128, o = tmem + 256 + s * 128, v = umma_desc_lo(sbase + SM::kV + p_stage * SM::kTile, SM::kHalf);
-          umma_ts4_one<8, 2048 / 16>(one, o, pt, v, id_o, p_first ? 0u : 1u);
-          umma_ts4_one<8, 2048 / 16>(one, o, pt + 32, v + 4 * (2048 / 16), id_o, 1u);
+        if (!((S ? look1 : look0) && skip_pv[S])) {
+          const uint32_t pt = tmem + S * 128, o = tmem + 256 + S * 128, v = v_lo + st * (SM::kTile / 16);
+          umma_ts4_one<8, kStep>(one, o, pt, v, id_o, first ? 0u : 1u);
+          umma_ts4_one<8, kStep>(one, o, pt + 32, v + 4 * kStep, id_o, 1u);
         }
-        umma_commit_one(one, &pv_done[s]);
-        if (p_last_v) umma_commit_one(one, &v_empty[p_stage]);
+        first = false;
+        umma_commit_one(one, &pv_done[S]);
+        if (S ? free1 : free0) umma_commit_one(one, &v_empty[st]);
+      };
+      constexpr std::integral_constant<int, 0> s0{};
+      constexpr std::integral_constant<int, 1> s1{};
+      auto score = [&](auto slot_c, const PmPlan& pl, int t, int st, uint32_t ph, bool last) {   // S = Q K^T
+        constexpr int S = decltype(slot_c)::value;
+        if (S ? pend1 : pend0) product(slot_c);                   // (S takes the place of the P before)
+        const uint32_t q = q_lo + (pl.single ? 0 : S * (SM::kTile / 16)), k = k_lo + st * (SM::kTile / 16);
+#pragma unroll
+        for (int x = 0; x < H; ++x) umma_ss4_one<2, 2>(one, tmem + S * 128, q + x * (SM::kHalf / 16), k + x * (SM::kHalf / 16), id_s, x > 0);
+        umma_commit_one(one, &s_full[S]);
+        if (last) umma_commit_one(one, &k_empty[st]);
+        (S ? pend1 : pend0) = true;
+        (S ? st1 : st0) = st;
+        (S ? ph1 : ph0) = ph;
+        (S ? free1 : free0) = last;
+        (S ? look1 : look0) = pl.template look<S>(t);
       };
       while (ok && wk.next(a, seqs)) {
         const PmPlan pl = pm_plan(a, wk, lane);
         if (pl.A >= pl.E) continue;
-        if (!warp_waits(q_full, seg & 1, lim)) { ok = false; break; }
+        if (!pm_wait(q_full, seg & 1, lim, abort_flag)) { ok = false; break; }
         ++seg;
-        tc_fence_after();
-        bool first[2] = {true, true};
-        for (int t = pl.A; t < pl.E && ok; ++t) {
-          const bool a0 = pl.act(0, t), a1 = pl.act(1, t);
-          if (!a0 && !a1) continue;
-          if (warp_aborted(abort_flag)) { ok = false; break; }
-          const int st = kt % NS, ph = (kt / NS) & 1;
-          if (!warp_waits(&k_full[st], ph, lim)) { ok = false; break; }
-          tc_fence_after();
+        first0 = first1 = true;
 #pragma unroll 1
-          for (int s = a0 ? 0 : 1; s < (a1 ? 2 : 1) && ok; ++s) {
-            if (pending && p_slot == s) product();
-            if (!ok) break;
-            const uint32_t q = umma_desc_lo(sbase + SM::kQ + (pl.single ? 0 : s * SM::kTile), 16), k = umma_desc_lo(sbase + SM::kK + st * SM::kTile, 16);
-#pragma unroll
-            for (int x = 0; x < H; ++x) umma_ss4_one<2, 2>(one, tmem + s * 128, q + x * (SM::kHalf / 16), k + x * (SM::kHalf / 16), id_s, x > 0);
-            umma_commit_one(one, &s_full[s]);
-            const bool last = s == 1 || !a1;
-            if (last) umma_commit_one(one, &k_empty[st]);
-            if (pending) product();
-            pending = true;
-            p_slot = s; p_stage = st; p_phase = ph;
-            p_first = first[s]; p_last_v = last;
-            first[s] = false;
+        for (int t = pl.A; t < pl.E; ++t) {
+          const bool act0 = pl.act<0>(t), act1 = pl.act<1>(t);
+          if (!act0 && !act1) continue;
+          const int st = kt % NS;
+          const uint32_t ph = (kt / NS) & 1;
+          if (!pm_wait(&k_full[st], ph, lim, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          if (act0) {
+            score(s0, pl, t, st, ph, !act1);
+            if (ok && pend1) product(s1);
           }
+          if (ok && act1) {
+            score(s1, pl, t, st, ph, true);
+            if (ok && pend0) product(s0);
+          }
+          if (!ok) break;
           ++kt;
         }
         if (!ok) break;
         umma_commit_one(one, q_empty);
-        if (pending) product();
+        if (pend0) product(s0);
+        if (ok && pend1) product(s1);
       }
       umma_commit_one(one, done);
       if (!warp_waits(done, 0, lim)) ok = false;
@@ -278,7 +321,6 @@ __global__ void __launch_bounds__(kPmThreads, 1)
     }
   } else if (any) {
     // -------------------------------------------------------------- softmax and epilogue: one row per thread -------------
-    warpgroup_reg_inc<224>();
     const int slot = wg - 1, row = tid - 128 * wg, pi = row / G, g = row % G;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + slot * 128 + lane_off, tO = tmem + 256 + slot * 128 + lane_off;
@@ -294,26 +336,21 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       if (valid) see = paged_sees(a, wk.row0, wk.n, wk.L, wk.prefix, i);
       const bool live = __any_sync(0xffffffffu, valid);
       const int lo_most = __reduce_max_sync(0xffffffffu, valid ? see.lo : 0), hi_least = __reduce_min_sync(0xffffffffu, valid ? see.hi : 0x7fffffff);
-      // a tile is looked over where any row of the row tile may see it in part: by closed forms, the same for all four warps
-      const int ia = i0, ib = min(wk.n, i0 + ppos) - 1;
-      const int all_lo = a.first_key ? 0x7fffffff : a.window > 0 ? max(0, wk.L - wk.n + ib - a.window + 1) : 0;
-      const int all_hi = min(wk.L, max(wk.L - wk.n + ia + 1, wk.prefix));
       float slope2 = 0.f;
       if (MODS && a.slopes && valid) slope2 = __ldg(a.slopes + wk.h * G + g) * kLog2e;
       const int pos = wk.L - wk.n + i;
       float m = -INFINITY, l = 0.f;
       int done_items = 0;
       for (int t = pl.A; t < pl.E; ++t) {
-        const bool mine = pl.act(slot, t);
-        if (!mine) { kt += pl.act(1 - slot, t); continue; }
-        if (warp_aborted(abort_flag)) { ok = false; break; }
+        const bool act0 = pl.act<0>(t), act1 = pl.act<1>(t);
+        if (!(slot ? act1 : act0)) { kt += act0 || act1; continue; }
         const int tok0 = t * kPmKeys;
-        const bool look = tok0 < all_lo || tok0 + kPmKeys > all_hi;
+        const bool look = slot ? pl.look<1>(t) : pl.look<0>(t);
         bool simt = false;
         if (look) {
           // values of this tile: zeroed behind the end where they are not finite; elsewhere such a value makes the tile special
           const int st = kt % NS;
-          if (!warp_waits(&v_full[st], (kt / NS) & 1, lim)) { ok = false; break; }
+          if (!pm_wait(&v_full[st], (kt / NS) & 1, lim, abort_flag)) { ok = false; break; }
           bool bad = false;
           unsigned char* vt = smem + SM::kV + st * SM::kTile + row * 16;
 #pragma unroll 4
@@ -329,68 +366,64 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           if (__any_sync(0xffffffffu, bad) && lane == 0) found_bad[mark] = n_scan + 1;
           __syncwarp();
           if (lane == 0) mbar_arrive1(&scanned[slot]);
-          if (!warp_waits(&scanned[slot], n_scan & 1, lim)) { ok = false; break; }
+          if (!pm_wait(&scanned[slot], n_scan & 1, lim, abort_flag)) { ok = false; break; }
           simt = __any_sync(0xffffffffu, found_bad[mark] == n_scan + 1);
           ++n_scan;
         }
-        if (!warp_waits(&s_full[slot], n & 1, lim)) { ok = false; break; }
+        if (!pm_wait(&s_full[slot], n & 1, lim, abort_flag)) { ok = false; break; }
         tc_fence_after();
         if (live) {
-          float s[kPmKeys];
-          {
-            uint32_t r0[32], r1[32], r2[32], r3[32];
-            tmem_ld32_async(tS, r0);
-            tmem_ld32_async(tS + 32, r1);
-            tmem_ld32_async(tS + 64, r2);
-            tmem_ld32_async(tS + 96, r3);
-            tmem_ld_wait32(r0);
-            tmem_ld_wait32(r1);
-            tmem_ld_wait32(r2);
-            tmem_ld_wait32(r3);
-#pragma unroll
-            for (int x = 0; x < 32; ++x) {
-              s[x] = __uint_as_float(r0[x]); s[32 + x] = __uint_as_float(r1[x]);
-              s[64 + x] = __uint_as_float(r2[x]); s[96 + x] = __uint_as_float(r3[x]);
-            }
-          }
-          if constexpr (MODS) {
-            if (a.softcap > 0.f) {                                // cap tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap)), in base 2
-              const float k1 = 2.f * sc2 / a.softcap, c2 = a.softcap * kLog2e;
-#pragma unroll
-              for (int x = 0; x < kPmKeys; ++x) s[x] = fmaf(-2.f * c2, rcp_approx(1.f + ex2(s[x] * k1)), c2);
-            } else {
-#pragma unroll
-              for (int x = 0; x < kPmKeys; ++x) s[x] *= sc2;
-            }
-            if (a.slopes) {
-              const float d0 = (float)(tok0 - pos);
-#pragma unroll
-              for (int x = 0; x < kPmKeys; ++x) s[x] = fmaf(-slope2, fabsf(d0 + (float)x), s[x]);
-            }
-          }
+          const bool part = tok0 < lo_most || tok0 + kPmKeys > hi_least;   // (warp-uniform)
           const float mul = MODS ? 1.f : sc2;
-          if (tok0 < lo_most || tok0 + kPmKeys > hi_least) {      // (warp-uniform)
+          // 32 columns of S at a time, the next 32 on their way: first for the maximum, then again for the exponentials (loading
+          // twice costs less than 128 registers per row)
+          auto scores = [&](uint32_t (&r)[32], float (&s)[32], int c) {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              const uint32_t bits = bits_between(see.lo - tok0 - 32 * w, see.hi - tok0 - 32 * w);
+            for (int x = 0; x < 32; ++x) s[x] = __uint_as_float(r[x]);
+            if constexpr (MODS) {
+              if (a.softcap > 0.f) {                              // cap tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap)), in base 2
+                const float k1 = 2.f * sc2 / a.softcap, c2 = a.softcap * kLog2e;
+#pragma unroll
+                for (int x = 0; x < 32; ++x) s[x] = fmaf(-2.f * c2, rcp_approx(1.f + ex2(s[x] * k1)), c2);
+              } else {
+#pragma unroll
+                for (int x = 0; x < 32; ++x) s[x] *= sc2;
+              }
+              if (a.slopes) {
+                const float d0 = (float)(tok0 + 32 * c - pos);
+#pragma unroll
+                for (int x = 0; x < 32; ++x) s[x] = fmaf(-slope2, fabsf(d0 + (float)x), s[x]);
+              }
+            }
+            if (part) {
+              const uint32_t bits = bits_between(see.lo - tok0 - 32 * c, see.hi - tok0 - 32 * c);
 #pragma unroll
               for (int x = 0; x < 32; ++x)
-                if (!(bits & (1u << x))) s[32 * w + x] = -INFINITY;
+                if (!(bits & (1u << x))) s[x] = -INFINITY;
             }
-          }
-          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          };
+          float mt = -INFINITY;
+          {
+            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            uint32_t r[2][32];
+            tmem_ld32_async(tS, r[0]);
 #pragma unroll
-          for (int x = 0; x < kPmKeys; x += 4) {
+            for (int c = 0; c < 4; ++c) {
+              tmem_ld_wait32(r[c & 1]);
+              if (c < 3) tmem_ld32_async(tS + 32 * (c + 1), r[(c + 1) & 1]);
+              float s[32];
+              scores(r[c & 1], s, c);
 #pragma unroll
-            for (int y = 0; y < 4; ++y) mx[y] = fmaxf(mx[y], s[x + y]);
+              for (int x = 0; x < 32; ++x) mx[x & 3] = fmaxf(mx[x & 3], s[x]);
+            }
+            mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * mul;
           }
-          const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * mul;
           // The first visible keys of a row set its maximum (its row of O is zero so far); later ones only move it when it would
           // let a probability exceed 2^8.
           const bool grow = mt > m + 8.f && m > -INFINITY;
           if (m == -INFINITY) m = mt;
           if (__any_sync(0xffffffffu, grow)) {
-            if (!warp_waits(&pv_done[slot], (n - 1) & 1, lim)) { ok = false; break; }   // every product with P so far
+            if (!pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) { ok = false; break; }   // every product with P so far
             tc_fence_after();
             const float m_new = grow ? mt : m, f = grow ? ex2(m - m_new) : 1.f;
             m = m_new;
@@ -407,25 +440,31 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           }
           const float nm = m == -INFINITY ? 0.f : -m;
           float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+          uint32_t r[2][32];
+          tmem_ld32_async(tS, r[0]);
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
+            tmem_ld_wait32(r[c & 1]);
+            if (c < 3) tmem_ld32_async(tS + 32 * (c + 1), r[(c + 1) & 1]);
+            float s[32];
+            scores(r[c & 1], s, c);
             uint32_t pk[16];
 #pragma unroll
             for (int x = 0; x < 16; ++x) {
-              const float2 v = __ffma2_rn(make_float2(s[32 * c + 2 * x], s[32 * c + 2 * x + 1]), make_float2(mul, mul), make_float2(nm, nm));
+              const float2 v = __ffma2_rn(make_float2(s[2 * x], s[2 * x + 1]), make_float2(mul, mul), make_float2(nm, nm));
               const float2 p = make_float2(ex2(v.x), ex2(v.y));
               if (x & 1) sum1 = __fadd2_rn(sum1, p); else sum0 = __fadd2_rn(sum0, p);
               pk[x] = pack_bf16(p.x, p.y);
             }
-            tmem_st16(tS + 16 * c, pk);
+            tmem_st16(tS + 16 * c, pk);                            // (over columns of S that are loaded)
           }
           l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
           tmem_st_wait();
         }
         if (simt) {
           // the product with V here: O += sum over the row's visible keys of p v
-          if (done_items > 0 && !warp_waits(&pv_done[slot], (n - 1) & 1, lim)) { ok = false; break; }
-          if (done_items == 0 && n_used > 0 && !warp_waits(&o_free[slot], (n_used - 1) & 1, lim)) { ok = false; break; }
+          if (done_items > 0 && !pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) { ok = false; break; }
+          if (done_items == 0 && n_used > 0 && !pm_wait(&o_free[slot], (n_used - 1) & 1, lim, abort_flag)) { ok = false; break; }
           tc_fence_after();
           const unsigned char* vt = smem + SM::kV + (kt % NS) * SM::kTile;
 #pragma unroll 1
@@ -471,7 +510,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0 && (warp & 3) == 0) skip_pv[slot] = simt;
+        if (look && lane == 0 && (warp & 3) == 0) skip_pv[slot] = simt;
         if (lane == 0) mbar_arrive1(&p_ready[slot]);
         ++n;
         ++kt;
@@ -481,7 +520,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       // ------------------------------------------------------------ end of the segment ----------------------------------
       const bool whole = wk.head && wk.tail;
       if (my > 0) {
-        if (!warp_waits(&pv_done[slot], (n - 1) & 1, lim)) { ok = false; break; }
+        if (!pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) { ok = false; break; }
         tc_fence_after();
         ++n_used;
       }
@@ -494,7 +533,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           __syncwarp();
           if (lane == 0) mbar_arrive1(halves);
         } else {
-          if (!warp_waits(halves, n_half & 1, lim)) { ok = false; break; }
+          if (!pm_wait(halves, n_half & 1, lim, abort_flag)) { ok = false; break; }
           tc_fence_after();
           const float2 o = ml_s[row];
           m1 = o.x;
@@ -553,8 +592,6 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       }
     }
     if (!ok) *abort_flag = 1;
-  } else {
-    warpgroup_reg_inc<224>();
   }
 
   // ---------------------------------------------------------------- end: tensor memory back -----------------------------
