@@ -97,7 +97,7 @@ __device__ __forceinline__ PmPlan pm_plan(const PagedAttend& a, const PagedWalk&
 }
 
 // Warp-uniform bounded wait that also ends when another role has given up.
-__device__ __noinline__ bool pm_wait_slow(uint64_t* bar, uint32_t parity, int limit, volatile int* abort_flag) {
+__device__ __forceinline__ bool pm_wait_slow(uint64_t* bar, uint32_t parity, int limit, volatile int* abort_flag) {
   if (limit <= 0) limit = kWaitLimitDefault;
   for (int it = 0; it < limit; ++it) {
     if (__all_sync(0xffffffffu, mbar_wait(bar, parity, 1))) return true;
@@ -119,6 +119,33 @@ __device__ __forceinline__ void tma_load_q(uint32_t dst, const CUtensorMap* map,
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
                "l"(map), "r"(0), "r"(half), "r"(head), "r"(tok), "r"(smem_u32(bar))
                : "memory");
+}
+// 128 consecutive columns of this thread's tensor-memory lane.
+__device__ __forceinline__ void tmem_ld128(uint32_t addr, uint32_t (&r)[128]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr + 0)
+      : "memory");
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+      : "r"(addr + 32)
+      : "memory");
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[64]), "=r"(r[65]), "=r"(r[66]), "=r"(r[67]), "=r"(r[68]), "=r"(r[69]), "=r"(r[70]), "=r"(r[71]), "=r"(r[72]), "=r"(r[73]), "=r"(r[74]), "=r"(r[75]), "=r"(r[76]), "=r"(r[77]), "=r"(r[78]), "=r"(r[79]), "=r"(r[80]), "=r"(r[81]), "=r"(r[82]), "=r"(r[83]), "=r"(r[84]), "=r"(r[85]), "=r"(r[86]), "=r"(r[87]), "=r"(r[88]), "=r"(r[89]), "=r"(r[90]), "=r"(r[91]), "=r"(r[92]), "=r"(r[93]), "=r"(r[94]), "=r"(r[95])
+      : "r"(addr + 64)
+      : "memory");
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[96]), "=r"(r[97]), "=r"(r[98]), "=r"(r[99]), "=r"(r[100]), "=r"(r[101]), "=r"(r[102]), "=r"(r[103]), "=r"(r[104]), "=r"(r[105]), "=r"(r[106]), "=r"(r[107]), "=r"(r[108]), "=r"(r[109]), "=r"(r[110]), "=r"(r[111]), "=r"(r[112]), "=r"(r[113]), "=r"(r[114]), "=r"(r[115]), "=r"(r[116]), "=r"(r[117]), "=r"(r[118]), "=r"(r[119]), "=r"(r[120]), "=r"(r[121]), "=r"(r[122]), "=r"(r[123]), "=r"(r[124]), "=r"(r[125]), "=r"(r[126]), "=r"(r[127])
+      : "r"(addr + 96)
+      : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]) :: "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[32]), "+r"(r[33]), "+r"(r[34]), "+r"(r[35]), "+r"(r[36]), "+r"(r[37]), "+r"(r[38]), "+r"(r[39]), "+r"(r[40]), "+r"(r[41]), "+r"(r[42]), "+r"(r[43]), "+r"(r[44]), "+r"(r[45]), "+r"(r[46]), "+r"(r[47]), "+r"(r[48]), "+r"(r[49]), "+r"(r[50]), "+r"(r[51]), "+r"(r[52]), "+r"(r[53]), "+r"(r[54]), "+r"(r[55]), "+r"(r[56]), "+r"(r[57]), "+r"(r[58]), "+r"(r[59]), "+r"(r[60]), "+r"(r[61]), "+r"(r[62]), "+r"(r[63]) :: "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[64]), "+r"(r[65]), "+r"(r[66]), "+r"(r[67]), "+r"(r[68]), "+r"(r[69]), "+r"(r[70]), "+r"(r[71]), "+r"(r[72]), "+r"(r[73]), "+r"(r[74]), "+r"(r[75]), "+r"(r[76]), "+r"(r[77]), "+r"(r[78]), "+r"(r[79]), "+r"(r[80]), "+r"(r[81]), "+r"(r[82]), "+r"(r[83]), "+r"(r[84]), "+r"(r[85]), "+r"(r[86]), "+r"(r[87]), "+r"(r[88]), "+r"(r[89]), "+r"(r[90]), "+r"(r[91]), "+r"(r[92]), "+r"(r[93]), "+r"(r[94]), "+r"(r[95]) :: "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[96]), "+r"(r[97]), "+r"(r[98]), "+r"(r[99]), "+r"(r[100]), "+r"(r[101]), "+r"(r[102]), "+r"(r[103]), "+r"(r[104]), "+r"(r[105]), "+r"(r[106]), "+r"(r[107]), "+r"(r[108]), "+r"(r[109]), "+r"(r[110]), "+r"(r[111]), "+r"(r[112]), "+r"(r[113]), "+r"(r[114]), "+r"(r[115]), "+r"(r[116]), "+r"(r[117]), "+r"(r[118]), "+r"(r[119]), "+r"(r[120]), "+r"(r[121]), "+r"(r[122]), "+r"(r[123]), "+r"(r[124]), "+r"(r[125]), "+r"(r[126]), "+r"(r[127]) :: "memory");
 }
 // bits a .. e - 1 of a word (a, e in any range)
 __device__ __forceinline__ uint32_t bits_between(int a, int e) {
@@ -183,6 +210,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
   const bool any = wk.seek(a, seqs, blockIdx.x * share, share);
 
   if (wg == 0) {
+    warpgroup_reg_dec<120>();                                     // (120 + 2 x 192 = 3 x 168, what the CTA is launched with)
     if ((warp == 0 || warp == 2) && any) {
       // ------------------------------------------------------------ TMA: queries and K, or V ----------------------------
       const bool is_k = warp == 0;
@@ -319,15 +347,16 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       if (!warp_waits(done, 0, lim)) ok = false;
       if (!ok) *abort_flag = 1;
     }
-  } else if (any) {
+  } else {
     // -------------------------------------------------------------- softmax and epilogue: one row per thread -------------
+    warpgroup_reg_inc<192>();
     const int slot = wg - 1, row = tid - 128 * wg, pi = row / G, g = row % G;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + slot * 128 + lane_off, tO = tmem + 256 + slot * 128 + lane_off;
     const float sc2 = a.sm_scale * kLog2e;
     bool ok = true;
     int kt = 0, n = 0, n_scan = 0, n_half = 0, n_used = 0;        // tiles of the CTA, items of this slot, look-overs, merged segments, segments that used O
-    while (ok && wk.next(a, seqs)) {
+    while (any && ok && wk.next(a, seqs)) {
       const PmPlan pl = pm_plan(a, wk, lane);
       const int my = pl.items(slot);
       const int i0 = wk.first_pos(a.w) + (pl.single ? 0 : slot * ppos), i = i0 + pi;
@@ -375,49 +404,36 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         if (live) {
           const bool part = tok0 < lo_most || tok0 + kPmKeys > hi_least;   // (warp-uniform)
           const float mul = MODS ? 1.f : sc2;
-          // 32 columns of S at a time, the next 32 on their way: first for the maximum, then again for the exponentials (loading
-          // twice costs less than 128 registers per row)
-          auto scores = [&](uint32_t (&r)[32], float (&s)[32], int c) {
+          uint32_t r[kPmKeys];
+          tmem_ld128(tS, r);
+          if constexpr (MODS) {
+            if (a.softcap > 0.f) {                                // cap tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap)), in base 2
+              const float k1 = 2.f * sc2 / a.softcap, c2 = a.softcap * kLog2e;
 #pragma unroll
-            for (int x = 0; x < 32; ++x) s[x] = __uint_as_float(r[x]);
-            if constexpr (MODS) {
-              if (a.softcap > 0.f) {                              // cap tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap)), in base 2
-                const float k1 = 2.f * sc2 / a.softcap, c2 = a.softcap * kLog2e;
+              for (int x = 0; x < kPmKeys; ++x) r[x] = __float_as_uint(fmaf(-2.f * c2, rcp_approx(1.f + ex2(__uint_as_float(r[x]) * k1)), c2));
+            } else {
 #pragma unroll
-                for (int x = 0; x < 32; ++x) s[x] = fmaf(-2.f * c2, rcp_approx(1.f + ex2(s[x] * k1)), c2);
-              } else {
-#pragma unroll
-                for (int x = 0; x < 32; ++x) s[x] *= sc2;
-              }
-              if (a.slopes) {
-                const float d0 = (float)(tok0 + 32 * c - pos);
-#pragma unroll
-                for (int x = 0; x < 32; ++x) s[x] = fmaf(-slope2, fabsf(d0 + (float)x), s[x]);
-              }
+              for (int x = 0; x < kPmKeys; ++x) r[x] = __float_as_uint(__uint_as_float(r[x]) * sc2);
             }
-            if (part) {
+            if (a.slopes) {
+              const float d0 = (float)(tok0 - pos);
+#pragma unroll
+              for (int x = 0; x < kPmKeys; ++x) r[x] = __float_as_uint(fmaf(-slope2, fabsf(d0 + (float)x), __uint_as_float(r[x])));
+            }
+          }
+          if (part) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
               const uint32_t bits = bits_between(see.lo - tok0 - 32 * c, see.hi - tok0 - 32 * c);
 #pragma unroll
               for (int x = 0; x < 32; ++x)
-                if (!(bits & (1u << x))) s[x] = -INFINITY;
+                if (!(bits & (1u << x))) r[32 * c + x] = 0xff800000u;
             }
-          };
-          float mt = -INFINITY;
-          {
-            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            uint32_t r[2][32];
-            tmem_ld32_async(tS, r[0]);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              tmem_ld_wait32(r[c & 1]);
-              if (c < 3) tmem_ld32_async(tS + 32 * (c + 1), r[(c + 1) & 1]);
-              float s[32];
-              scores(r[c & 1], s, c);
-#pragma unroll
-              for (int x = 0; x < 32; ++x) mx[x & 3] = fmaxf(mx[x & 3], s[x]);
-            }
-            mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * mul;
           }
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int x = 0; x < kPmKeys; x += 2) mx[x / 2 & 3] = fmaxf(mx[x / 2 & 3], fmaxf(__uint_as_float(r[x]), __uint_as_float(r[x + 1])));
+          const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * mul;
           // The first visible keys of a row set its maximum (its row of O is zero so far); later ones only move it when it would
           // let a probability exceed 2^8.
           const bool grow = mt > m + 8.f && m > -INFINITY;
@@ -440,23 +456,17 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           }
           const float nm = m == -INFINITY ? 0.f : -m;
           float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
-          uint32_t r[2][32];
-          tmem_ld32_async(tS, r[0]);
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            tmem_ld_wait32(r[c & 1]);
-            if (c < 3) tmem_ld32_async(tS + 32 * (c + 1), r[(c + 1) & 1]);
-            float s[32];
-            scores(r[c & 1], s, c);
             uint32_t pk[16];
 #pragma unroll
             for (int x = 0; x < 16; ++x) {
-              const float2 v = __ffma2_rn(make_float2(s[2 * x], s[2 * x + 1]), make_float2(mul, mul), make_float2(nm, nm));
+              const float2 v = __ffma2_rn(make_float2(__uint_as_float(r[32 * c + 2 * x]), __uint_as_float(r[32 * c + 2 * x + 1])), make_float2(mul, mul), make_float2(nm, nm));
               const float2 p = make_float2(ex2(v.x), ex2(v.y));
               if (x & 1) sum1 = __fadd2_rn(sum1, p); else sum0 = __fadd2_rn(sum0, p);
               pk[x] = pack_bf16(p.x, p.y);
             }
-            tmem_st16(tS + 16 * c, pk);                            // (over columns of S that are loaded)
+            tmem_st16(tS + 16 * c, pk);
           }
           l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
           tmem_st_wait();
