@@ -40,7 +40,8 @@ struct PmSmem {
   static constexpr int NS = D == 128 ? 2 : 4;                    // stages of K, and of V
   static constexpr int kQ = 0, kK = kQ + 2 * kTile, kV = kK + NS * kTile, kSeqs = kV + NS * kTile;
   static constexpr int kMl = kSeqs + (int)((sizeof(PagedSeqs) + 15) / 16 * 16);   // float2 [128]: maximum and sum of the second half
-  static constexpr int kBars = kMl + 128 * 8;
+  static constexpr int kWalk = kMl + 128 * 8;                     // PagedWalk [8]: where the softmax warps are
+  static constexpr int kBars = kWalk + 8 * 64;
   static constexpr int kNumBars = 4 * NS + 14;
   static constexpr int kMisc = kBars + kNumBars * 8;             // tensor-memory base, abort flag, skip flags [2], look-over marks [2][2]
   static constexpr int kBytes = kMisc + 48;
@@ -245,14 +246,12 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         ++seg;
         for (int t = pl.A; t < pl.E; ++t) {
           const int row_next = box_row(t + 1);
-          if (pl.act<0>(t) || pl.act<1>(t)) {
-            const int st = kt % NS;
-            if (kt >= NS && !pm_wait(&empty[st], ((kt / NS) - 1) & 1, lim, abort_flag)) { ok = false; break; }
-            if (lane == 0) mbar_expect_tx(&full[st], SM::kTile + (uint32_t)a.dbg_tx_extra);
-            __syncwarp();
-            if (lane < boxes) tma_load_box(dst + st * SM::kTile, map, hh * 64, row, &full[st]);
-            ++kt;
-          }
+          const int st = kt % NS;
+          if (kt >= NS && !pm_wait(&empty[st], ((kt / NS) - 1) & 1, lim, abort_flag)) { ok = false; break; }
+          if (lane == 0) mbar_expect_tx(&full[st], SM::kTile + (uint32_t)a.dbg_tx_extra);
+          __syncwarp();
+          if (lane < boxes) tma_load_box(dst + st * SM::kTile, map, hh * 64, row, &full[st]);
+          ++kt;
           row = row_next;
         }
       }
@@ -322,7 +321,6 @@ __global__ void __launch_bounds__(kPmThreads, 1)
 #pragma unroll 1
         for (int t = pl.A; t < pl.E; ++t) {
           const bool act0 = pl.act<0>(t), act1 = pl.act<1>(t);
-          if (!act0 && !act1) continue;
           const int st = kt % NS;
           const uint32_t ph = (kt / NS) & 1;
           if (!pm_wait(&k_full[st], ph, lim, abort_flag)) { ok = false; break; }
@@ -334,6 +332,11 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           if (ok && act1) {
             score(s1, pl, t, st, ph, true);
             if (ok && pend0) product(s0);
+          }
+          if (ok && !act0 && !act1) {                             // (between the two row tiles' documents)
+            if (!pm_wait(&v_full[st], ph, lim, abort_flag)) ok = false;
+            umma_commit_one(one, &k_empty[st]);
+            umma_commit_one(one, &v_empty[st]);
           }
           if (!ok) break;
           ++kt;
@@ -356,37 +359,61 @@ __global__ void __launch_bounds__(kPmThreads, 1)
     const float sc2 = a.sm_scale * kLog2e;
     bool ok = true;
     int kt = 0, n = 0, n_scan = 0, n_half = 0, n_used = 0;        // tiles of the CTA, items of this slot, look-overs, merged segments, segments that used O
-    while (any && ok && wk.next(a, seqs)) {
-      const PmPlan pl = pm_plan(a, wk, lane);
-      const int my = pl.items(slot);
-      const int i0 = wk.first_pos(a.w) + (pl.single ? 0 : slot * ppos), i = i0 + pi;
-      const bool valid = row < ppos * G && i < wk.n;
+    // The walk lies in shared memory, a copy per warp: the loop over the tiles needs the registers.
+    PagedWalk& kept = *reinterpret_cast<PagedWalk*>(smem + SM::kWalk + (warp - 4) * 64);
+    static_assert(sizeof(PagedWalk) <= 64, "the walk's copy");
+    if (lane == 0) kept = wk;
+    __syncwarp();
+    while (any && ok) {
+      int t, t_end, t_step, la, le, k_base, my;                   // this slot's tiles, those seen whole, the tile counter's offset
+      bool single, second;
       PagedSees see{0x7fffffff, 0};
-      if (valid) see = paged_sees(a, wk.row0, wk.n, wk.L, wk.prefix, i);
+      bool valid;
+      int pos;
+      float slope2 = 0.f;
+      {
+        PagedWalk wk = kept;
+        __syncwarp();
+        if (!wk.next(a, seqs)) break;
+        const PmPlan pl = pm_plan(a, wk, lane);
+        single = pl.single;
+        second = single && pl.items(1) > 0;
+        my = pl.items(slot);
+        t = single ? pl.A + slot : slot ? pl.a1 : pl.a0;
+        t_end = single ? pl.E : slot ? pl.e1 : pl.e0;
+        t_step = single ? 2 : 1;
+        la = single || !slot ? pl.la0 : pl.la1;
+        le = single || !slot ? pl.le0 : pl.le1;
+        k_base = kt - pl.A;
+        kt += pl.E - pl.A;
+        const int i = wk.first_pos(a.w) + (single ? 0 : slot * ppos) + pi;
+        valid = row < ppos * G && i < wk.n;
+        if (valid) see = paged_sees(a, wk.row0, wk.n, wk.L, wk.prefix, i);
+        if (MODS && a.slopes && valid) slope2 = __ldg(a.slopes + wk.h * G + g) * kLog2e;
+        pos = wk.L - wk.n + i;
+        if (lane == 0) kept = wk;
+        __syncwarp();
+      }
       const bool live = __any_sync(0xffffffffu, valid);
       const int lo_most = __reduce_max_sync(0xffffffffu, valid ? see.lo : 0), hi_least = __reduce_min_sync(0xffffffffu, valid ? see.hi : 0x7fffffff);
-      float slope2 = 0.f;
-      if (MODS && a.slopes && valid) slope2 = __ldg(a.slopes + wk.h * G + g) * kLog2e;
-      const int pos = wk.L - wk.n + i;
       float m = -INFINITY, l = 0.f;
       int done_items = 0;
-      for (int t = pl.A; t < pl.E; ++t) {
-        const bool act0 = pl.act<0>(t), act1 = pl.act<1>(t);
-        if (!(slot ? act1 : act0)) { kt += act0 || act1; continue; }
-        const int tok0 = t * kPmKeys;
-        const bool look = slot ? pl.look<1>(t) : pl.look<0>(t);
+#pragma unroll 1
+      for (; t < t_end; t += t_step) {
+        const int tok0 = t * kPmKeys, st = (k_base + t) % NS;
+        const bool look = t < la || t >= le;
         bool simt = false;
         if (look) {
           // values of this tile: zeroed behind the end where they are not finite; elsewhere such a value makes the tile special
-          const int st = kt % NS;
-          if (!pm_wait(&v_full[st], (kt / NS) & 1, lim, abort_flag)) { ok = false; break; }
+          if (!pm_wait(&v_full[st], ((k_base + t) / NS) & 1, lim, abort_flag)) { ok = false; break; }
+          const int L = kept.L;
           bool bad = false;
           unsigned char* vt = smem + SM::kV + st * SM::kTile + row * 16;
 #pragma unroll 4
           for (int x = 0; x < SM::kTile / 2048; ++x) {             // 16-byte pieces: rows row / 8 + 16 x of either array
             const uint4 v = *reinterpret_cast<const uint4*>(vt + x * 2048);
             if (pair_not_finite(v.x) | pair_not_finite(v.y) | pair_not_finite(v.z) | pair_not_finite(v.w)) {
-              if (tok0 + (row >> 3) + 16 * (x & 7) >= wk.L) *reinterpret_cast<uint4*>(vt + x * 2048) = make_uint4(0u, 0u, 0u, 0u);
+              if (tok0 + (row >> 3) + 16 * (x & 7) >= L) *reinterpret_cast<uint4*>(vt + x * 2048) = make_uint4(0u, 0u, 0u, 0u);
               else bad = true;
             }
           }
@@ -476,7 +503,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           if (done_items > 0 && !pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) { ok = false; break; }
           if (done_items == 0 && n_used > 0 && !pm_wait(&o_free[slot], (n_used - 1) & 1, lim, abort_flag)) { ok = false; break; }
           tc_fence_after();
-          const unsigned char* vt = smem + SM::kV + (kt % NS) * SM::kTile;
+          const unsigned char* vt = smem + SM::kV + st * SM::kTile;
 #pragma unroll 1
           for (int c = 0; c < D; c += 16) {
             float acc[16];
@@ -523,11 +550,11 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         if (look && lane == 0 && (warp & 3) == 0) skip_pv[slot] = simt;
         if (lane == 0) mbar_arrive1(&p_ready[slot]);
         ++n;
-        ++kt;
         ++done_items;
       }
       if (!ok) break;
       // ------------------------------------------------------------ end of the segment ----------------------------------
+      const PagedWalk wk = kept;
       const bool whole = wk.head && wk.tail;
       if (my > 0) {
         if (!pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) { ok = false; break; }
@@ -535,7 +562,6 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         ++n_used;
       }
       float m1 = -INFINITY, l1 = 0.f;
-      const bool second = pl.single && pl.items(1) > 0;
       if (second) {
         if (slot == 1) {                                          // the second half's maxima and sums go to the first's warps, O stays where it is
           ml_s[row] = make_float2(m, l);
@@ -551,15 +577,16 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         }
         ++n_half;
       }
-      if (pl.single && slot == 1) continue;
+      if (single && slot == 1) continue;
       // O of both halves relative to the larger maximum; an empty half (no key seen) takes no part
       const float M = fmaxf(m, m1);
       const float f0 = l == 0.f ? 0.f : ex2(m - M), f1 = l1 == 0.f ? 0.f : ex2(m1 - M);
       const float sum = (l == 0.f ? 0.f : l * f0) + (l1 == 0.f ? 0.f : l1 * f1);
       const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
       const float w0 = f0 * inv, w1 = f1 * inv;
+      const int i = wk.first_pos(a.w) + (single ? 0 : slot * ppos) + pi;
       const long long out_row = (long long)(wk.row0 + i) * a.pl.Hq + wk.h * G + g;
-      const long long part_row = (2LL * blockIdx.x + (wk.head ? 1 : 0)) * a.w.rows + (pl.single ? 0 : slot * ppos * G) + row;
+      const long long part_row = (2LL * blockIdx.x + (wk.head ? 1 : 0)) * a.w.rows + (single ? 0 : slot * ppos * G) + row;
       if (live) {
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
