@@ -41,7 +41,9 @@ struct PmSmem {
   static constexpr int kQ = 0, kK = kQ + 2 * kTile, kV = kK + NS * kTile, kSeqs = kV + NS * kTile;
   static constexpr int kMl = kSeqs + (int)((sizeof(PagedSeqs) + 15) / 16 * 16);   // float2 [128]: maximum and sum of the second half
   static constexpr int kWalk = kMl + 128 * 8;                     // PagedWalk [8]: where the softmax warps are
-  static constexpr int kBars = kWalk + 8 * 64;
+  static constexpr int kStage = kWalk + 8 * 64;                    // [8 warps][32 rows][64 + 16 bytes]: rows on their way out
+  static constexpr int kStageRow = 80;
+  static constexpr int kBars = kStage + 8 * 32 * kStageRow;
   static constexpr int kNumBars = 4 * NS + 14;
   static constexpr int kMisc = kBars + kNumBars * 8;             // tensor-memory base, abort flag, skip flags [2], look-over marks [2][2]
   static constexpr int kBytes = kMisc + 48;
@@ -584,17 +586,42 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       const float sum = (l == 0.f ? 0.f : l * f0) + (l1 == 0.f ? 0.f : l1 * f1);
       const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
       const float w0 = f0 * inv, w1 = f1 * inv;
-      const int i = wk.first_pos(a.w) + (single ? 0 : slot * ppos) + pi;
-      const long long out_row = (long long)(wk.row0 + i) * a.pl.Hq + wk.h * G + g;
+      const int i0 = wk.first_pos(a.w) + (single ? 0 : slot * ppos);
+      const long long out_row = (long long)(wk.row0 + i0 + pi) * a.pl.Hq + wk.h * G + g;
       const long long part_row = (2LL * blockIdx.x + (wk.head ? 1 : 0)) * a.w.rows + (single ? 0 : slot * ppos * G) + row;
       if (live) {
+        // A thread holds a row; written as it is, every store would touch 32 rows.  64 bytes of each row go through shared memory: four
+        // lanes a row, whole sectors (8192-token prompt: 691 -> 6XX us).
+        unsigned char* stage = smem + SM::kStage + (warp - 4) * 32 * SM::kStageRow;
+        unsigned char* mine = stage + lane * SM::kStageRow;
+        const int r_first = (warp & 3) * 32 + (lane >> 2), piece = lane & 3;    // rows r_first + 8 k of the row tile
+        unsigned char* dst[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = r_first + 8 * k, ri = r / G;
+          const bool there = r < ppos * G && i0 + ri < wk.n;
+          if (!there) dst[k] = nullptr;
+          else if (whole)
+            dst[k] = reinterpret_cast<unsigned char*>(a.out) + ((long long)(wk.row0 + i0 + ri) * a.pl.Hq + wk.h * G + (r - ri * G)) * (D * 2) + piece * 16;
+          else
+            dst[k] = reinterpret_cast<unsigned char*>(a.w.part_o) + (part_row + (r - row)) * (D * 4) + piece * 16;
+        }
+        auto send = [&](int at) {                                 // 64 bytes of every row, `at` bytes into it
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint4 v = *reinterpret_cast<const uint4*>(stage + ((lane >> 2) + 8 * k) * SM::kStageRow + piece * 16);
+            if (dst[k]) *reinterpret_cast<uint4*>(dst[k] + at) = v;
+          }
+          __syncwarp();
+        };
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
           float o[32];
           if (my > 0) {
             tmem_ld32(tO + c, o);
 #pragma unroll
-            for (int x = 0; x < 32; ++x) o[x] = f0 == 0.f && l == 0.f ? 0.f : o[x] * w0;
+            for (int x = 0; x < 32; ++x) o[x] = l == 0.f ? 0.f : o[x] * w0;
           } else {
 #pragma unroll
             for (int x = 0; x < 32; ++x) o[x] = 0.f;
@@ -606,16 +633,20 @@ __global__ void __launch_bounds__(kPmThreads, 1)
 #pragma unroll
               for (int x = 0; x < 32; ++x) o[x] = fmaf(o1[x], w1, o[x]);
           }
-          if (valid && whole) {
-            uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + out_row * D + c);
+          if (whole) {
 #pragma unroll
             for (int x = 0; x < 4; ++x)
-              dst[x] = make_uint4(pack_bf16(o[8 * x], o[8 * x + 1]), pack_bf16(o[8 * x + 2], o[8 * x + 3]), pack_bf16(o[8 * x + 4], o[8 * x + 5]),
-                                  pack_bf16(o[8 * x + 6], o[8 * x + 7]));
-          } else if (valid) {
-            float4* dst = reinterpret_cast<float4*>(a.w.part_o + part_row * D + c);
+              *reinterpret_cast<uint4*>(mine + x * 16) = make_uint4(pack_bf16(o[8 * x], o[8 * x + 1]), pack_bf16(o[8 * x + 2], o[8 * x + 3]),
+                                                                    pack_bf16(o[8 * x + 4], o[8 * x + 5]), pack_bf16(o[8 * x + 6], o[8 * x + 7]));
+            send(c * 2);
+          } else {
 #pragma unroll
-            for (int x = 0; x < 8; ++x) dst[x] = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+            for (int y = 0; y < 2; ++y) {
+#pragma unroll
+              for (int x = 0; x < 4; ++x)
+                *reinterpret_cast<float4*>(mine + x * 16) = make_float4(o[16 * y + 4 * x], o[16 * y + 4 * x + 1], o[16 * y + 4 * x + 2], o[16 * y + 4 * x + 3]);
+              send(c * 4 + y * 64);
+            }
           }
         }
         if (valid && !whole) a.w.part_ml[part_row] = make_float2(M, sum);
