@@ -66,6 +66,7 @@ struct PagedWork {
   int ppos, upos, TK;
   int by_unit;                          // dealt out by units instead of tiles
   int n_cta, min_tiles;
+  int extra;                            // what starting and ending a unit costs, in tiles: counted before its first tile when the work is dealt out
   int rows;                             // rows that a partial result holds
   float* part_o;                        // [2 n_cta][rows][d]
   float2* part_ml;                      // [2 n_cta][rows]  maximum (base 2), sum
@@ -104,10 +105,11 @@ __device__ __forceinline__ PagedSpan paged_span(const PagedWork& w, int window, 
   const int lo = window > 0 ? max(0, p0 - window + 1) : 0, hi = min(L, max(p1 + 1, prefix));
   return PagedSpan{lo / w.TK, (hi + w.TK - 1) / w.TK};
 }
+// What a unit counts for: its tiles and `extra` (one, where whole units are dealt out).
 __device__ __forceinline__ int paged_unit_tiles(const PagedWork& w, int window, int n, int L, int prefix, int u) {
   if (w.by_unit) return 1;
   const PagedSpan s = paged_span(w, window, n, L, prefix, u);
-  return s.t1 - s.t0;
+  return s.t1 - s.t0 + w.extra;
 }
 
 // Fills the table; all threads of the CTA (whole warps), ends with a barrier.  Returns the total.
@@ -196,27 +198,30 @@ struct PagedWalk {
     return true;
   }
   __device__ __forceinline__ bool next(const PagedAttend& a, const PagedSeqs& t) {
-    if (left <= 0) return false;
-    if (u >= paged_units(a.w, n)) {                  // the unit before was its head's last
-      u = 0;
-      if (++h == a.pl.Hkv) {
-        h = 0;
-        do ++b; while (b < a.pb.batch - 1 && t.pre[b + 1] == t.pre[b]);
-        load(t);
+    do {
+      if (left <= 0) return false;
+      if (u >= paged_units(a.w, n)) {                // the unit before was its head's last
+        u = 0;
+        if (++h == a.pl.Hkv) {
+          h = 0;
+          do ++b; while (b < a.pb.batch - 1 && t.pre[b + 1] == t.pre[b]);
+          load(t);
+        }
       }
-    }
-    const PagedSpan s = paged_span(a.w, a.window, n, L, prefix, u);
-    if (a.w.by_unit) {
-      t0 = s.t0; t1 = s.t1; head = tail = true;
-      left -= 1;
-    } else {
-      t0 = s.t0 + off;
-      t1 = (int)min((long long)s.t1, t0 + left);
-      head = off == 0; tail = t1 == s.t1;
-      left -= t1 - t0;
-    }
-    off = 0;
-    u_cur = u++;
+      const PagedSpan s = paged_span(a.w, a.window, n, L, prefix, u);
+      if (a.w.by_unit) {
+        t0 = s.t0; t1 = s.t1; head = tail = true;
+        left -= 1;
+      } else {                                       // the share holds off .. upto of the unit's extra and tiles
+        const int upto = (int)min((long long)(s.t1 - s.t0 + a.w.extra), off + left);
+        left -= upto - off;
+        t0 = s.t0 + max(0, off - a.w.extra);
+        t1 = s.t0 + max(0, upto - a.w.extra);
+        head = t0 == s.t0; tail = t1 == s.t1;
+      }
+      off = 0;
+      u_cur = u++;
+    } while (t0 == t1);                              // (a share's last bit, too short for a tile: the next share starts the unit)
     return true;
   }
   int u_cur;                            // unit of the current segment

@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedAtt
   const int cut = blockIdx.x + 1;                                  // the border between shares cut - 1 and cut
   const long long at = cut * share;
   PagedWalk wk;
-  if (!wk.seek(a, seqs, at, 1) || wk.off == 0 || wk.off > share) return;   // no border inside a unit, or not the unit's first
+  if (!wk.seek(a, seqs, at, 1) || wk.off <= a.w.extra || wk.off - a.w.extra > share) return;   // no border between a unit's tiles, or not its first
   const int off = wk.off;
   wk.next(a, seqs);
   const int tiles = paged_unit_tiles(a.w, a.window, wk.n, wk.L, wk.prefix, wk.u_cur);
@@ -392,6 +392,7 @@ void paged_plan_general(PagedWork* w, const PagedBatch& pb, const PagedLayout& p
   constexpr int per_sm = 2;
   w->by_unit = tiles <= 4;
   w->min_tiles = w->by_unit ? 1 : 2;
+  w->extra = 0;
   const long long most_ctas = w->by_unit ? units : (units * tiles + w->min_tiles - 1) / w->min_tiles;
   w->n_cta = (int)(most_ctas < (long long)per_sm * sm_count ? most_ctas : (long long)per_sm * sm_count);
   w->rows = (pb.max_new < w->upos ? pb.max_new : w->upos) * pl.G;

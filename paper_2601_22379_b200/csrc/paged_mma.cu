@@ -691,6 +691,7 @@ void paged_plan_mma(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, i
   const long long tiles = (pb.max_len + w->TK - 1) / w->TK, units = (long long)pb.batch * pl.Hkv * paged_units(*w, pb.max_new);
   w->by_unit = tiles <= 4;
   w->min_tiles = w->by_unit ? 1 : 2;
+  w->extra = pb.max_new <= w->ppos ? 1 : 2;
   const long long most = w->by_unit ? units : (units * tiles + w->min_tiles - 1) / w->min_tiles;
   w->n_cta = (int)(most < sm_count ? most : sm_count);
   w->rows = (pb.max_new < w->upos ? pb.max_new : w->upos) * pl.G;
