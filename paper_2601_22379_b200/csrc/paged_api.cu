@@ -199,10 +199,10 @@ static PagedBatch part_of(PagedBatch b, int first) {
   return b;
 }
 
-// The queries as [token][head][half of 64 channels], boxes of G heads x 128 / G tokens: the rows of a row tile, in their order.
-static bool make_q_map(void* out128, const void* q, const PagedLayout& pl, int64_t q_stride, int64_t total) {
-  return make_tile_map_4d(out128, const_cast<void*>(q), 64u, (unsigned)(pl.d / 64), (unsigned)pl.Hq, (unsigned)total, 128ull, (unsigned long long)pl.d * 2,
-                          (unsigned long long)q_stride * 2, (unsigned)pl.G, (unsigned)(128 / pl.G));
+// The queries as [token][head][half of 64 channels], boxes of G heads x the tokens of a row tile: its rows, in their order.
+static bool make_q_map(void* out128, const void* q, const PagedLayout& pl, int64_t q_stride, const PagedBatch& pb) {
+  return make_tile_map_4d(out128, const_cast<void*>(q), 64u, (unsigned)(pl.d / 64), (unsigned)pl.Hq, (unsigned)pb.total_new, 128ull, (unsigned long long)pl.d * 2,
+                          (unsigned long long)q_stride * 2, (unsigned)pl.G, (unsigned)paged_mma_positions(pb, pl));
 }
 
 extern "C" int spla_paged_query_workspace(const spla_paged_t* p, const spla_paged_batch_t* batch, size_t* bytes_out) {
@@ -262,7 +262,7 @@ extern "C" int spla_paged_attend(spla_paged_t* p, const spla_paged_batch_t* batc
   cudaStream_t s = (cudaStream_t)stream;
   cudaError_t e = cudaSuccess;
   PagedMaps maps;
-  const bool tensor = p->tensor && aligned(q, 16) && q_stride % 8 == 0 && make_q_map(maps.q, q, p->pl, q_stride, batch->total_new);
+  const bool tensor = p->tensor && aligned(q, 16) && q_stride % 8 == 0 && make_q_map(maps.q, q, p->pl, q_stride, pb);
   if (tensor) {
     memcpy(maps.k, p->maps.k, sizeof(maps.k));
     memcpy(maps.v, p->maps.v, sizeof(maps.v));

@@ -6,7 +6,10 @@
 // of one KV head) are in work at a time, each with its own softmax warps and its own S and O in tensor memory, so that the tensor cores
 // work on one while the other is in its exponentials:
 //   - a unit of more than one row tile: two row tiles against the same key tile, K and V are read once for both;
-//   - a unit of one row tile (single tokens, short chunks): the same rows against key tiles in turn, the two halves merged at the end.
+//   - a unit of one row tile (short chunks): the same rows against key tiles in turn, the two halves merged at the end.
+// Launches whose units have at most 32 rows (single tokens, FEW) hold the rows four times, a copy for each softmax warp, which takes 32 of
+// the tile's 128 keys: its row of P has zeros elsewhere, its rows of O and l are sums over its keys, and the four are merged at the end.
+// One warp with all 128 keys of the rows would be the whole chain, with 8 cycles of the exponential unit per key (32 when scores are capped).
 // P takes the place of S in tensor memory, as the left operand of O += P V, rounded to bf16 (its sum l is of the unrounded values).
 // The maximum is a stale one: O is rescaled only when it grows by more than 2^8.
 //
@@ -32,21 +35,23 @@ constexpr int kPmThreads = 384;
 constexpr int kPmKeys = 128;                       // keys per tile
 constexpr uint32_t kPmTmemCols = 512;              // S0, S1, O0, O1: 128 columns each
 
-template <int D>
+template <int D, bool FEW>
 struct PmSmem {
   static constexpr int H = D / 64;                               // arrays of 128-byte rows per operand
   static constexpr int kHalf = kPmKeys * 128;
   static constexpr int kTile = H * kHalf;                        // one K or V tile, or the queries of a row tile
-  static constexpr int NS = D == 128 ? 2 : 4;                    // stages of K, and of V
-  static constexpr int kQ = 0, kK = kQ + 2 * kTile, kV = kK + NS * kTile, kSeqs = kV + NS * kTile;
-  static constexpr int kMl = kSeqs + (int)((sizeof(PagedSeqs) + 15) / 16 * 16);   // float2 [128]: maximum and sum of the second half
+  // stages: V is held until its softmax is through, K only until the scores; one row tile leaves room for another of V
+  static constexpr int NK = D == 128 ? 2 : 4, NV = (D == 128 ? 2 : 4) + (FEW ? (D == 128 ? 1 : 2) : 0);
+  static constexpr int kQ = 0, kK = kQ + (FEW ? 1 : 2) * kTile, kV = kK + NK * kTile, kSeqs = kV + NV * kTile;
+  static constexpr int kMl = kSeqs + (int)((sizeof(PagedSeqs) + 15) / 16 * 16);   // float2 [128]: maximum and sum of the second half, of a quarter
   static constexpr int kWalk = kMl + 128 * 8;                     // PagedWalk [8]: where the softmax warps are
-  static constexpr int kStage = kWalk + 8 * 64;                    // [8 warps][32 rows][64 + 16 bytes]: rows on their way out
-  static constexpr int kStageRow = 80;
-  static constexpr int kBars = kStage + 8 * 32 * kStageRow;
-  static constexpr int kNumBars = 4 * NS + 14;
+  static constexpr int kStage = kWalk + 8 * 64;                   // [8 warps][32 rows][64 + 16 bytes], FEW [4 warps][32 rows][128 + 16]: rows on their way out
+  static constexpr int kStageRow = FEW ? 144 : 80;
+  static constexpr int kBars = kStage + 8 * 32 * 80;
+  static constexpr int kNumBars = 2 * NK + 2 * NV + 15;
   static constexpr int kMisc = kBars + kNumBars * 8;             // tensor-memory base, abort flag, skip flags [2], look-over marks [2][2]
   static constexpr int kBytes = kMisc + 48;
+  static_assert(4 * 32 * 144 <= 8 * 32 * 80, "rows on their way out");
   static_assert(kBytes <= 227 * 1024, "shared memory of the paged attention kernel");
 };
 
@@ -158,17 +163,17 @@ __device__ __forceinline__ uint32_t bits_between(int a, int e) {
 }
 __device__ __forceinline__ uint32_t pair_not_finite(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 
-template <int D, bool MODS>
+template <int D, bool MODS, bool FEW>
 __global__ void __launch_bounds__(kPmThreads, 1)
     paged_mma_kernel(const PagedAttend a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                      const __grid_constant__ CUtensorMap map_q) {
-  using SM = PmSmem<D>;
-  constexpr int H = SM::H, NS = SM::NS;
+  using SM = PmSmem<D, FEW>;
+  constexpr int H = SM::H, NK = SM::NK, NV = SM::NV;
   extern __shared__ __align__(1024) unsigned char smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + SM::kBars);
-  uint64_t *k_full = bars, *k_empty = k_full + NS, *v_full = k_empty + NS, *v_empty = v_full + NS, *q_full = v_empty + NS, *q_empty = q_full + 1,
+  uint64_t *k_full = bars, *k_empty = k_full + NK, *v_full = k_empty + NK, *v_empty = v_full + NV, *q_full = v_empty + NV, *q_empty = q_full + 1,
            *s_full = q_empty + 1, *p_ready = s_full + 2, *pv_done = p_ready + 2, *o_free = pv_done + 2, *scanned = o_free + 2, *halves = scanned + 2,
-           *done = halves + 1;
+           *quarters = halves + 1, *done = quarters + 1;
   uint32_t* tmem_base_s = reinterpret_cast<uint32_t*>(smem + SM::kMisc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SM::kMisc + 4);
   volatile int* skip_pv = reinterpret_cast<volatile int*>(smem + SM::kMisc + 8);    // [2]: this product with V has been formed by the softmax warps
@@ -178,10 +183,8 @@ __global__ void __launch_bounds__(kPmThreads, 1)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wg = warp >> 2;
 
   if (tid == 0) {
-    for (int s = 0; s < NS; ++s) {
-      mbar_init(&k_full[s], 1);  mbar_init(&k_empty[s], 1);
-      mbar_init(&v_full[s], 1);  mbar_init(&v_empty[s], 1);
-    }
+    for (int s = 0; s < NK; ++s) { mbar_init(&k_full[s], 1);  mbar_init(&k_empty[s], 1); }
+    for (int s = 0; s < NV; ++s) { mbar_init(&v_full[s], 1);  mbar_init(&v_empty[s], 1); }
     mbar_init(q_full, 1);
     mbar_init(q_empty, 1);
     for (int s = 0; s < 2; ++s) {
@@ -192,6 +195,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       found_bad[2 * s] = found_bad[2 * s + 1] = 0;
     }
     mbar_init(halves, 4);
+    mbar_init(quarters, 4);
     mbar_init(done, 1);
     mbar_init_done();
     *abort_flag = 0;
@@ -217,6 +221,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
     if ((warp == 0 || warp == 2) && any) {
       // ------------------------------------------------------------ TMA: queries and K, or V ----------------------------
       const bool is_k = warp == 0;
+      const int NS = is_k ? NK : NV;
       const int P = a.pl.P, npg = kPmKeys / P, boxes = npg * H, pg = lane / H, hh = lane % H;
       const uint32_t dst = sbase + (is_k ? SM::kK : SM::kV) + hh * SM::kHalf + pg * P * 128;
       const CUtensorMap* map = is_k ? &map_k : &map_v;
@@ -239,10 +244,12 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           if (seg > 0 && !pm_wait(q_empty, (seg - 1) & 1, lim, abort_flag)) { ok = false; break; }
           if (lane == 0) {
             const bool two = !pl.single && pl.items(1) > 0;
-            mbar_expect_tx(q_full, (two ? 2 : 1) * H * ppos * G * 128 + (uint32_t)a.dbg_tx_extra);
-            for (int s = 0; s < (two ? 2 : 1); ++s)
+            const int boxes_q = FEW ? 4 : two ? 2 : 1;             // (four copies of the same rows, or the row tiles)
+            mbar_expect_tx(q_full, boxes_q * H * ppos * G * 128 + (uint32_t)a.dbg_tx_extra);
+            for (int s = 0; s < boxes_q; ++s)
               for (int x = 0; x < H; ++x)
-                tma_load_q(sbase + SM::kQ + s * SM::kTile + x * SM::kHalf, &map_q, x, wk.h * G, wk.row0 + wk.first_pos(a.w) + s * ppos, q_full);
+                tma_load_q(sbase + SM::kQ + s * (FEW ? 32 * 128 : SM::kTile) + x * SM::kHalf, &map_q, x, wk.h * G,
+                           wk.row0 + wk.first_pos(a.w) + (FEW ? 0 : s * ppos), q_full);
           }
         }
         ++seg;
@@ -269,7 +276,8 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       const uint32_t one = elect_one();                           // (the whole warp runs this loop: see umma_ss_one)
       const uint32_t q_lo = umma_desc_lo(sbase + SM::kQ, 16), k_lo = umma_desc_lo(sbase + SM::kK, 16), v_lo = umma_desc_lo(sbase + SM::kV, SM::kHalf);
       bool ok = true;
-      int kt = 0, seg = 0;
+      uint32_t kt = 0;
+      int seg = 0;
       uint32_t n_p0 = 0, n_p1 = 0, n_o0 = 0, n_o1 = 0;            // items whose P was awaited, segments that used O
       // the item of either row tile whose product with V is to come: its stage and phase, whether it is the segment's first, whether
       // V is free after it, whether the softmax warps may have formed it
@@ -300,17 +308,17 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       };
       constexpr std::integral_constant<int, 0> s0{};
       constexpr std::integral_constant<int, 1> s1{};
-      auto score = [&](auto slot_c, const PmPlan& pl, int t, int st, uint32_t ph, bool last) {   // S = Q K^T
+      auto score = [&](auto slot_c, const PmPlan& pl, int t, bool last) {   // S = Q K^T
         constexpr int S = decltype(slot_c)::value;
         if (S ? pend1 : pend0) product(slot_c);                   // (S takes the place of the P before)
-        const uint32_t q = q_lo + (pl.single ? 0 : S * (SM::kTile / 16)), k = k_lo + st * (SM::kTile / 16);
+        const uint32_t q = q_lo + (FEW || pl.single ? 0 : S * (SM::kTile / 16)), k = k_lo + kt % NK * (SM::kTile / 16);
 #pragma unroll
         for (int x = 0; x < H; ++x) umma_ss4_one<2, 2>(one, tmem + S * 128, q + x * (SM::kHalf / 16), k + x * (SM::kHalf / 16), id_s, x > 0);
         umma_commit_one(one, &s_full[S]);
-        if (last) umma_commit_one(one, &k_empty[st]);
+        if (last) umma_commit_one(one, &k_empty[kt % NK]);
         (S ? pend1 : pend0) = true;
-        (S ? st1 : st0) = st;
-        (S ? ph1 : ph0) = ph;
+        (S ? st1 : st0) = kt % NV;
+        (S ? ph1 : ph0) = (kt / NV) & 1;
         (S ? free1 : free0) = last;
         (S ? look1 : look0) = pl.template look<S>(t);
       };
@@ -323,22 +331,20 @@ __global__ void __launch_bounds__(kPmThreads, 1)
 #pragma unroll 1
         for (int t = pl.A; t < pl.E; ++t) {
           const bool act0 = pl.act<0>(t), act1 = pl.act<1>(t);
-          const int st = kt % NS;
-          const uint32_t ph = (kt / NS) & 1;
-          if (!pm_wait(&k_full[st], ph, lim, abort_flag)) { ok = false; break; }
+          if (!pm_wait(&k_full[kt % NK], (kt / NK) & 1, lim, abort_flag)) { ok = false; break; }
           tc_fence_after();
           if (act0) {
-            score(s0, pl, t, st, ph, !act1);
+            score(s0, pl, t, !act1);
             if (ok && pend1) product(s1);
           }
           if (ok && act1) {
-            score(s1, pl, t, st, ph, true);
+            score(s1, pl, t, true);
             if (ok && pend0) product(s0);
           }
           if (ok && !act0 && !act1) {                             // (between the two row tiles' documents)
-            if (!pm_wait(&v_full[st], ph, lim, abort_flag)) ok = false;
-            umma_commit_one(one, &k_empty[st]);
-            umma_commit_one(one, &v_empty[st]);
+            if (!pm_wait(&v_full[kt % NV], (kt / NV) & 1, lim, abort_flag)) ok = false;
+            umma_commit_one(one, &k_empty[kt % NK]);
+            umma_commit_one(one, &v_empty[kt % NV]);
           }
           if (!ok) break;
           ++kt;
@@ -355,12 +361,14 @@ __global__ void __launch_bounds__(kPmThreads, 1)
   } else {
     // -------------------------------------------------------------- softmax and epilogue: one row per thread -------------
     warpgroup_reg_inc<192>();
-    const int slot = wg - 1, row = tid - 128 * wg, pi = row / G, g = row % G;
+    const int slot = wg - 1, thr = tid - 128 * wg, row = FEW ? lane : thr, pi = row / G, g = row % G;
+    constexpr int KEYS = FEW ? 32 : kPmKeys;                      // keys of a tile that a thread takes
+    const int kb = FEW ? 32 * (warp & 3) : 0;                     // the first of them
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + slot * 128 + lane_off, tO = tmem + 256 + slot * 128 + lane_off;
     const float sc2 = a.sm_scale * kLog2e;
     bool ok = true;
-    int kt = 0, n = 0, n_scan = 0, n_half = 0, n_used = 0;        // tiles of the CTA, items of this slot, look-overs, merged segments, segments that used O
+    int kt = 0, n = 0, n_scan = 0, n_half = 0, n_quarter = 0, n_used = 0;   // tiles of the CTA, items of this slot, look-overs, merges, segments that used O
     // The walk lies in shared memory, a copy per warp: the loop over the tiles needs the registers.
     PagedWalk& kept = *reinterpret_cast<PagedWalk*>(smem + SM::kWalk + (warp - 4) * 64);
     static_assert(sizeof(PagedWalk) <= 64, "the walk's copy");
@@ -402,20 +410,23 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       int done_items = 0;
 #pragma unroll 1
       for (; t < t_end; t += t_step) {
-        const int tok0 = t * kPmKeys, st = (k_base + t) % NS;
+        const int tok0 = t * kPmKeys, st = (uint32_t)(k_base + t) % NV;
         const bool look = t < la || t >= le;
         bool simt = false;
+        if (!pm_wait(&s_full[slot], n & 1, lim, abort_flag)) { ok = false; break; }
         if (look) {
-          // values of this tile: zeroed behind the end where they are not finite; elsewhere such a value makes the tile special
-          if (!pm_wait(&v_full[st], ((k_base + t) / NS) & 1, lim, abort_flag)) { ok = false; break; }
+          // (After the scores: they follow the row tile's product before, which waited for the V tiles up to two before this one, so that
+          // the parity below can only mean this one.)
+          // Values of this tile: zeroed behind the end where they are not finite; elsewhere such a value makes the tile special
+          if (!pm_wait(&v_full[st], ((uint32_t)(k_base + t) / NV) & 1, lim, abort_flag)) { ok = false; break; }
           const int L = kept.L;
           bool bad = false;
-          unsigned char* vt = smem + SM::kV + st * SM::kTile + row * 16;
+          unsigned char* vt = smem + SM::kV + st * SM::kTile + thr * 16;
 #pragma unroll 4
-          for (int x = 0; x < SM::kTile / 2048; ++x) {             // 16-byte pieces: rows row / 8 + 16 x of either array
+          for (int x = 0; x < SM::kTile / 2048; ++x) {             // 16-byte pieces: rows thr / 8 + 16 x of either array
             const uint4 v = *reinterpret_cast<const uint4*>(vt + x * 2048);
             if (pair_not_finite(v.x) | pair_not_finite(v.y) | pair_not_finite(v.z) | pair_not_finite(v.w)) {
-              if (tok0 + (row >> 3) + 16 * (x & 7) >= L) *reinterpret_cast<uint4*>(vt + x * 2048) = make_uint4(0u, 0u, 0u, 0u);
+              if (tok0 + (thr >> 3) + 16 * (x & 7) >= L) *reinterpret_cast<uint4*>(vt + x * 2048) = make_uint4(0u, 0u, 0u, 0u);
               else bad = true;
             }
           }
@@ -428,32 +439,37 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           simt = __any_sync(0xffffffffu, found_bad[mark] == n_scan + 1);
           ++n_scan;
         }
-        if (!pm_wait(&s_full[slot], n & 1, lim, abort_flag)) { ok = false; break; }
         tc_fence_after();
         if (live) {
-          const bool part = tok0 < lo_most || tok0 + kPmKeys > hi_least;   // (warp-uniform)
+          const int key0 = tok0 + kb;
+          const bool part = key0 < lo_most || key0 + KEYS > hi_least;     // (warp-uniform)
           const float mul = MODS ? 1.f : sc2;
-          uint32_t r[kPmKeys];
-          tmem_ld128(tS, r);
+          uint32_t r[KEYS];
+          if constexpr (FEW) {
+            tmem_ld32_async(tS + kb, r);
+            tmem_ld_wait32(r);
+          } else {
+            tmem_ld128(tS, r);
+          }
           if constexpr (MODS) {
             if (a.softcap > 0.f) {                                // cap tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap)), in base 2
               const float k1 = 2.f * sc2 / a.softcap, c2 = a.softcap * kLog2e;
 #pragma unroll
-              for (int x = 0; x < kPmKeys; ++x) r[x] = __float_as_uint(fmaf(-2.f * c2, rcp_approx(1.f + ex2(__uint_as_float(r[x]) * k1)), c2));
+              for (int x = 0; x < KEYS; ++x) r[x] = __float_as_uint(fmaf(-2.f * c2, rcp_approx(1.f + ex2(__uint_as_float(r[x]) * k1)), c2));
             } else {
 #pragma unroll
-              for (int x = 0; x < kPmKeys; ++x) r[x] = __float_as_uint(__uint_as_float(r[x]) * sc2);
+              for (int x = 0; x < KEYS; ++x) r[x] = __float_as_uint(__uint_as_float(r[x]) * sc2);
             }
             if (a.slopes) {
-              const float d0 = (float)(tok0 - pos);
+              const float d0 = (float)(key0 - pos);
 #pragma unroll
-              for (int x = 0; x < kPmKeys; ++x) r[x] = __float_as_uint(fmaf(-slope2, fabsf(d0 + (float)x), __uint_as_float(r[x])));
+              for (int x = 0; x < KEYS; ++x) r[x] = __float_as_uint(fmaf(-slope2, fabsf(d0 + (float)x), __uint_as_float(r[x])));
             }
           }
           if (part) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const uint32_t bits = bits_between(see.lo - tok0 - 32 * c, see.hi - tok0 - 32 * c);
+            for (int c = 0; c < KEYS / 32; ++c) {
+              const uint32_t bits = bits_between(see.lo - key0 - 32 * c, see.hi - key0 - 32 * c);
 #pragma unroll
               for (int x = 0; x < 32; ++x)
                 if (!(bits & (1u << x))) r[32 * c + x] = 0xff800000u;
@@ -461,7 +477,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           }
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int x = 0; x < kPmKeys; x += 2) mx[x / 2 & 3] = fmaxf(mx[x / 2 & 3], fmaxf(__uint_as_float(r[x]), __uint_as_float(r[x + 1])));
+          for (int x = 0; x < KEYS; x += 2) mx[x / 2 & 3] = fmaxf(mx[x / 2 & 3], fmaxf(__uint_as_float(r[x]), __uint_as_float(r[x + 1])));
           const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * mul;
           // The first visible keys of a row set its maximum (its row of O is zero so far); later ones only move it when it would
           // let a probability exceed 2^8.
@@ -486,7 +502,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           const float nm = m == -INFINITY ? 0.f : -m;
           float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < KEYS / 32; ++c) {
             uint32_t pk[16];
 #pragma unroll
             for (int x = 0; x < 16; ++x) {
@@ -495,7 +511,14 @@ __global__ void __launch_bounds__(kPmThreads, 1)
               if (x & 1) sum1 = __fadd2_rn(sum1, p); else sum0 = __fadd2_rn(sum0, p);
               pk[x] = pack_bf16(p.x, p.y);
             }
-            tmem_st16(tS + 16 * c, pk);
+            tmem_st16(tS + kb / 2 + 16 * c, pk);
+          }
+          if constexpr (FEW) {                                    // the keys of the other warps
+            uint32_t zero[16];
+#pragma unroll
+            for (int x = 0; x < 16; ++x) zero[x] = 0u;
+#pragma unroll
+            for (int c = 1; c < 4; ++c) tmem_st16(tS + (((warp & 3) + c) & 3) * 16, zero);
           }
           l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
           tmem_st_wait();
@@ -512,7 +535,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
 #pragma unroll
             for (int x = 0; x < 16; ++x) acc[x] = 0.f;
 #pragma unroll 1
-            for (int w = 0; w < 4; ++w) {
+            for (int w = FEW ? kb / 32 : 0; w < (FEW ? kb / 32 + 1 : 4); ++w) {
               uint32_t pw[16];
               tmem_ld16_async(tS + 16 * w, pw);
               tmem_ld_wait16(pw);
@@ -566,14 +589,14 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       float m1 = -INFINITY, l1 = 0.f;
       if (second) {
         if (slot == 1) {                                          // the second half's maxima and sums go to the first's warps, O stays where it is
-          ml_s[row] = make_float2(m, l);
+          ml_s[thr] = make_float2(m, l);
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive1(halves);
         } else {
           if (!pm_wait(halves, n_half & 1, lim, abort_flag)) { ok = false; break; }
           tc_fence_after();
-          const float2 o = ml_s[row];
+          const float2 o = ml_s[thr];
           m1 = o.x;
           l1 = o.y;
         }
@@ -581,17 +604,90 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       }
       if (single && slot == 1) continue;
       // O of both halves relative to the larger maximum; an empty half (no key seen) takes no part
-      const float M = fmaxf(m, m1);
-      const float f0 = l == 0.f ? 0.f : ex2(m - M), f1 = l1 == 0.f ? 0.f : ex2(m1 - M);
-      const float sum = (l == 0.f ? 0.f : l * f0) + (l1 == 0.f ? 0.f : l1 * f1);
+      float M = fmaxf(m, m1);
+      float f0 = l == 0.f ? 0.f : ex2(m - M), f1 = l1 == 0.f ? 0.f : ex2(m1 - M);
+      float sum = (l == 0.f ? 0.f : l * f0) + (l1 == 0.f ? 0.f : l1 * f1);
+      if constexpr (FEW) {                                        // ... and of the four warps' keys
+        ml_s[thr] = make_float2(M, sum);
+        __syncwarp();
+        if (lane == 0) mbar_arrive1(quarters);
+        if (!pm_wait(quarters, n_quarter & 1, lim, abort_flag)) { ok = false; break; }
+        ++n_quarter;
+        float top = -INFINITY, all = 0.f;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) top = fmaxf(top, ml_s[32 * x + lane].x);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float2 o = ml_s[32 * x + lane];
+          if (o.y != 0.f) all = fmaf(o.y, ex2(o.x - top), all);
+        }
+        const float f = sum == 0.f ? 0.f : ex2(M - top);
+        f0 *= f;
+        f1 *= f;
+        M = top;
+        sum = all;
+      }
       const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
       const float w0 = f0 * inv, w1 = f1 * inv;
       const int i0 = wk.first_pos(a.w) + (single ? 0 : slot * ppos);
       const long long out_row = (long long)(wk.row0 + i0 + pi) * a.pl.Hq + wk.h * G + g;
       const long long part_row = (2LL * blockIdx.x + (wk.head ? 1 : 0)) * a.w.rows + (single ? 0 : slot * ppos * G) + row;
-      if (live) {
+      if constexpr (FEW) {
+        // 32 columns of every row at a time from the four warps to shared memory; then a row by four threads, 8 columns each
+        unsigned char* stage = smem + SM::kStage;
+        const int r = thr >> 2, piece = thr & 3, ri = r / G;
+        const bool there = r < ppos * G && i0 + ri < wk.n;
+        const long long o_row = (long long)(wk.row0 + i0 + ri) * a.pl.Hq + wk.h * G + (r - ri * G);
+#pragma unroll 1
+        for (int c = 0; c < D && ok; c += 32) {
+          float o[32], o1[32];
+          if (my > 0) tmem_ld32(tO + c, o);
+          if (second) tmem_ld32(tO + 128 + c, o1);
+          if (valid) {
+#pragma unroll
+            for (int x = 0; x < 32; ++x) {
+              const float y = my > 0 && l != 0.f ? o[x] * w0 : 0.f;
+              o[x] = second && l1 != 0.f ? fmaf(o1[x], w1, y) : y;
+            }
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+              *reinterpret_cast<float4*>(stage + ((warp & 3) * 32 + lane) * SM::kStageRow + x * 16) = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive1(quarters);
+          if (!pm_wait(quarters, n_quarter & 1, lim, abort_flag)) { ok = false; break; }
+          ++n_quarter;
+          if (there) {
+            float4 v0 = make_float4(0.f, 0.f, 0.f, 0.f), v1 = v0;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const float4 a0 = *reinterpret_cast<const float4*>(stage + (x * 32 + r) * SM::kStageRow + piece * 32);
+              const float4 a1 = *reinterpret_cast<const float4*>(stage + (x * 32 + r) * SM::kStageRow + piece * 32 + 16);
+              v0.x += a0.x; v0.y += a0.y; v0.z += a0.z; v0.w += a0.w;
+              v1.x += a1.x; v1.y += a1.y; v1.z += a1.z; v1.w += a1.w;
+            }
+            if (whole) {
+              *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + o_row * D + c + piece * 8) =
+                  make_uint4(pack_bf16(v0.x, v0.y), pack_bf16(v0.z, v0.w), pack_bf16(v1.x, v1.y), pack_bf16(v1.z, v1.w));
+            } else {
+              float4* dst = reinterpret_cast<float4*>(a.w.part_o + (part_row + (r - row)) * D + c + piece * 8);
+              dst[0] = v0;
+              dst[1] = v1;
+            }
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive1(quarters);                  // (the next columns take the same place)
+          if (!pm_wait(quarters, n_quarter & 1, lim, abort_flag)) { ok = false; break; }
+          ++n_quarter;
+        }
+        if (!ok) break;
+        if (valid && (warp & 3) == 0) {
+          if (!whole) a.w.part_ml[part_row] = make_float2(M, sum);
+          else if (a.lse) a.lse[out_row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+        }
+      } else if (live) {
         // A thread holds a row; written as it is, every store would touch 32 rows.  64 bytes of each row go through shared memory: four
-        // lanes a row, whole sectors (8192-token prompt: 691 -> 6XX us).
+        // lanes a row, whole sectors (8192-token prompt: 691 -> 653 us).
         unsigned char* stage = smem + SM::kStage + (warp - 4) * 32 * SM::kStageRow;
         unsigned char* mine = stage + lane * SM::kStageRow;
         const int r_first = (warp & 3) * 32 + (lane >> 2), piece = lane & 3;    // rows r_first + 8 k of the row tile
@@ -673,25 +769,35 @@ __global__ void __launch_bounds__(kPmThreads, 1)
   }
 }
 
+template <int D, bool MODS, bool FEW>
+cudaError_t mma_launch(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
+  auto kern = paged_mma_kernel<D, MODS, FEW>;
+  constexpr int bytes = PmSmem<D, FEW>::kBytes;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e != cudaSuccess) return e;
+  return launch_ex(kern, dim3(a.w.n_cta), dim3(kPmThreads), bytes, s, 0, true, a, *reinterpret_cast<const CUtensorMap*>(maps.k),
+                   *reinterpret_cast<const CUtensorMap*>(maps.v), *reinterpret_cast<const CUtensorMap*>(maps.q));
+}
 template <int D>
 cudaError_t mma_d(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
-  auto kern = a.softcap > 0.f || a.slopes ? paged_mma_kernel<D, true> : paged_mma_kernel<D, false>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, PmSmem<D>::kBytes);
-  if (e != cudaSuccess) return e;
-  return launch_ex(kern, dim3(a.w.n_cta), dim3(kPmThreads), PmSmem<D>::kBytes, s, 0, true, a, *reinterpret_cast<const CUtensorMap*>(maps.k),
-                   *reinterpret_cast<const CUtensorMap*>(maps.v), *reinterpret_cast<const CUtensorMap*>(maps.q));
+  const bool mods = a.softcap > 0.f || a.slopes, few = a.w.ppos * a.pl.G <= 32;
+  if (few) return mods ? mma_launch<D, true, true>(a, maps, s) : mma_launch<D, false, true>(a, maps, s);
+  return mods ? mma_launch<D, true, false>(a, maps, s) : mma_launch<D, false, false>(a, maps, s);
 }
 
 }  // namespace
 
+int paged_mma_positions(const PagedBatch& pb, const PagedLayout& pl) { return (pb.max_new * pl.G <= 32 ? 32 : 128) / pl.G; }
+
 void paged_plan_mma(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int window, int sm_count) {
-  w->ppos = 128 / pl.G;
-  w->upos = 2 * w->ppos;
+  w->ppos = paged_mma_positions(pb, pl);
+  const bool few = w->ppos * pl.G <= 32;
+  w->upos = (few ? 1 : 2) * w->ppos;
   w->TK = kPmKeys;
   const long long tiles = (pb.max_len + w->TK - 1) / w->TK, units = (long long)pb.batch * pl.Hkv * paged_units(*w, pb.max_new);
   w->by_unit = tiles <= 4;
   w->min_tiles = w->by_unit ? 1 : 2;
-  w->extra = pb.max_new <= w->ppos ? 1 : 2;
+  w->extra = few ? 1 : 2;
   const long long most = w->by_unit ? units : (units * tiles + w->min_tiles - 1) / w->min_tiles;
   w->n_cta = (int)(most < sm_count ? most : sm_count);
   w->rows = (pb.max_new < w->upos ? pb.max_new : w->upos) * pl.G;
