@@ -324,7 +324,7 @@ int spla_rope_destroy(spla_rope_t *rope);   /* NULL is allowed */
 typedef struct {
   const void *in;                        /* DEVICE, aligned to its element */
   void *out;                             /* DEVICE; equal to `in` with equal strides (in place), else not overlapping it */
-  int32_t n_heads;
+  int32_t n_heads;                       /* 1..4096 */
   int64_t in_batch, in_token, in_head;   /* strides in elements */
   int64_t out_batch, out_token, out_head;
 } spla_rope_tensor_t;
@@ -340,7 +340,7 @@ int spla_rope_apply(const spla_rope_t *rope, const int32_t *positions, int32_t b
                     const spla_rope_tensor_t *q, const spla_rope_tensor_t *k, int32_t dtype, int32_t transpose, void *stream);
 
 typedef struct {
-  int32_t n_q_heads;     /* H_q */
+  int32_t n_q_heads;     /* H_q <= 4096 */
   int32_t n_kv_heads;    /* H_kv; G = H_q / H_kv must be an integer in [1, 16] */
   int32_t head_dim;      /* d: 64 or 128 */
   int32_t page_size;     /* P: 16, 32, 64 or 128 tokens */

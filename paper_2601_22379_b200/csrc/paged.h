@@ -7,6 +7,7 @@
 namespace spla {
 
 constexpr int kRopeMaxPairs = 128;
+constexpr int kRopeMaxHeads = 4096;     // of one tensor
 
 // Frequencies as 64-bit fractions of a turn: position x frequency wraps at whole turns by itself, so that what is left for
 // the sine and cosine is the exact angle modulo a turn, at any position.

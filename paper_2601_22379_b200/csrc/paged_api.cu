@@ -75,12 +75,12 @@ extern "C" int spla_rope_destroy(spla_rope_t* rope) {
 }
 
 // One group of heads of spla_rope_apply.
-static int rope_group(const spla_rope_tensor_t* t, int dim, int dtype, RopeGroup* g) {
+static int rope_group(const spla_rope_tensor_t* t, int dtype, RopeGroup* g) {
   if (!t->in || !t->out || t->n_heads < 1) return SPLA_ERR_INVALID_ARG;
+  if (t->n_heads > kRopeMaxHeads) return SPLA_ERR_UNSUPPORTED;
   const size_t e = dtype_bytes(dtype);
   if (!aligned(t->in, e) || !aligned(t->out, e)) return SPLA_ERR_INVALID_ARG;
   if (t->in == t->out && (t->in_batch != t->out_batch || t->in_token != t->out_token || t->in_head != t->out_head)) return SPLA_ERR_INVALID_ARG;
-  (void)dim;
   *g = RopeGroup{t->in, t->out, t->n_heads, 1, t->in_batch, t->in_token, t->in_head, t->out_batch, t->out_token, t->out_head, dtype == SPLA_F32};
   return SPLA_OK;
 }
@@ -89,8 +89,8 @@ extern "C" int spla_rope_apply(const spla_rope_t* rope, const int32_t* positions
                                const spla_rope_tensor_t* q, const spla_rope_tensor_t* k, int32_t dtype, int32_t transpose, void* stream) {
   if (!rope || !positions || !q || batch < 1 || n_tokens < 1 || !is_dtype(dtype) || !aligned(positions, 4)) return SPLA_ERR_INVALID_ARG;
   RopeGroup g[2];
-  int rc = rope_group(q, rope->t.dim, dtype, &g[0]);
-  if (rc == SPLA_OK && k) rc = rope_group(k, rope->t.dim, dtype, &g[1]);
+  int rc = rope_group(q, dtype, &g[0]);
+  if (rc == SPLA_OK && k) rc = rope_group(k, dtype, &g[1]);
   if (rc != SPLA_OK) return rc;
   cudaError_t e = launch_rope(rope->t, positions, batch, n_tokens, g, k ? 2 : 1, nullptr, nullptr, nullptr, nullptr, transpose != 0, (cudaStream_t)stream);
   return e == cudaSuccess ? SPLA_OK : cuda_fail(e, "spla_rope_apply");
@@ -107,7 +107,7 @@ extern "C" int spla_paged_create(const spla_paged_config_t* c, void* k_pages, vo
   const int G = c->n_q_heads / c->n_kv_heads, P = c->page_size;
   if (G > kMaxGroup || (c->head_dim != 64 && c->head_dim != 128)) return SPLA_ERR_UNSUPPORTED;
   if (P != 16 && P != 32 && P != 64 && P != 128) return SPLA_ERR_UNSUPPORTED;
-  if (c->n_kv_heads > 65535) return SPLA_ERR_UNSUPPORTED;
+  if (c->n_q_heads > kRopeMaxHeads) return SPLA_ERR_UNSUPPORTED;
   const int64_t hs = c->head_stride ? c->head_stride : P, ps = c->page_stride ? c->page_stride : (int64_t)c->n_kv_heads * P;
   if (hs < P || ps < P) return SPLA_ERR_INVALID_ARG;                               // rows of neighbouring heads or pages would overlap
   if (ps >= (1ll << 31) || hs >= (1ll << 31)) return SPLA_ERR_UNSUPPORTED;

@@ -21,6 +21,7 @@ struct RopeLaunch {
   int batch, tokens, tb;                 // tb: tokens per block
   int heads, rows_per_y;                 // (token, head) rows of a block are shared by the grid's y blocks
   int pieces;                            // pieces of a head = threads side by side
+  unsigned head_magic;                   // ceil(2^32 / heads): row / heads = high word of row x magic (rows x heads is far below 2^32)
   int transpose;
   int paged;
   PagedBatch pb;
@@ -28,26 +29,23 @@ struct RopeLaunch {
   void *k_pages, *v_pages;
 };
 
-template <int VEC>
-__device__ __forceinline__ void load_piece(const float* p, float (&x)[VEC]) {
-  if constexpr (VEC == 4) {
-    const float4 v = *reinterpret_cast<const float4*>(p);
-    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) x[i] = p[i];
-  }
+// VEC channels as they lie: VEC x sizeof(T) = 16 bytes, or one channel.
+__device__ __forceinline__ void load_raw(const void* p, uint32_t (&w)[4]) {
+  const uint4 v = *reinterpret_cast<const uint4*>(p);
+  w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
 }
-template <int VEC>
-__device__ __forceinline__ void load_piece(const __nv_bfloat16* p, float (&x)[VEC]) {
-  if constexpr (VEC == 8) {
-    const uint4 v = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+__device__ __forceinline__ void load_raw(const float* p, uint32_t (&w)[1]) { w[0] = *reinterpret_cast<const uint32_t*>(p); }
+__device__ __forceinline__ void load_raw(const __nv_bfloat16* p, uint32_t (&w)[1]) { w[0] = *reinterpret_cast<const uint16_t*>(p); }
+template <typename T, int VEC, int W>
+__device__ __forceinline__ void unpack(const uint32_t (&w)[W], float (&x)[VEC]) {
+  if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
+    for (int i = 0; i < VEC; ++i) x[i] = __uint_as_float(w[i]);
+  } else if constexpr (VEC == 1) {
+    x[0] = bf16_lo(w[0]);
   } else {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) x[i] = __bfloat162float(p[i]);
+    for (int i = 0; i < VEC; ++i) x[i] = i % 2 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
   }
 }
 template <int VEC>
@@ -84,58 +82,56 @@ __device__ __forceinline__ float2 turn_of(unsigned long long freq, int position,
 // VEC pairs per piece; both element types may occur in one launch with VEC = 1 only.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kRopeThreads)
-    rope_kernel(const RopeLaunch r, const __grid_constant__ RopeTable rt) {
+    rope_kernel(const __grid_constant__ RopeLaunch r, const __grid_constant__ RopeTable rt) {
+  constexpr int kWords = VEC == 1 ? 1 : 4;
   __shared__ __align__(16) float2 table[kRopeTable];      // [token][VEC pairs of piece 0, 1, ... two by two]
-  __shared__ long long tok_row[kRopeTokens];              // page row of the token's position for head 0; -1: nothing to store
+  __shared__ const T* in_at[kRopeTokens][3];              // first head of the token, by group
+  __shared__ T* out_at[kRopeTokens][3];                   // (null: nothing is written)
   __shared__ int tok_pos[kRopeTokens];
-  __shared__ int tok_at[kRopeTokens];                     // sequence of the token; -1: none
   pdl_wait();
   pdl_launch_dependents();
-  const int tid = threadIdx.x, pairs = rt.rot / 2;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, pairs = rt.rot / 2;
   const long long tok0 = (long long)blockIdx.x * r.tb;
   const long long n_tok = (long long)r.batch * r.tokens;
   const int nt = (int)min((long long)r.tb, n_tok - tok0);
-  if (tid < nt) {
-    const long long tok = tok0 + tid;
-    int pos = 0, at = 0;
-    long long row = 0;
+  if (r.paged && blockIdx.x == 0 && blockIdx.y == 0)      // every sequence's numbers are looked at once, those without tokens too
+    for (int b = tid; b < r.pb.batch; b += kRopeThreads) paged_seq(r.pb, r.pl.status, b);
+  static_assert(kRopeTokens <= kRopeThreads / 32, "a warp per token");
+  if (warp < nt) {
+    const long long tok = tok0 + warp;
+    int pos = 0;
+    bool there = true;
+    long long row = -1;                                   // page row of the token's position for head 0
     if (r.paged) {
-      int lo = 0, hi = r.pb.batch;                        // the last b with cu[b] <= tok
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (__ldg(r.pb.cu + mid) <= tok) lo = mid; else hi = mid;
+      int at = -1;                                        // the last b with cu[b] <= tok
+      for (int b0 = 0; b0 < r.pb.batch; b0 += 32) {
+        const int b = b0 + lane;
+        const unsigned in = __ballot_sync(0xffffffffu, b < r.pb.batch && __ldg(r.pb.cu + b) <= tok);
+        at += __popc(in);
+        if (in != 0xffffffffu) break;
       }
-      const PagedSeq s = paged_seq(r.pb, r.pl.status, lo);
-      at = lo;
-      row = -1;
-      if (s.n > 0 && tok >= s.row0 && tok < s.row0 + s.n) {
+      PagedSeq s{0, 0, 0};
+      if (at >= 0) s = paged_seq(r.pb, r.pl.status, at);
+      there = s.n > 0 && tok >= s.row0 && tok < s.row0 + s.n;
+      if (there) {
         pos = s.L - s.n + (int)(tok - s.row0);
-        const long long first = paged_row(r.pb, r.pl, lo, 0, pos >> r.pl.log_p);
-        if (first >= 0) row = first + (pos & (r.pl.P - 1));
-      } else {
-        at = -1;
+        row = paged_row(r.pb, r.pl, at, 0, pos >> r.pl.log_p);
+        if (row >= 0) row += pos & (r.pl.P - 1);
       }
     }
-    if (r.positions && at >= 0) pos = __ldg(r.positions + tok);
-    tok_pos[tid] = pos;
-    tok_row[tid] = row;
-    tok_at[tid] = at;
-  }
-  __syncthreads();
-  // entry of (token, pair): the pairs of a piece lie two by two, the pieces side by side, so that a warp's loads are contiguous
-  if (pairs > 0) {
-    const int n_pieces = pairs / VEC;
-    for (int x = tid; x < nt * pairs; x += kRopeThreads) {
-      const int t = x / pairs, i = x - t * pairs;
-      const float2 cs = turn_of(rt.freq[i], tok_pos[t], rt.amplitude, r.transpose != 0);
-      const int piece = i / VEC, j = i % VEC;
-      const int e = VEC == 1 ? i : ((j >> 1) * n_pieces + piece) * 2 + (j & 1);
-      table[t * pairs + e] = cs;
+    if (lane < 3) {
+      const long long b = r.batch == 1 ? 0 : tok / r.tokens, i = tok - b * r.tokens;
+      const RopeGroup& g = r.g[lane];
+      in_at[warp][lane] = reinterpret_cast<const T*>(g.in) + b * g.in_batch + i * g.in_token;
+      T* out = nullptr;
+      if (g.out) { if (there) out = reinterpret_cast<T*>(g.out) + b * g.out_batch + i * g.out_token; }
+      else if (row >= 0) out = reinterpret_cast<T*>(lane == 1 ? r.k_pages : r.v_pages) + row * rt.dim;
+      out_at[warp][lane] = out;
     }
+    if (lane == 0) tok_pos[warp] = r.positions && there ? __ldg(r.positions + tok) : pos;
   }
   __syncthreads();
   const int by = kRopeThreads / r.pieces, piece = tid % r.pieces, ty = tid / r.pieces;
-  if (ty >= by) return;
   const int rot_pieces = pairs / VEC;
   const bool turns_here = piece < rot_pieces;
   // channels of the piece: a and b of its pairs, or two runs of VEC channels to copy
@@ -143,7 +139,11 @@ __global__ void __launch_bounds__(kRopeThreads)
   if (!turns_here) { ca = rt.rot + (piece - rot_pieces) * 2 * VEC; cb = ca + VEC; }
   else if (rt.interleaved) { ca = piece * 2 * VEC; cb = ca + VEC; }
   else { ca = piece * VEC; cb = ca + pairs; }
-  const int rows = nt * r.heads, end = min(rows, ((int)blockIdx.y + 1) * r.rows_per_y);
+  const int end = ty < by ? min(nt * r.heads, ((int)blockIdx.y + 1) * r.rows_per_y) : 0;
+  const int n0 = r.g[0].n_heads, n01 = n0 + r.g[1].n_heads;
+  const long long is0 = r.g[0].in_head, is1 = r.g[1].in_head, is2 = r.g[2].in_head;
+  const long long os0 = r.g[0].out_head, os1 = r.g[1].out ? r.g[1].out_head : r.pl.head_stride * rt.dim,
+                  os2 = r.g[2].out ? r.g[2].out_head : r.pl.head_stride * rt.dim;
 
   struct Place {
     const T* in;
@@ -153,23 +153,45 @@ __global__ void __launch_bounds__(kRopeThreads)
   };
   auto place = [&](int row) {
     Place pl;
-    const int t = row / r.heads;
-    int h = row - t * r.heads;
+    const int t = r.heads == 1 ? row : (int)__umulhi((unsigned)row, r.head_magic), h = row - t * r.heads;
+    const int gi = (h >= n0) + (h >= n01);
+    const int hg = h - (gi == 0 ? 0 : gi == 1 ? n0 : n01);
     pl.t = t;
-    int gi = 0;
-    if (h >= r.g[0].n_heads) { h -= r.g[0].n_heads; gi = 1; }
-    if (gi == 1 && h >= r.g[1].n_heads) { h -= r.g[1].n_heads; gi = 2; }
-    const RopeGroup& g = r.g[gi];
-    const long long tok = tok0 + t;
-    const long long b = r.batch == 1 ? 0 : tok / r.tokens, i = tok - b * r.tokens;
-    pl.in = reinterpret_cast<const T*>(g.in) + b * g.in_batch + i * g.in_token + h * g.in_head;
-    pl.rot = turns_here && g.rotate;
-    if (g.out) pl.out = tok_at[t] < 0 ? nullptr : reinterpret_cast<T*>(g.out) + b * g.out_batch + i * g.out_token + h * g.out_head;
-    else if (tok_row[t] < 0) pl.out = nullptr;
-    else pl.out = reinterpret_cast<T*>(gi == 1 ? r.k_pages : r.v_pages) + (tok_row[t] + h * r.pl.head_stride) * rt.dim;
+    pl.in = in_at[t][gi] + hg * (gi == 0 ? is0 : gi == 1 ? is1 : is2);
+    pl.out = out_at[t][gi];
+    if (pl.out) pl.out += hg * (gi == 0 ? os0 : gi == 1 ? os1 : os2);
+    pl.rot = turns_here && (gi == 0 ? r.g[0].rotate : gi == 1 ? r.g[1].rotate : r.g[2].rotate);
     return pl;
   };
-  auto finish = [&](const Place& pl, float (&a)[VEC], float (&b)[VEC]) {
+  // two rows at a time; the first are on their way before the sines are formed
+  int row = blockIdx.y * r.rows_per_y + ty;
+  Place p0, p1;
+  uint32_t x0[kWords], y0[kWords], x1[kWords], y1[kWords];
+  auto fetch = [&]() {
+    p0.out = p1.out = nullptr;
+    if (row < end) p0 = place(row);
+    if (row + by < end) p1 = place(row + by);
+    if (p0.out) { load_raw(p0.in + ca, x0); load_raw(p0.in + cb, y0); }
+    if (p1.out) { load_raw(p1.in + ca, x1); load_raw(p1.in + cb, y1); }
+  };
+  fetch();
+  // entry of (token, pair): the pairs of a piece lie two by two, the pieces side by side, so that a warp's loads are contiguous
+  if (pairs > 0) {
+    const unsigned long long* freq = rt.freq;
+    asm("" : "+l"(freq));                                 // (an ordinary load: a constant one takes a turn per thread)
+    for (int x = tid; x < nt * pairs; x += kRopeThreads) {
+      const int t = x / pairs, i = x - t * pairs;
+      const float2 cs = turn_of(freq[i], tok_pos[t], rt.amplitude, r.transpose != 0);
+      const int pc = i / VEC, j = i % VEC;
+      const int e = VEC == 1 ? i : ((j >> 1) * rot_pieces + pc) * 2 + (j & 1);
+      table[t * pairs + e] = cs;
+    }
+  }
+  __syncthreads();
+  auto finish = [&](const Place& pl, const uint32_t (&x)[kWords], const uint32_t (&y)[kWords]) {
+    float a[VEC], b[VEC];
+    unpack<T, VEC>(x, a);
+    unpack<T, VEC>(y, b);
     if (pl.rot) {
       if constexpr (VEC == 1) {
         const float2 cs = table[pl.t * pairs + piece];
@@ -197,15 +219,11 @@ __global__ void __launch_bounds__(kRopeThreads)
     store_piece<VEC>(pl.out + ca, a);
     store_piece<VEC>(pl.out + cb, b);
   };
-  for (int row = blockIdx.y * r.rows_per_y + ty; row < end; row += 2 * by) {       // two rows at a time, loads first
-    const bool second = row + by < end;
-    const Place p0 = place(row), p1 = place(second ? row + by : row);
-    float a0[VEC], b0[VEC], a1[VEC], b1[VEC];
-    if (p0.out) { load_piece<VEC>(p0.in + ca, a0); load_piece<VEC>(p0.in + cb, b0); }
-    const bool do1 = second && p1.out;
-    if (do1) { load_piece<VEC>(p1.in + ca, a1); load_piece<VEC>(p1.in + cb, b1); }
-    if (p0.out) finish(p0, a0, b0);
-    if (do1) finish(p1, a1, b1);
+  while (p0.out || p1.out || row < end) {
+    if (p0.out) finish(p0, x0, y0);
+    if (p1.out) finish(p1, x1, y1);
+    row += 2 * by;
+    fetch();
   }
 }
 
@@ -219,6 +237,7 @@ bool wide(const RopeGroup& g, int e) {
 template <typename T, int VEC>
 cudaError_t rope_launch(RopeLaunch r, const RopeTable& rt, int sm_count, cudaStream_t s) {
   r.pieces = rt.dim / (2 * VEC);
+  r.head_magic = (unsigned)(((1ull << 32) + r.heads - 1) / r.heads);
   const int pairs = rt.rot / 2;
   // tokens per block: a full table's worth, so that every thread forms one or two sines; fewer where that would leave SMs idle
   const long long n_tok = (long long)r.batch * r.tokens;
