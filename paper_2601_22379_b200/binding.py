@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -372,16 +373,23 @@ class SplaCache:
 
 # ---- rotary positions and the paged cache ---------------------------------------------------------------------------
 _TYPE_CODE = {torch.bfloat16: SPLA_BF16, torch.float32: SPLA_F32}
+# The structures of the calls of a step, packed in one go: a ctypes.Structure takes 0.1 us per field
+_pack_rope_tensor = struct.Struct("@PPi6q").pack
+_pack_batch = struct.Struct("@PPP5i4x").pack
+_pack_mask = struct.Struct("@fiPPP").pack
+_device_now, _stream_now = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+assert struct.calcsize("@PPi6q") == C.sizeof(SplaRopeTensor) and struct.calcsize("@PPP5i4x") == C.sizeof(SplaPagedBatch)
+assert struct.calcsize("@fiPPP") == C.sizeof(SplaPagedMask)
 
 
 def _on(index: int, fn, *args) -> int:
     """fn(*args, stream) with device `index` the current one and its current stream as the last argument."""
-    before = torch._C._cuda_getDevice()
+    before = _device_now()
     if before == index:
-        return fn(*args, torch._C._cuda_getCurrentRawStream(index))
+        return fn(*args, _stream_now(index))
     torch.cuda.set_device(index)
     try:
-        return fn(*args, torch._C._cuda_getCurrentRawStream(index))
+        return fn(*args, _stream_now(index))
     finally:
         torch.cuda.set_device(before)
 
@@ -404,39 +412,41 @@ class Rope:
         self.handle = C.c_void_p()
         _check(self.lib.spla_rope_create(C.byref(cfg), C.byref(self.handle)), "spla_rope_create")
 
-    def _tensor(self, x: torch.Tensor, out: torch.Tensor | None, positions: torch.Tensor):
-        shape, xs = x.shape, x.stride()
-        if not (shape[:-2] == positions.shape and shape[-1] == self.head_dim and xs[-1] == 1 and x.dtype in _TYPE_CODE and x.is_cuda
-                and x.device == positions.device):
+    def _tensor(self, x: torch.Tensor, out: torch.Tensor | None, shape, dtype, device):
+        """`out` and the packed descriptor of x -> out, for positions of `shape`."""
+        xshape, xs = x.shape, x.stride()
+        if not (xshape[:-2] == shape and xshape[-1] == self.head_dim and xs[-1] == 1 and x.dtype is dtype and x.device == device and x.is_cuda):
             raise ValueError("rope: tensors [batch, tokens, heads, head_dim] or [tokens, heads, head_dim] of the positions' batch and device, "
-                             "bf16 or fp32, channels contiguous")
+                             "of one type, bf16 or fp32, channels contiguous")
         if out is None:
             out = torch.empty_like(x)                                        # (the strides of x where they are dense)
-            if out.stride(-1) != 1:
-                out = x.new_empty(shape)
-        elif not (out.shape == shape and out.dtype == x.dtype and out.device == x.device and out.stride(-1) == 1):
-            raise ValueError("rope: an output like its input, channels contiguous")
-        ys = out.stride()
+            ys = out.stride()
+            if ys[-1] != 1:
+                out = x.new_empty(xshape)
+                ys = out.stride()
+        else:
+            ys = out.stride()
+            if not (out.shape == xshape and out.dtype is dtype and out.device == device and ys[-1] == 1):
+                raise ValueError("rope: an output like its input, channels contiguous")
         if len(xs) == 3:
-            return out, SplaRopeTensor(x.data_ptr(), out.data_ptr(), shape[1], 0, xs[0], xs[1], 0, ys[0], ys[1])
-        return out, SplaRopeTensor(x.data_ptr(), out.data_ptr(), shape[2], xs[0], xs[1], xs[2], ys[0], ys[1], ys[2])
+            return out, _pack_rope_tensor(x.data_ptr(), out.data_ptr(), xshape[1], 0, xs[0], xs[1], 0, ys[0], ys[1])
+        return out, _pack_rope_tensor(x.data_ptr(), out.data_ptr(), xshape[2], xs[0], xs[1], xs[2], ys[0], ys[1], ys[2])
 
     def apply(self, positions: torch.Tensor, q: torch.Tensor, k: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
               k_out: torch.Tensor | None = None, transpose: bool = False):
         """Rotates q (and k) to `positions` (int32 [batch, tokens] or [tokens]); any strides, channels contiguous.  `q_out=q`
         works in place.  `transpose`: the gradient of the rotation.  Returns q_out, or (q_out, k_out)."""
-        shape = positions.shape
-        if not (positions.dtype == torch.int32 and positions.is_contiguous() and 1 <= len(shape) <= 2):
-            raise ValueError("rope: positions int32 [batch, tokens] or [tokens], contiguous")
-        q_out, tq = self._tensor(q, q_out, positions)
+        shape, dtype, device = positions.shape, q.dtype, positions.device
+        if not (positions.dtype is torch.int32 and positions.is_contiguous() and 1 <= len(shape) <= 2 and dtype in _TYPE_CODE):
+            raise ValueError("rope: positions int32 [batch, tokens] or [tokens], contiguous; q bf16 or fp32")
+        q_out, tq = self._tensor(q, q_out, shape, dtype, device)
         tk = None
         if k is not None:
-            if k.dtype != q.dtype:
-                raise ValueError("rope: q and k of one type")
-            k_out, tk = self._tensor(k, k_out, positions)
-        if positions.numel():
-            rc = _on(positions.get_device(), self.lib.spla_rope_apply, self.handle, positions.data_ptr(), shape[0] if len(shape) == 2 else 1, shape[-1],
-                     C.addressof(tq), None if tk is None else C.addressof(tk), _TYPE_CODE[q.dtype], int(transpose))
+            k_out, tk = self._tensor(k, k_out, shape, dtype, device)
+        n = shape[-1]
+        batch = shape[0] if len(shape) == 2 else 1
+        if n and batch:
+            rc = _on(device.index, self.lib.spla_rope_apply, self.handle, positions.data_ptr(), batch, n, tq, tk, _TYPE_CODE[dtype], 1 if transpose else 0)
             if rc != SPLA_OK:
                 raise SplaError(rc, "spla_rope_apply")
         return q_out if k is None else (q_out, k_out)
@@ -495,20 +505,21 @@ class PagedCache:
                    C.byref(self.handle)), "spla_paged_create")
 
     def _batch(self, total, cu_new, seq_lens, page_table, max_new, max_len):
-        shape, n, dev = page_table.shape, seq_lens.shape[0], self.device
-        if not (cu_new.dtype == seq_lens.dtype == page_table.dtype == torch.int32 and cu_new.device == seq_lens.device == page_table.device == dev
-                and cu_new.is_contiguous() and seq_lens.is_contiguous() and len(shape) == 2 and page_table.stride(1) == 1
+        """The packed spla_paged_batch_t."""
+        shape, ts, n, dev, i32 = page_table.shape, page_table.stride(), seq_lens.shape[0], self.device, torch.int32
+        if not (cu_new.dtype is i32 and seq_lens.dtype is i32 and page_table.dtype is i32 and cu_new.device == dev and seq_lens.device == dev
+                and page_table.device == dev and cu_new.is_contiguous() and seq_lens.is_contiguous() and len(shape) == 2 and ts[1] == 1
                 and cu_new.shape[0] == n + 1 and shape[0] == n):
             raise ValueError("paged cache: int32 cu_new [batch + 1], seq_lens [batch], page_table [batch, columns] on the cache's device")
         # (the table's columns bound max_len; its rows may be further apart)
         if max_len > shape[1] * self.page_size:
             raise ValueError("paged cache: max_len is more than the page table's columns hold")
-        return SplaPagedBatch(cu_new.data_ptr(), seq_lens.data_ptr(), page_table.data_ptr(), n, total, max_new, max_len, page_table.stride(0) if n > 1 else shape[1])
+        return _pack_batch(cu_new.data_ptr(), seq_lens.data_ptr(), page_table.data_ptr(), n, total, max_new, max_len, ts[0] if n > 1 else shape[1])
 
     def _rows(self, x, total, heads, dtype, what):
         """Elements between the tokens of x [total, heads, d]."""
         d, xs = self.head_dim, x.stride()
-        if not (x.shape == (total, heads, d) and x.dtype == dtype and x.device == self.device and xs[2] == 1 and xs[1] == d):
+        if not (x.shape == (total, heads, d) and x.dtype is dtype and x.device == self.device and xs[2] == 1 and xs[1] == d):
             raise ValueError(f"paged cache: {what} [tokens, {heads}, {d}] of its type, heads contiguous")
         return xs[0] if total > 1 else heads * d
 
@@ -534,7 +545,7 @@ class PagedCache:
             # the store needs no bounds of its own: a sequence may be as long as the table has columns
             most = min(page_table.shape[1] * self.page_size, 1 << 24)
             b = self._batch(total, cu_new, seq_lens, page_table, min(total, most), most)
-            rc = _on(self.index, self.lib.spla_paged_append, self.handle, C.addressof(b), None if rope is None else rope.handle, _ptr(positions),
+            rc = _on(self.index, self.lib.spla_paged_append, self.handle, b, None if rope is None else rope.handle, _ptr(positions),
                      k.data_ptr(), ks, v.data_ptr(), vs, qp, qs, op, os_)
             if rc != SPLA_OK:
                 raise SplaError(rc, "spla_paged_append")
@@ -556,20 +567,22 @@ class PagedCache:
             lse = torch.empty((total, hq), dtype=torch.float32, device=dev)
         elif not (lse.shape == (total, hq) and lse.dtype == torch.float32 and lse.device == dev and lse.is_contiguous()):
             raise ValueError("paged cache: lse fp32 [total, H_q]")
-        for x, n, t, what in ((slopes, hq, torch.float32, "slopes fp32 [H_q]"), (first_key, total, torch.int32, "first_key int32 [total]"),
-                              (prefix_lens, seq_lens.shape[0], torch.int32, "prefix_lens int32 [batch]")):
-            if x is not None and not (x.dtype == t and x.numel() == n and x.is_contiguous() and x.device == dev):
-                raise ValueError(f"paged cache: {what}")
+        if slopes is not None or first_key is not None or prefix_lens is not None:
+            for x, n, t, what in ((slopes, hq, torch.float32, "slopes fp32 [H_q]"), (first_key, total, torch.int32, "first_key int32 [total]"),
+                                  (prefix_lens, seq_lens.shape[0], torch.int32, "prefix_lens int32 [batch]")):
+                if x is not None and not (x.dtype is t and x.numel() == n and x.is_contiguous() and x.device == dev):
+                    raise ValueError(f"paged cache: {what}")
         if total:
             b = self._batch(total, cu_new, seq_lens, page_table, max_new, max_len)
-            mask = SplaPagedMask(softcap, window, _ptr(slopes), _ptr(first_key), _ptr(prefix_lens))
+            mask = _pack_mask(softcap, window, _ptr(slopes) or 0, _ptr(first_key) or 0, _ptr(prefix_lens) or 0)
             nbytes = C.c_size_t()
             # (what the call refuses it refuses below too, with its name)
-            self.lib.spla_paged_query_workspace(self.handle, C.addressof(b), C.byref(nbytes))
+            self.lib.spla_paged_query_workspace(self.handle, b, C.byref(nbytes))
+            n = nbytes.value
             # a scratch of the call's own, from the stream's pool: calls on other streams and captured graphs share nothing
-            ws = torch.empty(nbytes.value, dtype=torch.uint8, device=dev) if nbytes.value else None
-            rc = _on(self.index, self.lib.spla_paged_attend, self.handle, C.addressof(b), q.data_ptr(), qs, C.addressof(mask), out.data_ptr(),
-                     lse.data_ptr(), _ptr(ws), nbytes.value)
+            ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+            rc = _on(self.index, self.lib.spla_paged_attend, self.handle, b, q.data_ptr(), qs, mask, out.data_ptr(), lse.data_ptr(),
+                     None if ws is None else ws.data_ptr(), n)
             if rc != SPLA_OK:
                 raise SplaError(rc, "spla_paged_attend")
         return out, lse
