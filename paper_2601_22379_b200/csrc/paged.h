@@ -64,7 +64,7 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& pb, int* status,
 constexpr int kPagedMaxBatch = 512;    // sequences per launch (the host cuts larger batches)
 
 struct PagedWork {
-  int ppos, upos, TK;
+  int ppos, upos, log_tk;               // TK = 2^log_tk
   int by_unit;                          // dealt out by units instead of tiles
   int n_cta, min_tiles;
   int extra;                            // what starting and ending a unit costs, in tiles: counted before its first tile when the work is dealt out
@@ -104,7 +104,7 @@ struct PagedSpan {
 __device__ __forceinline__ PagedSpan paged_span(const PagedWork& w, int window, int n, int L, int prefix, int u) {
   const int p0 = L - n + u * w.upos, p1 = L - n + min(n, (u + 1) * w.upos) - 1;
   const int lo = window > 0 ? max(0, p0 - window + 1) : 0, hi = min(L, max(p1 + 1, prefix));
-  return PagedSpan{lo / w.TK, (hi + w.TK - 1) / w.TK};
+  return PagedSpan{lo >> w.log_tk, (hi + (1 << w.log_tk) - 1) >> w.log_tk};
 }
 // What a unit counts for: its tiles and `extra` (one, where whole units are dealt out).
 __device__ __forceinline__ int paged_unit_tiles(const PagedWork& w, int window, int n, int L, int prefix, int u) {
@@ -113,41 +113,67 @@ __device__ __forceinline__ int paged_unit_tiles(const PagedWork& w, int window, 
   return s.t1 - s.t0 + w.extra;
 }
 
+// What one sequence counts for, per head.  Whole warps: sequences of many units are counted by the warp together.
+__device__ __forceinline__ long long paged_seq_tiles(const PagedAttend& a, int n, int L, int prefix, int lane) {
+  const int nu = paged_units(a.w, n);
+  int sum = 0;
+  if (nu <= 4)
+    for (int u = 0; u < nu; ++u) sum += paged_unit_tiles(a.w, a.window, n, L, prefix, u);
+  for (unsigned many = __ballot_sync(0xffffffffu, nu > 4); many; many &= many - 1) {
+    const int who = __ffs(many) - 1;
+    const int n_ = __shfl_sync(0xffffffffu, n, who), L_ = __shfl_sync(0xffffffffu, L, who), p_ = __shfl_sync(0xffffffffu, prefix, who),
+              nu_ = __shfl_sync(0xffffffffu, nu, who);
+    int part = 0;
+    for (int u = lane; u < nu_; u += 32) part += paged_unit_tiles(a.w, a.window, n_, L_, p_, u);
+    part = __reduce_add_sync(0xffffffffu, part);
+    if (lane == who) sum = part;
+  }
+  return sum;
+}
+__device__ __forceinline__ long long paged_scan(long long v, int lane) {   // inclusive, over a warp
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long x = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += x;
+  }
+  return v;
+}
+
 // Fills the table; all threads of the CTA (whole warps), ends with a barrier.  Returns the total.
 __device__ __forceinline__ long long paged_fill_seqs(const PagedAttend& a, PagedSeqs& t, int tid, int threads) {
-  const int batch = a.pb.batch;
-  for (int b = tid; b < batch; b += threads) {
-    const PagedSeq s = paged_seq(a.pb, a.pl.status, b);
-    const int pre = a.prefix ? __ldg(a.prefix + b) : 0;
-    t.row0[b] = s.row0; t.n[b] = s.n; t.L[b] = s.L; t.prefix[b] = pre;
-    const int nu = paged_units(a.w, s.n);
-    long long sum = 0;
-    if (nu <= 4)
-      for (int u = 0; u < nu; ++u) sum += paged_unit_tiles(a.w, a.window, s.n, s.L, pre, u);
-    t.pre[b + 1] = sum;
+  const int batch = a.pb.batch, lane = tid & 31;
+  if (batch <= 32) {                    // every warp for itself, all of them the same values: one barrier, which is the caller's anyway
+    int n = 0, L = 0, pre = 0;
+    if (lane < batch) {
+      pre = a.prefix ? __ldg(a.prefix + lane) : 0;
+      const PagedSeq s = paged_seq(a.pb, a.pl.status, lane);
+      n = s.n; L = s.L;
+      t.row0[lane] = s.row0; t.n[lane] = n; t.L[lane] = L; t.prefix[lane] = pre;
+    }
+    const long long v = paged_scan(paged_seq_tiles(a, n, L, pre, lane) * a.pl.Hkv, lane);
+    if (lane < batch) t.pre[lane + 1] = v;
+    if (lane == 0) t.pre[0] = 0;
+    __syncthreads();
+    return t.pre[batch];
   }
-  __syncthreads();
-  for (int b = tid >> 5; b < batch; b += threads >> 5) {
-    const int n = t.n[b], nu = paged_units(a.w, n);
-    if (nu <= 4) continue;
-    int sum = 0;
-    for (int u = tid & 31; u < nu; u += 32) sum += paged_unit_tiles(a.w, a.window, n, t.L[b], t.prefix[b], u);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if ((tid & 31) == 0) t.pre[b + 1] = sum;
+  for (int b0 = tid - lane; b0 < batch; b0 += threads) {
+    const int b = b0 + lane;
+    int n = 0, L = 0, pre = 0;
+    if (b < batch) {
+      pre = a.prefix ? __ldg(a.prefix + b) : 0;
+      const PagedSeq s = paged_seq(a.pb, a.pl.status, b);
+      n = s.n; L = s.L;
+      t.row0[b] = s.row0; t.n[b] = n; t.L[b] = L; t.prefix[b] = pre;
+    }
+    const long long sum = paged_seq_tiles(a, n, L, pre, lane);
+    if (b < batch) t.pre[b + 1] = sum;
   }
   __syncthreads();
   if (tid < 32) {
     long long carry = 0;
     for (int b0 = 0; b0 < batch; b0 += 32) {
       const int b = b0 + tid;
-      long long v = b < batch ? t.pre[b + 1] * a.pl.Hkv : 0;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long x = __shfl_up_sync(0xffffffffu, v, o);
-        if (tid >= o) v += x;
-      }
-      v += carry;
+      const long long v = paged_scan(b < batch ? t.pre[b + 1] * a.pl.Hkv : 0, tid) + carry;
       carry = __shfl_sync(0xffffffffu, v, 31);
       if (b < batch) t.pre[b + 1] = v;
     }
@@ -159,7 +185,8 @@ __device__ __forceinline__ long long paged_fill_seqs(const PagedAttend& a, Paged
 
 // Tiles (units) per CTA.
 __device__ __forceinline__ long long paged_share(const PagedWork& w, long long total) {
-  const long long per = (total + w.n_cta - 1) / w.n_cta;
+  const long long up = total + w.n_cta - 1;
+  const long long per = up < (1ll << 31) ? (long long)((unsigned)up / (unsigned)w.n_cta) : up / w.n_cta;
   return per < w.min_tiles ? w.min_tiles : per;
 }
 
@@ -185,9 +212,17 @@ struct PagedWalk {
     }
     b = lo;
     load(t);
-    const long long per_head = (t.pre[b + 1] - t.pre[b]) / a.pl.Hkv, rem = at - t.pre[b];
-    h = (int)(rem / per_head);
-    int in_head = (int)(rem - h * per_head);
+    const long long all = t.pre[b + 1] - t.pre[b], rem = at - t.pre[b];
+    int in_head;
+    if (all < (1ll << 31)) {
+      const unsigned per_head = (unsigned)all / (unsigned)a.pl.Hkv;
+      h = (int)((unsigned)rem / per_head);
+      in_head = (int)((unsigned)rem - (unsigned)h * per_head);
+    } else {
+      const long long per_head = all / a.pl.Hkv;
+      h = (int)(rem / per_head);
+      in_head = (int)(rem - h * per_head);
+    }
     u = 0;
     for (;;) {
       const int c = paged_unit_tiles(a.w, a.window, n, L, prefix, u);

@@ -387,8 +387,8 @@ void paged_plan_general(PagedWork* w, const PagedBatch& pb, const PagedLayout& p
   const int most = pb.max_new * pl.G;                              // rows that a sequence has for one KV head, at most
   const int R = most <= 4 ? 4 : most <= 16 ? 16 : 64;
   w->ppos = w->upos = R / pl.G;
-  w->TK = R == 64 ? 32 : 64;
-  const long long tiles = (pb.max_len + w->TK - 1) / w->TK, units = (long long)pb.batch * pl.Hkv * paged_units(*w, pb.max_new);
+  w->log_tk = R == 64 ? 5 : 6;
+  const long long tiles = (pb.max_len + (1 << w->log_tk) - 1) >> w->log_tk, units = (long long)pb.batch * pl.Hkv * paged_units(*w, pb.max_new);
   constexpr int per_sm = 2;
   w->by_unit = tiles <= 4;
   w->min_tiles = w->by_unit ? 1 : 2;

@@ -45,13 +45,13 @@ struct PmSmem {
   static constexpr int kQ = 0, kK = kQ + (FEW ? 1 : 2) * kTile, kV = kK + NK * kTile, kSeqs = kV + NV * kTile;
   static constexpr int kMl = kSeqs + (int)((sizeof(PagedSeqs) + 15) / 16 * 16);   // float2 [128]: maximum and sum of the second half, of a quarter
   static constexpr int kWalk = kMl + 128 * 8;                     // PagedWalk [8]: where the softmax warps are
-  static constexpr int kStage = kWalk + 8 * 64;                   // [8 warps][32 rows][64 + 16 bytes], FEW [4 warps][32 rows][128 + 16]: rows on their way out
-  static constexpr int kStageRow = FEW ? 144 : 80;
+  static constexpr int kStage = kWalk + 8 * 64;                   // [8 warps][32 rows][64 + 16 bytes], FEW [4 warps][8 rows][512 + 16] or fewer columns of more rows: rows on their way out
+  static constexpr int kStageRow = 80;
   static constexpr int kBars = kStage + 8 * 32 * 80;
   static constexpr int kNumBars = 2 * NK + 2 * NV + 15;
   static constexpr int kMisc = kBars + kNumBars * 8;             // tensor-memory base, abort flag, skip flags [2], look-over marks [2][2]
   static constexpr int kBytes = kMisc + 48;
-  static_assert(4 * 32 * 144 <= 8 * 32 * 80, "rows on their way out");
+  static_assert(4 * 32 * 144 <= 8 * 32 * 80 && 4 * 16 * 272 <= 8 * 32 * 80 && 4 * 8 * 528 <= 8 * 32 * 80, "rows on their way out");
   static_assert(kBytes <= 227 * 1024, "shared memory of the paged attention kernel");
 };
 
@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
     __syncwarp();
     while (any && ok) {
       int t, t_end, t_step, la, le, k_base, my;                   // this slot's tiles, those seen whole, the tile counter's offset
-      bool single, second;
+      bool single, second, alike;
       PagedSees see{0x7fffffff, 0};
       bool valid;
       int pos;
@@ -388,6 +388,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         const PmPlan pl = pm_plan(a, wk, lane);
         single = pl.single;
         second = single && pl.items(1) > 0;
+        alike = wk.n == 1;
         my = pl.items(slot);
         t = single ? pl.A + slot : slot ? pl.a1 : pl.a0;
         t_end = single ? pl.E : slot ? pl.e1 : pl.e0;
@@ -398,14 +399,15 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         kt += pl.E - pl.A;
         const int i = wk.first_pos(a.w) + (single ? 0 : slot * ppos) + pi;
         valid = row < ppos * G && i < wk.n;
-        if (valid) see = paged_sees(a, wk.row0, wk.n, wk.L, wk.prefix, i);
+        if (valid || alike) see = paged_sees(a, wk.row0, wk.n, wk.L, wk.prefix, alike ? 0 : i);
         if (MODS && a.slopes && valid) slope2 = __ldg(a.slopes + wk.h * G + g) * kLog2e;
         pos = wk.L - wk.n + i;
         if (lane == 0) kept = wk;
         __syncwarp();
       }
       const bool live = __any_sync(0xffffffffu, valid);
-      const int lo_most = __reduce_max_sync(0xffffffffu, valid ? see.lo : 0), hi_least = __reduce_min_sync(0xffffffffu, valid ? see.hi : 0x7fffffff);
+      const bool counts = valid || alike;
+      const int lo_most = __reduce_max_sync(0xffffffffu, counts ? see.lo : 0), hi_least = __reduce_min_sync(0xffffffffu, counts ? see.hi : 0x7fffffff);
       float m = -INFINITY, l = 0.f;
       int done_items = 0;
 #pragma unroll 1
@@ -417,17 +419,38 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         if (look) {
           // (After the scores: they follow the row tile's product before, which waited for the V tiles up to two before this one, so that
           // the parity below can only mean this one.)
-          // Values of this tile: zeroed behind the end where they are not finite; elsewhere such a value makes the tile special
+          // Values of this tile.  Where all rows see the same keys (single tokens) the rows of the others are zeroed; otherwise they are
+          // looked over: zeroed behind the end where they are not finite, and elsewhere such a value makes the tile special.
           if (!pm_wait(&v_full[st], ((uint32_t)(k_base + t) / NV) & 1, lim, abort_flag)) { ok = false; break; }
-          const int L = kept.L;
+          unsigned char* vt = smem + SM::kV + st * SM::kTile;
           bool bad = false;
-          unsigned char* vt = smem + SM::kV + st * SM::kTile + thr * 16;
-#pragma unroll 4
-          for (int x = 0; x < SM::kTile / 2048; ++x) {             // 16-byte pieces: rows thr / 8 + 16 x of either array
-            const uint4 v = *reinterpret_cast<const uint4*>(vt + x * 2048);
-            if (pair_not_finite(v.x) | pair_not_finite(v.y) | pair_not_finite(v.z) | pair_not_finite(v.w)) {
-              if (tok0 + (thr >> 3) + 16 * (x & 7) >= L) *reinterpret_cast<uint4*>(vt + x * 2048) = make_uint4(0u, 0u, 0u, 0u);
-              else bad = true;
+          if (alike) {
+            const int from = lo_most - tok0, to = hi_least - tok0;
+            for (int j = thr >> 3; j < kPmKeys; j += 16)           // a row of 128 bytes by eight threads
+              if (j < from || j >= to) {
+#pragma unroll
+                for (int x = 0; x < H; ++x) *reinterpret_cast<uint4*>(vt + x * SM::kHalf + j * 128 + (thr & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+              }
+          } else {
+            vt += thr * 16;                                       // 16-byte pieces: rows thr / 8 + 16 x of either array
+            __nv_bfloat162 most = __floats2bfloat162_rn(0.f, 0.f); // the largest magnitude, NaN above all
+#pragma unroll 8
+            for (int x = 0; x < SM::kTile / 2048; ++x) {
+              const uint4 v = *reinterpret_cast<const uint4*>(vt + x * 2048);
+              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) most = __hmax2_nan(most, __habs2(*reinterpret_cast<const __nv_bfloat162*>(&w[e])));
+            }
+            if (pair_not_finite(*reinterpret_cast<const uint32_t*>(&most))) {
+              const int L = kept.L;
+#pragma unroll 1
+              for (int x = 0; x < SM::kTile / 2048; ++x) {
+                const uint4 v = *reinterpret_cast<const uint4*>(vt + x * 2048);
+                if (pair_not_finite(v.x) | pair_not_finite(v.y) | pair_not_finite(v.z) | pair_not_finite(v.w)) {
+                  if (tok0 + (thr >> 3) + 16 * (x & 7) >= L) *reinterpret_cast<uint4*>(vt + x * 2048) = make_uint4(0u, 0u, 0u, 0u);
+                  else bad = true;
+                }
+              }
             }
           }
           proxy_fence();                                          // (zeros written -> tensor core)
@@ -633,52 +656,58 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       const long long out_row = (long long)(wk.row0 + i0 + pi) * a.pl.Hq + wk.h * G + g;
       const long long part_row = (2LL * blockIdx.x + (wk.head ? 1 : 0)) * a.w.rows + (single ? 0 : slot * ppos * G) + row;
       if constexpr (FEW) {
-        // 32 columns of every row at a time from the four warps to shared memory; then a row by four threads, 8 columns each
+        // The four warps' rows meet in shared memory, as many columns at a time as fit; a thread adds and writes 8 columns of a row.
+        const int n_rows = min(ppos, wk.n - i0) * G, cols = n_rows <= 8 ? (D < 128 ? D : 128) : n_rows <= 16 ? 64 : 32;
+        const int r_cap = n_rows <= 8 ? 8 : n_rows <= 16 ? 16 : 32, r_bytes = cols * 4 + 16, pieces = cols >> 3;
         unsigned char* stage = smem + SM::kStage;
-        const int r = thr >> 2, piece = thr & 3, ri = r / G;
-        const bool there = r < ppos * G && i0 + ri < wk.n;
+        const int r = thr / pieces, piece = thr - r * pieces, ri = r / G;
         const long long o_row = (long long)(wk.row0 + i0 + ri) * a.pl.Hq + wk.h * G + (r - ri * G);
 #pragma unroll 1
-        for (int c = 0; c < D && ok; c += 32) {
-          float o[32], o1[32];
-          if (my > 0) tmem_ld32(tO + c, o);
-          if (second) tmem_ld32(tO + 128 + c, o1);
-          if (valid) {
+        for (int c0 = 0; c0 < D; c0 += cols) {
+          if (c0 > 0) {                                           // (the columns before are out of the way)
+            __syncwarp();
+            if (lane == 0) mbar_arrive1(quarters);
+            if (!pm_wait(quarters, n_quarter & 1, lim, abort_flag)) { ok = false; break; }
+            ++n_quarter;
+          }
+#pragma unroll 1
+          for (int c = 0; c < cols; c += 32) {
+            float o[32], o1[32];
+            if (my > 0) tmem_ld32(tO + c0 + c, o);
+            if (second) tmem_ld32(tO + 128 + c0 + c, o1);
+            if (valid) {
 #pragma unroll
-            for (int x = 0; x < 32; ++x) {
-              const float y = my > 0 && l != 0.f ? o[x] * w0 : 0.f;
-              o[x] = second && l1 != 0.f ? fmaf(o1[x], w1, y) : y;
+              for (int x = 0; x < 32; ++x) {
+                const float y = my > 0 && l != 0.f ? o[x] * w0 : 0.f;
+                o[x] = second && l1 != 0.f ? fmaf(o1[x], w1, y) : y;
+              }
+              unsigned char* to = stage + ((warp & 3) * r_cap + lane) * r_bytes + c * 4;
+#pragma unroll
+              for (int x = 0; x < 8; ++x) *reinterpret_cast<float4*>(to + x * 16) = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
             }
-#pragma unroll
-            for (int x = 0; x < 8; ++x)
-              *reinterpret_cast<float4*>(stage + ((warp & 3) * 32 + lane) * SM::kStageRow + x * 16) = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
           }
           __syncwarp();
           if (lane == 0) mbar_arrive1(quarters);
           if (!pm_wait(quarters, n_quarter & 1, lim, abort_flag)) { ok = false; break; }
           ++n_quarter;
-          if (there) {
+          if (r < n_rows) {
             float4 v0 = make_float4(0.f, 0.f, 0.f, 0.f), v1 = v0;
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-              const float4 a0 = *reinterpret_cast<const float4*>(stage + (x * 32 + r) * SM::kStageRow + piece * 32);
-              const float4 a1 = *reinterpret_cast<const float4*>(stage + (x * 32 + r) * SM::kStageRow + piece * 32 + 16);
+              const float4* from = reinterpret_cast<const float4*>(stage + (x * r_cap + r) * r_bytes + piece * 32);
+              const float4 a0 = from[0], a1 = from[1];
               v0.x += a0.x; v0.y += a0.y; v0.z += a0.z; v0.w += a0.w;
               v1.x += a1.x; v1.y += a1.y; v1.z += a1.z; v1.w += a1.w;
             }
             if (whole) {
-              *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + o_row * D + c + piece * 8) =
+              *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + o_row * D + c0 + piece * 8) =
                   make_uint4(pack_bf16(v0.x, v0.y), pack_bf16(v0.z, v0.w), pack_bf16(v1.x, v1.y), pack_bf16(v1.z, v1.w));
             } else {
-              float4* dst = reinterpret_cast<float4*>(a.w.part_o + (part_row + (r - row)) * D + c + piece * 8);
+              float4* dst = reinterpret_cast<float4*>(a.w.part_o + (part_row + (r - row)) * D + c0 + piece * 8);
               dst[0] = v0;
               dst[1] = v1;
             }
           }
-          __syncwarp();
-          if (lane == 0) mbar_arrive1(quarters);                  // (the next columns take the same place)
-          if (!pm_wait(quarters, n_quarter & 1, lim, abort_flag)) { ok = false; break; }
-          ++n_quarter;
         }
         if (!ok) break;
         if (valid && (warp & 3) == 0) {
@@ -793,8 +822,9 @@ void paged_plan_mma(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, i
   w->ppos = paged_mma_positions(pb, pl);
   const bool few = w->ppos * pl.G <= 32;
   w->upos = (few ? 1 : 2) * w->ppos;
-  w->TK = kPmKeys;
-  const long long tiles = (pb.max_len + w->TK - 1) / w->TK, units = (long long)pb.batch * pl.Hkv * paged_units(*w, pb.max_new);
+  w->log_tk = 7;
+  static_assert(kPmKeys == 1 << 7, "keys per tile");
+  const long long tiles = (pb.max_len + kPmKeys - 1) / kPmKeys, units = (long long)pb.batch * pl.Hkv * paged_units(*w, pb.max_new);
   w->by_unit = tiles <= 4;
   w->min_tiles = w->by_unit ? 1 : 2;
   w->extra = few ? 1 : 2;
