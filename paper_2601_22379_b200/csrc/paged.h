@@ -97,34 +97,40 @@ struct PagedSeqs {
 
 __host__ __device__ __forceinline__ int paged_units(const PagedWork& w, int n) { return n <= w.ppos ? (n > 0) : (n + w.upos - 1) / w.upos; }
 
-// Key tiles [t0, t1) that unit u of a sequence walks (its documents' starts are left aside here).  Never empty: a position sees itself.
+// Key tiles [t0, t1) that unit u of a sequence may walk.  Never empty: a position sees itself.  From e0 on they count when the work is
+// dealt out: the tiles before are behind the start of its first token's document, where there is nothing to walk as long as
+// documents follow one another (what is walked goes by every token's own start).
 struct PagedSpan {
-  int t0, t1;
+  int t0, t1, e0;
 };
-__device__ __forceinline__ PagedSpan paged_span(const PagedWork& w, int window, int n, int L, int prefix, int u) {
+__device__ __forceinline__ PagedSpan paged_span(const PagedAttend& a, int row0, int n, int L, int prefix, int u) {
+  const PagedWork& w = a.w;
   const int p0 = L - n + u * w.upos, p1 = L - n + min(n, (u + 1) * w.upos) - 1;
-  const int lo = window > 0 ? max(0, p0 - window + 1) : 0, hi = min(L, max(p1 + 1, prefix));
-  return PagedSpan{lo >> w.log_tk, (hi + (1 << w.log_tk) - 1) >> w.log_tk};
+  const int lo = a.window > 0 ? max(0, p0 - a.window + 1) : 0, hi = min(L, max(p1 + 1, prefix));
+  PagedSpan s{lo >> w.log_tk, (hi + (1 << w.log_tk) - 1) >> w.log_tk, 0};
+  s.e0 = s.t0;
+  if (a.first_key && !w.by_unit) s.e0 = min(max(s.t0, __ldg(a.first_key + row0 + u * w.upos) >> w.log_tk), s.t1 - 1);
+  return s;
 }
 // What a unit counts for: its tiles and `extra` (one, where whole units are dealt out).
-__device__ __forceinline__ int paged_unit_tiles(const PagedWork& w, int window, int n, int L, int prefix, int u) {
-  if (w.by_unit) return 1;
-  const PagedSpan s = paged_span(w, window, n, L, prefix, u);
-  return s.t1 - s.t0 + w.extra;
+__device__ __forceinline__ int paged_unit_tiles(const PagedAttend& a, int row0, int n, int L, int prefix, int u) {
+  if (a.w.by_unit) return 1;
+  const PagedSpan s = paged_span(a, row0, n, L, prefix, u);
+  return s.t1 - s.e0 + a.w.extra;
 }
 
 // What one sequence counts for, per head.  Whole warps: sequences of many units are counted by the warp together.
-__device__ __forceinline__ long long paged_seq_tiles(const PagedAttend& a, int n, int L, int prefix, int lane) {
+__device__ __forceinline__ long long paged_seq_tiles(const PagedAttend& a, int row0, int n, int L, int prefix, int lane) {
   const int nu = paged_units(a.w, n);
   int sum = 0;
   if (nu <= 4)
-    for (int u = 0; u < nu; ++u) sum += paged_unit_tiles(a.w, a.window, n, L, prefix, u);
+    for (int u = 0; u < nu; ++u) sum += paged_unit_tiles(a, row0, n, L, prefix, u);
   for (unsigned many = __ballot_sync(0xffffffffu, nu > 4); many; many &= many - 1) {
     const int who = __ffs(many) - 1;
     const int n_ = __shfl_sync(0xffffffffu, n, who), L_ = __shfl_sync(0xffffffffu, L, who), p_ = __shfl_sync(0xffffffffu, prefix, who),
-              nu_ = __shfl_sync(0xffffffffu, nu, who);
+              nu_ = __shfl_sync(0xffffffffu, nu, who), r_ = __shfl_sync(0xffffffffu, row0, who);
     int part = 0;
-    for (int u = lane; u < nu_; u += 32) part += paged_unit_tiles(a.w, a.window, n_, L_, p_, u);
+    for (int u = lane; u < nu_; u += 32) part += paged_unit_tiles(a, r_, n_, L_, p_, u);
     part = __reduce_add_sync(0xffffffffu, part);
     if (lane == who) sum = part;
   }
@@ -143,14 +149,14 @@ __device__ __forceinline__ long long paged_scan(long long v, int lane) {   // in
 __device__ __forceinline__ long long paged_fill_seqs(const PagedAttend& a, PagedSeqs& t, int tid, int threads) {
   const int batch = a.pb.batch, lane = tid & 31;
   if (batch <= 32) {                    // every warp for itself, all of them the same values: one barrier, which is the caller's anyway
-    int n = 0, L = 0, pre = 0;
+    int row0 = 0, n = 0, L = 0, pre = 0;
     if (lane < batch) {
       pre = a.prefix ? __ldg(a.prefix + lane) : 0;
       const PagedSeq s = paged_seq(a.pb, a.pl.status, lane);
-      n = s.n; L = s.L;
-      t.row0[lane] = s.row0; t.n[lane] = n; t.L[lane] = L; t.prefix[lane] = pre;
+      row0 = s.row0; n = s.n; L = s.L;
+      t.row0[lane] = row0; t.n[lane] = n; t.L[lane] = L; t.prefix[lane] = pre;
     }
-    const long long v = paged_scan(paged_seq_tiles(a, n, L, pre, lane) * a.pl.Hkv, lane);
+    const long long v = paged_scan(paged_seq_tiles(a, row0, n, L, pre, lane) * a.pl.Hkv, lane);
     if (lane < batch) t.pre[lane + 1] = v;
     if (lane == 0) t.pre[0] = 0;
     __syncthreads();
@@ -158,14 +164,14 @@ __device__ __forceinline__ long long paged_fill_seqs(const PagedAttend& a, Paged
   }
   for (int b0 = tid - lane; b0 < batch; b0 += threads) {
     const int b = b0 + lane;
-    int n = 0, L = 0, pre = 0;
+    int row0 = 0, n = 0, L = 0, pre = 0;
     if (b < batch) {
       pre = a.prefix ? __ldg(a.prefix + b) : 0;
       const PagedSeq s = paged_seq(a.pb, a.pl.status, b);
-      n = s.n; L = s.L;
-      t.row0[b] = s.row0; t.n[b] = n; t.L[b] = L; t.prefix[b] = pre;
+      row0 = s.row0; n = s.n; L = s.L;
+      t.row0[b] = row0; t.n[b] = n; t.L[b] = L; t.prefix[b] = pre;
     }
-    const long long sum = paged_seq_tiles(a, n, L, pre, lane);
+    const long long sum = paged_seq_tiles(a, row0, n, L, pre, lane);
     if (b < batch) t.pre[b + 1] = sum;
   }
   __syncthreads();
@@ -225,7 +231,7 @@ struct PagedWalk {
     }
     u = 0;
     for (;;) {
-      const int c = paged_unit_tiles(a.w, a.window, n, L, prefix, u);
+      const int c = paged_unit_tiles(a, row0, n, L, prefix, u);
       if (in_head < c) break;
       in_head -= c;
       ++u;
@@ -244,16 +250,17 @@ struct PagedWalk {
           load(t);
         }
       }
-      const PagedSpan s = paged_span(a.w, a.window, n, L, prefix, u);
+      const PagedSpan s = paged_span(a, row0, n, L, prefix, u);
       if (a.w.by_unit) {
         t0 = s.t0; t1 = s.t1; head = tail = true;
         left -= 1;
       } else {                                       // the share holds off .. upto of the unit's extra and tiles
-        const int upto = (int)min((long long)(s.t1 - s.t0 + a.w.extra), off + left);
+        const int upto = (int)min((long long)(s.t1 - s.e0 + a.w.extra), off + left);
         left -= upto - off;
-        t0 = s.t0 + max(0, off - a.w.extra);
-        t1 = s.t0 + max(0, upto - a.w.extra);
-        head = t0 == s.t0; tail = t1 == s.t1;
+        head = off <= a.w.extra;
+        t0 = head ? s.t0 : s.e0 + off - a.w.extra;
+        t1 = upto <= a.w.extra ? t0 : s.e0 + upto - a.w.extra;
+        tail = t1 == s.t1;
       }
       off = 0;
       u_cur = u++;

@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedAtt
   if (!wk.seek(a, seqs, at, 1) || wk.off <= a.w.extra || wk.off - a.w.extra > share) return;   // no border between a unit's tiles, or not its first
   const int off = wk.off;
   wk.next(a, seqs);
-  const int tiles = paged_unit_tiles(a.w, a.window, wk.n, wk.L, wk.prefix, wk.u_cur);
+  const int tiles = paged_unit_tiles(a, wk.row0, wk.n, wk.L, wk.prefix, wk.u_cur);
   const int parts = 1 + (int)((tiles - off + share - 1) / share);  // share cut - 1 (its second slot), then cut, cut + 1, ... (their first slots)
   const int i0 = wk.first_pos(a.w), rows = min(wk.n - i0, wk.n_pos(a.w)) * G;
   constexpr int V = D / 32;
