@@ -206,7 +206,7 @@ struct PagedWalk {
   bool head, tail;                      // it starts / ends the unit
 
   __device__ __forceinline__ void load(const PagedSeqs& t) { row0 = t.row0[b]; n = t.n[b]; L = t.L[b]; prefix = t.prefix[b]; }
-  // Goes to tile `at` of all; false if there is none.
+  // Goes to tile `at` of all; false if there is none.  Whole warps.
   __device__ __forceinline__ bool seek(const PagedAttend& a, const PagedSeqs& t, long long at, long long count) {
     const long long total = t.pre[a.pb.batch];
     left = min(count, total - at);
@@ -229,14 +229,24 @@ struct PagedWalk {
       h = (int)(rem / per_head);
       in_head = (int)(rem - h * per_head);
     }
-    u = 0;
-    for (;;) {
-      const int c = paged_unit_tiles(a, row0, n, L, prefix, u);
-      if (in_head < c) break;
-      in_head -= c;
-      ++u;
+    const int lane = threadIdx.x & 31, nu = paged_units(a.w, n);
+    for (u = 0;; u += 32) {             // 32 units at a time
+      const int c = u + lane < nu ? paged_unit_tiles(a, row0, n, L, prefix, u + lane) : 0;
+      int upto = c;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+      }
+      const unsigned past = __ballot_sync(0xffffffffu, upto > in_head);
+      if (past || u + 32 >= nu) {
+        const int who = past ? __ffs(past) - 1 : 0;
+        off = in_head - __shfl_sync(0xffffffffu, upto - c, who);
+        u += who;
+        break;
+      }
+      in_head -= __shfl_sync(0xffffffffu, upto, 31);
     }
-    off = in_head;
     return true;
   }
   __device__ __forceinline__ bool next(const PagedAttend& a, const PagedSeqs& t) {

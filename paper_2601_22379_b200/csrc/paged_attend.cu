@@ -5,31 +5,40 @@
 //
 // One pass over the keys with the running maximum and sum of the softmax in base 2.  A CTA walks tiles of TK keys for R query
 // rows: scores from row pieces in shared memory (four rows x KT keys per thread, packed FMAs over two channels), then the
-// product with V (four rows x CW channels per thread, the tile's tokens shared by TS threads).  R = 4, 16 and 64 by the rows that a
-// unit has at most; a row tile's products cost the same however few of its rows are real.  4 and 16 rows are bound by reading K and V, 64 by the FMA pipe.
+// product with V (four rows x CW channels per thread, the tile's tokens shared by TS threads).  K of the next tile is on its way from
+// when the scores are done, V from when the product is done (asynchronous copies where the cache is fp32), the page table one tile ahead of that.
+// R = 4, 16, 64 and 128 by the rows that a unit has at most; a row tile's products cost the same however few of its rows are real.
+// 4 and 16 rows are bound by reading K and V, more by the FMA pipe.
 #include "paged.h"
 
 namespace spla {
 
 namespace {
 
-constexpr int kPgThreads = 256;
-
 template <int R, int D>
 struct PgShape {
+  static constexpr int THREADS = R == 128 ? 512 : 256;
   static constexpr int TK = R == 64 ? 32 : 64;
-  static constexpr int KT = R == 64 ? 2 : 1;                       // keys per thread
+  static constexpr int KT = R == 128 ? 4 : R == 64 ? 2 : 1;        // keys per thread
   static constexpr int RG = R / 4;                                 // groups of four rows
-  static constexpr int CS = kPgThreads / (RG * (TK / KT));         // threads that share the channels of a score
-  static constexpr int CW = R == 64 ? D / 16 : 4;                  // channels per thread in the product with V
-  static constexpr int TS = kPgThreads / (RG * (D / CW));          // threads that share a tile's tokens there
+  static constexpr int CS = THREADS / (RG * (TK / KT));            // threads that share the channels of a score
+  static constexpr int CW = R >= 64 ? D / 16 : 4;                  // channels per thread in the product with V
+  static constexpr int TS = THREADS / (RG * (D / CW));             // threads that share a tile's tokens there
   static constexpr int LD = D + 4, LP = TK + 4;
   static constexpr int kQ = 0, kK = kQ + R * LD * 4, kV = kK + TK * LD * 4, kP = kV + TK * D * 4, kFac = kP + R * LP * 4, kLo = kFac + R * 4,
-                       kHi = kLo + R * 4, kSum = kHi + R * 4, kMax = kSum + R * 4, kSeqs = (kMax + R * 4 + 15) / 16 * 16,
-                       kBytes = kSeqs + (int)sizeof(PagedSeqs);
+                       kHi = kLo + R * 4, kSum = kHi + R * 4, kMax = kSum + R * 4, kTop = kMax + R * 4, kRows = (kTop + R * 8 * 4 + 15) / 16 * 16,
+                       kSeqs = kRows + 2 * (TK / 16) * 8, kBytes = kSeqs + (int)sizeof(PagedSeqs);
   static_assert(CS >= 1 && TS >= 1 && D % (4 * CS) == 0, "shape");
   static_assert((TS - 1) * R * D * 4 <= TK * (LD + D) * 4, "the partial products of a unit fit the K and V tiles");
+  static_assert(kBytes <= 227 * 1024, "shared memory of the general kernel");
 };
+
+__device__ __forceinline__ void copy16(void* dst, const void* src, bool there) {   // asynchronous; zeros where there is nothing
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 template <typename T>
 __device__ __forceinline__ float4 load4(const T* p) {
@@ -41,10 +50,10 @@ __device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<f
 __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) { *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)); }
 
 template <typename TQ, typename TKV, int R, int D>
-__global__ void __launch_bounds__(kPgThreads, 2)
+__global__ void __launch_bounds__((PgShape<R, D>::THREADS), R == 128 ? 1 : 2)
     paged_general_kernel(const PagedAttend a, const TKV* __restrict__ k_pages, const TKV* __restrict__ v_pages) {
   using S = PgShape<R, D>;
-  constexpr int TK = S::TK, KT = S::KT, CS = S::CS, CW = S::CW, TS = S::TS, LD = S::LD, LP = S::LP, D4 = D / 4;
+  constexpr int THREADS = S::THREADS, TK = S::TK, KT = S::KT, CS = S::CS, CW = S::CW, TS = S::TS, LD = S::LD, LP = S::LP, D4 = D / 4;
   extern __shared__ __align__(16) unsigned char smem[];
   float* qs = reinterpret_cast<float*>(smem + S::kQ);
   float* ks = reinterpret_cast<float*>(smem + S::kK);
@@ -55,11 +64,13 @@ __global__ void __launch_bounds__(kPgThreads, 2)
   int* hi_s = reinterpret_cast<int*>(smem + S::kHi);
   float* sum_s = reinterpret_cast<float*>(smem + S::kSum);
   float* max_s = reinterpret_cast<float*>(smem + S::kMax);
+  float* top_s = reinterpret_cast<float*>(smem + S::kTop);        // [R][warps of a row group]
+  long long* rows_s = reinterpret_cast<long long*>(smem + S::kRows);   // [2][TK / 16]: first row of every 16 tokens of a tile, -1: none
   PagedSeqs& seqs = *reinterpret_cast<PagedSeqs*>(smem + S::kSeqs);
   pdl_wait();
   pdl_launch_dependents();
   const int tid = threadIdx.x, G = a.pl.G;
-  const long long share = paged_share(a.w, paged_fill_seqs(a, seqs, tid, kPgThreads));
+  const long long share = paged_share(a.w, paged_fill_seqs(a, seqs, tid, THREADS));
   PagedWalk wk;
   if (!wk.seek(a, seqs, blockIdx.x * share, share)) return;
   // scores: thread = (channel share, key, row group); product: (channel group, token share, row group)
@@ -67,10 +78,34 @@ __global__ void __launch_bounds__(kPgThreads, 2)
   const int cg = tid % (D / CW), ts = tid / (D / CW) % TS, rp = tid / (D / CW * TS);
   const float sc = a.sm_scale, inv_cap = a.softcap > 0.f ? 1.f / a.softcap : 0.f;
   while (wk.next(a, seqs)) {
-    const int i0 = wk.first_pos(a.w), rows = wk.n_pos(a.w) > wk.n - i0 ? (wk.n - i0) * G : wk.n_pos(a.w) * G;
+    const int i0 = wk.first_pos(a.w), rows = min(wk.n - i0, wk.n_pos(a.w)) * G;
     const int pos0 = wk.L - wk.n + i0;
+    auto find_rows = [&](int t) {                                  // a few threads: where tile t lies
+      if (tid < TK / 16 && t < wk.t1) {
+        const int tok = t * TK + tid * 16;
+        long long row = -1;
+        if (tok < wk.L) {
+          row = paged_row(a.pb, a.pl, wk.b, wk.h, tok >> a.pl.log_p);
+          if (row >= 0) row += tok & (a.pl.P - 1);
+        }
+        rows_s[(t & 1) * (TK / 16) + tid] = row;
+      }
+    };
+    auto fetch = [&](const TKV* pages, float* to, int ld, int t) { // one tile of K or V
+#pragma unroll
+      for (int x0 = 0; x0 < TK * D4; x0 += THREADS) {
+        const int x = x0 + tid, j = x / D4, c = x % D4;
+        const long long row = rows_s[(t & 1) * (TK / 16) + j / 16];
+        const bool there = row >= 0 && t * TK + j < wk.L;
+        const TKV* from = pages + (there ? (row + j % 16) * D + c * 4 : 0);
+        if constexpr (sizeof(TKV) == 4) copy16(to + j * ld + c * 4, from, there);
+        else *reinterpret_cast<float4*>(to + j * ld + c * 4) = there ? load4(from) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      copies_close();
+    };
     __syncthreads();                                               // the segment before is done with shared memory
-    for (int x = tid; x < R * D4; x += kPgThreads) {
+    find_rows(wk.t0);
+    for (int x = tid; x < R * D4; x += THREADS) {
       const int r = x / D4, c = x % D4;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       if (r < rows) {
@@ -80,11 +115,13 @@ __global__ void __launch_bounds__(kPgThreads, 2)
       }
       *reinterpret_cast<float4*>(qs + r * LD + c * 4) = v;
     }
+    bool sees_any = false;
     if (tid < R) {
       PagedSees s{0, 0};
       if (tid < rows) s = paged_sees(a, wk.row0, wk.n, wk.L, wk.prefix, i0 + tid / G);
       lo_s[tid] = s.lo;
       hi_s[tid] = s.hi;
+      sees_any = s.lo < s.hi;
     }
     float slope[4];
 #pragma unroll
@@ -97,28 +134,41 @@ __global__ void __launch_bounds__(kPgThreads, 2)
 #pragma unroll
       for (int x = 0; x < CW; ++x) o[i][x] = 0.f;
     }
-#pragma unroll 1
-    for (int t = wk.t0; t < wk.t1; ++t) {
-      const int tok0 = t * TK;
-      __syncthreads();                                             // rows' bounds; the tile before is used up
-      bool bad = false;                                            // a value that is not finite
-#pragma unroll
-      for (int x0 = 0; x0 < TK * D4; x0 += kPgThreads) {
-        const int x = x0 + tid, j = x / D4, c = x % D4, tok = tok0 + j;
-        float4 kv = make_float4(0.f, 0.f, 0.f, 0.f), vv = kv;
-        if (tok < wk.L) {
-          const long long first = paged_row(a.pb, a.pl, wk.b, wk.h, tok >> a.pl.log_p);
-          if (first >= 0) {
-            const long long at = (first + (tok & (a.pl.P - 1))) * D + c * 4;
-            kv = load4(k_pages + at);
-            vv = load4(v_pages + at);
-          }
+    sees_any = __syncthreads_or(sees_any);                         // (rows' bounds; where the first tile lies)
+    // the tiles that some row sees (of a segment's, those before all documents' starts and behind all rows' ends are passed over), and
+    // the keys that all rows see
+    int t_from = wk.t0, t_to = sees_any ? wk.t1 : wk.t0, all_lo, all_hi;
+    {
+      int lo = lo_s[0], hi = hi_s[rows - 1];                       // (both grow with the position, but for documents)
+      all_lo = lo_s[rows - 1];
+      all_hi = hi_s[0];
+      if (a.first_key) {
+        lo = 0x7fffffff;
+        for (int r = 0; r < rows; r += G) {
+          if (lo_s[r] < hi_s[r]) lo = min(lo, lo_s[r]);
+          all_lo = max(all_lo, lo_s[r]);
         }
-        *reinterpret_cast<float4*>(ks + j * LD + c * 4) = kv;
-        *reinterpret_cast<float4*>(vs + j * D + c * 4) = vv;
-        bad |= !(fabsf(vv.x) < INFINITY && fabsf(vv.y) < INFINITY && fabsf(vv.z) < INFINITY && fabsf(vv.w) < INFINITY);
       }
-      bad = __syncthreads_or(bad);
+      if (sees_any) {
+        t_from = max(t_from, lo / TK);
+        t_to = min(t_to, (hi + TK - 1) / TK);
+      }
+    }
+    if (t_from < t_to) {
+      if (t_from != wk.t0) {
+        find_rows(t_from);
+        __syncthreads();
+      }
+      fetch(k_pages, ks, LD, t_from);
+      fetch(v_pages, vs, D, t_from);
+    }
+#pragma unroll 1
+    for (int t = t_from; t < t_to; ++t) {
+      const int tok0 = t * TK;
+      const bool part = tok0 < all_lo || tok0 + TK > all_hi;       // some row does not see all of it
+      find_rows(t + 1);
+      copies_wait<1>();                                            // K is here
+      __syncthreads();
       // ---- scores of four rows x KT keys, this thread's share of the channels
       float2 acc[4][KT];
 #pragma unroll
@@ -144,7 +194,7 @@ __global__ void __launch_bounds__(kPgThreads, 2)
       float s[4][KT], mt[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int r = rg * 4 + i, lo = lo_s[r], hi = hi_s[r], pos = pos0 + r / G;
+        const int r = rg * 4 + i, pos = pos0 + r / G;
         mt[i] = -INFINITY;
 #pragma unroll
         for (int y = 0; y < KT; ++y) {
@@ -155,27 +205,28 @@ __global__ void __launch_bounds__(kPgThreads, 2)
           if (a.softcap > 0.f) v = a.softcap * tanhf(v * inv_cap);
           const int j = tok0 + kg + y * (TK / KT);
           if (slope[i] != 0.f) v -= slope[i] * (float)abs(pos - j);
-          s[i][y] = j >= lo && j < hi ? v * kLog2e : -INFINITY;
+          s[i][y] = !part || (j >= lo_s[r] && j < hi_s[r]) ? v * kLog2e : -INFINITY;
           mt[i] = fmaxf(mt[i], s[i][y]);
         }
       }
-      constexpr int kRowThreads = CS * (TK / KT);                  // 16 (R = 64: half a warp), 64 (two warps) or 256
+      constexpr int kRowThreads = CS * (TK / KT);                  // 16 (R >= 64: half a warp), 64 (two warps) or 256
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int w = kRowThreads < 32 ? kRowThreads / 2 : 16; w >= CS; w >>= 1) mt[i] = fmaxf(mt[i], __shfl_xor_sync(0xffffffffu, mt[i], w));
-      if constexpr (kRowThreads > 32) {                            // across the warps of a row group, through the score tile
-        constexpr int W = kRowThreads / 32;
-        const int w = tid / 32 % W;
+      constexpr int W = kRowThreads > 32 ? kRowThreads / 32 : 1;   // warps of a row group: their maxima meet in shared memory
+      if constexpr (W > 1) {
         if (tid % 32 == 0)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) ps[(rg * 4 + i) * LP + w] = mt[i];
-        __syncthreads();
+          for (int i = 0; i < 4; ++i) top_s[(rg * 4 + i) * 8 + tid / 32 % W] = mt[i];
+      }
+      __syncthreads();                                             // (K is used up; the maxima; where the next tile lies)
+      if (t + 1 < t_to) fetch(k_pages, ks, LD, t + 1); else copies_close();
+      if constexpr (W > 1) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int x = 0; x < W; ++x) mt[i] = fmaxf(mt[i], ps[(rg * 4 + i) * LP + x]);
-        __syncthreads();
+          for (int x = 0; x < W; ++x) mt[i] = fmaxf(mt[i], top_s[(rg * 4 + i) * 8 + x]);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -190,7 +241,16 @@ __global__ void __launch_bounds__(kPgThreads, 2)
           if (cs == 0) ps[(rg * 4 + i) * LP + kg + y * (TK / KT)] = p;
         }
       }
-      __syncthreads();
+      copies_wait<1>();                                            // V is here
+      bool bad = false;                                            // a value that is not finite, in a tile that some row does not see all of
+      if (part) {
+#pragma unroll
+        for (int x0 = 0; x0 < TK * D4; x0 += THREADS) {            // (what this thread has brought)
+          const float4 v = *reinterpret_cast<const float4*>(vs + (x0 + tid) * 4);
+          bad |= !(fabsf(v.x) < INFINITY && fabsf(v.y) < INFINITY && fabsf(v.z) < INFINITY && fabsf(v.w) < INFINITY);
+        }
+      }
+      bad = __syncthreads_or(bad);
       // ---- product with V: four rows x CW channels, every TS-th group of four tokens
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -232,7 +292,10 @@ __global__ void __launch_bounds__(kPgThreads, 2)
             for (int x = 0; x < CW; ++x) o[i][x] = fmaf(ps[r * LP + j], vs[j * D + x / 4 * (D * 4 / CW) + cg * 4 + x % 4], o[i][x]);
           }
       }
+      __syncthreads();                                             // (V and P are used up)
+      if (t + 1 < t_to) fetch(v_pages, vs, D, t + 1); else copies_close();
     }
+    copies_wait<0>();
     // ---- end of the segment: sums over the threads of a row, then over the token shares
     constexpr int kRowThreads = CS * (TK / KT);
 #pragma unroll
@@ -369,12 +432,13 @@ cudaError_t general_launch(const PagedAttend& a, const void* k, const void* v, c
   auto kern = paged_general_kernel<TQ, TKV, R, D>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, PgShape<R, D>::kBytes);
   if (e != cudaSuccess) return e;
-  return launch_ex(kern, dim3(a.w.n_cta), dim3(kPgThreads), PgShape<R, D>::kBytes, s, 0, true, a, reinterpret_cast<const TKV*>(k), reinterpret_cast<const TKV*>(v));
+  return launch_ex(kern, dim3(a.w.n_cta), dim3(PgShape<R, D>::THREADS), PgShape<R, D>::kBytes, s, 0, true, a, reinterpret_cast<const TKV*>(k), reinterpret_cast<const TKV*>(v));
 }
 template <typename TQ, typename TKV, int D>
 cudaError_t general_rows(const PagedAttend& a, const void* k, const void* v, cudaStream_t s) {
   const int r = a.w.ppos * a.pl.G;
-  return r <= 4 ? general_launch<TQ, TKV, 4, D>(a, k, v, s) : r <= 16 ? general_launch<TQ, TKV, 16, D>(a, k, v, s) : general_launch<TQ, TKV, 64, D>(a, k, v, s);
+  return r <= 4 ? general_launch<TQ, TKV, 4, D>(a, k, v, s) : r <= 16 ? general_launch<TQ, TKV, 16, D>(a, k, v, s)
+         : r <= 64 ? general_launch<TQ, TKV, 64, D>(a, k, v, s) : general_launch<TQ, TKV, 128, D>(a, k, v, s);
 }
 template <typename TQ, typename TKV>
 cudaError_t general_dim(const PagedAttend& a, const void* k, const void* v, cudaStream_t s) {
@@ -385,11 +449,11 @@ cudaError_t general_dim(const PagedAttend& a, const void* k, const void* v, cuda
 
 void paged_plan_general(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int window, int sm_count) {
   const int most = pb.max_new * pl.G;                              // rows that a sequence has for one KV head, at most
-  const int R = most <= 4 ? 4 : most <= 16 ? 16 : 64;
+  const int R = most <= 4 ? 4 : most <= 16 ? 16 : most <= 64 ? 64 : 128;
   w->ppos = w->upos = R / pl.G;
   w->log_tk = R == 64 ? 5 : 6;
   const long long tiles = (pb.max_len + (1 << w->log_tk) - 1) >> w->log_tk, units = (long long)pb.batch * pl.Hkv * paged_units(*w, pb.max_new);
-  constexpr int per_sm = 2;
+  const int per_sm = R == 128 ? 1 : 2;
   w->by_unit = tiles <= 4;
   w->min_tiles = w->by_unit ? 1 : 2;
   w->extra = 0;
