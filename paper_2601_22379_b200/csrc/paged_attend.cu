@@ -7,8 +7,8 @@
 // rows: scores from row pieces in shared memory (four rows x KT keys per thread, packed FMAs over two channels), then the
 // product with V (four rows x CW channels per thread, the tile's tokens shared by TS threads).  K of the next tile is on its way from
 // when the scores are done, V from when the product is done (asynchronous copies where the cache is fp32), the page table one tile ahead of that.
-// R = 4, 16, 64 and 128 by the rows that a unit has at most; a row tile's products cost the same however few of its rows are real.
-// 4 and 16 rows are bound by reading K and V, more by the FMA pipe.
+// R = 4, 16 and 64 by the rows that a unit has at most; a row tile's products cost the same however few of its rows are real.
+// 4 and 16 rows are bound by reading K and V, 64 by the FMA pipe (in use half of the time: the phases of a tile alternate with barriers).
 #include "paged.h"
 
 namespace spla {
@@ -17,12 +17,12 @@ namespace {
 
 template <int R, int D>
 struct PgShape {
-  static constexpr int THREADS = R == 128 ? 512 : 256;
+  static constexpr int THREADS = 256;
   static constexpr int TK = R == 64 ? 32 : 64;
-  static constexpr int KT = R == 128 ? 4 : R == 64 ? 2 : 1;        // keys per thread
+  static constexpr int KT = R == 64 ? 2 : 1;       // keys per thread
   static constexpr int RG = R / 4;                                 // groups of four rows
   static constexpr int CS = THREADS / (RG * (TK / KT));            // threads that share the channels of a score
-  static constexpr int CW = R >= 64 ? D / 16 : 4;                  // channels per thread in the product with V
+  static constexpr int CW = R == 64 ? D / 16 : 4;                  // channels per thread in the product with V
   static constexpr int TS = THREADS / (RG * (D / CW));             // threads that share a tile's tokens there
   static constexpr int LD = D + 4, LP = TK + 4;
   static constexpr int kQ = 0, kK = kQ + R * LD * 4, kV = kK + TK * LD * 4, kP = kV + TK * D * 4, kFac = kP + R * LP * 4, kLo = kFac + R * 4,
@@ -50,7 +50,7 @@ __device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<f
 __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) { *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)); }
 
 template <typename TQ, typename TKV, int R, int D>
-__global__ void __launch_bounds__((PgShape<R, D>::THREADS), R == 128 ? 1 : 2)
+__global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
     paged_general_kernel(const PagedAttend a, const TKV* __restrict__ k_pages, const TKV* __restrict__ v_pages) {
   using S = PgShape<R, D>;
   constexpr int THREADS = S::THREADS, TK = S::TK, KT = S::KT, CS = S::CS, CW = S::CW, TS = S::TS, LD = S::LD, LP = S::LP, D4 = D / 4;
@@ -209,7 +209,7 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), R == 128 ? 1 : 2)
           mt[i] = fmaxf(mt[i], s[i][y]);
         }
       }
-      constexpr int kRowThreads = CS * (TK / KT);                  // 16 (R >= 64: half a warp), 64 (two warps) or 256
+      constexpr int kRowThreads = CS * (TK / KT);                  // 16 (R = 64: half a warp), 64 (two warps) or 256
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -437,8 +437,7 @@ cudaError_t general_launch(const PagedAttend& a, const void* k, const void* v, c
 template <typename TQ, typename TKV, int D>
 cudaError_t general_rows(const PagedAttend& a, const void* k, const void* v, cudaStream_t s) {
   const int r = a.w.ppos * a.pl.G;
-  return r <= 4 ? general_launch<TQ, TKV, 4, D>(a, k, v, s) : r <= 16 ? general_launch<TQ, TKV, 16, D>(a, k, v, s)
-         : r <= 64 ? general_launch<TQ, TKV, 64, D>(a, k, v, s) : general_launch<TQ, TKV, 128, D>(a, k, v, s);
+  return r <= 4 ? general_launch<TQ, TKV, 4, D>(a, k, v, s) : r <= 16 ? general_launch<TQ, TKV, 16, D>(a, k, v, s) : general_launch<TQ, TKV, 64, D>(a, k, v, s);
 }
 template <typename TQ, typename TKV>
 cudaError_t general_dim(const PagedAttend& a, const void* k, const void* v, cudaStream_t s) {
@@ -449,11 +448,11 @@ cudaError_t general_dim(const PagedAttend& a, const void* k, const void* v, cuda
 
 void paged_plan_general(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int window, int sm_count) {
   const int most = pb.max_new * pl.G;                              // rows that a sequence has for one KV head, at most
-  const int R = most <= 4 ? 4 : most <= 16 ? 16 : most <= 64 ? 64 : 128;
+  const int R = most <= 4 ? 4 : most <= 16 ? 16 : 64;
   w->ppos = w->upos = R / pl.G;
   w->log_tk = R == 64 ? 5 : 6;
   const long long tiles = (pb.max_len + (1 << w->log_tk) - 1) >> w->log_tk, units = (long long)pb.batch * pl.Hkv * paged_units(*w, pb.max_new);
-  const int per_sm = R == 128 ? 1 : 2;
+  constexpr int per_sm = 2;
   w->by_unit = tiles <= 4;
   w->min_tiles = w->by_unit ? 1 : 2;
   w->extra = 0;
