@@ -369,48 +369,69 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
 }
 
 // Joins the partial results of a cut unit: the share before its first cut holds its head, the shares after hold the rest.
-// A CTA per cut, which finds nothing to do unless it is the first of its unit; a warp per row.
+// A CTA per cut, which finds nothing to do unless it is the first of its unit.  A warp per row, or several where there are fewer than
+// eight rows: each sums a run of the parts, the runs' sums meet in shared memory, in order.
 constexpr int kJoinThreads = 256;
 template <typename TO, int D>
 __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedAttend a) {
   __shared__ PagedSeqs seqs;
-  pdl_wait();
-  pdl_launch_dependents();
-  const int tid = threadIdx.x, lane = tid & 31, G = a.pl.G;
+  __shared__ float run_o[kJoinThreads / 32][D];
+  __shared__ float run_sum[kJoinThreads / 32];
+  // Lengths and tables are older than the kernel before (it waited for them before it let this one start): which unit this CTA joins
+  // is found while that one still runs.
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = a.pl.G;
   const long long total = paged_fill_seqs(a, seqs, tid, kJoinThreads), share = paged_share(a.w, total);
   const int cut = blockIdx.x + 1;                                  // the border between shares cut - 1 and cut
   const long long at = cut * share;
   PagedWalk wk;
-  if (!wk.seek(a, seqs, at, 1) || wk.off <= a.w.extra || wk.off - a.w.extra > share) return;   // no border between a unit's tiles, or not its first
+  const bool mine = wk.seek(a, seqs, at, 1) && wk.off > a.w.extra && wk.off - a.w.extra <= share;   // a border between a unit's tiles, its first
+  pdl_wait();
+  pdl_launch_dependents();
+  if (!mine) return;
   const int off = wk.off;
   wk.next(a, seqs);
   const int tiles = paged_unit_tiles(a, wk.row0, wk.n, wk.L, wk.prefix, wk.u_cur);
   const int parts = 1 + (int)((tiles - off + share - 1) / share);  // share cut - 1 (its second slot), then cut, cut + 1, ... (their first slots)
   const int i0 = wk.first_pos(a.w), rows = min(wk.n - i0, wk.n_pos(a.w)) * G;
   constexpr int V = D / 32;
-  for (int r = blockIdx.y * (kJoinThreads / 32) + (tid >> 5); r < rows; r += gridDim.y * (kJoinThreads / 32)) {
-    float M = -INFINITY;
-    for (int x = lane; x < parts; x += 32) {
-      const float2 ml = a.w.part_ml[(x == 0 ? 2LL * (cut - 1) + 1 : 2LL * (cut + x - 1)) * a.w.rows + r];
-      M = fmaxf(M, ml.x);
-    }
-    M = warp_max(M);
-    float o[V], sum = 0.f;
+  const int per_row = rows >= 8 ? 1 : rows >= 4 ? 2 : rows >= 2 ? 4 : 8, at_once = 8 / per_row;   // warps per row, rows at a time
+  const int run = warp % per_row, x0 = parts * run / per_row, x1 = parts * (run + 1) / per_row;
+  for (int r0 = blockIdx.y * at_once; r0 < rows; r0 += gridDim.y * at_once) {
+    const int r = r0 + warp / per_row;
+    float o[V], sum = 0.f, M = -INFINITY;
 #pragma unroll
     for (int x = 0; x < V; ++x) o[x] = 0.f;
-#pragma unroll 4
-    for (int x = 0; x < parts; ++x) {
-      const long long slot = (x == 0 ? 2LL * (cut - 1) + 1 : 2LL * (cut + x - 1)) * a.w.rows + r;
-      const float2 ml = a.w.part_ml[slot];
-      float v[V];
-      load_vec<V>(a.w.part_o + slot * D + lane * V, v);
-      const float w = ex2(ml.x - M);                               // (only where the part has seen a key: its output is 0 otherwise)
-      if (ml.y != 0.f) {
-        sum = fmaf(ml.y, w, sum);
+    if (r < rows) {
+      for (int x = lane; x < parts; x += 32) M = fmaxf(M, a.w.part_ml[(x == 0 ? 2LL * (cut - 1) + 1 : 2LL * (cut + x - 1)) * a.w.rows + r].x);
+      M = warp_max(M);
+#pragma unroll 8
+      for (int x = x0; x < x1; ++x) {
+        const long long slot = (x == 0 ? 2LL * (cut - 1) + 1 : 2LL * (cut + x - 1)) * a.w.rows + r;
+        const float2 ml = a.w.part_ml[slot];
+        float v[V];
+        load_vec<V>(a.w.part_o + slot * D + lane * V, v);
+        if (ml.y != 0.f) {                                         // (a part that has seen no key takes no part)
+          const float w = ex2(ml.x - M);
+          sum = fmaf(ml.y, w, sum);
 #pragma unroll
-        for (int y = 0; y < V; ++y) o[y] = fmaf(v[y], w, o[y]);
+          for (int y = 0; y < V; ++y) o[y] = fmaf(v[y], w, o[y]);
+        }
       }
     }
+    if (per_row > 1) {
+      __syncthreads();                                             // (the rows before have been read)
+#pragma unroll
+      for (int y = 0; y < V; ++y) run_o[warp][lane * V + y] = o[y];
+      if (lane == 0) run_sum[warp] = sum;
+      __syncthreads();
+      if (run > 0) continue;
+      for (int x = 1; x < per_row; ++x) {
+        sum += run_sum[warp + x];
+#pragma unroll
+        for (int y = 0; y < V; ++y) o[y] += run_o[warp + x][lane * V + y];
+      }
+    }
+    if (r >= rows) continue;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const long long row = (long long)(wk.row0 + i0 + r / G) * a.pl.Hq + wk.h * G + r % G;
 #pragma unroll
