@@ -44,11 +44,11 @@ struct PmSmem {
   static constexpr int NK = D == 128 ? 2 : 4, NV = (D == 128 ? 2 : 4) + (FEW ? (D == 128 ? 1 : 2) : 0);
   static constexpr int kQ = 0, kK = kQ + (FEW ? 1 : 2) * kTile, kV = kK + NK * kTile, kSeqs = kV + NV * kTile;
   static constexpr int kMl = kSeqs + (int)((sizeof(PagedSeqs) + 15) / 16 * 16);   // float2 [128]: maximum and sum of the second half, of a quarter
-  static constexpr int kWalk = kMl + 128 * 8;                     // PagedWalk [8]: where the softmax warps are
-  static constexpr int kStage = kWalk + 8 * 64;                   // [8 warps][32 rows][64 + 16 bytes], FEW [4 warps][8 rows][512 + 16] or fewer columns of more rows: rows on their way out
+  static constexpr int kSegs = kMl + 128 * 8;                     // PmSeg [4]: the segments that come next
+  static constexpr int kStage = kSegs + 4 * 96;                   // [8 warps][32 rows][64 + 16 bytes], FEW [4 warps][8 rows][512 + 16] or fewer columns of more rows: rows on their way out
   static constexpr int kStageRow = 80;
   static constexpr int kBars = kStage + 8 * 32 * 80;
-  static constexpr int kNumBars = 2 * NK + 2 * NV + 15;
+  static constexpr int kNumBars = 2 * NK + 2 * NV + 15 + 8;
   static constexpr int kMisc = kBars + kNumBars * 8;             // tensor-memory base, abort flag, skip flags [2], look-over marks [2][2]
   static constexpr int kBytes = kMisc + 48;
   static_assert(4 * 32 * 144 <= 8 * 32 * 80 && 4 * 16 * 272 <= 8 * 32 * 80 && 4 * 8 * 528 <= 8 * 32 * 80, "rows on their way out");
@@ -103,6 +103,15 @@ __device__ __forceinline__ PmPlan pm_plan(const PagedAttend& a, const PagedWalk&
   p.E = h0 && h1 ? max(p.e0, p.e1) : h0 ? p.e0 : p.e1;
   return p;
 }
+
+// One segment as the scheduling warp hands it to the other roles.
+struct PmSeg {
+  PmPlan pl;
+  int b, h, row0, n, L, prefix, first;             // first: its first new token, in the sequence
+  bool head, tail, end;                            // end: none is left
+};
+constexpr int kPmSegs = 4;
+static_assert(sizeof(PmSeg) <= 96, "a segment's place");
 
 // Warp-uniform bounded wait that also ends when another role has given up.
 __device__ __forceinline__ bool pm_wait_slow(uint64_t* bar, uint32_t parity, int limit, volatile int* abort_flag) {
@@ -173,7 +182,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + SM::kBars);
   uint64_t *k_full = bars, *k_empty = k_full + NK, *v_full = k_empty + NK, *v_empty = v_full + NV, *q_full = v_empty + NV, *q_empty = q_full + 1,
            *s_full = q_empty + 1, *p_ready = s_full + 2, *pv_done = p_ready + 2, *o_free = pv_done + 2, *scanned = o_free + 2, *halves = scanned + 2,
-           *quarters = halves + 1, *done = quarters + 1;
+           *quarters = halves + 1, *done = quarters + 1, *seg_full = done + 1, *seg_empty = seg_full + kPmSegs;
   uint32_t* tmem_base_s = reinterpret_cast<uint32_t*>(smem + SM::kMisc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SM::kMisc + 4);
   volatile int* skip_pv = reinterpret_cast<volatile int*>(smem + SM::kMisc + 8);    // [2]: this product with V has been formed by the softmax warps
@@ -197,6 +206,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
     mbar_init(halves, 4);
     mbar_init(quarters, 4);
     mbar_init(done, 1);
+    for (int s = 0; s < kPmSegs; ++s) { mbar_init(&seg_full[s], 1);  mbar_init(&seg_empty[s], 11); }   // K, V, MMA and eight softmax warps
     mbar_init_done();
     *abort_flag = 0;
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
@@ -213,12 +223,23 @@ __global__ void __launch_bounds__(kPmThreads, 1)
   const uint32_t sbase = smem_u32(smem);
   const int lim = a.wait_limit;
   const int ppos = a.w.ppos, G = a.pl.G;
-  PagedWalk wk;
-  const bool any = wk.seek(a, seqs, blockIdx.x * share, share);
+  PmSeg* segs = reinterpret_cast<PmSeg*>(smem + SM::kSegs);
+  // The CTA's segments, one after the other: the body returns false to give up.
+  auto each_segment = [&](bool& ok, auto body) {
+#pragma unroll 1
+    for (int i = 0; ok; ++i) {
+      if (!pm_wait(&seg_full[i % kPmSegs], (i / kPmSegs) & 1, lim, abort_flag)) { ok = false; break; }
+      const PmSeg& sg = segs[i % kPmSegs];
+      if (sg.end) break;
+      if (!body(sg)) { ok = false; break; }
+      __syncwarp();
+      if (lane == 0) mbar_arrive1(&seg_empty[i % kPmSegs]);
+    }
+  };
 
   if (wg == 0) {
     warpgroup_reg_dec<120>();                                     // (120 + 2 x 192 = 3 x 168, what the CTA is launched with)
-    if ((warp == 0 || warp == 2) && any) {
+    if (warp == 0 || warp == 2) {
       // ------------------------------------------------------------ TMA: queries and K, or V ----------------------------
       const bool is_k = warp == 0;
       const int NS = is_k ? NK : NV;
@@ -229,46 +250,48 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       const int n_rows = (int)((a.pl.n_pages - 1) * a.pl.page_stride + (a.pl.Hkv - 1) * a.pl.head_stride + P);   // (a box there reads zeros)
       int kt = 0, seg = 0;
       bool ok = true;
-      while (ok && wk.next(a, seqs)) {
-        const PmPlan pl = pm_plan(a, wk, lane);
-        if (pl.A >= pl.E) continue;
+      each_segment(ok, [&](const PmSeg& sg) {
+        const PmPlan pl = sg.pl;
+        if (pl.A >= pl.E) return true;
+        const int L = sg.L, b = sg.b, h = sg.h;
         // row of this lane's box in tile t; loaded a tile ahead
         auto box_row = [&](int t) {
           const int index = t * npg + pg;
           long long r = -1;
-          if (lane < boxes && t < pl.E && index * P < wk.L) r = paged_row(a.pb, a.pl, wk.b, wk.h, index);
+          if (lane < boxes && t < pl.E && index * P < L) r = paged_row(a.pb, a.pl, b, h, index);
           return r < 0 ? n_rows : (int)r;
         };
         int row = box_row(pl.A);
         if (is_k) {
-          if (seg > 0 && !pm_wait(q_empty, (seg - 1) & 1, lim, abort_flag)) { ok = false; break; }
+          if (seg > 0 && !pm_wait(q_empty, (seg - 1) & 1, lim, abort_flag)) return false;
           if (lane == 0) {
             const bool two = !pl.single && pl.items(1) > 0;
             const int boxes_q = FEW ? 4 : two ? 2 : 1;             // (four copies of the same rows, or the row tiles)
             mbar_expect_tx(q_full, boxes_q * H * ppos * G * 128 + (uint32_t)a.dbg_tx_extra);
             for (int s = 0; s < boxes_q; ++s)
               for (int x = 0; x < H; ++x)
-                tma_load_q(sbase + SM::kQ + s * (FEW ? 32 * 128 : SM::kTile) + x * SM::kHalf, &map_q, x, wk.h * G,
-                           wk.row0 + wk.first_pos(a.w) + (FEW ? 0 : s * ppos), q_full);
+                tma_load_q(sbase + SM::kQ + s * (FEW ? 32 * 128 : SM::kTile) + x * SM::kHalf, &map_q, x, h * G,
+                           sg.row0 + sg.first + (FEW ? 0 : s * ppos), q_full);
           }
         }
         ++seg;
         for (int t = pl.A; t < pl.E; ++t) {
           const int row_next = box_row(t + 1);
           const int st = kt % NS;
-          if (kt >= NS && !pm_wait(&empty[st], ((kt / NS) - 1) & 1, lim, abort_flag)) { ok = false; break; }
+          if (kt >= NS && !pm_wait(&empty[st], ((kt / NS) - 1) & 1, lim, abort_flag)) return false;
           if (lane == 0) mbar_expect_tx(&full[st], SM::kTile + (uint32_t)a.dbg_tx_extra);
           __syncwarp();
           if (lane < boxes) tma_load_box(dst + st * SM::kTile, map, hh * 64, row, &full[st]);
           ++kt;
           row = row_next;
         }
-      }
+        return true;
+      });
       if (!ok) *abort_flag = 1;
       // every copy has landed before the CTA leaves, whatever the other roles do
       for (int x = max(0, kt - NS); x < kt; ++x) warp_waits(&full[x % NS], (x / NS) & 1, lim);
       if (is_k && seg > 0) warp_waits(q_full, (seg - 1) & 1, lim);
-    } else if (warp == 1 && any) {
+    } else if (warp == 1) {
       // ------------------------------------------------------------ MMA issuer -----------------------------------------
       constexpr uint32_t id_s = umma_idesc(true, false, false, 128, kPmKeys);
       constexpr uint32_t id_o = umma_idesc(true, false, true, 128, D);
@@ -322,16 +345,16 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         (S ? free1 : free0) = last;
         (S ? look1 : look0) = pl.template look<S>(t);
       };
-      while (ok && wk.next(a, seqs)) {
-        const PmPlan pl = pm_plan(a, wk, lane);
-        if (pl.A >= pl.E) continue;
-        if (!pm_wait(q_full, seg & 1, lim, abort_flag)) { ok = false; break; }
+      each_segment(ok, [&](const PmSeg& sg) {
+        const PmPlan pl = sg.pl;
+        if (pl.A >= pl.E) return true;
+        if (!pm_wait(q_full, seg & 1, lim, abort_flag)) return false;
         ++seg;
         first0 = first1 = true;
 #pragma unroll 1
         for (int t = pl.A; t < pl.E; ++t) {
           const bool act0 = pl.act<0>(t), act1 = pl.act<1>(t);
-          if (!pm_wait(&k_full[kt % NK], (kt / NK) & 1, lim, abort_flag)) { ok = false; break; }
+          if (!pm_wait(&k_full[kt % NK], (kt / NK) & 1, lim, abort_flag)) return false;
           tc_fence_after();
           if (act0) {
             score(s0, pl, t, !act1);
@@ -346,17 +369,40 @@ __global__ void __launch_bounds__(kPmThreads, 1)
             umma_commit_one(one, &k_empty[kt % NK]);
             umma_commit_one(one, &v_empty[kt % NV]);
           }
-          if (!ok) break;
+          if (!ok) return false;
           ++kt;
         }
-        if (!ok) break;
         umma_commit_one(one, q_empty);
         if (pend0) product(s0);
         if (ok && pend1) product(s1);
-      }
+        return ok;
+      });
       umma_commit_one(one, done);
       if (!warp_waits(done, 0, lim)) ok = false;
       if (!ok) *abort_flag = 1;
+    } else {
+      // ------------------------------------------------------------ scheduling: the share's segments, ahead of their use ---
+      PagedWalk wk;
+      bool more = wk.seek(a, seqs, blockIdx.x * share, share);
+#pragma unroll 1
+      for (int i = 0;; ++i) {
+        more = more && wk.next(a, seqs);
+        PmSeg sg;
+        if (more) sg.pl = pm_plan(a, wk, lane);
+        if (i >= kPmSegs && !pm_wait(&seg_empty[i % kPmSegs], (i / kPmSegs - 1) & 1, lim, abort_flag)) { *abort_flag = 1; break; }
+        if (lane == 0) {
+          sg.end = !more;
+          if (more) {
+            sg.b = wk.b; sg.h = wk.h; sg.row0 = wk.row0; sg.n = wk.n; sg.L = wk.L; sg.prefix = wk.prefix;
+            sg.first = wk.first_pos(a.w);
+            sg.head = wk.head; sg.tail = wk.tail;
+          }
+          segs[i % kPmSegs] = sg;
+          mbar_arrive1(&seg_full[i % kPmSegs]);
+        }
+        __syncwarp();
+        if (!more) break;
+      }
     }
   } else {
     // -------------------------------------------------------------- softmax and epilogue: one row per thread -------------
@@ -369,12 +415,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
     const float sc2 = a.sm_scale * kLog2e;
     bool ok = true;
     int kt = 0, n = 0, n_scan = 0, n_half = 0, n_quarter = 0, n_used = 0;   // tiles of the CTA, items of this slot, look-overs, merges, segments that used O
-    // The walk lies in shared memory, a copy per warp: the loop over the tiles needs the registers.
-    PagedWalk& kept = *reinterpret_cast<PagedWalk*>(smem + SM::kWalk + (warp - 4) * 64);
-    static_assert(sizeof(PagedWalk) <= 64, "the walk's copy");
-    if (lane == 0) kept = wk;
-    __syncwarp();
-    while (any && ok) {
+    each_segment(ok, [&](const PmSeg& sg) {
       int t, t_end, t_step, la, le, k_base, my;                   // this slot's tiles, those seen whole, the tile counter's offset
       bool single, second, alike;
       PagedSees see{0x7fffffff, 0};
@@ -382,13 +423,10 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       int pos;
       float slope2 = 0.f;
       {
-        PagedWalk wk = kept;
-        __syncwarp();
-        if (!wk.next(a, seqs)) break;
-        const PmPlan pl = pm_plan(a, wk, lane);
+        const PmPlan pl = sg.pl;
         single = pl.single;
         second = single && pl.items(1) > 0;
-        alike = wk.n == 1;
+        alike = sg.n == 1;
         my = pl.items(slot);
         t = single ? pl.A + slot : slot ? pl.a1 : pl.a0;
         t_end = single ? pl.E : slot ? pl.e1 : pl.e0;
@@ -397,13 +435,11 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         le = single || !slot ? pl.le0 : pl.le1;
         k_base = kt - pl.A;
         kt += pl.E - pl.A;
-        const int i = wk.first_pos(a.w) + (single ? 0 : slot * ppos) + pi;
-        valid = row < ppos * G && i < wk.n;
-        if (valid || alike) see = paged_sees(a, wk.row0, wk.n, wk.L, wk.prefix, alike ? 0 : i);
-        if (MODS && a.slopes && valid) slope2 = __ldg(a.slopes + wk.h * G + g) * kLog2e;
-        pos = wk.L - wk.n + i;
-        if (lane == 0) kept = wk;
-        __syncwarp();
+        const int i = sg.first + (single ? 0 : slot * ppos) + pi;
+        valid = row < ppos * G && i < sg.n;
+        if (valid || alike) see = paged_sees(a, sg.row0, sg.n, sg.L, sg.prefix, alike ? 0 : i);
+        if (MODS && a.slopes && valid) slope2 = __ldg(a.slopes + sg.h * G + g) * kLog2e;
+        pos = sg.L - sg.n + i;
       }
       const bool live = __any_sync(0xffffffffu, valid);
       const bool counts = valid || alike;
@@ -415,13 +451,13 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         const int tok0 = t * kPmKeys, st = (uint32_t)(k_base + t) % NV;
         const bool look = t < la || t >= le;
         bool simt = false;
-        if (!pm_wait(&s_full[slot], n & 1, lim, abort_flag)) { ok = false; break; }
+        if (!pm_wait(&s_full[slot], n & 1, lim, abort_flag)) return false;
         if (look) {
           // (After the scores: they follow the row tile's product before, which waited for the V tiles up to two before this one, so that
           // the parity below can only mean this one.)
           // Values of this tile.  Where all rows see the same keys (single tokens) the rows of the others are zeroed; otherwise they are
           // looked over: zeroed behind the end where they are not finite, and elsewhere such a value makes the tile special.
-          if (!pm_wait(&v_full[st], ((uint32_t)(k_base + t) / NV) & 1, lim, abort_flag)) { ok = false; break; }
+          if (!pm_wait(&v_full[st], ((uint32_t)(k_base + t) / NV) & 1, lim, abort_flag)) return false;
           unsigned char* vt = smem + SM::kV + st * SM::kTile;
           bool bad = false;
           if (alike) {
@@ -442,7 +478,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
               for (int e = 0; e < 4; ++e) most = __hmax2_nan(most, __habs2(*reinterpret_cast<const __nv_bfloat162*>(&w[e])));
             }
             if (pair_not_finite(*reinterpret_cast<const uint32_t*>(&most))) {
-              const int L = kept.L;
+              const int L = sg.L;
 #pragma unroll 1
               for (int x = 0; x < SM::kTile / 2048; ++x) {
                 const uint4 v = *reinterpret_cast<const uint4*>(vt + x * 2048);
@@ -458,7 +494,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           if (__any_sync(0xffffffffu, bad) && lane == 0) found_bad[mark] = n_scan + 1;
           __syncwarp();
           if (lane == 0) mbar_arrive1(&scanned[slot]);
-          if (!pm_wait(&scanned[slot], n_scan & 1, lim, abort_flag)) { ok = false; break; }
+          if (!pm_wait(&scanned[slot], n_scan & 1, lim, abort_flag)) return false;
           simt = __any_sync(0xffffffffu, found_bad[mark] == n_scan + 1);
           ++n_scan;
         }
@@ -507,7 +543,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           const bool grow = mt > m + 8.f && m > -INFINITY;
           if (m == -INFINITY) m = mt;
           if (__any_sync(0xffffffffu, grow)) {
-            if (!pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) { ok = false; break; }   // every product with P so far
+            if (!pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) return false;   // every product with P so far
             tc_fence_after();
             const float m_new = grow ? mt : m, f = grow ? ex2(m - m_new) : 1.f;
             m = m_new;
@@ -548,8 +584,8 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         }
         if (simt) {
           // the product with V here: O += sum over the row's visible keys of p v
-          if (done_items > 0 && !pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) { ok = false; break; }
-          if (done_items == 0 && n_used > 0 && !pm_wait(&o_free[slot], (n_used - 1) & 1, lim, abort_flag)) { ok = false; break; }
+          if (done_items > 0 && !pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) return false;
+          if (done_items == 0 && n_used > 0 && !pm_wait(&o_free[slot], (n_used - 1) & 1, lim, abort_flag)) return false;
           tc_fence_after();
           const unsigned char* vt = smem + SM::kV + st * SM::kTile;
 #pragma unroll 1
@@ -600,12 +636,10 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         ++n;
         ++done_items;
       }
-      if (!ok) break;
       // ------------------------------------------------------------ end of the segment ----------------------------------
-      const PagedWalk wk = kept;
-      const bool whole = wk.head && wk.tail;
+      const bool whole = sg.head && sg.tail;
       if (my > 0) {
-        if (!pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) { ok = false; break; }
+        if (!pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) return false;
         tc_fence_after();
         ++n_used;
       }
@@ -617,7 +651,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           __syncwarp();
           if (lane == 0) mbar_arrive1(halves);
         } else {
-          if (!pm_wait(halves, n_half & 1, lim, abort_flag)) { ok = false; break; }
+          if (!pm_wait(halves, n_half & 1, lim, abort_flag)) return false;
           tc_fence_after();
           const float2 o = ml_s[thr];
           m1 = o.x;
@@ -625,7 +659,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         }
         ++n_half;
       }
-      if (single && slot == 1) continue;
+      if (single && slot == 1) return true;
       // O of both halves relative to the larger maximum; an empty half (no key seen) takes no part
       float M = fmaxf(m, m1);
       float f0 = l == 0.f ? 0.f : ex2(m - M), f1 = l1 == 0.f ? 0.f : ex2(m1 - M);
@@ -634,7 +668,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         ml_s[thr] = make_float2(M, sum);
         __syncwarp();
         if (lane == 0) mbar_arrive1(quarters);
-        if (!pm_wait(quarters, n_quarter & 1, lim, abort_flag)) { ok = false; break; }
+        if (!pm_wait(quarters, n_quarter & 1, lim, abort_flag)) return false;
         ++n_quarter;
         float top = -INFINITY, all = 0.f;
 #pragma unroll
@@ -652,22 +686,22 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       }
       const float inv = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
       const float w0 = f0 * inv, w1 = f1 * inv;
-      const int i0 = wk.first_pos(a.w) + (single ? 0 : slot * ppos);
-      const long long out_row = (long long)(wk.row0 + i0 + pi) * a.pl.Hq + wk.h * G + g;
-      const long long part_row = (2LL * blockIdx.x + (wk.head ? 1 : 0)) * a.w.rows + (single ? 0 : slot * ppos * G) + row;
+      const int i0 = sg.first + (single ? 0 : slot * ppos);
+      const long long out_row = (long long)(sg.row0 + i0 + pi) * a.pl.Hq + sg.h * G + g;
+      const long long part_row = (2LL * blockIdx.x + (sg.head ? 1 : 0)) * a.w.rows + (single ? 0 : slot * ppos * G) + row;
       if constexpr (FEW) {
         // The four warps' rows meet in shared memory, as many columns at a time as fit; a thread adds and writes 8 columns of a row.
-        const int n_rows = min(ppos, wk.n - i0) * G, cols = n_rows <= 8 ? (D < 128 ? D : 128) : n_rows <= 16 ? 64 : 32;
+        const int n_rows = min(ppos, sg.n - i0) * G, cols = n_rows <= 8 ? (D < 128 ? D : 128) : n_rows <= 16 ? 64 : 32;
         const int r_cap = n_rows <= 8 ? 8 : n_rows <= 16 ? 16 : 32, r_bytes = cols * 4 + 16, pieces = cols >> 3;
         unsigned char* stage = smem + SM::kStage;
         const int r = thr / pieces, piece = thr - r * pieces, ri = r / G;
-        const long long o_row = (long long)(wk.row0 + i0 + ri) * a.pl.Hq + wk.h * G + (r - ri * G);
+        const long long o_row = (long long)(sg.row0 + i0 + ri) * a.pl.Hq + sg.h * G + (r - ri * G);
 #pragma unroll 1
         for (int c0 = 0; c0 < D; c0 += cols) {
           if (c0 > 0) {                                           // (the columns before are out of the way)
             __syncwarp();
             if (lane == 0) mbar_arrive1(quarters);
-            if (!pm_wait(quarters, n_quarter & 1, lim, abort_flag)) { ok = false; break; }
+            if (!pm_wait(quarters, n_quarter & 1, lim, abort_flag)) return false;
             ++n_quarter;
           }
 #pragma unroll 1
@@ -688,7 +722,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           }
           __syncwarp();
           if (lane == 0) mbar_arrive1(quarters);
-          if (!pm_wait(quarters, n_quarter & 1, lim, abort_flag)) { ok = false; break; }
+          if (!pm_wait(quarters, n_quarter & 1, lim, abort_flag)) return false;
           ++n_quarter;
           if (r < n_rows) {
             float4 v0 = make_float4(0.f, 0.f, 0.f, 0.f), v1 = v0;
@@ -709,7 +743,6 @@ __global__ void __launch_bounds__(kPmThreads, 1)
             }
           }
         }
-        if (!ok) break;
         if (valid && (warp & 3) == 0) {
           if (!whole) a.w.part_ml[part_row] = make_float2(M, sum);
           else if (a.lse) a.lse[out_row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
@@ -724,10 +757,10 @@ __global__ void __launch_bounds__(kPmThreads, 1)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int r = r_first + 8 * k, ri = r / G;
-          const bool there = r < ppos * G && i0 + ri < wk.n;
+          const bool there = r < ppos * G && i0 + ri < sg.n;
           if (!there) dst[k] = nullptr;
           else if (whole)
-            dst[k] = reinterpret_cast<unsigned char*>(a.out) + ((long long)(wk.row0 + i0 + ri) * a.pl.Hq + wk.h * G + (r - ri * G)) * (D * 2) + piece * 16;
+            dst[k] = reinterpret_cast<unsigned char*>(a.out) + ((long long)(sg.row0 + i0 + ri) * a.pl.Hq + sg.h * G + (r - ri * G)) * (D * 2) + piece * 16;
           else
             dst[k] = reinterpret_cast<unsigned char*>(a.w.part_o) + (part_row + (r - row)) * (D * 4) + piece * 16;
         }
@@ -783,7 +816,8 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         if (my > 0) mbar_arrive1(&o_free[slot]);
         if (second) mbar_arrive1(&o_free[1]);
       }
-    }
+      return true;
+    });
     if (!ok) *abort_flag = 1;
   }
 
