@@ -71,6 +71,7 @@ struct PagedWork {
   int rows;                             // rows that a partial result holds
   float* part_o;                        // [2 n_cta][rows][d]
   float2* part_ml;                      // [2 n_cta][rows]  maximum (base 2), sum
+  int4* cuts;                           // [n_cta] of the unit whose first cut is the start of a share: rows (0: no such unit), parts, first row of its tokens, KV head
 };
 
 struct PagedAttend {
@@ -276,6 +277,14 @@ struct PagedWalk {
       u_cur = u++;
     } while (t0 == t1);                              // (a share's last bit, too short for a tile: the next share starts the unit)
     return true;
+  }
+  // What the join has to know of the cut at the start of share `cut`, `mine` = seek(), before next().
+  __device__ __forceinline__ int4 cut_here(const PagedAttend& a, bool mine, long long share) const {
+    // (a border between two tiles of the unit, and its first: the share before holds the unit's head)
+    if (!mine || off <= a.w.extra || off - a.w.extra > share) return make_int4(0, 0, 0, 0);
+    const int tiles = paged_unit_tiles(a, row0, n, L, prefix, u), i0 = u * a.w.upos;
+    const int parts = 1 + (int)((tiles - off + share - 1) / share);   // the share before (its second slot), then this one and those after (their first)
+    return make_int4(min(n - i0, n <= a.w.ppos ? a.w.ppos : a.w.upos) * a.pl.G, parts, row0 + i0, h);
   }
   int u_cur;                            // unit of the current segment
   __device__ __forceinline__ int first_pos(const PagedWork& w) const { return u_cur * w.upos; }   // index of its first new token in the sequence

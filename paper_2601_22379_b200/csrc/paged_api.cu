@@ -190,7 +190,17 @@ static size_t plan_attend(const spla_paged* p, const PagedBatch& pb, bool tensor
   if (tensor) paged_plan_mma(w, pb, p->pl, window, sms);
   else paged_plan_general(w, pb, p->pl, window, sms);
   if (w->by_unit || w->n_cta < 2) return 0;
-  return align_up((size_t)2 * w->n_cta * w->rows * p->pl.d * 4, 256) + align_up((size_t)2 * w->n_cta * w->rows * 8, 256);
+  const size_t rows = (size_t)2 * w->n_cta * w->rows;
+  return align_up(rows * p->pl.d * 4, 256) + align_up(rows * 8, 256) + align_up((size_t)w->n_cta * 16, 256);
+}
+// ... and their places in the workspace (no cuts: whole units only).
+static void place_parts(const spla_paged* p, size_t bytes, void* workspace, PagedWork* w) {
+  if (!bytes) return;
+  const size_t rows = (size_t)2 * w->n_cta * w->rows;
+  char* at = reinterpret_cast<char*>(workspace);
+  w->part_o = reinterpret_cast<float*>(at);
+  w->part_ml = reinterpret_cast<float2*>(at + align_up(rows * p->pl.d * 4, 256));
+  w->cuts = reinterpret_cast<int4*>(at + align_up(rows * p->pl.d * 4, 256) + align_up(rows * 8, 256));
 }
 
 static PagedBatch part_of(PagedBatch b, int first) {
@@ -270,9 +280,8 @@ extern "C" int spla_paged_attend(spla_paged_t* p, const spla_paged_batch_t* batc
   for (int first = 0; first < batch->batch && e == cudaSuccess; first += kPagedMaxBatch) {
     a.pb = part_of(pb, first);
     a.prefix = mask->prefix_lens ? mask->prefix_lens + first : nullptr;
-    plan_attend(p, a.pb, tensor, a.window, &a.w);
-    a.w.part_o = reinterpret_cast<float*>(workspace);
-    a.w.part_ml = reinterpret_cast<float2*>((char*)workspace + align_up((size_t)2 * a.w.n_cta * a.w.rows * p->pl.d * 4, 256));
+    a.w = PagedWork{};
+    place_parts(p, plan_attend(p, a.pb, tensor, a.window, &a.w), workspace, &a.w);
     e = tensor ? launch_paged_mma(a, maps, s) : launch_paged_general(a, p->k_pages, p->v_pages, q16, kv16, s);
     if (e == cudaSuccess) e = launch_paged_join(a, q16, s);
   }

@@ -72,7 +72,12 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
   const int tid = threadIdx.x, G = a.pl.G;
   const long long share = paged_share(a.w, paged_fill_seqs(a, seqs, tid, THREADS));
   PagedWalk wk;
-  if (!wk.seek(a, seqs, blockIdx.x * share, share)) return;
+  const bool any = wk.seek(a, seqs, blockIdx.x * share, share);
+  if (a.w.cuts && tid < 32) {
+    const int4 cut = wk.cut_here(a, any, share);
+    if (tid == 0) a.w.cuts[blockIdx.x] = cut;
+  }
+  if (!any) return;
   // scores: thread = (channel share, key, row group); product: (channel group, token share, row group)
   const int cs = tid % CS, kg = tid / CS % (TK / KT), rg = tid / (CS * (TK / KT));
   const int cg = tid % (D / CW), ts = tid / (D / CW) % TS, rp = tid / (D / CW * TS);
@@ -369,30 +374,45 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
 }
 
 // Joins the partial results of a cut unit: the share before its first cut holds its head, the shares after hold the rest.
-// A CTA per cut, which finds nothing to do unless it is the first of its unit.  A warp per row, or several where there are fewer than
-// eight rows: each sums a run of the parts, the runs' sums meet in shared memory, in order.
+// A few CTAs per cut, which find nothing to do unless it is the first of its unit.  32 rows and more (two or three parts, mostly): a thread
+// takes four channels of a row.  Fewer rows (many parts): a warp or several per row, each sums a run of the parts, the runs' sums
+// meet in shared memory, in order.
 constexpr int kJoinThreads = 256;
 template <typename TO, int D>
 __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedAttend a) {
-  __shared__ PagedSeqs seqs;
   __shared__ float run_o[kJoinThreads / 32][D];
   __shared__ float run_sum[kJoinThreads / 32];
-  // Lengths and tables are older than the kernel before (it waited for them before it let this one start): which unit this CTA joins
-  // is found while that one still runs.
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = a.pl.G;
-  const long long total = paged_fill_seqs(a, seqs, tid, kJoinThreads), share = paged_share(a.w, total);
-  const int cut = blockIdx.x + 1;                                  // the border between shares cut - 1 and cut
-  const long long at = cut * share;
-  PagedWalk wk;
-  const bool mine = wk.seek(a, seqs, at, 1) && wk.off > a.w.extra && wk.off - a.w.extra <= share;   // a border between a unit's tiles, its first
   pdl_wait();
   pdl_launch_dependents();
-  if (!mine) return;
-  const int off = wk.off;
-  wk.next(a, seqs);
-  const int tiles = paged_unit_tiles(a, wk.row0, wk.n, wk.L, wk.prefix, wk.u_cur);
-  const int parts = 1 + (int)((tiles - off + share - 1) / share);  // share cut - 1 (its second slot), then cut, cut + 1, ... (their first slots)
-  const int i0 = wk.first_pos(a.w), rows = min(wk.n - i0, wk.n_pos(a.w)) * G;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = a.pl.G;
+  const int cut = blockIdx.x + 1;                                  // the border between shares cut - 1 and cut
+  const int4 c = a.w.cuts[cut];
+  const int rows = c.x, parts = c.y;
+  if (rows == 0) return;
+  auto slot_of = [&](int x) { return x == 0 ? 2LL * (cut - 1) + 1 : 2LL * (cut + x - 1); };
+  auto out_row = [&](int r) { return (long long)(c.z + r / G) * a.pl.Hq + c.w * G + r % G; };
+  if (rows >= 32) {
+    for (int x = blockIdx.y * kJoinThreads + tid; x < rows * (D / 4); x += gridDim.y * kJoinThreads) {
+      const int r = x / (D / 4), ch = x % (D / 4) * 4;
+      float M = -INFINITY, sum = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int y = 0; y < parts; ++y) {                            // (the running maximum: one pass)
+        const long long at = slot_of(y) * a.w.rows + r;
+        const float2 ml = a.w.part_ml[at];
+        const float4 v = *reinterpret_cast<const float4*>(a.w.part_o + at * D + ch);
+        if (ml.y == 0.f) continue;                                 // (a part that has seen no key takes no part)
+        const float top = fmaxf(M, ml.x), f = M == top ? 1.f : ex2(M - top), w = ex2(ml.x - top);
+        M = top;
+        sum = fmaf(ml.y, w, sum * f);
+        o.x = fmaf(v.x, w, o.x * f); o.y = fmaf(v.y, w, o.y * f); o.z = fmaf(v.z, w, o.z * f); o.w = fmaf(v.w, w, o.w * f);
+      }
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      const long long row = out_row(r);
+      store4(reinterpret_cast<TO*>(a.out) + row * D + ch, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+      if (ch == 0 && a.lse) a.lse[row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+    }
+    return;
+  }
   constexpr int V = D / 32;
   const int per_row = rows >= 8 ? 1 : rows >= 4 ? 2 : rows >= 2 ? 4 : 8, at_once = 8 / per_row;   // warps per row, rows at a time
   const int run = warp % per_row, x0 = parts * run / per_row, x1 = parts * (run + 1) / per_row;
@@ -402,15 +422,15 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedAtt
 #pragma unroll
     for (int x = 0; x < V; ++x) o[x] = 0.f;
     if (r < rows) {
-      for (int x = lane; x < parts; x += 32) M = fmaxf(M, a.w.part_ml[(x == 0 ? 2LL * (cut - 1) + 1 : 2LL * (cut + x - 1)) * a.w.rows + r].x);
+      for (int x = lane; x < parts; x += 32) M = fmaxf(M, a.w.part_ml[slot_of(x) * a.w.rows + r].x);
       M = warp_max(M);
 #pragma unroll 8
       for (int x = x0; x < x1; ++x) {
-        const long long slot = (x == 0 ? 2LL * (cut - 1) + 1 : 2LL * (cut + x - 1)) * a.w.rows + r;
-        const float2 ml = a.w.part_ml[slot];
+        const long long at = slot_of(x) * a.w.rows + r;
+        const float2 ml = a.w.part_ml[at];
         float v[V];
-        load_vec<V>(a.w.part_o + slot * D + lane * V, v);
-        if (ml.y != 0.f) {                                         // (a part that has seen no key takes no part)
+        load_vec<V>(a.w.part_o + at * D + lane * V, v);
+        if (ml.y != 0.f) {
           const float w = ex2(ml.x - M);
           sum = fmaf(ml.y, w, sum);
 #pragma unroll
@@ -433,7 +453,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedAtt
     }
     if (r >= rows) continue;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const long long row = (long long)(wk.row0 + i0 + r / G) * a.pl.Hq + wk.h * G + r % G;
+    const long long row = out_row(r);
 #pragma unroll
     for (int y = 0; y < V; ++y) o[y] *= inv;
     TO* out = reinterpret_cast<TO*>(a.out) + row * D + lane * V;
@@ -488,11 +508,11 @@ cudaError_t launch_paged_general(const PagedAttend& a, const void* k, const void
 }
 
 cudaError_t launch_paged_join(const PagedAttend& a, int out_bf16, cudaStream_t s) {
-  if (a.w.by_unit || a.w.n_cta < 2) return cudaSuccess;
+  if (!a.w.cuts) return cudaSuccess;
   auto kern = a.pl.d == 128 ? (out_bf16 ? paged_join_kernel<__nv_bfloat16, 128> : paged_join_kernel<float, 128>)
                             : (out_bf16 ? paged_join_kernel<__nv_bfloat16, 64> : paged_join_kernel<float, 64>);
-  const int ys = (a.w.rows + 7) / 8;
-  return launch_ex(kern, dim3(a.w.n_cta - 1, ys < 8 ? ys : 8), dim3(kJoinThreads), 0, s, 0, true, a);
+  const int ys = a.w.rows >= 32 ? (a.w.rows * (a.pl.d / 4) + 2 * kJoinThreads - 1) / (2 * kJoinThreads) : (a.w.rows + 7) / 8;   // two items a thread at most, or a row a warp
+  return launch_ex(kern, dim3(a.w.n_cta - 1, ys < 16 ? ys : 16), dim3(kJoinThreads), 0, s, 0, true, a);
 }
 
 }  // namespace spla

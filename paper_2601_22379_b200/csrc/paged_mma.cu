@@ -384,6 +384,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       // ------------------------------------------------------------ scheduling: the share's segments, ahead of their use ---
       PagedWalk wk;
       bool more = wk.seek(a, seqs, blockIdx.x * share, share);
+      const int4 cut = a.w.cuts ? wk.cut_here(a, more, share) : make_int4(0, 0, 0, 0);
 #pragma unroll 1
       for (int i = 0;; ++i) {
         more = more && wk.next(a, seqs);
@@ -403,6 +404,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         __syncwarp();
         if (!more) break;
       }
+      if (a.w.cuts && lane == 0) a.w.cuts[blockIdx.x] = cut;
     }
   } else {
     // -------------------------------------------------------------- softmax and epilogue: one row per thread -------------
