@@ -81,56 +81,16 @@ __device__ __forceinline__ float2 turn_of(unsigned long long freq, int position,
 
 // VEC pairs per piece; both element types may occur in one launch with VEC = 1 only.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kRopeThreads)
+__global__ void __launch_bounds__(kRopeThreads, sizeof(T) == 4 ? 5 : 4)
     rope_kernel(const __grid_constant__ RopeLaunch r, const __grid_constant__ RopeTable rt) {
   constexpr int kWords = VEC == 1 ? 1 : 4;
   __shared__ __align__(16) float2 table[kRopeTable];      // [token][VEC pairs of piece 0, 1, ... two by two]
-  __shared__ const T* in_at[kRopeTokens][3];              // first head of the token, by group
-  __shared__ T* out_at[kRopeTokens][3];                   // (null: nothing is written)
+  __shared__ T* out_at[kRopeTokens][3];                   // pages: first head of the token, by group (null: nothing is written)
   __shared__ int tok_pos[kRopeTokens];
   pdl_wait();
   pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, pairs = rt.rot / 2;
-  const long long tok0 = (long long)blockIdx.x * r.tb;
-  const long long n_tok = (long long)r.batch * r.tokens;
-  const int nt = (int)min((long long)r.tb, n_tok - tok0);
-  if (r.paged && blockIdx.x == 0 && blockIdx.y == 0)      // every sequence's numbers are looked at once, those without tokens too
-    for (int b = tid; b < r.pb.batch; b += kRopeThreads) paged_seq(r.pb, r.pl.status, b);
-  static_assert(kRopeTokens <= kRopeThreads / 32, "a warp per token");
-  if (warp < nt) {
-    const long long tok = tok0 + warp;
-    int pos = 0;
-    bool there = true;
-    long long row = -1;                                   // page row of the token's position for head 0
-    if (r.paged) {
-      int at = -1;                                        // the last b with cu[b] <= tok
-      for (int b0 = 0; b0 < r.pb.batch; b0 += 32) {
-        const int b = b0 + lane;
-        const unsigned in = __ballot_sync(0xffffffffu, b < r.pb.batch && __ldg(r.pb.cu + b) <= tok);
-        at += __popc(in);
-        if (in != 0xffffffffu) break;
-      }
-      PagedSeq s{0, 0, 0};
-      if (at >= 0) s = paged_seq(r.pb, r.pl.status, at);
-      there = s.n > 0 && tok >= s.row0 && tok < s.row0 + s.n;
-      if (there) {
-        pos = s.L - s.n + (int)(tok - s.row0);
-        row = paged_row(r.pb, r.pl, at, 0, pos >> r.pl.log_p);
-        if (row >= 0) row += pos & (r.pl.P - 1);
-      }
-    }
-    if (lane < 3) {
-      const long long b = r.batch == 1 ? 0 : tok / r.tokens, i = tok - b * r.tokens;
-      const RopeGroup& g = r.g[lane];
-      in_at[warp][lane] = reinterpret_cast<const T*>(g.in) + b * g.in_batch + i * g.in_token;
-      T* out = nullptr;
-      if (g.out) { if (there) out = reinterpret_cast<T*>(g.out) + b * g.out_batch + i * g.out_token; }
-      else if (row >= 0) out = reinterpret_cast<T*>(lane == 1 ? r.k_pages : r.v_pages) + row * rt.dim;
-      out_at[warp][lane] = out;
-    }
-    if (lane == 0) tok_pos[warp] = r.positions && there ? __ldg(r.positions + tok) : pos;
-  }
-  __syncthreads();
+  const int tok0 = blockIdx.x * r.tb, nt = min(r.tb, r.tokens - tok0), batch = blockIdx.z;
   const int by = kRopeThreads / r.pieces, piece = tid % r.pieces, ty = tid / r.pieces;
   const int rot_pieces = pairs / VEC;
   const bool turns_here = piece < rot_pieces;
@@ -141,47 +101,77 @@ __global__ void __launch_bounds__(kRopeThreads)
   else { ca = piece * VEC; cb = ca + pairs; }
   const int end = ty < by ? min(nt * r.heads, ((int)blockIdx.y + 1) * r.rows_per_y) : 0;
   const int n0 = r.g[0].n_heads, n01 = n0 + r.g[1].n_heads;
-  const long long is0 = r.g[0].in_head, is1 = r.g[1].in_head, is2 = r.g[2].in_head;
-  const long long os0 = r.g[0].out_head, os1 = r.g[1].out ? r.g[1].out_head : r.pl.head_stride * rt.dim,
-                  os2 = r.g[2].out ? r.g[2].out_head : r.pl.head_stride * rt.dim;
 
   struct Place {
-    const T* in;
-    T* out;
-    int t;
-    bool rot;
+    int t, h, gi;                                         // token of the block, head of the group, group
   };
   auto place = [&](int row) {
     Place pl;
-    const int t = r.heads == 1 ? row : (int)__umulhi((unsigned)row, r.head_magic), h = row - t * r.heads;
-    const int gi = (h >= n0) + (h >= n01);
-    const int hg = h - (gi == 0 ? 0 : gi == 1 ? n0 : n01);
-    pl.t = t;
-    pl.in = in_at[t][gi] + hg * (gi == 0 ? is0 : gi == 1 ? is1 : is2);
-    pl.out = out_at[t][gi];
-    if (pl.out) pl.out += hg * (gi == 0 ? os0 : gi == 1 ? os1 : os2);
-    pl.rot = turns_here && (gi == 0 ? r.g[0].rotate : gi == 1 ? r.g[1].rotate : r.g[2].rotate);
+    pl.t = r.heads == 1 ? row : (int)__umulhi((unsigned)row, r.head_magic);
+    const int h = row - pl.t * r.heads;
+    pl.gi = (h >= n0) + (h >= n01);
+    pl.h = h - (pl.gi == 0 ? 0 : pl.gi == 1 ? n0 : n01);
     return pl;
   };
-  // two rows at a time; the first are on their way before the sines are formed
+  // two rows at a time; the first are on their way before the tokens' places and the sines are known
   int row = blockIdx.y * r.rows_per_y + ty;
   Place p0, p1;
   uint32_t x0[kWords], y0[kWords], x1[kWords], y1[kWords];
+  auto load = [&](const Place& pl, uint32_t (&x)[kWords], uint32_t (&y)[kWords]) {
+    const RopeGroup& g = pl.gi == 0 ? r.g[0] : pl.gi == 1 ? r.g[1] : r.g[2];
+    const T* in = reinterpret_cast<const T*>(g.in) + batch * g.in_batch + (long long)(tok0 + pl.t) * g.in_token + pl.h * g.in_head;
+    load_raw(in + ca, x);
+    load_raw(in + cb, y);
+  };
   auto fetch = [&]() {
-    p0.out = p1.out = nullptr;
     if (row < end) p0 = place(row);
     if (row + by < end) p1 = place(row + by);
-    if (p0.out) { load_raw(p0.in + ca, x0); load_raw(p0.in + cb, y0); }
-    if (p1.out) { load_raw(p1.in + ca, x1); load_raw(p1.in + cb, y1); }
+    if (row < end) load(p0, x0, y0);
+    if (row + by < end) load(p1, x1, y1);
   };
   fetch();
+  if (r.paged) {
+    if (blockIdx.x == 0 && blockIdx.y == 0)               // every sequence's numbers are looked at once, those without tokens too
+      for (int b = tid; b < r.pb.batch; b += kRopeThreads) paged_seq(r.pb, r.pl.status, b);
+    static_assert(kRopeTokens <= kRopeThreads / 32, "a warp per token");
+    if (warp < nt) {
+      const int tok = tok0 + warp;
+      int at = -1;                                        // the last b with cu[b] <= tok
+      for (int b0 = 0; b0 < r.pb.batch; b0 += 32) {
+        const int b = b0 + lane;
+        const unsigned in = __ballot_sync(0xffffffffu, b < r.pb.batch && __ldg(r.pb.cu + b) <= tok);
+        at += __popc(in);
+        if (in != 0xffffffffu) break;
+      }
+      PagedSeq s{0, 0, 0};
+      if (at >= 0) s = paged_seq(r.pb, r.pl.status, at);
+      const bool there = s.n > 0 && tok >= s.row0 && tok < s.row0 + s.n;
+      int pos = 0;
+      long long page_row = -1;                            // of the token's position for head 0
+      if (there) {
+        pos = s.L - s.n + (tok - s.row0);
+        page_row = paged_row(r.pb, r.pl, at, 0, pos >> r.pl.log_p);
+        if (page_row >= 0) page_row += pos & (r.pl.P - 1);
+      }
+      if (lane < 3) {
+        const RopeGroup& g = lane == 0 ? r.g[0] : lane == 1 ? r.g[1] : r.g[2];
+        T* out = nullptr;
+        if (g.out) { if (there) out = reinterpret_cast<T*>(g.out) + (long long)tok * g.out_token; }
+        else if (page_row >= 0) out = reinterpret_cast<T*>(lane == 1 ? r.k_pages : r.v_pages) + page_row * rt.dim;
+        out_at[warp][lane] = out;
+      }
+      if (lane == 0) tok_pos[warp] = r.positions && there ? __ldg(r.positions + tok) : pos;
+    }
+    __syncthreads();
+  }
   // entry of (token, pair): the pairs of a piece lie two by two, the pieces side by side, so that a warp's loads are contiguous
   if (pairs > 0) {
     const unsigned long long* freq = rt.freq;
     asm("" : "+l"(freq));                                 // (an ordinary load: a constant one takes a turn per thread)
     for (int x = tid; x < nt * pairs; x += kRopeThreads) {
       const int t = x / pairs, i = x - t * pairs;
-      const float2 cs = turn_of(freq[i], tok_pos[t], rt.amplitude, r.transpose != 0);
+      const int pos = r.paged ? tok_pos[t] : __ldg(r.positions + (long long)batch * r.tokens + tok0 + t);
+      const float2 cs = turn_of(freq[i], pos, rt.amplitude, r.transpose != 0);
       const int pc = i / VEC, j = i % VEC;
       const int e = VEC == 1 ? i : ((j >> 1) * rot_pieces + pc) * 2 + (j & 1);
       table[t * pairs + e] = cs;
@@ -192,7 +182,16 @@ __global__ void __launch_bounds__(kRopeThreads)
     float a[VEC], b[VEC];
     unpack<T, VEC>(x, a);
     unpack<T, VEC>(y, b);
-    if (pl.rot) {
+    const RopeGroup& g = pl.gi == 0 ? r.g[0] : pl.gi == 1 ? r.g[1] : r.g[2];
+    T* out;
+    if (r.paged) {
+      out = out_at[pl.t][pl.gi];
+      if (!out) return;
+      out += pl.h * (g.out ? g.out_head : r.pl.head_stride * rt.dim);
+    } else {
+      out = reinterpret_cast<T*>(g.out) + batch * g.out_batch + (long long)(tok0 + pl.t) * g.out_token + pl.h * g.out_head;
+    }
+    if (turns_here && g.rotate) {
       if constexpr (VEC == 1) {
         const float2 cs = table[pl.t * pairs + piece];
         const float x = a[0], y = b[0];
@@ -216,14 +215,12 @@ __global__ void __launch_bounds__(kRopeThreads)
         }
       }
     }
-    store_piece<VEC>(pl.out + ca, a);
-    store_piece<VEC>(pl.out + cb, b);
+    store_piece<VEC>(out + ca, a);
+    store_piece<VEC>(out + cb, b);
   };
-  while (p0.out || p1.out || row < end) {
-    if (p0.out) finish(p0, x0, y0);
-    if (p1.out) finish(p1, x1, y1);
-    row += 2 * by;
-    fetch();
+  for (; row < end; row += 2 * by, fetch()) {
+    finish(p0, x0, y0);
+    if (row + by < end) finish(p1, x1, y1);
   }
 }
 
@@ -240,22 +237,36 @@ cudaError_t rope_launch(RopeLaunch r, const RopeTable& rt, int sm_count, cudaStr
   r.head_magic = (unsigned)(((1ull << 32) + r.heads - 1) / r.heads);
   const int pairs = rt.rot / 2;
   // tokens per block: a full table's worth, so that every thread forms one or two sines; fewer where that would leave SMs idle
-  const long long n_tok = (long long)r.batch * r.tokens;
   int tb = pairs > 0 ? kRopeThreads / pairs : kRopeTokens;
   if (tb < 1) tb = 1;
   if (tb > kRopeTokens) tb = kRopeTokens;
-  while (tb > 1 && (n_tok + tb - 1) / tb < 2LL * sm_count) tb /= 2;
+  auto blocks = [&](int x) { return (long long)((r.tokens + x - 1) / x) * r.batch; };
+  while (tb > 1 && blocks(tb) < 2LL * sm_count) tb /= 2;
+  if (tb > r.tokens) tb = r.tokens;
   r.tb = tb;
-  const long long blocks = (n_tok + tb - 1) / tb;
   const int by = kRopeThreads / r.pieces, rows = tb * r.heads;
   int ys = 1;
-  if (blocks < 2LL * sm_count) {
+  if (blocks(tb) < 2LL * sm_count) {
     ys = (rows + by - 1) / by;
-    const long long most = (4LL * sm_count + blocks - 1) / blocks;
+    const long long most = (4LL * sm_count + blocks(tb) - 1) / blocks(tb);
     if (ys > most) ys = (int)most;
   }
   r.rows_per_y = (rows + ys - 1) / ys;
-  return launch_ex(rope_kernel<T, VEC>, dim3((unsigned)blocks, (rows + r.rows_per_y - 1) / r.rows_per_y), dim3(kRopeThreads), 0, s, 0, true, r, rt);
+  // (the grid's third dimension ends at 65535)
+  const int batch = r.batch;
+  cudaError_t e = cudaSuccess;
+  for (int b = 0; b < batch && e == cudaSuccess; b += 65535) {
+    RopeLaunch part = r;
+    part.batch = batch - b < 65535 ? batch - b : 65535;
+    if (r.positions) part.positions = r.positions + (long long)b * r.tokens;
+    for (RopeGroup& g : part.g) {
+      if (g.in) g.in = (const char*)g.in + b * g.in_batch * (long long)sizeof(T);
+      if (g.out) g.out = (char*)g.out + b * g.out_batch * (long long)sizeof(T);
+    }
+    e = launch_ex(rope_kernel<T, VEC>, dim3((r.tokens + tb - 1) / tb, (rows + r.rows_per_y - 1) / r.rows_per_y, part.batch), dim3(kRopeThreads), 0, s, 0,
+                  true, part, rt);
+  }
+  return e;
 }
 
 }  // namespace
@@ -282,6 +293,18 @@ cudaError_t launch_rope(const RopeTable& rt, const int* positions, int batch, in
       r.heads += r.g[i].n_heads;
     }
     if (r.heads == 0) continue;
+    // a batch whose tokens follow one another, or of one token each, is one list of tokens
+    r.batch = batch;
+    r.tokens = tokens;
+    bool list = batch > 1 && (long long)batch * tokens < (1ll << 31);
+    for (int i = 0; i < 3 && list; ++i)
+      if (r.g[i].n_heads > 0) list = tokens == 1 || (r.g[i].in_batch == tokens * r.g[i].in_token && r.g[i].out_batch == tokens * r.g[i].out_token);
+    if (list) {
+      for (RopeGroup& g : r.g)
+        if (tokens == 1) { g.in_token = g.in_batch; g.out_token = g.out_batch; }
+      r.tokens = batch * tokens;
+      r.batch = 1;
+    }
     if (f32) e = fast ? rope_launch<float, 4>(r, rt, sm, s) : rope_launch<float, 1>(r, rt, sm, s);
     else e = fast ? rope_launch<__nv_bfloat16, 8>(r, rt, sm, s) : rope_launch<__nv_bfloat16, 1>(r, rt, sm, s);
   }
