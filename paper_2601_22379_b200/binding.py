@@ -535,7 +535,7 @@ class PagedCache:
         if q is not None:
             qs = self._rows(q, total, self.n_q_heads, self.q_torch_dtype, "q")
             if q_out is None:
-                q_out = q.new_empty(q.shape)
+                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
             os_ = self._rows(q_out, total, self.n_q_heads, self.q_torch_dtype, "q_out")
             qp, op = q.data_ptr(), q_out.data_ptr()
         if positions is not None and not (positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == total
@@ -560,7 +560,7 @@ class PagedCache:
         total, hq, dev = q.shape[0], self.n_q_heads, self.device
         qs = self._rows(q, total, hq, self.q_torch_dtype, "q")
         if out is None:
-            out = q.new_empty(q.shape)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif not (out.shape == q.shape and out.dtype == q.dtype and out.device == dev and out.is_contiguous()):
             raise ValueError("paged cache: a contiguous out like q")
         if lse is None:

@@ -124,7 +124,7 @@ extern "C" int spla_paged_create(const spla_paged_config_t* c, void* k_pages, vo
   p->k_pages = k_pages;
   p->v_pages = v_pages;
   if (p->cfg.sm_scale == 0.f) p->cfg.sm_scale = 1.0f / sqrtf((float)c->head_dim);
-  p->sm_count = 0;
+  p->sm_count = device_sm_count();
   // the tensor-core kernel: bf16, rows that a TMA coordinate can name
   const int64_t rows = (c->n_pages - 1) * ps + (c->n_kv_heads - 1) * hs + P;
   p->tensor = c->kv_dtype == SPLA_BF16 && c->q_dtype == SPLA_BF16 && !(c->flags & SPLA_GENERAL_KERNELS) && rows < (1ll << 31) - 256 &&
@@ -186,9 +186,8 @@ extern "C" int spla_paged_append(spla_paged_t* p, const spla_paged_batch_t* batc
 
 // The plan of one launch (a batch of at most kPagedMaxBatch sequences) and the bytes of its partial results.
 static size_t plan_attend(const spla_paged* p, const PagedBatch& pb, bool tensor, int window, PagedWork* w) {
-  const int sms = p->sm_count ? p->sm_count : device_sm_count();
-  if (tensor) paged_plan_mma(w, pb, p->pl, window, sms);
-  else paged_plan_general(w, pb, p->pl, window, sms);
+  if (tensor) paged_plan_mma(w, pb, p->pl, window, p->sm_count);
+  else paged_plan_general(w, pb, p->pl, window, p->sm_count);
   if (w->by_unit || w->n_cta < 2) return 0;
   const size_t rows = (size_t)2 * w->n_cta * w->rows;
   return align_up(rows * p->pl.d * 4, 256) + align_up(rows * 8, 256) + align_up((size_t)w->n_cta * 16, 256);

@@ -471,7 +471,8 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedAtt
 template <typename TQ, typename TKV, int R, int D>
 cudaError_t general_launch(const PagedAttend& a, const void* k, const void* v, cudaStream_t s) {
   auto kern = paged_general_kernel<TQ, TKV, R, D>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, PgShape<R, D>::kBytes);
+  static unsigned long long allowed = 0;
+  cudaError_t e = allow_smem_once(kern, PgShape<R, D>::kBytes, allowed);
   if (e != cudaSuccess) return e;
   return launch_ex(kern, dim3(a.w.n_cta), dim3(PgShape<R, D>::THREADS), PgShape<R, D>::kBytes, s, 0, true, a, reinterpret_cast<const TKV*>(k), reinterpret_cast<const TKV*>(v));
 }

@@ -838,7 +838,8 @@ template <int D, bool MODS, bool FEW>
 cudaError_t mma_launch(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
   auto kern = paged_mma_kernel<D, MODS, FEW>;
   constexpr int bytes = PmSmem<D, FEW>::kBytes;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  static unsigned long long allowed = 0;
+  cudaError_t e = allow_smem_once(kern, bytes, allowed);
   if (e != cudaSuccess) return e;
   return launch_ex(kern, dim3(a.w.n_cta), dim3(kPmThreads), bytes, s, 0, true, a, *reinterpret_cast<const CUtensorMap*>(maps.k),
                    *reinterpret_cast<const CUtensorMap*>(maps.v), *reinterpret_cast<const CUtensorMap*>(maps.q));

@@ -47,6 +47,19 @@ inline cudaError_t launch_ex(void (*kern)(KArgs...), dim3 grid, dim3 block, size
   return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
 }
 
+// Lets a kernel take more than 48 KB of dynamic shared memory: asked for once per device and kernel (a call costs about 0.3 us).
+template <typename K>
+inline cudaError_t allow_smem_once(K kern, int bytes, unsigned long long& devices) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (__atomic_load_n(&devices, __ATOMIC_RELAXED) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev < 64) __atomic_fetch_or(&devices, bit, __ATOMIC_RELAXED);
+  return e;
+}
+
 // How many clusters of `cluster_x` CTAs of this kernel the device holds at once (all CTAs of a cluster sit in one
 // GPC, so this is less than CTA slots / cluster size); -1 if the query fails.
 template <typename... KArgs>
