@@ -315,8 +315,8 @@ typedef struct {
 
 typedef struct spla_rope spla_rope_t; /* opaque host-side table of frequencies */
 
-/* HOST pointers; no device memory is involved.  The frequencies are computed in double precision and kept as 64-bit
- * fractions of a turn, so that the angle of a position is exact modulo whole turns up to 2^31 (to 2^-64 of a turn per position). */
+/* HOST pointers; no device memory is involved.  The frequencies are computed in double precision and kept as 64-bit fractions of a
+ * turn: position x frequency loses nothing on the way to the angle modulo a turn, however far the position. */
 int spla_rope_create(const spla_rope_config_t *config, spla_rope_t **rope_out);
 int spla_rope_destroy(spla_rope_t *rope);   /* NULL is allowed */
 
@@ -368,7 +368,8 @@ int spla_paged_destroy(spla_paged_t *paged);   /* NULL is allowed */
  * seq_lens[b] - n_b ..; seq_lens counts them.  Rows from cu_new[batch] on are not touched.  Position x of sequence b lies in page
  * page_table[b * table_stride + x / P].  A sequence whose numbers are not consistent (cu_new not ascending inside [0, total_new],
  * n_b > max_new, seq_lens[b] < n_b or > max_len) is skipped, its rows are not touched, and SPLA_ERR_BOUNDS is latched.  The
- * tokens of a page number outside [0, n_pages) are not stored, read as zeros, and latch SPLA_ERR_BOUNDS.
+ * tokens of a page number outside [0, n_pages) are not stored, read as zeros, and latch SPLA_ERR_BOUNDS.  Sequences may share
+ * pages that they read; a position that is written belongs to one sequence.
  */
 typedef struct {
   const int32_t *cu_new;      /* DEVICE [batch + 1] */
@@ -397,7 +398,7 @@ int spla_paged_append(spla_paged_t *paged, const spla_paged_batch_t *batch, cons
  *   s = sm_scale q.k;  softcap > 0: s = softcap tanh(s / softcap);  slopes: s -= slopes[head] |p - j|.
  * Visible are the j with max(0, p - window + 1, first_key) <= j < min(seq_len, max(p + 1, prefix_len)). */
 typedef struct {
-  float softcap;               /* 0: none */
+  float softcap;               /* 0: none; else at least 1e-6 */
   int32_t window;              /* 0: none; else the last `window` positions, the query's own among them */
   const float *slopes;         /* DEVICE fp32 [H_q] or NULL */
   const int32_t *first_key;    /* DEVICE int32 [total_new] or NULL: where the document of each new token starts */
@@ -424,6 +425,9 @@ int spla_paged_attend(spla_paged_t *paged, const spla_paged_batch_t *batch, cons
 
 /* As spla_sync_status, for the status word of `paged`. */
 int spla_paged_sync_status(spla_paged_t *paged, void *stream);
+
+/* As spla_debug_wait_hook, for the tensor-core kernel of spla_paged_attend. */
+int spla_paged_debug_wait_hook(spla_paged_t *paged, int32_t max_wait_polls, int32_t extra_expected_bytes);
 
 /* Static, NUL-terminated description of a status code. */
 const char *spla_status_string(int status);

@@ -26,6 +26,7 @@ EXPORTS = ["spla_query_sizes", "spla_init_cache", "spla_append_tokens", "spla_de
            "spla_copy_scores", "spla_sync_status", "spla_set_length_bound", "spla_debug_wait_hook", "spla_destroy_cache",
            "spla_rope_create", "spla_rope_destroy", "spla_rope_apply", "spla_paged_create", "spla_paged_destroy",
            "spla_paged_append", "spla_paged_query_workspace", "spla_paged_attend", "spla_paged_sync_status",
+           "spla_paged_debug_wait_hook",
            "spla_launch_count", "spla_status_string", "spla_last_cuda_error"]
 
 
@@ -120,6 +121,7 @@ def load(path: str | None = None) -> C.CDLL:
     lib.spla_paged_query_workspace.argtypes = [vp, vp, C.POINTER(C.c_size_t)]
     lib.spla_paged_attend.argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, C.c_size_t, vp]
     lib.spla_paged_sync_status.argtypes = [vp, vp]
+    lib.spla_paged_debug_wait_hook.argtypes = [vp, i32, i32]
     for name in EXPORTS[:-3]:
         getattr(lib, name).restype = C.c_int
     lib.spla_launch_count.argtypes = []
@@ -589,6 +591,10 @@ class PagedCache:
 
     def sync_status(self) -> int:
         return _on(self.index, self.lib.spla_paged_sync_status, self.handle)
+
+    def debug_wait_hook(self, max_wait_polls: int, extra_expected_bytes: int):
+        """Test hook, as SplaCache.debug_wait_hook: waits of the tensor-core attention that run out."""
+        _check(self.lib.spla_paged_debug_wait_hook(self.handle, max_wait_polls, extra_expected_bytes), "spla_paged_debug_wait_hook")
 
     def close(self):
         if getattr(self, "handle", None) is not None and self.handle.value:

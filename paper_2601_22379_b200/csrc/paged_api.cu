@@ -246,7 +246,7 @@ extern "C" int spla_paged_attend(spla_paged_t* p, const spla_paged_batch_t* batc
   spla_paged_mask_t none;
   memset(&none, 0, sizeof(none));
   if (!mask) mask = &none;
-  if (!(mask->softcap >= 0.f) || !isfinite(mask->softcap) || mask->window < 0) return SPLA_ERR_INVALID_ARG;
+  if (!(mask->softcap >= 0.f) || !isfinite(mask->softcap) || (mask->softcap > 0.f && mask->softcap < 1e-6f) || mask->window < 0) return SPLA_ERR_INVALID_ARG;
   if ((mask->slopes && !aligned(mask->slopes, 4)) || (mask->first_key && !aligned(mask->first_key, 4)) || (mask->prefix_lens && !aligned(mask->prefix_lens, 4)))
     return SPLA_ERR_INVALID_ARG;
   size_t need = 0;
@@ -296,4 +296,11 @@ extern "C" int spla_paged_sync_status(spla_paged_t* p, void* stream) {
   if (e == cudaSuccess && st != 0) e = cudaMemsetAsync(p->pl.status, 0, sizeof(int), s);
   if (e != cudaSuccess) return cuda_fail(e, "spla_paged_sync_status");
   return st;
+}
+
+extern "C" int spla_paged_debug_wait_hook(spla_paged_t* p, int32_t max_wait_polls, int32_t extra_expected_bytes) {
+  if (!p || max_wait_polls < 0 || extra_expected_bytes < 0 || (extra_expected_bytes % 16)) return SPLA_ERR_INVALID_ARG;
+  p->wait_limit = max_wait_polls;
+  p->dbg_tx_extra = extra_expected_bytes;
+  return SPLA_OK;
 }

@@ -513,10 +513,23 @@ __global__ void __launch_bounds__(kPmThreads, 1)
             tmem_ld128(tS, r);
           }
           if constexpr (MODS) {
-            if (a.softcap > 0.f) {                                // cap tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap)), in base 2
+            if (a.softcap > 0.f) {
+              // cap tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap)), in base 2: off by some 2^-22 cap, whatever x is.  Where that is much
+              // (caps far above the scores) small x / cap go by the series instead: u - u^3 / 3 + 2 u^5 / 15 - 17 u^7 / 315.
               const float k1 = 2.f * sc2 / a.softcap, c2 = a.softcap * kLog2e;
+              if (a.softcap <= 64.f) {
 #pragma unroll
-              for (int x = 0; x < KEYS; ++x) r[x] = __float_as_uint(fmaf(-2.f * c2, rcp_approx(1.f + ex2(__uint_as_float(r[x]) * k1)), c2));
+                for (int x = 0; x < KEYS; ++x) r[x] = __float_as_uint(fmaf(-2.f * c2, rcp_approx(1.f + ex2(__uint_as_float(r[x]) * k1)), c2));
+              } else {
+                const float to_u = a.sm_scale / a.softcap;
+#pragma unroll
+                for (int x = 0; x < KEYS; ++x) {
+                  const float sx = __uint_as_float(r[x]), u = sx * to_u, u2 = u * u;
+                  const float series = fmaf(u2, fmaf(u2, fmaf(u2, -17.f / 315.f, 2.f / 15.f), -1.f / 3.f), 1.f) * u * c2;
+                  const float closed = fmaf(-2.f * c2, rcp_approx(1.f + ex2(sx * k1)), c2);
+                  r[x] = __float_as_uint(fabsf(u) < 0.125f ? series : closed);
+                }
+              }
             } else {
 #pragma unroll
               for (int x = 0; x < KEYS; ++x) r[x] = __float_as_uint(__uint_as_float(r[x]) * sc2);

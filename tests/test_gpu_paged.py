@@ -102,6 +102,77 @@ def test_masks(kv, q, flags, mask, d):
 
 
 @kinds
+@pytest.mark.parametrize("mask", ["cap", "cap-high", "slopes", "window", "documents", "prefix", "all"])
+@pytest.mark.parametrize("hq,d", [(4, 128), (16, 64), (10, 64)])
+def test_masks_of_few_tokens(kv, q, flags, mask, hq, d):
+    """The same where no sequence has more than three new tokens."""
+    b = Batch([1, 2, 3, 1, 0, 1], [400, 300, 0, 65, 31, 1000], hq=hq, hkv=2, d=d, P=32, kv=kv, q=q, flags=flags, extra_cols=2)
+    first = torch.tensor([200, 10000, 290, 1, -5, 2, 66, 999], dtype=torch.int32)
+    slopes = torch.arange(hq) % 4 * 0.25
+    kw = {"cap": dict(softcap=5.0), "cap-high": dict(softcap=3000.0), "slopes": dict(slopes=slopes), "window": dict(window=37), "documents": dict(first_key=first),
+          "prefix": dict(prefix_lens=torch.tensor([0, 340, 5, 10000, 3, 100], dtype=torch.int32)),
+          "all": dict(softcap=8.0, slopes=slopes, window=90, first_key=first, prefix_lens=torch.tensor([390, 350, 7, 0, 0, 60], dtype=torch.int32))}[mask]
+    b.run(**kw)
+
+
+@kinds
+def test_cold_and_busy(kv, q, flags):
+    """The same bits whether the inputs are in the cache or not, whatever the scratch held before."""
+    batches = [Batch([1, 1, 2, 130], [20000, 17, 5001, 9000], hq=8, hkv=2, d=128, P=64, kv=kv, q=q, flags=flags),
+               Batch([1, 1, 2, 3], [9000, 17, 5001, 300], hq=8, hkv=2, d=128, P=64, kv=kv, q=q, flags=flags),
+               Batch([200, 170, 300], [1000, 300, 0], hq=8, hkv=2, d=64, P=16, kv=kv, q=q, flags=flags)]
+    flush = torch.empty(200 << 20, dtype=torch.uint8, device=DEV)
+    first = [b.run() for b in batches]
+    for it in range(30):
+        for b, (o, l) in zip(batches, first):
+            if it % 3 == 1:
+                flush.fill_(it)
+            torch.full((8 << 20,), math.nan, device=DEV)
+            out, lse = b.attend()
+            assert torch.equal(out, o) and torch.equal(lse, l), it
+
+
+def test_waits_that_run_out():
+    """Copies that never complete: the kernel gives up, reports it, and works again afterwards."""
+    for new in ([1, 2], [150, 40]):
+        b = Batch(new, [500, 900], hq=8, hkv=2, d=128, kv="bf16")
+        want, want_lse = b.run()
+        b.cache.debug_wait_hook(1 << 14, 16)
+        b.attend()
+        assert b.cache.sync_status() == binding.SPLA_ERR_TIMEOUT
+        b.cache.debug_wait_hook(0, 0)
+        out, lse = b.attend()
+        assert b.cache.sync_status() == 0 and torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "f32"])
+def test_offsets_past_32_bits(kv):
+    """A pool of more than 2^32 elements, the sequences in its last pages and its first."""
+    t = TYPES[kv]
+    hkv, P, d = 8, 128, 128
+    n_pages = (1 << 32) // (hkv * P * d) + 7
+    kp, vp = (torch.empty(n_pages, hkv, P, d, dtype=t, device=DEV) for _ in range(2))
+    table = torch.tensor([[n_pages - 1, 0, n_pages - 2], [n_pages - 3, n_pages - 4, 5]], dtype=torch.int32)
+    lens, new = [300, 260], [300, 260]
+    g = torch.Generator().manual_seed(2)
+    k, v, q = (torch.randn(560, h, d, generator=g).to(t) for h in (hkv, hkv, 16))
+    cu, ln, tb = torch.tensor([0, 300, 560], dtype=torch.int32, device=DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), table.to(DEV)
+    cache = binding.PagedCache(kp, vp, n_q_heads=16)
+    cache.append(k.to(DEV), v.to(DEV), cu, ln, tb)
+    out, lse = cache.attend(q.to(DEV), cu, ln, tb, 300, 300)
+    assert cache.sync_status() == 0
+    small_k, small_v = torch.zeros(6, hkv, P, d, dtype=t), torch.zeros(6, hkv, P, d, dtype=t)
+    own = torch.arange(6, dtype=torch.int32).view(2, 3)
+    for s in range(2):
+        j = torch.arange(lens[s])
+        small_k[own[s].long()[j // P], :, j % P] = k[int(cu[s]):int(cu[s]) + lens[s]]
+        small_v[own[s].long()[j // P], :, j % P] = v[int(cu[s]):int(cu[s]) + lens[s]]
+    o, l, ob, lb = ref.attend(q, small_k, small_v, cu.cpu(), lens, own, tensor_cores=kv == "bf16")
+    ref.check(lse, l, lb, what="lse")
+    ref.check(out, o, ob, t, "out")
+
+
+@kinds
 def test_long(kv, q, flags):
     """Long sequences beside short ones: units cut between many CTAs, joined in order; twice the same bits."""
     b = Batch([1, 1, 2, 130], [20000, 17, 5001, 9000], hq=8, hkv=2, d=128, P=64, kv=kv, q=q, flags=flags)
@@ -146,12 +217,13 @@ def test_rows_behind_the_last_sequence(kv, q, flags):
 
 @kinds
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-def test_not_finite_values_of_hidden_keys(kv, q, flags, bad):
+@pytest.mark.parametrize("new,hit", [([60, 1, 140], (130, 100, 77)), ([3, 1, 2], (101, 100, 77)), ([3, 1, 1], (102, 141, 220))], ids=["chunks", "few", "few-edges"])
+def test_not_finite_values_of_hidden_keys(kv, q, flags, bad, new, hit):
     """Values and keys that are not finite, of later tokens, before the window, in other documents: rows that do not see them are as without."""
-    b = Batch([60, 1, 140], [100, 260, 0], hq=4, hkv=2, d=128, kv=kv, q=q, flags=flags)
+    b = Batch(new, [100, 260, 0 if new[2] > 100 else 218], hq=4, hkv=2, d=128, kv=kv, q=q, flags=flags)
     b.run(window=120)
     want, want_lse, bound, lse_bound = ref.attend(b.q, b.k, b.v, b.cu_cpu, b.lens, b.table_cpu, window=120, tensor_cores=b.tensor_cores)
-    hit = {0: 130, 1: 100, 2: 77}                                             # sequence: token
+    hit = {s: t for s, t in enumerate(hit) if t < b.lens[s]}                  # sequence: token
     k, v = b.k.clone(), b.v.clone()
     for s, t in hit.items():
         page = int(b.table_cpu[s, t // b.P])

@@ -134,13 +134,21 @@ def test_attend_arguments(lib):
     assert call(paged_h=None) == INVALID and call(q=None) == INVALID and call(out=None) == INVALID
     assert call(q=4097) == INVALID and call(out=8192 + 8) == INVALID and call(lse=4098) == INVALID and call(qs=1023) == INVALID and call(qs=-1024) == INVALID
     assert call(ws=(1 << 20) + 16) == INVALID
-    for bad in (dict(softcap=-1.0), dict(softcap=math.nan), dict(softcap=math.inf), dict(window=-1), dict(slopes=4098), dict(first_key=4097), dict(prefix_lens=4099)):
+    for bad in (dict(softcap=-1.0), dict(softcap=math.nan), dict(softcap=math.inf), dict(softcap=1e-7), dict(window=-1), dict(slopes=4098), dict(first_key=4097), dict(prefix_lens=4099)):
         assert call(mask=m(**bad)) == INVALID, bad
     long = batch(max_len=1 << 20, table_stride=1 << 14)
     assert lib.spla_paged_query_workspace(h, C.addressof(long), C.byref(n)) == OK and n.value > 0
     assert call(bb=long, ws=None, nb=0) == INVALID and call(bb=long, nb=n.value - 1) == INVALID
     lib.spla_paged_destroy(h)
     assert lib.spla_paged_destroy(None) == OK
+
+
+def test_wait_hook_arguments(lib):
+    _, h = paged(lib)
+    hook = lib.spla_paged_debug_wait_hook
+    assert hook(None, 0, 0) == INVALID and hook(h, -1, 0) == INVALID and hook(h, 0, 8) == INVALID and hook(h, 0, -16) == INVALID
+    assert hook(h, 1000, 16) == OK and hook(h, 0, 0) == OK
+    lib.spla_paged_destroy(h)
 
 
 def test_python_checks():
