@@ -61,12 +61,13 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& pb, int* status,
 // same number of tiles however ragged the lengths are.  A unit that a share's border cuts leaves partial results (maximum, sum,
 // unnormalised output per row) that a second kernel joins, in the order of the shares: no atomics, the same bits every time.
 // Short caches are dealt out by whole units instead, which needs no second kernel.
-constexpr int kPagedMaxBatch = 512;    // sequences per launch (the host cuts larger batches)
+constexpr int kPagedMaxBatch = 384;    // sequences per launch (the host cuts larger batches)
 
 struct PagedWork {
   int ppos, upos, log_tk;               // TK = 2^log_tk
   int by_unit;                          // dealt out by units instead of tiles
   int n_cta, min_tiles;
+  int narrow;                           // all tiles together are below 2^31, by the host's bounds
   int extra;                            // what starting and ending a unit costs, in tiles: counted before its first tile when the work is dealt out
   int rows;                             // rows that a partial result holds
   float* part_o;                        // [2 n_cta][rows][d]
@@ -93,7 +94,7 @@ struct PagedAttend {
 // Sequence table of a CTA, in shared memory.
 struct PagedSeqs {
   long long pre[kPagedMaxBatch + 1];    // tiles (units) before a sequence, all heads
-  int row0[kPagedMaxBatch], n[kPagedMaxBatch], L[kPagedMaxBatch], prefix[kPagedMaxBatch];
+  int row0[kPagedMaxBatch], n[kPagedMaxBatch], L[kPagedMaxBatch], prefix[kPagedMaxBatch], per_head[kPagedMaxBatch];   // per_head: tiles (units) of one head
 };
 
 __host__ __device__ __forceinline__ int paged_units(const PagedWork& w, int n) { return n <= w.ppos ? (n > 0) : (n + w.upos - 1) / w.upos; }
@@ -121,7 +122,7 @@ __device__ __forceinline__ int paged_unit_tiles(const PagedAttend& a, int row0, 
 }
 
 // What one sequence counts for, per head.  Whole warps: sequences of many units are counted by the warp together.
-__device__ __forceinline__ long long paged_seq_tiles(const PagedAttend& a, int row0, int n, int L, int prefix, int lane) {
+__device__ __forceinline__ int paged_seq_tiles(const PagedAttend& a, int row0, int n, int L, int prefix, int lane) {
   const int nu = paged_units(a.w, n);
   int sum = 0;
   if (nu <= 4)
@@ -137,10 +138,11 @@ __device__ __forceinline__ long long paged_seq_tiles(const PagedAttend& a, int r
   }
   return sum;
 }
-__device__ __forceinline__ long long paged_scan(long long v, int lane) {   // inclusive, over a warp
+template <typename N>
+__device__ __forceinline__ N paged_scan(N v, int lane) {                   // inclusive, over a warp
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long x = __shfl_up_sync(0xffffffffu, v, o);
+    const N x = __shfl_up_sync(0xffffffffu, v, o);
     if (lane >= o) v += x;
   }
   return v;
@@ -157,7 +159,9 @@ __device__ __forceinline__ long long paged_fill_seqs(const PagedAttend& a, Paged
       row0 = s.row0; n = s.n; L = s.L;
       t.row0[lane] = row0; t.n[lane] = n; t.L[lane] = L; t.prefix[lane] = pre;
     }
-    const long long v = paged_scan(paged_seq_tiles(a, row0, n, L, pre, lane) * a.pl.Hkv, lane);
+    const int per_head = paged_seq_tiles(a, row0, n, L, pre, lane);
+    const long long v = a.w.narrow ? paged_scan(per_head * a.pl.Hkv, lane) : paged_scan((long long)per_head * a.pl.Hkv, lane);
+    if (lane < batch) t.per_head[lane] = per_head;
     if (lane < batch) t.pre[lane + 1] = v;
     if (lane == 0) t.pre[0] = 0;
     __syncthreads();
@@ -172,15 +176,15 @@ __device__ __forceinline__ long long paged_fill_seqs(const PagedAttend& a, Paged
       row0 = s.row0; n = s.n; L = s.L;
       t.row0[b] = row0; t.n[b] = n; t.L[b] = L; t.prefix[b] = pre;
     }
-    const long long sum = paged_seq_tiles(a, row0, n, L, pre, lane);
-    if (b < batch) t.pre[b + 1] = sum;
+    const int per_head = paged_seq_tiles(a, row0, n, L, pre, lane);
+    if (b < batch) t.per_head[b] = per_head;
   }
   __syncthreads();
   if (tid < 32) {
     long long carry = 0;
     for (int b0 = 0; b0 < batch; b0 += 32) {
       const int b = b0 + tid;
-      const long long v = paged_scan(b < batch ? t.pre[b + 1] * a.pl.Hkv : 0, tid) + carry;
+      const long long v = paged_scan(b < batch ? (long long)t.per_head[b] * a.pl.Hkv : 0ll, tid) + carry;
       carry = __shfl_sync(0xffffffffu, v, 31);
       if (b < batch) t.pre[b + 1] = v;
     }
@@ -193,44 +197,43 @@ __device__ __forceinline__ long long paged_fill_seqs(const PagedAttend& a, Paged
 // Tiles (units) per CTA.
 __device__ __forceinline__ long long paged_share(const PagedWork& w, long long total) {
   const long long up = total + w.n_cta - 1;
-  const long long per = up < (1ll << 31) ? (long long)((unsigned)up / (unsigned)w.n_cta) : up / w.n_cta;
+  const long long per = w.narrow ? (long long)((unsigned)up / (unsigned)w.n_cta) : up / w.n_cta;
   return per < w.min_tiles ? w.min_tiles : per;
 }
 
 // A CTA's walk over its share: one segment (a run of key tiles of one unit) after the other.  Every role keeps its own copy.
 struct PagedWalk {
   long long left;                       // tiles (units) still to walk
-  int b, h, u, off;                     // off: tiles of the unit that earlier segments (other CTAs) have
+  int b, h, u, off, units;              // off: tiles of the unit that earlier segments (other CTAs) have; units of a head
   int row0, n, L, prefix;
   // the current segment
   int t0, t1;                           // key tiles
   bool head, tail;                      // it starts / ends the unit
 
-  __device__ __forceinline__ void load(const PagedSeqs& t) { row0 = t.row0[b]; n = t.n[b]; L = t.L[b]; prefix = t.prefix[b]; }
+  __device__ __forceinline__ void load(const PagedWork& w, const PagedSeqs& t) { row0 = t.row0[b]; n = t.n[b]; L = t.L[b]; prefix = t.prefix[b]; units = paged_units(w, n); }
   // Goes to tile `at` of all; false if there is none.  Whole warps.
   __device__ __forceinline__ bool seek(const PagedAttend& a, const PagedSeqs& t, long long at, long long count) {
     const long long total = t.pre[a.pb.batch];
     left = min(count, total - at);
     if (left <= 0) { left = 0; return false; }
-    int lo = 0, hi = a.pb.batch;        // the last b with pre[b] <= at
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (t.pre[mid] <= at) lo = mid; else hi = mid;
+    const int lane = threadIdx.x & 31;
+    b = -1;                             // the last b with pre[b] <= at
+    for (int b0 = 0;; b0 += 32) {
+      const unsigned in = __ballot_sync(0xffffffffu, b0 + lane < a.pb.batch && t.pre[b0 + lane] <= at);
+      b += __popc(in);
+      if (in != 0xffffffffu) break;
     }
-    b = lo;
-    load(t);
-    const long long all = t.pre[b + 1] - t.pre[b], rem = at - t.pre[b];
-    int in_head;
-    if (all < (1ll << 31)) {
-      const unsigned per_head = (unsigned)all / (unsigned)a.pl.Hkv;
-      h = (int)((unsigned)rem / per_head);
-      in_head = (int)((unsigned)rem - (unsigned)h * per_head);
-    } else {
-      const long long per_head = all / a.pl.Hkv;
-      h = (int)(rem / per_head);
-      in_head = (int)(rem - h * per_head);
+    load(a.w, t);
+    const int per_head = t.per_head[b];
+    const long long rem = at - t.pre[b];
+    h = a.w.narrow ? (int)((unsigned)rem / (unsigned)per_head) : (int)(rem / per_head);
+    int in_head = (int)(rem - (long long)h * per_head);
+    if (units == 1) {
+      u = 0;
+      off = in_head;
+      return true;
     }
-    const int lane = threadIdx.x & 31, nu = paged_units(a.w, n);
+    const int nu = units;
     for (u = 0;; u += 32) {             // 32 units at a time
       const int c = u + lane < nu ? paged_unit_tiles(a, row0, n, L, prefix, u + lane) : 0;
       int upto = c;
@@ -253,12 +256,12 @@ struct PagedWalk {
   __device__ __forceinline__ bool next(const PagedAttend& a, const PagedSeqs& t) {
     do {
       if (left <= 0) return false;
-      if (u >= paged_units(a.w, n)) {                // the unit before was its head's last
+      if (u >= units) {                              // the unit before was its head's last
         u = 0;
         if (++h == a.pl.Hkv) {
           h = 0;
           do ++b; while (b < a.pb.batch - 1 && t.pre[b + 1] == t.pre[b]);
-          load(t);
+          load(a.w, t);
         }
       }
       const PagedSpan s = paged_span(a, row0, n, L, prefix, u);
@@ -312,6 +315,12 @@ __device__ __forceinline__ long long paged_row(const PagedBatch& pb, const Paged
     return -1;
   }
   return page * pl.page_stride + h * pl.head_stride;
+}
+
+// Whether all tiles (and extras) that a launch may have are below 2^31.
+inline bool paged_narrow(const PagedWork& w, const PagedBatch& pb, const PagedLayout& pl) {
+  const double units = (double)pl.Hkv * ((double)pb.total_new / w.upos + pb.batch), tiles = pb.max_len / (double)(1 << w.log_tk) + 1 + w.extra;
+  return units * tiles + w.n_cta < 2147483647.0;
 }
 
 struct PagedMaps {                      // TMA tensor maps (CUtensorMap), opaque to the host code

@@ -500,6 +500,7 @@ void paged_plan_general(PagedWork* w, const PagedBatch& pb, const PagedLayout& p
   w->extra = 0;
   const long long most_ctas = w->by_unit ? units : (units * tiles + w->min_tiles - 1) / w->min_tiles;
   w->n_cta = (int)(most_ctas < (long long)per_sm * sm_count ? most_ctas : (long long)per_sm * sm_count);
+  w->narrow = paged_narrow(*w, pb, pl);
   w->rows = (pb.max_new < w->upos ? pb.max_new : w->upos) * pl.G;
 }
 

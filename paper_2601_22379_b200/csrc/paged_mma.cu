@@ -880,6 +880,7 @@ void paged_plan_mma(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, i
   w->extra = few ? 1 : 2;
   const long long most = w->by_unit ? units : (units * tiles + w->min_tiles - 1) / w->min_tiles;
   w->n_cta = (int)(most < sm_count ? most : sm_count);
+  w->narrow = paged_narrow(*w, pb, pl);
   w->rows = (pb.max_new < w->upos ? pb.max_new : w->upos) * pl.G;
 }
 
