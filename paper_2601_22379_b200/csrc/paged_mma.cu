@@ -127,6 +127,12 @@ __device__ __forceinline__ bool pm_wait(uint64_t* bar, uint32_t parity, int limi
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, 1)) || pm_wait_slow(bar, parity, limit, abort_flag);
 }
 
+constexpr float kCapNear = 0.375f;                 // up to here tanh goes by a polynomial
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
 __device__ __forceinline__ float rcp_approx(float x) {
   float y;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -415,6 +421,8 @@ __global__ void __launch_bounds__(kPmThreads, 1)
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + slot * 128 + lane_off, tO = tmem + 256 + slot * 128 + lane_off;
     const float sc2 = a.sm_scale * kLog2e;
+    const float to_u = MODS && a.softcap > 0.f ? a.sm_scale / a.softcap : 0.f, sq_u = to_u * to_u;
+    const float cap0 = 0.99999994f * sc2, cap1 = -0.33331972f * sc2 * sq_u, cap2 = 0.13284431f * sc2 * sq_u * sq_u, cap3 = -0.048268907f * sc2 * sq_u * sq_u * sq_u;   // (a score of 1 is sc2 in base 2)
     bool ok = true;
     int kt = 0, n = 0, n_scan = 0, n_half = 0, n_quarter = 0, n_used = 0;   // tiles of the CTA, items of this slot, look-overs, merges, segments that used O
     each_segment(ok, [&](const PmSeg& sg) {
@@ -514,20 +522,33 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           }
           if constexpr (MODS) {
             if (a.softcap > 0.f) {
-              // cap tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap)), in base 2: off by some 2^-22 cap, whatever x is.  Where that is much
-              // (caps far above the scores) small x / cap go by the series instead: u - u^3 / 3 + 2 u^5 / 15 - 17 u^7 / 315.
-              const float k1 = 2.f * sc2 / a.softcap, c2 = a.softcap * kLog2e;
-              if (a.softcap <= 64.f) {
+              // cap tanh(u), u = x / cap, in base 2.  Up to |u| = 3/8 an odd polynomial (interpolated at Chebyshev nodes, 6e-8 off), its coefficients
+              // scaled to the raw scores; where a row of the warp has more, 1 - 2 / (1 + e^(2 |u|)) there, which alone would be off by
+              // 2^-22 of the cap, however small the score, and takes two of the exponential unit's turns per key.
+              float most = 0.f;
 #pragma unroll
-                for (int x = 0; x < KEYS; ++x) r[x] = __float_as_uint(fmaf(-2.f * c2, rcp_approx(1.f + ex2(__uint_as_float(r[x]) * k1)), c2));
+              for (int x = 0; x < KEYS; x += 2) most = max3(most, fabsf(__uint_as_float(r[x])), fabsf(__uint_as_float(r[x + 1])));
+              auto near = [&](float2 v) {
+                const float2 z = __fmul2_rn(v, v);
+                float2 y = __ffma2_rn(z, make_float2(cap3, cap3), make_float2(cap2, cap2));
+                y = __ffma2_rn(z, y, make_float2(cap1, cap1));
+                return __fmul2_rn(__ffma2_rn(z, y, make_float2(cap0, cap0)), v);
+              };
+              if (!__any_sync(0xffffffffu, valid && most * to_u >= kCapNear)) {
+#pragma unroll
+                for (int x = 0; x < KEYS; x += 2) {
+                  const float2 y = near(make_float2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])));
+                  r[x] = __float_as_uint(y.x);
+                  r[x + 1] = __float_as_uint(y.y);
+                }
               } else {
-                const float to_u = a.sm_scale / a.softcap;
+                const float c2 = a.softcap * kLog2e, k2 = 2.f * kLog2e * to_u;
 #pragma unroll
-                for (int x = 0; x < KEYS; ++x) {
-                  const float sx = __uint_as_float(r[x]), u = sx * to_u, u2 = u * u;
-                  const float series = fmaf(u2, fmaf(u2, fmaf(u2, -17.f / 315.f, 2.f / 15.f), -1.f / 3.f), 1.f) * u * c2;
-                  const float closed = fmaf(-2.f * c2, rcp_approx(1.f + ex2(sx * k1)), c2);
-                  r[x] = __float_as_uint(fabsf(u) < 0.125f ? series : closed);
+                for (int x = 0; x < KEYS; x += 2) {
+                  const float2 v = make_float2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), y = near(v);
+                  const float t0 = fmaf(-2.f, rcp_approx(1.f + ex2(fabsf(v.x) * k2)), 1.f), t1 = fmaf(-2.f, rcp_approx(1.f + ex2(fabsf(v.y) * k2)), 1.f);
+                  r[x] = __float_as_uint(fabsf(v.x) * to_u >= kCapNear ? copysignf(t0 * c2, v.x) : y.x);
+                  r[x + 1] = __float_as_uint(fabsf(v.y) * to_u >= kCapNear ? copysignf(t1 * c2, v.y) : y.y);
                 }
               }
             } else {
