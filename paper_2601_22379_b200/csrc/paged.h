@@ -333,12 +333,12 @@ struct PagedMaps {                      // TMA tensor maps (CUtensorMap), opaque
 cudaError_t launch_rope(const RopeTable& rt, const int* positions, int batch, int tokens, const RopeGroup* groups, int n_groups,
                         const PagedBatch* pb, const PagedLayout* pl, void* k_pages, void* v_pages, int transpose, cudaStream_t s);
 // paged_attend.cu: fp32 kernels for every type, and the join of cut units
-void paged_plan_general(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int window, int sm_count);
+void paged_plan_general(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int sm_count);
 cudaError_t launch_paged_general(const PagedAttend& a, const void* k_pages, const void* v_pages, int q_bf16, int kv_bf16, cudaStream_t s);
 cudaError_t launch_paged_join(const PagedAttend& a, int out_bf16, cudaStream_t s);
 // paged_mma.cu: bf16 on tcgen05
 int paged_mma_positions(const PagedBatch& pb, const PagedLayout& pl);   // new tokens of a row tile: the query boxes' size
-void paged_plan_mma(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int window, int sm_count);
+void paged_plan_mma(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int sm_count);
 cudaError_t launch_paged_mma(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s);
 
 }  // namespace spla

@@ -185,9 +185,9 @@ extern "C" int spla_paged_append(spla_paged_t* p, const spla_paged_batch_t* batc
 }
 
 // The plan of one launch (a batch of at most kPagedMaxBatch sequences) and the bytes of its partial results.
-static size_t plan_attend(const spla_paged* p, const PagedBatch& pb, bool tensor, int window, PagedWork* w) {
-  if (tensor) paged_plan_mma(w, pb, p->pl, window, p->sm_count);
-  else paged_plan_general(w, pb, p->pl, window, p->sm_count);
+static size_t plan_attend(const spla_paged* p, const PagedBatch& pb, bool tensor, PagedWork* w) {
+  if (tensor) paged_plan_mma(w, pb, p->pl, p->sm_count);
+  else paged_plan_general(w, pb, p->pl, p->sm_count);
   if (w->by_unit || w->n_cta < 2) return 0;
   const size_t rows = (size_t)2 * w->n_cta * w->rows;
   return align_up(rows * p->pl.d * 4, 256) + align_up(rows * 8, 256) + align_up((size_t)w->n_cta * 16, 256);
@@ -225,7 +225,7 @@ extern "C" int spla_paged_query_workspace(const spla_paged_t* p, const spla_page
     part.batch = pb.batch - first < kPagedMaxBatch ? pb.batch - first : kPagedMaxBatch;
     for (int tensor = 0; tensor <= (p->tensor ? 1 : 0); ++tensor) {   // (queries that TMA does not take go to the general kernel)
       PagedWork w = {};
-      const size_t n = plan_attend(p, part, tensor != 0, 0, &w);
+      const size_t n = plan_attend(p, part, tensor != 0, &w);
       if (n > most) most = n;
     }
   }
@@ -280,7 +280,7 @@ extern "C" int spla_paged_attend(spla_paged_t* p, const spla_paged_batch_t* batc
     a.pb = part_of(pb, first);
     a.prefix = mask->prefix_lens ? mask->prefix_lens + first : nullptr;
     a.w = PagedWork{};
-    place_parts(p, plan_attend(p, a.pb, tensor, a.window, &a.w), workspace, &a.w);
+    place_parts(p, plan_attend(p, a.pb, tensor, &a.w), workspace, &a.w);
     e = tensor ? launch_paged_mma(a, maps, s) : launch_paged_general(a, p->k_pages, p->v_pages, q16, kv16, s);
     if (e == cudaSuccess) e = launch_paged_join(a, q16, s);
   }

@@ -7,18 +7,26 @@
 // work on one while the other is in its exponentials:
 //   - a unit of more than one row tile: two row tiles against the same key tile, K and V are read once for both;
 //   - a unit of one row tile (short chunks): the same rows against key tiles in turn, the two halves merged at the end.
-// Launches whose units have at most 32 rows (single tokens, FEW) hold the rows four times, a copy for each softmax warp, which takes 32 of
-// the tile's 128 keys: its row of P has zeros elsewhere, its rows of O and l are sums over its keys, and the four are merged at the end.
-// One warp with all 128 keys of the rows would be the whole chain, with 8 cycles of the exponential unit per key (32 when scores are capped).
-// P takes the place of S in tensor memory, as the left operand of O += P V, rounded to bf16 (its sum l is of the unrounded values).
-// The maximum is a stale one: O is rescaled only when it grows by more than 2^8.
+// Launches whose units have at most 32 rows (single tokens, FEW) hold the rows four times, a copy for each softmax warp, which takes 32
+// of the tile's 128 keys: its row of P has zeros elsewhere, its rows of O and l are sums over its keys, and the four are merged at the
+// end.  (One warp with all 128 keys of the rows was the whole chain: capped scores of 64 ragged sequences 978 us, 618 so.)
+// P takes the place of S in tensor memory, as the left operand of O += P V, rounded to bf16, half a step of 2^-8, as the outputs are;
+// its sum l is of the unrounded values, so that lse is as exact as the scores.  The maximum is a stale one: O is rescaled only when it
+// grows by more than 2^8.
 //
-// Warps: 0 and 2 TMA (pages of K and the query rows as boxes of G heads x positions; pages of V), 1 the MMA issuer, 4 to 7 and 8 to 11 softmax and
-// epilogue of either row tile, one row per thread.
+// Warps: 0 and 2 TMA (pages of K and the query rows as boxes of G heads x positions; pages of V), 1 the MMA issuer, 3 plans the
+// segments ahead of the others, 4 to 7 and 8 to 11 softmax and epilogue of either row tile, one row per thread.
+//
+// What bounds it.  Single tokens: reading K and V (8 sequences of 32768, 8 KV heads: 6.2 TB/s, 0.95 of a copy's rate).  Prompts:
+// products issue at about 82 cycles each (64 would be the tensor pipe's own time: S reads both operands from shared memory, at its
+// full rate), 16 per row tile and key tile, and each row tile's chain of scores, softmax (about 1900 cycles), P and product is not quite
+// hidden behind the other's: 8192 tokens, 32 heads of 128: 0.53 ms, 1.03 PFLOP/s.  Slower, on the same box: scores in halves of 64 keys with
+// two buffers (623 us: twice the instructions at the same 82 cycles); P handed over in halves (561); a quarter of the exponentials by
+// polynomial on the FMA pipe (565); loading S twice instead of holding a row in registers.
 //
 // Keys outside a row's mask: their scores are replaced before the maximum, whatever they are.  Values are looked over in tiles that
-// some row sees only in part: behind the sequence's end they are zeroed, and where one that is not finite is inside, the tile's product with V is formed by
-// the softmax warps, visible keys only (0 x infinity is no 0).
+// some row sees only in part: behind the sequence's end they are zeroed, and where one that is not finite is inside, the tile's product
+// with V is formed by the softmax warps, visible keys only (0 x infinity is no 0).
 //
 // Every wait is bounded; on expiry the CTA's roles leave their loops, copies and products in flight are waited for, tensor memory is
 // released and the time-out status latched.  No multicast.
@@ -889,16 +897,19 @@ cudaError_t mma_d(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
 
 int paged_mma_positions(const PagedBatch& pb, const PagedLayout& pl) { return (pb.max_new * pl.G <= 32 ? 32 : 128) / pl.G; }
 
-void paged_plan_mma(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int window, int sm_count) {
+void paged_plan_mma(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int sm_count) {
   w->ppos = paged_mma_positions(pb, pl);
   const bool few = w->ppos * pl.G <= 32;
   w->upos = (few ? 1 : 2) * w->ppos;
   w->log_tk = 7;
   static_assert(kPmKeys == 1 << 7, "keys per tile");
   const long long tiles = (pb.max_len + kPmKeys - 1) / kPmKeys, units = (long long)pb.batch * pl.Hkv * paged_units(*w, pb.max_new);
-  w->by_unit = tiles <= 4;
+  // Whole units where none is long (one head's 500 tokens in us: whole 11.3, cut 15.3; 64 sequences of them 35.1 and 49.7), and up to
+  // 12 tiles where there is about a CTA for each (16 sequences of 1000 tokens 16.8 and 23.9, of 1500 21.8 and 29.3, a prompt of 1000 28.1 and 38.5; with
+  // fewer units, 8 of 1000 tokens: 14.7 and 14.1; with more, ragged prompts of up to 1000 x 16: 165 and 146).
+  w->by_unit = tiles <= 4 || (tiles <= 12 && units <= sm_count && 4 * units >= sm_count);
   w->min_tiles = w->by_unit ? 1 : 2;
-  w->extra = few ? 1 : 2;
+  w->extra = few ? 1 : 2;                // (a prompt of 8192 tokens with 0, 1, 2, 3, 4: 656, 616, 577, 582, 588 us; single tokens: no difference within 2 %)
   const long long most = w->by_unit ? units : (units * tiles + w->min_tiles - 1) / w->min_tiles;
   w->n_cta = (int)(most < sm_count ? most : sm_count);
   w->narrow = paged_narrow(*w, pb, pl);
