@@ -8,9 +8,10 @@
 // product with V (four rows x CW channels per thread, the tile's tokens shared by TS threads).  K of the next tile is on its way from
 // when the scores are done, V from when the product is done (asynchronous copies where the cache is fp32), the page table one tile ahead of that.
 // R = 4, 16 and 64 by the rows that a unit has at most; a row tile's products cost the same however few of its rows are real.
-// 4 rows are bound by reading K and V (8 sequences of 32000, 8 heads of 128: 2.1 GB in 474 us, 4.4 TB/s), 16 by shared memory's reads for the
-// scores (G = 8, the same cache: 755 us), 64 by the FMA pipe, in use half of the time: the phases of a tile alternate with barriers (1024 tokens, 32
-// heads: 0.34 ms, 26 TFLOP/s; row tiles of 128 in one CTA of 512 threads, or with eight rows per thread: within 7 %).
+// 4 rows are bound by reading K and V (8 sequences of 32000, 8 heads of 128: 2.1 GB in 474 us, 4.4 TB/s), 16 by shared memory's reads for
+// the scores (G = 8, the same cache: 755 us), 64 by the FMA pipe, in use half of the time: the phases of a tile alternate with barriers
+// (300 tokens on 3000 x 4, 32 heads of 128: 1.72 ms, 36 TFLOP/s; with tiles of 32 keys and P beside K 1.88; row tiles of 128 in
+// one CTA of 512 threads, or with eight rows per thread: within 7 % of that).
 #include "paged.h"
 
 namespace spla {
@@ -20,17 +21,19 @@ namespace {
 template <int R, int D>
 struct PgShape {
   static constexpr int THREADS = 256;
-  static constexpr int TK = R == 64 ? 32 : 64;
-  static constexpr int KT = R == 64 ? 2 : 1;       // keys per thread
+  static constexpr int TK = 64;
+  static constexpr bool OVER = R == 64;                            // P takes the place of K (two CTAs per SM; the copies of K and V start together then)
+  static constexpr int KT = R == 64 ? 4 : 1;       // keys per thread
   static constexpr int RG = R / 4;                                 // groups of four rows
   static constexpr int CS = THREADS / (RG * (TK / KT));            // threads that share the channels of a score
   static constexpr int CW = R == 64 ? D / 16 : 4;                  // channels per thread in the product with V
   static constexpr int TS = THREADS / (RG * (D / CW));             // threads that share a tile's tokens there
   static constexpr int LD = D + 4, LP = TK + 4;
-  static constexpr int kQ = 0, kK = kQ + R * LD * 4, kV = kK + TK * LD * 4, kP = kV + TK * D * 4, kFac = kP + R * LP * 4, kLo = kFac + R * 4,
+  static constexpr int kQ = 0, kK = kQ + R * LD * 4, kV = kK + TK * LD * 4, kP = OVER ? kK : kV + TK * D * 4, kFac = kV + TK * D * 4 + (OVER ? 0 : R * LP * 4), kLo = kFac + R * 4,
                        kHi = kLo + R * 4, kSum = kHi + R * 4, kMax = kSum + R * 4, kTop = kMax + R * 4, kRows = (kTop + R * 8 * 4 + 15) / 16 * 16,
                        kSeqs = kRows + 2 * (TK / 16) * 8, kBytes = kSeqs + (int)sizeof(PagedSeqs);
   static_assert(CS >= 1 && TS >= 1 && D % (4 * CS) == 0, "shape");
+  static_assert(!OVER || LP <= LD, "P in the place of K");
   static_assert((TS - 1) * R * D * 4 <= TK * (LD + D) * 4, "the partial products of a unit fit the K and V tiles");
   static_assert(kBytes <= 227 * 1024, "shared memory of the general kernel");
 };
@@ -228,7 +231,9 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
           for (int i = 0; i < 4; ++i) top_s[(rg * 4 + i) * 8 + tid / 32 % W] = mt[i];
       }
       __syncthreads();                                             // (K is used up; the maxima; where the next tile lies)
-      if (t + 1 < t_to) fetch(k_pages, ks, LD, t + 1); else copies_close();
+      if constexpr (!S::OVER) {
+        if (t + 1 < t_to) fetch(k_pages, ks, LD, t + 1); else copies_close();
+      }
       if constexpr (W > 1) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -248,7 +253,7 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
           if (cs == 0) ps[(rg * 4 + i) * LP + kg + y * (TK / KT)] = p;
         }
       }
-      copies_wait<1>();                                            // V is here
+      copies_wait<S::OVER ? 0 : 1>();                              // V is here
       bool bad = false;                                            // a value that is not finite, in a tile that some row does not see all of
       if (part) {
 #pragma unroll
@@ -300,7 +305,12 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
           }
       }
       __syncthreads();                                             // (V and P are used up)
-      if (t + 1 < t_to) fetch(v_pages, vs, D, t + 1); else copies_close();
+      if (t + 1 < t_to) {
+        if constexpr (S::OVER) fetch(k_pages, ks, LD, t + 1);
+        fetch(v_pages, vs, D, t + 1);
+      } else {
+        copies_close();
+      }
     }
     copies_wait<0>();
     // ---- end of the segment: sums over the threads of a row, then over the token shares
@@ -494,10 +504,10 @@ void paged_plan_general(PagedWork* w, const PagedBatch& pb, const PagedLayout& p
   const int most = pb.max_new * pl.G;                              // rows that a sequence has for one KV head, at most
   const int R = most <= 4 ? 4 : most <= 16 ? 16 : 64;
   w->ppos = w->upos = R / pl.G;
-  w->log_tk = R == 64 ? 5 : 6;
+  w->log_tk = 6;
   const long long tiles = (pb.max_len + (1 << w->log_tk) - 1) >> w->log_tk, units = (long long)pb.batch * pl.Hkv * paged_units(*w, pb.max_new);
   constexpr int per_sm = 2;
-  w->by_unit = tiles <= 4;
+  w->by_unit = tiles <= (R == 64 ? 2 : 4);   // (a prompt of 200 tokens, 32 heads: whole units 48 us, cut 38)
   w->min_tiles = w->by_unit ? 1 : 2;
   w->extra = 0;
   const long long most_ctas = w->by_unit ? units : (units * tiles + w->min_tiles - 1) / w->min_tiles;
