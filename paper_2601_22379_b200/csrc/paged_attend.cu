@@ -507,8 +507,8 @@ void paged_plan_general(PagedWork* w, const PagedBatch& pb, const PagedLayout& p
   w->log_tk = 6;
   const long long tiles = (pb.max_len + (1 << w->log_tk) - 1) >> w->log_tk, units = (long long)pb.batch * pl.Hkv * paged_units(*w, pb.max_new);
   constexpr int per_sm = 2;
-  w->by_unit = tiles <= (R == 64 ? 2 : 4);   // (a prompt of 200 tokens, 32 heads: whole units 48 us, cut 38)
-  w->min_tiles = w->by_unit ? 1 : 2;
+  w->by_unit = tiles <= (R == 64 ? 2 : 4);   // (prompts of 100 tokens x 4, 32 heads: whole 42 us, cut 49; of 200: whole 48, cut 32)
+  w->min_tiles = w->by_unit || R == 64 ? 1 : 2;               // (the same prompt with shares of two tiles at least: 51 us)
   w->extra = 0;
   const long long most_ctas = w->by_unit ? units : (units * tiles + w->min_tiles - 1) / w->min_tiles;
   w->n_cta = (int)(most_ctas < (long long)per_sm * sm_count ? most_ctas : (long long)per_sm * sm_count);
