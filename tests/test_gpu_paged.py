@@ -1,5 +1,7 @@
 """The paged cache: appending (with the rotation on the way) and attention over it, against plain float64 forms."""
 import math
+import os
+import random
 
 import pytest
 import torch
@@ -72,7 +74,7 @@ kinds = pytest.mark.parametrize("kv,q,flags", KINDS, ids=["bf16", "bf16-general"
 
 
 @kinds
-@pytest.mark.parametrize("d,P", [(128, 64), (64, 16), (128, 128), (64, 32)])
+@pytest.mark.parametrize("d,P", [(128, 64), (64, 16), (128, 128), (64, 32), (128, 16), (64, 128)])
 @pytest.mark.parametrize("new,old", [([1], [0]), ([1, 1, 1], [0, 63, 64]), ([1, 1], [127, 500]), ([5, 0, 1, 33], [0, 3, 700, 130]), ([150, 2], [40, 1000]), ([0, 0, 7], [5, 0, 0])],
                          ids=["one", "page-ends", "tile-ends", "ragged", "chunk", "empty"])
 def test_attend(kv, q, flags, d, P, new, old):
@@ -337,6 +339,61 @@ def test_many_sequences(kv, q, flags):
     old = torch.randint(0, 40, (n,), generator=g).tolist()
     b = Batch(new, old, hq=2, hkv=1, d=64, P=16, kv=kv, q=q, flags=flags)
     b.run()
+
+
+def test_two_threads():
+    """Calls from two threads, each on its own stream: the handle holds nothing that a call changes."""
+    import threading
+    b = Batch([1, 1, 66], [4000, 30, 900], hq=8, hkv=2, d=128, kv="bf16")
+    want, want_lse = b.run()
+    wrong = []
+
+    def work():
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(40):
+                out, lse = b.attend()
+                stream.synchronize()
+                if not (torch.equal(out, want) and torch.equal(lse, want_lse)):
+                    wrong.append(1)
+
+    threads = [threading.Thread(target=work) for _ in range(2)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    assert not wrong
+
+
+@pytest.mark.parametrize("seed", [int(os.environ.get("SPLA_FUZZ_OFFSET", "0")) + i for i in range(60)])
+def test_drawn(seed):
+    """Anything the documentation allows, at once."""
+    r = random.Random(9000 + seed)
+    kv, q, flags = r.choice([KINDS[0]] * 4 + KINDS[1:])
+    B, hkv, G, d, P = r.choice([1, 2, 3, 7, 20, 33]), r.choice([1, 2, 3]), r.choice([1, 2, 3, 4, 5, 7, 8, 11, 16]), r.choice([64, 128]), r.choice([16, 32, 64, 128])
+    few = r.random() < 0.5
+    new = [r.choice([0, 1, 1, r.randint(1, 3 if few else 150)]) for _ in range(B)]
+    if not sum(new):
+        new[0] = 1
+    old = [r.choice([0, r.randint(0, 30), r.randint(0, 700), r.randint(0, 3000)]) for _ in range(B)]
+    b = Batch(new, old, hq=G * hkv, hkv=hkv, d=d, P=P, kv=kv, q=q, flags=flags, seed=seed, extra_rows=r.choice([0, 3]), extra_cols=r.choice([0, 5]))
+    kw = {}
+    if r.random() < 0.3:
+        kw["softcap"] = r.choice([1.0, 5.0, 30.0, 500.0])
+    if r.random() < 0.3:
+        kw["window"] = r.choice([1, 2, 17, 128, 400])
+    if r.random() < 0.3:
+        kw["slopes"] = torch.tensor([r.choice([0.0, 0.01, 0.3, 2.0]) for _ in range(G * hkv)])
+    if r.random() < 0.3:
+        kw["first_key"] = torch.tensor([max(-1, r.choice([0, p, p - r.randint(0, 200), p + 1])) for n, o in zip(new, old) for p in range(o, o + n)] + [0] * (b.rows - b.total),
+                                       dtype=torch.int32)
+    if r.random() < 0.3:
+        kw["prefix_lens"] = torch.tensor([r.choice([0, 5, 100, 5000]) for _ in range(B)], dtype=torch.int32)
+    bounds = dict(max_new=b.max_new + r.choice([0, 0, 40]), max_len=min(b.max_len + r.choice([0, 0, 300]), b.table.shape[1] * P))
+    bounds["max_new"] = min(bounds["max_new"], bounds["max_len"])
+    out, lse = b.attend(**kw, **bounds)
+    assert b.cache.sync_status() == 0
+    b.check(out, lse, **{k: (v[:b.total] if k == "first_key" else v) for k, v in kw.items()})
+    again, lse2 = b.attend(**kw, **bounds)
+    assert torch.equal(out[:b.total], again[:b.total]) and torch.equal(lse[:b.total], lse2[:b.total])
 
 
 # ---- append ---------------------------------------------------------------------------------------------------------
