@@ -14,8 +14,9 @@ namespace spla {
 namespace {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeTable = 512;          // (token, pair) entries of a block's table, at most
-constexpr int kRopeTokens = 8;           // tokens of a block, at most
+constexpr int kRopeTable = 2048;         // (token, pair) entries of a block's table, at most
+constexpr int kRopeTokens = 32;          // tokens of a block, at most
+constexpr int kRopePerWarp = kRopeTokens / (kRopeThreads / 32);
 
 struct RopeLaunch {
   RopeGroup g[3];
@@ -135,16 +136,21 @@ __global__ void __launch_bounds__(kRopeThreads, sizeof(T) == 4 ? 5 : 4)
   if (r.paged) {
     if (blockIdx.x == 0 && blockIdx.y == 0)               // every sequence's numbers are looked at once, those without tokens too
       for (int b = tid; b < r.pb.batch; b += kRopeThreads) paged_seq(r.pb, r.pl.status, b);
-    static_assert(kRopeTokens <= kRopeThreads / 32, "a warp per token");
-    if (warp < nt) {
-      const int tok = tok0 + warp;
-      int at = -1;                                        // the last b with cu[b] <= tok
-      for (int b0 = 0; b0 < r.pb.batch; b0 += 32) {
-        const int b = b0 + lane;
-        const unsigned in = __ballot_sync(0xffffffffu, b < r.pb.batch && __ldg(r.pb.cu + b) <= tok);
-        at += __popc(in);
-        if (in != 0xffffffffu) break;
+    // a warp's tokens: warp, warp + 8, ...; lane k ends up with the k-th
+    const int tok = tok0 + warp + lane * (kRopeThreads / 32);
+    int at = -1;                                          // the last b with cu[b] <= tok
+    for (int b0 = 0; b0 < r.pb.batch; b0 += 32) {
+      const int cu = b0 + lane < r.pb.batch ? __ldg(r.pb.cu + b0 + lane) : 0x7fffffff;
+      bool all = false;
+#pragma unroll
+      for (int k = 0; k < kRopePerWarp; ++k) {
+        const unsigned in = __ballot_sync(0xffffffffu, cu <= tok0 + warp + k * (kRopeThreads / 32));
+        if (lane == k) at += __popc(in);
+        all |= in == 0xffffffffu;
       }
+      if (!all) break;
+    }
+    if (lane < kRopePerWarp && tok < tok0 + nt) {
       PagedSeq s{0, 0, 0};
       if (at >= 0) s = paged_seq(r.pb, r.pl.status, at);
       const bool there = s.n > 0 && tok >= s.row0 && tok < s.row0 + s.n;
@@ -155,14 +161,11 @@ __global__ void __launch_bounds__(kRopeThreads, sizeof(T) == 4 ? 5 : 4)
         page_row = paged_row(r.pb, r.pl, at, 0, pos >> r.pl.log_p);
         if (page_row >= 0) page_row += pos & (r.pl.P - 1);
       }
-      if (lane < 3) {
-        const RopeGroup& g = lane == 0 ? r.g[0] : lane == 1 ? r.g[1] : r.g[2];
-        T* out = nullptr;
-        if (g.out) { if (there) out = reinterpret_cast<T*>(g.out) + (long long)tok * g.out_token; }
-        else if (page_row >= 0) out = reinterpret_cast<T*>(lane == 1 ? r.k_pages : r.v_pages) + page_row * rt.dim;
-        out_at[warp][lane] = out;
-      }
-      if (lane == 0) tok_pos[warp] = r.positions && there ? __ldg(r.positions + tok) : pos;
+      const int t = tok - tok0;
+      out_at[t][0] = r.g[0].out && there ? reinterpret_cast<T*>(r.g[0].out) + (long long)tok * r.g[0].out_token : nullptr;
+      out_at[t][1] = page_row >= 0 ? reinterpret_cast<T*>(r.k_pages) + page_row * rt.dim : nullptr;
+      out_at[t][2] = page_row >= 0 ? reinterpret_cast<T*>(r.v_pages) + page_row * rt.dim : nullptr;
+      tok_pos[t] = r.positions && there ? __ldg(r.positions + tok) : pos;
     }
     __syncthreads();
   }
@@ -238,15 +241,21 @@ cudaError_t rope_launch(RopeLaunch r, const RopeTable& rt, int sm_count, cudaStr
   r.pieces = rt.dim / (2 * VEC);
   r.head_magic = (unsigned)(((1ull << 32) + r.heads - 1) / r.heads);
   const int pairs = rt.rot / 2;
-  // tokens per block: a full table's worth, so that every thread forms one or two sines; fewer where that would leave SMs idle
-  int tb = pairs > 0 ? kRopeThreads / pairs : kRopeTokens;
-  if (tb < 1) tb = 1;
+  // tokens per block: a sine for every thread (eight tokens at most: with 16 of 24 small fp32 heads 42 us in place of 37), and four rows for every
+  // thread where heads are few, so that what comes before the first row pays (6 heads of 128, 80000 tokens: 22 tokens 69 us, 4 tokens 111);
+  // fewer where that would leave SMs idle
+  const int by = kRopeThreads / r.pieces;
+  int tb = pairs > 0 && kRopeThreads / pairs < 8 ? kRopeThreads / pairs : 8;
+  if (tb < (4 * by + r.heads - 1) / r.heads) tb = (4 * by + r.heads - 1) / r.heads;
   if (tb > kRopeTokens) tb = kRopeTokens;
+  if (tb * pairs > kRopeTable) tb = kRopeTable / pairs;
+  if (tb < 1) tb = 1;
+  while (tb > 1 && (long long)tb * r.heads * r.heads >= (1ll << 32)) tb /= 2;   // (see head_magic)
   auto blocks = [&](int x) { return (long long)((r.tokens + x - 1) / x) * r.batch; };
   while (tb > 1 && blocks(tb) < 2LL * sm_count) tb /= 2;
   if (tb > r.tokens) tb = r.tokens;
   r.tb = tb;
-  const int by = kRopeThreads / r.pieces, rows = tb * r.heads;
+  const int rows = tb * r.heads;
   int ys = 1;
   if (blocks(tb) < 2LL * sm_count) {
     ys = (rows + by - 1) / by;

@@ -446,6 +446,27 @@ def test_append(kv, q, d, P, rope, packed):
         assert torch.equal(qi[:b.total], alone[:b.total])
 
 
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (4, 1)])
+def test_append_of_many_tokens_of_few_heads(hq, hkv):
+    """Blocks of many tokens across sequences of a few, empty ones among them."""
+    g = torch.Generator().manual_seed(7)
+    new = torch.randint(0, 60, (150,), generator=g).tolist()
+    b = Batch(new, torch.randint(0, 70, (150,), generator=g).tolist(), hq=hq, hkv=hkv, d=128, P=16, extra_rows=9)
+    k, v, q = (torch.randn(b.rows, h, 128, generator=g).to(torch.bfloat16).to(DEV) for h in (hkv, hkv, hq))
+    r = binding.Rope(128)
+    out = b.cache.append(k, v, b.cu, b.lens_t, b.table, q=q, rope=r)
+    assert b.cache.sync_status() == 0
+    pos = torch.cat([torch.arange(o, o + n) for n, o in zip(b.new, b.old)])
+    f = ref.frequencies(128)
+    wq, eq = ref.rotate(q[:b.total].cpu(), pos, 128, False, f)
+    wk, ek = ref.rotate(k[:b.total].cpu(), pos, 128, False, f)
+    ref.check(out[:b.total], wq, eq, torch.bfloat16)
+    seq = torch.repeat_interleave(torch.arange(150), torch.tensor(b.new))
+    page = b.table_cpu[seq, pos // 16].long()
+    ref.check(b.kd.cpu()[page, :, pos % 16], wk, ek, torch.bfloat16)
+    assert torch.equal(b.vd.cpu()[page, :, pos % 16], v[:b.total].cpu())
+
+
 def test_append_skips_what_does_not_fit():
     b = Batch([2, 3, 4], [30, 10, 60], d=64, P=32)
     k = torch.randn(9, 2, 64, device=DEV).bfloat16()

@@ -30,7 +30,8 @@ def _check(rope_args, positions, x, y, transpose=False):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("d,rot,heads,tokens", [(128, 0, (32, 8), 8), (128, 64, (5, 1), 1), (64, 16, (3, 3), 301), (64, 6, (4, 2), 33), (256, 0, (2, 1), 5),
-                                                (8, 2, (7, 1), 70), (72, 0, (1, 1), 9), (128, 128, (1, 1), 4097), (96, 48, (12, 4), 77), (16, 16, (40, 8), 3)])
+                                                (8, 2, (7, 1), 70), (72, 0, (1, 1), 9), (128, 128, (1, 1), 4097), (96, 48, (12, 4), 77), (16, 16, (40, 8), 3),
+                                                (128, 0, (1, 1), 20011), (64, 4, (4096, 4096), 3), (8, 2, (4096, 4095), 700)])
 def test_rotation(dtype, interleaved, d, rot, heads, tokens):
     args = dict(head_dim=d, rot_dim=rot, interleaved=interleaved)
     pos = (torch.arange(tokens, dtype=torch.int32) * 131 % 100003).to(DEV)
