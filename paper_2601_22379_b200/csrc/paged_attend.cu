@@ -133,6 +133,8 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
       hi_s[tid] = s.hi;
       sees_any = s.lo < s.hi;
     }
+    // a warp whose rows are all behind the unit's last has nothing to compute (its rows of scores and of the product are the same)
+    const bool idle = tid / 32 * 32 / (CS * (TK / KT)) * 4 >= rows;
     float slope[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) slope[i] = a.slopes && rg * 4 + i < rows ? __ldg(a.slopes + wk.h * G + (rg * 4 + i) % G) : 0.f;
@@ -179,78 +181,82 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
       find_rows(t + 1);
       copies_wait<1>();                                            // K is here
       __syncthreads();
-      // ---- scores of four rows x KT keys, this thread's share of the channels
-      float2 acc[4][KT];
+      float s[4][KT], mt[4];
+      constexpr int kRowThreads = CS * (TK / KT);                  // 16 (R = 64: half a warp), 64 (two warps) or 256
+      constexpr int W = kRowThreads > 32 ? kRowThreads / 32 : 1;   // warps of a row group: their maxima meet in shared memory
+      if (!idle) {
+        // ---- scores of four rows x KT keys, this thread's share of the channels
+        float2 acc[4][KT];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int y = 0; y < KT; ++y) acc[i][y] = make_float2(0.f, 0.f);
+          for (int y = 0; y < KT; ++y) acc[i][y] = make_float2(0.f, 0.f);
 #pragma unroll 4
-      for (int c = cs * 4; c < D; c += 4 * CS) {
-        float4 kx[KT];
+        for (int c = cs * 4; c < D; c += 4 * CS) {
+          float4 kx[KT];
 #pragma unroll
-        for (int y = 0; y < KT; ++y) kx[y] = *reinterpret_cast<const float4*>(ks + (kg + y * (TK / KT)) * LD + c);
+          for (int y = 0; y < KT; ++y) kx[y] = *reinterpret_cast<const float4*>(ks + (kg + y * (TK / KT)) * LD + c);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float4 qx = *reinterpret_cast<const float4*>(qs + (rg * 4 + i) * LD + c);
+          for (int i = 0; i < 4; ++i) {
+            const float4 qx = *reinterpret_cast<const float4*>(qs + (rg * 4 + i) * LD + c);
 #pragma unroll
-          for (int y = 0; y < KT; ++y) {
-            acc[i][y] = __ffma2_rn(make_float2(qx.x, qx.y), make_float2(kx[y].x, kx[y].y), acc[i][y]);
-            acc[i][y] = __ffma2_rn(make_float2(qx.z, qx.w), make_float2(kx[y].z, kx[y].w), acc[i][y]);
+            for (int y = 0; y < KT; ++y) {
+              acc[i][y] = __ffma2_rn(make_float2(qx.x, qx.y), make_float2(kx[y].x, kx[y].y), acc[i][y]);
+              acc[i][y] = __ffma2_rn(make_float2(qx.z, qx.w), make_float2(kx[y].z, kx[y].w), acc[i][y]);
+            }
           }
         }
-      }
-      // ---- running maximum and sum; every row belongs to CS x TK / KT neighbouring threads
-      float s[4][KT], mt[4];
+        // ---- running maximum and sum; every row belongs to CS x TK / KT neighbouring threads
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = rg * 4 + i, pos = pos0 + r / G;
-        mt[i] = -INFINITY;
+        for (int i = 0; i < 4; ++i) {
+          const int r = rg * 4 + i, pos = pos0 + r / G;
+          mt[i] = -INFINITY;
 #pragma unroll
-        for (int y = 0; y < KT; ++y) {
-          float v = acc[i][y].x + acc[i][y].y;
+          for (int y = 0; y < KT; ++y) {
+            float v = acc[i][y].x + acc[i][y].y;
 #pragma unroll
-          for (int w = 1; w < CS; w <<= 1) v += __shfl_xor_sync(0xffffffffu, v, w);
-          v *= sc;
-          if (a.softcap > 0.f) v = a.softcap * tanhf(v * inv_cap);
-          const int j = tok0 + kg + y * (TK / KT);
-          if (slope[i] != 0.f) v -= slope[i] * (float)abs(pos - j);
-          s[i][y] = !part || (j >= lo_s[r] && j < hi_s[r]) ? v * kLog2e : -INFINITY;
-          mt[i] = fmaxf(mt[i], s[i][y]);
+            for (int w = 1; w < CS; w <<= 1) v += __shfl_xor_sync(0xffffffffu, v, w);
+            v *= sc;
+            if (a.softcap > 0.f) v = a.softcap * tanhf(v * inv_cap);
+            const int j = tok0 + kg + y * (TK / KT);
+            if (slope[i] != 0.f) v -= slope[i] * (float)abs(pos - j);
+            s[i][y] = !part || (j >= lo_s[r] && j < hi_s[r]) ? v * kLog2e : -INFINITY;
+            mt[i] = fmaxf(mt[i], s[i][y]);
+          }
         }
-      }
-      constexpr int kRowThreads = CS * (TK / KT);                  // 16 (R = 64: half a warp), 64 (two warps) or 256
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int w = kRowThreads < 32 ? kRowThreads / 2 : 16; w >= CS; w >>= 1) mt[i] = fmaxf(mt[i], __shfl_xor_sync(0xffffffffu, mt[i], w));
-      constexpr int W = kRowThreads > 32 ? kRowThreads / 32 : 1;   // warps of a row group: their maxima meet in shared memory
-      if constexpr (W > 1) {
-        if (tid % 32 == 0)
+          for (int w = kRowThreads < 32 ? kRowThreads / 2 : 16; w >= CS; w >>= 1) mt[i] = fmaxf(mt[i], __shfl_xor_sync(0xffffffffu, mt[i], w));
+        if constexpr (W > 1) {
+          if (tid % 32 == 0)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) top_s[(rg * 4 + i) * 8 + tid / 32 % W] = mt[i];
+            for (int i = 0; i < 4; ++i) top_s[(rg * 4 + i) * 8 + tid / 32 % W] = mt[i];
+        }
       }
       __syncthreads();                                             // (K is used up; the maxima; where the next tile lies)
       if constexpr (!S::OVER) {
         if (t + 1 < t_to) fetch(k_pages, ks, LD, t + 1); else copies_close();
       }
-      if constexpr (W > 1) {
+      if (!idle) {
+        if constexpr (W > 1) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int x = 0; x < W; ++x) mt[i] = fmaxf(mt[i], top_s[(rg * 4 + i) * 8 + x]);
-      }
+            for (int x = 0; x < W; ++x) mt[i] = fmaxf(mt[i], top_s[(rg * 4 + i) * 8 + x]);
+        }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float mn = fmaxf(m[i], mt[i]), f = m[i] == mn ? 1.f : ex2(m[i] - mn), nm = mn == -INFINITY ? 0.f : -mn;
-        m[i] = mn;
-        l[i] *= f;
-        if (tid % kRowThreads == 0) fac[rg * 4 + i] = f;
+        for (int i = 0; i < 4; ++i) {
+          const float mn = fmaxf(m[i], mt[i]), f = m[i] == mn ? 1.f : ex2(m[i] - mn), nm = mn == -INFINITY ? 0.f : -mn;
+          m[i] = mn;
+          l[i] *= f;
+          if (tid % kRowThreads == 0) fac[rg * 4 + i] = f;
 #pragma unroll
-        for (int y = 0; y < KT; ++y) {
-          const float p = ex2(s[i][y] + nm);
-          l[i] += p;                                               // (this thread's keys only, until the segment's end)
-          if (cs == 0) ps[(rg * 4 + i) * LP + kg + y * (TK / KT)] = p;
+          for (int y = 0; y < KT; ++y) {
+            const float p = ex2(s[i][y] + nm);
+            l[i] += p;                                               // (this thread's keys only, until the segment's end)
+            if (cs == 0) ps[(rg * 4 + i) * LP + kg + y * (TK / KT)] = p;
+          }
         }
       }
       copies_wait<S::OVER ? 0 : 1>();                              // V is here
@@ -264,45 +270,47 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
       }
       bad = __syncthreads_or(bad);
       // ---- product with V: four rows x CW channels, every TS-th group of four tokens
+      if (!idle) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float f = fac[rp * 4 + i];
+        for (int i = 0; i < 4; ++i) {
+          const float f = fac[rp * 4 + i];
 #pragma unroll
-        for (int x = 0; x < CW; ++x) o[i][x] *= f;
-      }
-      if (!bad) {
+          for (int x = 0; x < CW; ++x) o[i][x] *= f;
+        }
+        if (!bad) {
 #pragma unroll 2
-        for (int j = ts * 4; j < TK; j += 4 * TS) {
-          float4 p[4];
+          for (int j = ts * 4; j < TK; j += 4 * TS) {
+            float4 p[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) p[i] = *reinterpret_cast<const float4*>(ps + (rp * 4 + i) * LP + j);
+            for (int i = 0; i < 4; ++i) p[i] = *reinterpret_cast<const float4*>(ps + (rp * 4 + i) * LP + j);
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            float4 v[CW / 4];
+            for (int y = 0; y < 4; ++y) {
+              float4 v[CW / 4];
 #pragma unroll
-            for (int x = 0; x < CW / 4; ++x) v[x] = *reinterpret_cast<const float4*>(vs + (j + y) * D + x * (D * 4 / CW) + cg * 4);
+              for (int x = 0; x < CW / 4; ++x) v[x] = *reinterpret_cast<const float4*>(vs + (j + y) * D + x * (D * 4 / CW) + cg * 4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float w = y == 0 ? p[i].x : y == 1 ? p[i].y : y == 2 ? p[i].z : p[i].w;
+              for (int i = 0; i < 4; ++i) {
+                const float w = y == 0 ? p[i].x : y == 1 ? p[i].y : y == 2 ? p[i].z : p[i].w;
 #pragma unroll
-              for (int x = 0; x < CW / 4; ++x) {
-                float2* d = reinterpret_cast<float2*>(&o[i][x * 4]);
-                d[0] = __ffma2_rn(make_float2(w, w), make_float2(v[x].x, v[x].y), d[0]);
-                d[1] = __ffma2_rn(make_float2(w, w), make_float2(v[x].z, v[x].w), d[1]);
+                for (int x = 0; x < CW / 4; ++x) {
+                  float2* d = reinterpret_cast<float2*>(&o[i][x * 4]);
+                  d[0] = __ffma2_rn(make_float2(w, w), make_float2(v[x].x, v[x].y), d[0]);
+                  d[1] = __ffma2_rn(make_float2(w, w), make_float2(v[x].z, v[x].w), d[1]);
+                }
               }
             }
           }
-        }
-      } else {                                                     // 0 x infinity is no 0: hidden keys stay out
+        } else {                                                     // 0 x infinity is no 0: hidden keys stay out
 #pragma unroll 1
-        for (int j = ts; j < TK; j += TS)
+          for (int j = ts; j < TK; j += TS)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = rp * 4 + i;
-            if (tok0 + j < lo_s[r] || tok0 + j >= hi_s[r]) continue;
+            for (int i = 0; i < 4; ++i) {
+              const int r = rp * 4 + i;
+              if (tok0 + j < lo_s[r] || tok0 + j >= hi_s[r]) continue;
 #pragma unroll
-            for (int x = 0; x < CW; ++x) o[i][x] = fmaf(ps[r * LP + j], vs[j * D + x / 4 * (D * 4 / CW) + cg * 4 + x % 4], o[i][x]);
-          }
+              for (int x = 0; x < CW; ++x) o[i][x] = fmaf(ps[r * LP + j], vs[j * D + x / 4 * (D * 4 / CW) + cg * 4 + x % 4], o[i][x]);
+            }
+        }
       }
       __syncthreads();                                             // (V and P are used up)
       if (t + 1 < t_to) {
