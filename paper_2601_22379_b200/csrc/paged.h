@@ -72,6 +72,7 @@ struct PagedWork {
   int rows;                             // rows that a partial result holds
   float* part_o;                        // [2 n_cta][rows][d]
   float2* part_ml;                      // [2 n_cta][rows]  maximum (base 2), sum
+  float* drain;                         // [2 n_cta][128 (d + 1)]  what the tensor cores' sums so far have been taken into (null: no walk is that long)
   int4* cuts;                           // [n_cta] of the unit whose first cut is the start of a share: rows (0: no such unit), parts, first row of its tokens, KV head
 };
 
@@ -337,6 +338,7 @@ void paged_plan_general(PagedWork* w, const PagedBatch& pb, const PagedLayout& p
 cudaError_t launch_paged_general(const PagedAttend& a, const void* k_pages, const void* v_pages, int q_bf16, int kv_bf16, cudaStream_t s);
 cudaError_t launch_paged_join(const PagedAttend& a, int out_bf16, cudaStream_t s);
 // paged_mma.cu: bf16 on tcgen05
+size_t paged_mma_drain_bytes(const PagedWork& w, const PagedBatch& pb, const PagedLayout& pl);
 int paged_mma_positions(const PagedBatch& pb, const PagedLayout& pl);   // new tokens of a row tile: the query boxes' size
 void paged_plan_mma(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int sm_count);
 cudaError_t launch_paged_mma(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s);

@@ -184,22 +184,26 @@ extern "C" int spla_paged_append(spla_paged_t* p, const spla_paged_batch_t* batc
   return e == cudaSuccess ? SPLA_OK : cuda_fail(e, "spla_paged_append");
 }
 
-// The plan of one launch (a batch of at most kPagedMaxBatch sequences) and the bytes of its partial results.
-static size_t plan_attend(const spla_paged* p, const PagedBatch& pb, bool tensor, PagedWork* w) {
+// The plan of one launch (a batch of at most kPagedMaxBatch sequences), the bytes of its partial results and of the sums of long walks,
+// and their places in the workspace, where there is one (no cuts: whole units only).
+static size_t plan_attend(const spla_paged* p, const PagedBatch& pb, bool tensor, PagedWork* w, void* workspace) {
   if (tensor) paged_plan_mma(w, pb, p->pl, p->sm_count);
   else paged_plan_general(w, pb, p->pl, p->sm_count);
-  if (w->by_unit || w->n_cta < 2) return 0;
-  const size_t rows = (size_t)2 * w->n_cta * w->rows;
-  return align_up(rows * p->pl.d * 4, 256) + align_up(rows * 8, 256) + align_up((size_t)w->n_cta * 16, 256);
-}
-// ... and their places in the workspace (no cuts: whole units only).
-static void place_parts(const spla_paged* p, size_t bytes, void* workspace, PagedWork* w) {
-  if (!bytes) return;
-  const size_t rows = (size_t)2 * w->n_cta * w->rows;
-  char* at = reinterpret_cast<char*>(workspace);
-  w->part_o = reinterpret_cast<float*>(at);
-  w->part_ml = reinterpret_cast<float2*>(at + align_up(rows * p->pl.d * 4, 256));
-  w->cuts = reinterpret_cast<int4*>(at + align_up(rows * p->pl.d * 4, 256) + align_up(rows * 8, 256));
+  size_t used = 0;
+  auto take = [&](size_t bytes) {
+    char* at = workspace ? reinterpret_cast<char*>(workspace) + used : nullptr;
+    used += align_up(bytes, 256);
+    return reinterpret_cast<void*>(at);
+  };
+  if (!w->by_unit && w->n_cta >= 2) {
+    const size_t rows = (size_t)2 * w->n_cta * w->rows;
+    w->part_o = reinterpret_cast<float*>(take(rows * p->pl.d * 4));
+    w->part_ml = reinterpret_cast<float2*>(take(rows * 8));
+    w->cuts = reinterpret_cast<int4*>(take((size_t)w->n_cta * 16));
+  }
+  const size_t drain = tensor ? paged_mma_drain_bytes(*w, pb, p->pl) : 0;
+  if (drain) w->drain = reinterpret_cast<float*>(take(drain));
+  return used;
 }
 
 static PagedBatch part_of(PagedBatch b, int first) {
@@ -225,7 +229,7 @@ extern "C" int spla_paged_query_workspace(const spla_paged_t* p, const spla_page
     part.batch = pb.batch - first < kPagedMaxBatch ? pb.batch - first : kPagedMaxBatch;
     for (int tensor = 0; tensor <= (p->tensor ? 1 : 0); ++tensor) {   // (queries that TMA does not take go to the general kernel)
       PagedWork w = {};
-      const size_t n = plan_attend(p, part, tensor != 0, &w);
+      const size_t n = plan_attend(p, part, tensor != 0, &w, nullptr);
       if (n > most) most = n;
     }
   }
@@ -280,7 +284,7 @@ extern "C" int spla_paged_attend(spla_paged_t* p, const spla_paged_batch_t* batc
     a.pb = part_of(pb, first);
     a.prefix = mask->prefix_lens ? mask->prefix_lens + first : nullptr;
     a.w = PagedWork{};
-    place_parts(p, plan_attend(p, a.pb, tensor, &a.w), workspace, &a.w);
+    plan_attend(p, a.pb, tensor, &a.w, workspace);
     e = tensor ? launch_paged_mma(a, maps, s) : launch_paged_general(a, p->k_pages, p->v_pages, q16, kv16, s);
     if (e == cudaSuccess) e = launch_paged_join(a, q16, s);
   }

@@ -12,7 +12,8 @@
 // end.  (One warp with all 128 keys of the rows was the whole chain: capped scores of 64 ragged sequences 978 us, 618 so.)
 // P takes the place of S in tensor memory, as the left operand of O += P V, rounded to bf16, half a step of 2^-8, as the outputs are;
 // its sum l is of the unrounded values, so that lse is as exact as the scores.  The maximum is a stale one: O is rescaled only when it
-// grows by more than 2^8.
+// grows by more than 2^8.  The tensor core truncates when it adds into an accumulator: every kPmDrain tiles the softmax warps take O into fp32
+// sums of their own in the workspace (sums of a million keys came out 0.4 % low without, of four million 2.3 %).
 //
 // Warps: 0 and 2 TMA (pages of K and the query rows as boxes of G heads x positions; pages of V), 1 the MMA issuer, 3 plans the
 // segments ahead of the others, 4 to 7 and 8 to 11 softmax and epilogue of either row tile, one row per thread.
@@ -41,6 +42,7 @@ namespace {
 
 constexpr int kPmThreads = 384;
 constexpr int kPmKeys = 128;                       // keys per tile
+constexpr int kPmDrain = 128;                      // tiles that are added up in O before it is drained: 1024 truncations, each of less than 2^-23: 2^-13 at most
 constexpr uint32_t kPmTmemCols = 512;              // S0, S1, O0, O1: 128 columns each
 
 template <int D, bool FEW>
@@ -166,7 +168,53 @@ __device__ __forceinline__ uint32_t bits_between(int a, int e) {
 }
 __device__ __forceinline__ uint32_t pair_not_finite(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 
-template <int D, bool MODS, bool FEW>
+// A thread's row of O into its sums, [slot of a CTA][D / 4][128 threads] 16 bytes each and then [128] of l: sums = sums f + O, or O where there
+// are none yet.  And back, for the end of a segment: O = sums f + O; returns l.
+__device__ __forceinline__ float* pm_sums(float* drain, int slot, int d) { return drain + (2LL * blockIdx.x + slot) * (128 * (d + 1)); }
+template <int D>
+__device__ __forceinline__ void pm_drain(uint32_t tO, float* drain, int slot, int thr, float f, bool fresh, float l) {
+  float *place = pm_sums(drain, slot, D) + 4 * thr, *place_l = pm_sums(drain, slot, D) + 128 * D + thr;
+#pragma unroll 1
+  for (int c = 0; c < D; c += 16) {
+    uint32_t o[16];
+    tmem_ld16_async(tO + c, o);
+    tmem_ld_wait16(o);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      float4* at = reinterpret_cast<float4*>(place) + (c / 4 + x) * 128;
+      float4 v = make_float4(__uint_as_float(o[4 * x]), __uint_as_float(o[4 * x + 1]), __uint_as_float(o[4 * x + 2]), __uint_as_float(o[4 * x + 3]));
+      if (!fresh) {
+        const float4 s = *at;
+        v.x = fmaf(s.x, f, v.x); v.y = fmaf(s.y, f, v.y); v.z = fmaf(s.z, f, v.z); v.w = fmaf(s.w, f, v.w);
+      }
+      *at = v;
+    }
+  }
+  *place_l = fresh ? l : fmaf(*place_l, f, l);
+}
+template <int D>
+__device__ __forceinline__ float pm_undrain(uint32_t tO, float* drain, int slot, int thr, float f, float l) {
+  const float *place = pm_sums(drain, slot, D) + 4 * thr, *place_l = pm_sums(drain, slot, D) + 128 * D + thr;
+#pragma unroll 1
+  for (int c = 0; c < D; c += 16) {
+    uint32_t o[16];
+    tmem_ld16_async(tO + c, o);
+    tmem_ld_wait16(o);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float4 s = *(reinterpret_cast<const float4*>(place) + (c / 4 + x) * 128);
+      const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+      for (int y = 0; y < 4; ++y) o[4 * x + y] = __float_as_uint(fmaf(v[y], f, __uint_as_float(o[4 * x + y])));
+    }
+    tmem_st16(tO + c, o);
+  }
+  tmem_st_wait();
+  return fmaf(*place_l, f, l);
+}
+
+// LONG: caches of more than kPmDrain tiles (the others go without what drains O: 106 us for a mixed batch in place of 108).
+template <int D, bool MODS, bool FEW, bool LONG>
 __global__ void __launch_bounds__(kPmThreads, 1)
     paged_mma_kernel(const PagedAttend a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                      const __grid_constant__ CUtensorMap map_q) {
@@ -296,14 +344,15 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       uint32_t kt = 0;
       int seg = 0;
       uint32_t n_p0 = 0, n_p1 = 0, n_o0 = 0, n_o1 = 0;            // items whose P was awaited, segments that used O
-      // the item of either row tile whose product with V is to come: its stage and phase, whether it is the segment's first, whether
-      // V is free after it, whether the softmax warps may have formed it
+      // the item of either row tile whose product with V is to come: its stage and phase, whether it is the segment's first, its number
+      // there, whether V is free after it, whether the softmax warps may have formed it
       bool pend0 = false, pend1 = false, first0 = true, first1 = true, free0 = false, free1 = false, look0 = false, look1 = false;
-      int st0 = 0, st1 = 0;
+      int st0 = 0, st1 = 0, it0 = 0, it1 = 0;
       uint32_t ph0 = 0, ph1 = 0;
       auto product = [&](auto slot_c) {                           // O (+)= P V
         constexpr int S = decltype(slot_c)::value;
         bool &pend = S ? pend1 : pend0, &first = S ? first1 : first0;
+        int& it = S ? it1 : it0;
         uint32_t &n_p = S ? n_p1 : n_p0, &n_o = S ? n_o1 : n_o0;
         const int st = S ? st1 : st0;
         pend = false;
@@ -316,10 +365,11 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         tc_fence_after();
         if (!((S ? look1 : look0) && skip_pv[S])) {
           const uint32_t pt = tmem + S * 128, o = tmem + 256 + S * 128, v = v_lo + st * (SM::kTile / 16);
-          umma_ts4_one<8, kStep>(one, o, pt, v, id_o, first ? 0u : 1u);
+          umma_ts4_one<8, kStep>(one, o, pt, v, id_o, first || (LONG && it % kPmDrain == 0) ? 0u : 1u);
           umma_ts4_one<8, kStep>(one, o, pt + 32, v + 4 * kStep, id_o, 1u);
         }
         first = false;
+        if (LONG) ++it;
         umma_commit_one(one, &pv_done[S]);
         if (S ? free1 : free0) umma_commit_one(one, &v_empty[st]);
       };
@@ -345,6 +395,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         if (!pm_wait(q_full, seg & 1, lim, abort_flag)) return false;
         ++seg;
         first0 = first1 = true;
+        it0 = it1 = 0;
 #pragma unroll 1
         for (int t = pl.A; t < pl.E; ++t) {
           const bool act0 = pl.act<0>(t), act1 = pl.act<1>(t);
@@ -443,7 +494,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       const bool live = __any_sync(0xffffffffu, valid);
       const bool counts = valid || alike;
       const int lo_most = __reduce_max_sync(0xffffffffu, counts ? see.lo : 0), hi_least = __reduce_min_sync(0xffffffffu, counts ? see.hi : 0x7fffffff);
-      float m = -INFINITY, l = 0.f;
+      float m = -INFINITY, l = 0.f, fd = 1.f;                      // fd: what the sums of drained tiles are behind the maximum
       int done_items = 0;
 #pragma unroll 1
       for (; t < t_end; t += t_step) {
@@ -451,6 +502,13 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         const bool look = t < la || t >= le;
         bool simt = false;
         if (!pm_wait(&s_full[slot], n & 1, lim, abort_flag)) return false;
+        if (LONG && done_items > 0 && done_items % kPmDrain == 0 && live) {
+          if (!pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) return false;
+          tc_fence_after();
+          pm_drain<D>(tO, a.w.drain, slot, thr, fd, done_items == kPmDrain, l);   // (the next product starts O anew)
+          l = 0.f;
+          fd = 1.f;
+        }
         if (look) {
           // (After the scores: they were issued behind the products of all tiles up to two before this one, each of which waited for its V, so
           // that the parity below can only mean this tile.)
@@ -573,6 +631,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
             const float m_new = grow ? mt : m, f = grow ? ex2(m - m_new) : 1.f;
             m = m_new;
             l *= f;
+            if (LONG) fd *= f;
 #pragma unroll 1
             for (int c = 0; c < D; c += 16) {
               uint32_t o[16];
@@ -608,6 +667,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           tmem_st_wait();
         }
         if (simt) {
+          const bool begun = LONG ? done_items % kPmDrain != 0 : done_items > 0;          // O holds products already
           // the product with V here: O += sum over the row's visible keys of p v
           if (done_items > 0 && !pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) return false;
           if (done_items == 0 && n_used > 0 && !pm_wait(&o_free[slot], (n_used - 1) & 1, lim, abort_flag)) return false;
@@ -644,12 +704,12 @@ __global__ void __launch_bounds__(kPmThreads, 1)
               __syncwarp();
             }
             uint32_t o[16];
-            if (done_items > 0) {
+            if (begun) {
               tmem_ld16_async(tO + c, o);
               tmem_ld_wait16(o);
             }
 #pragma unroll
-            for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(done_items > 0 ? __uint_as_float(o[x]) + acc[x] : acc[x]);
+            for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(begun ? __uint_as_float(o[x]) + acc[x] : acc[x]);
             tmem_st16(tO + c, o);
           }
           tmem_st_wait();
@@ -668,6 +728,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         tc_fence_after();
         ++n_used;
       }
+      if (LONG && my > kPmDrain && live) l = pm_undrain<D>(tO, a.w.drain, slot, thr, fd, l);
       float m1 = -INFINITY, l1 = 0.f;
       if (second) {
         if (slot == 1) {                                          // the second half's maxima and sums go to the first's warps, O stays where it is
@@ -857,15 +918,19 @@ __global__ void __launch_bounds__(kPmThreads, 1)
   }
 }
 
-template <int D, bool MODS, bool FEW>
-cudaError_t mma_launch(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
-  auto kern = paged_mma_kernel<D, MODS, FEW>;
+template <int D, bool MODS, bool FEW, bool LONG>
+cudaError_t mma_variant(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
+  auto kern = paged_mma_kernel<D, MODS, FEW, LONG>;
   constexpr int bytes = PmSmem<D, FEW>::kBytes;
   static unsigned long long allowed = 0;
   cudaError_t e = allow_smem_once(kern, bytes, allowed);
   if (e != cudaSuccess) return e;
   return launch_ex(kern, dim3(a.w.n_cta), dim3(kPmThreads), bytes, s, 0, true, a, *reinterpret_cast<const CUtensorMap*>(maps.k),
                    *reinterpret_cast<const CUtensorMap*>(maps.v), *reinterpret_cast<const CUtensorMap*>(maps.q));
+}
+template <int D, bool MODS, bool FEW>
+cudaError_t mma_launch(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
+  return a.w.drain ? mma_variant<D, MODS, FEW, true>(a, maps, s) : mma_variant<D, MODS, FEW, false>(a, maps, s);
 }
 template <int D>
 cudaError_t mma_d(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
@@ -875,6 +940,10 @@ cudaError_t mma_d(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
 }
 
 }  // namespace
+
+size_t paged_mma_drain_bytes(const PagedWork& w, const PagedBatch& pb, const PagedLayout& pl) {
+  return pb.max_len > kPmDrain * kPmKeys ? (size_t)w.n_cta * 2 * 128 * (pl.d + 1) * 4 : 0;
+}
 
 int paged_mma_positions(const PagedBatch& pb, const PagedLayout& pl) { return (pb.max_new * pl.G <= 32 ? 32 : 128) / pl.G; }
 

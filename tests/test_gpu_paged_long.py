@@ -1,0 +1,91 @@
+"""Attention over a long paged cache: what the tensor cores add up stays as exact as the documentation says, however many keys there are."""
+import math
+
+import pytest
+import torch
+
+from paper_2601_22379_b200 import binding
+from tests import paged_reference as ref
+from tests.test_gpu_paged import Batch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("sequences,new,G", [(1, 148 * 16, 16), (148, 1, 8)], ids=["chunk", "single"])
+def test_sums_of_four_million_keys(d, sequences, new, G):
+    """All keys alike, so that the result is the mean of the values: every unit is walked by one CTA from end to end."""
+    L, P = 1 << 22, 128
+    g = torch.Generator(device=DEV).manual_seed(1)
+    k = torch.zeros(L // P, 1, P, d, device=DEV, dtype=torch.bfloat16)
+    v = (torch.rand(L // P, 1, P, d, device=DEV, generator=g) + 0.5).to(torch.bfloat16)
+    table = torch.arange(L // P, dtype=torch.int32, device=DEV).expand(sequences, -1).contiguous()
+    q = torch.randn(sequences * new, G, d, device=DEV, generator=g).to(torch.bfloat16)
+    cu = torch.arange(sequences + 1, dtype=torch.int32, device=DEV) * new
+    lens = torch.full((sequences,), L, dtype=torch.int32, device=DEV)
+    cache = binding.PagedCache(k, v, n_q_heads=G)
+    out, lse = cache.attend(q, cu, lens, table, new, L, prefix_lens=lens)
+    assert cache.sync_status() == 0
+    want = v.view(-1, d).double().mean(0)
+    # scores of 0: probabilities of 1, products exact.  1024 additions that truncate by less than 2^-23 of the sum between two drains; 256 drains, the
+    # sum of l in as many parts, and the division round by 2^-24 each; the output by half a step
+    err = 2.0 ** -13 + (256 + 256 + 8) * 2.0 ** -24
+    assert float((out.double() / want - 1).abs().max()) <= err + (1 + err) * 2.0 ** -8
+    assert abs(float((out.double() / want - 1).mean())) <= err + 2.0 ** -8 / 4     # (and the roundings of many outputs go either way)
+    assert float((lse.double() - math.log(L)).abs().max()) <= 2.0 ** -22 * (1 + math.log(L))
+
+
+def _rising(b, top):
+    """Keys whose scores grow along the sequence, so that the running maximum moves again and again."""
+    for s, x in enumerate(b.lens):
+        j = torch.arange(x)
+        page = b.table_cpu[s].long()[j // b.P]
+        grow = (1 + top * j.double() / x).to(b.kv_t)
+        b.k[page, :, j % b.P] = (b.k[page, :, j % b.P].double() * grow.double()[:, None, None]).to(b.kv_t)
+    b.kd.copy_(b.k)
+
+
+@pytest.mark.parametrize("d,hq,hkv", [(64, 4, 1), (128, 5, 1)])
+@pytest.mark.parametrize("new,old", [([150], [40000]), ([40, 1], [33000, 70]), ([3], [70000]), ([70], [16384 - 70]), ([130], [16384 - 100])],
+                         ids=["two-row-tiles", "one-row-tile", "few", "no-drain", "just-one"])
+@pytest.mark.parametrize("mask", ["causal", "cap", "window"])
+def test_walks_that_are_drained(d, hq, hkv, new, old, mask):
+    """More tiles than are added up in one go, with maxima that move before and after.  One KV head and copies of the sequence keep all CTAs busy, so that a
+    unit's walk is long."""
+    copies = 160 if len(new) == 1 else 80
+    b = Batch(new, old, hq=hq, hkv=hkv, d=d, P=128)
+    _rising(b, 3.0)
+    kw = {"causal": {}, "cap": dict(softcap=20.0), "window": dict(window=30000)}[mask]
+    n = b.total
+    cu = torch.cat([b.cu_cpu[:-1].long() + n * i for i in range(copies)] + [torch.tensor([n * copies])]).to(torch.int32).to(DEV)
+    q = b.qd.repeat(copies, 1, 1)
+    out, lse = b.cache.attend(q, cu, b.lens_t.repeat(copies), b.table.repeat(copies, 1), b.max_new, b.max_len, **kw)
+    assert b.cache.sync_status() == 0
+    o, l, ob, lb = ref.attend(b.q, b.k, b.v, b.cu_cpu, b.lens, b.table_cpu, tensor_cores=True, **kw)
+    # (truncations between two drains: 2^-13 of the values' mean magnitude, a 32nd of what the probabilities' rounding may add)
+    for i in (0, 1, copies // 2, copies - 1):
+        ref.check(lse[i * n:(i + 1) * n], l, lb, what="lse")
+        ref.check(out[i * n:(i + 1) * n], o, ob * (1 + 2.0 ** -5), b.q_t, "out")
+    again, lse2 = b.cache.attend(q, cu, b.lens_t.repeat(copies), b.table.repeat(copies, 1), b.max_new, b.max_len, **kw)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("old", [16384 - 140, 16384 - 1, 32768 - 100, 32768 + 20])
+@pytest.mark.parametrize("new", [150, 40])
+def test_not_finite_values_just_after_a_drain(new, old):
+    """Values that are not finite, of later tokens, in the first tiles after the sums were taken away."""
+    copies = 160
+    b = Batch([new], [old], hq=2, hkv=1, d=128, P=128)
+    cu = (torch.arange(copies + 1, dtype=torch.int32) * new).to(DEV)
+    args = (b.qd.repeat(copies, 1, 1), cu, b.lens_t.repeat(copies), b.table.repeat(copies, 1), b.max_new, b.max_len)
+    o, l, ob, lb = ref.attend(b.q, b.k, b.v, b.cu_cpu, b.lens, b.table_cpu, tensor_cores=True)
+    hit = old + new // 2                                                      # seen by the second half of the new tokens
+    b.vd[int(b.table_cpu[0, hit // b.P]), 0, hit % b.P, 5] = math.nan
+    out, lse = b.cache.attend(*args)
+    assert b.cache.sync_status() == 0
+    assert bool(torch.isnan(out.view(copies, new, 2, 128)[:, new // 2:, :, 5]).all())
+    o[new // 2:, :, 5] = math.nan                                             # (left out of the comparison)
+    for i in (0, copies - 1):
+        ref.check(lse[i * new:(i + 1) * new], l, lb, what="lse")
+        ref.check(out[i * new:(i + 1) * new], o, ob * (1 + 2.0 ** -5), b.q_t, "out")
