@@ -523,12 +523,17 @@ class PagedCache:
         d, xs = self.head_dim, x.stride()
         if not (x.shape == (total, heads, d) and x.dtype is dtype and x.device == self.device and xs[2] == 1 and xs[1] == d):
             raise ValueError(f"paged cache: {what} [tokens, {heads}, {d}] of its type, heads contiguous")
-        return xs[0] if total > 1 else heads * d
+        if total <= 1:
+            return heads * d
+        if xs[0] < heads * d:                                                # (0, an expanded tensor's, would mean "dense" to the library)
+            raise ValueError(f"paged cache: {what} whose tokens are at least {heads * d} elements apart")
+        return xs[0]
 
     def append(self, k: torch.Tensor, v: torch.Tensor, cu_new: torch.Tensor, seq_lens: torch.Tensor, page_table: torch.Tensor,
                q: torch.Tensor | None = None, rope: Rope | None = None, positions: torch.Tensor | None = None, q_out: torch.Tensor | None = None):
         """Stores k, v [total, H_kv, d] at the last n_b positions of every sequence, keys rotated by `rope`; rotates q [total, H_q, d]
-        beside them and returns it (None without q).  Tokens may be any stride apart; `q_out=q` works in place."""
+        beside them and returns it (None without q).  Tokens may be any stride apart that keeps them off each other (no expanded tensors);
+        `q_out=q` works in place."""
         total, hkv, kt = k.shape[0], self.n_kv_heads, self.k_pages.dtype
         ks = self._rows(k, total, hkv, kt, "k")
         vs = self._rows(v, total, hkv, kt, "v")

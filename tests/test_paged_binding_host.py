@@ -1,0 +1,46 @@
+"""What the binding of the paged cache and the rotary positions refuses before it calls the library: tensors on the CPU, no device."""
+import pytest
+import torch
+
+from paper_2601_22379_b200 import binding
+
+
+def cache(hq=4, hkv=2, d=64, P=16):
+    """A cache without a handle: a call that gets past the checks of its tensors fails in the library."""
+    c = binding.PagedCache.__new__(binding.PagedCache)
+    c.k_pages = c.v_pages = torch.zeros(3, hkv, P, d)
+    c.device, c.index = torch.device("cpu"), 0
+    c.page_size, c.n_q_heads, c.n_kv_heads, c.head_dim, c.q_torch_dtype = P, hq, hkv, d, torch.float32
+    return c
+
+
+def sequences(total):
+    i = lambda *x: torch.tensor(x, dtype=torch.int32)  # noqa: E731
+    return i(0, total), i(total), torch.arange(3, dtype=torch.int32)[None]
+
+
+def expanded(heads, total=5, d=64):
+    """One token, repeated by a stride of 0."""
+    return torch.zeros(1, heads, d).expand(total, heads, d)
+
+
+@pytest.mark.parametrize("bad", ["k", "v", "q", "q_out"])
+def test_append_refuses_tokens_that_lie_on_each_other(bad):
+    x = dict(k=torch.zeros(5, 2, 64), v=torch.zeros(5, 2, 64), q=torch.zeros(5, 4, 64), q_out=torch.zeros(5, 4, 64))
+    x[bad] = expanded(2 if bad in "kv" else 4)
+    with pytest.raises(ValueError, match="elements apart"):
+        cache().append(x["k"], x["v"], *sequences(5), q=x["q"], q_out=x["q_out"])
+
+
+def test_attend_refuses_queries_that_lie_on_each_other():
+    for q in (expanded(4), torch.zeros(5 * 64 + 4 * 64).as_strided((5, 4, 64), (64, 64, 1))):
+        with pytest.raises(ValueError, match="elements apart"):
+            cache().attend(q, *sequences(5), 5, 48)
+
+
+def test_strides_of_tokens():
+    c = cache()
+    rows = lambda x, heads: c._rows(x, x.shape[0], heads, torch.float32, "x")  # noqa: E731
+    assert rows(torch.zeros(5, 4, 64), 4) == 256
+    assert rows(torch.zeros(5, 9, 64)[:, 2:6], 4) == 576                      # inside a packed projection
+    assert rows(expanded(4, total=1), 4) == 256                               # one token has no neighbour
