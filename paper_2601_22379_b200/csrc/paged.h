@@ -94,8 +94,8 @@ struct PagedAttend {
 
 // Sequence table of a CTA, in shared memory.
 struct PagedSeqs {
-  long long pre[kPagedMaxBatch + 1];    // tiles (units) before a sequence, all heads
-  int row0[kPagedMaxBatch], n[kPagedMaxBatch], L[kPagedMaxBatch], prefix[kPagedMaxBatch], per_head[kPagedMaxBatch];   // per_head: tiles (units) of one head
+  long long pre[kPagedMaxBatch + 1];    // tiles (units) before a sequence, all heads (2^31 in one head: 40000 new tokens behind 2^24 cached ones, G = 16)
+  int row0[kPagedMaxBatch], n[kPagedMaxBatch], L[kPagedMaxBatch], prefix[kPagedMaxBatch];
 };
 
 __host__ __device__ __forceinline__ int paged_units(const PagedWork& w, int n) { return n <= w.ppos ? (n > 0) : (n + w.upos - 1) / w.upos; }
@@ -123,18 +123,24 @@ __device__ __forceinline__ int paged_unit_tiles(const PagedAttend& a, int row0, 
 }
 
 // What one sequence counts for, per head.  Whole warps: sequences of many units are counted by the warp together.
-__device__ __forceinline__ int paged_seq_tiles(const PagedAttend& a, int row0, int n, int L, int prefix, int lane) {
+__device__ __forceinline__ long long paged_seq_tiles(const PagedAttend& a, int row0, int n, int L, int prefix, int lane) {
   const int nu = paged_units(a.w, n);
-  int sum = 0;
+  int few = 0;
   if (nu <= 4)
-    for (int u = 0; u < nu; ++u) sum += paged_unit_tiles(a, row0, n, L, prefix, u);
+    for (int u = 0; u < nu; ++u) few += paged_unit_tiles(a, row0, n, L, prefix, u);
+  long long sum = few;
   for (unsigned many = __ballot_sync(0xffffffffu, nu > 4); many; many &= many - 1) {
     const int who = __ffs(many) - 1;
     const int n_ = __shfl_sync(0xffffffffu, n, who), L_ = __shfl_sync(0xffffffffu, L, who), p_ = __shfl_sync(0xffffffffu, prefix, who),
               nu_ = __shfl_sync(0xffffffffu, nu, who), r_ = __shfl_sync(0xffffffffu, row0, who);
-    int part = 0;
+    long long part = 0;
     for (int u = lane; u < nu_; u += 32) part += paged_unit_tiles(a, r_, n_, L_, p_, u);
-    part = __reduce_add_sync(0xffffffffu, part);
+    if (a.w.narrow) {
+      part = __reduce_add_sync(0xffffffffu, (int)part);
+    } else {
+#pragma unroll 1
+      for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
+    }
     if (lane == who) sum = part;
   }
   return sum;
@@ -160,9 +166,8 @@ __device__ __forceinline__ long long paged_fill_seqs(const PagedAttend& a, Paged
       row0 = s.row0; n = s.n; L = s.L;
       t.row0[lane] = row0; t.n[lane] = n; t.L[lane] = L; t.prefix[lane] = pre;
     }
-    const int per_head = paged_seq_tiles(a, row0, n, L, pre, lane);
-    const long long v = a.w.narrow ? paged_scan(per_head * a.pl.Hkv, lane) : paged_scan((long long)per_head * a.pl.Hkv, lane);
-    if (lane < batch) t.per_head[lane] = per_head;
+    const long long per_head = paged_seq_tiles(a, row0, n, L, pre, lane);
+    const long long v = a.w.narrow ? paged_scan((int)per_head * a.pl.Hkv, lane) : paged_scan(per_head * a.pl.Hkv, lane);
     if (lane < batch) t.pre[lane + 1] = v;
     if (lane == 0) t.pre[0] = 0;
     __syncthreads();
@@ -177,15 +182,15 @@ __device__ __forceinline__ long long paged_fill_seqs(const PagedAttend& a, Paged
       row0 = s.row0; n = s.n; L = s.L;
       t.row0[b] = row0; t.n[b] = n; t.L[b] = L; t.prefix[b] = pre;
     }
-    const int per_head = paged_seq_tiles(a, row0, n, L, pre, lane);
-    if (b < batch) t.per_head[b] = per_head;
+    const long long per_head = paged_seq_tiles(a, row0, n, L, pre, lane);
+    if (b < batch) t.pre[b + 1] = per_head * a.pl.Hkv;
   }
   __syncthreads();
   if (tid < 32) {
     long long carry = 0;
     for (int b0 = 0; b0 < batch; b0 += 32) {
       const int b = b0 + tid;
-      const long long v = paged_scan(b < batch ? (long long)t.per_head[b] * a.pl.Hkv : 0ll, tid) + carry;
+      const long long v = paged_scan(b < batch ? t.pre[b + 1] : 0ll, tid) + carry;
       carry = __shfl_sync(0xffffffffu, v, 31);
       if (b < batch) t.pre[b + 1] = v;
     }
@@ -225,13 +230,13 @@ struct PagedWalk {
       if (in != 0xffffffffu) break;
     }
     load(a.w, t);
-    const int per_head = t.per_head[b];
-    const long long rem = at - t.pre[b];
+    const long long rem = at - t.pre[b], all = t.pre[b + 1] - t.pre[b];
+    const long long per_head = a.w.narrow ? (long long)((unsigned)all / (unsigned)a.pl.Hkv) : all / a.pl.Hkv;
     h = a.w.narrow ? (int)((unsigned)rem / (unsigned)per_head) : (int)(rem / per_head);
-    int in_head = (int)(rem - (long long)h * per_head);
+    long long in_head = rem - h * per_head;
     if (units == 1) {
       u = 0;
-      off = in_head;
+      off = (int)in_head;
       return true;
     }
     const int nu = units;
@@ -246,7 +251,7 @@ struct PagedWalk {
       const unsigned past = __ballot_sync(0xffffffffu, upto > in_head);
       if (past || u + 32 >= nu) {
         const int who = past ? __ffs(past) - 1 : 0;
-        off = in_head - __shfl_sync(0xffffffffu, upto - c, who);
+        off = (int)in_head - __shfl_sync(0xffffffffu, upto - c, who);
         u += who;
         break;
       }

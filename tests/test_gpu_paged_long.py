@@ -89,3 +89,25 @@ def test_not_finite_values_just_after_a_drain(new, old):
     for i in (0, copies - 1):
         ref.check(lse[i * new:(i + 1) * new], l, lb, what="lse")
         ref.check(out[i * new:(i + 1) * new], o, ob * (1 + 2.0 ** -5), b.q_t, "out")
+
+
+@pytest.mark.parametrize("kv", ["bf16", "f32"])
+@pytest.mark.parametrize("few", [True, False])
+def test_bounds_whose_tiles_pass_32_bits(kv, few):
+    """Bounds so loose that the tiles which they allow pass 2^31: the work is dealt out in 64 bits, the results are the same within rounding."""
+    g = torch.Generator().manual_seed(5)
+    n = 384
+    new = torch.randint(0, 3 if few else 70, (n,), generator=g).tolist()
+    old = torch.randint(0, 900, (n,), generator=g).tolist()
+    hkv = 64
+    b = Batch(new, old, hq=hkv, hkv=hkv, d=64, P=128, kv=kv, extra_cols=(1 << 24) // 128 - 8)
+    assert hkv * n * (1 << 24) // 128 > 1 << 31
+    tight, tight_lse = b.attend()
+    out, lse = b.attend(max_len=1 << 24)
+    assert b.cache.sync_status() == 0
+    some = [0, 1, 2, 200, n - 2, n - 1]
+    b.check(out, lse, seqs=some)
+    b.check(tight, tight_lse, seqs=some)
+    # (both within half a step of the type and the probabilities' rounding of the same numbers: values' mean magnitude below 1)
+    lim = 2.0 ** -8 * (tight.float().abs() + 2) * 2 if kv == "bf16" else torch.full_like(tight, 1e-5)
+    assert bool(((out.float() - tight.float()).abs() <= lim).all()) and float((lse - tight_lse).abs().max()) < 1e-5
