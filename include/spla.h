@@ -367,7 +367,8 @@ int spla_paged_destroy(spla_paged_t *paged);   /* NULL is allowed */
  * The new tokens of a call: rows cu_new[b] .. cu_new[b + 1] - 1 belong to sequence b and are its last n_b tokens, at positions
  * seq_lens[b] - n_b ..; seq_lens counts them.  Rows from cu_new[batch] on are not touched.  Position x of sequence b lies in page
  * page_table[b * table_stride + x / P].  A sequence whose numbers are not consistent (cu_new not ascending inside [0, total_new],
- * n_b > max_new, seq_lens[b] < n_b or > max_len) is skipped, its rows are not touched, and SPLA_ERR_BOUNDS is latched.  The
+ * n_b > max_new, seq_lens[b] < n_b or > max_len) is skipped, its rows are not touched, and SPLA_ERR_BOUNDS is latched; so is one
+ * whose cu_new[b] is below an earlier one inside [0, total_new]: no row belongs to two sequences.  The
  * tokens of a page number outside [0, n_pages) are not stored, read as zeros, and latch SPLA_ERR_BOUNDS.  Sequences may share
  * pages that they read; a position that is written belongs to one sequence.
  */

@@ -31,6 +31,7 @@ struct PagedBatch {
   const int* lens;                      // [batch] cached tokens, the new ones included
   const int* table;                     // [batch][table_stride]
   int batch, total_new, max_new, max_len, table_stride;
+  int first;                            // sequences of the call before these (earlier launches')
 };
 
 struct PagedLayout {
@@ -40,18 +41,71 @@ struct PagedLayout {
 };
 
 // One sequence's new tokens: first row, count, cached tokens; n = 0 where there is nothing to do or the numbers do not fit together.
+// Besides, a sequence is served only if no earlier prefix sum inside [0, total_new] is above its first row, so that a row has one owner
+// whatever the prefix sums are.  That takes a look at them all only where some sequence's own numbers do not fit (prefix sums that
+// do not ascend belong to one whose do not).
 struct PagedSeq {
   int row0, n, L;
+  bool fits;
 };
 __device__ __forceinline__ PagedSeq paged_seq(const PagedBatch& pb, int* status, int b) {
   const int r0 = __ldg(pb.cu + b), r1 = __ldg(pb.cu + b + 1), L = __ldg(pb.lens + b);
-  PagedSeq s{r0, r1 - r0, L};
-  const bool fits = r0 >= 0 && r1 >= r0 && r1 <= pb.total_new && r1 - r0 <= pb.max_new && L >= r1 - r0 && L <= pb.max_len;
-  if (!fits) {
+  PagedSeq s{r0, r1 - r0, L, false};
+  s.fits = r0 >= 0 && r1 >= r0 && r1 <= pb.total_new && r1 - r0 <= pb.max_new && L >= r1 - r0 && L <= pb.max_len;
+  if (!s.fits) {
     atomicExch(status, kStatusBounds);
     s.n = 0;
   }
   return s;
+}
+
+// A prefix sum for comparisons of order: those outside [0, total_new] take no part.
+__device__ __forceinline__ int paged_order(const PagedBatch& pb, int c) { return c >= 0 && c <= pb.total_new ? c : -1; }
+// The largest of a warp's values up to each lane, and `before`.
+__device__ __forceinline__ int paged_max_scan(int v, int before, int lane) {
+  v = max(v, before);
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) v = max(v, __shfl_up_sync(0xffffffffu, v, o));   // (lanes below o get their own)
+  return v;
+}
+// The sequence that may own a row of the new tokens, -1: none.  Lane k < K of a warp asks for row + k step.  (Its own numbers are the caller's to check.)
+// The last one that starts at or before the row, as long as the prefix sums ascend.  Where they do not, the one before the first prefix sum above
+// the row, if no earlier one is above its own.
+template <int K>
+__device__ __forceinline__ int paged_owner(const PagedBatch& pb, int row, int step, int lane) {
+  int at = -1;
+  bool ascend = true;
+  for (int b0 = 0; b0 < pb.batch; b0 += 32) {
+    const int b = b0 + lane, c = b < pb.batch ? __ldg(pb.cu + b) : 0x7fffffff;
+    if (b > 0 && b < pb.batch) ascend &= c >= __ldg(pb.cu + b - 1);
+    bool more = false;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const unsigned in = __ballot_sync(0xffffffffu, c <= row + k * step);
+      if (lane == k) at += __popc(in);
+      more |= in == 0xffffffffu;
+    }
+    if (!more) break;
+  }
+  if (__all_sync(0xffffffffu, ascend)) return at;
+  at = -1;
+  int top = -1;
+  bool open = true;
+#pragma unroll 1
+  for (int b0 = 0; b0 < pb.batch; b0 += 32) {
+    const int c = b0 + lane < pb.batch ? paged_order(pb, __ldg(pb.cu + b0 + lane)) : 0x7fffffff, upto = paged_max_scan(c, top, lane);
+    const unsigned sound = __ballot_sync(0xffffffffu, c == upto);
+    top = __shfl_sync(0xffffffffu, upto, 31);
+#pragma unroll 1
+    for (int k = 0; k < K; ++k) {
+      const unsigned in = __ballot_sync(0xffffffffu, c <= row + k * step);
+      if (lane != k || !open) continue;
+      open = in == 0xffffffffu;
+      const int last = open ? 31 : __ffs(~in) - 2;
+      if (last >= 0) at = (sound >> last) & 1 ? b0 + last : -1;
+    }
+  }
+  return at;
 }
 
 // ---- division of the attention's work --------------------------------------------------------------------------------
@@ -158,12 +212,19 @@ __device__ __forceinline__ N paged_scan(N v, int lane) {                   // in
 // Fills the table; all threads of the CTA (whole warps), ends with a barrier.  Returns the total.
 __device__ __forceinline__ long long paged_fill_seqs(const PagedAttend& a, PagedSeqs& t, int tid, int threads) {
   const int batch = a.pb.batch, lane = tid & 31;
-  if (batch <= 32) {                    // every warp for itself, all of them the same values: one barrier, which is the caller's anyway
+  if (batch <= 32 && a.pb.first == 0) { // every warp for itself, all of them the same values: one barrier, which is the caller's anyway
     int row0 = 0, n = 0, L = 0, pre = 0;
+    bool fits = true;
     if (lane < batch) {
       pre = a.prefix ? __ldg(a.prefix + lane) : 0;
       const PagedSeq s = paged_seq(a.pb, a.pl.status, lane);
-      row0 = s.row0; n = s.n; L = s.L;
+      row0 = s.row0; n = s.n; L = s.L; fits = s.fits;
+    }
+    if (!__all_sync(0xffffffffu, fits)) {
+      const int c = paged_order(a.pb, row0);
+      if (c != paged_max_scan(lane < batch ? c : -1, -1, lane)) n = 0;
+    }
+    if (lane < batch) {
       t.row0[lane] = row0; t.n[lane] = n; t.L[lane] = L; t.prefix[lane] = pre;
     }
     const long long per_head = paged_seq_tiles(a, row0, n, L, pre, lane);
@@ -173,23 +234,38 @@ __device__ __forceinline__ long long paged_fill_seqs(const PagedAttend& a, Paged
     __syncthreads();
     return t.pre[batch];
   }
+  bool fits = true;
+  for (int b = tid - a.pb.first; b < 0; b += threads) {              // (sequences of earlier launches: their prefix sums)
+    const int c = __ldg(a.pb.cu + b);
+    fits &= c >= 0 && c <= __ldg(a.pb.cu + b + 1) && c <= a.pb.total_new;
+  }
   for (int b0 = tid - lane; b0 < batch; b0 += threads) {
     const int b = b0 + lane;
     int row0 = 0, n = 0, L = 0, pre = 0;
     if (b < batch) {
       pre = a.prefix ? __ldg(a.prefix + b) : 0;
       const PagedSeq s = paged_seq(a.pb, a.pl.status, b);
-      row0 = s.row0; n = s.n; L = s.L;
+      row0 = s.row0; n = s.n; L = s.L; fits &= s.fits;
       t.row0[b] = row0; t.n[b] = n; t.L[b] = L; t.prefix[b] = pre;
     }
     const long long per_head = paged_seq_tiles(a, row0, n, L, pre, lane);
     if (b < batch) t.pre[b + 1] = per_head * a.pl.Hkv;
   }
-  __syncthreads();
+  const bool look = __syncthreads_or(!fits);
   if (tid < 32) {
+    int top = -1;
+    if (look) {
+      for (int b = tid - a.pb.first; b < 0; b += 32) top = max(top, paged_order(a.pb, __ldg(a.pb.cu + b)));
+      top = __reduce_max_sync(0xffffffffu, top);
+    }
     long long carry = 0;
     for (int b0 = 0; b0 < batch; b0 += 32) {
       const int b = b0 + tid;
+      if (look) {
+        const int c = b < batch ? paged_order(a.pb, t.row0[b]) : -1, upto = paged_max_scan(c, top, tid);
+        top = __shfl_sync(0xffffffffu, upto, 31);
+        if (b < batch && c != upto) { t.n[b] = 0; t.pre[b + 1] = 0; }
+      }
       const long long v = paged_scan(b < batch ? t.pre[b + 1] : 0ll, tid) + carry;
       carry = __shfl_sync(0xffffffffu, v, 31);
       if (b < batch) t.pre[b + 1] = v;

@@ -150,7 +150,7 @@ static int check_batch(const spla_paged* p, const spla_paged_batch_t* b, bool po
 
 static PagedBatch device_batch(const spla_paged_batch_t* b) {
   return PagedBatch{b->cu_new, b->seq_lens, b->page_table, b->batch, b->total_new, b->max_new < b->total_new ? b->max_new : b->total_new,
-                    b->max_len, b->table_stride};
+                    b->max_len, b->table_stride, 0};
 }
 
 extern "C" int spla_paged_append(spla_paged_t* p, const spla_paged_batch_t* batch, const spla_rope_t* rope, const int32_t* positions,
@@ -207,6 +207,7 @@ static size_t plan_attend(const spla_paged* p, const PagedBatch& pb, bool tensor
 }
 
 static PagedBatch part_of(PagedBatch b, int first) {
+  b.first = first;
   b.cu += first; b.lens += first; b.table += (long long)first * b.table_stride;
   b.batch = b.batch - first < kPagedMaxBatch ? b.batch - first : kPagedMaxBatch;
   return b;

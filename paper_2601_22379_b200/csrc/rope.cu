@@ -138,20 +138,9 @@ __global__ void __launch_bounds__(kRopeThreads, sizeof(T) == 4 ? 5 : 4)
       for (int b = tid; b < r.pb.batch; b += kRopeThreads) paged_seq(r.pb, r.pl.status, b);
     // a warp's tokens: warp, warp + 8, ...; lane k ends up with the k-th
     const int tok = tok0 + warp + lane * (kRopeThreads / 32);
-    int at = -1;                                          // the last b with cu[b] <= tok
-    for (int b0 = 0; b0 < r.pb.batch; b0 += 32) {
-      const int cu = b0 + lane < r.pb.batch ? __ldg(r.pb.cu + b0 + lane) : 0x7fffffff;
-      bool all = false;
-#pragma unroll
-      for (int k = 0; k < kRopePerWarp; ++k) {
-        const unsigned in = __ballot_sync(0xffffffffu, cu <= tok0 + warp + k * (kRopeThreads / 32));
-        if (lane == k) at += __popc(in);
-        all |= in == 0xffffffffu;
-      }
-      if (!all) break;
-    }
+    const int at = paged_owner<kRopePerWarp>(r.pb, tok0 + warp, kRopeThreads / 32, lane);
     if (lane < kRopePerWarp && tok < tok0 + nt) {
-      PagedSeq s{0, 0, 0};
+      PagedSeq s{0, 0, 0, false};
       if (at >= 0) s = paged_seq(r.pb, r.pl.status, at);
       const bool there = s.n > 0 && tok >= s.row0 && tok < s.row0 + s.n;
       int pos = 0;

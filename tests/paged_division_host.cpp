@@ -73,6 +73,7 @@ static int __reduce_add_sync(unsigned, int v) { const long long* all = warp::mee
 static int __reduce_max_sync(unsigned, int v) { const long long* all = warp::meet(v); return (int)*std::max_element(all, all + 32); }
 static int __reduce_min_sync(unsigned, int v) { const long long* all = warp::meet(v); return (int)*std::min_element(all, all + 32); }
 static void __syncthreads() { warp::meet(0); }
+static int __syncthreads_or(int p) { return __ballot_sync(0xffffffffu, p) != 0; }
 static int __popc(unsigned v) { return __builtin_popcount(v); }
 static int __ffs(int v) { return __builtin_ffs(v); }
 static int atomicExch(int* p, int v) { const int o = *p; *p = v; return o; }
@@ -101,6 +102,11 @@ void fill() {
   const long long all = spla::paged_fill_seqs(A, *seqs, warp::lane, 32);
   if (warp::lane == 0) { total = all; share = spla::paged_share(A.w, all); }
 }
+int owner_base, owner_step, owner_of[4];
+void owner() {
+  const int b = spla::paged_owner<4>(A.pb, owner_base, owner_step, warp::lane);
+  if (warp::lane < 4) owner_of[warp::lane] = b;
+}
 void walk() {
   spla::PagedWalk wk;
   const bool any = wk.seek(A, *seqs, cta * share, share);
@@ -118,7 +124,8 @@ void walk() {
 }  // namespace
 
 extern "C" {
-// plan: ppos, upos, log_tk, by_unit, n_cta, min_tiles, extra, Hkv, G, total_new, max_new, max_len, window, narrow (-1: as the launch would have it).
+// plan: ppos, upos, log_tk, by_unit, n_cta, min_tiles, extra, Hkv, G, total_new, max_new, max_len, window, narrow (-1: as the launch would have it), first
+// (sequences of earlier launches: cu, lens and prefix start with theirs).
 // out: total, share, status, narrow; pre[batch + 1], n[batch]
 void division_fill(const int* plan, int batch, const int* cu, const int* lens, const int* prefix, const int* first_key, long long* out, long long* pre, int* n) {
   static int status;
@@ -126,14 +133,21 @@ void division_fill(const int* plan, int batch, const int* cu, const int* lens, c
   A = spla::PagedAttend{};
   A.w.ppos = plan[0]; A.w.upos = plan[1]; A.w.log_tk = plan[2]; A.w.by_unit = plan[3]; A.w.n_cta = plan[4]; A.w.min_tiles = plan[5]; A.w.extra = plan[6];
   A.pl.Hkv = plan[7]; A.pl.G = plan[8]; A.pl.status = &status;
-  A.pb.cu = cu; A.pb.lens = lens; A.pb.batch = batch; A.pb.total_new = plan[9]; A.pb.max_new = plan[10]; A.pb.max_len = plan[11];
-  A.window = plan[12]; A.prefix = prefix; A.first_key = first_key;
+  A.pb.first = plan[14];
+  A.pb.cu = cu + plan[14]; A.pb.lens = lens + plan[14]; A.pb.batch = batch; A.pb.total_new = plan[9]; A.pb.max_new = plan[10]; A.pb.max_len = plan[11];
+  A.window = plan[12]; A.prefix = prefix ? prefix + plan[14] : nullptr; A.first_key = first_key;
   A.w.narrow = plan[13] < 0 ? spla::paged_narrow(A.w, A.pb, A.pl) : plan[13];
   if (!seqs) seqs.reset(new spla::PagedSeqs);
   warp::run(fill);
   out[0] = total; out[1] = share; out[2] = status; out[3] = A.w.narrow;
   for (int b = 0; b <= batch; ++b) pre[b] = seqs->pre[b];
   for (int b = 0; b < batch; ++b) n[b] = seqs->n[b];
+}
+// The sequences that the append looks up for the tokens base + k step, k < 4 (-1: none), in the batch of the last division_fill.
+void division_owner(int base, int step, int* out) {
+  owner_base = base; owner_step = step;
+  warp::run(owner);
+  std::copy(owner_of, owner_of + 4, out);
 }
 // Segments of one CTA: [count][b, h, u, t0, t1, head, tail, positions]; the cut at its start: rows, parts, first row, head.
 int division_walk(int which, int room, long long* segments, int* cut) {

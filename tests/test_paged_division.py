@@ -25,7 +25,7 @@ class Division:
     """A launch: its plan (as the host makes it for that many CTAs), its sequences, and what the device makes of them."""
 
     def __init__(self, lib, cu, lens, kernel="mma", G=4, hkv=2, few=False, ctas=148, window=0, prefix=None, first_key=None, total_new=None, max_new=None, max_len=None,
-                 narrow=-1, by_unit=0):
+                 narrow=-1, by_unit=0, first=0):
         self.lib, self.cu, self.lens, self.hkv, self.G = lib, cu, lens, hkv, G
         R = (32 if few else 128) if kernel == "mma" else (4 if few else 64)
         self.ppos = R // G
@@ -33,12 +33,12 @@ class Division:
         self.log_tk = 7 if kernel == "mma" else 6
         self.extra = (1 if few else 2) if kernel == "mma" else 0
         self.ctas, self.by_unit, self.window, self.prefix = ctas, by_unit, window, prefix
-        B = len(lens)
+        B = len(lens) - first
         total_new = cu[-1] if total_new is None else total_new
         max_new = max(b - a for a, b in zip(cu, cu[1:])) if max_new is None else max_new
         arr = lambda x: None if x is None else (C.c_int * len(x))(*x)  # noqa: E731
         plan = arr([self.ppos, self.upos, self.log_tk, by_unit, ctas, 1 if by_unit or (kernel != "mma" and not few) else 2, self.extra, hkv, G, total_new, max_new,
-                    max(lens) if max_len is None else max_len, window, narrow])
+                    max(lens) if max_len is None else max_len, window, narrow, first])
         out, pre, n = (C.c_longlong * 4)(), (C.c_longlong * (B + 1))(), (C.c_int * B)()
         self.keep = (arr(cu), arr(lens), arr(prefix), arr(first_key))              # (the walks read them)
         lib.division_fill(plan, B, *self.keep, out, pre, n)
@@ -136,3 +136,77 @@ def test_tiles_past_32_bits(lib, kernel, new, old, G, hkv):
     d.check_totals()
     for cta in (101, 295) if new > 1000000 else (0, 1, 101, 294, 295):
         d.check_walk(cta)
+
+
+def _sound(cu, lens, total, max_new, max_len):
+    """The sequences whose own numbers fit, and those that a call serves: no earlier prefix sum inside [0, total] is above their first row."""
+    own, served, top = [], [], -1
+    for b, L in enumerate(lens):
+        r0, r1 = cu[b], cu[b + 1]
+        own.append(0 <= r0 <= r1 <= total and r1 - r0 <= max_new and r1 - r0 <= L <= max_len)
+        served.append(own[-1] and r0 >= top)
+        if 0 <= r0 <= total:
+            top = max(top, r0)
+    return own, served
+
+
+def _spoilt(r, B, kind):
+    """Prefix sums with mistakes in them."""
+    new = [r.choice([0, 1, 2, r.randint(0, 9)]) for _ in range(B)]
+    cu = [0]
+    for n in new:
+        cu.append(cu[-1] + n)
+    total = cu[-1] + r.choice([0, 3])
+    if kind == "alternating":
+        cu = [0 if i % 2 == 0 else total for i in range(B + 1)]
+    elif kind == "one":
+        cu[r.randrange(B + 1)] = r.randint(0, total)
+    elif kind == "far":
+        cu[r.randrange(B + 1)] = r.choice([-5, total + 1, 1 << 30, -(1 << 31)])
+    elif kind == "several":
+        for _ in range(r.randint(1, B)):
+            cu[r.randrange(B + 1)] = r.choice([r.randint(0, total), r.randint(0, total), -1, total + 7])
+    elif kind == "shuffled":
+        r.shuffle(cu)
+    return cu, max(total, 1)
+
+
+@pytest.mark.parametrize("kind", ["sound", "one", "far", "several", "shuffled", "alternating"])
+@pytest.mark.parametrize("seed", range(8))
+def test_every_row_has_one_owner(lib, kind, seed):
+    """Prefix sums that do not ascend: the sequences that are served own rows of their own, and the append finds the same ones."""
+    r = random.Random(100 * seed + len(kind))
+    B = r.choice([1, 3, 8, 31, 32, 33, 64, 97])
+    cu, total = _spoilt(r, B, kind)
+    max_new, max_len = r.choice([4, 12, total]), 500
+    lens = [r.choice([0, 3, 20, 500, 500, 500, 501]) for _ in range(B)]
+    own, want = _sound(cu, lens, total, max_new, max_len)
+    launches = [(0, B)] if r.random() < 0.5 else [(0, B // 2), (B // 2, B)]
+    got = []
+    for first, end in launches:
+        if first == end:
+            continue
+        d = Division(lib, cu[:end + 1], lens[:end], hkv=2, G=4, few=True, total_new=total, max_new=max_new, max_len=max_len, first=first)
+        got += d.n
+        assert d.pre[-1] == d.total and d.total >= 0
+        assert (d.status != 0) == (not all(own[first:end]))
+    if not all(want):
+        assert not all(own)                                                   # (some sequence before reports it)
+    assert [n > 0 for n in got] == [w and cu[b + 1] > cu[b] for b, w in enumerate(want)]
+    rows = [None] * total
+    for b, w in enumerate(want):
+        if w:
+            for row in range(cu[b], cu[b + 1]):
+                assert rows[row] is None
+                rows[row] = b
+    d = Division(lib, cu, lens, few=True, total_new=total, max_new=max_new, max_len=max_len)
+    out = (C.c_int * 4)()
+    step = 8
+    for base in range(0, total, 4 * step):
+        for w in range(step):
+            lib.division_owner(C.c_int(base + w), C.c_int(step), out)
+            for k in range(4):
+                row, b = base + w + k * step, out[k]
+                if row < total:
+                    there = b >= 0 and own[b] and cu[b] <= row < cu[b + 1]
+                    assert (b if there else None) == rows[row]
