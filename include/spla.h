@@ -349,7 +349,7 @@ typedef struct {
   int32_t q_dtype;       /* spla_dtype_t of q and out */
   int64_t page_stride;   /* rows (of d elements) from a page of a head to the same head's in the next page; 0 -> H_kv * P */
   int64_t head_stride;   /* rows from a page of a head to the next head's; 0 -> P.  Rows of different (page, head) must not overlap */
-  float sm_scale;        /* multiplies q.k; 0 -> 1/sqrt(d) */
+  float sm_scale;        /* multiplies q.k, at most 2.3e38; 0 -> 1/sqrt(d) */
   uint32_t flags;        /* SPLA_GENERAL_KERNELS or 0 */
 } spla_paged_config_t;
 
@@ -419,8 +419,8 @@ int spla_paged_query_workspace(const spla_paged_t *paged, const spla_paged_batch
  *   out:  DEVICE [total_new][H_q][d] q_dtype.  lse: DEVICE fp32 [total_new][H_q] or NULL: ln of the sum of exp(s).
  *   workspace: DEVICE, 256-byte aligned, as spla_paged_query_workspace says; NULL where that is 0.  Calls that may overlap need
  *         one each.
- * bf16 caches and queries run on the tensor cores (probabilities rounded to bf16, sums in fp32); the others, and
- * SPLA_GENERAL_KERNELS, in fp32.  Results do not depend on max_new, max_len or the rows of other sequences beyond rounding.
+ * bf16 caches and queries run on the tensor cores (probabilities rounded to bf16, sums in fp32); the others, scales far
+ * above the cap (10^5 times and more), and SPLA_GENERAL_KERNELS, in fp32.  Results do not depend on max_new, max_len or the rows of other sequences beyond rounding.
  */
 int spla_paged_attend(spla_paged_t *paged, const spla_paged_batch_t *batch, const void *q, int64_t q_stride,
                       const spla_paged_mask_t *mask, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);

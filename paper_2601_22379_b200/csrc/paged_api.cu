@@ -101,7 +101,7 @@ extern "C" int spla_paged_create(const spla_paged_config_t* c, void* k_pages, vo
   if (!c || !k_pages || !v_pages || !status || !paged_out) return SPLA_ERR_INVALID_ARG;
   if (c->n_q_heads < 1 || c->n_kv_heads < 1 || c->n_q_heads % c->n_kv_heads || c->n_pages < 1) return SPLA_ERR_INVALID_ARG;
   if (!is_dtype(c->kv_dtype) || !is_dtype(c->q_dtype)) return SPLA_ERR_INVALID_ARG;
-  if (!(c->sm_scale >= 0.f) || !isfinite(c->sm_scale) || (c->flags & ~SPLA_GENERAL_KERNELS)) return SPLA_ERR_INVALID_ARG;
+  if (!(c->sm_scale >= 0.f) || !isfinite(c->sm_scale * kLog2e) || (c->flags & ~SPLA_GENERAL_KERNELS)) return SPLA_ERR_INVALID_ARG;
   if (c->page_stride < 0 || c->head_stride < 0) return SPLA_ERR_INVALID_ARG;
   if (!aligned(k_pages, 256) || !aligned(v_pages, 256) || !aligned(status, 4)) return SPLA_ERR_INVALID_ARG;
   const int G = c->n_q_heads / c->n_kv_heads, P = c->page_size;
@@ -219,6 +219,13 @@ static bool make_q_map(void* out128, const void* q, const PagedLayout& pl, int64
                           (unsigned long long)q_stride * 2, (unsigned)pl.G, (unsigned)paged_mma_positions(pb, pl));
 }
 
+// Whether the tensor-core kernel's polynomial for scores under a cap has finite coefficients (the largest is 0.0483 s log2 e (s / cap)^6); with a scale so far
+// above the cap (s = 3 and a cap of 10^-6, s = 4 10^5 and a cap of 1), the general kernel's tanh serves the call.
+static bool cap_fits(float sm_scale, float softcap) {
+  const double s = sm_scale, u = s / softcap;
+  return softcap == 0.f || 0.0697 * s * u * u * u * u * u * u < 1e38;
+}
+
 extern "C" int spla_paged_query_workspace(const spla_paged_t* p, const spla_paged_batch_t* batch, size_t* bytes_out) {
   const int rc = check_batch(p, batch, false);
   if (rc != SPLA_OK) return rc;
@@ -276,7 +283,7 @@ extern "C" int spla_paged_attend(spla_paged_t* p, const spla_paged_batch_t* batc
   cudaStream_t s = (cudaStream_t)stream;
   cudaError_t e = cudaSuccess;
   PagedMaps maps;
-  const bool tensor = p->tensor && aligned(q, 16) && q_stride % 8 == 0 && make_q_map(maps.q, q, p->pl, q_stride, pb);
+  const bool tensor = p->tensor && aligned(q, 16) && q_stride % 8 == 0 && cap_fits(p->cfg.sm_scale, mask->softcap) && make_q_map(maps.q, q, p->pl, q_stride, pb);
   if (tensor) {
     memcpy(maps.k, p->maps.k, sizeof(maps.k));
     memcpy(maps.v, p->maps.v, sizeof(maps.v));

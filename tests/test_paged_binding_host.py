@@ -44,3 +44,17 @@ def test_strides_of_tokens():
     assert rows(torch.zeros(5, 4, 64), 4) == 256
     assert rows(torch.zeros(5, 9, 64)[:, 2:6], 4) == 576                      # inside a packed projection
     assert rows(expanded(4, total=1), 4) == 256                               # one token has no neighbour
+
+
+def test_scales_that_overflow_are_refused():
+    """A scale whose product with log2 e is not finite: scores of 0 would be 0 x infinity."""
+    import ctypes as C
+
+    from paper_2601_22379_b200 import build
+    build.build()
+    lib = binding.load()
+    for scale, want in ((2.3e38, binding.SPLA_OK), (2.4e38, binding.SPLA_ERR_INVALID_ARG), (3.4e38, binding.SPLA_ERR_INVALID_ARG)):
+        h = C.c_void_p()
+        cfg = binding.SplaPagedConfig(8, 2, 128, 64, 10, 1, 1, 0, 0, scale, 0)
+        assert lib.spla_paged_create(C.byref(cfg), 4096, 8192, 256, C.byref(h)) == want
+        lib.spla_paged_destroy(h)
