@@ -289,7 +289,8 @@ int spla_destroy_cache(spla_cache_t *cache);
  * densely.  These calls give it both: spla_rope_apply rotates queries and keys, spla_paged_append stores new tokens in
  * pages (rotating them on the way), spla_paged_attend attends to all cached tokens that a mask leaves.
  * spla_paged_attend also reads the K/V of an SPLA cache as it lies: page_size = B, page_stride = B,
- * head_stride = max_blocks * B, and page numbers b * H_kv * max_blocks + block.
+ * head_stride = max_blocks * B, and page numbers b * H_kv * max_blocks + block.  (Not spla_paged_append: the SPLA cache's
+ * statistics, state and lengths would not know of its tokens.  New ones go there by spla_append_tokens.)
  * The general rules at the top of this file hold.
  * ------------------------------------------------------------------------------------------------------------------ */
 

@@ -471,6 +471,8 @@ class PagedCache:
     New tokens of all sequences come as one list of rows: cu_new int32 [batch + 1] says which rows are whose, seq_lens int32 [batch]
     how many tokens a sequence has with them, page_table int32 [batch, columns] where they lie."""
 
+    _of_spla = False
+
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, n_q_heads: int, q_dtype: str | None = None, sm_scale: float = 0.0, flags: int = 0):
         if not (k_pages.is_cuda and k_pages.dim() == 4 and k_pages.is_contiguous() and v_pages.is_contiguous() and k_pages.dtype in _TYPE_CODE
                 and v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype and v_pages.device == k_pages.device):
@@ -480,12 +482,14 @@ class PagedCache:
 
     @classmethod
     def of(cls, cache: SplaCache, sm_scale: float | None = None, flags: int = 0) -> "PagedCache":
-        """The K/V of an SPLA cache as pages (its blocks), for dense attention over it: `table()` names the pages."""
+        """The K/V of an SPLA cache as pages (its blocks), for dense attention over it: `table()` names the pages.  Read only: tokens are appended by
+        the SPLA cache, whose statistics, state and lengths go with them."""
         cfg, self = cache.cfg, cls.__new__(cls)
         hkv, B, mb = cfg.n_kv_heads, cfg.block_size, cache.max_blocks
         n_pages = (cfg.batch - 1) * hkv * mb + mb
         self._create(cache.bufs.k_cache, cache.bufs.v_cache, n_pages, hkv, B, cfg.head_dim, B, mb * B, cfg.n_q_heads,
                      "bf16" if cfg.q_dtype == SPLA_BF16 else "f32", cfg.sm_scale if sm_scale is None else sm_scale, flags)
+        self._of_spla = True
         self._table = (torch.arange(cfg.batch, dtype=torch.int32, device=self.device)[:, None] * (hkv * mb)
                        + torch.arange(mb, dtype=torch.int32, device=self.device))
         return self
@@ -534,6 +538,8 @@ class PagedCache:
         """Stores k, v [total, H_kv, d] at the last n_b positions of every sequence, keys rotated by `rope`; rotates q [total, H_q, d]
         beside them and returns it (None without q).  Tokens may be any stride apart that keeps them off each other (no expanded tensors);
         `q_out=q` works in place."""
+        if self._of_spla:
+            raise ValueError("paged cache: the pages of an SPLA cache are read only; append to the SPLA cache")
         total, hkv, kt = k.shape[0], self.n_kv_heads, self.k_pages.dtype
         ks = self._rows(k, total, hkv, kt, "k")
         vs = self._rows(v, total, hkv, kt, "v")

@@ -58,3 +58,22 @@ def test_scales_that_overflow_are_refused():
         cfg = binding.SplaPagedConfig(8, 2, 128, 64, 10, 1, 1, 0, 0, scale, 0)
         assert lib.spla_paged_create(C.byref(cfg), 4096, 8192, 256, C.byref(h)) == want
         lib.spla_paged_destroy(h)
+
+
+def test_pages_of_an_spla_cache_are_not_appended_to():
+    """Its statistics, state and lengths would not know of the tokens.  (`of` without a device: the cache's handle is not made.)"""
+    class Spla:
+        cfg = binding.make_config(batch=2, n_q_heads=4, n_kv_heads=2, head_dim=64, block_size=16, top_k=2, max_context=48)
+        max_blocks = 3
+
+        class bufs:
+            k_cache = v_cache = torch.zeros(2, 2, 3, 16, 64)
+
+    class Paged(binding.PagedCache):
+        def _create(self, k, v, *args):
+            self.__dict__.update(cache().__dict__, k_pages=k, v_pages=v)
+
+    c = Paged.of(Spla)
+    assert c.table().tolist() == [[0, 1, 2], [6, 7, 8]]
+    with pytest.raises(ValueError, match="SPLA cache"):
+        c.append(torch.zeros(5, 2, 64), torch.zeros(5, 2, 64), *sequences(5))
