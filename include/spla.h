@@ -412,8 +412,9 @@ int spla_paged_query_workspace(const spla_paged_t *paged, const spla_paged_batch
 
 /*
  * Softmax attention of the new tokens over the cache, which holds them already.  Keys outside a query's mask do not touch its
- * result, whatever they hold; a visible key or value that is not finite makes what it reaches not finite (infinite or NaN).  A query
- * that sees no key yields out = 0 and lse = -infinity.
+ * result, whatever they hold.  Of visible ones: a score of NaN or +infinity (before the distance) makes the query's out and lse NaN; a
+ * score of -infinity is weight 0; with softcap an infinite score is the cap, of its sign.  A value that is not finite makes its channel of out not
+ * finite (infinite or NaN).  A query that sees no key, or only keys of weight 0, yields out = 0 and lse = -infinity.
  *   q:    DEVICE [total_new][H_q][d] q_dtype, rows q_stride elements apart (0 -> H_q * d), aligned to the element (to 16 bytes for
  *         the tensor-core kernel).
  *   mask: HOST or NULL (causal only).
