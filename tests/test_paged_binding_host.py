@@ -77,3 +77,20 @@ def test_pages_of_an_spla_cache_are_not_appended_to():
     assert c.table().tolist() == [[0, 1, 2], [6, 7, 8]]
     with pytest.raises(ValueError, match="SPLA cache"):
         c.append(torch.zeros(5, 2, 64), torch.zeros(5, 2, 64), *sequences(5))
+
+
+def test_imports_without_torchs_cuda_internals():
+    """Host-only use (configurations, argument checks) of a torch that was built without CUDA."""
+    import os
+    import subprocess
+    import sys
+    code = ("import torch\n"
+            "for name in ('_cuda_getDevice', '_cuda_getCurrentRawStream'):\n"
+            "    if hasattr(torch._C, name): delattr(torch._C, name)\n"
+            "from paper_2601_22379_b200 import binding\n"
+            "binding.make_config(batch=1, n_q_heads=2, n_kv_heads=1, head_dim=64, block_size=16, top_k=1, max_context=16)\n"
+            "assert callable(binding._device_now) and callable(binding._stream_now)\n"
+            "print('imported')\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True)
+    assert done.stdout.strip() == "imported", done.stderr[-500:]
