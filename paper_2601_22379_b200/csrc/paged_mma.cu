@@ -63,9 +63,13 @@ struct PmSmem {
   static constexpr int kBytes = kMisc + 48;
   static_assert(4 * 32 * 144 <= 8 * 32 * 80 && 4 * 16 * 272 <= 8 * 32 * 80 && 4 * 8 * 528 <= 8 * 32 * 80, "rows on their way out");
   static_assert(kBytes <= 227 * 1024, "shared memory of the paged attention kernel");
+  static_assert(kPmKeys >= 128, "positions of a row tile (see PmPlan)");
 };
 
 // What the roles agree on for one segment: which key tiles either row tile walks, and which of them every row sees whole.
+// No tile between A and E is walked by neither: row tile 1 has at most 128 positions, as many as a tile has keys, right behind those of row
+// tile 0, so that the first key that one of its rows sees lies at most 127 behind the last that row tile 0 sees: a1 <= e0 (and e1 >= e0 > a0),
+// whatever the documents, the window and the prefix.
 struct PmPlan {
   bool single;                                     // one row tile, key tiles in turn
   int a0, e0, a1, e1;                              // key tiles of row tile 0, of row tile 1
@@ -408,11 +412,6 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           if (ok && act1) {
             score(s1, pl, t, true);
             if (ok && pend0) product(s0);
-          }
-          if (ok && !act0 && !act1) {                             // (between the two row tiles' documents)
-            if (!pm_wait(&v_full[kt % NV], (kt / NV) & 1, lim, abort_flag)) ok = false;
-            umma_commit_one(one, &k_empty[kt % NK]);
-            umma_commit_one(one, &v_empty[kt % NV]);
           }
           if (!ok) return false;
           ++kt;
