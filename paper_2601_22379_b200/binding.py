@@ -516,7 +516,7 @@ class PagedCache:
         """The packed spla_paged_batch_t."""
         shape, ts, n, dev, i32 = page_table.shape, page_table.stride(), seq_lens.shape[0], self.device, torch.int32
         if not (cu_new.dtype is i32 and seq_lens.dtype is i32 and page_table.dtype is i32 and cu_new.device == dev and seq_lens.device == dev
-                and page_table.device == dev and cu_new.is_contiguous() and seq_lens.is_contiguous() and len(shape) == 2 and ts[1] == 1
+                and page_table.device == dev and cu_new.is_contiguous() and seq_lens.is_contiguous() and len(shape) == 2 and (ts[1] == 1 or shape[1] == 1)
                 and cu_new.shape[0] == n + 1 and shape[0] == n):
             raise ValueError("paged cache: int32 cu_new [batch + 1], seq_lens [batch], page_table [batch, columns] on the cache's device")
         # (the table's columns bound max_len; its rows may be further apart)
@@ -527,7 +527,7 @@ class PagedCache:
     def _rows(self, x, total, heads, dtype, what):
         """Elements between the tokens of x [total, heads, d]."""
         d, xs = self.head_dim, x.stride()
-        if not (x.shape == (total, heads, d) and x.dtype is dtype and x.device == self.device and xs[2] == 1 and xs[1] == d):
+        if not (x.shape == (total, heads, d) and x.dtype is dtype and x.device == self.device and xs[2] == 1 and (xs[1] == d or heads == 1)):
             raise ValueError(f"paged cache: {what} [tokens, {heads}, {d}] of its type, heads contiguous")
         if total <= 1:
             return heads * d

@@ -94,3 +94,15 @@ def test_imports_without_torchs_cuda_internals():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True)
     assert done.stdout.strip() == "imported", done.stderr[-500:]
+
+
+def test_strides_of_axes_of_one():
+    """The stride of an axis of length one says nothing: one head, one page."""
+    c = cache(hq=1, hkv=1)
+    k = torch.zeros(1, 5, 64).transpose(0, 1)                                 # head-major, one head
+    assert k.stride(1) == 5 * 64 and c._rows(k, 5, 1, torch.float32, "k") == 64
+    table = torch.zeros(1, 2, dtype=torch.int32).T
+    cu, lens = torch.zeros(3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    assert table.shape == (2, 1) and table.stride(1) == 2
+    packed = binding.SplaPagedBatch.from_buffer_copy(c._batch(5, cu, lens, table, 5, 16))
+    assert packed.table_stride == 1 and packed.batch == 2
