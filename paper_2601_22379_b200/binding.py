@@ -432,6 +432,8 @@ class Rope:
             ys = out.stride()
             if not (out.shape == xshape and out.dtype is dtype and out.device == device and ys[-1] == 1):
                 raise ValueError("rope: an output like its input, channels contiguous")
+            if 0 in ys and any(y == 0 and n > 1 for y, n in zip(ys, xshape)):
+                raise ValueError("rope: an output whose elements lie on each other")
         if len(xs) == 3:
             return out, _pack_rope_tensor(x.data_ptr(), out.data_ptr(), xshape[1], 0, xs[0], xs[1], 0, ys[0], ys[1])
         return out, _pack_rope_tensor(x.data_ptr(), out.data_ptr(), xshape[2], xs[0], xs[1], xs[2], ys[0], ys[1], ys[2])
