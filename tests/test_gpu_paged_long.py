@@ -1,5 +1,6 @@
 """Attention over a long paged cache: what the tensor cores add up stays as exact as the documentation says, however many keys there are."""
 import math
+import random
 
 import pytest
 import torch
@@ -111,3 +112,71 @@ def test_bounds_whose_tiles_pass_32_bits(kv, few):
     # (both within half a step of the type and the probabilities' rounding of the same numbers: values' mean magnitude below 1)
     lim = 2.0 ** -8 * (tight.float().abs() + 2) * 2 if kv == "bf16" else torch.full_like(tight, 1e-5)
     assert bool(((out.float() - tight.float()).abs() <= lim).all()) and float((lse - tight_lse).abs().max()) < 1e-5
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_drawn_with_the_bounds_of_a_long_cache(seed):
+    """Anything the documentation allows, with bounds that let a sequence be 20000 to 200000 tokens long, as a program plans that serves any length."""
+    r = random.Random(400 + seed)
+    B, hkv, G, d, P = r.choice([1, 2, 5, 40]), r.choice([1, 2, 3]), r.choice([1, 2, 4, 5, 8, 16]), r.choice([64, 128]), r.choice([16, 64, 128])
+    few = r.random() < 0.5
+    new = [r.choice([0, 1, r.randint(1, 2 if few else 200)]) for _ in range(B)]
+    new[0] = new[0] or 1
+    old = [r.choice([0, r.randint(0, 700), r.randint(0, 3000), 17000 if B < 5 else 100]) for _ in range(B)]
+    top = r.choice([20000, 200000])
+    b = Batch(new, old, hq=G * hkv, hkv=hkv, d=d, P=P, seed=seed, extra_cols=top // P)
+    kw = {}
+    if r.random() < 0.3:
+        kw["softcap"] = r.choice([5.0, 30.0])
+    if r.random() < 0.3:
+        kw["window"] = r.choice([1, 200, 16500])
+    if r.random() < 0.3:
+        kw["slopes"] = torch.tensor([r.choice([0.0, 0.01, 0.3]) for _ in range(G * hkv)])
+    if r.random() < 0.3:
+        kw["first_key"] = torch.tensor([max(-1, r.choice([0, p, p - r.randint(0, 200), p + 1])) for n, o in zip(new, old) for p in range(o, o + n)], dtype=torch.int32)
+    if r.random() < 0.3:
+        kw["prefix_lens"] = torch.tensor([r.choice([0, 100, 18000]) for _ in range(B)], dtype=torch.int32)
+    bounds = dict(max_len=max(top, b.max_len))
+    out, lse = b.attend(**kw, **bounds)
+    assert b.cache.sync_status() == 0
+    b.check(out, lse, **kw)
+    again, lse2 = b.attend(**kw, **bounds)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("new,old", [([1, 2], [500, 900]), ([150, 40], [500, 900]), ([150] * 40, [20000] * 40)], ids=["few", "chunks", "drained"])
+def test_waits_that_run_out_in_a_long_cache(new, old):
+    """As for short ones: the kernel gives up, reports it, and works again afterwards."""
+    b = Batch(new, old, hq=8, hkv=2, d=128, kv="bf16", extra_cols=40000 // 64)
+    want, want_lse = b.attend(max_len=40000)
+    assert b.cache.sync_status() == 0
+    b.check(want, want_lse, seqs=[0, 1])
+    b.cache.debug_wait_hook(1 << 14, 16)
+    b.attend(max_len=40000)
+    assert b.cache.sync_status() == binding.SPLA_ERR_TIMEOUT
+    b.cache.debug_wait_hook(0, 0)
+    out, lse = b.attend(max_len=40000)
+    assert b.cache.sync_status() == 0 and torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+def test_graphs_of_a_long_cache():
+    """Two captured calls whose walks are drained, replayed at once, beside an eager one: each has sums of its own."""
+    b = Batch([130] * 20, [34000] * 20, hq=8, hkv=1, d=64, P=128)
+    want, want_lse = b.attend()
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            res = b.attend()
+        graphs.append((g, res))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            graphs[0][0].replay()
+        graphs[1][0].replay()
+        out, lse = b.attend()
+    torch.cuda.synchronize()
+    assert b.cache.sync_status() == 0 and torch.equal(out, want) and torch.equal(lse, want_lse)
+    for _, (go, gl) in graphs:
+        assert torch.equal(go, want) and torch.equal(gl, want_lse)
