@@ -8,10 +8,10 @@
 // product with V (four rows x CW channels per thread, the tile's tokens shared by TS threads).  K of the next tile is on its way from
 // when the scores are done, V from when the product is done (asynchronous copies where the cache is fp32), the page table one tile ahead of that.
 // R = 4, 16 and 64 by the rows that a unit has at most; a row tile's products cost the same however few of its rows are real.
-// 4 rows are bound by reading K and V (8 sequences of 32000, 8 heads of 128: 2.1 GB in 474 us, 4.4 TB/s), 16 by shared memory's reads for
-// the scores (G = 8, the same cache: 755 us), 64 by the FMA pipe, in use half of the time: the phases of a tile alternate with barriers
-// (300 tokens on 3000 x 4, 32 heads of 128: 1.72 ms, 36 TFLOP/s; with tiles of 32 keys and P beside K 1.88; row tiles of 128 in
-// one CTA of 512 threads, or with eight rows per thread: within 7 % of that).
+// 4 rows are bound by reading K and V (8 sequences of 32000, 8 heads of 128: 2.1 GB in 493 us, 4.3 TB/s; bf16 caches, which are not copied
+// asynchronously, 1.05 GB in 1.20 ms), 16 by shared memory's reads for the scores (G = 8, the same cache: 523 us), 64 by the FMA pipe, in use half
+// of the time: the phases of a tile alternate with barriers (300 tokens on 3000 x 4, 32 heads of 128: 1.54 ms, 36 TFLOP/s; tiles of 32
+// keys with P beside K are 9 % slower, row tiles of 128 in one CTA of 512 threads, or with eight rows per thread, within 7 %).
 #include "paged.h"
 
 namespace spla {

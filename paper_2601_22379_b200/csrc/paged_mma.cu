@@ -9,21 +9,23 @@
 //   - a unit of one row tile (short chunks): the same rows against key tiles in turn, the two halves merged at the end.
 // Launches whose units have at most 32 rows (single tokens, FEW) hold the rows four times, a copy for each softmax warp, which takes 32
 // of the tile's 128 keys: its row of P has zeros elsewhere, its rows of O and l are sums over its keys, and the four are merged at the
-// end.  (One warp with all 128 keys of the rows was the whole chain: capped scores of 64 ragged sequences 978 us, 618 so.)
-// P takes the place of S in tensor memory, as the left operand of O += P V, rounded to bf16, half a step of 2^-8, as the outputs are;
-// its sum l is of the unrounded values, so that lse is as exact as the scores.  The maximum is a stale one: O is rescaled only when it
+// end.  (One warp with all 128 keys of the rows was the whole chain: capped scores of 64 ragged sequences 978 us, 618 so on the same box.)
+// P takes the place of S in tensor memory, as the left operand of O += P V, rounded to bf16, half a step of 2^-8, as the outputs are
+// (error of out against float64, 2-norm: 2.3e-3 for single tokens, 2.1e-3 for prompts, of which the rounding of out is 1.7e-3; a second part of P
+// would take 24 products in place of 16, and their issue is what bounds prompts).  Its sum l is of the unrounded values, so that lse is as
+// exact as the scores.  The maximum is a stale one: O is rescaled only when it
 // grows by more than 2^8.  The tensor core truncates when it adds into an accumulator: every kPmDrain tiles the softmax warps take O into fp32
 // sums of their own in the workspace (sums of a million keys came out 0.4 % low without, of four million 2.3 %).
 //
 // Warps: 0 and 2 TMA (pages of K and the query rows as boxes of G heads x positions; pages of V), 1 the MMA issuer, 3 plans the
 // segments ahead of the others, 4 to 7 and 8 to 11 softmax and epilogue of either row tile, one row per thread.
 //
-// What bounds it.  Single tokens: reading K and V (8 sequences of 32768, 8 KV heads: 6.2 TB/s, 0.95 of a copy's rate).  Prompts:
-// products issue at about 82 cycles each (64 would be the tensor pipe's own time: S reads both operands from shared memory, at its
-// full rate), 16 per row tile and key tile, and each row tile's chain of scores, softmax (about 1900 cycles), P and product is not quite
-// hidden behind the other's: 8192 tokens, 32 heads of 128: 0.53 ms, 1.03 PFLOP/s.  Slower, on the same box: scores in halves of 64 keys with
-// two buffers (623 us: twice the instructions at the same 82 cycles); P handed over in halves (561); a quarter of the exponentials by
-// polynomial on the FMA pipe (565); loading S twice instead of holding a row in registers.
+// What bounds it.  Single tokens: reading K and V (8 sequences of 32768, 8 KV heads: 5.7 to 6.0 TB/s by box, 0.87 to 0.92 of a copy's
+// rate).  Prompts: products issue at about 82 cycles each (64 would be the tensor pipe's own time: S reads both operands from shared
+// memory, at its full rate), 16 per row tile and key tile, and each row tile's chain of scores, softmax (about 1900 cycles), P and product is
+// not quite hidden behind the other's: 8192 tokens, 32 heads of 128: 0.59 to 0.62 ms by box, 0.89 to 0.93 PFLOP/s.  Slower, on a box where
+// this took 533 us: scores in halves of 64 keys with two buffers (623 us: twice the instructions at the same 82 cycles); P handed over in
+// halves (561); a quarter of the exponentials by polynomial on the FMA pipe (565); loading S twice instead of holding a row in registers.
 //
 // Keys outside a row's mask: their scores are replaced before the maximum, whatever they are.  Values are looked over in tiles that
 // some row sees only in part: behind the sequence's end they are zeroed, and where one that is not finite is inside, the tile's product

@@ -4,9 +4,10 @@
 // every thread keeps one piece of a head (VEC pairs: 16 bytes of either half, or 32 bytes of neighbouring pairs) and walks the
 // (token, head) rows of the block, queries, keys and values as one list.  The angle is exact: the frequency is a 64-bit fraction of a
 // turn, position x frequency wraps at whole turns in integer arithmetic, and only the remainder (its top 32 bits) becomes a float.
-// Bound by memory: every channel is read and written once, 6 flops per pair (32768 tokens of 32 + 8 heads of 128, half rotated: 110 us,
-// 6.1 TB/s, 0.93 of a copy's rate; small calls by a launch: 8 tokens 2.3 us).  The first rows' loads are issued before the tokens' places and
-// the sines are known (175 -> 115 us with bases once per token, no 64-bit divisions; 115 -> 110 with the loads first).
+// Bound by memory: every channel is read and written once, 6 flops per pair (32768 tokens of 32 + 8 heads of 128: 111 us in a graph,
+// 6.0 TB/s, 0.92 of a copy's rate, one channel at a time, VEC = 1, 369; small calls by a launch: 8 tokens 2.2 us).  The first rows' loads are
+// issued before the tokens' places and the sines are known (175 -> 115 us with bases once per token, no 64-bit divisions; 115 -> 110 with
+// the loads first).
 #include "paged.h"
 
 namespace spla {
