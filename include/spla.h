@@ -340,6 +340,32 @@ typedef struct {
 int spla_rope_apply(const spla_rope_t *rope, const int32_t *positions, int32_t batch, int32_t n_tokens,
                     const spla_rope_tensor_t *q, const spla_rope_tensor_t *k, int32_t dtype, int32_t transpose, void *stream);
 
+/*
+ * Norms of queries and keys, head by head, and their rotation in the same pass: y = R n, n_c = x_c r w_c, r = 1 / sqrt(mean_c x_c^2 + eps) over the
+ * head's channels (all of them, whatever part is rotated), R the rotation of spla_rope_apply; fp32, rounded once.
+ */
+typedef struct {
+  const float *q_weight, *k_weight;  /* DEVICE fp32 [head_dim]: w of queries and of keys, shared by their heads */
+  float eps;                         /* >= 0 */
+} spla_head_norm_t;
+
+/* As spla_rope_apply, without `transpose`.  Both weights are given (k_weight with k only). */
+int spla_rope_norm_apply(const spla_rope_t *rope, const int32_t *positions, int32_t batch, int32_t n_tokens, const spla_rope_tensor_t *q,
+                         const spla_rope_tensor_t *k, int32_t dtype, const spla_head_norm_t *norm, void *stream);
+
+/*
+ * The gradients of spla_rope_norm_apply, u = R^T dy: dx_c = r (w_c u_c - x_c r^2 mean_c(w_c u_c x_c)), dw_c = sum of u_c x_c r over tokens and heads (fp32,
+ * always added in the same order).
+ *   q_grad, k_grad: HOST descriptors; in: dy, out: dx (in the place of dy or x with equal strides, else overlapping neither).
+ *   q, k:           HOST descriptors of x, as spla_rope_norm_apply took it; `out` is not used.  k and k_grad may both be NULL.
+ *   dq_weight, dk_weight: DEVICE fp32 [head_dim], written.
+ *   workspace:      DEVICE scratch, 16-byte aligned, as spla_rope_norm_query_workspace says for the heads of q and k together.
+ */
+int spla_rope_norm_backward(const spla_rope_t *rope, const int32_t *positions, int32_t batch, int32_t n_tokens, const spla_rope_tensor_t *q_grad,
+                            const spla_rope_tensor_t *q, const spla_rope_tensor_t *k_grad, const spla_rope_tensor_t *k, int32_t dtype,
+                            const spla_head_norm_t *norm, float *dq_weight, float *dk_weight, void *workspace, size_t workspace_bytes, void *stream);
+int spla_rope_norm_query_workspace(const spla_rope_t *rope, int32_t batch, int32_t n_tokens, int32_t n_heads, size_t *bytes_out);
+
 typedef struct {
   int32_t n_q_heads;     /* H_q <= 4096 */
   int32_t n_kv_heads;    /* H_kv; G = H_q / H_kv must be an integer in [1, 16] */
@@ -363,6 +389,20 @@ typedef struct spla_paged spla_paged_t; /* opaque host-side descriptor */
  */
 int spla_paged_create(const spla_paged_config_t *config, void *k_pages, void *v_pages, int32_t *status, spla_paged_t **paged_out);
 int spla_paged_destroy(spla_paged_t *paged);   /* NULL is allowed */
+
+/*
+ * The same with pages of 8 bits: e4m3 values (4 exponent, 3 mantissa bits, to 448), and for every 16 tokens of a KV head a scale, a power of two.
+ * A value stands for e4m3 x 2^(byte - 127).  Half the memory of a bf16 cache; everything that takes a spla_paged_t takes one of these.
+ *   k_pages, v_pages:   as above, a byte per element.
+ *   k_scales, v_scales: DEVICE, a byte for each 16 rows: [n_pages][H_kv][P / 16].  Exponents (byte - 127) are between -40 and 40; others are read as the nearest.
+ *   config: kv_dtype is the type of k_new and v_new and has to be q_dtype; page_stride and head_stride 0 (or what that stands for).
+ * Appending: the scale of a block of 16 tokens is the least 2^e, e in [-40, 40], with every magnitude of the block at most 448 2^e; values are
+ * rounded to the nearest e4m3 (beyond 448 2^40: 448 2^40; NaN and infinities: NaN, without part in the scale).  A block whose first token is among the
+ * new ones starts anew, whatever its bytes were; one that was begun before keeps its scale where that is large enough, or else
+ * its tokens before the new ones are rounded again to the larger one (exact, but for values that come below 2^-6 of it).
+ */
+int spla_paged_create_scaled(const spla_paged_config_t *config, void *k_pages, void *v_pages, uint8_t *k_scales, uint8_t *v_scales, int32_t *status,
+                           spla_paged_t **paged_out);
 
 /*
  * The new tokens of a call: rows cu_new[b] .. cu_new[b + 1] - 1 belong to sequence b and are its last n_b tokens, at positions
@@ -396,6 +436,18 @@ int spla_paged_append(spla_paged_t *paged, const spla_paged_batch_t *batch, cons
                       const void *k_new, int64_t k_stride, const void *v_new, int64_t v_stride, const void *q, int64_t q_stride,
                       void *q_out, int64_t q_out_stride, void *stream);
 
+/* The same with the keys and queries normed before they are rotated (spla_head_norm_t; NULL, or a NULL weight: those are not). */
+int spla_paged_append_norm(spla_paged_t *paged, const spla_paged_batch_t *batch, const spla_rope_t *rope, const int32_t *positions,
+                           const spla_head_norm_t *norm, const void *k_new, int64_t k_stride, const void *v_new, int64_t v_stride, const void *q,
+                           int64_t q_stride, void *q_out, int64_t q_out_stride, void *stream);
+
+/*
+ * Reads cached tokens back: row cu_new[b] + i of k_out, v_out (DEVICE [total_new][H_kv][d] out_dtype, 16-byte aligned) is token seq_lens[b] - n_b + i of
+ * sequence b, as spla_paged_append stored it.  8-bit values times their scale are exact in either type; an fp32 cache is rounded to bf16.  Rows of no
+ * sequence, and of one whose numbers are not consistent, are not touched; those of a bad page number are zeros.
+ */
+int spla_paged_read(spla_paged_t *paged, const spla_paged_batch_t *batch, void *k_out, void *v_out, int32_t out_dtype, void *stream);
+
 /* What a query's scores go through.  Query at position p, key at position j:
  *   s = sm_scale q.k;  softcap > 0: s = softcap tanh(s / softcap);  slopes: s -= slopes[head] |p - j|.
  * Visible are the j with max(0, p - window + 1, first_key) <= j < min(seq_len, max(p + 1, prefix_len)). */
@@ -426,6 +478,13 @@ int spla_paged_query_workspace(const spla_paged_t *paged, const spla_paged_batch
  */
 int spla_paged_attend(spla_paged_t *paged, const spla_paged_batch_t *batch, const void *q, int64_t q_stride,
                       const spla_paged_mask_t *mask, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The same with sinks: besides the window's keys the sequence's first `sinks` tokens stay visible, j < sinks (and j < min(seq_len, max(p + 1, prefix_len))).
+ * sinks >= 0; without a window they change nothing.  Not together with first_key (SPLA_ERR_UNSUPPORTED).
+ */
+int spla_paged_attend_sinks(spla_paged_t *paged, const spla_paged_batch_t *batch, const void *q, int64_t q_stride, const spla_paged_mask_t *mask,
+                            int32_t sinks, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
 
 /* As spla_sync_status, for the status word of `paged`. */
 int spla_paged_sync_status(spla_paged_t *paged, void *stream);

@@ -24,9 +24,10 @@ EXPORTS = ["spla_query_sizes", "spla_init_cache", "spla_append_tokens", "spla_de
            "spla_select_blocks_noalloc", "spla_select", "spla_append_decode", "spla_prefill",
            "spla_query_prefill_workspace",
            "spla_copy_scores", "spla_sync_status", "spla_set_length_bound", "spla_debug_wait_hook", "spla_destroy_cache",
-           "spla_rope_create", "spla_rope_destroy", "spla_rope_apply", "spla_paged_create", "spla_paged_destroy",
-           "spla_paged_append", "spla_paged_query_workspace", "spla_paged_attend", "spla_paged_sync_status",
-           "spla_paged_debug_wait_hook",
+           "spla_rope_create", "spla_rope_destroy", "spla_rope_apply", "spla_rope_norm_apply", "spla_rope_norm_backward",
+           "spla_rope_norm_query_workspace", "spla_paged_create", "spla_paged_create_scaled", "spla_paged_destroy",
+           "spla_paged_append", "spla_paged_append_norm", "spla_paged_read", "spla_paged_query_workspace", "spla_paged_attend",
+           "spla_paged_attend_sinks", "spla_paged_sync_status", "spla_paged_debug_wait_hook",
            "spla_launch_count", "spla_status_string", "spla_last_cuda_error"]
 
 
@@ -64,6 +65,10 @@ class SplaRopeTensor(C.Structure):
     _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("n_heads", C.c_int32),
                 ("in_batch", C.c_int64), ("in_token", C.c_int64), ("in_head", C.c_int64),
                 ("out_batch", C.c_int64), ("out_token", C.c_int64), ("out_head", C.c_int64)]
+
+
+class SplaHeadNorm(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float)]
 
 
 class SplaPagedConfig(C.Structure):
@@ -116,6 +121,13 @@ def load(path: str | None = None) -> C.CDLL:
     lib.spla_rope_destroy.argtypes = [vp]
     lib.spla_rope_apply.argtypes = [vp, vp, i32, i32, vp, vp, i32, i32, vp]
     lib.spla_paged_create.argtypes = [C.POINTER(SplaPagedConfig), vp, vp, vp, C.POINTER(vp)]
+    lib.spla_rope_norm_apply.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp, vp]
+    lib.spla_rope_norm_backward.argtypes = [vp, vp, i32, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.spla_rope_norm_query_workspace.argtypes = [vp, i32, i32, i32, C.POINTER(C.c_size_t)]
+    lib.spla_paged_create_scaled.argtypes = [C.POINTER(SplaPagedConfig), vp, vp, vp, vp, vp, C.POINTER(vp)]
+    lib.spla_paged_append_norm.argtypes = [vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.spla_paged_read.argtypes = [vp, vp, vp, vp, i32, vp]
+    lib.spla_paged_attend_sinks.argtypes = [vp, vp, vp, i64, vp, i32, vp, vp, vp, C.c_size_t, vp]
     lib.spla_paged_destroy.argtypes = [vp]
     lib.spla_paged_append.argtypes = [vp, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp]
     lib.spla_paged_query_workspace.argtypes = [vp, vp, C.POINTER(C.c_size_t)]
@@ -379,11 +391,12 @@ _TYPE_CODE = {torch.bfloat16: SPLA_BF16, torch.float32: SPLA_F32}
 _pack_rope_tensor = struct.Struct("@PPi6q").pack
 _pack_batch = struct.Struct("@PPP5i4x").pack
 _pack_mask = struct.Struct("@fiPPP").pack
+_pack_norm = struct.Struct("@PPf4x").pack
 # (torch's own short ways to the current device and stream, 0.1 us each, where there are any: a torch without CUDA has none)
 _device_now = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _stream_now = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 assert struct.calcsize("@PPi6q") == C.sizeof(SplaRopeTensor) and struct.calcsize("@PPP5i4x") == C.sizeof(SplaPagedBatch)
-assert struct.calcsize("@fiPPP") == C.sizeof(SplaPagedMask)
+assert struct.calcsize("@fiPPP") == C.sizeof(SplaPagedMask) and struct.calcsize("@PPf4x") == C.sizeof(SplaHeadNorm)
 
 
 def _on(index: int, fn, *args) -> int:
@@ -396,6 +409,13 @@ def _on(index: int, fn, *args) -> int:
         return fn(*args, _stream_now(index))
     finally:
         torch.cuda.set_device(before)
+
+
+def _norm_weight(w: torch.Tensor, head_dim: int, device) -> int:
+    """Address of a norm's weight."""
+    if not (w.dtype is torch.float32 and w.shape == (head_dim,) and w.device == device and w.is_contiguous()):
+        raise ValueError("head norm: a weight fp32 [head_dim] on the device of what it weighs, contiguous")
+    return w.data_ptr()
 
 
 class Rope:
@@ -457,6 +477,78 @@ class Rope:
                 raise SplaError(rc, "spla_rope_apply")
         return q_out if k is None else (q_out, k_out)
 
+    def _places(self, positions, q):
+        shape, dtype, device = positions.shape, q.dtype, positions.device
+        if not (positions.dtype is torch.int32 and positions.is_contiguous() and 1 <= len(shape) <= 2 and dtype in _TYPE_CODE):
+            raise ValueError("rope: positions int32 [batch, tokens] or [tokens], contiguous; q bf16 or fp32")
+        return shape, dtype, device, shape[0] if len(shape) == 2 else 1, shape[-1]
+
+    def norm_apply(self, positions: torch.Tensor, q: torch.Tensor, q_weight: torch.Tensor, k: torch.Tensor | None = None,
+                   k_weight: torch.Tensor | None = None, eps: float = 1e-6, q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None):
+        """Norms every head of q (and k) over its channels, times the weight (fp32 [head_dim]), and rotates it to `positions`, in one pass:
+        `apply(x / sqrt(mean(x^2) + eps) * weight)`.  Tensors as for `apply`.  Returns q_out, or (q_out, k_out)."""
+        shape, dtype, device, batch, n = self._places(positions, q)
+        if (k is None) != (k_weight is None):
+            raise ValueError("head norm: k and k_weight go together")
+        q_out, tq = self._tensor(q, q_out, shape, dtype, device)
+        tk = None
+        if k is not None:
+            k_out, tk = self._tensor(k, k_out, shape, dtype, device)
+        norm = _pack_norm(_norm_weight(q_weight, self.head_dim, device), 0 if k is None else _norm_weight(k_weight, self.head_dim, device), eps)
+        if n and batch:
+            rc = _on(device.index, self.lib.spla_rope_norm_apply, self.handle, positions.data_ptr(), batch, n, tq, tk, _TYPE_CODE[dtype], norm)
+            if rc != SPLA_OK:
+                raise SplaError(rc, "spla_rope_norm_apply")
+        return q_out if k is None else (q_out, k_out)
+
+    def norm_backward(self, positions: torch.Tensor, dq_out: torch.Tensor, q: torch.Tensor, q_weight: torch.Tensor, dk_out: torch.Tensor | None = None,
+                      k: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float = 1e-6, dq: torch.Tensor | None = None,
+                      dk: torch.Tensor | None = None):
+        """The gradients of `norm_apply(positions, q, q_weight, k, k_weight, eps)` for dq_out, dk_out of its outputs: (dq, dq_weight), or
+        (dq, dq_weight, dk, dk_weight); those of the weights in fp32.  `dq=dq_out` works in place."""
+        shape, dtype, device, batch, n = self._places(positions, q)
+        if not (k is None) == (k_weight is None) == (dk_out is None):
+            raise ValueError("head norm: k, k_weight and dk_out go together")
+        _, xq = self._input(q, shape, dtype, device)
+        if dq_out.shape != q.shape or (k is not None and dk_out.shape != k.shape):
+            raise ValueError("head norm: gradients like their tensors")
+        dq, tq = self._tensor(dq_out, dq, shape, dtype, device)
+        xk = tk = dk_weight = None
+        heads, wk = q.shape[-2], 0
+        if k is not None:
+            _, xk = self._input(k, shape, dtype, device)
+            dk, tk = self._tensor(dk_out, dk, shape, dtype, device)
+            heads += k.shape[-2]
+            wk = _norm_weight(k_weight, self.head_dim, device)
+        norm = _pack_norm(_norm_weight(q_weight, self.head_dim, device), wk, eps)
+        if n and batch:
+            nbytes = C.c_size_t()
+            rc = _on(device.index, lambda *a: self.lib.spla_rope_norm_query_workspace(*a[:-1]), self.handle, batch, n, heads, C.byref(nbytes))
+            if rc != SPLA_OK:
+                raise SplaError(rc, "spla_rope_norm_query_workspace")
+            # the weights' gradients and the call's own scratch, from the stream's pool
+            dq_weight = torch.empty(self.head_dim, dtype=torch.float32, device=device)
+            if k is not None:
+                dk_weight = torch.empty(self.head_dim, dtype=torch.float32, device=device)
+            ws = torch.empty(nbytes.value, dtype=torch.uint8, device=device)
+            rc = _on(device.index, self.lib.spla_rope_norm_backward, self.handle, positions.data_ptr(), batch, n, tq, xq, tk, xk, _TYPE_CODE[dtype], norm,
+                     dq_weight.data_ptr(), _ptr(dk_weight), ws.data_ptr(), nbytes.value)
+            if rc != SPLA_OK:
+                raise SplaError(rc, "spla_rope_norm_backward")
+        else:
+            dq_weight = torch.zeros(self.head_dim, dtype=torch.float32, device=device)
+            dk_weight = None if k is None else torch.zeros(self.head_dim, dtype=torch.float32, device=device)
+        return (dq, dq_weight) if k is None else (dq, dq_weight, dk, dk_weight)
+
+    def _input(self, x, shape, dtype, device):
+        """The packed descriptor of an input alone (its strides may be 0)."""
+        xshape, xs = x.shape, x.stride()
+        if not (xshape[:-2] == shape and xshape[-1] == self.head_dim and xs[-1] == 1 and x.dtype is dtype and x.device == device and x.is_cuda):
+            raise ValueError("rope: tensors [batch, tokens, heads, head_dim] or [tokens, heads, head_dim] of the positions' batch and device, "
+                             "of one type, bf16 or fp32, channels contiguous")
+        s = (0, *xs) if len(xs) == 3 else xs
+        return None, _pack_rope_tensor(x.data_ptr(), x.data_ptr(), xshape[-2], s[0], s[1], s[2], s[0], s[1], s[2])
+
     def close(self):
         if getattr(self, "handle", None) is not None and self.handle.value:
             self.lib.spla_rope_destroy(self.handle)
@@ -472,17 +564,45 @@ class Rope:
 class PagedCache:
     """K/V in pages (`spla_paged_create`): k_pages, v_pages [n_pages, H_kv, P, d], bf16 or fp32, kept by the caller's tensors.
 
+    Or in 8 bits (`spla_paged_create_scaled`): k_pages, v_pages torch.float8_e4m3fn with k_scales, v_scales torch.float8_e8m0fnu
+    [n_pages, H_kv, P / 16], a power of two for every 16 tokens of a head; new tokens and queries have the type `q_dtype`.  `PagedCache.pages`
+    makes the tensors.
+
     New tokens of all sequences come as one list of rows: cu_new int32 [batch + 1] says which rows are whose, seq_lens int32 [batch]
     how many tokens a sequence has with them, page_table int32 [batch, columns] where they lie."""
 
     _of_spla = False
+    _new_dtype = None                                                        # of new tokens, where it is not the pages'
 
-    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, n_q_heads: int, q_dtype: str | None = None, sm_scale: float = 0.0, flags: int = 0):
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, n_q_heads: int, q_dtype: str | None = None, sm_scale: float = 0.0, flags: int = 0,
+                 k_scales: torch.Tensor | None = None, v_scales: torch.Tensor | None = None):
+        if k_scales is not None or v_scales is not None:
+            self._create_scaled(k_pages, v_pages, n_q_heads, q_dtype or "bf16", sm_scale, flags, k_scales, v_scales)
+            return
         if not (k_pages.is_cuda and k_pages.dim() == 4 and k_pages.is_contiguous() and v_pages.is_contiguous() and k_pages.dtype in _TYPE_CODE
                 and v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype and v_pages.device == k_pages.device):
             raise ValueError("paged cache: contiguous k_pages, v_pages [n_pages, H_kv, P, d] of one type and device")
         n_pages, hkv, P, d = k_pages.shape
         self._create(k_pages, v_pages, n_pages, hkv, P, d, 0, 0, n_q_heads, q_dtype, sm_scale, flags)
+
+    def _create_scaled(self, k, v, n_q_heads, q_dtype, sm_scale, flags, ks, vs):
+        e4m3, e8m0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+        if not (k.is_cuda and k.dim() == 4 and k.dtype == v.dtype == e4m3 and v.shape == k.shape and ks is not None and vs is not None
+                and ks.dtype == vs.dtype == e8m0 and ks.shape == vs.shape == (k.shape[0], k.shape[1], k.shape[2] // 16)
+                and all(x.is_contiguous() and x.device == k.device for x in (k, v, ks, vs))):
+            raise ValueError("paged cache: contiguous float8_e4m3fn k_pages, v_pages [n_pages, H_kv, P, d] and float8_e8m0fnu k_scales, v_scales "
+                             "[n_pages, H_kv, P / 16] of one device")
+        n_pages, hkv, P, d = k.shape
+        self.k_scales, self.v_scales = ks, vs
+        self._new_dtype = {"bf16": torch.bfloat16, "f32": torch.float32}[q_dtype]
+        self._create(k, v, n_pages, hkv, P, d, 0, 0, n_q_heads, q_dtype, sm_scale, flags)
+
+    @staticmethod
+    def pages(n_pages: int, n_kv_heads: int, page_size: int, head_dim: int, device="cuda") -> dict:
+        """The tensors of an 8-bit cache without tokens, as `PagedCache(**PagedCache.pages(...), n_q_heads=...)` takes them."""
+        values = lambda: torch.zeros(n_pages, n_kv_heads, page_size, head_dim, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)  # noqa: E731
+        scales = lambda: torch.full((n_pages, n_kv_heads, page_size // 16), 127, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu)  # noqa: E731
+        return dict(k_pages=values(), v_pages=values(), k_scales=scales(), v_scales=scales())
 
     @classmethod
     def of(cls, cache: SplaCache, sm_scale: float | None = None, flags: int = 0) -> "PagedCache":
@@ -507,12 +627,16 @@ class PagedCache:
         self.k_pages, self.v_pages, self.device = k, v, k.device
         self.page_size, self.n_q_heads, self.n_kv_heads, self.head_dim = P, n_q_heads, hkv, d
         self.q_torch_dtype = {"bf16": torch.bfloat16, "f32": torch.float32, None: k.dtype}[q_dtype]
+        new = self._new_dtype
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
-        cfg = SplaPagedConfig(n_q_heads, hkv, d, P, n_pages, _TYPE_CODE[k.dtype], _TYPE_CODE[self.q_torch_dtype], page_stride, head_stride, sm_scale, flags)
+        cfg = SplaPagedConfig(n_q_heads, hkv, d, P, n_pages, _TYPE_CODE[new or k.dtype], _TYPE_CODE[self.q_torch_dtype], page_stride, head_stride, sm_scale, flags)
         self.index = k.get_device()
         self.handle = C.c_void_p()
-        _check(_on(self.index, lambda *a: self.lib.spla_paged_create(*a[:-1]), C.byref(cfg), k.data_ptr(), v.data_ptr(), self.status.data_ptr(),
-                   C.byref(self.handle)), "spla_paged_create")
+        create, scales = self.lib.spla_paged_create, ()
+        if new is not None:
+            create, scales = self.lib.spla_paged_create_scaled, (self.k_scales.data_ptr(), self.v_scales.data_ptr())
+        _check(_on(self.index, lambda *a: create(*a[:-1]), C.byref(cfg), k.data_ptr(), v.data_ptr(), *scales, self.status.data_ptr(),
+                   C.byref(self.handle)), create.__name__)
 
     def _batch(self, total, cu_new, seq_lens, page_table, max_new, max_len):
         """The packed spla_paged_batch_t."""
@@ -538,13 +662,14 @@ class PagedCache:
         return xs[0]
 
     def append(self, k: torch.Tensor, v: torch.Tensor, cu_new: torch.Tensor, seq_lens: torch.Tensor, page_table: torch.Tensor,
-               q: torch.Tensor | None = None, rope: Rope | None = None, positions: torch.Tensor | None = None, q_out: torch.Tensor | None = None):
+               q: torch.Tensor | None = None, rope: Rope | None = None, positions: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
+               q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float = 1e-6):
         """Stores k, v [total, H_kv, d] at the last n_b positions of every sequence, keys rotated by `rope`; rotates q [total, H_q, d]
         beside them and returns it (None without q).  Tokens may be any stride apart that keeps them off each other (no expanded tensors);
-        `q_out=q` works in place."""
+        `q_out=q` works in place.  With `k_weight`, `q_weight` (fp32 [d]) keys and queries are normed head by head before (`Rope.norm_apply`)."""
         if self._of_spla:
             raise ValueError("paged cache: the pages of an SPLA cache are read only; append to the SPLA cache")
-        total, hkv, kt = k.shape[0], self.n_kv_heads, self.k_pages.dtype
+        total, hkv, kt = k.shape[0], self.n_kv_heads, self._new_dtype or self.k_pages.dtype
         ks = self._rows(k, total, hkv, kt, "k")
         vs = self._rows(v, total, hkv, kt, "v")
         qs = os_ = 0
@@ -562,18 +687,45 @@ class PagedCache:
             # the store needs no bounds of its own: a sequence may be as long as the table has columns
             most = min(page_table.shape[1] * self.page_size, 1 << 24)
             b = self._batch(total, cu_new, seq_lens, page_table, min(total, most), most)
-            rc = _on(self.index, self.lib.spla_paged_append, self.handle, b, None if rope is None else rope.handle, _ptr(positions),
+            norm = None
+            if q_weight is not None or k_weight is not None:
+                norm = _pack_norm(*(0 if w is None else _norm_weight(w, self.head_dim, self.device) for w in (q_weight, k_weight)), eps)
+            rc = _on(self.index, self.lib.spla_paged_append_norm, self.handle, b, None if rope is None else rope.handle, _ptr(positions), norm,
                      k.data_ptr(), ks, v.data_ptr(), vs, qp, qs, op, os_)
             if rc != SPLA_OK:
                 raise SplaError(rc, "spla_paged_append")
         return q_out
 
+    def read(self, cu_new: torch.Tensor, seq_lens: torch.Tensor, page_table: torch.Tensor, total: int, dtype: torch.dtype | None = None,
+             k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None):
+        """The last n_b cached tokens of every sequence as rows k, v [total, H_kv, d], where `append` took them from: in `dtype` (bf16 or fp32;
+        default: that of the queries).  Rows of no sequence are not written."""
+        shape = (total, self.n_kv_heads, self.head_dim)
+        if dtype is None:
+            dtype = self.q_torch_dtype if k_out is None else k_out.dtype
+        if dtype not in _TYPE_CODE:
+            raise ValueError("paged cache: tokens are read as bf16 or fp32")
+        rows = []
+        for x in (k_out, v_out):
+            if x is None:
+                x = torch.empty(shape, dtype=dtype, device=self.device)
+            elif not (x.shape == shape and x.dtype is dtype and x.device == self.device and x.is_contiguous()):
+                raise ValueError("paged cache: contiguous k_out, v_out [total, H_kv, d] of one type")
+            rows.append(x)
+        if total:
+            most = min(page_table.shape[1] * self.page_size, 1 << 24)
+            b = self._batch(total, cu_new, seq_lens, page_table, min(total, most), most)
+            rc = _on(self.index, self.lib.spla_paged_read, self.handle, b, rows[0].data_ptr(), rows[1].data_ptr(), _TYPE_CODE[dtype])
+            if rc != SPLA_OK:
+                raise SplaError(rc, "spla_paged_read")
+        return rows[0], rows[1]
+
     def attend(self, q: torch.Tensor, cu_new: torch.Tensor, seq_lens: torch.Tensor, page_table: torch.Tensor, max_new: int, max_len: int,
                out: torch.Tensor | None = None, lse: torch.Tensor | None = None, softcap: float = 0.0, window: int = 0,
-               slopes: torch.Tensor | None = None, first_key: torch.Tensor | None = None, prefix_lens: torch.Tensor | None = None):
+               slopes: torch.Tensor | None = None, first_key: torch.Tensor | None = None, prefix_lens: torch.Tensor | None = None, sinks: int = 0):
         """Attention of the new tokens' queries q [total, H_q, d] over the cache, which holds their keys already; max_new and max_len
         bound the new tokens and the length of any sequence.  Returns out [total, H_q, d] and lse fp32 [total, H_q].  See
-        spla_paged_mask_t for the mask."""
+        spla_paged_mask_t for the mask; `sinks` first tokens stay visible beside a window (`spla_paged_attend_sinks`)."""
         total, hq, dev = q.shape[0], self.n_q_heads, self.device
         qs = self._rows(q, total, hq, self.q_torch_dtype, "q")
         if out is None:
@@ -598,7 +750,7 @@ class PagedCache:
             n = nbytes.value
             # a scratch of the call's own, from the stream's pool: calls on other streams and captured graphs share nothing
             ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
-            rc = _on(self.index, self.lib.spla_paged_attend, self.handle, b, q.data_ptr(), qs, mask, out.data_ptr(), lse.data_ptr(),
+            rc = _on(self.index, self.lib.spla_paged_attend_sinks, self.handle, b, q.data_ptr(), qs, mask, sinks, out.data_ptr(), lse.data_ptr(),
                      None if ws is None else ws.data_ptr(), n)
             if rc != SPLA_OK:
                 raise SplaError(rc, "spla_paged_attend")

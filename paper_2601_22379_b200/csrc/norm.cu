@@ -1,0 +1,261 @@
+// Norms of queries and keys, head by head, with the rotation to their positions in the same pass; and the gradients of that.
+//
+//   n_c = x_c r w_c,  r = (mean_c x_c^2 + eps)^(-1/2),  y = R n          (R: the rotation, an orthogonal map times its amplitude)
+//   u = R^T dy,  dw_c = sum over tokens and heads of u_c x_c r,  dx_c = r (w_c u_c - x_c r^2 mean_c(w_c u_c x_c))
+//
+// A CTA takes a few tokens: their sines into shared memory, then all rows (one head of one token) of the queries, then of the keys.  A row
+// belongs to a power of two of neighbouring lanes, 16 bytes of either half (or of neighbouring pairs) each, so that its sums are a few
+// shuffles, its channels stay in registers, and every element is read and written once.  r is formed again in the backward
+// pass: x has to be read anyway.
+// Gradients of the weights: a thread adds its channels up in registers over all rows that its CTA takes (the grid is one wave then), the CTA's
+// rows meet in shared memory, and a second kernel adds the CTAs' sums in their order: no atomics, the same bits every time.
+// All arithmetic in fp32, one rounding at the end.
+// @figures
+#include "rope_device.cuh"
+
+namespace spla {
+
+namespace {
+
+constexpr int kNormThreads = 256;
+constexpr int kNormTable = 2048;         // (token, pair) entries of a CTA's table, at most
+constexpr int kNormMaxDim = 2 * kRopeMaxPairs;
+
+struct NormLaunch {
+  NormGroup g[2];                        // queries, keys
+  const int* positions;
+  int tokens, tb, tiles_per_batch;       // of a batch entry; per tile
+  int tiles;                             // of all batch entries
+  int rows_per_y;
+  unsigned head_magic[2];                // as in RopeLaunch
+  float eps, per_channel;
+  int width;                             // lanes of a row
+  float* part;                           // [CTAs][2][dim]: sums for the weights' gradients
+};
+
+template <typename T, class ROW, bool BWD>
+__global__ void __launch_bounds__(kNormThreads, BWD ? 2 : 3)
+    norm_kernel(const __grid_constant__ NormLaunch r, const __grid_constant__ RopeTable rt) {
+  constexpr int CH = ROW::CH, WORDS = ROW::WORDS, ROWS = BWD ? 1 : 2;   // rows that a thread has on their way at a time
+  constexpr bool loose = ROW::CH == ROW::WORDS && sizeof(ROW) == sizeof(LooseRow<T, CH>);
+  __shared__ __align__(16) float2 table[kNormTable];               // and the rows' sums for the weights, at the end
+  __shared__ __align__(16) float w_s[2][kNormMaxDim];
+  __shared__ float rows_s[loose ? kNormThreads / 32 : 1][loose ? kNormMaxDim : 1];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int tid = threadIdx.x, pairs = rt.rot / 2, dim = rt.dim;
+  const int width = r.width, by = kNormThreads / width, ty = tid / width;
+  const ROW row(rt, tid % width);
+  float* own_row = rows_s[loose ? tid / 32 : 0];
+  for (int x = tid; x < 2 * dim; x += kNormThreads) {
+    const int g = x >= dim;
+    if (r.g[g].n_heads > 0) w_s[g][x - g * dim] = __ldg(r.g[g].weight + x - g * dim);
+  }
+  float acc[2][BWD ? CH : 1];
+#pragma unroll
+  for (int i = 0; i < (BWD ? CH : 1); ++i) acc[0][i] = acc[1][i] = 0.f;
+  for (int tile = blockIdx.x; tile < r.tiles; tile += gridDim.x) {
+    const int b = tile / r.tiles_per_batch, tok0 = (tile - b * r.tiles_per_batch) * r.tb, nt = min(r.tb, r.tokens - tok0);
+    const int* pos = r.positions + (long long)b * r.tokens + tok0;
+    if (tile != (int)blockIdx.x) __syncthreads();                  // (the table before is used up)
+    fill_turns<ROW>(rt, table, nt, tid, kNormThreads, BWD, [&](int t) { return __ldg(pos + t); });
+    __syncthreads();
+    const int first = (int)blockIdx.y * r.rows_per_y, last = first + r.rows_per_y, n_q = nt * r.g[0].n_heads, n_all = n_q + nt * r.g[1].n_heads;
+    auto group = [&](const NormGroup& g, int gi, int from, int to, float (&sum)[BWD ? CH : 1]) {
+      if (from >= to) return;
+      const unsigned magic = r.head_magic[gi];
+      // (whole warps: a row's lanes meet in shuffles)
+#pragma unroll 1
+      for (int r0 = from; r0 < to; r0 += ROWS * by) {
+        uint32_t raw[ROWS][WORDS], raw_g[ROWS][BWD ? WORDS : 1];
+        int tk[ROWS];
+        T* out[ROWS];
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+          const int x = r0 + k * by + ty;
+          tk[k] = 0;
+          out[k] = nullptr;
+          if (x >= to || !row.here) continue;
+          const int t = g.n_heads == 1 ? x : (int)__umulhi((unsigned)x, magic), h = x - t * g.n_heads;
+          tk[k] = t;
+          const long long tok = tok0 + t;
+          row.load(reinterpret_cast<const T*>(g.x) + b * g.x_batch + tok * g.x_token + h * g.x_head, raw[k]);
+          if constexpr (BWD) row.load(reinterpret_cast<const T*>(g.dy) + b * g.dy_batch + tok * g.dy_token + h * g.dy_head, raw_g[k]);
+          out[k] = reinterpret_cast<T*>(g.out) + b * g.out_batch + tok * g.out_token + h * g.out_head;
+        }
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+          float x[CH];
+          row.values(raw[k], x);
+          if (!out[k])
+#pragma unroll
+            for (int i = 0; i < CH; ++i) x[i] = 0.f;
+          const float rms = row_rms(x, width, r.per_channel, r.eps);
+          const float2* tab = table + tk[k] * pairs;
+          float w[CH];
+          row.weights(w_s[gi], w);
+          if constexpr (!BWD) {
+#pragma unroll
+            for (int i = 0; i < CH; ++i) x[i] = x[i] * rms * w[i];
+            row.turn(x, tab, own_row);
+            if (out[k]) row.store(out[k], x);
+          } else {
+            float u[CH];
+            row.values(raw_g[k], u);
+            row.turn(u, tab, own_row);
+            float dot = 0.f;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+              if (!out[k]) u[i] = 0.f;
+              sum[i] = fmaf(u[i] * x[i], rms, sum[i]);
+              u[i] *= w[i];
+              dot = fmaf(u[i], x[i], dot);
+            }
+            dot = row_sum(dot, width) * r.per_channel * rms * rms;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) u[i] = rms * (u[i] - x[i] * dot);
+            if (out[k]) row.store(out[k], u);
+          }
+        }
+      }
+    };
+    group(r.g[0], 0, min(first, n_q), min(last, n_q), acc[0]);
+    if (r.g[1].n_heads > 0) group(r.g[1], 1, max(first, n_q) - n_q, min(last, n_all) - n_q, acc[1]);
+  }
+  if constexpr (BWD) {
+    float* red = reinterpret_cast<float*>(table);                  // [by][dim]
+    for (int g = 0; g < 2; ++g) {
+      if (r.g[g].n_heads == 0) continue;
+      __syncthreads();
+      if (row.here)
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+          if (row.channel(i) < dim) red[ty * dim + row.channel(i)] = g ? acc[1][i] : acc[0][i];
+      __syncthreads();
+      for (int c = tid; c < dim; c += kNormThreads) {
+        float s = 0.f;
+        for (int y = 0; y < by; ++y) s += red[y * dim + c];
+        r.part[((long long)(blockIdx.y * gridDim.x + blockIdx.x) * 2 + g) * dim + c] = s;
+      }
+    }
+  }
+}
+
+// Sums of `n` CTAs for 32 channels of one weight, in their order: every warp a run of the CTAs, then the runs.
+constexpr int kNormSumWarps = 16;
+__global__ void __launch_bounds__(32 * kNormSumWarps) norm_sum_kernel(const float* part, int n, int dim, float* dq, float* dk) {
+  __shared__ float runs[kNormSumWarps][32];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, g = blockIdx.y;
+  float* out = g ? dk : dq;
+  if (!out) return;
+  const int from = (int)((long long)n * warp / kNormSumWarps), to = (int)((long long)n * (warp + 1) / kNormSumWarps);
+  float s = 0.f;
+  if (c < dim)
+#pragma unroll 8
+    for (int x = from; x < to; ++x) s += part[((long long)x * 2 + g) * dim + c];
+  runs[warp][lane] = s;
+  __syncthreads();
+  if (warp == 0 && c < dim) {
+    float all = 0.f;
+#pragma unroll
+    for (int x = 0; x < kNormSumWarps; ++x) all += runs[x][lane];
+    out[c] = all;
+  }
+}
+
+struct NormPlan {
+  int tb, tiles_per_batch, ys, rows_per_y, grid_x;
+  long long tiles;
+};
+// tokens and heads alone decide it: the sums that the weights' gradients take are the same for any addresses
+NormPlan plan_norm(const RopeTable& rt, int batch, int tokens, int heads, bool backward, int sm_count) {
+  NormPlan p;
+  const int pairs = rt.rot / 2;
+  // tokens of a tile: a sine for every thread, rows for every thread where heads are few, less where SMs would idle (as in rope.cu)
+  constexpr int by = 32;
+  int tb = kNormThreads / pairs < 8 ? kNormThreads / pairs : 8;
+  if (tb < (4 * by + heads - 1) / heads) tb = (4 * by + heads - 1) / heads;
+  if (tb > 64) tb = 64;
+  if (tb * pairs > kNormTable) tb = kNormTable / pairs;
+  if (tb < 1) tb = 1;
+  while (tb > 1 && (long long)tb * heads * heads >= (1ll << 32)) tb /= 2;      // (see head_magic)
+  auto tiles = [&](int x) { return (long long)((tokens + x - 1) / x) * batch; };
+  while (tb > 1 && tiles(tb) < 2LL * sm_count) tb /= 2;
+  if (tb > tokens) tb = tokens;
+  p.tb = tb;
+  p.tiles_per_batch = (tokens + tb - 1) / tb;
+  p.tiles = tiles(tb);
+  const int rows = tb * heads;
+  p.ys = 1;
+  if (p.tiles < 2LL * sm_count) {
+    p.ys = (rows + by - 1) / by;
+    const long long most = (4LL * sm_count + p.tiles - 1) / p.tiles;
+    if (p.ys > most) p.ys = (int)most;
+  }
+  p.rows_per_y = (rows + p.ys - 1) / p.ys;
+  p.ys = (rows + p.rows_per_y - 1) / p.rows_per_y;
+  const long long wave = (2LL * sm_count + p.ys - 1) / p.ys;
+  p.grid_x = (int)(backward && wave < p.tiles ? wave : p.tiles);
+  return p;
+}
+
+template <typename T, class ROW, bool BWD>
+cudaError_t norm_launch(const NormLaunch& r, const NormPlan& p, const RopeTable& rt, cudaStream_t s) {
+  return launch_ex(norm_kernel<T, ROW, BWD>, dim3(p.grid_x, p.ys), dim3(kNormThreads), 0, s, 0, true, r, rt);
+}
+template <typename T, bool BWD>
+cudaError_t norm_rows(NormLaunch& r, const NormPlan& p, const RopeTable& rt, bool wide, cudaStream_t s) {
+  constexpr int vec = 16 / (int)sizeof(T);
+  if (!wide) {
+    r.width = 32;
+    return norm_launch<T, LooseRow<T, kNormMaxDim / 32>, BWD>(r, p, rt, s);
+  }
+  for (r.width = 1; r.width < rt.dim / (2 * vec);) r.width *= 2;
+  return norm_launch<T, WideRow<T, vec>, BWD>(r, p, rt, s);
+}
+
+}  // namespace
+
+size_t norm_part_bytes(const RopeTable& rt, int batch, int tokens, int heads, int sm_count) {
+  const NormPlan p = plan_norm(rt, batch, tokens, heads, true, sm_count);
+  return (size_t)p.grid_x * p.ys * 2 * rt.dim * 4;
+}
+
+cudaError_t launch_norm(const RopeTable& rt, const int* positions, int batch, int tokens, const NormGroup& q, const NormGroup& k, float eps, int f32,
+                        bool backward, float* dq_weight, float* dk_weight, void* workspace, cudaStream_t s) {
+  const int sm = device_sm_count(), heads = q.n_heads + k.n_heads;
+  const NormPlan p = plan_norm(rt, batch, tokens, heads, backward, sm);
+  if (p.tiles >= (1ll << 31)) return cudaErrorInvalidValue;
+  NormLaunch r = {};
+  r.g[0] = q;
+  r.g[1] = k;
+  r.positions = positions;
+  r.tokens = tokens;
+  r.tb = p.tb;
+  r.tiles_per_batch = p.tiles_per_batch;
+  r.tiles = (int)p.tiles;
+  r.rows_per_y = p.rows_per_y;
+  r.eps = eps;
+  r.per_channel = 1.f / (float)rt.dim;
+  r.part = reinterpret_cast<float*>(workspace);
+  const int e = f32 ? 4 : 2;
+  bool wide = wide_rotation(rt, e);
+  for (int i = 0; i < 2; ++i) {
+    const NormGroup& g = r.g[i];
+    if (g.n_heads == 0) continue;
+    r.head_magic[i] = (unsigned)(((1ull << 32) + g.n_heads - 1) / g.n_heads);
+    wide = wide && wide_strides(g.x, e, g.x_batch, g.x_token, g.x_head) && wide_strides(g.out, e, g.out_batch, g.out_token, g.out_head) &&
+           (!backward || wide_strides(g.dy, e, g.dy_batch, g.dy_token, g.dy_head));
+  }
+  cudaError_t err;
+  if (backward) err = f32 ? norm_rows<float, true>(r, p, rt, wide, s) : norm_rows<__nv_bfloat16, true>(r, p, rt, wide, s);
+  else err = f32 ? norm_rows<float, false>(r, p, rt, wide, s) : norm_rows<__nv_bfloat16, false>(r, p, rt, wide, s);
+  if (err == cudaSuccess && backward)
+    err = launch_ex(norm_sum_kernel, dim3((rt.dim + 31) / 32, 2), dim3(32 * kNormSumWarps), 0, s, 0, true, (const float*)workspace, p.grid_x * p.ys, rt.dim,
+                    dq_weight, k.n_heads ? dk_weight : (float*)nullptr);
+  return err;
+}
+
+}  // namespace spla

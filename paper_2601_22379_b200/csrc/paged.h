@@ -26,6 +26,34 @@ struct RopeGroup {
   int elem_f32;                         // element type: 1 = fp32, 0 = bf16
 };
 
+// One tensor of launch_norm: x -> out, and in the backward pass the gradient dy of y.  Strides in elements.
+struct NormGroup {
+  const void *x, *dy;
+  void* out;
+  const float* weight;                  // [dim]
+  int n_heads;                          // 0: not there
+  long long x_batch, x_token, x_head, dy_batch, dy_token, dy_head, out_batch, out_token, out_head;
+};
+
+// The new tokens of launch_store; strides in elements between tokens.
+struct StoreGroups {
+  const void *q, *k, *v;
+  void* q_out;
+  long long q_stride, k_stride, v_stride, q_out_stride;
+  int q_f32, kv_f32;
+  const float *q_weight, *k_weight;     // null: not normed
+  float eps;
+  const int* positions;
+};
+
+// What the pages hold.  8-bit pages: e4m3 values, and for every 16 rows (tokens of a head) the scale 2^(byte - 127).
+enum { kPagesBf16 = 0, kPagesF32 = 1, kPagesE4m3 = 2 };
+struct PagedPages {
+  void *k, *v;
+  unsigned char *k_scales, *v_scales;
+  int type;
+};
+
 struct PagedBatch {
   const int* cu;                        // [batch + 1] rows of the new tokens
   const int* lens;                      // [batch] cached tokens, the new ones included
@@ -144,6 +172,9 @@ struct PagedAttend {
   const int* first_key;
   const int* prefix;
   int wait_limit, dbg_tx_extra;         // as in Params
+  int sinks;                            // so many first tokens are visible besides the window
+  int from_new, to_new;                 // sequences of so many new tokens are this launch's (0, 0: all of them); the others are passed over
+  const unsigned char *k_scales, *v_scales;   // of 8-bit pages
 };
 
 // Sequence table of a CTA, in shared memory.
@@ -154,17 +185,28 @@ struct PagedSeqs {
 
 __host__ __device__ __forceinline__ int paged_units(const PagedWork& w, int n) { return n <= w.ppos ? (n > 0) : (n + w.upos - 1) / w.upos; }
 
-// Key tiles [t0, t1) that unit u of a sequence may walk.  Never empty: a position sees itself.  From e0 on they count when the work is
+// New tokens of a sequence as far as they are this launch's.
+__device__ __forceinline__ int paged_mine(const PagedAttend& a, int n) { return a.to_new > 0 && (n < a.from_new || n > a.to_new) ? 0 : n; }
+
+// Key tiles [t0, t1) that unit u of a sequence may walk.  With a window and sinks the tiles are numbered without those between the sinks' and the
+// window's: the first `ns` are tiles 0 .. ns - 1, the others lie `skip` tiles further on.  Never empty: a position sees itself.  From e0 on they count when the work is
 // dealt out: the tiles before are behind the start of its first token's document, where there is nothing to walk as long as
 // documents follow one another (what is walked goes by every token's own start).
 struct PagedSpan {
   int t0, t1, e0;
+  int ns, skip;
 };
 __device__ __forceinline__ PagedSpan paged_span(const PagedAttend& a, int row0, int n, int L, int prefix, int u) {
   const PagedWork& w = a.w;
   const int p0 = L - n + u * w.upos, p1 = L - n + min(n, (u + 1) * w.upos) - 1;
   const int lo = a.window > 0 ? max(0, p0 - a.window + 1) : 0, hi = min(L, max(p1 + 1, prefix));
-  PagedSpan s{lo >> w.log_tk, (hi + (1 << w.log_tk) - 1) >> w.log_tk, 0};
+  PagedSpan s{lo >> w.log_tk, (hi + (1 << w.log_tk) - 1) >> w.log_tk, 0, 0, 0};
+  if (a.sinks > 0 && s.t0 > 0) {
+    s.ns = min(s.t0, (min(a.sinks, hi) + (1 << w.log_tk) - 1) >> w.log_tk);
+    s.skip = s.t0 - s.ns;
+    s.t0 = 0;
+    s.t1 -= s.skip;
+  }
   s.e0 = s.t0;
   if (a.first_key && !w.by_unit) s.e0 = min(max(s.t0, __ldg(a.first_key + row0 + u * w.upos) >> w.log_tk), s.t1 - 1);
   return s;
@@ -218,7 +260,7 @@ __device__ __forceinline__ long long paged_fill_seqs(const PagedAttend& a, Paged
     if (lane < batch) {
       pre = a.prefix ? __ldg(a.prefix + lane) : 0;
       const PagedSeq s = paged_seq(a.pb, a.pl.status, lane);
-      row0 = s.row0; n = s.n; L = s.L; fits = s.fits;
+      row0 = s.row0; n = paged_mine(a, s.n); L = s.L; fits = s.fits;
     }
     if (!__all_sync(0xffffffffu, fits)) {
       const int c = paged_order(a.pb, row0);
@@ -245,7 +287,7 @@ __device__ __forceinline__ long long paged_fill_seqs(const PagedAttend& a, Paged
     if (b < batch) {
       pre = a.prefix ? __ldg(a.prefix + b) : 0;
       const PagedSeq s = paged_seq(a.pb, a.pl.status, b);
-      row0 = s.row0; n = s.n; L = s.L; fits &= s.fits;
+      row0 = s.row0; n = paged_mine(a, s.n); L = s.L; fits &= s.fits;
       t.row0[b] = row0; t.n[b] = n; t.L[b] = L; t.prefix[b] = pre;
     }
     const long long per_head = paged_seq_tiles(a, row0, n, L, pre, lane);
@@ -290,6 +332,7 @@ struct PagedWalk {
   int row0, n, L, prefix;
   // the current segment
   int t0, t1;                           // key tiles
+  int ns, skip;                         // see PagedSpan
   bool head, tail;                      // it starts / ends the unit
 
   __device__ __forceinline__ void load(const PagedWork& w, const PagedSeqs& t) { row0 = t.row0[b]; n = t.n[b]; L = t.L[b]; prefix = t.prefix[b]; units = paged_units(w, n); }
@@ -347,6 +390,7 @@ struct PagedWalk {
         }
       }
       const PagedSpan s = paged_span(a, row0, n, L, prefix, u);
+      ns = s.ns; skip = s.skip;
       if (a.w.by_unit) {
         t0 = s.t0; t1 = s.t1; head = tail = true;
         left -= 1;
@@ -376,7 +420,7 @@ struct PagedWalk {
   __device__ __forceinline__ int n_pos(const PagedWork& w) const { return min(n - u_cur * w.upos, n <= w.ppos ? w.ppos : w.upos); }
 };
 
-// Keys [lo, hi) that the new token with index i of a sequence sees.
+// Keys [lo, hi) that the new token with index i of a sequence sees, besides those before both `hi` and a.sinks.
 struct PagedSees {
   int lo, hi;
 };
@@ -405,6 +449,12 @@ inline bool paged_narrow(const PagedWork& w, const PagedBatch& pb, const PagedLa
   return units * tiles + w.n_cta < 2147483647.0;
 }
 
+// Scales of 8-bit pages: exponents between -40 and 40 (others are read as the nearest).
+constexpr int kExpMin = -40, kExpMax = 40;
+__device__ __forceinline__ int paged_exponent(const unsigned char* p) { return min(max((int)__ldg(p) - 127, kExpMin), kExpMax); }
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((127 + e) << 23); }
+__device__ __forceinline__ float paged_scale(const unsigned char* scales, long long row) { return power_of_two(paged_exponent(scales + (row >> 4))); }
+
 struct PagedMaps {                      // TMA tensor maps (CUtensorMap), opaque to the host code
   alignas(64) unsigned char k[128];
   alignas(64) unsigned char v[128];
@@ -414,9 +464,16 @@ struct PagedMaps {                      // TMA tensor maps (CUtensorMap), opaque
 // rope.cu: rotates / copies up to three groups; with `pages` the groups with out == null go to k_pages (group 1) and v_pages (group 2)
 cudaError_t launch_rope(const RopeTable& rt, const int* positions, int batch, int tokens, const RopeGroup* groups, int n_groups,
                         const PagedBatch* pb, const PagedLayout* pl, void* k_pages, void* v_pages, int transpose, cudaStream_t s);
+// store.cu: appends to pages of any type with norms, and to 8-bit pages; reads cached tokens back
+cudaError_t launch_store(const RopeTable* rope, const StoreGroups& g, const PagedBatch& pb, const PagedLayout& pl, const PagedPages& pages, cudaStream_t s);
+cudaError_t launch_read(const PagedBatch& pb, const PagedLayout& pl, const PagedPages& pages, void* k_out, void* v_out, int out_f32, cudaStream_t s);
+// norm.cu
+size_t norm_part_bytes(const RopeTable& rt, int batch, int tokens, int heads, int sm_count);
+cudaError_t launch_norm(const RopeTable& rt, const int* positions, int batch, int tokens, const NormGroup& q, const NormGroup& k, float eps, int f32,
+                        bool backward, float* dq_weight, float* dk_weight, void* workspace, cudaStream_t s);
 // paged_attend.cu: fp32 kernels for every type, and the join of cut units
 void paged_plan_general(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int sm_count);
-cudaError_t launch_paged_general(const PagedAttend& a, const void* k_pages, const void* v_pages, int q_bf16, int kv_bf16, cudaStream_t s);
+cudaError_t launch_paged_general(const PagedAttend& a, const PagedPages& pages, int q_bf16, cudaStream_t s);
 cudaError_t launch_paged_join(const PagedAttend& a, int out_bf16, cudaStream_t s);
 // paged_mma.cu: bf16 on tcgen05
 size_t paged_mma_drain_bytes(const PagedWork& w, const PagedBatch& pb, const PagedLayout& pl);

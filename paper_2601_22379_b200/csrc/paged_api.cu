@@ -17,7 +17,7 @@ struct spla_rope {
 struct spla_paged {
   spla_paged_config_t cfg;
   PagedLayout pl;
-  void *k_pages, *v_pages;
+  PagedPages pages;
   PagedMaps maps;
   bool tensor;                          // bf16 cache and queries, tensor maps made: the tensor-core kernel serves it
   int sm_count;
@@ -96,8 +96,76 @@ extern "C" int spla_rope_apply(const spla_rope_t* rope, const int32_t* positions
   return e == cudaSuccess ? SPLA_OK : cuda_fail(e, "spla_rope_apply");
 }
 
+static bool norm_fits(const spla_head_norm_t* n) {
+  return n->eps >= 0.f && isfinite(n->eps) && (!n->q_weight || aligned(n->q_weight, 4)) && (!n->k_weight || aligned(n->k_weight, 4));
+}
+
+static bool rope_norm_tensor(const spla_rope_tensor_t* t, int dtype, bool out) {
+  const size_t e = dtype_bytes(dtype);
+  return t->in && aligned(t->in, e) && t->n_heads >= 1 && (!out || (t->out && aligned(t->out, e)));
+}
+static NormGroup norm_group(const spla_rope_tensor_t* x, const spla_rope_tensor_t* dy, const float* weight) {
+  NormGroup g = {};
+  if (!x) return g;
+  const spla_rope_tensor_t* o = dy ? dy : x;
+  g.x = x->in; g.out = o->out; g.weight = weight; g.n_heads = x->n_heads;
+  g.x_batch = x->in_batch; g.x_token = x->in_token; g.x_head = x->in_head;
+  g.out_batch = o->out_batch; g.out_token = o->out_token; g.out_head = o->out_head;
+  if (dy) { g.dy = dy->in; g.dy_batch = dy->in_batch; g.dy_token = dy->in_token; g.dy_head = dy->in_head; }
+  return g;
+}
+static bool same_in_place(const void* in, int64_t b, int64_t t, int64_t h, const spla_rope_tensor_t* o) {
+  return in != o->out || (b == o->out_batch && t == o->out_token && h == o->out_head);
+}
+static int check_norm(const spla_rope_t* rope, const int32_t* positions, int32_t batch, int32_t n_tokens, const spla_rope_tensor_t* q, const spla_rope_tensor_t* k,
+                      int32_t dtype, const spla_head_norm_t* norm, bool out) {
+  if (!rope || !positions || !q || batch < 1 || n_tokens < 1 || !is_dtype(dtype) || !aligned(positions, 4) || !norm || !norm_fits(norm)) return SPLA_ERR_INVALID_ARG;
+  if (!norm->q_weight || (k && !norm->k_weight) || !rope_norm_tensor(q, dtype, out) || (k && !rope_norm_tensor(k, dtype, out))) return SPLA_ERR_INVALID_ARG;
+  if (q->n_heads > kRopeMaxHeads || (k && k->n_heads > kRopeMaxHeads) || (int64_t)batch * n_tokens >= (1ll << 31)) return SPLA_ERR_UNSUPPORTED;
+  return SPLA_OK;
+}
+
+extern "C" int spla_rope_norm_apply(const spla_rope_t* rope, const int32_t* positions, int32_t batch, int32_t n_tokens, const spla_rope_tensor_t* q,
+                                    const spla_rope_tensor_t* k, int32_t dtype, const spla_head_norm_t* norm, void* stream) {
+  const int rc = check_norm(rope, positions, batch, n_tokens, q, k, dtype, norm, true);
+  if (rc != SPLA_OK) return rc;
+  if (!same_in_place(q->in, q->in_batch, q->in_token, q->in_head, q) || (k && !same_in_place(k->in, k->in_batch, k->in_token, k->in_head, k))) return SPLA_ERR_INVALID_ARG;
+  cudaError_t e = launch_norm(rope->t, positions, batch, n_tokens, norm_group(q, nullptr, norm->q_weight), norm_group(k, nullptr, norm->k_weight), norm->eps,
+                              dtype == SPLA_F32, false, nullptr, nullptr, nullptr, (cudaStream_t)stream);
+  return e == cudaSuccess ? SPLA_OK : cuda_fail(e, "spla_rope_norm_apply");
+}
+
+extern "C" int spla_rope_norm_query_workspace(const spla_rope_t* rope, int32_t batch, int32_t n_tokens, int32_t n_heads, size_t* bytes_out) {
+  if (!rope || batch < 1 || n_tokens < 1 || n_heads < 1 || !bytes_out) return SPLA_ERR_INVALID_ARG;
+  if (n_heads > 2 * kRopeMaxHeads || (int64_t)batch * n_tokens >= (1ll << 31)) return SPLA_ERR_UNSUPPORTED;
+  *bytes_out = norm_part_bytes(rope->t, batch, n_tokens, n_heads, device_sm_count());
+  return SPLA_OK;
+}
+
+extern "C" int spla_rope_norm_backward(const spla_rope_t* rope, const int32_t* positions, int32_t batch, int32_t n_tokens, const spla_rope_tensor_t* q_grad,
+                                       const spla_rope_tensor_t* q, const spla_rope_tensor_t* k_grad, const spla_rope_tensor_t* k, int32_t dtype,
+                                       const spla_head_norm_t* norm, float* dq_weight, float* dk_weight, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_norm(rope, positions, batch, n_tokens, q, k, dtype, norm, false);
+  if (rc != SPLA_OK) return rc;
+  if (!q_grad || (k == nullptr) != (k_grad == nullptr) || !dq_weight || (k && !dk_weight) || !aligned(dq_weight, 4) || !aligned(dk_weight, 4)) return SPLA_ERR_INVALID_ARG;
+  if (!rope_norm_tensor(q_grad, dtype, true) || q_grad->n_heads != q->n_heads || (k && (!rope_norm_tensor(k_grad, dtype, true) || k_grad->n_heads != k->n_heads)))
+    return SPLA_ERR_INVALID_ARG;
+  for (int i = 0; i < 2; ++i) {                                                    // (dx may take the place of dy or of x)
+    const spla_rope_tensor_t *g = i ? k_grad : q_grad, *x = i ? k : q;
+    if (g && (!same_in_place(g->in, g->in_batch, g->in_token, g->in_head, g) || !same_in_place(x->in, x->in_batch, x->in_token, x->in_head, g))) return SPLA_ERR_INVALID_ARG;
+  }
+  size_t need = 0;
+  const int rw = spla_rope_norm_query_workspace(rope, batch, n_tokens, q->n_heads + (k ? k->n_heads : 0), &need);
+  if (rw != SPLA_OK) return rw;
+  if (!workspace || !aligned(workspace, 16) || workspace_bytes < need) return SPLA_ERR_INVALID_ARG;
+  cudaError_t e = launch_norm(rope->t, positions, batch, n_tokens, norm_group(q, q_grad, norm->q_weight), norm_group(k, k_grad, norm->k_weight), norm->eps,
+                              dtype == SPLA_F32, true, dq_weight, dk_weight, workspace, (cudaStream_t)stream);
+  return e == cudaSuccess ? SPLA_OK : cuda_fail(e, "spla_rope_norm_backward");
+}
+
 // ---- the paged cache -------------------------------------------------------------------------------------------------
-extern "C" int spla_paged_create(const spla_paged_config_t* c, void* k_pages, void* v_pages, int32_t* status, spla_paged_t** paged_out) {
+// k_scales: null for pages of 16 or 32 bits.
+static int create_paged(const spla_paged_config_t* c, void* k_pages, void* v_pages, uint8_t* k_scales, uint8_t* v_scales, int32_t* status, spla_paged_t** paged_out) {
   if (!c || !k_pages || !v_pages || !status || !paged_out) return SPLA_ERR_INVALID_ARG;
   if (c->n_q_heads < 1 || c->n_kv_heads < 1 || c->n_q_heads % c->n_kv_heads || c->n_pages < 1) return SPLA_ERR_INVALID_ARG;
   if (!is_dtype(c->kv_dtype) || !is_dtype(c->q_dtype)) return SPLA_ERR_INVALID_ARG;
@@ -111,6 +179,8 @@ extern "C" int spla_paged_create(const spla_paged_config_t* c, void* k_pages, vo
   const int64_t hs = c->head_stride ? c->head_stride : P, ps = c->page_stride ? c->page_stride : (int64_t)c->n_kv_heads * P;
   if (hs < P || ps < P) return SPLA_ERR_INVALID_ARG;                               // rows of neighbouring heads or pages would overlap
   if (ps >= (1ll << 31) || hs >= (1ll << 31)) return SPLA_ERR_UNSUPPORTED;
+  // (a row's scale is found by its number: pages and heads without gaps; a row of new tokens is one launch's)
+  if (k_scales && (hs != P || ps != (int64_t)c->n_kv_heads * P || c->q_dtype != c->kv_dtype)) return SPLA_ERR_UNSUPPORTED;
   spla_paged* p = new (std::nothrow) spla_paged;
   if (!p) return SPLA_ERR_INVALID_ARG;
   memset(p, 0, sizeof(*p));
@@ -121,16 +191,25 @@ extern "C" int spla_paged_create(const spla_paged_config_t* c, void* k_pages, vo
   p->pl.page_stride = ps;
   p->pl.head_stride = hs;
   p->pl.status = status;
-  p->k_pages = k_pages;
-  p->v_pages = v_pages;
+  p->pages = PagedPages{k_pages, v_pages, k_scales, v_scales, k_scales ? kPagesE4m3 : c->kv_dtype == SPLA_F32 ? kPagesF32 : kPagesBf16};
   if (p->cfg.sm_scale == 0.f) p->cfg.sm_scale = 1.0f / sqrtf((float)c->head_dim);
   p->sm_count = device_sm_count();
   // the tensor-core kernel: bf16, rows that a TMA coordinate can name
   const int64_t rows = (c->n_pages - 1) * ps + (c->n_kv_heads - 1) * hs + P;
-  p->tensor = c->kv_dtype == SPLA_BF16 && c->q_dtype == SPLA_BF16 && !(c->flags & SPLA_GENERAL_KERNELS) && rows < (1ll << 31) - 256 &&
+  p->tensor = !k_scales && c->kv_dtype == SPLA_BF16 && c->q_dtype == SPLA_BF16 && !(c->flags & SPLA_GENERAL_KERNELS) && rows < (1ll << 31) - 256 &&
               make_kv_map(p->maps.k, k_pages, c->head_dim, P, rows) && make_kv_map(p->maps.v, v_pages, c->head_dim, P, rows);
   *paged_out = p;
   return SPLA_OK;
+}
+
+extern "C" int spla_paged_create(const spla_paged_config_t* c, void* k_pages, void* v_pages, int32_t* status, spla_paged_t** paged_out) {
+  return create_paged(c, k_pages, v_pages, nullptr, nullptr, status, paged_out);
+}
+
+extern "C" int spla_paged_create_scaled(const spla_paged_config_t* c, void* k_pages, void* v_pages, uint8_t* k_scales, uint8_t* v_scales, int32_t* status,
+                                      spla_paged_t** paged_out) {
+  if (!k_scales || !v_scales) return SPLA_ERR_INVALID_ARG;
+  return create_paged(c, k_pages, v_pages, k_scales, v_scales, status, paged_out);
 }
 
 extern "C" int spla_paged_destroy(spla_paged_t* paged) {
@@ -153,9 +232,9 @@ static PagedBatch device_batch(const spla_paged_batch_t* b) {
                     b->max_len, b->table_stride, 0};
 }
 
-extern "C" int spla_paged_append(spla_paged_t* p, const spla_paged_batch_t* batch, const spla_rope_t* rope, const int32_t* positions,
-                                 const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const void* q, int64_t q_stride,
-                                 void* q_out, int64_t q_out_stride, void* stream) {
+extern "C" int spla_paged_append_norm(spla_paged_t* p, const spla_paged_batch_t* batch, const spla_rope_t* rope, const int32_t* positions,
+                                      const spla_head_norm_t* norm, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                                      const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, void* stream) {
   const int rc = check_batch(p, batch, true);
   if (rc != SPLA_OK) return rc;
   if (!k_new || !v_new || (q == nullptr) != (q_out == nullptr) || (rope && rope->t.dim != p->pl.d)) return SPLA_ERR_INVALID_ARG;
@@ -170,18 +249,41 @@ extern "C" int spla_paged_append(spla_paged_t* p, const spla_paged_batch_t* batc
   if (!aligned(k_new, ke) || !aligned(v_new, ke) || (q && (!aligned(q, qe) || !aligned(q_out, qe)))) return SPLA_ERR_INVALID_ARG;
   if (q && q == q_out && q_stride != q_out_stride) return SPLA_ERR_INVALID_ARG;
   if (positions && !aligned(positions, 4)) return SPLA_ERR_INVALID_ARG;
-  RopeTable none;
-  if (!rope) {
-    memset(&none, 0, sizeof(none));
-    none.dim = d;
-  }
+  if (norm && !norm_fits(norm)) return SPLA_ERR_INVALID_ARG;
+  const bool normed = norm && (norm->k_weight || (q && norm->q_weight));
   const int kv32 = p->cfg.kv_dtype == SPLA_F32, q32 = p->cfg.q_dtype == SPLA_F32, turn = rope != nullptr;
-  const RopeGroup g[3] = {{q, q_out, q ? p->pl.Hq : 0, turn, 0, q_stride, d, 0, q_out_stride, d, q32},
-                          {k_new, nullptr, p->pl.Hkv, turn, 0, k_stride, d, 0, 0, 0, kv32},
-                          {v_new, nullptr, p->pl.Hkv, 0, 0, v_stride, d, 0, 0, 0, kv32}};
   const PagedBatch pb = device_batch(batch);
-  cudaError_t e = launch_rope(rope ? rope->t : none, positions, 1, batch->total_new, g, 3, &pb, &p->pl, p->k_pages, p->v_pages, 0, (cudaStream_t)stream);
+  cudaError_t e;
+  if (p->pages.type == kPagesE4m3 || normed) {
+    const StoreGroups g{q, k_new, v_new, q_out, q_stride, k_stride, v_stride, q_out_stride, q32, kv32, norm ? norm->q_weight : nullptr,
+                        norm ? norm->k_weight : nullptr, norm ? norm->eps : 0.f, positions};
+    e = launch_store(rope ? &rope->t : nullptr, g, pb, p->pl, p->pages, (cudaStream_t)stream);
+  } else {
+    RopeTable none;
+    if (!rope) {
+      memset(&none, 0, sizeof(none));
+      none.dim = d;
+    }
+    const RopeGroup g[3] = {{q, q_out, q ? p->pl.Hq : 0, turn, 0, q_stride, d, 0, q_out_stride, d, q32},
+                            {k_new, nullptr, p->pl.Hkv, turn, 0, k_stride, d, 0, 0, 0, kv32},
+                            {v_new, nullptr, p->pl.Hkv, 0, 0, v_stride, d, 0, 0, 0, kv32}};
+    e = launch_rope(rope ? rope->t : none, positions, 1, batch->total_new, g, 3, &pb, &p->pl, p->pages.k, p->pages.v, 0, (cudaStream_t)stream);
+  }
   return e == cudaSuccess ? SPLA_OK : cuda_fail(e, "spla_paged_append");
+}
+
+extern "C" int spla_paged_append(spla_paged_t* p, const spla_paged_batch_t* batch, const spla_rope_t* rope, const int32_t* positions,
+                                 const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const void* q, int64_t q_stride,
+                                 void* q_out, int64_t q_out_stride, void* stream) {
+  return spla_paged_append_norm(p, batch, rope, positions, nullptr, k_new, k_stride, v_new, v_stride, q, q_stride, q_out, q_out_stride, stream);
+}
+
+extern "C" int spla_paged_read(spla_paged_t* p, const spla_paged_batch_t* batch, void* k_out, void* v_out, int32_t out_dtype, void* stream) {
+  const int rc = check_batch(p, batch, true);
+  if (rc != SPLA_OK) return rc;
+  if (!k_out || !v_out || !is_dtype(out_dtype) || !aligned(k_out, 16) || !aligned(v_out, 16)) return SPLA_ERR_INVALID_ARG;
+  cudaError_t e = launch_read(device_batch(batch), p->pl, p->pages, k_out, v_out, out_dtype == SPLA_F32, (cudaStream_t)stream);
+  return e == cudaSuccess ? SPLA_OK : cuda_fail(e, "spla_paged_read");
 }
 
 // The plan of one launch (a batch of at most kPagedMaxBatch sequences), the bytes of its partial results and of the sums of long walks,
@@ -245,8 +347,8 @@ extern "C" int spla_paged_query_workspace(const spla_paged_t* p, const spla_page
   return SPLA_OK;
 }
 
-extern "C" int spla_paged_attend(spla_paged_t* p, const spla_paged_batch_t* batch, const void* q, int64_t q_stride,
-                                 const spla_paged_mask_t* mask, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t* batch, const void* q, int64_t q_stride, const spla_paged_mask_t* mask,
+                                       int32_t sinks, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
   const int rc = check_batch(p, batch, true);
   if (rc != SPLA_OK) return rc;
   const int qe = dtype_bytes(p->cfg.q_dtype);
@@ -261,6 +363,8 @@ extern "C" int spla_paged_attend(spla_paged_t* p, const spla_paged_batch_t* batc
   if (!(mask->softcap >= 0.f) || !isfinite(mask->softcap) || (mask->softcap > 0.f && mask->softcap < 1e-6f) || mask->window < 0) return SPLA_ERR_INVALID_ARG;
   if ((mask->slopes && !aligned(mask->slopes, 4)) || (mask->first_key && !aligned(mask->first_key, 4)) || (mask->prefix_lens && !aligned(mask->prefix_lens, 4)))
     return SPLA_ERR_INVALID_ARG;
+  if (sinks < 0) return SPLA_ERR_INVALID_ARG;
+  if (sinks > 0 && mask->first_key) return SPLA_ERR_UNSUPPORTED;                   // (which document's first tokens?)
   size_t need = 0;
   spla_paged_query_workspace(p, batch, &need);
   if (need && (!workspace || workspace_bytes < need)) return SPLA_ERR_INVALID_ARG;
@@ -274,12 +378,15 @@ extern "C" int spla_paged_attend(spla_paged_t* p, const spla_paged_batch_t* batc
   a.sm_scale = p->cfg.sm_scale;
   a.softcap = mask->softcap;
   a.window = mask->window;
+  a.sinks = mask->window > 0 ? sinks : 0;
   a.slopes = mask->slopes;
   a.first_key = mask->first_key;
   a.wait_limit = p->wait_limit;
   a.dbg_tx_extra = p->dbg_tx_extra;
   const PagedBatch pb = device_batch(batch);
-  const int q16 = p->cfg.q_dtype == SPLA_BF16, kv16 = p->cfg.kv_dtype == SPLA_BF16;
+  a.k_scales = p->pages.k_scales;
+  a.v_scales = p->pages.v_scales;
+  const int q16 = p->cfg.q_dtype == SPLA_BF16;
   cudaStream_t s = (cudaStream_t)stream;
   cudaError_t e = cudaSuccess;
   PagedMaps maps;
@@ -293,10 +400,15 @@ extern "C" int spla_paged_attend(spla_paged_t* p, const spla_paged_batch_t* batc
     a.prefix = mask->prefix_lens ? mask->prefix_lens + first : nullptr;
     a.w = PagedWork{};
     plan_attend(p, a.pb, tensor, &a.w, workspace);
-    e = tensor ? launch_paged_mma(a, maps, s) : launch_paged_general(a, p->k_pages, p->v_pages, q16, kv16, s);
+    e = tensor ? launch_paged_mma(a, maps, s) : launch_paged_general(a, p->pages, q16, s);
     if (e == cudaSuccess) e = launch_paged_join(a, q16, s);
   }
   return e == cudaSuccess ? SPLA_OK : cuda_fail(e, "spla_paged_attend");
+}
+
+extern "C" int spla_paged_attend(spla_paged_t* p, const spla_paged_batch_t* batch, const void* q, int64_t q_stride,
+                                 const spla_paged_mask_t* mask, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  return spla_paged_attend_sinks(p, batch, q, q_stride, mask, 0, out, lse, workspace, workspace_bytes, stream);
 }
 
 extern "C" int spla_paged_sync_status(spla_paged_t* p, void* stream) {

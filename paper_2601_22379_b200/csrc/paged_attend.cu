@@ -12,6 +12,8 @@
 // asynchronously, 1.05 GB in 1.20 ms), 16 by shared memory's reads for the scores (G = 8, the same cache: 523 us), 64 by the FMA pipe, in use half
 // of the time: the phases of a tile alternate with barriers (300 tokens on 3000 x 4, 32 heads of 128: 1.54 ms, 36 TFLOP/s; tiles of 32
 // keys with P beside K are 9 % slower, row tiles of 128 in one CTA of 512 threads, or with eight rows per thread, within 7 %).
+#include <cuda_fp8.h>
+
 #include "paged.h"
 
 namespace spla {
@@ -45,6 +47,14 @@ __device__ __forceinline__ void copies_close() { asm volatile("cp.async.commit_g
 template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+// Four e4m3 values (of 8-bit pages) times their scale.
+using E4m3 = unsigned char;
+__device__ __forceinline__ float4 load4(const E4m3* p, float mul) {
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+  const float2 a = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffffu), __NV_E4M3)));
+  const float2 b = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3)));
+  return make_float4(a.x * mul, a.y * mul, b.x * mul, b.y * mul);
+}
 template <typename T>
 __device__ __forceinline__ float4 load4(const T* p) {
   float v[4];
@@ -90,9 +100,10 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
   while (wk.next(a, seqs)) {
     const int i0 = wk.first_pos(a.w), rows = min(wk.n - i0, wk.n_pos(a.w)) * G;
     const int pos0 = wk.L - wk.n + i0;
+    auto first_tok = [&](int t) { return (t < wk.ns ? t : t + wk.skip) * TK; };
     auto find_rows = [&](int t) {                                  // a few threads: where tile t lies
       if (tid < TK / 16 && t < wk.t1) {
-        const int tok = t * TK + tid * 16;
+        const int tok = first_tok(t) + tid * 16;
         long long row = -1;
         if (tok < wk.L) {
           row = paged_row(a.pb, a.pl, wk.b, wk.h, tok >> a.pl.log_p);
@@ -101,14 +112,17 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
         rows_s[(t & 1) * (TK / 16) + tid] = row;
       }
     };
-    auto fetch = [&](const TKV* pages, float* to, int ld, int t) { // one tile of K or V
+    auto fetch = [&](const TKV* pages, const unsigned char* scales, float* to, int ld, int t) { // one tile of K or V
+      const int tok0 = first_tok(t);
 #pragma unroll
       for (int x0 = 0; x0 < TK * D4; x0 += THREADS) {
         const int x = x0 + tid, j = x / D4, c = x % D4;
         const long long row = rows_s[(t & 1) * (TK / 16) + j / 16];
-        const bool there = row >= 0 && t * TK + j < wk.L;
+        const bool there = row >= 0 && tok0 + j < wk.L;
         const TKV* from = pages + (there ? (row + j % 16) * D + c * 4 : 0);
         if constexpr (sizeof(TKV) == 4) copy16(to + j * ld + c * 4, from, there);
+        else if constexpr (sizeof(TKV) == 1)
+          *reinterpret_cast<float4*>(to + j * ld + c * 4) = there ? load4(from, paged_scale(scales, row + j % 16)) : make_float4(0.f, 0.f, 0.f, 0.f);
         else *reinterpret_cast<float4*>(to + j * ld + c * 4) = there ? load4(from) : make_float4(0.f, 0.f, 0.f, 0.f);
       }
       copies_close();
@@ -131,7 +145,7 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
       if (tid < rows) s = paged_sees(a, wk.row0, wk.n, wk.L, wk.prefix, i0 + tid / G);
       lo_s[tid] = s.lo;
       hi_s[tid] = s.hi;
-      sees_any = s.lo < s.hi;
+      sees_any = s.lo < s.hi || (s.hi > 0 && a.sinks > 0);
     }
     // a warp whose rows are all behind the unit's last has nothing to compute (its rows of scores and of the product are the same)
     const bool idle = tid / 32 * 32 / (CS * (TK / KT)) * 4 >= rows;
@@ -162,8 +176,8 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
         }
       }
       if (sees_any) {
-        t_from = max(t_from, lo / TK);
-        t_to = min(t_to, (hi + TK - 1) / TK);
+        t_from = max(t_from, a.sinks > 0 ? 0 : lo / TK);
+        t_to = min(t_to, (hi + TK - 1) / TK - wk.skip);
       }
     }
     if (t_from < t_to) {
@@ -171,12 +185,12 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
         find_rows(t_from);
         __syncthreads();
       }
-      fetch(k_pages, ks, LD, t_from);
-      fetch(v_pages, vs, D, t_from);
+      fetch(k_pages, a.k_scales, ks, LD, t_from);
+      fetch(v_pages, a.v_scales, vs, D, t_from);
     }
 #pragma unroll 1
     for (int t = t_from; t < t_to; ++t) {
-      const int tok0 = t * TK;
+      const int tok0 = first_tok(t), sinks = a.sinks;
       const bool part = tok0 < all_lo || tok0 + TK > all_hi;       // some row does not see all of it
       find_rows(t + 1);
       copies_wait<1>();                                            // K is here
@@ -220,7 +234,7 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
             if (a.softcap > 0.f) v = a.softcap * tanhf(v * inv_cap);
             const int j = tok0 + kg + y * (TK / KT);
             if (slope[i] != 0.f) v -= slope[i] * (float)abs(pos - j);
-            s[i][y] = !part || (j >= lo_s[r] && j < hi_s[r]) ? v * kLog2e : -INFINITY;
+            s[i][y] = !part || ((j >= lo_s[r] || j < sinks) && j < hi_s[r]) ? v * kLog2e : -INFINITY;
             mt[i] = fmaxf(mt[i], s[i][y]);
           }
         }
@@ -236,7 +250,7 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
       }
       __syncthreads();                                             // (K is used up; the maxima; where the next tile lies)
       if constexpr (!S::OVER) {
-        if (t + 1 < t_to) fetch(k_pages, ks, LD, t + 1); else copies_close();
+        if (t + 1 < t_to) fetch(k_pages, a.k_scales, ks, LD, t + 1); else copies_close();
       }
       if (!idle) {
         if constexpr (W > 1) {
@@ -306,7 +320,7 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int r = rp * 4 + i;
-              if (tok0 + j < lo_s[r] || tok0 + j >= hi_s[r]) continue;
+              if ((tok0 + j < lo_s[r] && tok0 + j >= sinks) || tok0 + j >= hi_s[r]) continue;
 #pragma unroll
               for (int x = 0; x < CW; ++x) o[i][x] = fmaf(ps[r * LP + j], vs[j * D + x / 4 * (D * 4 / CW) + cg * 4 + x % 4], o[i][x]);
             }
@@ -314,8 +328,8 @@ __global__ void __launch_bounds__((PgShape<R, D>::THREADS), 2)
       }
       __syncthreads();                                             // (V and P are used up)
       if (t + 1 < t_to) {
-        if constexpr (S::OVER) fetch(k_pages, ks, LD, t + 1);
-        fetch(v_pages, vs, D, t + 1);
+        if constexpr (S::OVER) fetch(k_pages, a.k_scales, ks, LD, t + 1);
+        fetch(v_pages, a.v_scales, vs, D, t + 1);
       } else {
         copies_close();
       }
@@ -524,9 +538,11 @@ void paged_plan_general(PagedWork* w, const PagedBatch& pb, const PagedLayout& p
   w->rows = (pb.max_new < w->upos ? pb.max_new : w->upos) * pl.G;
 }
 
-cudaError_t launch_paged_general(const PagedAttend& a, const void* k, const void* v, int q_bf16, int kv_bf16, cudaStream_t s) {
-  if (q_bf16) return kv_bf16 ? general_dim<__nv_bfloat16, __nv_bfloat16>(a, k, v, s) : general_dim<__nv_bfloat16, float>(a, k, v, s);
-  return kv_bf16 ? general_dim<float, __nv_bfloat16>(a, k, v, s) : general_dim<float, float>(a, k, v, s);
+cudaError_t launch_paged_general(const PagedAttend& a, const PagedPages& pages, int q_bf16, cudaStream_t s) {
+  const void *k = pages.k, *v = pages.v;
+  if (pages.type == kPagesE4m3) return q_bf16 ? general_dim<__nv_bfloat16, E4m3>(a, k, v, s) : general_dim<float, E4m3>(a, k, v, s);
+  if (pages.type == kPagesBf16) return q_bf16 ? general_dim<__nv_bfloat16, __nv_bfloat16>(a, k, v, s) : general_dim<float, __nv_bfloat16>(a, k, v, s);
+  return q_bf16 ? general_dim<__nv_bfloat16, float>(a, k, v, s) : general_dim<float, float>(a, k, v, s);
 }
 
 cudaError_t launch_paged_join(const PagedAttend& a, int out_bf16, cudaStream_t s) {

@@ -57,7 +57,7 @@ struct PmSmem {
   static constexpr int kQ = 0, kK = kQ + (FEW ? 1 : 2) * kTile, kV = kK + NK * kTile, kSeqs = kV + NV * kTile;
   static constexpr int kMl = kSeqs + (int)((sizeof(PagedSeqs) + 15) / 16 * 16);   // float2 [128]: maximum and sum of the second half, of a quarter
   static constexpr int kSegs = kMl + 128 * 8;                     // PmSeg [4]: the segments that come next
-  static constexpr int kStage = kSegs + 4 * 96;                   // [8 warps][32 rows][64 + 16 bytes], FEW [4 warps][8 rows][512 + 16] or fewer columns of more rows: rows on their way out
+  static constexpr int kStage = kSegs + 4 * 112;                   // [8 warps][32 rows][64 + 16 bytes], FEW [4 warps][8 rows][512 + 16] or fewer columns of more rows: rows on their way out
   static constexpr int kStageRow = 80;
   static constexpr int kBars = kStage + 8 * 32 * 80;
   static constexpr int kNumBars = 2 * NK + 2 * NV + 15 + 8;
@@ -102,11 +102,12 @@ __device__ __forceinline__ void pm_row_tile(const PagedAttend& a, const PagedWal
     lo = __reduce_min_sync(0xffffffffu, least);
     all_lo = __reduce_max_sync(0xffffffffu, most);
   }
-  if (lo >= hi) return;
-  ta = max(wk.t0, lo / kPmKeys);
-  te = max(ta, min(wk.t1, (hi + kPmKeys - 1) / kPmKeys));
-  la = all_lo / kPmKeys + (all_lo % kPmKeys != 0);
-  le = all_hi / kPmKeys;
+  if (lo >= hi && a.sinks == 0) return;
+  // (numbers without the tiles between the sinks' and the window's; those of the sinks are partly seen)
+  ta = max(wk.t0, a.sinks > 0 ? 0 : lo / kPmKeys);
+  te = max(ta, min(wk.t1, (hi + kPmKeys - 1) / kPmKeys - wk.skip));
+  la = all_lo / kPmKeys + (all_lo % kPmKeys != 0) - wk.skip;
+  le = all_hi / kPmKeys - wk.skip;
 }
 __device__ __forceinline__ PmPlan pm_plan(const PagedAttend& a, const PagedWalk& wk, int lane) {
   PmPlan p;
@@ -124,10 +125,11 @@ __device__ __forceinline__ PmPlan pm_plan(const PagedAttend& a, const PagedWalk&
 struct PmSeg {
   PmPlan pl;
   int b, h, row0, n, L, prefix, first;             // first: its first new token, in the sequence
+  int ns, skip;                                    // see PagedSpan
   bool head, tail, end;                            // end: none is left
 };
 constexpr int kPmSegs = 4;
-static_assert(sizeof(PmSeg) <= 96, "a segment's place");
+static_assert(sizeof(PmSeg) <= 112, "a segment's place");
 
 // Warp-uniform bounded wait that also ends when another role has given up.
 __device__ __forceinline__ bool pm_wait_slow(uint64_t* bar, uint32_t parity, int limit, volatile int* abort_flag) {
@@ -301,10 +303,10 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       each_segment(ok, [&](const PmSeg& sg) {
         const PmPlan pl = sg.pl;
         if (pl.A >= pl.E) return true;
-        const int L = sg.L, b = sg.b, h = sg.h;
+        const int L = sg.L, b = sg.b, h = sg.h, ns = sg.ns, skip = sg.skip;
         // row of this lane's box in tile t; loaded a tile ahead
         auto box_row = [&](int t) {
-          const int index = t * npg + pg;
+          const int index = (t < ns ? t : t + skip) * npg + pg;
           long long r = -1;
           if (lane < boxes && t < pl.E && index * P < L) r = paged_row(a.pb, a.pl, b, h, index);
           return r < 0 ? n_rows : (int)r;
@@ -443,6 +445,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
             sg.b = wk.b; sg.h = wk.h; sg.row0 = wk.row0; sg.n = wk.n; sg.L = wk.L; sg.prefix = wk.prefix;
             sg.first = wk.first_pos(a.w);
             sg.head = wk.head; sg.tail = wk.tail;
+            sg.ns = wk.ns; sg.skip = wk.skip;
           }
           segs[i % kPmSegs] = sg;
           mbar_arrive1(&seg_full[i % kPmSegs]);
@@ -497,9 +500,10 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       const int lo_most = __reduce_max_sync(0xffffffffu, counts ? see.lo : 0), hi_least = __reduce_min_sync(0xffffffffu, counts ? see.hi : 0x7fffffff);
       float m = -INFINITY, l = 0.f, fd = 1.f;                      // fd: what the sums of drained tiles are behind the maximum
       int done_items = 0;
+      const int ns = sg.ns, skip = sg.skip, sinks = a.sinks;
 #pragma unroll 1
       for (; t < t_end; t += t_step) {
-        const int tok0 = t * kPmKeys, st = (uint32_t)(k_base + t) % NV;
+        const int tok0 = (t < ns ? t : t + skip) * kPmKeys, st = (uint32_t)(k_base + t) % NV;
         const bool look = t < la || t >= le;
         bool simt = false;
         if (!pm_wait(&s_full[slot], n & 1, lim, abort_flag)) return false;
@@ -521,7 +525,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           if (alike) {
             const int from = lo_most - tok0, to = hi_least - tok0;
             for (int j = thr >> 3; j < kPmKeys; j += 16)           // a row of 128 bytes by eight threads
-              if (j < from || j >= to) {
+              if ((j < from && tok0 + j >= sinks) || j >= to) {
 #pragma unroll
                 for (int x = 0; x < H; ++x) *reinterpret_cast<uint4*>(vt + x * SM::kHalf + j * 128 + (thr & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
               }
@@ -612,7 +616,8 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           if (part) {
 #pragma unroll
             for (int c = 0; c < KEYS / 32; ++c) {
-              const uint32_t bits = bits_between(see.lo - key0 - 32 * c, see.hi - key0 - 32 * c);
+              const int c0 = key0 + 32 * c;
+              const uint32_t bits = bits_between(see.lo - c0, see.hi - c0) | bits_between(-c0, min(sinks, see.hi) - c0);
 #pragma unroll
               for (int x = 0; x < 32; ++x)
                 if (!(bits & (1u << x))) r[32 * c + x] = 0xff800000u;
@@ -684,7 +689,8 @@ __global__ void __launch_bounds__(kPmThreads, 1)
               uint32_t pw[16];
               tmem_ld16_async(tS + 16 * w, pw);
               tmem_ld_wait16(pw);
-              const uint32_t bits = valid ? bits_between(see.lo - tok0 - 32 * w, see.hi - tok0 - 32 * w) : 0u;
+              const int c0 = tok0 + 32 * w;
+              const uint32_t bits = valid ? bits_between(see.lo - c0, see.hi - c0) | bits_between(-c0, min(sinks, see.hi) - c0) : 0u;
 #pragma unroll
               for (int y = 0; y < 32; ++y) {
                 if (!(bits & (1u << y))) continue;

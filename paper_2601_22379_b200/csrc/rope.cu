@@ -8,7 +8,7 @@
 // 6.0 TB/s, 0.92 of a copy's rate, one channel at a time, VEC = 1, 369; small calls by a launch: 8 tokens 2.2 us).  The first rows' loads are
 // issued before the tokens' places and the sines are known (175 -> 115 us with bases once per token, no 64-bit divisions; 115 -> 110 with
 // the loads first).
-#include "paged.h"
+#include "rope_device.cuh"
 
 namespace spla {
 
@@ -32,56 +32,6 @@ struct RopeLaunch {
   PagedLayout pl;
   void *k_pages, *v_pages;
 };
-
-// VEC channels as they lie: VEC x sizeof(T) = 16 bytes, or one channel.
-__device__ __forceinline__ void load_raw(const void* p, uint32_t (&w)[4]) {
-  const uint4 v = *reinterpret_cast<const uint4*>(p);
-  w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-}
-__device__ __forceinline__ void load_raw(const float* p, uint32_t (&w)[1]) { w[0] = *reinterpret_cast<const uint32_t*>(p); }
-__device__ __forceinline__ void load_raw(const __nv_bfloat16* p, uint32_t (&w)[1]) { w[0] = *reinterpret_cast<const uint16_t*>(p); }
-template <typename T, int VEC, int W>
-__device__ __forceinline__ void unpack(const uint32_t (&w)[W], float (&x)[VEC]) {
-  if constexpr (sizeof(T) == 4) {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) x[i] = __uint_as_float(w[i]);
-  } else if constexpr (VEC == 1) {
-    x[0] = bf16_lo(w[0]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) x[i] = i % 2 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
-  }
-}
-template <int VEC>
-__device__ __forceinline__ void store_piece(float* p, const float (&x)[VEC]) {
-  if constexpr (VEC == 4) {
-    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) p[i] = x[i];
-  }
-}
-template <int VEC>
-__device__ __forceinline__ void store_piece(__nv_bfloat16* p, const float (&x)[VEC]) {
-  if constexpr (VEC == 8) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) p[i] = __float2bfloat16_rn(x[i]);
-  }
-}
-
-// Angle of a position: sine and cosine of 2 pi frac(position x freq).
-__device__ __forceinline__ float2 turn_of(unsigned long long freq, int position, float amplitude, bool back) {
-  const unsigned long long phase = (unsigned long long)(long long)position * freq;
-  const float half_turns = (float)(int)(phase >> 32) * (1.f / 2147483648.f);       // [-1, 1]
-  float s, c;
-  sincospif(half_turns, &s, &c);
-  return make_float2(c * amplitude, (back ? -s : s) * amplitude);
-}
 
 // VEC pairs per piece; both element types may occur in one launch with VEC = 1 only.
 template <typename T, int VEC>
@@ -193,21 +143,7 @@ __global__ void __launch_bounds__(kRopeThreads, sizeof(T) == 4 ? 5 : 4)
         a[0] = x * cs.x - y * cs.y;
         b[0] = y * cs.x + x * cs.y;
       } else {
-        const float4* tab = reinterpret_cast<const float4*>(table + pl.t * pairs) + piece;
-#pragma unroll
-        for (int j = 0; j < VEC / 2; ++j) {
-          const float4 cs = tab[j * rot_pieces];
-          if (rt.interleaved) {                            // a then b hold neighbouring pairs (x, y), (x, y), ...
-            float* v = 4 * j < VEC ? a + 4 * j : b + 4 * j - VEC;
-            const float x0 = v[0], y0 = v[1], x1 = v[2], y1 = v[3];
-            v[0] = x0 * cs.x - y0 * cs.y; v[1] = y0 * cs.x + x0 * cs.y;
-            v[2] = x1 * cs.z - y1 * cs.w; v[3] = y1 * cs.z + x1 * cs.w;
-          } else {
-            const float x0 = a[2 * j], y0 = b[2 * j], x1 = a[2 * j + 1], y1 = b[2 * j + 1];
-            a[2 * j] = x0 * cs.x - y0 * cs.y; b[2 * j] = y0 * cs.x + x0 * cs.y;
-            a[2 * j + 1] = x1 * cs.z - y1 * cs.w; b[2 * j + 1] = y1 * cs.z + x1 * cs.w;
-          }
-        }
+        turn_piece<VEC>(a, b, reinterpret_cast<const float4*>(table + pl.t * pairs) + piece, rot_pieces, rt.interleaved);
       }
     }
     store_piece<VEC>(out + ca, a);
