@@ -174,7 +174,7 @@ struct PagedAttend {
   int wait_limit, dbg_tx_extra;         // as in Params
   int sinks;                            // so many first tokens are visible besides the window
   int from_new, to_new;                 // sequences of so many new tokens are this launch's (0, 0: all of them); the others are passed over
-  const unsigned char *k_scales, *v_scales;   // of 8-bit pages
+  const unsigned char *k_bytes, *v_bytes, *k_scales, *v_scales;   // 8-bit pages
 };
 
 // Sequence table of a CTA, in shared memory.
@@ -475,10 +475,16 @@ cudaError_t launch_norm(const RopeTable& rt, const int* positions, int batch, in
 void paged_plan_general(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int sm_count);
 cudaError_t launch_paged_general(const PagedAttend& a, const PagedPages& pages, int q_bf16, cudaStream_t s);
 cudaError_t launch_paged_join(const PagedAttend& a, int out_bf16, cudaStream_t s);
+// paged_few.cu: 8-bit pages, bf16 queries, at most 16 rows per sequence and KV head
+int paged_few_positions(const PagedLayout& pl);   // new tokens of a sequence that it takes, at most
+void paged_plan_few(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int sm_count);
+cudaError_t launch_paged_few(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s);
 // paged_mma.cu: bf16 on tcgen05
 size_t paged_mma_drain_bytes(const PagedWork& w, const PagedBatch& pb, const PagedLayout& pl);
 int paged_mma_positions(const PagedBatch& pb, const PagedLayout& pl);   // new tokens of a row tile: the query boxes' size
 void paged_plan_mma(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int sm_count);
 cudaError_t launch_paged_mma(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s);
+cudaError_t launch_paged_mma_bytes64(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s);    // ... and over 8-bit pages
+cudaError_t launch_paged_mma_bytes128(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s);
 
 }  // namespace spla

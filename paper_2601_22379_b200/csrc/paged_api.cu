@@ -20,6 +20,7 @@ struct spla_paged {
   PagedPages pages;
   PagedMaps maps;
   bool tensor;                          // bf16 cache and queries, tensor maps made: the tensor-core kernel serves it
+  bool few;                             // 8-bit pages and bf16 queries, maps made: paged_few.cu serves sequences of few rows, the tensor-core kernel the others
   int sm_count;
   int wait_limit, dbg_tx_extra;
 };
@@ -198,6 +199,9 @@ static int create_paged(const spla_paged_config_t* c, void* k_pages, void* v_pag
   const int64_t rows = (c->n_pages - 1) * ps + (c->n_kv_heads - 1) * hs + P;
   p->tensor = !k_scales && c->kv_dtype == SPLA_BF16 && c->q_dtype == SPLA_BF16 && !(c->flags & SPLA_GENERAL_KERNELS) && rows < (1ll << 31) - 256 &&
               make_kv_map(p->maps.k, k_pages, c->head_dim, P, rows) && make_kv_map(p->maps.v, v_pages, c->head_dim, P, rows);
+  // (scales of 2^60 and more would leave the range that its exponents are kept in)
+  p->few = k_scales && c->q_dtype == SPLA_BF16 && !(c->flags & SPLA_GENERAL_KERNELS) && rows < (1ll << 31) - 256 && p->cfg.sm_scale < 1.15e18f &&
+           make_byte_map(p->maps.k, k_pages, c->head_dim, P, rows) && make_byte_map(p->maps.v, v_pages, c->head_dim, P, rows);
   *paged_out = p;
   return SPLA_OK;
 }
@@ -286,10 +290,16 @@ extern "C" int spla_paged_read(spla_paged_t* p, const spla_paged_batch_t* batch,
   return e == cudaSuccess ? SPLA_OK : cuda_fail(e, "spla_paged_read");
 }
 
+// Which kernel a launch is: fp32 arithmetic, bf16 on the tensor cores, 8-bit pages with few rows, 8-bit pages on the tensor cores.
+enum PagedKernel { kGeneral, kTensor, kFew, kTensorBytes };
+
 // The plan of one launch (a batch of at most kPagedMaxBatch sequences), the bytes of its partial results and of the sums of long walks,
 // and their places in the workspace, where there is one (no cuts: whole units only).
-static size_t plan_attend(const spla_paged* p, const PagedBatch& pb, bool tensor, PagedWork* w, void* workspace) {
+static size_t plan_attend(const spla_paged* p, PagedBatch pb, PagedKernel kernel, PagedWork* w, void* workspace) {
+  const bool tensor = kernel == kTensor || kernel == kTensorBytes;
+  if (kernel == kFew && pb.max_new > paged_few_positions(p->pl)) pb.max_new = paged_few_positions(p->pl);   // (the others are another launch's)
   if (tensor) paged_plan_mma(w, pb, p->pl, p->sm_count);
+  else if (kernel == kFew) paged_plan_few(w, pb, p->pl, p->sm_count);
   else paged_plan_general(w, pb, p->pl, p->sm_count);
   size_t used = 0;
   auto take = [&](size_t bytes) {
@@ -337,9 +347,10 @@ extern "C" int spla_paged_query_workspace(const spla_paged_t* p, const spla_page
   for (int first = 0; first < batch->batch; first += kPagedMaxBatch) {
     PagedBatch part = pb;
     part.batch = pb.batch - first < kPagedMaxBatch ? pb.batch - first : kPagedMaxBatch;
-    for (int tensor = 0; tensor <= (p->tensor ? 1 : 0); ++tensor) {   // (queries that TMA does not take go to the general kernel)
+    for (PagedKernel kernel : {kGeneral, kTensor, kFew, kTensorBytes}) {   // (queries that TMA does not take go to the general kernel)
+      if ((kernel == kTensor && !p->tensor) || ((kernel == kFew || kernel == kTensorBytes) && !p->few)) continue;
       PagedWork w = {};
-      const size_t n = plan_attend(p, part, tensor != 0, &w, nullptr);
+      const size_t n = plan_attend(p, part, kernel, &w, nullptr);
       if (n > most) most = n;
     }
   }
@@ -384,24 +395,45 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
   a.wait_limit = p->wait_limit;
   a.dbg_tx_extra = p->dbg_tx_extra;
   const PagedBatch pb = device_batch(batch);
+  a.k_bytes = reinterpret_cast<const unsigned char*>(p->pages.k);
+  a.v_bytes = reinterpret_cast<const unsigned char*>(p->pages.v);
   a.k_scales = p->pages.k_scales;
   a.v_scales = p->pages.v_scales;
   const int q16 = p->cfg.q_dtype == SPLA_BF16;
   cudaStream_t s = (cudaStream_t)stream;
   cudaError_t e = cudaSuccess;
   PagedMaps maps;
-  const bool tensor = p->tensor && aligned(q, 16) && q_stride % 8 == 0 && cap_fits(p->cfg.sm_scale, mask->softcap) && make_q_map(maps.q, q, p->pl, q_stride, pb);
-  if (tensor) {
+  const bool rows16 = aligned(q, 16) && q_stride % 8 == 0, few = p->few && rows16;
+  const bool tensor = (p->tensor || (few && pb.max_new > paged_few_positions(p->pl))) && rows16 && cap_fits(p->cfg.sm_scale, mask->softcap) &&
+                      make_q_map(maps.q, q, p->pl, q_stride, pb);
+  if (tensor || few) {
     memcpy(maps.k, p->maps.k, sizeof(maps.k));
     memcpy(maps.v, p->maps.v, sizeof(maps.v));
   }
+  auto launch = [&](PagedKernel kernel, int from_new, int to_new) {
+    if (e != cudaSuccess) return;
+    a.from_new = from_new;
+    a.to_new = to_new;
+    a.w = PagedWork{};
+    plan_attend(p, a.pb, kernel, &a.w, workspace);
+    switch (kernel) {
+      case kTensor: e = launch_paged_mma(a, maps, s); break;
+      case kFew: e = launch_paged_few(a, maps, s); break;
+      case kTensorBytes: e = p->pl.d == 128 ? launch_paged_mma_bytes128(a, maps, s) : launch_paged_mma_bytes64(a, maps, s); break;
+      default: e = launch_paged_general(a, p->pages, q16, s);
+    }
+    if (e == cudaSuccess) e = launch_paged_join(a, q16, s);
+  };
   for (int first = 0; first < batch->batch && e == cudaSuccess; first += kPagedMaxBatch) {
     a.pb = part_of(pb, first);
     a.prefix = mask->prefix_lens ? mask->prefix_lens + first : nullptr;
-    a.w = PagedWork{};
-    plan_attend(p, a.pb, tensor, &a.w, workspace);
-    e = tensor ? launch_paged_mma(a, maps, s) : launch_paged_general(a, p->pages, q16, s);
-    if (e == cudaSuccess) e = launch_paged_join(a, q16, s);
+    if (few) {                                                                     // two launches where a sequence may have more rows
+      const int most = paged_few_positions(p->pl);
+      launch(kFew, 0, most);
+      if (a.pb.max_new > most) launch(tensor ? kTensorBytes : kGeneral, most + 1, 0x7fffffff);
+    } else {
+      launch(tensor ? kTensor : kGeneral, 0, 0);
+    }
   }
   return e == cudaSuccess ? SPLA_OK : cuda_fail(e, "spla_paged_attend");
 }

@@ -1,0 +1,519 @@
+// Attention over 8-bit pages for few query rows (single tokens, and a few of them: at most 16 rows of positions x the G heads of a KV head).
+//
+//   s_j = 2^a 2^ek(j) (q' . k8_j),  x_j = s_j scale log2 e (cap, distance),  y_j = x_j + ev(j),
+//   w_j = 2^(y_j - m),  O += sum w_j v8_j,  l += sum w_j 2^-ev(j);  out = O / l,  lse = ln 2 (m + log2 l)
+//
+// The pages are read once and 8 bits at a time: that is what bounds such calls, so nothing else may take longer.  A tile of 128 tokens comes by TMA;
+// every one of eight warps takes the 16 tokens of it that share a scale, from shared memory straight into the fragments of mma.m16n8k16
+// (e4m3 is exact in fp16), rows of queries against tokens, and keeps its own running maximum, sum and output, which meet at the end of a
+// segment.  (tcgen05 would want the values widened in shared memory: four times the traffic there, and 128 rows for 16.)  Which channel is which of a
+// product's k, and which of its columns, is free: a lane takes 32 neighbouring bytes of a token of K, 16 of a token of V.
+// The scales never touch the values: K's multiply a warp's 16 scores, V's are exponents and go into that of the weights, so that the
+// weights of a row are all at most 2^15 whatever the blocks' scales are, and fp16 holds them to 2^-12 of themselves and 2^-40 of the largest.  Queries are
+// scaled by a power of two to below 2^15: fp16 holds bf16's eight bits down to 2^-28 of a row's largest channel.  Products are exact, sums fp32: each
+// tile's are started anew and added to O in fp32 (the tensor core truncates when it adds into an accumulator).
+//
+// Warps: 0 to 7 as above; 8 brings tiles, scales and queries; 9 plans the segments ahead (paged.h).  Waits are bounded as in the other kernels.  No multicast.
+// @figures
+#include <cuda_fp16.h>
+
+#include "paged_tiles.cuh"
+
+namespace spla {
+
+namespace {
+
+constexpr int kPfWarps = 8;                        // that compute
+constexpr int kPfThreads = 32 * (kPfWarps + 4);     // (whole groups of four warps, which share registers out: two of the last are idle)
+constexpr int kPfKeys = 128;                       // tokens of a tile: 16 for each warp
+constexpr int kPfRows = 16;
+constexpr int kPfSegs = 4;                         // segments planned ahead
+static_assert(kPfKeys == 16 * kPfWarps, "a block of a scale for each warp");
+
+struct PfSeg {
+  int b, h, row0, n, L, prefix;
+  int t0, t1, ns, skip;                            // key tiles
+  bool head, tail, end;
+};
+
+template <int D>
+struct PfSmem {
+  static constexpr int kTile = kPfKeys * D, NS = D == 128 ? 4 : 7;   // K and V of a stage: 2 kTile
+  static constexpr int kRing = 0, kMerge = NS * 2 * kTile;           // float [8 warps][16 rows][D]
+  static constexpr int kQ = kMerge + kPfWarps * kPfRows * D * 4;     // bf16 [kPfSegs][16][D]
+  static constexpr int kScales = kQ + kPfSegs * kPfRows * D * 2;     // int [NS][16]: exponents of K's blocks, of V's
+  static constexpr int kMl = kScales + NS * 64;                      // float2 [8][16]
+  static constexpr int kSegs = kMl + kPfWarps * kPfRows * 8;
+  static constexpr int kSeqs = kSegs + (kPfSegs * (int)sizeof(PfSeg) + 15) / 16 * 16;
+  static constexpr int kBars = kSeqs + ((int)sizeof(PagedSeqs) + 15) / 16 * 16;
+  static constexpr int kMisc = kBars + (2 * NS + 3 * kPfSegs + 2) * 8;
+  static constexpr int kBytes = kMisc + 16;
+  static_assert(kBytes <= 227 * 1024, "shared memory");
+};
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t has_nan8(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ uint32_t nan8_to_zero(uint32_t w) {
+  const uint32_t m = has_nan8(w) >> 7;             // 1 in the bytes that are NaN
+  return w & ~(m * 0xffu);
+}
+// 16-byte piece `c` of row `row` of a tile, as TMA's swizzle lays it.
+template <int D>
+__device__ __forceinline__ int piece_at(int row, int c) { return row * D + ((D == 128 ? c ^ (row & 7) : c ^ ((row >> 1) & 3)) << 4); }
+
+template <int D, bool MODS>
+__global__ void __launch_bounds__(kPfThreads, 1)
+    paged_few_kernel(const __grid_constant__ PagedAttend a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+  using SM = PfSmem<D>;
+  constexpr int NS = SM::NS, NT = D / 8;           // column tiles of the output
+  extern __shared__ __align__(1024) unsigned char smem[];
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + SM::kBars);
+  uint64_t *full = bars, *empty = full + NS, *seg_full = empty + NS, *seg_empty = seg_full + kPfSegs, *q_full = seg_empty + kPfSegs,
+           *merge_full = q_full + kPfSegs, *merge_free = merge_full + 1;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SM::kMisc);
+  PfSeg* segs = reinterpret_cast<PfSeg*>(smem + SM::kSegs);
+  PagedSeqs& seqs = *reinterpret_cast<PagedSeqs*>(smem + SM::kSeqs);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) {
+    for (int s = 0; s < NS; ++s) { mbar_init(&full[s], 1);  mbar_init(&empty[s], kPfWarps); }
+    for (int s = 0; s < kPfSegs; ++s) { mbar_init(&seg_full[s], 1);  mbar_init(&seg_empty[s], kPfWarps + 1);  mbar_init(&q_full[s], 1); }
+    mbar_init(merge_full, kPfWarps);
+    mbar_init(merge_free, kPfWarps);
+    mbar_init_done();
+    *abort_flag = 0;
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+  }
+  pdl_wait();
+  pdl_launch_dependents();
+  const long long share = paged_share(a.w, paged_fill_seqs(a, seqs, tid, kPfThreads));   // (ends with a barrier)
+  const int lim = a.wait_limit, G = a.pl.G;
+  bool ok = true;
+
+  if (warp >= kPfWarps) {
+  warpgroup_reg_dec<88>();                         // (88 + 2 x 208 = 3 x 168, what the CTA is launched with)
+  if (warp == kPfWarps + 1) {
+    // -------------------------------------------------------------- the share's segments, ahead of their use ----------------
+    PagedWalk wk;
+    bool more = wk.seek(a, seqs, blockIdx.x * share, share);
+    const int4 cut = a.w.cuts ? wk.cut_here(a, more, share) : make_int4(0, 0, 0, 0);
+#pragma unroll 1
+    for (int i = 0;; ++i) {
+      more = more && wk.next(a, seqs);
+      PfSeg sg;
+      if (more) {
+        sg.t0 = wk.t0; sg.t1 = wk.t1; sg.ns = wk.ns; sg.skip = wk.skip;
+        if (a.first_key) {                         // documents: from the first that a token sees on
+          int least = 0x7fffffff;
+          if (lane < wk.n) least = paged_sees(a, wk.row0, wk.n, wk.L, wk.prefix, lane).lo;
+          sg.t0 = min(sg.t1, max(sg.t0, __reduce_min_sync(0xffffffffu, least) / kPfKeys));
+        }
+      }
+      if (i >= kPfSegs && !pm_wait(&seg_empty[i % kPfSegs], (i / kPfSegs - 1) & 1, lim, abort_flag)) { ok = false; break; }
+      if (lane == 0) {
+        sg.end = !more;
+        if (more) {
+          sg.b = wk.b; sg.h = wk.h; sg.row0 = wk.row0; sg.n = wk.n; sg.L = wk.L; sg.prefix = wk.prefix;
+          sg.head = wk.head; sg.tail = wk.tail;
+        }
+        segs[i % kPfSegs] = sg;
+        mbar_arrive1(&seg_full[i % kPfSegs]);
+      }
+      __syncwarp();
+      if (!more) break;
+    }
+    if (a.w.cuts && lane == 0) a.w.cuts[blockIdx.x] = cut;
+  } else if (warp == kPfWarps) {
+    // -------------------------------------------------------------- tiles, scales, queries ----------------------------------
+    // Lane 16 v + i: K's (v = 0) or V's (v = 1) block i of a tile: its scale, and where it is the first of a page, the page's box.
+    const int i8 = lane & 15, is_v = lane >> 4, P = a.pl.P;
+    const bool mine = i8 < kPfKeys / 16, boxes = mine && (16 * i8 & (P - 1)) == 0;
+    const CUtensorMap* map = is_v ? &map_v : &map_k;
+    const unsigned char* scales = is_v ? a.v_scales : a.k_scales;
+    const uint32_t dst = smem_u32(smem) + SM::kRing + is_v * SM::kTile + 16 * i8 * D;
+    const int n_rows = (int)((long long)a.pl.n_pages * a.pl.page_stride);          // (a box there reads zeros)
+    int* sc_s = reinterpret_cast<int*>(smem + SM::kScales);
+    int kt = 0, i = 0;
+    for (; ok; ++i) {
+      const int slot = i % kPfSegs;
+      if (!pm_wait(&seg_full[slot], (i / kPfSegs) & 1, lim, abort_flag)) { ok = false; break; }
+      const PfSeg sg = segs[slot];
+      if (sg.end) break;
+      if (lane == 0) mbar_expect_tx(&q_full[slot], sg.n * G * D * 2 + (uint32_t)a.dbg_tx_extra);
+      __syncwarp();
+      if (lane < sg.n)
+        bulk_g2s(smem + SM::kQ + (slot * kPfRows + lane * G) * D * 2,
+                 reinterpret_cast<const __nv_bfloat16*>(a.q) + (sg.row0 + lane) * a.q_stride + (long long)sg.h * G * D, G * D * 2, &q_full[slot]);
+      auto find = [&](int t) {                     // cache row of this lane's block, -1: none
+        const int tok = (t < sg.ns ? t : t + sg.skip) * kPfKeys + 16 * i8;
+        if (!mine || t >= sg.t1 || tok >= sg.L) return -1;
+        const long long r = paged_row(a.pb, a.pl, sg.b, sg.h, tok >> a.pl.log_p);
+        return r < 0 ? -1 : (int)(r + (tok & (P - 1)));
+      };
+      auto scale = [&](int row) { return row < 0 ? 0 : paged_exponent(scales + (row >> 4)); };
+      int row = find(sg.t0), row1 = find(sg.t0 + 1), e = scale(row);
+#pragma unroll 1
+      for (int t = sg.t0; t < sg.t1; ++t) {
+        const int row2 = find(t + 2), e1 = scale(row1);            // (on their way while this tile's place gets free)
+        const int st = kt % NS;
+        if (kt >= NS && !pm_wait(&empty[st], ((kt / NS) - 1) & 1, lim, abort_flag)) { ok = false; break; }
+        if (mine) sc_s[st * 16 + is_v * 8 + i8] = e;
+        __syncwarp();
+        if (lane == 0) mbar_expect_tx(&full[st], 2 * SM::kTile + (uint32_t)a.dbg_tx_extra);
+        __syncwarp();
+        if (boxes) tma_load_box(dst + st * 2 * SM::kTile, map, 0, row < 0 ? n_rows : row, &full[st]);
+        ++kt;
+        row = row1;
+        row1 = row2;
+        e = e1;
+      }
+      if (!ok) { ++i; break; }                     // (its queries are on their way)
+      __syncwarp();
+      if (lane == 0) mbar_arrive1(&seg_empty[slot]);
+    }
+    if (!ok) *abort_flag = 1;
+    // every copy has landed before the CTA leaves, whatever the other roles do
+    for (int x = max(0, kt - NS); x < kt; ++x) warp_waits(&full[x % NS], (x / NS) & 1, lim);
+    for (int x = max(0, i - kPfSegs); x < i; ++x) warp_waits(&q_full[x % kPfSegs], (x / kPfSegs) & 1, lim);
+  }
+  } else {
+    // -------------------------------------------------------------- scores, weights, output ----------------------------------
+    warpgroup_reg_inc<208>();
+    const int g = lane >> 2, t4 = lane & 3;        // rows g and g + 8 of the queries; a column of K, of V; two columns of the results
+    const float sc2 = a.sm_scale * kLog2e;
+    const float cap = a.softcap, to_u = MODS && cap > 0.f ? 1.f / (cap * kLog2e) : 0.f;
+    const int* sc_s = reinterpret_cast<const int*>(smem + SM::kScales);
+    float2* ml_s = reinterpret_cast<float2*>(smem + SM::kMl);
+    float* merge = reinterpret_cast<float*>(smem + SM::kMerge);
+    int kt = 0;
+#pragma unroll 1
+    for (int i = 0; ok; ++i) {
+      const int slot = i % kPfSegs;
+      if (!pm_wait(&seg_full[slot], (i / kPfSegs) & 1, lim, abort_flag)) { ok = false; break; }
+      const PfSeg& sg = segs[slot];
+      if (sg.end) break;
+      const int rows = sg.n * G, t0 = sg.t0, t1 = sg.t1;
+      // what the rows see
+      PagedSees see[2];
+      float slope2[2];
+      int pos[2];
+      int lo_least = 0x7fffffff, lo_most = 0, hi_least = 0x7fffffff, hi_most = 0;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int r = g + 8 * x, pi = r / G;
+        see[x] = PagedSees{0x7fffffff, 0};
+        slope2[x] = 0.f;
+        pos[x] = sg.L - sg.n + pi;
+        if (r < rows) {
+          see[x] = paged_sees(a, sg.row0, sg.n, sg.L, sg.prefix, pi);
+          if (MODS && a.slopes) slope2[x] = __ldg(a.slopes + sg.h * G + r - pi * G) * kLog2e;
+          lo_least = min(lo_least, see[x].lo);
+          lo_most = max(lo_most, see[x].lo);
+          hi_least = min(hi_least, see[x].hi);
+          hi_most = max(hi_most, see[x].hi);
+        }
+      }
+      lo_least = __reduce_min_sync(0xffffffffu, lo_least);
+      lo_most = __reduce_max_sync(0xffffffffu, lo_most);
+      hi_least = __reduce_min_sync(0xffffffffu, hi_least);
+      hi_most = __reduce_max_sync(0xffffffffu, hi_most);
+      const int ns = sg.ns, skip = sg.skip, sinks = a.sinks;
+      const bool alike = sg.n == 1;
+      // queries as fragments: k-step j takes bytes 4 j .. of the lane's 32 (16) channels
+      uint32_t qf[D / 16][4];
+      int qe[2];
+      if (!pm_wait(&q_full[slot], (i / kPfSegs) & 1, lim, abort_flag)) { ok = false; break; }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int r = g + 8 * x;
+        uint32_t w[D / 8];
+        if (r < rows) {
+          const uint4* from = reinterpret_cast<const uint4*>(smem + SM::kQ + (slot * kPfRows + r) * D * 2 + t4 * (D / 2));
+#pragma unroll
+          for (int y = 0; y < D / 32; ++y) {
+            const uint4 v = from[y];
+            w[4 * y] = v.x; w[4 * y + 1] = v.y; w[4 * y + 2] = v.z; w[4 * y + 3] = v.w;
+          }
+        } else {
+#pragma unroll
+          for (int y = 0; y < D / 8; ++y) w[y] = 0u;
+        }
+        float top = 0.f;
+#pragma unroll
+        for (int y = 0; y < D / 8; ++y) {
+          const float lo = fabsf(bf16_lo(w[y])), hi = fabsf(bf16_hi(w[y]));
+          if (lo < INFINITY) top = fmaxf(top, lo);
+          if (hi < INFINITY) top = fmaxf(top, hi);
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        qe[x] = top > 0.f ? max((__float_as_int(top) >> 23) - 127 - 14, -100) : 0;
+        const float mul = power_of_two(-qe[x]);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+          qf[j][x] = pack_f16(bf16_lo(w[2 * j]) * mul, bf16_hi(w[2 * j]) * mul);
+          qf[j][2 + x] = pack_f16(bf16_lo(w[2 * j + 1]) * mul, bf16_hi(w[2 * j + 1]) * mul);
+        }
+      }
+      float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+      float o[NT][4];
+#pragma unroll
+      for (int x = 0; x < NT; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
+#pragma unroll 1
+      for (int t = t0; t < t1; ++t, ++kt) {
+        const int st = kt % NS, key0 = (t < ns ? t : t + skip) * kPfKeys + 16 * warp;
+        if (!pm_wait(&full[st], (kt / NS) & 1, lim, abort_flag)) { ok = false; break; }
+        if (key0 < hi_most && (key0 + 16 > lo_least || key0 < sinks)) {
+          const bool part = key0 < lo_most || key0 + 16 > hi_least;
+          const unsigned char *kt_s = smem + SM::kRing + st * 2 * SM::kTile, *vt_s = kt_s + SM::kTile;
+          const int ek = sc_s[st * 16 + warp], ev = sc_s[st * 16 + 8 + warp];
+          // ---- scores: two tiles of 8 tokens, the channels' sums in two parts
+          float s[2][2][4];
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt) {
+            const int row = 16 * warp + 8 * nt + g;
+            uint32_t w[D / 16];
+#pragma unroll
+            for (int x = 0; x < D / 64; ++x) {
+              const uint4 v = *reinterpret_cast<const uint4*>(kt_s + piece_at<D>(row, t4 * (D / 64) + x));
+              w[4 * x] = v.x; w[4 * x + 1] = v.y; w[4 * x + 2] = v.z; w[4 * x + 3] = v.w;
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y) s[nt][y][0] = s[nt][y][1] = s[nt][y][2] = s[nt][y][3] = 0.f;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) {
+              uint32_t b0, b1;
+              widen(w[j], b0, b1);
+              mma_f16(s[nt][j & 1], qf[j], b0, b1);
+            }
+          }
+          // values on their way: tokens 2 t4, + 1, + 8, + 9; channels D / 8 g ..
+          uint32_t v[4][D / 32];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int row = 16 * warp + 2 * t4 + (x & 1) + 4 * (x & 2);
+            if constexpr (D == 128) {
+              const uint4 y = *reinterpret_cast<const uint4*>(vt_s + piece_at<D>(row, g));
+              v[x][0] = y.x; v[x][1] = y.y; v[x][2] = y.z; v[x][3] = y.w;
+            } else {
+              const uint2 y = *reinterpret_cast<const uint2*>(vt_s + piece_at<D>(row, g >> 1) + (g & 1) * 8);
+              v[x][0] = y.x; v[x][1] = y.y;
+            }
+          }
+          // ---- weights of two rows x four tokens
+          float p[2][4], f[2];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const float up = power_of_two(min(max(qe[x] + ek, -126), 127));
+            float top = -INFINITY;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              float z = (s[y >> 1][0][2 * x + (y & 1)] + s[y >> 1][1][2 * x + (y & 1)]) * up * sc2;
+              if constexpr (MODS) {
+                if (cap > 0.f) {                   // cap tanh(z / cap), in base 2 (see paged_mma.cu)
+                  const float u = z * to_u, u2 = u * u;
+                  const float near = fmaf(u2, fmaf(u2, fmaf(u2, -0.048268907f, 0.13284431f), -0.33331972f), 0.99999994f) * u;
+                  const float far = copysignf(fmaf(-2.f, rcp_approx(1.f + ex2(fabsf(u) * (2.f * kLog2e))), 1.f), u);
+                  z = (fabsf(u) >= kCapNear ? far : near) * (cap * kLog2e);
+                }
+                if (a.slopes) z = fmaf(-slope2[x], fabsf((float)(key0 - pos[x] + 2 * t4 + (y & 1) + 4 * (y & 2))), z);
+              }
+              if (part) {
+                const int j = key0 + 2 * t4 + (y & 1) + 4 * (y & 2);
+                if (!((j >= see[x].lo || j < sinks) && j < see[x].hi)) z = -INFINITY;
+              }
+              p[x][y] = z;
+              top = fmaxf(top, z);
+            }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const float mn = fmaxf(m[x], top + (float)(ev - 15));           // (the largest weight is 2^15)
+            f[x] = m[x] == mn ? 1.f : ex2(m[x] - mn);
+            m[x] = mn;
+            const float nm = mn == -INFINITY ? 0.f : (float)ev - mn;
+            float sum = 0.f;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              p[x][y] = ex2(p[x][y] + nm);
+              sum += p[x][y];
+            }
+            l[x] = fmaf(l[x], f[x], sum * power_of_two(-ev));
+          }
+          const uint32_t pf[4] = {pack_f16(p[0][0], p[0][1]), pack_f16(p[1][0], p[1][1]), pack_f16(p[0][2], p[0][3]), pack_f16(p[1][2], p[1][3])};
+          bool bad = false;
+          if (part) {                              // values that no row sees are zeroed (0 x NaN is no 0)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const int j = key0 + 2 * t4 + (x & 1) + 4 * (x & 2);
+              const bool seen = j < hi_most && (j >= lo_least || j < sinks);
+#pragma unroll
+              for (int y = 0; y < D / 32; ++y) {
+                if (!seen) v[x][y] = 0u;
+                if (!alike && has_nan8(v[x][y])) {
+                  bad = true;
+                  v[x][y] = nan8_to_zero(v[x][y]);
+                }
+              }
+            }
+            bad = __any_sync(0xffffffffu, bad);
+          }
+          // ---- output: tile x holds channels D / 8 column + x
+          const float2 f0 = make_float2(f[0], f[0]), f1 = make_float2(f[1], f[1]);
+#pragma unroll
+          for (int y = 0; y < D / 32; ++y) {
+            uint32_t b[2][4];                      // of tokens (2 t4, + 1) and (+ 8, + 9): four channels
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              widen(__byte_perm(v[2 * x][y], v[2 * x + 1][y], 0x5140), b[x][0], b[x][1]);
+              widen(__byte_perm(v[2 * x][y], v[2 * x + 1][y], 0x7362), b[x][2], b[x][3]);
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              float c[4] = {0.f, 0.f, 0.f, 0.f};
+              mma_f16(c, pf, b[0][x], b[1][x]);
+              float (&d)[4] = o[4 * y + x];
+              const float2 d0 = __ffma2_rn(make_float2(d[0], d[1]), f0, make_float2(c[0], c[1]));
+              const float2 d1 = __ffma2_rn(make_float2(d[2], d[3]), f1, make_float2(c[2], c[3]));
+              d[0] = d0.x; d[1] = d0.y; d[2] = d1.x; d[3] = d1.y;
+            }
+          }
+          if (bad) {                               // rows that see a token with such a value: its channels are NaN
+#pragma unroll 1
+            for (int j = 0; j < 16; ++j) {
+              const int key = key0 + j;
+              const bool sees0 = (key >= see[0].lo || key < sinks) && key < see[0].hi, sees1 = (key >= see[1].lo || key < sinks) && key < see[1].hi;
+              if (!sees0 && !sees1) continue;
+              const float nan = __int_as_float(0x7fffffff);
+#pragma unroll
+              for (int x = 0; x < D / 4; x += 4) { // columns 2 t4 and 2 t4 + 1: D / 4 channels
+                const int c = t4 * (D / 4) + x;
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(vt_s + piece_at<D>(16 * warp + j, c >> 4) + (c & 15)), which = has_nan8(w);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                  constexpr int half = D / 8;
+                  const int tile = (x + y) % half, col = (x + y) / half;
+                  if (which & (0x80u << (8 * y))) {
+                    if (sees0) o[tile][col] = nan;
+                    if (sees1) o[tile][2 + col] = nan;
+                  }
+                }
+              }
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive1(&empty[st]);
+      }
+      if (!ok) break;
+      // ---- the eight warps' results meet: 16 bytes of a row at a time, laid so that neither side meets itself on a bank
+      if (i > 0 && !pm_wait(merge_free, (i - 1) & 1, lim, abort_flag)) { ok = false; break; }
+      constexpr int Q4 = D / 16;                   // 16-byte pieces that a lane has of a row
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        l[x] += __shfl_xor_sync(0xffffffffu, l[x], 1);
+        l[x] += __shfl_xor_sync(0xffffffffu, l[x], 2);
+        const int r = g + 8 * x;
+        if (r >= rows) continue;
+        if (t4 == 0) ml_s[warp * kPfRows + r] = make_float2(m[x], l[x]);
+        const int turn = D == 128 ? (2 * t4) ^ (g & 1) : (t4 >> 1) | ((g & 1) << 1);
+        float4* to = reinterpret_cast<float4*>(merge + (warp * kPfRows + r) * D) + t4 * Q4;
+#pragma unroll
+        for (int y = 0; y < Q4; ++y) {
+          constexpr int half = D / 8;
+          const int c = 4 * y, col = 2 * x + c / half, tile = c % half;
+          to[y ^ turn] = make_float4(o[tile][col], o[tile + 1][col], o[tile + 2][col], o[tile + 3][col]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive1(merge_full);
+      if (!pm_wait(merge_full, i & 1, lim, abort_flag)) { ok = false; break; }
+      const bool whole = sg.head && sg.tail;
+      const long long part0 = (2LL * blockIdx.x + (sg.head ? 1 : 0)) * a.w.rows;
+#pragma unroll 1
+      for (int x = tid; x < rows * (D / 4); x += 32 * kPfWarps) {
+        const int r = x / (D / 4), q4 = x % (D / 4), tt = q4 / Q4, gg = r & 7;
+        const int at = tt * Q4 + (q4 % Q4 ^ (D == 128 ? (2 * tt) ^ (gg & 1) : (tt >> 1) | ((gg & 1) << 1)));
+        float M = -INFINITY, sum = 0.f;
+        float2 ml[kPfWarps];
+#pragma unroll
+        for (int y = 0; y < kPfWarps; ++y) {
+          ml[y] = ml_s[y * kPfRows + r];
+          if (ml[y].y != 0.f) M = fmaxf(M, ml[y].x);
+        }
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int y = 0; y < kPfWarps; ++y) {
+          if (ml[y].y == 0.f) continue;            // (no token seen)
+          const float w = ex2(ml[y].x - M);
+          const float4 z = *(reinterpret_cast<const float4*>(merge + (y * kPfRows + r) * D) + at);
+          sum = fmaf(ml[y].y, w, sum);
+          v.x = fmaf(z.x, w, v.x); v.y = fmaf(z.y, w, v.y); v.z = fmaf(z.z, w, v.z); v.w = fmaf(z.w, w, v.w);
+        }
+        const int pi = r / G;
+        const long long out_row = (long long)(sg.row0 + pi) * a.pl.Hq + sg.h * G + r - pi * G;
+        if (whole) {
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+          *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.out) + out_row * D + 4 * q4) =
+              make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
+          if (q4 == 0 && a.lse) a.lse[out_row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+        } else {
+          *reinterpret_cast<float4*>(a.w.part_o + (part0 + r) * D + 4 * q4) = v;
+          if (q4 == 0) a.w.part_ml[part0 + r] = make_float2(M, sum);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive1(merge_free);
+        mbar_arrive1(&seg_empty[slot]);
+      }
+    }
+  }
+  if (!ok) *abort_flag = 1;
+  __syncwarp();
+  __syncthreads();
+  if (*abort_flag && tid == 0) atomicExch(a.pl.status, kStatusTimeout);
+}
+
+template <int D, bool MODS>
+cudaError_t few_launch(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
+  auto kern = paged_few_kernel<D, MODS>;
+  static unsigned long long allowed = 0;
+  cudaError_t e = allow_smem_once(kern, PfSmem<D>::kBytes, allowed);
+  if (e != cudaSuccess) return e;
+  return launch_ex(kern, dim3(a.w.n_cta), dim3(kPfThreads), PfSmem<D>::kBytes, s, 0, true, a, *reinterpret_cast<const CUtensorMap*>(maps.k),
+                   *reinterpret_cast<const CUtensorMap*>(maps.v));
+}
+
+}  // namespace
+
+int paged_few_positions(const PagedLayout& pl) { return kPfRows / pl.G; }
+
+void paged_plan_few(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int sm_count) {
+  w->ppos = w->upos = paged_few_positions(pl);
+  w->log_tk = 7;
+  static_assert(kPfKeys == 1 << 7, "tokens per tile");
+  const long long tiles = (pb.max_len + kPfKeys - 1) / kPfKeys, units = (long long)pb.batch * pl.Hkv;
+  w->by_unit = tiles <= 4 || (tiles <= 12 && units <= sm_count && 4 * units >= sm_count);   // (as in paged_mma.cu)
+  w->min_tiles = w->by_unit ? 1 : 2;
+  w->extra = 1;
+  const long long most = w->by_unit ? units : (units * tiles + w->min_tiles - 1) / w->min_tiles;
+  w->n_cta = (int)(most < sm_count ? most : sm_count);
+  w->narrow = paged_narrow(*w, pb, pl);
+  w->rows = (pb.max_new < w->upos ? pb.max_new : w->upos) * pl.G;
+}
+
+cudaError_t launch_paged_few(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
+  const bool mods = a.softcap > 0.f || a.slopes;
+  if (a.pl.d == 128) return mods ? few_launch<128, true>(a, maps, s) : few_launch<128, false>(a, maps, s);
+  return mods ? few_launch<64, true>(a, maps, s) : few_launch<64, false>(a, maps, s);
+}
+
+}  // namespace spla

@@ -74,6 +74,19 @@ bool spla::make_kv_map(void* out128, void* base, int d, int B, unsigned long lon
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// ... a matrix [rows][d] of bytes, d 64 or 128, with boxes of B whole rows (swizzled over 128 or 64 bytes, as long as a row is)
+bool spla::make_byte_map(void* out128, void* base, int d, int B, unsigned long long rows) {
+  TensorMapEncodeFn encode = tensor_map_encoder();
+  if (!encode) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)d, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)d};
+  const cuuint32_t box[2] = {(cuuint32_t)d, (cuuint32_t)B};
+  const cuuint32_t estr[2] = {1u, 1u};
+  return encode(reinterpret_cast<CUtensorMap*>(out128), CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, estr,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // [n3][n2][n1][n0] bf16 elements with the given byte strides, boxes of [b3][b2][1][n0] (n0 x 2 = 128 bytes, 128-byte swizzle).
 bool spla::make_tile_map_4d(void* out128, void* base, unsigned n0, unsigned n1, unsigned n2, unsigned n3, unsigned long long s1, unsigned long long s2,
                             unsigned long long s3, unsigned b2, unsigned b3) {
