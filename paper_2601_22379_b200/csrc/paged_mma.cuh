@@ -47,11 +47,12 @@ namespace {
 
 constexpr int kPmThreads = 384;
 constexpr int kPmWiden = 128;                      // threads more that widen 8-bit pages
+constexpr int kPmScales = 8;                       // tiles whose scales are kept: more than are between the widening and the softmax (NK + 2)
 constexpr int kPmKeys = 128;                       // keys per tile
 constexpr int kPmDrain = 128;                      // tiles that are added up in O before it is drained: 1024 truncations, each of less than 2^-23: 2^-13 at most
 constexpr uint32_t kPmTmemCols = 512;              // S0, S1, O0, O1: 128 columns each
 
-template <int D, bool FEW>
+template <int D, bool FEW, bool BYTES>
 struct PmSmem {
   static constexpr int H = D / 64;                               // arrays of 128-byte rows per operand
   static constexpr int kHalf = kPmKeys * 128;
@@ -64,9 +65,11 @@ struct PmSmem {
   static constexpr int kStage = kSegs + 4 * 112;                   // [8 warps][32 rows][64 + 16 bytes], FEW [4 warps][8 rows][512 + 16] or fewer columns of more rows: rows on their way out
   static constexpr int kStageRow = 80;
   static constexpr int kBars = kStage + 8 * 32 * 80;
-  static constexpr int kNumBars = 2 * NK + 2 * NV + 15 + 8;
-  static constexpr int kMisc = kBars + kNumBars * 8;             // tensor-memory base, abort flag, skip flags [2], look-over marks [2][2]
-  static constexpr int kBytes = kMisc + 48;
+  static constexpr int kNumBars = 2 * NK + 2 * NV + 15 + 8 + (BYTES ? 1 + kPmScales : 0);
+  static constexpr int kMisc = (kBars + kNumBars * 8 + 15) / 16 * 16;   // tensor-memory base, abort flag, skip flags [2], look-over marks [2][2]
+  static constexpr int kScales = kMisc + 48;                     // BYTES: float4 [kPmScales][8]: 2^ek, ev, 2^-ev of a tile's blocks
+  static constexpr int kQe = kScales + (BYTES ? kPmScales * 8 * 16 : 0);   // BYTES: short [4 segments][2][128]: exponents of the queries' rows
+  static constexpr int kBytes = kQe + (BYTES ? 4 * 2 * 128 * 2 : 0);
   static_assert(4 * 32 * 144 <= 8 * 32 * 80 && 4 * 16 * 272 <= 8 * 32 * 80 && 4 * 8 * 528 <= 8 * 32 * 80, "rows on their way out");
   static_assert(kBytes <= 227 * 1024, "shared memory of the paged attention kernel");
   static_assert(kPmKeys >= 128, "positions of a row tile (see PmPlan)");
@@ -148,6 +151,12 @@ __device__ __forceinline__ void tmem_ld128(uint32_t addr, uint32_t (&r)[128]) {
   for (int x = 0; x < 4; ++x) tmem_ld_wait32(reinterpret_cast<uint32_t(&)[32]>(r[32 * x]));
 }
 __device__ __forceinline__ uint32_t pair_not_finite(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ uint32_t pair_not_finite_f16(uint32_t w) { return ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u; }
+__device__ __forceinline__ float f16_lo(uint32_t w) { return __low2float(*reinterpret_cast<const __half2*>(&w)); }
+__device__ __forceinline__ float f16_hi(uint32_t w) { return __high2float(*reinterpret_cast<const __half2*>(&w)); }
+// 8-bit pages: a row's first maximum gets weight 2^11, later ones may grow to 2^15 before O is rescaled: fp16 holds weights to 2^-12 of themselves, and down to 2^-35 of
+// the largest (weights below, of 2^24 tokens at most, are 2^-12 of it together).
+constexpr float kPmHead = 11.f, kPmGrow = 4.f;
 
 // A thread's row of O into its sums, [slot of a CTA][D / 4][128 threads] 16 bytes each and then [128] of l: sums = sums f + O, or O where there
 // are none yet.  And back, for the end of a segment: O = sums f + O; returns l.
@@ -199,13 +208,15 @@ template <int D, bool MODS, bool FEW, bool LONG, bool BYTES>
 __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
     paged_mma_kernel(const PagedAttend a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                      const __grid_constant__ CUtensorMap map_q) {
-  using SM = PmSmem<D, FEW>;
+  using SM = PmSmem<D, FEW, BYTES>;
+  static_assert(!BYTES || SM::NK + 2 <= kPmScales, "scales of tiles on their way");
   constexpr int H = SM::H, NK = SM::NK, NV = SM::NV, THREADS = kPmThreads + (BYTES ? kPmWiden : 0);
   extern __shared__ __align__(1024) unsigned char smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + SM::kBars);
   uint64_t *k_full = bars, *k_empty = k_full + NK, *v_full = k_empty + NK, *v_empty = v_full + NV, *q_full = v_empty + NV, *q_empty = q_full + 1,
            *s_full = q_empty + 1, *p_ready = s_full + 2, *pv_done = p_ready + 2, *o_free = pv_done + 2, *scanned = o_free + 2, *halves = scanned + 2,
-           *quarters = halves + 1, *done = quarters + 1, *seg_full = done + 1, *seg_empty = seg_full + kPmSegs;
+           *quarters = halves + 1, *done = quarters + 1, *seg_full = done + 1, *seg_empty = seg_full + kPmSegs, *q_ready = seg_empty + kPmSegs,
+           *sc_full = q_ready + 1;                                 // (the last two of 8-bit pages only)
   uint32_t* tmem_base_s = reinterpret_cast<uint32_t*>(smem + SM::kMisc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SM::kMisc + 4);
   volatile int* skip_pv = reinterpret_cast<volatile int*>(smem + SM::kMisc + 8);    // [2]: this product with V has been formed by the softmax warps
@@ -230,6 +241,10 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
     mbar_init(halves, 4);
     mbar_init(quarters, 4);
     mbar_init(done, 1);
+    if (BYTES) {
+      mbar_init(q_ready, kPmWiden / 32);
+      for (int s = 0; s < kPmScales; ++s) mbar_init(&sc_full[s], kPmWiden / 32);
+    }
     for (int s = 0; s < kPmSegs; ++s) { mbar_init(&seg_full[s], 1);  mbar_init(&seg_empty[s], BYTES ? 14 : 11); }   // K, V (queries, four that widen), MMA and eight softmax warps
     mbar_init_done();
     *abort_flag = 0;
@@ -248,6 +263,7 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
   const int lim = a.wait_limit;
   const int ppos = a.w.ppos, G = a.pl.G;
   PmSeg* segs = reinterpret_cast<PmSeg*>(smem + SM::kSegs);
+  auto seg_at = [&](const PmSeg& sg) { return (int)(&sg - segs); };   // place of a segment: free again when every role is done with it
   // The CTA's segments, one after the other: the body returns false to give up.
   auto each_segment = [&](bool& ok, auto body) {
 #pragma unroll 1
@@ -262,7 +278,7 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
   };
 
   if (wg == 0) {
-    warpgroup_reg_dec<BYTES ? 72 : 120>();                        // (120 + 2 x 192 = 3 x 168, 72 + 72 + 2 x 184 = 4 x 128: what the CTA is launched with)
+    warpgroup_reg_dec<BYTES ? 64 : 120>();                        // (120 + 2 x 192 = 3 x 168, 64 + 80 + 2 x 184 = 4 x 128: what the CTA is launched with)
     if (BYTES && warp == 2) {
     } else if (warp == 0 || warp == 2) {
       // ------------------------------------------------------------ TMA: queries and K, or V ----------------------------
@@ -318,8 +334,8 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
       if (is_k && seg > 0) warp_waits(q_full, (seg - 1) & 1, lim);
     } else if (warp == 1) {
       // ------------------------------------------------------------ MMA issuer -----------------------------------------
-      constexpr uint32_t id_s = umma_idesc(true, false, false, 128, kPmKeys);
-      constexpr uint32_t id_o = umma_idesc(true, false, true, 128, D);
+      constexpr uint32_t id_s = umma_idesc(!BYTES, false, false, 128, kPmKeys);
+      constexpr uint32_t id_o = umma_idesc(!BYTES, false, true, 128, D);
       constexpr uint32_t kStep = 2048 / 16;                       // 16 keys of V
       const uint32_t one = elect_one();                           // (the whole warp runs this loop: see umma_ss_one)
       const uint32_t q_lo = umma_desc_lo(sbase + SM::kQ, 16), k_lo = umma_desc_lo(sbase + SM::kK, 16), v_lo = umma_desc_lo(sbase + SM::kV, SM::kHalf);
@@ -375,7 +391,7 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
       each_segment(ok, [&](const PmSeg& sg) {
         const PmPlan pl = sg.pl;
         if (pl.A >= pl.E) return true;
-        if (!pm_wait(q_full, seg & 1, lim, abort_flag)) return false;
+        if (!pm_wait(BYTES ? q_ready : q_full, seg & 1, lim, abort_flag)) return false;
         ++seg;
         first0 = first1 = true;
         it0 = it1 = 0;
@@ -431,18 +447,20 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
       if (a.w.cuts && lane == 0) a.w.cuts[blockIdx.x] = cut;
     }
   } else if (BYTES && wg == 3) {
-    // -------------------------------------------------------------- 8-bit pages: tiles as bf16, by way of registers ---------
-    // A thread takes 16 bytes of every 16 (or 32) tokens, which are under way until the tile's place is free: e4m3 -> fp16 -> fp32, times the
-    // scale, -> bf16, all of it exact, into the two halves' rows as TMA would lay them.
-    warpgroup_reg_dec<72>();
+    // -------------------------------------------------------------- 8-bit pages: tiles as fp16, by way of registers ---------
+    // e4m3 is exact in fp16; the scales stay out of the products (see the softmax).  A thread takes 16 bytes of every 16 (or 32) tokens; the next tile's
+    // are under way as soon as its registers are free.  Two rows x four pieces of one half are stored side by side: no bank twice.
+    warpgroup_reg_dec<80>();
     constexpr int PIECES = D / 16, NX = kPmKeys * PIECES / kPmWiden;
-    const int thr = tid - kPmThreads, piece = thr % PIECES, r16 = thr / PIECES % 16, b_odd = thr / PIECES / 16;
+    const int thr = tid - kPmThreads, piece = D == 128 ? (lane & 3) + (lane >> 1 & 4) : lane & 3;
+    const int r16 = D == 128 ? (lane >> 2 & 1) + (lane >> 3 & 2) + 4 * (warp & 3) : thr / PIECES % 16, b_odd = D == 128 ? 0 : thr / PIECES / 16;
+    const int half = (piece >> 2) * SM::kHalf, c0 = 2 * (piece & 3);
     bool ok = true;
-    int kt = 0;
+    int kt = 0, seg = 0;
     each_segment(ok, [&](const PmSeg& sg) {
-      const int A = sg.pl.A, E = sg.pl.E, L = sg.L, b = sg.b, h = sg.h, ns = sg.ns, skip = sg.skip;
+      const int A = sg.pl.A, E = sg.pl.E, L = sg.L, b = sg.b, h = sg.h;
       if (A >= E) return true;
-      auto first_tok = [&](int t) { return (t < ns ? t : t + skip) * kPmKeys; };
+      auto first_tok = [&](int t) { return (t < sg.ns ? t : t + sg.skip) * kPmKeys; };
       // lane i (mod 8): cache row of a tile's block i, -1: none; a tile ahead
       auto find = [&](int t) {
         const int tok = first_tok(t) + 16 * (lane & 7);
@@ -450,51 +468,87 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
         const long long r = paged_row(a.pb, a.pl, b, h, tok >> a.pl.log_p);
         return r < 0 ? -1 : (int)(r + (tok & (a.pl.P - 1)));
       };
-      const unsigned char* scales = lane & 8 ? a.v_scales : a.k_scales;      // lanes 0 to 7: K's, 8 to 15: V's
+      uint4 raw[NX];
+      auto load = [&](int x, const unsigned char* pages, int row, int t) {
+        const int block = D == 128 ? x : 2 * x + b_odd, r = __shfl_sync(0xffffffffu, row, block);
+        raw[x] = make_uint4(0u, 0u, 0u, 0u);
+        if (r >= 0 && first_tok(t) + 16 * block + r16 < L) raw[x] = *reinterpret_cast<const uint4*>(pages + (long long)(r + r16) * D + piece * 16);
+      };
+      auto store = [&](int x, unsigned char* tile) {
+        const int at = 16 * (D == 128 ? x : 2 * x + b_odd) + r16;
+        uint4 y0, y1;
+        widen(raw[x].x, y0.x, y0.y);
+        widen(raw[x].y, y0.z, y0.w);
+        widen(raw[x].z, y1.x, y1.y);
+        widen(raw[x].w, y1.z, y1.w);
+        *reinterpret_cast<uint4*>(tile + half + at * 128 + ((c0 ^ (at & 7)) << 4)) = y0;
+        *reinterpret_cast<uint4*>(tile + half + at * 128 + ((c0 + 1 ^ (at & 7)) << 4)) = y1;
+      };
+      auto filled = [&](uint64_t* full) {
+        proxy_fence();                                            // (tile written -> tensor core)
+        __syncwarp();
+        if (lane == 0) mbar_arrive1(full);
+      };
       int row = find(A);
+#pragma unroll
+      for (int x = 0; x < NX; ++x) load(x, a.k_bytes, row, A);
+      // queries: rows scaled to below 2^15 and rounded to fp16, in their places; a thread a row
+      if (!pm_wait(q_full, seg & 1, lim, abort_flag)) return false;
+      ++seg;
+      for (int s = 0; s < (FEW || sg.pl.single || sg.pl.items(1) == 0 ? 1 : 2); ++s) {
+        unsigned char* qr = smem + SM::kQ + s * SM::kTile + thr * 128;
+        float top = 0.f;
+#pragma unroll 4
+        for (int c = 0; c < 8 * H; ++c) {
+          const uint4 v = *reinterpret_cast<const uint4*>(qr + (c >> 3) * SM::kHalf + (((c & 7) ^ (thr & 7)) << 4));
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float lo = fabsf(bf16_lo(w[i])), hi = fabsf(bf16_hi(w[i]));
+            if (lo < INFINITY) top = fmaxf(top, lo);
+            if (hi < INFINITY) top = fmaxf(top, hi);
+          }
+        }
+        const int e = top > 0.f ? max((__float_as_int(top) >> 23) - 127 - 14, -100) : 0;
+        const float mul = power_of_two(-e);
+#pragma unroll 4
+        for (int c = 0; c < 8 * H; ++c) {
+          uint4* at = reinterpret_cast<uint4*>(qr + (c >> 3) * SM::kHalf + (((c & 7) ^ (thr & 7)) << 4));
+          const uint4 v = *at;
+          *at = make_uint4(pack_f16(bf16_lo(v.x) * mul, bf16_hi(v.x) * mul), pack_f16(bf16_lo(v.y) * mul, bf16_hi(v.y) * mul),
+                           pack_f16(bf16_lo(v.z) * mul, bf16_hi(v.z) * mul), pack_f16(bf16_lo(v.w) * mul, bf16_hi(v.w) * mul));
+        }
+        reinterpret_cast<short*>(smem + SM::kQe)[(seg_at(sg) * 2 + s) * 128 + thr] = (short)e;
+      }
+      filled(q_ready);
 #pragma unroll 1
       for (int t = A; t < E; ++t, ++kt) {
-        const int e = row < 0 ? 0 : paged_exponent(scales + (row >> 4)), row_next = find(t + 1), tok0 = first_tok(t);
-#pragma unroll 1
-        for (int is_v = 0; is_v < 2; ++is_v) {
-          const unsigned char* pages = is_v ? a.v_bytes : a.k_bytes;
-          uint4 raw[NX];
-#pragma unroll
-          for (int x = 0; x < NX; ++x) {
-            const int block = D == 128 ? x : 2 * x + b_odd, r = __shfl_sync(0xffffffffu, row, block);
-            raw[x] = make_uint4(0u, 0u, 0u, 0u);
-            if (r >= 0 && tok0 + 16 * block + r16 < L) raw[x] = *reinterpret_cast<const uint4*>(pages + (long long)(r + r16) * D + piece * 16);
-          }
-          const int n = is_v ? NV : NK, st = kt % n;
-          uint64_t *full = is_v ? v_full : k_full, *empty = is_v ? v_empty : k_empty;
-          if (kt >= n && !pm_wait(&empty[st], ((kt / n) - 1) & 1, lim, abort_flag)) return false;
-          unsigned char* tile = smem + (is_v ? SM::kV : SM::kK) + st * SM::kTile + (piece >> 2) * SM::kHalf;
-#pragma unroll
-          for (int x = 0; x < NX; ++x) {
-            const int block = D == 128 ? x : 2 * x + b_odd, at = 16 * block + r16;
-            const float mul = power_of_two(__shfl_sync(0xffffffffu, e, 8 * is_v + block));
-            const uint32_t w[4] = {raw[x].x, raw[x].y, raw[x].z, raw[x].w};
-            uint32_t y[8];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t lo, hi;
-              widen(w[i], lo, hi);
-              const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&lo)), q = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-              y[2 * i] = pack_bf16(p.x * mul, p.y * mul);
-              y[2 * i + 1] = pack_bf16(q.x * mul, q.y * mul);
-            }
-            // (the eight lanes of a row fill the two halves' even pieces, then their odd ones; the second half's the other way round: no bank twice)
-            const bool turn = piece & 4;
-            const uint4 v0 = make_uint4(turn ? y[4] : y[0], turn ? y[5] : y[1], turn ? y[6] : y[2], turn ? y[7] : y[3]);
-            const uint4 v1 = make_uint4(turn ? y[0] : y[4], turn ? y[1] : y[5], turn ? y[2] : y[6], turn ? y[3] : y[7]);
-            const int c0 = 2 * (piece & 3) + turn, c1 = 2 * (piece & 3) + !turn;
-            *reinterpret_cast<uint4*>(tile + at * 128 + ((c0 ^ (at & 7)) << 4)) = v0;
-            *reinterpret_cast<uint4*>(tile + at * 128 + ((c1 ^ (at & 7)) << 4)) = v1;
-          }
-          proxy_fence();                                          // (tile written -> tensor core)
-          __syncwarp();
-          if (lane == 0) mbar_arrive1(&full[st]);
+        const int row_next = find(t + 1);
+        int e = 0;
+        if ((warp & 3) == 0 && lane < 16) e = row < 0 ? 0 : paged_exponent((lane & 8 ? a.v_scales : a.k_scales) + (row >> 4));
+        int st = kt % NK;
+        if (kt >= NK && !pm_wait(&k_empty[st], ((kt / NK) - 1) & 1, lim, abort_flag)) return false;
+        if ((warp & 3) == 0) {                                    // (free: see kPmScales)
+          const int ev = __shfl_sync(0xffffffffu, e, 8 + (lane & 7));
+          if (lane < 8)
+            reinterpret_cast<float4*>(smem + SM::kScales)[(kt % kPmScales) * 8 + lane] = make_float4(power_of_two(e), (float)ev, power_of_two(-ev), 0.f);
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive1(&sc_full[kt % kPmScales]);    // (all four: behind the exponents of the queries)
+#pragma unroll
+        for (int x = 0; x < NX; ++x) {
+          store(x, smem + SM::kK + st * SM::kTile);
+          load(x, a.v_bytes, row, t);
+        }
+        filled(&k_full[st]);
+        st = kt % NV;
+        if (kt >= NV && !pm_wait(&v_empty[st], ((kt / NV) - 1) & 1, lim, abort_flag)) return false;
+#pragma unroll
+        for (int x = 0; x < NX; ++x) {
+          store(x, smem + SM::kV + st * SM::kTile);
+          load(x, a.k_bytes, row_next, t + 1);
+        }
+        filled(&v_full[st]);
         row = row_next;
       }
       return true;
@@ -512,6 +566,10 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
     const float to_u = MODS && a.softcap > 0.f ? a.sm_scale / a.softcap : 0.f, sq_u = to_u * to_u;
     const float cap0 = 0.99999994f * sc2, cap1 = -0.33331972f * sc2 * sq_u, cap2 = 0.13284431f * sc2 * sq_u * sq_u,
                 cap3 = -0.048268907f * sc2 * sq_u * sq_u * sq_u;   // (a score of 1 is sc2 in base 2)
+    auto not_finite = [](uint32_t w) { return BYTES ? pair_not_finite_f16(w) : pair_not_finite(w); };
+    auto val_lo = [](uint32_t w) { return BYTES ? f16_lo(w) : bf16_lo(w); };
+    auto val_hi = [](uint32_t w) { return BYTES ? f16_hi(w) : bf16_hi(w); };
+    const float4* scales_s = reinterpret_cast<const float4*>(smem + SM::kScales) + kb / 16;   // BYTES: of this warp's keys
     bool ok = true;
     int kt = 0, n = 0, n_scan = 0, n_half = 0, n_quarter = 0, n_used = 0;   // tiles of the CTA, items of this slot, look-overs, merges, segments that used O
     each_segment(ok, [&](const PmSeg& sg) {
@@ -543,6 +601,7 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
       const bool live = __any_sync(0xffffffffu, valid);
       const bool counts = valid || alike;
       const int lo_most = __reduce_max_sync(0xffffffffu, counts ? see.lo : 0), hi_least = __reduce_min_sync(0xffffffffu, counts ? see.hi : 0x7fffffff);
+      float up = 0.f;                                              // BYTES: 2^(exponent of the row's queries)
       float m = -INFINITY, l = 0.f, fd = 1.f;                      // fd: what the sums of drained tiles are behind the maximum
       int done_items = 0;
 #pragma unroll 1
@@ -576,19 +635,23 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
           } else {
             vt += thr * 16;                                       // 16-byte pieces: rows thr / 8 + 16 x of either array
             __nv_bfloat162 most = __floats2bfloat162_rn(0.f, 0.f); // the largest magnitude, NaN above all
+            __half2 most_h = __floats2half2_rn(0.f, 0.f);
 #pragma unroll 8
             for (int x = 0; x < SM::kTile / 2048; ++x) {
               const uint4 v = *reinterpret_cast<const uint4*>(vt + x * 2048);
               const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-              for (int e = 0; e < 4; ++e) most = __hmax2_nan(most, __habs2(*reinterpret_cast<const __nv_bfloat162*>(&w[e])));
+              for (int e = 0; e < 4; ++e) {
+                if constexpr (BYTES) most_h = __hmax2_nan(most_h, __habs2(*reinterpret_cast<const __half2*>(&w[e])));
+                else most = __hmax2_nan(most, __habs2(*reinterpret_cast<const __nv_bfloat162*>(&w[e])));
+              }
             }
-            if (pair_not_finite(*reinterpret_cast<const uint32_t*>(&most))) {
+            if (BYTES ? not_finite(*reinterpret_cast<const uint32_t*>(&most_h)) : not_finite(*reinterpret_cast<const uint32_t*>(&most))) {
               const int L = sg.L;
 #pragma unroll 1
               for (int x = 0; x < SM::kTile / 2048; ++x) {
                 const uint4 v = *reinterpret_cast<const uint4*>(vt + x * 2048);
-                if (pair_not_finite(v.x) | pair_not_finite(v.y) | pair_not_finite(v.z) | pair_not_finite(v.w)) {
+                if (not_finite(v.x) | not_finite(v.y) | not_finite(v.z) | not_finite(v.w)) {
                   if (tok0 + (thr >> 3) + 16 * (x & 7) >= L) *reinterpret_cast<uint4*>(vt + x * 2048) = make_uint4(0u, 0u, 0u, 0u);
                   else bad = true;
                 }
@@ -609,12 +672,28 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
           const int key0 = tok0 + kb;
           const bool part = key0 < lo_most || key0 + KEYS > hi_least;     // (warp-uniform)
           const float mul = MODS ? 1.f : sc2;
+          const float4* scales = scales_s + (uint32_t)(k_base + t) % kPmScales * 8;   // BYTES: 2^ek, ev, 2^-ev of every 16 keys
+          if (BYTES && !pm_wait(&sc_full[(uint32_t)(k_base + t) % kPmScales], ((uint32_t)(k_base + t) / kPmScales) & 1, lim, abort_flag)) return false;
+          if (BYTES && done_items == 0)
+            up = power_of_two(reinterpret_cast<const short*>(smem + SM::kQe)[seg_at(sg) * 256 + (FEW ? lane : (single ? 0 : slot * 128) + thr)]);
           uint32_t r[KEYS];
           if constexpr (FEW) {
             tmem_ld32_async(tS + kb, r);
             tmem_ld_wait32(r);
           } else {
             tmem_ld128(tS, r);
+          }
+          if constexpr (BYTES && MODS) {                          // scores as they would be of the queries and keys themselves
+#pragma unroll
+            for (int c = 0; c < KEYS / 16; ++c) {
+              const float f = fminf(scales[c].x * up, 3e38f);
+#pragma unroll
+              for (int x = 16 * c; x < 16 * c + 16; x += 2) {
+                const float2 v = __fmul2_rn(make_float2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), make_float2(f, f));
+                r[x] = __float_as_uint(v.x);
+                r[x + 1] = __float_as_uint(v.y);
+              }
+            }
           }
           if constexpr (MODS) {
             if (a.softcap > 0.f) {
@@ -667,13 +746,28 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
                 if (!(bits & (1u << x))) r[32 * c + x] = 0xff800000u;
             }
           }
-          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          // 8-bit pages: block c's scores are c_c r, a value stands for its fp16 times 2^ev, which goes into the weight: y = c_c r + ev, weight 2^(y - m)
+          auto factor = [&](int c) { return MODS ? 1.f : fminf(fmaxf(scales[c].x * sc2 * up, 1e-37f), 3e38f); };
+          float mt;
+          if constexpr (BYTES) {
+            mt = -INFINITY;
 #pragma unroll
-          for (int x = 0; x < KEYS; x += 2) mx[x / 2 & 3] = fmaxf(mx[x / 2 & 3], fmaxf(__uint_as_float(r[x]), __uint_as_float(r[x + 1])));
-          const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * mul;
+            for (int c = 0; c < KEYS / 16; ++c) {
+              float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+              for (int x = 16 * c; x < 16 * c + 16; x += 2) mx[x / 2 & 1] = max3(mx[x / 2 & 1], __uint_as_float(r[x]), __uint_as_float(r[x + 1]));
+              mt = fmaxf(mt, fmaf(fmaxf(mx[0], mx[1]), factor(c), scales[c].y));
+            }
+            mt -= kPmHead;
+          } else {
+            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int x = 0; x < KEYS; x += 2) mx[x / 2 & 3] = fmaxf(mx[x / 2 & 3], fmaxf(__uint_as_float(r[x]), __uint_as_float(r[x + 1])));
+            mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * mul;
+          }
           // The first visible keys of a row set its maximum (its row of O is zero so far); later ones only move it when it would
           // let a probability exceed 2^8.
-          const bool grow = mt > m + 8.f && m > -INFINITY;
+          const bool grow = mt > m + (BYTES ? kPmGrow : 8.f) && m > -INFINITY;
           if (m == -INFINITY) m = mt;
           if (__any_sync(0xffffffffu, grow)) {
             if (!pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) return false;   // every product with P so far
@@ -693,18 +787,40 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
             }
           }
           const float nm = m == -INFINITY ? 0.f : -m;
-          float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+          if constexpr (BYTES) {
 #pragma unroll
-          for (int c = 0; c < KEYS / 32; ++c) {
-            uint32_t pk[16];
+            for (int c = 0; c < KEYS / 32; ++c) {
+              uint32_t pk[16];
 #pragma unroll
-            for (int x = 0; x < 16; ++x) {
-              const float2 v = __ffma2_rn(make_float2(__uint_as_float(r[32 * c + 2 * x]), __uint_as_float(r[32 * c + 2 * x + 1])), make_float2(mul, mul), make_float2(nm, nm));
-              const float2 p = make_float2(ex2(v.x), ex2(v.y));
-              if (x & 1) sum1 = __fadd2_rn(sum1, p); else sum0 = __fadd2_rn(sum0, p);
-              pk[x] = pack_bf16(p.x, p.y);
+              for (int y = 0; y < 2; ++y) {
+                const float f = factor(2 * c + y), add = scales[2 * c + y].y + nm;
+                float2 part = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int x = 8 * y; x < 8 * y + 8; ++x) {
+                  const float2 v = __ffma2_rn(make_float2(__uint_as_float(r[32 * c + 2 * x]), __uint_as_float(r[32 * c + 2 * x + 1])), make_float2(f, f), make_float2(add, add));
+                  const float2 p = make_float2(ex2(v.x), ex2(v.y));
+                  part = __fadd2_rn(part, p);
+                  pk[x] = pack_f16(p.x, p.y);
+                }
+                l = fmaf(part.x + part.y, scales[2 * c + y].z, l);
+              }
+              tmem_st16(tS + kb / 2 + 16 * c, pk);
             }
-            tmem_st16(tS + kb / 2 + 16 * c, pk);
+          } else {
+            float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+#pragma unroll
+            for (int c = 0; c < KEYS / 32; ++c) {
+              uint32_t pk[16];
+#pragma unroll
+              for (int x = 0; x < 16; ++x) {
+                const float2 v = __ffma2_rn(make_float2(__uint_as_float(r[32 * c + 2 * x]), __uint_as_float(r[32 * c + 2 * x + 1])), make_float2(mul, mul), make_float2(nm, nm));
+                const float2 p = make_float2(ex2(v.x), ex2(v.y));
+                if (x & 1) sum1 = __fadd2_rn(sum1, p); else sum0 = __fadd2_rn(sum0, p);
+                pk[x] = pack_bf16(p.x, p.y);
+              }
+              tmem_st16(tS + kb / 2 + 16 * c, pk);
+            }
+            l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
           }
           if constexpr (FEW) {                                    // the keys of the other warps
             uint32_t zero[16];
@@ -713,7 +829,6 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
 #pragma unroll
             for (int c = 1; c < 4; ++c) tmem_st16(tS + (((warp & 3) + c) & 3) * 16, zero);
           }
-          l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
           tmem_st_wait();
         }
         if (simt) {
@@ -738,7 +853,7 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
 #pragma unroll
               for (int y = 0; y < 32; ++y) {
                 if (!(bits & (1u << y))) continue;
-                const float p = (y & 1) ? bf16_hi(pw[y >> 1]) : bf16_lo(pw[y >> 1]);
+                const float p = (y & 1) ? val_hi(pw[y >> 1]) : val_lo(pw[y >> 1]);
                 const int j = 32 * w + y;
                 const unsigned char* vr = vt + (c >> 6) * SM::kHalf + j * 128;
 #pragma unroll
@@ -747,8 +862,8 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
                   const uint32_t q[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                   for (int z = 0; z < 4; ++z) {
-                    acc[8 * x + 2 * z] = fmaf(p, bf16_lo(q[z]), acc[8 * x + 2 * z]);
-                    acc[8 * x + 2 * z + 1] = fmaf(p, bf16_hi(q[z]), acc[8 * x + 2 * z + 1]);
+                    acc[8 * x + 2 * z] = fmaf(p, val_lo(q[z]), acc[8 * x + 2 * z]);
+                    acc[8 * x + 2 * z + 1] = fmaf(p, val_hi(q[z]), acc[8 * x + 2 * z + 1]);
                   }
                 }
               }
@@ -972,7 +1087,7 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
 template <int D, bool MODS, bool FEW, bool LONG, bool BYTES>
 cudaError_t mma_variant(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
   auto kern = paged_mma_kernel<D, MODS, FEW, LONG, BYTES>;
-  constexpr int bytes = PmSmem<D, FEW>::kBytes;
+  constexpr int bytes = PmSmem<D, FEW, BYTES>::kBytes;
   static unsigned long long allowed = 0;
   cudaError_t e = allow_smem_once(kern, bytes, allowed);
   if (e != cudaSuccess) return e;

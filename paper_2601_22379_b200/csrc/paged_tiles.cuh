@@ -1,6 +1,8 @@
 // What the attention kernels with roles share.
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "paged.h"
 #include "umma.cuh"
 
@@ -39,6 +41,10 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t& lo, uint32_t& hi) {
       "cvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
       : "=r"(lo), "=r"(hi)
       : "r"(w));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
 }
 // bits a .. e - 1 of a word (a, e in any range)
 __device__ __forceinline__ uint32_t bits_between(int a, int e) {
