@@ -489,7 +489,9 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
         __syncwarp();
         if (lane == 0) mbar_arrive1(full);
       };
-      int row = find(A);
+      // (scales a tile ahead, the first warp)
+      auto exponent = [&](int row) { return row < 0 || lane >= 16 ? 0 : paged_exponent((lane & 8 ? a.v_scales : a.k_scales) + (row >> 4)); };
+      int row = find(A), row_next = find(A + 1), e = (warp & 3) == 0 ? exponent(row) : 0;
 #pragma unroll
       for (int x = 0; x < NX; ++x) load(x, a.k_bytes, row, A);
       // queries: rows scaled to below 2^15 and rounded to fp16, in their places; a thread a row
@@ -523,9 +525,7 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
       filled(q_ready);
 #pragma unroll 1
       for (int t = A; t < E; ++t, ++kt) {
-        const int row_next = find(t + 1);
-        int e = 0;
-        if ((warp & 3) == 0 && lane < 16) e = row < 0 ? 0 : paged_exponent((lane & 8 ? a.v_scales : a.k_scales) + (row >> 4));
+        const int row_later = find(t + 2), e_next = (warp & 3) == 0 ? exponent(row_next) : 0;
         int st = kt % NK;
         if (kt >= NK && !pm_wait(&k_empty[st], ((kt / NK) - 1) & 1, lim, abort_flag)) return false;
         if ((warp & 3) == 0) {                                    // (free: see kPmScales)
@@ -550,6 +550,8 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
         }
         filled(&v_full[st]);
         row = row_next;
+        row_next = row_later;
+        e = e_next;
       }
       return true;
     });
