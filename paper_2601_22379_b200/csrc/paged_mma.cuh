@@ -46,30 +46,32 @@ namespace spla {
 namespace {
 
 constexpr int kPmThreads = 384;
-constexpr int kPmWiden = 128;                      // threads more that widen 8-bit pages
-constexpr int kPmScales = 8;                       // tiles whose scales are kept: more than are between the widening and the softmax (NK + 2)
+constexpr int kPmScales = 8;                       // tiles whose scales are kept: more than are between their copies and the softmax (NK + 2)
 constexpr int kPmKeys = 128;                       // keys per tile
 constexpr int kPmDrain = 128;                      // tiles that are added up in O before it is drained: 1024 truncations, each of less than 2^-23: 2^-13 at most
 constexpr uint32_t kPmTmemCols = 512;              // S0, S1, O0, O1: 128 columns each
 
 template <int D, bool FEW, bool BYTES>
 struct PmSmem {
-  static constexpr int H = D / 64;                               // arrays of 128-byte rows per operand
+  static constexpr int H = D / 64;                               // arrays of 128-byte rows per operand of 16 bits
   static constexpr int kHalf = kPmKeys * 128;
-  static constexpr int kTile = H * kHalf;                        // one K or V tile, or the queries of a row tile
-  // stages: V is held until its softmax is through, K only until the scores; one row tile leaves room for another of V
-  static constexpr int NK = D == 128 ? 2 : 4, NV = (D == 128 ? 2 : 4) + (FEW ? (D == 128 ? 1 : 2) : 0);
-  static constexpr int kQ = 0, kK = kQ + (FEW ? 1 : 2) * kTile, kV = kK + NK * kTile, kSeqs = kV + NV * kTile;
+  static constexpr int kTile = H * kHalf;                        // one tile of 16 bits, or the queries of a row tile (two parts of 8 bits)
+  static constexpr int kRaw = kPmKeys * D;                       // one of 8 bits
+  // stages: V is held until its softmax is through, K only until the scores; one row tile leaves room for another of V.  8-bit pages: K as it is, V as it
+  // comes (NR) and widened
+  static constexpr int NK = BYTES ? (D == 128 && !FEW ? 2 : 4) : D == 128 ? 2 : 4;
+  static constexpr int NV = (D == 128 ? 2 : 4) + (FEW && !BYTES ? (D == 128 ? 1 : 2) : 0), NR = BYTES ? (D == 128 ? 2 : 4) : 0;
+  static constexpr int kKTile = BYTES ? kRaw : kTile;
+  static constexpr int kQ = 0, kK = kQ + (FEW ? 1 : 2) * kTile, kV = kK + NK * kKTile, kR = kV + NV * kTile, kSeqs = kR + NR * kRaw;
   static constexpr int kMl = kSeqs + (int)((sizeof(PagedSeqs) + 15) / 16 * 16);   // float2 [128]: maximum and sum of the second half, of a quarter
   static constexpr int kSegs = kMl + 128 * 8;                     // PmSeg [4]: the segments that come next
   static constexpr int kStage = kSegs + 4 * 112;                   // [8 warps][32 rows][64 + 16 bytes], FEW [4 warps][8 rows][512 + 16] or fewer columns of more rows: rows on their way out
   static constexpr int kStageRow = 80;
   static constexpr int kBars = kStage + 8 * 32 * 80;
-  static constexpr int kNumBars = 2 * NK + 2 * NV + 15 + 8 + (BYTES ? 1 + kPmScales : 0);
+  static constexpr int kNumBars = 2 * NK + 2 * NV + 15 + 8 + (BYTES ? 2 * NR + kPmScales : 0);
   static constexpr int kMisc = (kBars + kNumBars * 8 + 15) / 16 * 16;   // tensor-memory base, abort flag, skip flags [2], look-over marks [2][2]
   static constexpr int kScales = kMisc + 48;                     // BYTES: float4 [kPmScales][8]: 2^ek, ev, 2^-ev of a tile's blocks
-  static constexpr int kQe = kScales + (BYTES ? kPmScales * 8 * 16 : 0);   // BYTES: short [4 segments][2][128]: exponents of the queries' rows
-  static constexpr int kBytes = kQe + (BYTES ? 4 * 2 * 128 * 2 : 0);
+  static constexpr int kBytes = kScales + (BYTES ? kPmScales * 8 * 16 : 0);
   static_assert(4 * 32 * 144 <= 8 * 32 * 80 && 4 * 16 * 272 <= 8 * 32 * 80 && 4 * 8 * 528 <= 8 * 32 * 80, "rows on their way out");
   static_assert(kBytes <= 227 * 1024, "shared memory of the paged attention kernel");
   static_assert(kPmKeys >= 128, "positions of a row tile (see PmPlan)");
@@ -154,6 +156,25 @@ __device__ __forceinline__ uint32_t pair_not_finite(uint32_t w) { return ((w & 0
 __device__ __forceinline__ uint32_t pair_not_finite_f16(uint32_t w) { return ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u; }
 __device__ __forceinline__ float f16_lo(uint32_t w) { return __low2float(*reinterpret_cast<const __half2*>(&w)); }
 __device__ __forceinline__ float f16_hi(uint32_t w) { return __high2float(*reinterpret_cast<const __half2*>(&w)); }
+// Four bf16 values times `mul` (a power of two) as four e4m3 and, of what that leaves, four e5m2.  An infinity is left to the second type, which has one.
+__device__ __forceinline__ void split_e4m3(uint32_t w0, uint32_t w1, float mul, bool finite, uint32_t& first, uint32_t& second) {
+  float x[4] = {bf16_lo(w0) * mul, bf16_hi(w0) * mul, bf16_lo(w1) * mul, bf16_hi(w1) * mul};
+  uint32_t infinite = 0u;
+  if (!finite)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (fabsf(x[i]) == INFINITY) {
+        infinite |= (x[i] > 0.f ? 0x7cu : 0xfcu) << (8 * i);
+        x[i] = 0.f;
+      }
+  const uint32_t h = __nv_cvt_float2_to_fp8x2(make_float2(x[0], x[1]), __NV_SATFINITE, __NV_E4M3) |
+                     (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(x[2], x[3]), __NV_SATFINITE, __NV_E4M3) << 16;
+  uint32_t lo, hi;
+  widen(h, lo, hi);
+  first = h;
+  second = infinite | __nv_cvt_float2_to_fp8x2(make_float2(x[0] - f16_lo(lo), x[1] - f16_hi(lo)), __NV_SATFINITE, __NV_E5M2) |
+           (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(x[2] - f16_lo(hi), x[3] - f16_hi(hi)), __NV_SATFINITE, __NV_E5M2) << 16;
+}
 // 8-bit pages: a row's first maximum gets weight 2^11, later ones may grow to 2^15 before O is rescaled: fp16 holds weights to 2^-12 of themselves, and down to 2^-35 of
 // the largest (weights below, of 2^24 tokens at most, are 2^-12 of it together).
 constexpr float kPmHead = 11.f, kPmGrow = 4.f;
@@ -205,18 +226,19 @@ __device__ __forceinline__ float pm_undrain(uint32_t tO, float* drain, int slot,
 
 // LONG: caches of more than kPmDrain tiles (the others go without what drains O: 106 us for a mixed batch in place of 108).
 template <int D, bool MODS, bool FEW, bool LONG, bool BYTES>
-__global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
+__global__ void __launch_bounds__(kPmThreads, 1)
     paged_mma_kernel(const PagedAttend a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                      const __grid_constant__ CUtensorMap map_q) {
   using SM = PmSmem<D, FEW, BYTES>;
   static_assert(!BYTES || SM::NK + 2 <= kPmScales, "scales of tiles on their way");
-  constexpr int H = SM::H, NK = SM::NK, NV = SM::NV, THREADS = kPmThreads + (BYTES ? kPmWiden : 0);
+  constexpr int H = SM::H, NK = SM::NK, NV = SM::NV;
   extern __shared__ __align__(1024) unsigned char smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + SM::kBars);
   uint64_t *k_full = bars, *k_empty = k_full + NK, *v_full = k_empty + NK, *v_empty = v_full + NV, *q_full = v_empty + NV, *q_empty = q_full + 1,
            *s_full = q_empty + 1, *p_ready = s_full + 2, *pv_done = p_ready + 2, *o_free = pv_done + 2, *scanned = o_free + 2, *halves = scanned + 2,
-           *quarters = halves + 1, *done = quarters + 1, *seg_full = done + 1, *seg_empty = seg_full + kPmSegs, *q_ready = seg_empty + kPmSegs,
-           *sc_full = q_ready + 1;                                 // (the last two of 8-bit pages only)
+           *quarters = halves + 1, *done = quarters + 1, *seg_full = done + 1, *seg_empty = seg_full + kPmSegs,
+           *r_full = seg_empty + kPmSegs, *r_empty = r_full + SM::NR, *sc_full = r_empty + SM::NR;   // (the last three of 8-bit pages only)
+  uint64_t* q_ready = q_full;                                     // [2] of 8-bit pages: the softmax warps bring the queries of their row tiles (q_empty is not used)
   uint32_t* tmem_base_s = reinterpret_cast<uint32_t*>(smem + SM::kMisc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SM::kMisc + 4);
   volatile int* skip_pv = reinterpret_cast<volatile int*>(smem + SM::kMisc + 8);    // [2]: this product with V has been formed by the softmax warps
@@ -226,11 +248,10 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wg = warp >> 2;
 
   if (tid == 0) {
-    constexpr int brings = BYTES ? kPmWiden / 32 : 1;               // warps that fill a tile, or the copy that does
-    for (int s = 0; s < NK; ++s) { mbar_init(&k_full[s], brings);  mbar_init(&k_empty[s], 1); }
-    for (int s = 0; s < NV; ++s) { mbar_init(&v_full[s], brings);  mbar_init(&v_empty[s], 1); }
-    mbar_init(q_full, 1);
-    mbar_init(q_empty, 1);
+    for (int s = 0; s < NK; ++s) { mbar_init(&k_full[s], 1);  mbar_init(&k_empty[s], 1); }
+    for (int s = 0; s < NV; ++s) { mbar_init(&v_full[s], 1);  mbar_init(&v_empty[s], 1); }
+    mbar_init(q_full, BYTES ? 4 : 1);
+    mbar_init(q_empty, BYTES ? 4 : 1);
     for (int s = 0; s < 2; ++s) {
       mbar_init(&s_full[s], 1);  mbar_init(&p_ready[s], 4);
       mbar_init(&pv_done[s], 1);  mbar_init(&o_free[s], 4);
@@ -242,28 +263,27 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
     mbar_init(quarters, 4);
     mbar_init(done, 1);
     if (BYTES) {
-      mbar_init(q_ready, kPmWiden / 32);
-      for (int s = 0; s < kPmScales; ++s) mbar_init(&sc_full[s], kPmWiden / 32);
+      for (int s = 0; s < SM::NR; ++s) { mbar_init(&r_full[s], 1);  mbar_init(&r_empty[s], 1); }
+      for (int s = 0; s < kPmScales; ++s) mbar_init(&sc_full[s], 1);
     }
-    for (int s = 0; s < kPmSegs; ++s) { mbar_init(&seg_full[s], 1);  mbar_init(&seg_empty[s], BYTES ? 14 : 11); }   // K, V (queries, four that widen), MMA and eight softmax warps
+    for (int s = 0; s < kPmSegs; ++s) { mbar_init(&seg_full[s], 1);  mbar_init(&seg_empty[s], 11); }   // K, V, MMA and eight softmax warps
     mbar_init_done();
     *abort_flag = 0;
-    if (!BYTES) asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
-    if (!BYTES) asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+    if (!BYTES) asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
   }
   if (warp == 1) tmem_alloc(tmem_base_s, kPmTmemCols);
   pdl_wait();
   pdl_launch_dependents();
   tc_fence_before();
-  const long long share = paged_share(a.w, paged_fill_seqs(a, seqs, tid, THREADS));   // (ends with a barrier)
+  const long long share = paged_share(a.w, paged_fill_seqs(a, seqs, tid, kPmThreads));   // (ends with a barrier)
   tc_fence_after();
   const uint32_t tmem = *tmem_base_s;
   const uint32_t sbase = smem_u32(smem);
   const int lim = a.wait_limit;
   const int ppos = a.w.ppos, G = a.pl.G;
   PmSeg* segs = reinterpret_cast<PmSeg*>(smem + SM::kSegs);
-  auto seg_at = [&](const PmSeg& sg) { return (int)(&sg - segs); };   // place of a segment: free again when every role is done with it
   // The CTA's segments, one after the other: the body returns false to give up.
   auto each_segment = [&](bool& ok, auto body) {
 #pragma unroll 1
@@ -278,8 +298,103 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
   };
 
   if (wg == 0) {
-    warpgroup_reg_dec<BYTES ? 64 : 120>();                        // (120 + 2 x 192 = 3 x 168, 64 + 80 + 2 x 184 = 4 x 128: what the CTA is launched with)
-    if (BYTES && warp == 2) {
+    warpgroup_reg_dec<120>();                                     // (120 + 2 x 192 = 3 x 168, what the CTA is launched with)
+    if (BYTES && (warp == 0 || warp == 2)) {
+      if (warp == 0) {
+        // ---------------------------------------------------------- 8-bit pages: TMA of K and V, scales ---------------------
+        // Lane 8 u + i knows block i of the group's tile u: its cache row and scales, which come a group of four tiles ahead (a byte of a scale comes from
+        // memory like anything else, behind the page's number).  Boxes: lane i of K, 8 + i of V, where a page starts.
+        const int i8 = lane & 7, P = a.pl.P;
+        const bool is_v = lane & 8, boxes = lane < 16 && (16 * i8 & (P - 1)) == 0;
+        const uint32_t dst = sbase + (is_v ? SM::kR : SM::kK) + 16 * i8 * D;
+        const CUtensorMap* map = is_v ? &map_v : &map_k;
+        const int n_rows = (int)((long long)a.pl.n_pages * a.pl.page_stride);   // (a box there reads zeros)
+        float4* scales = reinterpret_cast<float4*>(smem + SM::kScales);
+        int kt = 0, k_more = 0;                                   // tiles under way; one of K more
+        bool ok = true;
+        each_segment(ok, [&](const PmSeg& sg) {
+          const int A = sg.pl.A, E = sg.pl.E;
+          auto find = [&](int t0) {                               // cache row of this lane's block of the group from t0 on, -1: none
+            const int t = t0 + (lane >> 3), tok = (t < sg.ns ? t : t + sg.skip) * kPmKeys + 16 * i8;
+            if (t >= E || tok >= sg.L) return -1;
+            const long long r = paged_row(a.pb, a.pl, sg.b, sg.h, tok >> a.pl.log_p);
+            return r < 0 ? -1 : (int)(r + (tok & (P - 1)));
+          };
+          auto exponent = [&](const unsigned char* from, int row) { return row < 0 ? 0 : paged_exponent(from + (row >> 4)); };
+          int row = find(A), row1 = find(A + 4), ek = exponent(a.k_scales, row), ev = exponent(a.v_scales, row);
+#pragma unroll 1
+          for (int t0 = A; t0 < E; t0 += 4) {
+            const int row2 = find(t0 + 8), ek1 = exponent(a.k_scales, row1), ev1 = exponent(a.v_scales, row1);
+#pragma unroll 1
+            for (int u = 0; u < min(4, E - t0); ++u, ++kt) {
+              const int sk = kt % NK, sr = kt % SM::NR, r = __shfl_sync(0xffffffffu, row, 8 * u + i8);
+              if (kt >= NK && !pm_wait(&k_empty[sk], ((kt / NK) - 1) & 1, lim, abort_flag)) return false;
+              if (lane >> 3 == u) scales[(kt % kPmScales) * 8 + i8] = make_float4(power_of_two(ek), (float)ev, power_of_two(-ev), 0.f);   // (free: see kPmScales)
+              __syncwarp();
+              if (lane == 0) {
+                mbar_arrive1(&sc_full[kt % kPmScales]);
+                mbar_expect_tx(&k_full[sk], SM::kRaw + (uint32_t)a.dbg_tx_extra);
+              }
+              __syncwarp();
+              if (boxes && !is_v) tma_load_box(dst + sk * SM::kRaw, map, 0, r < 0 ? n_rows : r, &k_full[sk]);
+              // (K is counted as under way from here on, V from its own)
+              if (kt >= SM::NR && !pm_wait(&r_empty[sr], ((kt / SM::NR) - 1) & 1, lim, abort_flag)) { k_more = 1; return false; }
+              if (lane == 0) mbar_expect_tx(&r_full[sr], SM::kRaw + (uint32_t)a.dbg_tx_extra);
+              __syncwarp();
+              if (boxes && is_v) tma_load_box(dst + sr * SM::kRaw, map, 0, r < 0 ? n_rows : r, &r_full[sr]);
+            }
+            row = row1;
+            row1 = row2;
+            ek = ek1;
+            ev = ev1;
+          }
+          return true;
+        });
+        if (!ok) *abort_flag = 1;
+        // every copy has landed before the CTA leaves, whatever the other roles do
+        for (int x = max(0, kt + k_more - NK); x < kt + k_more; ++x) warp_waits(&k_full[x % NK], (x / NK) & 1, lim);
+        for (int x = max(0, kt - SM::NR); x < kt; ++x) warp_waits(&r_full[x % SM::NR], (x / SM::NR) & 1, lim);
+      } else {
+        // ---------------------------------------------------------- 8-bit pages: V as fp16, in which e4m3 is exact -----------
+        // (its scales stay out of the products: see the softmax.)  A lane takes 16 bytes of every fourth (or eighth) token; two rows x four pieces of one
+        // array are stored side by side: no bank twice.
+        constexpr int PIECES = D / 16, ROWS = 32 / PIECES;        // of a row; rows at a time
+        const int piece = D == 128 ? (lane & 3) + (lane >> 1 & 4) : lane & 3, r0 = D == 128 ? (lane >> 2 & 1) + (lane >> 3 & 2) : lane >> 2;
+        const int c0 = 2 * (piece & 3);
+        int kt = 0;
+        bool ok = true;
+        each_segment(ok, [&](const PmSeg& sg) {
+          const int A = sg.pl.A, E = sg.pl.E;
+#pragma unroll 1
+          for (int t = A; t < E; ++t, ++kt) {
+            const int st = kt % NV, sr = kt % SM::NR;
+            if (!pm_wait(&r_full[sr], (kt / SM::NR) & 1, lim, abort_flag)) return false;
+            if (kt >= NV && !pm_wait(&v_empty[st], ((kt / NV) - 1) & 1, lim, abort_flag)) return false;
+            const unsigned char* raw = smem + SM::kR + sr * SM::kRaw + r0 * D;
+            unsigned char* tile = smem + SM::kV + st * SM::kTile + (piece >> 2) * SM::kHalf + r0 * 128;
+#pragma unroll 8
+            for (int x = 0; x < kPmKeys / ROWS; ++x) {
+              const int at = ROWS * x, row = at + r0;
+              const uint4 w = *reinterpret_cast<const uint4*>(raw + at * D + ((D == 128 ? piece ^ (row & 7) : piece ^ (row >> 1 & 3)) << 4));
+              uint4 y0, y1;
+              widen(w.x, y0.x, y0.y);
+              widen(w.y, y0.z, y0.w);
+              widen(w.z, y1.x, y1.y);
+              widen(w.w, y1.z, y1.w);
+              *reinterpret_cast<uint4*>(tile + at * 128 + ((c0 ^ (row & 7)) << 4)) = y0;
+              *reinterpret_cast<uint4*>(tile + at * 128 + (((c0 + 1) ^ (row & 7)) << 4)) = y1;
+            }
+            proxy_fence();                                        // (tile written -> tensor core)
+            __syncwarp();
+            if (lane == 0) {
+              mbar_arrive1(&v_full[st]);
+              mbar_arrive1(&r_empty[sr]);
+            }
+          }
+          return true;
+        });
+        if (!ok) *abort_flag = 1;
+      }
     } else if (warp == 0 || warp == 2) {
       // ------------------------------------------------------------ TMA: queries and K, or V ----------------------------
       const bool is_k = warp == 0;
@@ -302,7 +417,7 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
           if (lane < boxes && t < pl.E && index * P < L) r = paged_row(a.pb, a.pl, b, h, index);
           return r < 0 ? n_rows : (int)r;
         };
-        int row = BYTES ? 0 : box_row(pl.A);
+        int row = box_row(pl.A);
         if (is_k) {
           if (seg > 0 && !pm_wait(q_empty, (seg - 1) & 1, lim, abort_flag)) return false;
           if (lane == 0) {
@@ -316,7 +431,7 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
           }
         }
         ++seg;
-        for (int t = pl.A; !BYTES && t < pl.E; ++t) {
+        for (int t = pl.A; t < pl.E; ++t) {
           const int row_next = box_row(t + 1);
           const int st = kt % NS;
           if (kt >= NS && !pm_wait(&empty[st], ((kt / NS) - 1) & 1, lim, abort_flag)) return false;
@@ -334,14 +449,15 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
       if (is_k && seg > 0) warp_waits(q_full, (seg - 1) & 1, lim);
     } else if (warp == 1) {
       // ------------------------------------------------------------ MMA issuer -----------------------------------------
-      constexpr uint32_t id_s = umma_idesc(!BYTES, false, false, 128, kPmKeys);
+      constexpr uint32_t id_s = BYTES ? umma_idesc8(0, 0, 128, kPmKeys) : umma_idesc(true, false, false, 128, kPmKeys);
+      constexpr uint32_t id_s_low = umma_idesc8(1, 0, 128, kPmKeys);   // BYTES: of the queries' second part, e5m2
       constexpr uint32_t id_o = umma_idesc(!BYTES, false, true, 128, D);
       constexpr uint32_t kStep = 2048 / 16;                       // 16 keys of V
       const uint32_t one = elect_one();                           // (the whole warp runs this loop: see umma_ss_one)
       const uint32_t q_lo = umma_desc_lo(sbase + SM::kQ, 16), k_lo = umma_desc_lo(sbase + SM::kK, 16), v_lo = umma_desc_lo(sbase + SM::kV, SM::kHalf);
       bool ok = true;
       uint32_t kt = 0;
-      int seg = 0;
+      int seg = 0, n_q0 = 0, n_q1 = 0;
       uint32_t n_p0 = 0, n_p1 = 0, n_o0 = 0, n_o1 = 0;            // items whose P was awaited, segments that used O
       // the item of either row tile whose product with V is to come: its stage and phase, whether it is the segment's first, its number
       // there, whether V is free after it, whether the softmax warps may have formed it
@@ -377,9 +493,16 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
       auto score = [&](auto slot_c, const PmPlan& pl, int t, bool last) {   // S = Q K^T
         constexpr int S = decltype(slot_c)::value;
         if (S ? pend1 : pend0) product(slot_c);                   // (S takes the place of the P before)
-        const uint32_t q = q_lo + (FEW || pl.single ? 0 : S * (SM::kTile / 16)), k = k_lo + kt % NK * (SM::kTile / 16);
+        const uint32_t q = q_lo + (FEW || pl.single ? 0 : S * (SM::kTile / 16)), k = k_lo + kt % NK * (SM::kKTile / 16);
+        if constexpr (BYTES && D == 128) {                        // 32 channels a step: the first part's array, the second's
+          umma8_ss4_one<kUmmaDescHi>(one, tmem + S * 128, q, q + 2, q + 4, q + 6, k, k + 2, k + 4, k + 6, id_s, id_s, 0u);
+          umma8_ss4_one<kUmmaDescHi>(one, tmem + S * 128, q + SM::kRaw / 16, q + SM::kRaw / 16 + 2, q + SM::kRaw / 16 + 4, q + SM::kRaw / 16 + 6, k, k + 2, k + 4, k + 6, id_s_low, id_s_low, 1u);
+        } else if constexpr (BYTES) {                             // both parts in a row of 128 bytes
+          umma8_ss4_one<kUmmaDescHi64>(one, tmem + S * 128, q, q + 2, q + 4, q + 6, k, k + 2, k, k + 2, id_s, id_s_low, 0u);
+        } else {
 #pragma unroll
-        for (int x = 0; x < H; ++x) umma_ss4_one<2, 2>(one, tmem + S * 128, q + x * (SM::kHalf / 16), k + x * (SM::kHalf / 16), id_s, x > 0);
+          for (int x = 0; x < H; ++x) umma_ss4_one<2, 2>(one, tmem + S * 128, q + x * (SM::kHalf / 16), k + x * (SM::kHalf / 16), id_s, x > 0);
+        }
         umma_commit_one(one, &s_full[S]);
         if (last) umma_commit_one(one, &k_empty[kt % NK]);
         (S ? pend1 : pend0) = true;
@@ -391,8 +514,19 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
       each_segment(ok, [&](const PmSeg& sg) {
         const PmPlan pl = sg.pl;
         if (pl.A >= pl.E) return true;
-        if (!pm_wait(BYTES ? q_ready : q_full, seg & 1, lim, abort_flag)) return false;
-        ++seg;
+        if constexpr (BYTES) {
+          if (pl.items(0) > 0) {
+            if (!pm_wait(&q_ready[0], n_q0 & 1, lim, abort_flag)) return false;
+            ++n_q0;
+          }
+          if (!pl.single && pl.items(1) > 0) {
+            if (!pm_wait(&q_ready[1], n_q1 & 1, lim, abort_flag)) return false;
+            ++n_q1;
+          }
+        } else {
+          if (!pm_wait(q_full, seg & 1, lim, abort_flag)) return false;
+          ++seg;
+        }
         first0 = first1 = true;
         it0 = it1 = 0;
 #pragma unroll 1
@@ -411,7 +545,7 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
           if (!ok) return false;
           ++kt;
         }
-        umma_commit_one(one, q_empty);
+        if (!BYTES) umma_commit_one(one, q_empty);
         if (pend0) product(s0);
         if (ok && pend1) product(s1);
         return ok;
@@ -446,119 +580,9 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
       }
       if (a.w.cuts && lane == 0) a.w.cuts[blockIdx.x] = cut;
     }
-  } else if (BYTES && wg == 3) {
-    // -------------------------------------------------------------- 8-bit pages: tiles as fp16, by way of registers ---------
-    // e4m3 is exact in fp16; the scales stay out of the products (see the softmax).  A thread takes 16 bytes of every 16 (or 32) tokens; the next tile's
-    // are under way as soon as its registers are free.  Two rows x four pieces of one half are stored side by side: no bank twice.
-    warpgroup_reg_dec<80>();
-    constexpr int PIECES = D / 16, NX = kPmKeys * PIECES / kPmWiden;
-    const int thr = tid - kPmThreads, piece = D == 128 ? (lane & 3) + (lane >> 1 & 4) : lane & 3;
-    const int r16 = D == 128 ? (lane >> 2 & 1) + (lane >> 3 & 2) + 4 * (warp & 3) : thr / PIECES % 16, b_odd = D == 128 ? 0 : thr / PIECES / 16;
-    const int half = (piece >> 2) * SM::kHalf, c0 = 2 * (piece & 3);
-    bool ok = true;
-    int kt = 0, seg = 0;
-    each_segment(ok, [&](const PmSeg& sg) {
-      const int A = sg.pl.A, E = sg.pl.E, L = sg.L, b = sg.b, h = sg.h;
-      if (A >= E) return true;
-      auto first_tok = [&](int t) { return (t < sg.ns ? t : t + sg.skip) * kPmKeys; };
-      // lane i (mod 8): cache row of a tile's block i, -1: none; a tile ahead
-      auto find = [&](int t) {
-        const int tok = first_tok(t) + 16 * (lane & 7);
-        if (t >= E || tok >= L) return -1;
-        const long long r = paged_row(a.pb, a.pl, b, h, tok >> a.pl.log_p);
-        return r < 0 ? -1 : (int)(r + (tok & (a.pl.P - 1)));
-      };
-      uint4 raw[NX];
-      auto load = [&](int x, const unsigned char* pages, int row, int t) {
-        const int block = D == 128 ? x : 2 * x + b_odd, r = __shfl_sync(0xffffffffu, row, block);
-        raw[x] = make_uint4(0u, 0u, 0u, 0u);
-        if (r >= 0 && first_tok(t) + 16 * block + r16 < L) raw[x] = *reinterpret_cast<const uint4*>(pages + (long long)(r + r16) * D + piece * 16);
-      };
-      auto store = [&](int x, unsigned char* tile) {
-        const int at = 16 * (D == 128 ? x : 2 * x + b_odd) + r16;
-        uint4 y0, y1;
-        widen(raw[x].x, y0.x, y0.y);
-        widen(raw[x].y, y0.z, y0.w);
-        widen(raw[x].z, y1.x, y1.y);
-        widen(raw[x].w, y1.z, y1.w);
-        *reinterpret_cast<uint4*>(tile + half + at * 128 + ((c0 ^ (at & 7)) << 4)) = y0;
-        *reinterpret_cast<uint4*>(tile + half + at * 128 + ((c0 + 1 ^ (at & 7)) << 4)) = y1;
-      };
-      auto filled = [&](uint64_t* full) {
-        proxy_fence();                                            // (tile written -> tensor core)
-        __syncwarp();
-        if (lane == 0) mbar_arrive1(full);
-      };
-      // (scales a tile ahead, the first warp)
-      auto exponent = [&](int row) { return row < 0 || lane >= 16 ? 0 : paged_exponent((lane & 8 ? a.v_scales : a.k_scales) + (row >> 4)); };
-      int row = find(A), row_next = find(A + 1), e = (warp & 3) == 0 ? exponent(row) : 0;
-#pragma unroll
-      for (int x = 0; x < NX; ++x) load(x, a.k_bytes, row, A);
-      // queries: rows scaled to below 2^15 and rounded to fp16, in their places; a thread a row
-      if (!pm_wait(q_full, seg & 1, lim, abort_flag)) return false;
-      ++seg;
-      for (int s = 0; s < (FEW || sg.pl.single || sg.pl.items(1) == 0 ? 1 : 2); ++s) {
-        unsigned char* qr = smem + SM::kQ + s * SM::kTile + thr * 128;
-        float top = 0.f;
-#pragma unroll 4
-        for (int c = 0; c < 8 * H; ++c) {
-          const uint4 v = *reinterpret_cast<const uint4*>(qr + (c >> 3) * SM::kHalf + (((c & 7) ^ (thr & 7)) << 4));
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float lo = fabsf(bf16_lo(w[i])), hi = fabsf(bf16_hi(w[i]));
-            if (lo < INFINITY) top = fmaxf(top, lo);
-            if (hi < INFINITY) top = fmaxf(top, hi);
-          }
-        }
-        const int e = top > 0.f ? max((__float_as_int(top) >> 23) - 127 - 14, -100) : 0;
-        const float mul = power_of_two(-e);
-#pragma unroll 4
-        for (int c = 0; c < 8 * H; ++c) {
-          uint4* at = reinterpret_cast<uint4*>(qr + (c >> 3) * SM::kHalf + (((c & 7) ^ (thr & 7)) << 4));
-          const uint4 v = *at;
-          *at = make_uint4(pack_f16(bf16_lo(v.x) * mul, bf16_hi(v.x) * mul), pack_f16(bf16_lo(v.y) * mul, bf16_hi(v.y) * mul),
-                           pack_f16(bf16_lo(v.z) * mul, bf16_hi(v.z) * mul), pack_f16(bf16_lo(v.w) * mul, bf16_hi(v.w) * mul));
-        }
-        reinterpret_cast<short*>(smem + SM::kQe)[(seg_at(sg) * 2 + s) * 128 + thr] = (short)e;
-      }
-      filled(q_ready);
-#pragma unroll 1
-      for (int t = A; t < E; ++t, ++kt) {
-        const int row_later = find(t + 2), e_next = (warp & 3) == 0 ? exponent(row_next) : 0;
-        int st = kt % NK;
-        if (kt >= NK && !pm_wait(&k_empty[st], ((kt / NK) - 1) & 1, lim, abort_flag)) return false;
-        if ((warp & 3) == 0) {                                    // (free: see kPmScales)
-          const int ev = __shfl_sync(0xffffffffu, e, 8 + (lane & 7));
-          if (lane < 8)
-            reinterpret_cast<float4*>(smem + SM::kScales)[(kt % kPmScales) * 8 + lane] = make_float4(power_of_two(e), (float)ev, power_of_two(-ev), 0.f);
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive1(&sc_full[kt % kPmScales]);    // (all four: behind the exponents of the queries)
-#pragma unroll
-        for (int x = 0; x < NX; ++x) {
-          store(x, smem + SM::kK + st * SM::kTile);
-          load(x, a.v_bytes, row, t);
-        }
-        filled(&k_full[st]);
-        st = kt % NV;
-        if (kt >= NV && !pm_wait(&v_empty[st], ((kt / NV) - 1) & 1, lim, abort_flag)) return false;
-#pragma unroll
-        for (int x = 0; x < NX; ++x) {
-          store(x, smem + SM::kV + st * SM::kTile);
-          load(x, a.k_bytes, row_next, t + 1);
-        }
-        filled(&v_full[st]);
-        row = row_next;
-        row_next = row_later;
-        e = e_next;
-      }
-      return true;
-    });
-    if (!ok) *abort_flag = 1;
   } else {
     // -------------------------------------------------------------- softmax and epilogue: one row per thread -------------
-    warpgroup_reg_inc<BYTES ? 184 : 192>();
+    warpgroup_reg_inc<192>();
     const int slot = wg - 1, thr = tid - 128 * wg, row = FEW ? lane : thr, pi = row / G, g = row % G;
     constexpr int KEYS = FEW ? 32 : kPmKeys;                      // keys of a tile that a thread takes
     const int kb = FEW ? 32 * (warp & 3) : 0;                     // the first of them
@@ -604,6 +628,53 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
       const bool counts = valid || alike;
       const int lo_most = __reduce_max_sync(0xffffffffu, counts ? see.lo : 0), hi_least = __reduce_min_sync(0xffffffffu, counts ? see.hi : 0x7fffffff);
       float up = 0.f;                                              // BYTES: 2^(exponent of the row's queries)
+      if constexpr (BYTES) {
+        // The row's queries, scaled by a power of two to below 448, as e4m3 and what that leaves as e5m2: bf16's eight bits as four and three and their signs, exactly
+        // down to 2^-14 of the row's largest channel, within 2^-22 of it below.  (The products with the row tile's queries before are through: this
+        // warpgroup has had their scores, or word of the other's.)
+        if (my > 0) {
+          const bool bring = FEW || single ? slot == 0 : true, there = FEW ? row < ppos * G && sg.first + pi < sg.n : valid;
+          const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(a.q) + (sg.row0 + sg.first + (single || FEW ? 0 : slot * ppos) + pi) * a.q_stride +
+                                                          (long long)(sg.h * G + g) * D);
+          float top = 0.f;
+          bool finite = true;
+#pragma unroll 4
+          for (int c = 0; c < D / 8; ++c) {
+            const uint4 v = there ? q[c] : make_uint4(0u, 0u, 0u, 0u);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float lo = fabsf(bf16_lo(w[i])), hi = fabsf(bf16_hi(w[i]));
+              if (lo < INFINITY) top = fmaxf(top, lo); else finite = false;
+              if (hi < INFINITY) top = fmaxf(top, hi); else finite = false;
+            }
+          }
+          const int e = top > 0.f ? max((__float_as_int(top) >> 23) - 127 - 7, -100) : 0;
+          up = power_of_two(e);
+          if (bring) {
+            const float mul = power_of_two(-e);
+            unsigned char* to = smem + SM::kQ + (FEW || single ? 0 : slot * SM::kTile) + thr * 128;
+            finite = __all_sync(0xffffffffu, finite);
+#pragma unroll 2
+            for (int c = 0; c < D / 16; ++c) {                    // 16 channels: a piece of 16 bytes of either part
+              uint32_t part[2][4];
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const uint4 v = there ? q[2 * c + i] : make_uint4(0u, 0u, 0u, 0u);
+                split_e4m3(v.x, v.y, mul, finite, part[0][2 * i], part[1][2 * i]);
+                split_e4m3(v.z, v.w, mul, finite, part[0][2 * i + 1], part[1][2 * i + 1]);
+              }
+              // of heads of 128 the parts are arrays of their own, of 64 the halves of a row
+              unsigned char *t0 = to + ((c ^ (thr & 7)) << 4), *t1 = D == 128 ? t0 + SM::kRaw : to + ((c + 4 ^ (thr & 7)) << 4);
+              *reinterpret_cast<uint4*>(t0) = make_uint4(part[0][0], part[0][1], part[0][2], part[0][3]);
+              *reinterpret_cast<uint4*>(t1) = make_uint4(part[1][0], part[1][1], part[1][2], part[1][3]);
+            }
+            proxy_fence();                                        // (written -> tensor core)
+            __syncwarp();
+            if (lane == 0) mbar_arrive1(&q_ready[FEW || single ? 0 : slot]);
+          }
+        }
+      }
       float m = -INFINITY, l = 0.f, fd = 1.f;                      // fd: what the sums of drained tiles are behind the maximum
       int done_items = 0;
 #pragma unroll 1
@@ -676,8 +747,6 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
           const float mul = MODS ? 1.f : sc2;
           const float4* scales = scales_s + (uint32_t)(k_base + t) % kPmScales * 8;   // BYTES: 2^ek, ev, 2^-ev of every 16 keys
           if (BYTES && !pm_wait(&sc_full[(uint32_t)(k_base + t) % kPmScales], ((uint32_t)(k_base + t) / kPmScales) & 1, lim, abort_flag)) return false;
-          if (BYTES && done_items == 0)
-            up = power_of_two(reinterpret_cast<const short*>(smem + SM::kQe)[seg_at(sg) * 256 + (FEW ? lane : (single ? 0 : slot * 128) + thr)]);
           uint32_t r[KEYS];
           if constexpr (FEW) {
             tmem_ld32_async(tS + kb, r);
@@ -685,13 +754,15 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
           } else {
             tmem_ld128(tS, r);
           }
-          if constexpr (BYTES && MODS) {                          // scores as they would be of the queries and keys themselves
+          // 8-bit pages: a score of block c is r 2^(eq + ek), times the scale; a value stands for its fp16 times 2^ev, which goes into the weight:
+          // y = r c_c + ev, weight 2^(y - m).  (Under a cap, or with a distance: the scores first, ev behind those.)
+          if constexpr (BYTES) {
 #pragma unroll
             for (int c = 0; c < KEYS / 16; ++c) {
-              const float f = fminf(scales[c].x * up, 3e38f);
+              const float f = fminf(fmaxf(MODS ? scales[c].x * up : scales[c].x * sc2 * up, 1e-37f), 3e38f), add = MODS ? 0.f : scales[c].y;
 #pragma unroll
               for (int x = 16 * c; x < 16 * c + 16; x += 2) {
-                const float2 v = __fmul2_rn(make_float2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), make_float2(f, f));
+                const float2 v = __ffma2_rn(make_float2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), make_float2(f, f), make_float2(add, add));
                 r[x] = __float_as_uint(v.x);
                 r[x + 1] = __float_as_uint(v.y);
               }
@@ -737,6 +808,14 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
 #pragma unroll
               for (int x = 0; x < KEYS; ++x) r[x] = __float_as_uint(fmaf(-slope2, fabsf(d0 + (float)x), __uint_as_float(r[x])));
             }
+            if constexpr (BYTES) {
+#pragma unroll
+              for (int c = 0; c < KEYS / 16; ++c) {
+                const float add = scales[c].y;
+#pragma unroll
+                for (int x = 16 * c; x < 16 * c + 16; ++x) r[x] = __float_as_uint(__uint_as_float(r[x]) + add);
+              }
+            }
           }
           if (part) {
 #pragma unroll
@@ -748,25 +827,10 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
                 if (!(bits & (1u << x))) r[32 * c + x] = 0xff800000u;
             }
           }
-          // 8-bit pages: block c's scores are c_c r, a value stands for its fp16 times 2^ev, which goes into the weight: y = c_c r + ev, weight 2^(y - m)
-          auto factor = [&](int c) { return MODS ? 1.f : fminf(fmaxf(scales[c].x * sc2 * up, 1e-37f), 3e38f); };
-          float mt;
-          if constexpr (BYTES) {
-            mt = -INFINITY;
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int c = 0; c < KEYS / 16; ++c) {
-              float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-              for (int x = 16 * c; x < 16 * c + 16; x += 2) mx[x / 2 & 1] = max3(mx[x / 2 & 1], __uint_as_float(r[x]), __uint_as_float(r[x + 1]));
-              mt = fmaxf(mt, fmaf(fmaxf(mx[0], mx[1]), factor(c), scales[c].y));
-            }
-            mt -= kPmHead;
-          } else {
-            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int x = 0; x < KEYS; x += 2) mx[x / 2 & 3] = fmaxf(mx[x / 2 & 3], fmaxf(__uint_as_float(r[x]), __uint_as_float(r[x + 1])));
-            mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * mul;
-          }
+          for (int x = 0; x < KEYS; x += 2) mx[x / 2 & 3] = fmaxf(mx[x / 2 & 3], fmaxf(__uint_as_float(r[x]), __uint_as_float(r[x + 1])));
+          const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * (BYTES ? 1.f : mul) - (BYTES ? kPmHead : 0.f);
           // The first visible keys of a row set its maximum (its row of O is zero so far); later ones only move it when it would
           // let a probability exceed 2^8.
           const bool grow = mt > m + (BYTES ? kPmGrow : 8.f) && m > -INFINITY;
@@ -795,11 +859,10 @@ __global__ void __launch_bounds__(kPmThreads + (BYTES ? kPmWiden : 0), 1)
               uint32_t pk[16];
 #pragma unroll
               for (int y = 0; y < 2; ++y) {
-                const float f = factor(2 * c + y), add = scales[2 * c + y].y + nm;
                 float2 part = make_float2(0.f, 0.f);
 #pragma unroll
                 for (int x = 8 * y; x < 8 * y + 8; ++x) {
-                  const float2 v = __ffma2_rn(make_float2(__uint_as_float(r[32 * c + 2 * x]), __uint_as_float(r[32 * c + 2 * x + 1])), make_float2(f, f), make_float2(add, add));
+                  const float2 v = __fadd2_rn(make_float2(__uint_as_float(r[32 * c + 2 * x]), __uint_as_float(r[32 * c + 2 * x + 1])), make_float2(nm, nm));
                   const float2 p = make_float2(ex2(v.x), ex2(v.y));
                   part = __fadd2_rn(part, p);
                   pk[x] = pack_f16(p.x, p.y);
@@ -1093,7 +1156,7 @@ cudaError_t mma_variant(const PagedAttend& a, const PagedMaps& maps, cudaStream_
   static unsigned long long allowed = 0;
   cudaError_t e = allow_smem_once(kern, bytes, allowed);
   if (e != cudaSuccess) return e;
-  return launch_ex(kern, dim3(a.w.n_cta), dim3(kPmThreads + (BYTES ? kPmWiden : 0)), bytes, s, 0, true, a, *reinterpret_cast<const CUtensorMap*>(maps.k),
+  return launch_ex(kern, dim3(a.w.n_cta), dim3(kPmThreads), bytes, s, 0, true, a, *reinterpret_cast<const CUtensorMap*>(maps.k),
                    *reinterpret_cast<const CUtensorMap*>(maps.v), *reinterpret_cast<const CUtensorMap*>(maps.q));
 }
 template <int D, bool MODS, bool FEW, bool BYTES>

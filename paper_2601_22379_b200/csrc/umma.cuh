@@ -16,6 +16,11 @@ __host__ __device__ constexpr uint32_t umma_idesc(bool bf16, bool a_mn, bool b_m
          ((uint32_t)(N / 8) << 17) | ((uint32_t)(M / 16) << 24);
 }
 
+// kind::f8f6f4, operands of 8 bits, K-major: types at bits 7 (A) and 10 (B), 0 = e4m3, 1 = e5m2, each operand its own.  A step is 32 k: 32 bytes.
+__host__ __device__ constexpr uint32_t umma_idesc8(uint32_t a_type, uint32_t b_type, int M, int N) {
+  return (1u << 4) | (a_type << 7) | (b_type << 10) | ((uint32_t)(N / 8) << 17) | ((uint32_t)(M / 16) << 24);
+}
+
 // Shared-memory matrix descriptor of an operand stored as rows of 128 bytes with the 128-byte swizzle (atoms of 8 rows,
 // 1024-byte aligned): start address / 16, leading byte offset / 16 at bit 16, stride byte offset (between groups of 8
 // rows) / 16 at bit 32, descriptor version 1 at bit 46, layout type 2 at bit 61.
@@ -26,6 +31,7 @@ __host__ __device__ constexpr uint32_t umma_idesc(bool bf16, bool a_mn, bool b_m
 // In two words, for loops that step through an operand: the low word grows by bytes / 16 (shared memory ends below the 18
 // bits that the address field covers, so it never carries), the high word is the same for all.
 constexpr uint32_t kUmmaDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+constexpr uint32_t kUmmaDescHi64 = (512u >> 4) | (1u << 14) | (4u << 29);   // rows of 64 bytes with the 64-byte swizzle
 __device__ __forceinline__ uint32_t umma_desc_lo(uint32_t smem_addr, uint32_t lead_bytes) { return (smem_addr >> 4) | ((lead_bytes >> 4) << 16); }
 __device__ __forceinline__ uint64_t umma_desc_of(uint32_t lo) { return ((uint64_t)kUmmaDescHi << 32) | lo; }
 
@@ -56,6 +62,23 @@ __device__ __forceinline__ void umma_ss4_one(uint32_t one, uint32_t tmem_d, uint
       ::"r"(tmem_d), "l"(umma_desc_of(lo_a)), "l"(umma_desc_of(lo_a + DA)), "l"(umma_desc_of(lo_a + 2 * DA)), "l"(umma_desc_of(lo_a + 3 * DA)),
         "l"(umma_desc_of(lo_b)), "l"(umma_desc_of(lo_b + DB)), "l"(umma_desc_of(lo_b + 2 * DB)), "l"(umma_desc_of(lo_b + 3 * DB)),
         "r"(idesc), "r"(accumulate), "r"(0u), "r"(one)
+      : "memory");
+}
+// ... kind::f8f6f4: four steps with descriptors of their own, A in rows of 128 bytes, B as HI_B says; the first two of type id0, the others of id1.
+template <uint32_t HI_B>
+__device__ __forceinline__ void umma8_ss4_one(uint32_t one, uint32_t tmem_d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1,
+                                              uint32_t b2, uint32_t b3, uint32_t id0, uint32_t id1, uint32_t accumulate) {
+  const uint64_t hi_b = (uint64_t)HI_B << 32;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %11, 0;\n\t"
+      "setp.ne.b32 q, %13, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %5, %9, {%12, %12, %12, %12}, p;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %2, %6, %9, {%12, %12, %12, %12}, 1;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %3, %7, %10, {%12, %12, %12, %12}, 1;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %4, %8, %10, {%12, %12, %12, %12}, 1;\n\t}"
+      ::"r"(tmem_d), "l"(umma_desc_of(a0)), "l"(umma_desc_of(a1)), "l"(umma_desc_of(a2)), "l"(umma_desc_of(a3)),
+        "l"(hi_b | b0), "l"(hi_b | b1), "l"(hi_b | b2), "l"(hi_b | b3), "r"(id0), "r"(id1), "r"(accumulate), "r"(0u), "r"(one)
       : "memory");
 }
 // ... with A in tensor memory (row m in lane m, two 16-bit k per 32-bit column), DA columns further per step.
