@@ -174,7 +174,8 @@ struct PagedAttend {
   int wait_limit, dbg_tx_extra;         // as in Params
   int sinks;                            // so many first tokens are visible besides the window
   int from_new, to_new;                 // sequences of so many new tokens are this launch's (0, 0: all of them); the others are passed over
-  const unsigned char *k_bytes, *v_bytes, *k_scales, *v_scales;   // 8-bit pages
+  const unsigned char *k_scales, *v_scales;   // of 8-bit pages
+  const signed char* q_exp;             // exponents of the queries' rows, where paged_split.cu has scaled them
 };
 
 // Sequence table of a CTA, in shared memory.
@@ -479,6 +480,9 @@ cudaError_t launch_paged_join(const PagedAttend& a, int out_bf16, cudaStream_t s
 int paged_few_positions(const PagedLayout& pl);   // new tokens of a sequence that it takes, at most
 void paged_plan_few(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int sm_count);
 cudaError_t launch_paged_few(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s);
+// paged_split.cu: bf16 queries as two parts of 8 bits, [token][head][part][d], and the exponents of the rows' scales [token][head]
+size_t paged_split_bytes(const PagedLayout& pl, int total_new, size_t* exps);
+cudaError_t launch_paged_split(const PagedLayout& pl, const void* q, long long q_stride, int total_new, unsigned char* parts, signed char* exps, cudaStream_t s);
 // paged_mma.cu: bf16 on tcgen05
 size_t paged_mma_drain_bytes(const PagedWork& w, const PagedBatch& pb, const PagedLayout& pl);
 int paged_mma_positions(const PagedBatch& pb, const PagedLayout& pl);   // new tokens of a row tile: the query boxes' size

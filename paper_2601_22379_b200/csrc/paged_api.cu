@@ -295,13 +295,15 @@ enum PagedKernel { kGeneral, kTensor, kFew, kTensorBytes };
 
 // The plan of one launch (a batch of at most kPagedMaxBatch sequences), the bytes of its partial results and of the sums of long walks,
 // and their places in the workspace, where there is one (no cuts: whole units only).
+// (8-bit pages: where a sequence may have more rows than the kernel for few takes, the queries' parts lie in front, the same for all launches of a call.)
 static size_t plan_attend(const spla_paged* p, PagedBatch pb, PagedKernel kernel, PagedWork* w, void* workspace) {
-  const bool tensor = kernel == kTensor || kernel == kTensorBytes;
+  const bool tensor = kernel == kTensor || kernel == kTensorBytes, parts = (kernel == kFew || kernel == kTensorBytes) && pb.max_new > paged_few_positions(p->pl);
   if (kernel == kFew && pb.max_new > paged_few_positions(p->pl)) pb.max_new = paged_few_positions(p->pl);   // (the others are another launch's)
   if (tensor) paged_plan_mma(w, pb, p->pl, p->sm_count);
   else if (kernel == kFew) paged_plan_few(w, pb, p->pl, p->sm_count);
   else paged_plan_general(w, pb, p->pl, p->sm_count);
-  size_t used = 0;
+  size_t used = 0, exps;
+  if (parts) used = align_up(paged_split_bytes(p->pl, pb.total_new, &exps), 256);
   auto take = [&](size_t bytes) {
     char* at = workspace ? reinterpret_cast<char*>(workspace) + used : nullptr;
     used += align_up(bytes, 256);
@@ -325,7 +327,8 @@ static PagedBatch part_of(PagedBatch b, int first) {
   return b;
 }
 
-// The queries as [token][head][half of 64 channels], boxes of G heads x the tokens of a row tile: its rows, in their order.
+// The queries as [token][head][half of 64 channels], boxes of G heads x the tokens of a row tile: its rows, in their order.  (The parts of paged_split.cu lie
+// the same way: 2 d bytes a head, in pieces of 128.)
 static bool make_q_map(void* out128, const void* q, const PagedLayout& pl, int64_t q_stride, const PagedBatch& pb) {
   return make_tile_map_4d(out128, const_cast<void*>(q), 64u, (unsigned)(pl.d / 64), (unsigned)pl.Hq, (unsigned)pb.total_new, 128ull, (unsigned long long)pl.d * 2,
                           (unsigned long long)q_stride * 2, (unsigned)pl.G, (unsigned)paged_mma_positions(pb, pl));
@@ -395,8 +398,6 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
   a.wait_limit = p->wait_limit;
   a.dbg_tx_extra = p->dbg_tx_extra;
   const PagedBatch pb = device_batch(batch);
-  a.k_bytes = reinterpret_cast<const unsigned char*>(p->pages.k);
-  a.v_bytes = reinterpret_cast<const unsigned char*>(p->pages.v);
   a.k_scales = p->pages.k_scales;
   a.v_scales = p->pages.v_scales;
   const int q16 = p->cfg.q_dtype == SPLA_BF16;
@@ -404,8 +405,9 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
   cudaError_t e = cudaSuccess;
   PagedMaps maps;
   const bool rows16 = aligned(q, 16) && q_stride % 8 == 0, few = p->few && rows16;
-  const bool tensor = (p->tensor || (few && pb.max_new > paged_few_positions(p->pl))) && rows16 && cap_fits(p->cfg.sm_scale, mask->softcap) &&
-                      make_q_map(maps.q, q, p->pl, q_stride, pb);
+  const bool parts = few && pb.max_new > paged_few_positions(p->pl);               // some sequences may have more rows: their queries in two parts
+  const bool tensor = (p->tensor || parts) && rows16 && cap_fits(p->cfg.sm_scale, mask->softcap) &&
+                      make_q_map(maps.q, parts ? workspace : q, p->pl, parts ? q_row : q_stride, pb);
   if (tensor || few) {
     memcpy(maps.k, p->maps.k, sizeof(maps.k));
     memcpy(maps.v, p->maps.v, sizeof(maps.v));
@@ -424,13 +426,20 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
     }
     if (e == cudaSuccess) e = launch_paged_join(a, q16, s);
   };
+  if (parts && tensor) {
+    size_t exps;
+    paged_split_bytes(p->pl, pb.total_new, &exps);
+    unsigned char* at = reinterpret_cast<unsigned char*>(workspace);
+    a.q_exp = reinterpret_cast<signed char*>(at + exps);
+    e = launch_paged_split(p->pl, q, q_stride, pb.total_new, at, reinterpret_cast<signed char*>(at + exps), s);
+  }
   for (int first = 0; first < batch->batch && e == cudaSuccess; first += kPagedMaxBatch) {
     a.pb = part_of(pb, first);
     a.prefix = mask->prefix_lens ? mask->prefix_lens + first : nullptr;
     if (few) {                                                                     // two launches where a sequence may have more rows
       const int most = paged_few_positions(p->pl);
       launch(kFew, 0, most);
-      if (a.pb.max_new > most) launch(tensor ? kTensorBytes : kGeneral, most + 1, 0x7fffffff);
+      if (parts) launch(tensor ? kTensorBytes : kGeneral, most + 1, 0x7fffffff);
     } else {
       launch(tensor ? kTensor : kGeneral, 0, 0);
     }

@@ -156,25 +156,6 @@ __device__ __forceinline__ uint32_t pair_not_finite(uint32_t w) { return ((w & 0
 __device__ __forceinline__ uint32_t pair_not_finite_f16(uint32_t w) { return ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u; }
 __device__ __forceinline__ float f16_lo(uint32_t w) { return __low2float(*reinterpret_cast<const __half2*>(&w)); }
 __device__ __forceinline__ float f16_hi(uint32_t w) { return __high2float(*reinterpret_cast<const __half2*>(&w)); }
-// Four bf16 values times `mul` (a power of two) as four e4m3 and, of what that leaves, four e5m2.  An infinity is left to the second type, which has one.
-__device__ __forceinline__ void split_e4m3(uint32_t w0, uint32_t w1, float mul, bool finite, uint32_t& first, uint32_t& second) {
-  float x[4] = {bf16_lo(w0) * mul, bf16_hi(w0) * mul, bf16_lo(w1) * mul, bf16_hi(w1) * mul};
-  uint32_t infinite = 0u;
-  if (!finite)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (fabsf(x[i]) == INFINITY) {
-        infinite |= (x[i] > 0.f ? 0x7cu : 0xfcu) << (8 * i);
-        x[i] = 0.f;
-      }
-  const uint32_t h = __nv_cvt_float2_to_fp8x2(make_float2(x[0], x[1]), __NV_SATFINITE, __NV_E4M3) |
-                     (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(x[2], x[3]), __NV_SATFINITE, __NV_E4M3) << 16;
-  uint32_t lo, hi;
-  widen(h, lo, hi);
-  first = h;
-  second = infinite | __nv_cvt_float2_to_fp8x2(make_float2(x[0] - f16_lo(lo), x[1] - f16_hi(lo)), __NV_SATFINITE, __NV_E5M2) |
-           (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(x[2] - f16_lo(hi), x[3] - f16_hi(hi)), __NV_SATFINITE, __NV_E5M2) << 16;
-}
 // 8-bit pages: a row's first maximum gets weight 2^11, later ones may grow to 2^15 before O is rescaled: fp16 holds weights to 2^-12 of themselves, and down to 2^-35 of
 // the largest (weights below, of 2^24 tokens at most, are 2^-12 of it together).
 constexpr float kPmHead = 11.f, kPmGrow = 4.f;
@@ -238,7 +219,6 @@ __global__ void __launch_bounds__(kPmThreads, 1)
            *s_full = q_empty + 1, *p_ready = s_full + 2, *pv_done = p_ready + 2, *o_free = pv_done + 2, *scanned = o_free + 2, *halves = scanned + 2,
            *quarters = halves + 1, *done = quarters + 1, *seg_full = done + 1, *seg_empty = seg_full + kPmSegs,
            *r_full = seg_empty + kPmSegs, *r_empty = r_full + SM::NR, *sc_full = r_empty + SM::NR;   // (the last three of 8-bit pages only)
-  uint64_t* q_ready = q_full;                                     // [2] of 8-bit pages: the softmax warps bring the queries of their row tiles (q_empty is not used)
   uint32_t* tmem_base_s = reinterpret_cast<uint32_t*>(smem + SM::kMisc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SM::kMisc + 4);
   volatile int* skip_pv = reinterpret_cast<volatile int*>(smem + SM::kMisc + 8);    // [2]: this product with V has been formed by the softmax warps
@@ -250,8 +230,8 @@ __global__ void __launch_bounds__(kPmThreads, 1)
   if (tid == 0) {
     for (int s = 0; s < NK; ++s) { mbar_init(&k_full[s], 1);  mbar_init(&k_empty[s], 1); }
     for (int s = 0; s < NV; ++s) { mbar_init(&v_full[s], 1);  mbar_init(&v_empty[s], 1); }
-    mbar_init(q_full, BYTES ? 4 : 1);
-    mbar_init(q_empty, BYTES ? 4 : 1);
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 1);
     for (int s = 0; s < 2; ++s) {
       mbar_init(&s_full[s], 1);  mbar_init(&p_ready[s], 4);
       mbar_init(&pv_done[s], 1);  mbar_init(&o_free[s], 4);
@@ -271,7 +251,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
     *abort_flag = 0;
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
-    if (!BYTES) asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
   }
   if (warp == 1) tmem_alloc(tmem_base_s, kPmTmemCols);
   pdl_wait();
@@ -297,6 +277,15 @@ __global__ void __launch_bounds__(kPmThreads, 1)
     }
   };
 
+  // The queries of a segment, by one thread.  (8-bit pages: their two parts are what the halves of a head are otherwise.)
+  auto copy_q = [&](const PmSeg& sg) {
+    const int boxes_q = FEW ? 4 : !sg.pl.single && sg.pl.items(1) > 0 ? 2 : 1;     // (four copies of the same rows, or the row tiles)
+    mbar_expect_tx(q_full, boxes_q * H * ppos * G * 128 + (uint32_t)a.dbg_tx_extra);
+    for (int s = 0; s < boxes_q; ++s)
+      for (int x = 0; x < H; ++x)
+        tma_load_q(sbase + SM::kQ + s * (FEW ? 32 * 128 : SM::kTile) + x * SM::kHalf, &map_q, x, sg.h * G, sg.row0 + sg.first + (FEW ? 0 : s * ppos), q_full);
+  };
+
   if (wg == 0) {
     warpgroup_reg_dec<120>();                                     // (120 + 2 x 192 = 3 x 168, what the CTA is launched with)
     if (BYTES && (warp == 0 || warp == 2)) {
@@ -310,10 +299,14 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         const CUtensorMap* map = is_v ? &map_v : &map_k;
         const int n_rows = (int)((long long)a.pl.n_pages * a.pl.page_stride);   // (a box there reads zeros)
         float4* scales = reinterpret_cast<float4*>(smem + SM::kScales);
-        int kt = 0, k_more = 0;                                   // tiles under way; one of K more
+        int kt = 0, k_more = 0, seg = 0;                          // tiles under way; one of K more
         bool ok = true;
         each_segment(ok, [&](const PmSeg& sg) {
           const int A = sg.pl.A, E = sg.pl.E;
+          if (A >= E) return true;
+          if (seg > 0 && !pm_wait(q_empty, (seg - 1) & 1, lim, abort_flag)) return false;
+          if (lane == 0) copy_q(sg);
+          ++seg;
           auto find = [&](int t0) {                               // cache row of this lane's block of the group from t0 on, -1: none
             const int t = t0 + (lane >> 3), tok = (t < sg.ns ? t : t + sg.skip) * kPmKeys + 16 * i8;
             if (t >= E || tok >= sg.L) return -1;
@@ -354,6 +347,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         // every copy has landed before the CTA leaves, whatever the other roles do
         for (int x = max(0, kt + k_more - NK); x < kt + k_more; ++x) warp_waits(&k_full[x % NK], (x / NK) & 1, lim);
         for (int x = max(0, kt - SM::NR); x < kt; ++x) warp_waits(&r_full[x % SM::NR], (x / SM::NR) & 1, lim);
+        if (seg > 0) warp_waits(q_full, (seg - 1) & 1, lim);
       } else {
         // ---------------------------------------------------------- 8-bit pages: V as fp16, in which e4m3 is exact -----------
         // (its scales stay out of the products: see the softmax.)  A lane takes 16 bytes of every fourth (or eighth) token; two rows x four pieces of one
@@ -420,15 +414,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         int row = box_row(pl.A);
         if (is_k) {
           if (seg > 0 && !pm_wait(q_empty, (seg - 1) & 1, lim, abort_flag)) return false;
-          if (lane == 0) {
-            const bool two = !pl.single && pl.items(1) > 0;
-            const int boxes_q = FEW ? 4 : two ? 2 : 1;             // (four copies of the same rows, or the row tiles)
-            mbar_expect_tx(q_full, boxes_q * H * ppos * G * 128 + (uint32_t)a.dbg_tx_extra);
-            for (int s = 0; s < boxes_q; ++s)
-              for (int x = 0; x < H; ++x)
-                tma_load_q(sbase + SM::kQ + s * (FEW ? 32 * 128 : SM::kTile) + x * SM::kHalf, &map_q, x, h * G,
-                           sg.row0 + sg.first + (FEW ? 0 : s * ppos), q_full);
-          }
+          if (lane == 0) copy_q(sg);
         }
         ++seg;
         for (int t = pl.A; t < pl.E; ++t) {
@@ -457,7 +443,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       const uint32_t q_lo = umma_desc_lo(sbase + SM::kQ, 16), k_lo = umma_desc_lo(sbase + SM::kK, 16), v_lo = umma_desc_lo(sbase + SM::kV, SM::kHalf);
       bool ok = true;
       uint32_t kt = 0;
-      int seg = 0, n_q0 = 0, n_q1 = 0;
+      int seg = 0;
       uint32_t n_p0 = 0, n_p1 = 0, n_o0 = 0, n_o1 = 0;            // items whose P was awaited, segments that used O
       // the item of either row tile whose product with V is to come: its stage and phase, whether it is the segment's first, its number
       // there, whether V is free after it, whether the softmax warps may have formed it
@@ -514,19 +500,8 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       each_segment(ok, [&](const PmSeg& sg) {
         const PmPlan pl = sg.pl;
         if (pl.A >= pl.E) return true;
-        if constexpr (BYTES) {
-          if (pl.items(0) > 0) {
-            if (!pm_wait(&q_ready[0], n_q0 & 1, lim, abort_flag)) return false;
-            ++n_q0;
-          }
-          if (!pl.single && pl.items(1) > 0) {
-            if (!pm_wait(&q_ready[1], n_q1 & 1, lim, abort_flag)) return false;
-            ++n_q1;
-          }
-        } else {
-          if (!pm_wait(q_full, seg & 1, lim, abort_flag)) return false;
-          ++seg;
-        }
+        if (!pm_wait(q_full, seg & 1, lim, abort_flag)) return false;
+        ++seg;
         first0 = first1 = true;
         it0 = it1 = 0;
 #pragma unroll 1
@@ -545,7 +520,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
           if (!ok) return false;
           ++kt;
         }
-        if (!BYTES) umma_commit_one(one, q_empty);
+        umma_commit_one(one, q_empty);
         if (pend0) product(s0);
         if (ok && pend1) product(s1);
         return ok;
@@ -628,52 +603,8 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       const bool counts = valid || alike;
       const int lo_most = __reduce_max_sync(0xffffffffu, counts ? see.lo : 0), hi_least = __reduce_min_sync(0xffffffffu, counts ? see.hi : 0x7fffffff);
       float up = 0.f;                                              // BYTES: 2^(exponent of the row's queries)
-      if constexpr (BYTES) {
-        // The row's queries, scaled by a power of two to below 448, as e4m3 and what that leaves as e5m2: bf16's eight bits as four and three and their signs, exactly
-        // down to 2^-14 of the row's largest channel, within 2^-22 of it below.  (The products with the row tile's queries before are through: this
-        // warpgroup has had their scores, or word of the other's.)
-        if (my > 0) {
-          const bool bring = FEW || single ? slot == 0 : true, there = FEW ? row < ppos * G && sg.first + pi < sg.n : valid;
-          const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(a.q) + (sg.row0 + sg.first + (single || FEW ? 0 : slot * ppos) + pi) * a.q_stride +
-                                                          (long long)(sg.h * G + g) * D);
-          float top = 0.f;
-          bool finite = true;
-#pragma unroll 4
-          for (int c = 0; c < D / 8; ++c) {
-            const uint4 v = there ? q[c] : make_uint4(0u, 0u, 0u, 0u);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float lo = fabsf(bf16_lo(w[i])), hi = fabsf(bf16_hi(w[i]));
-              if (lo < INFINITY) top = fmaxf(top, lo); else finite = false;
-              if (hi < INFINITY) top = fmaxf(top, hi); else finite = false;
-            }
-          }
-          const int e = top > 0.f ? max((__float_as_int(top) >> 23) - 127 - 7, -100) : 0;
-          up = power_of_two(e);
-          if (bring) {
-            const float mul = power_of_two(-e);
-            unsigned char* to = smem + SM::kQ + (FEW || single ? 0 : slot * SM::kTile) + thr * 128;
-            finite = __all_sync(0xffffffffu, finite);
-#pragma unroll 2
-            for (int c = 0; c < D / 16; ++c) {                    // 16 channels: a piece of 16 bytes of either part
-              uint32_t part[2][4];
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const uint4 v = there ? q[2 * c + i] : make_uint4(0u, 0u, 0u, 0u);
-                split_e4m3(v.x, v.y, mul, finite, part[0][2 * i], part[1][2 * i]);
-                split_e4m3(v.z, v.w, mul, finite, part[0][2 * i + 1], part[1][2 * i + 1]);
-              }
-              // of heads of 128 the parts are arrays of their own, of 64 the halves of a row
-              unsigned char *t0 = to + ((c ^ (thr & 7)) << 4), *t1 = D == 128 ? t0 + SM::kRaw : to + ((c + 4 ^ (thr & 7)) << 4);
-              *reinterpret_cast<uint4*>(t0) = make_uint4(part[0][0], part[0][1], part[0][2], part[0][3]);
-              *reinterpret_cast<uint4*>(t1) = make_uint4(part[1][0], part[1][1], part[1][2], part[1][3]);
-            }
-            proxy_fence();                                        // (written -> tensor core)
-            __syncwarp();
-            if (lane == 0) mbar_arrive1(&q_ready[FEW || single ? 0 : slot]);
-          }
-        }
+      if constexpr (BYTES) {                                       // (known when the first scores are there)
+        if (valid && my > 0) up = power_of_two(__ldg(a.q_exp + (long long)(sg.row0 + sg.first + (single ? 0 : slot * ppos) + pi) * a.pl.Hq + sg.h * G + g));
       }
       float m = -INFINITY, l = 0.f, fd = 1.f;                      // fd: what the sums of drained tiles are behind the maximum
       int done_items = 0;
