@@ -2,7 +2,7 @@
 //
 // A row is scaled by a power of two, so that its largest magnitude is in [128, 256); the first part is each channel rounded to e4m3, which takes the first four
 // of bf16's eight bits, the second what that leaves, as e5m2: three bits and a sign, all there is left down to 2^-14 of the row's largest channel,
-// within 2^-22 of it below.  Bound by memory: 4 bytes in and out per channel (a prompt of 8192 tokens, 32 heads of 128: @split).
+// within 2^-21 of it below.  Bound by memory: 4 bytes in and out per channel (a prompt of 8192 tokens, 32 heads of 128: @split).
 #include <cuda_fp8.h>
 
 #include "paged_tiles.cuh"
