@@ -11,6 +11,8 @@
 // rows meet in shared memory, and a second kernel adds the CTAs' sums in their order: no atomics, the same bits every time.
 // All arithmetic in fp32, one rounding at the end.
 // @figures
+#include <type_traits>
+
 #include "rope_device.cuh"
 
 namespace spla {
@@ -27,7 +29,7 @@ struct NormLaunch {
   int tokens, tb, tiles_per_batch;       // of a batch entry; per tile
   int tiles;                             // of all batch entries
   int rows_per_y;
-  unsigned head_magic[2];                // as in RopeLaunch
+  unsigned head_magic[3];                // as in RopeLaunch: of the queries' heads, the keys', all
   float eps, per_channel;
   int width;                             // lanes of a row
   float* part;                           // [CTAs][2][dim]: sums for the weights' gradients
@@ -36,8 +38,8 @@ struct NormLaunch {
 template <typename T, class ROW, bool BWD>
 __global__ void __launch_bounds__(kNormThreads, BWD ? 2 : 3)
     norm_kernel(const __grid_constant__ NormLaunch r, const __grid_constant__ RopeTable rt) {
-  constexpr int CH = ROW::CH, WORDS = ROW::WORDS, ROWS = BWD ? 1 : 2;   // rows that a thread has on their way at a time
-  constexpr bool loose = ROW::CH == ROW::WORDS && sizeof(ROW) == sizeof(LooseRow<T, CH>);
+  constexpr int CH = ROW::CH, WORDS = ROW::WORDS;
+  constexpr bool loose = sizeof(ROW) == sizeof(LooseRow<T, CH>);
   __shared__ __align__(16) float2 table[kNormTable];               // and the rows' sums for the weights, at the end
   __shared__ __align__(16) float w_s[2][kNormMaxDim];
   __shared__ float rows_s[loose ? kNormThreads / 32 : 1][loose ? kNormMaxDim : 1];
@@ -47,82 +49,148 @@ __global__ void __launch_bounds__(kNormThreads, BWD ? 2 : 3)
   const int width = r.width, by = kNormThreads / width, ty = tid / width;
   const ROW row(rt, tid % width);
   float* own_row = rows_s[loose ? tid / 32 : 0];
-  for (int x = tid; x < 2 * dim; x += kNormThreads) {
-    const int g = x >= dim;
-    if (r.g[g].n_heads > 0) w_s[g][x - g * dim] = __ldg(r.g[g].weight + x - g * dim);
-  }
-  float acc[2][BWD ? CH : 1];
-#pragma unroll
-  for (int i = 0; i < (BWD ? CH : 1); ++i) acc[0][i] = acc[1][i] = 0.f;
-  for (int tile = blockIdx.x; tile < r.tiles; tile += gridDim.x) {
-    const int b = tile / r.tiles_per_batch, tok0 = (tile - b * r.tiles_per_batch) * r.tb, nt = min(r.tb, r.tokens - tok0);
-    const int* pos = r.positions + (long long)b * r.tokens + tok0;
-    if (tile != (int)blockIdx.x) __syncthreads();                  // (the table before is used up)
-    fill_turns<ROW>(rt, table, nt, tid, kNormThreads, BWD, [&](int t) { return __ldg(pos + t); });
-    __syncthreads();
-    const int first = (int)blockIdx.y * r.rows_per_y, last = first + r.rows_per_y, n_q = nt * r.g[0].n_heads, n_all = n_q + nt * r.g[1].n_heads;
-    auto group = [&](const NormGroup& g, int gi, int from, int to, float (&sum)[BWD ? CH : 1]) {
-      if (from >= to) return;
-      const unsigned magic = r.head_magic[gi];
-      // (whole warps: a row's lanes meet in shuffles)
-#pragma unroll 1
-      for (int r0 = from; r0 < to; r0 += ROWS * by) {
-        uint32_t raw[ROWS][WORDS], raw_g[ROWS][BWD ? WORDS : 1];
-        int tk[ROWS];
-        T* out[ROWS];
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-          const int x = r0 + k * by + ty;
-          tk[k] = 0;
-          out[k] = nullptr;
-          if (x >= to || !row.here) continue;
-          const int t = g.n_heads == 1 ? x : (int)__umulhi((unsigned)x, magic), h = x - t * g.n_heads;
-          tk[k] = t;
-          const long long tok = tok0 + t;
-          row.load(reinterpret_cast<const T*>(g.x) + b * g.x_batch + tok * g.x_token + h * g.x_head, raw[k]);
-          if constexpr (BWD) row.load(reinterpret_cast<const T*>(g.dy) + b * g.dy_batch + tok * g.dy_token + h * g.dy_head, raw_g[k]);
-          out[k] = reinterpret_cast<T*>(g.out) + b * g.out_batch + tok * g.out_token + h * g.out_head;
-        }
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-          float x[CH];
-          row.values(raw[k], x);
-          if (!out[k])
-#pragma unroll
-            for (int i = 0; i < CH; ++i) x[i] = 0.f;
-          const float rms = row_rms(x, width, r.per_channel, r.eps);
-          const float2* tab = table + tk[k] * pairs;
-          float w[CH];
-          row.weights(w_s[gi], w);
-          if constexpr (!BWD) {
-#pragma unroll
-            for (int i = 0; i < CH; ++i) x[i] = x[i] * rms * w[i];
-            row.turn(x, tab, own_row);
-            if (out[k]) row.store(out[k], x);
-          } else {
-            float u[CH];
-            row.values(raw_g[k], u);
-            row.turn(u, tab, own_row);
-            float dot = 0.f;
-#pragma unroll
-            for (int i = 0; i < CH; ++i) {
-              if (!out[k]) u[i] = 0.f;
-              sum[i] = fmaf(u[i] * x[i], rms, sum[i]);
-              u[i] *= w[i];
-              dot = fmaf(u[i], x[i], dot);
-            }
-            dot = row_sum(dot, width) * r.per_channel * rms * rms;
-#pragma unroll
-            for (int i = 0; i < CH; ++i) u[i] = rms * (u[i] - x[i] * dot);
-            if (out[k]) row.store(out[k], u);
-          }
-        }
+  const int n0 = r.g[0].n_heads, n_all = n0 + r.g[1].n_heads;
+  struct Place {
+    int t, h, gi;                                                  // token of the tile, head, group; t < 0: none
+  };
+  int b = 0, tok0 = 0;
+  auto load = [&](const Place& p, uint32_t (&x)[WORDS], uint32_t (&g)[BWD ? WORDS : 1]) {
+    if (p.t < 0 || !row.here) return;
+    const NormGroup& gr = p.gi ? r.g[1] : r.g[0];
+    const long long tok = tok0 + p.t;
+    row.load(reinterpret_cast<const T*>(gr.x) + b * gr.x_batch + tok * gr.x_token + p.h * gr.x_head, x);
+    if constexpr (BWD) row.load(reinterpret_cast<const T*>(gr.dy) + b * gr.dy_batch + tok * gr.dy_token + p.h * gr.dy_head, g);
+  };
+  auto out_of = [&](const Place& p) {
+    const NormGroup& gr = p.gi ? r.g[1] : r.g[0];
+    return reinterpret_cast<T*>(gr.out) + b * gr.out_batch + (long long)(tok0 + p.t) * gr.out_token + p.h * gr.out_head;
+  };
+  auto weights = [&]() {
+    for (int x = tid; x < 2 * dim; x += kNormThreads) {
+      const int g = x >= dim;
+      if (r.g[g].n_heads > 0) w_s[g][x - g * dim] = __ldg(r.g[g].weight + x - g * dim);
+    }
+  };
+
+  if constexpr (!BWD) {
+    // one tile; two rows at a time, the first on their way before the sines are known; (token, head) rows as one list
+    const int tile = blockIdx.x;
+    b = tile / r.tiles_per_batch;
+    tok0 = (tile - b * r.tiles_per_batch) * r.tb;
+    const int nt = min(r.tb, r.tokens - tok0), end = min(nt * n_all, ((int)blockIdx.y + 1) * r.rows_per_y);
+    auto place = [&](int x) {
+      Place p{-1, 0, 0};
+      if (x < end) {
+        p.t = n_all == 1 ? x : (int)__umulhi((unsigned)x, r.head_magic[2]);
+        p.h = x - p.t * n_all;
+        p.gi = p.h >= n0;
+        if (p.gi) p.h -= n0;
       }
+      return p;
     };
-    group(r.g[0], 0, min(first, n_q), min(last, n_q), acc[0]);
-    if (r.g[1].n_heads > 0) group(r.g[1], 1, max(first, n_q) - n_q, min(last, n_all) - n_q, acc[1]);
-  }
-  if constexpr (BWD) {
+    int x0 = (int)blockIdx.y * r.rows_per_y;                       // (whole warps: a row's lanes meet in shuffles)
+    Place p[2];
+    uint32_t raw[2][WORDS], none[1];
+    auto fetch = [&]() {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) p[k] = place(x0 + k * by + ty);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) load(p[k], raw[k], none);
+    };
+    fetch();
+    weights();
+    const int* pos = r.positions + (long long)b * r.tokens + tok0;
+    fill_turns<ROW>(rt, table, nt, tid, kNormThreads, false, [&](int t) { return __ldg(pos + t); });
+    __syncthreads();
+#pragma unroll 1
+    for (; x0 < end; x0 += 2 * by, fetch()) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        float x[CH], w[CH];
+        row.values(raw[k], x);
+        if (p[k].t < 0 || !row.here)
+#pragma unroll
+          for (int i = 0; i < CH; ++i) x[i] = 0.f;
+        const float rms = row_rms(x, width, r.per_channel, r.eps);
+        row.weights(w_s[p[k].gi], w);
+        row_scale(x, rms, w);
+        row.turn(x, table + max(p[k].t, 0) * pairs, own_row);
+        if (p[k].t >= 0 && row.here) row.store(out_of(p[k]), x);
+      }
+    }
+  } else {
+    // tiles one after the other; queries' rows, then keys', whose weights' gradients are sums of their own; the next row is on its way
+    weights();
+    float acc[2][CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) acc[0][i] = acc[1][i] = 0.f;
+    for (int tile = blockIdx.x; tile < r.tiles; tile += gridDim.x) {
+      b = tile / r.tiles_per_batch;
+      tok0 = (tile - b * r.tiles_per_batch) * r.tb;
+      const int nt = min(r.tb, r.tokens - tok0);
+      const int first = (int)blockIdx.y * r.rows_per_y, last = first + r.rows_per_y, rows0 = nt * n0, rows1 = nt * (n_all - n0);
+      const int from[2] = {min(first, rows0), max(first, rows0) - rows0}, to[2] = {min(last, rows0), min(last, rows0 + rows1) - rows0};
+      uint32_t raw[WORDS], raw_g[WORDS];
+      Place p;
+      auto fetch = [&](int gi, int x) {
+        const int heads = gi ? n_all - n0 : n0;
+        p = Place{-1, 0, gi};
+        if (x < to[gi]) {
+          p.t = heads == 1 ? x : (int)__umulhi((unsigned)x, gi ? r.head_magic[1] : r.head_magic[0]);
+          p.h = x - p.t * heads;
+        }
+        load(p, raw, raw_g);
+      };
+      auto sums = [&](auto group_c) {
+        constexpr int GI = decltype(group_c)::value;
+        float (&sum)[CH] = acc[GI];
+#pragma unroll 1
+        for (int x0 = from[GI]; x0 < to[GI]; x0 += by) {
+          float x[CH], u[CH];
+          const Place here = p;
+          const bool there = here.t >= 0 && row.here;
+          row.values(raw, x);
+          row.values(raw_g, u);
+          // (the next row's registers are free)
+          if (GI == 0 && x0 + by >= to[0]) fetch(1, from[1] + ty);
+          else fetch(GI, x0 + by + ty);
+          if (!there)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) x[i] = u[i] = 0.f;
+          const float rms = row_rms(x, width, r.per_channel, r.eps);
+          row.turn(u, table + max(here.t, 0) * pairs, own_row);
+          float w[CH];
+          row.weights(w_s[GI], w);
+          float2 dot2 = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int i = 0; i < CH; i += 2) {
+            const float2 u2 = make_float2(u[i], u[i + 1]), x2 = make_float2(x[i], x[i + 1]);
+            const float2 s2 = __ffma2_rn(__fmul2_rn(u2, x2), make_float2(rms, rms), make_float2(sum[i], sum[i + 1]));
+            sum[i] = s2.x;
+            sum[i + 1] = s2.y;
+            const float2 g2 = __fmul2_rn(u2, make_float2(w[i], w[i + 1]));
+            dot2 = __ffma2_rn(g2, x2, dot2);
+            u[i] = g2.x;
+            u[i + 1] = g2.y;
+          }
+          const float dot = -(row_sum(dot2.x + dot2.y, width) * r.per_channel * rms * rms);
+#pragma unroll
+          for (int i = 0; i < CH; i += 2) {
+            const float2 y = __fmul2_rn(__ffma2_rn(make_float2(x[i], x[i + 1]), make_float2(dot, dot), make_float2(u[i], u[i + 1])), make_float2(rms, rms));
+            u[i] = y.x;
+            u[i + 1] = y.y;
+          }
+          if (there) row.store(out_of(here), u);
+        }
+      };
+      fetch(from[0] < to[0] ? 0 : 1, (from[0] < to[0] ? from[0] : from[1]) + ty);
+      if (tile != (int)blockIdx.x) __syncthreads();                // (the table before is used up)
+      const int* pos = r.positions + (long long)b * r.tokens + tok0;
+      fill_turns<ROW>(rt, table, nt, tid, kNormThreads, true, [&](int t) { return __ldg(pos + t); });
+      __syncthreads();
+      sums(std::integral_constant<int, 0>{});
+      sums(std::integral_constant<int, 1>{});
+    }
     float* red = reinterpret_cast<float*>(table);                  // [by][dim]
     for (int g = 0; g < 2; ++g) {
       if (r.g[g].n_heads == 0) continue;
@@ -173,16 +241,22 @@ struct NormPlan {
 NormPlan plan_norm(const RopeTable& rt, int batch, int tokens, int heads, bool backward, int sm_count) {
   NormPlan p;
   const int pairs = rt.rot / 2;
-  // tokens of a tile: a sine for every thread, rows for every thread where heads are few, less where SMs would idle (as in rope.cu)
   constexpr int by = 32;
-  int tb = kNormThreads / pairs < 8 ? kNormThreads / pairs : 8;
-  if (tb < (4 * by + heads - 1) / heads) tb = (4 * by + heads - 1) / heads;
-  if (tb > 64) tb = 64;
-  if (tb * pairs > kNormTable) tb = kNormTable / pairs;
+  auto tiles = [&](int x) { return (long long)((tokens + x - 1) / x) * batch; };
+  int tb, most = kNormTable / pairs < 64 ? kNormTable / pairs : 64;
+  if (backward) {
+    // two CTAs an SM, each as many tiles as the next, as large as the table of sines allows: what comes before a tile's first row is rarely paid
+    const long long wave = 2LL * sm_count, rounds = (tiles(most) + wave - 1) / wave;
+    for (tb = most; tb > 1 && tiles(tb - 1) <= rounds * wave;) --tb;
+  } else {
+    // a sine for every thread, rows for every thread where heads are few (as in rope.cu)
+    tb = kNormThreads / pairs < 8 ? kNormThreads / pairs : 8;
+    if (tb < (4 * by + heads - 1) / heads) tb = (4 * by + heads - 1) / heads;
+    if (tb > most) tb = most;
+  }
   if (tb < 1) tb = 1;
   while (tb > 1 && (long long)tb * heads * heads >= (1ll << 32)) tb /= 2;      // (see head_magic)
-  auto tiles = [&](int x) { return (long long)((tokens + x - 1) / x) * batch; };
-  while (tb > 1 && tiles(tb) < 2LL * sm_count) tb /= 2;
+  while (tb > 1 && tiles(tb) < (backward ? 1LL : 2LL) * sm_count) tb /= 2;
   if (tb > tokens) tb = tokens;
   p.tb = tb;
   p.tiles_per_batch = (tokens + tb - 1) / tb;
@@ -191,8 +265,8 @@ NormPlan plan_norm(const RopeTable& rt, int batch, int tokens, int heads, bool b
   p.ys = 1;
   if (p.tiles < 2LL * sm_count) {
     p.ys = (rows + by - 1) / by;
-    const long long most = (4LL * sm_count + p.tiles - 1) / p.tiles;
-    if (p.ys > most) p.ys = (int)most;
+    const long long many = ((backward ? 2LL : 4LL) * sm_count + p.tiles - 1) / p.tiles;
+    if (p.ys > many) p.ys = (int)many;
   }
   p.rows_per_y = (rows + p.ys - 1) / p.ys;
   p.ys = (rows + p.rows_per_y - 1) / p.rows_per_y;
@@ -246,6 +320,7 @@ cudaError_t launch_norm(const RopeTable& rt, const int* positions, int batch, in
     const NormGroup& g = r.g[i];
     if (g.n_heads == 0) continue;
     r.head_magic[i] = (unsigned)(((1ull << 32) + g.n_heads - 1) / g.n_heads);
+    r.head_magic[2] = (unsigned)(((1ull << 32) + heads - 1) / heads);
     wide = wide && wide_strides(g.x, e, g.x_batch, g.x_token, g.x_head) && wide_strides(g.out, e, g.out_batch, g.out_token, g.out_head) &&
            (!backward || wide_strides(g.dy, e, g.dy_batch, g.dy_token, g.dy_head));
   }

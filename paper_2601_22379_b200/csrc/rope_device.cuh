@@ -111,13 +111,27 @@ struct WideRow {
       y[i] = v.x; y[i + 1] = v.y; y[i + 2] = v.z; y[i + 3] = v.w;
     }
   }
-  // place of pair i in a token's table of sines
-  static __device__ __forceinline__ int entry(int i, int pairs) {
+  // Pair i into a token's table of sines: two pairs' cosines, then their sines; the pieces side by side, so that a warp's loads are contiguous.
+  static __device__ __forceinline__ void put(float2* table, int i, int pairs, float2 cs) {
     const int pc = i / VEC, j = i % VEC;
-    return ((j >> 1) * (pairs / VEC) + pc) * 2 + (j & 1);
+    float* at = reinterpret_cast<float*>(table) + ((j >> 1) * (pairs / VEC) + pc) * 4 + (j & 1);
+    at[0] = cs.x;
+    at[2] = cs.y;
   }
-  __device__ __forceinline__ void turn(float (&x)[CH], const float2* table, float*) const {
-    if (turns) turn_piece<VEC>(x, x + VEC, reinterpret_cast<const float4*>(table) + piece, rot_pieces, interleaved);
+  __device__ __forceinline__ void turn(float (&x)[CH], const float2* table, float*) const {   // two pairs at a time
+    if (!turns) return;
+    const float4* tab = reinterpret_cast<const float4*>(table) + piece;
+#pragma unroll
+    for (int j = 0; j < VEC / 2; ++j) {
+      const float4 cs = tab[j * rot_pieces];
+      if (interleaved) two(cs, x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+      else two(cs, x[2 * j], x[VEC + 2 * j], x[2 * j + 1], x[VEC + 2 * j + 1]);
+    }
+  }
+  static __device__ __forceinline__ void two(float4 cs, float& a0, float& b0, float& a1, float& b1) {
+    const float2 c = make_float2(cs.x, cs.y), s = make_float2(cs.z, cs.w), a = make_float2(a0, a1), b = make_float2(b0, b1);
+    const float2 y = __ffma2_rn(make_float2(-b.x, -b.y), s, __fmul2_rn(a, c)), z = __ffma2_rn(a, s, __fmul2_rn(b, c));
+    a0 = y.x; a1 = y.y; b0 = z.x; b1 = z.y;
   }
   __device__ __forceinline__ void store(T* row, const float (&x)[CH]) const {
     store_piece<VEC>(row + ca, *reinterpret_cast<const float(*)[VEC]>(x));
@@ -148,7 +162,7 @@ struct LooseRow {
 #pragma unroll
     for (int i = 0; i < N; ++i) y[i] = channel(i) < dim ? w[channel(i)] : 0.f;
   }
-  static __device__ __forceinline__ int entry(int i, int) { return i; }
+  static __device__ __forceinline__ void put(float2* table, int i, int, float2 cs) { table[i] = cs; }
   __device__ __forceinline__ void turn(float (&x)[CH], const float2* table, float* row) const {   // whole warps; row: its own dim floats
     const int pairs = rot / 2;
     __syncwarp();
@@ -183,13 +197,23 @@ __device__ __forceinline__ float row_sum(float v, int width) {
 // 1 / sqrt(mean x^2 + eps)
 template <int CH>
 __device__ __forceinline__ float row_rms(const float (&x)[CH], int width, float per_channel, float eps) {
-  float s = 0.f;
+  float2 s = make_float2(0.f, 0.f);
 #pragma unroll
-  for (int i = 0; i < CH; ++i) s = fmaf(x[i], x[i], s);
-  return rsqrtf(fmaf(row_sum(s, width), per_channel, eps));
+  for (int i = 0; i < CH; i += 2) s = __ffma2_rn(make_float2(x[i], x[i + 1]), make_float2(x[i], x[i + 1]), s);
+  return rsqrtf(fmaf(row_sum(s.x + s.y, width), per_channel, eps));
+}
+// x = x f w
+template <int CH>
+__device__ __forceinline__ void row_scale(float (&x)[CH], float f, const float (&w)[CH]) {
+#pragma unroll
+  for (int i = 0; i < CH; i += 2) {
+    const float2 y = __fmul2_rn(__fmul2_rn(make_float2(x[i], x[i + 1]), make_float2(f, f)), make_float2(w[i], w[i + 1]));
+    x[i] = y.x;
+    x[i + 1] = y.y;
+  }
 }
 
-// Sines and cosines of nt tokens for the rows of class ROW, by all threads of the CTA: table[t * pairs + entry].  `position`: of token t.
+// Sines and cosines of nt tokens for the rows of class ROW, by all threads of the CTA: table[t * pairs ..].  `position`: of token t.
 template <class ROW, typename F>
 __device__ __forceinline__ void fill_turns(const RopeTable& rt, float2* table, int nt, int tid, int threads, bool back, F position) {
   const unsigned long long* freq = rt.freq;
@@ -197,7 +221,7 @@ __device__ __forceinline__ void fill_turns(const RopeTable& rt, float2* table, i
   const int pairs = rt.rot / 2;
   for (int x = tid; x < nt * pairs; x += threads) {
     const int t = x / pairs, i = x - t * pairs;
-    table[t * pairs + ROW::entry(i, pairs)] = turn_of(freq[i], position(t), rt.amplitude, back);
+    ROW::put(table + t * pairs, i, pairs, turn_of(freq[i], position(t), rt.amplitude, back));
   }
 }
 

@@ -50,20 +50,16 @@ __device__ __forceinline__ float2 unpack_e4m3(unsigned two) {
   const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
   return __half22float2(__half2(h));
 }
-// Infinity has no place in the format: it is stored as what it would lead to, NaN.
-__device__ __forceinline__ float finite_or_nan(float x) { return fabsf(x) <= 3.4028235e38f ? x : __int_as_float(0x7fffffff); }
-
 // Bytes of a lane's channels: n contiguous ones.
 template <int N>
 __device__ __forceinline__ void store_bytes(unsigned char* p, const float* x, float mul) {
   if constexpr (N == 1) {
-    *p = (unsigned char)pack_e4m3(finite_or_nan(x[0] * mul), 0.f);
+    *p = (unsigned char)pack_e4m3(x[0] * mul, 0.f);
   } else {
     uint32_t w[N / 4];
 #pragma unroll
     for (int i = 0; i < N / 4; ++i)
-      w[i] = pack_e4m3(finite_or_nan(x[4 * i] * mul), finite_or_nan(x[4 * i + 1] * mul)) |
-             pack_e4m3(finite_or_nan(x[4 * i + 2] * mul), finite_or_nan(x[4 * i + 3] * mul)) << 16;
+      w[i] = pack_e4m3(x[4 * i] * mul, x[4 * i + 1] * mul) | pack_e4m3(x[4 * i + 2] * mul, x[4 * i + 3] * mul) << 16;
     if constexpr (N == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
     else *reinterpret_cast<uint32_t*>(p) = w[0];
   }
@@ -218,8 +214,7 @@ __global__ void __launch_bounds__(kStoreThreads, 2) store_kernel(const __grid_co
           if (norm) {
             float w[CH];
             row.weights(w_s[gi], w);
-#pragma unroll
-            for (int i = 0; i < CH; ++i) x[p][i] = x[p][i] * rms * w[i];
+            row_scale(x[p], rms, w);
           }
         }
         if (loose) {
@@ -231,10 +226,7 @@ __global__ void __launch_bounds__(kStoreThreads, 2) store_kernel(const __grid_co
           if (there) row.store(reinterpret_cast<T*>(r.q_out) + (long long)(tok0 + t0 + t) * r.q_out_stride + (long long)hg * D, x[p]);
         } else if constexpr (E8) {
 #pragma unroll
-          for (int i = 0; i < CH; ++i) {
-            const float a = fabsf(x[p][i]);
-            if (a <= 3.4028235e38f) top = fmaxf(top, a);   // (what is not finite takes no part in the scale)
-          }
+          for (int i = 0; i < CH; i += 2) top = fmaxf(top, fmaxf(fabsf(x[p][i]), fabsf(x[p][i + 1])));   // (NaN takes no part)
         } else if (there && crow >= 0) {
           row.store(reinterpret_cast<TC*>(gi == 1 ? r.k_pages : r.v_pages) + (crow + t) * D, x[p]);
         }
@@ -245,6 +237,23 @@ __global__ void __launch_bounds__(kStoreThreads, 2) store_kernel(const __grid_co
         for (int o = 16; o > 0; o >>= 1) {
           const float other = __shfl_xor_sync(0xffffffffu, top, o);
           if (o < W || many == 1) top = fmaxf(top, other);
+        }
+        if (__any_sync(0xffffffffu, top == INFINITY)) {    // infinities take no part in the scale either, and have no place in the format: NaN
+          float fine = 0.f;
+#pragma unroll
+          for (int p = 0; p < PASSES; ++p)
+            if (p < passes)
+#pragma unroll
+              for (int i = 0; i < CH; ++i) {
+                if (fabsf(x[p][i]) == INFINITY) x[p][i] = __int_as_float(0x7fffffff);
+                fine = fmaxf(fine, fabsf(x[p][i]));
+              }
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) {
+            const float other = __shfl_xor_sync(0xffffffffu, fine, o);
+            if (o < W || many == 1) fine = fmaxf(fine, other);
+          }
+          top = fine;
         }
         if (scale_at) {
           unsigned char* page = reinterpret_cast<unsigned char*>(gi == 1 ? r.k_pages : r.v_pages);
