@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(kNormThreads, BWD ? 2 : 3)
     };
     int x0 = (int)blockIdx.y * r.rows_per_y;                       // (whole warps: a row's lanes meet in shuffles)
     Place p[2];
-    uint32_t raw[2][WORDS], none[1];
+    uint32_t raw[2][WORDS] = {}, none[1];
     auto fetch = [&]() {
 #pragma unroll
       for (int k = 0; k < 2; ++k) p[k] = place(x0 + k * by + ty);
@@ -107,8 +107,8 @@ __global__ void __launch_bounds__(kNormThreads, BWD ? 2 : 3)
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         float x[CH], w[CH];
-        row.values(raw[k], x);
-        if (p[k].t < 0 || !row.here)
+        row.values(raw[k], x);                                     // (of no row: whatever, and not stored)
+        if (!loose && !row.here)                                   // (lanes beside a row's: nothing to its sum)
 #pragma unroll
           for (int i = 0; i < CH; ++i) x[i] = 0.f;
         const float rms = row_rms(x, width, r.per_channel, r.eps);
@@ -154,9 +154,10 @@ __global__ void __launch_bounds__(kNormThreads, BWD ? 2 : 3)
           // (the next row's registers are free)
           if (GI == 0 && x0 + by >= to[0]) fetch(1, from[1] + ty);
           else fetch(GI, x0 + by + ty);
-          if (!there)
+          if (!there) {
 #pragma unroll
             for (int i = 0; i < CH; ++i) x[i] = u[i] = 0.f;
+          }
           const float rms = row_rms(x, width, r.per_channel, r.eps);
           row.turn(u, table + max(here.t, 0) * pairs, own_row);
           float w[CH];

@@ -121,11 +121,12 @@ struct WideRow {
   __device__ __forceinline__ void turn(float (&x)[CH], const float2* table, float*) const {   // two pairs at a time
     if (!turns) return;
     const float4* tab = reinterpret_cast<const float4*>(table) + piece;
+    if (interleaved) {
 #pragma unroll
-    for (int j = 0; j < VEC / 2; ++j) {
-      const float4 cs = tab[j * rot_pieces];
-      if (interleaved) two(cs, x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
-      else two(cs, x[2 * j], x[VEC + 2 * j], x[2 * j + 1], x[VEC + 2 * j + 1]);
+      for (int j = 0; j < VEC / 2; ++j) two(tab[j * rot_pieces], x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC / 2; ++j) two(tab[j * rot_pieces], x[2 * j], x[VEC + 2 * j], x[2 * j + 1], x[VEC + 2 * j + 1]);
     }
   }
   static __device__ __forceinline__ void two(float4 cs, float& a0, float& b0, float& a1, float& b1) {
@@ -189,9 +190,13 @@ struct LooseRow {
 
 // Sum over the `width` neighbouring lanes of a row (a power of two); the same in all of them.
 __device__ __forceinline__ float row_sum(float v, int width) {
+  if (width == 8) {                                         // (the usual one)
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
-    if (o < width) v += __shfl_xor_sync(0xffffffffu, v, o);
+    for (int o = 4; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  } else {
+#pragma unroll 1
+    for (int o = width >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  }
   return v;
 }
 // 1 / sqrt(mean x^2 + eps)

@@ -10,6 +10,8 @@
 // stores.  Queries go the same way without the scale.  New values are read once, written once; a block's earlier tokens are touched only when
 // its scale grows.
 // @figures
+#include <type_traits>
+
 #include "rope_device.cuh"
 
 namespace spla {
@@ -134,7 +136,6 @@ template <typename T, class ROW, bool E8, int D>
 __global__ void __launch_bounds__(kStoreThreads, 2) store_kernel(const __grid_constant__ StoreLaunch r, const __grid_constant__ RopeTable rt) {
   constexpr int CH = ROW::CH, WORDS = ROW::WORDS, W = D / CH, S = 32 / W, PASSES = kStoreTokens / S;
   constexpr bool loose = W == 32 && WORDS == CH;
-  using TC = T;
   __shared__ __align__(16) float2 table[(kStoreReach - 1) * (D / 2)];
   __shared__ __align__(16) float w_s[2][D];
   __shared__ float rows_s[loose ? kStoreThreads / 32 : 1][loose ? D : 1];
@@ -173,104 +174,133 @@ __global__ void __launch_bounds__(kStoreThreads, 2) store_kernel(const __grid_co
   if (r.turn) fill_turns<ROW>(rt, table, nt, tid, kStoreThreads, false, [&](int t) { return at.turn_pos[t]; });
   __syncthreads();
   const int n_runs = n_runs_s, pairs = rt.rot / 2, h_first = blockIdx.y * r.heads_per_y, h_end = min(h_first + r.heads_per_y, r.n_q + 2 * r.n_kv);
+  // heads of the queries, the keys, the values that are this block's
+  int h0[3], hn[3];
+#pragma unroll
+  for (int g = 0; g < 3; ++g) {
+    const int before = g == 0 ? 0 : g == 1 ? r.n_q : r.n_q + r.n_kv, n = g == 0 ? r.n_q : r.n_kv;
+    h0[g] = min(max(h_first - before, 0), n);
+    hn[g] = min(max(h_end - before, 0), n) - h0[g];
+  }
   int before = 0;                                          // pieces of work of the runs before, modulo the warps
   for (int run = 0; run < n_runs; ++run) {
-    const int t0 = run_at[run], len = run_len[run], many = len == 1 ? S : 1, pieces = (h_end - h_first + many - 1) / many;
-    const int pos0 = at.pos[t0], off = pos0 % kStoreTokens;
+    const int t0 = run_at[run], len = run_len[run], many = len == 1 ? S : 1;
+    const int off = at.pos[t0] % kStoreTokens, first = many > 1 ? 0 : slot;          // the lane's first token; the next is S further
     const long long cache_row0 = at.cache_row[t0];         // (a run lies in one page)
-    for (int u = (warp - before) & 7; u < pieces; u += kStoreThreads / 32) {
-      const int h = h_first + u * many + (many > 1 ? slot : 0);
-      const bool head = h < h_end;
-      const int gi = (h >= r.n_q) + (h >= r.n_q + r.n_kv), hg = h - (gi == 0 ? 0 : gi == 1 ? r.n_q : r.n_q + r.n_kv);
-      const T* in = reinterpret_cast<const T*>(gi == 0 ? r.q : gi == 1 ? r.k : r.v) + (long long)hg * D;
-      const long long stride = gi == 0 ? r.q_stride : gi == 1 ? r.k_stride : r.v_stride;
-      const int first = many > 1 ? 0 : slot, passes = many > 1 ? 1 : (len + S - 1) / S;   // token of this lane's row: first + S pass
-      uint32_t raw[PASSES][WORDS];
+    // one head of the run (`many` heads of its one token) of the queries (GI 0), the keys (1) or the values (2); N rows a lane, at most
+    auto piece = [&](auto group_c, auto norm_c, auto rows_c, int h) {
+      constexpr int GI = decltype(group_c)::value, N = decltype(rows_c)::value;
+      constexpr bool NORM = decltype(norm_c)::value;
+      h += many > 1 ? slot : 0;
+      const bool head = h < h0[GI] + hn[GI];
+      const long long stride = GI == 0 ? r.q_stride : GI == 1 ? r.k_stride : r.v_stride;
+      const T* in = reinterpret_cast<const T*>(GI == 0 ? r.q : GI == 1 ? r.k : r.v) + (long long)h * D + (tok0 + t0 + first) * stride;
+      const int mine = head ? many > 1 ? 1 : (len - first + S - 1) / S : 0;   // rows of the lane
+      uint32_t raw[N][WORDS];
 #pragma unroll
-      for (int p = 0; p < PASSES; ++p)
-        if (p < passes && head && first + S * p < len) row.load(in + (long long)(tok0 + t0 + first + S * p) * stride, raw[p]);
-      const bool norm = gi == 0 ? r.q_weight != nullptr : gi == 1 && r.k_weight != nullptr, turn = r.turn && gi < 2;
+      for (int p = 0; p < N; ++p)
+        if (p < mine) {
+          row.load(in, raw[p]);
+          in += S * stride;
+        } else {
+#pragma unroll
+          for (int i = 0; i < WORDS; ++i) raw[p][i] = 0u;
+        }
       unsigned char* scale_at = nullptr;
       int e_old = kExpMin;
-      const long long crow = cache_row0 < 0 ? -1 : cache_row0 + (long long)hg * r.pl.head_stride;
-      if constexpr (E8) {
-        if (gi > 0 && head && crow >= 0) {
-          scale_at = (gi == 1 ? r.k_scales : r.v_scales) + (crow >> 4);
+      const long long crow = GI == 0 || cache_row0 < 0 ? -1 : cache_row0 + (long long)h * r.pl.head_stride;
+      if constexpr (E8 && GI > 0) {
+        if (head && crow >= 0) {
+          scale_at = (GI == 1 ? r.k_scales : r.v_scales) + (crow >> 4);
           if (off > 0) e_old = held_exponent(scale_at);
         }
       }
-      float x[PASSES][CH], top = 0.f;
-#pragma unroll
-      for (int p = 0; p < PASSES; ++p) {
-        if (p >= passes) break;                            // (whole warps)
-        const int t = first + S * p;
-        const bool there = head && t < len;
-        if (there) row.values(raw[p], x[p]);
-        else
-#pragma unroll
-          for (int i = 0; i < CH; ++i) x[p][i] = 0.f;
-        if (__any_sync(0xffffffffu, norm)) {
-          const float rms = row_rms(x[p], W, 1.f / D, r.eps);
-          if (norm) {
-            float w[CH];
-            row.weights(w_s[gi], w);
-            row_scale(x[p], rms, w);
-          }
+      const float2* tab = table + (t0 + first) * pairs;
+      T* out = GI == 0 ? reinterpret_cast<T*>(r.q_out) + (tok0 + t0 + first) * r.q_out_stride + (long long)h * D
+                       : E8 ? nullptr : reinterpret_cast<T*>(GI == 1 ? r.k_pages : r.v_pages) + (crow + first) * D;
+      const long long out_stride = GI == 0 ? S * r.q_out_stride : S * D;
+      auto finished = [&](float (&x)[CH], int p) {         // (whole warps)
+        row.values(raw[p], x);
+        if constexpr (NORM) {
+          const float rms = row_rms(x, W, 1.f / D, r.eps);
+          float w[CH];
+          row.weights(w_s[GI], w);
+          row_scale(x, rms, w);
         }
-        if (loose) {
-          if (__any_sync(0xffffffffu, turn)) row.turn(x[p], table + (t0 + min(t, len - 1)) * pairs, own_row);
-        } else if (turn) {
-          row.turn(x[p], table + (t0 + min(t, len - 1)) * pairs, own_row);
+        if (GI < 2 && r.turn) row.turn(x, tab + (p < mine ? S * p * pairs : 0), own_row);
+      };
+      if constexpr (GI == 0 || !E8) {
+#pragma unroll
+        for (int p = 0; p < N; ++p) {
+          float x[CH];
+          finished(x, p);
+          if (p < mine && (GI == 0 || crow >= 0)) row.store(out, x);
+          out += out_stride;
         }
-        if (gi == 0) {
-          if (there) row.store(reinterpret_cast<T*>(r.q_out) + (long long)(tok0 + t0 + t) * r.q_out_stride + (long long)hg * D, x[p]);
-        } else if constexpr (E8) {
+      } else {
+        float x[N][CH], top = 0.f;
+#pragma unroll
+        for (int p = 0; p < N; ++p) {
+          finished(x[p], p);
 #pragma unroll
           for (int i = 0; i < CH; i += 2) top = fmaxf(top, fmaxf(fabsf(x[p][i]), fabsf(x[p][i + 1])));   // (NaN takes no part)
-        } else if (there && crow >= 0) {
-          row.store(reinterpret_cast<TC*>(gi == 1 ? r.k_pages : r.v_pages) + (crow + t) * D, x[p]);
         }
-      }
-      if constexpr (E8) {
         // the lanes of a row, and where the rows are one head's tokens, all of them
+        auto over_rows = [&](float v) {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-          const float other = __shfl_xor_sync(0xffffffffu, top, o);
-          if (o < W || many == 1) top = fmaxf(top, other);
-        }
+          for (int o = 16; o > 0; o >>= 1) {
+            const float other = __shfl_xor_sync(0xffffffffu, v, o);
+            if (o < W || many == 1) v = fmaxf(v, other);
+          }
+          return v;
+        };
+        top = over_rows(top);
         if (__any_sync(0xffffffffu, top == INFINITY)) {    // infinities take no part in the scale either, and have no place in the format: NaN
           float fine = 0.f;
 #pragma unroll
-          for (int p = 0; p < PASSES; ++p)
-            if (p < passes)
+          for (int p = 0; p < N; ++p)
 #pragma unroll
-              for (int i = 0; i < CH; ++i) {
-                if (fabsf(x[p][i]) == INFINITY) x[p][i] = __int_as_float(0x7fffffff);
-                fine = fmaxf(fine, fabsf(x[p][i]));
-              }
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1) {
-            const float other = __shfl_xor_sync(0xffffffffu, fine, o);
-            if (o < W || many == 1) fine = fmaxf(fine, other);
-          }
-          top = fine;
+            for (int i = 0; i < CH; ++i) {
+              if (fabsf(x[p][i]) == INFINITY) x[p][i] = __int_as_float(0x7fffffff);
+              fine = fmaxf(fine, fabsf(x[p][i]));
+            }
+          top = over_rows(fine);
         }
         if (scale_at) {
-          unsigned char* page = reinterpret_cast<unsigned char*>(gi == 1 ? r.k_pages : r.v_pages);
+          unsigned char* page = reinterpret_cast<unsigned char*>(GI == 1 ? r.k_pages : r.v_pages) + crow * D;
           const int e = max(scale_exponent(top), e_old);
           if (off > 0 && e > e_old) {                      // the tokens before: rounded again, each row by the lanes that hold one
             const float less = power_of_two(e_old - e);
-            for (int t = many > 1 ? 0 : slot; t < off; t += many > 1 ? 1 : S) rescale_row8(row, page + (crow - off + t) * D, less);
+#pragma unroll 1
+            for (int t = first; t < off; t += many > 1 ? 1 : S) rescale_row8(row, page + (t - off) * D, less);
           }
           const float mul = power_of_two(-e);
 #pragma unroll
-          for (int p = 0; p < PASSES; ++p)
-            if (p < passes && first + S * p < len) store_row8(row, page + (crow + first + S * p) * D, x[p], mul);
+          for (int p = 0; p < N; ++p)
+            if (p < mine) store_row8(row, page + (first + S * p) * D, x[p], mul);
           if ((many > 1 ? lane % W : lane) == 0) *scale_at = (unsigned char)(e + 127);
         }
       }
-    }
-    before += pieces;
+    };
+    auto heads = [&](auto rows_c) {
+      constexpr std::integral_constant<int, 0> queries{};
+      constexpr std::integral_constant<int, 1> keys{};
+      constexpr std::integral_constant<int, 2> vals{};
+      constexpr std::true_type normed{};
+      constexpr std::false_type plain{};
+      const int n0 = (hn[0] + many - 1) / many, n1 = n0 + (hn[1] + many - 1) / many, n2 = n1 + (hn[2] + many - 1) / many;
+      for (int u = (warp - before) & 7; u < n2; u += kStoreThreads / 32) {
+        if (u < n0) {
+          if (r.q_weight) piece(queries, normed, rows_c, h0[0] + u * many); else piece(queries, plain, rows_c, h0[0] + u * many);
+        } else if (u < n1) {
+          if (r.k_weight) piece(keys, normed, rows_c, h0[1] + (u - n0) * many); else piece(keys, plain, rows_c, h0[1] + (u - n0) * many);
+        } else {
+          piece(vals, plain, rows_c, h0[2] + (u - n1) * many);
+        }
+      }
+      before += n2;
+    };
+    if (len <= S) heads(std::integral_constant<int, 1>{}); else heads(std::integral_constant<int, PASSES>{});
   }
 }
 
