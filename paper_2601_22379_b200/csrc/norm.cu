@@ -29,14 +29,14 @@ struct NormLaunch {
   int tokens, tb, tiles_per_batch;       // of a batch entry; per tile
   int tiles;                             // of all batch entries
   int rows_per_y;
-  unsigned head_magic[3];                // as in RopeLaunch: of the queries' heads, the keys', all
+  unsigned head_magic[2];                // as in RopeLaunch
   float eps, per_channel;
   int width;                             // lanes of a row
   float* part;                           // [CTAs][2][dim]: sums for the weights' gradients
 };
 
 template <typename T, class ROW, bool BWD>
-__global__ void __launch_bounds__(kNormThreads, BWD ? 2 : 3)
+__global__ void __launch_bounds__(kNormThreads, BWD ? 2 : 4)
     norm_kernel(const __grid_constant__ NormLaunch r, const __grid_constant__ RopeTable rt) {
   constexpr int CH = ROW::CH, WORDS = ROW::WORDS;
   constexpr bool loose = sizeof(ROW) == sizeof(LooseRow<T, CH>);
@@ -50,147 +50,144 @@ __global__ void __launch_bounds__(kNormThreads, BWD ? 2 : 3)
   const ROW row(rt, tid % width);
   float* own_row = rows_s[loose ? tid / 32 : 0];
   const int n0 = r.g[0].n_heads, n_all = n0 + r.g[1].n_heads;
-  struct Place {
-    int t, h, gi;                                                  // token of the tile, head, group; t < 0: none
-  };
-  int b = 0, tok0 = 0;
-  auto load = [&](const Place& p, uint32_t (&x)[WORDS], uint32_t (&g)[BWD ? WORDS : 1]) {
-    if (p.t < 0 || !row.here) return;
-    const NormGroup& gr = p.gi ? r.g[1] : r.g[0];
-    const long long tok = tok0 + p.t;
-    row.load(reinterpret_cast<const T*>(gr.x) + b * gr.x_batch + tok * gr.x_token + p.h * gr.x_head, x);
-    if constexpr (BWD) row.load(reinterpret_cast<const T*>(gr.dy) + b * gr.dy_batch + tok * gr.dy_token + p.h * gr.dy_head, g);
-  };
-  auto out_of = [&](const Place& p) {
-    const NormGroup& gr = p.gi ? r.g[1] : r.g[0];
-    return reinterpret_cast<T*>(gr.out) + b * gr.out_batch + (long long)(tok0 + p.t) * gr.out_token + p.h * gr.out_head;
-  };
   auto weights = [&]() {
     for (int x = tid; x < 2 * dim; x += kNormThreads) {
       const int g = x >= dim;
       if (r.g[g].n_heads > 0) w_s[g][x - g * dim] = __ldg(r.g[g].weight + x - g * dim);
     }
   };
-
-  if constexpr (!BWD) {
-    // one tile; two rows at a time, the first on their way before the sines are known; (token, head) rows as one list
-    const int tile = blockIdx.x;
+  constexpr std::integral_constant<int, 0> queries{};
+  constexpr std::integral_constant<int, 1> keys{};
+  // The rows of a tile that are this block's: of the queries, then of the keys.
+  int b, tok0, nt, from[2], to[2];
+  auto start = [&](int tile) {
     b = tile / r.tiles_per_batch;
     tok0 = (tile - b * r.tiles_per_batch) * r.tb;
-    const int nt = min(r.tb, r.tokens - tok0), end = min(nt * n_all, ((int)blockIdx.y + 1) * r.rows_per_y);
-    auto place = [&](int x) {
-      Place p{-1, 0, 0};
-      if (x < end) {
-        p.t = n_all == 1 ? x : (int)__umulhi((unsigned)x, r.head_magic[2]);
-        p.h = x - p.t * n_all;
-        p.gi = p.h >= n0;
-        if (p.gi) p.h -= n0;
-      }
-      return p;
-    };
-    int x0 = (int)blockIdx.y * r.rows_per_y;                       // (whole warps: a row's lanes meet in shuffles)
-    Place p[2];
-    uint32_t raw[2][WORDS] = {}, none[1];
-    auto fetch = [&]() {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) p[k] = place(x0 + k * by + ty);
-#pragma unroll
-      for (int k = 0; k < 2; ++k) load(p[k], raw[k], none);
-    };
-    fetch();
-    weights();
+    nt = min(r.tb, r.tokens - tok0);
+    const int first = (int)blockIdx.y * r.rows_per_y, last = first + r.rows_per_y, rows0 = nt * n0, rows1 = nt * (n_all - n0);
+    from[0] = min(first, rows0);
+    to[0] = min(last, rows0);
+    from[1] = max(first, rows0) - rows0;
+    to[1] = min(last, rows0 + rows1) - rows0;
+  };
+  auto sines = [&]() {
     const int* pos = r.positions + (long long)b * r.tokens + tok0;
-    fill_turns<ROW>(rt, table, nt, tid, kNormThreads, false, [&](int t) { return __ldg(pos + t); });
-    __syncthreads();
-#pragma unroll 1
-    for (; x0 < end; x0 += 2 * by, fetch()) {
+    fill_turns<ROW>(rt, table, nt, tid, kNormThreads, BWD, [&](int t) { return __ldg(pos + t); });
+  };
+  // Up to N rows of a thread on their way: row x0 + k by + ty of the group.  (Which group is known to the compiler: its strides are constants then.)
+  constexpr int N = 1;
+  int tk[N];                                                       // token of the tile, -1: none
+  T* out[N];
+  uint32_t raw[N][WORDS] = {}, raw_g[N][BWD ? WORDS : 1] = {};
+  auto fetch = [&](auto group_c, int x0) {
+    constexpr int GI = decltype(group_c)::value;
+    const NormGroup& g = r.g[GI];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        float x[CH], w[CH];
-        row.values(raw[k], x);                                     // (of no row: whatever, and not stored)
-        if (!loose && !row.here)                                   // (lanes beside a row's: nothing to its sum)
-#pragma unroll
-          for (int i = 0; i < CH; ++i) x[i] = 0.f;
-        const float rms = row_rms(x, width, r.per_channel, r.eps);
-        row.weights(w_s[p[k].gi], w);
-        row_scale(x, rms, w);
-        row.turn(x, table + max(p[k].t, 0) * pairs, own_row);
-        if (p[k].t >= 0 && row.here) row.store(out_of(p[k]), x);
-      }
+    for (int k = 0; k < N; ++k) {
+      const int x = x0 + k * by + ty;
+      tk[k] = -1;
+      if (x >= to[GI] || !row.here) continue;
+      const int t = g.n_heads == 1 ? x : (int)__umulhi((unsigned)x, r.head_magic[GI]), h = x - t * g.n_heads;
+      const long long tok = tok0 + t;
+      tk[k] = t;
+      out[k] = reinterpret_cast<T*>(g.out) + b * g.out_batch + tok * g.out_token + h * g.out_head;
+      row.load(reinterpret_cast<const T*>(g.x) + b * g.x_batch + tok * g.x_token + h * g.x_head, raw[k]);
+      if constexpr (BWD) row.load(reinterpret_cast<const T*>(g.dy) + b * g.dy_batch + tok * g.dy_token + h * g.dy_head, raw_g[k]);
     }
+  };
+  auto fetch_first = [&]() {
+    if (from[0] < to[0]) fetch(queries, from[0]); else fetch(keys, from[1]);
+  };
+  // (what comes behind the rows from x0 on)
+  auto fetch_next = [&](auto group_c, int x0) {
+    constexpr int GI = decltype(group_c)::value;
+    if (GI == 0 && x0 + N * by >= to[0]) fetch(keys, from[1]); else fetch(group_c, x0 + N * by);
+  };
+  float acc[2][BWD ? CH : 1];
+
+  if constexpr (!BWD) {
+    // one tile; the first rows are on their way before the sines are known
+    start(blockIdx.x);
+    fetch_first();
+    weights();
+    sines();
+    __syncthreads();
+    auto group = [&](auto group_c) {
+      constexpr int GI = decltype(group_c)::value;
+#pragma unroll 1
+      for (int x0 = from[GI]; x0 < to[GI]; x0 += N * by) {         // (whole warps: a row's lanes meet in shuffles)
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          float x[CH], w[CH];
+          row.values(raw[k], x);                                   // (of no row: whatever, and not stored)
+          if (!loose && !row.here)                                 // (lanes beside a row's: nothing to its sum)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) x[i] = 0.f;
+          const float rms = row_rms(x, width, r.per_channel, r.eps);
+          row.weights(w_s[GI], w);
+          row_scale(x, rms, w);
+          row.turn(x, table + max(tk[k], 0) * pairs, own_row);
+          if (tk[k] >= 0) row.store(out[k], x);
+        }
+        fetch_next(group_c, x0);
+      }
+    };
+    group(queries);
+    group(keys);
   } else {
     // tiles one after the other; queries' rows, then keys', whose weights' gradients are sums of their own; the next row is on its way
     weights();
-    float acc[2][CH];
 #pragma unroll
     for (int i = 0; i < CH; ++i) acc[0][i] = acc[1][i] = 0.f;
-    for (int tile = blockIdx.x; tile < r.tiles; tile += gridDim.x) {
-      b = tile / r.tiles_per_batch;
-      tok0 = (tile - b * r.tiles_per_batch) * r.tb;
-      const int nt = min(r.tb, r.tokens - tok0);
-      const int first = (int)blockIdx.y * r.rows_per_y, last = first + r.rows_per_y, rows0 = nt * n0, rows1 = nt * (n_all - n0);
-      const int from[2] = {min(first, rows0), max(first, rows0) - rows0}, to[2] = {min(last, rows0), min(last, rows0 + rows1) - rows0};
-      uint32_t raw[WORDS], raw_g[WORDS];
-      Place p;
-      auto fetch = [&](int gi, int x) {
-        const int heads = gi ? n_all - n0 : n0;
-        p = Place{-1, 0, gi};
-        if (x < to[gi]) {
-          p.t = heads == 1 ? x : (int)__umulhi((unsigned)x, gi ? r.head_magic[1] : r.head_magic[0]);
-          p.h = x - p.t * heads;
-        }
-        load(p, raw, raw_g);
-      };
-      auto sums = [&](auto group_c) {
-        constexpr int GI = decltype(group_c)::value;
-        float (&sum)[CH] = acc[GI];
+    auto group = [&](auto group_c) {
+      constexpr int GI = decltype(group_c)::value;
+      float (&sum)[CH] = acc[GI];
 #pragma unroll 1
-        for (int x0 = from[GI]; x0 < to[GI]; x0 += by) {
-          float x[CH], u[CH];
-          const Place here = p;
-          const bool there = here.t >= 0 && row.here;
-          row.values(raw, x);
-          row.values(raw_g, u);
-          // (the next row's registers are free)
-          if (GI == 0 && x0 + by >= to[0]) fetch(1, from[1] + ty);
-          else fetch(GI, x0 + by + ty);
-          if (!there) {
+      for (int x0 = from[GI]; x0 < to[GI]; x0 += by) {
+        float x[CH], u[CH];
+        const int t = tk[0];
+        T* const to_row = out[0];
+        row.values(raw[0], x);
+        row.values(raw_g[0], u);
+        fetch_next(group_c, x0);                                   // (its registers are free)
+        if (t < 0) {
 #pragma unroll
-            for (int i = 0; i < CH; ++i) x[i] = u[i] = 0.f;
-          }
-          const float rms = row_rms(x, width, r.per_channel, r.eps);
-          row.turn(u, table + max(here.t, 0) * pairs, own_row);
-          float w[CH];
-          row.weights(w_s[GI], w);
-          float2 dot2 = make_float2(0.f, 0.f);
-#pragma unroll
-          for (int i = 0; i < CH; i += 2) {
-            const float2 u2 = make_float2(u[i], u[i + 1]), x2 = make_float2(x[i], x[i + 1]);
-            const float2 s2 = __ffma2_rn(__fmul2_rn(u2, x2), make_float2(rms, rms), make_float2(sum[i], sum[i + 1]));
-            sum[i] = s2.x;
-            sum[i + 1] = s2.y;
-            const float2 g2 = __fmul2_rn(u2, make_float2(w[i], w[i + 1]));
-            dot2 = __ffma2_rn(g2, x2, dot2);
-            u[i] = g2.x;
-            u[i + 1] = g2.y;
-          }
-          const float dot = -(row_sum(dot2.x + dot2.y, width) * r.per_channel * rms * rms);
-#pragma unroll
-          for (int i = 0; i < CH; i += 2) {
-            const float2 y = __fmul2_rn(__ffma2_rn(make_float2(x[i], x[i + 1]), make_float2(dot, dot), make_float2(u[i], u[i + 1])), make_float2(rms, rms));
-            u[i] = y.x;
-            u[i + 1] = y.y;
-          }
-          if (there) row.store(out_of(here), u);
+          for (int i = 0; i < CH; ++i) x[i] = u[i] = 0.f;
         }
-      };
-      fetch(from[0] < to[0] ? 0 : 1, (from[0] < to[0] ? from[0] : from[1]) + ty);
+        const float rms = row_rms(x, width, r.per_channel, r.eps);
+        row.turn(u, table + max(t, 0) * pairs, own_row);
+        float w[CH];
+        row.weights(w_s[GI], w);
+        float2 dot2 = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < CH; i += 2) {
+          const float2 u2 = make_float2(u[i], u[i + 1]), x2 = make_float2(x[i], x[i + 1]);
+          const float2 s2 = __ffma2_rn(__fmul2_rn(u2, x2), make_float2(rms, rms), make_float2(sum[i], sum[i + 1]));
+          sum[i] = s2.x;
+          sum[i + 1] = s2.y;
+          const float2 g2 = __fmul2_rn(u2, make_float2(w[i], w[i + 1]));
+          dot2 = __ffma2_rn(g2, x2, dot2);
+          u[i] = g2.x;
+          u[i + 1] = g2.y;
+        }
+        const float dot = -(row_sum(dot2.x + dot2.y, width) * r.per_channel * rms * rms);
+#pragma unroll
+        for (int i = 0; i < CH; i += 2) {
+          const float2 y = __fmul2_rn(__ffma2_rn(make_float2(x[i], x[i + 1]), make_float2(dot, dot), make_float2(u[i], u[i + 1])), make_float2(rms, rms));
+          u[i] = y.x;
+          u[i + 1] = y.y;
+        }
+        if (t >= 0) row.store(to_row, u);
+      }
+    };
+    for (int tile = blockIdx.x; tile < r.tiles; tile += gridDim.x) {
+      start(tile);
+      fetch_first();
       if (tile != (int)blockIdx.x) __syncthreads();                // (the table before is used up)
-      const int* pos = r.positions + (long long)b * r.tokens + tok0;
-      fill_turns<ROW>(rt, table, nt, tid, kNormThreads, true, [&](int t) { return __ldg(pos + t); });
+      sines();
       __syncthreads();
-      sums(std::integral_constant<int, 0>{});
-      sums(std::integral_constant<int, 1>{});
+      group(queries);
+      group(keys);
     }
     float* red = reinterpret_cast<float*>(table);                  // [by][dim]
     for (int g = 0; g < 2; ++g) {
@@ -250,9 +247,10 @@ NormPlan plan_norm(const RopeTable& rt, int batch, int tokens, int heads, bool b
     const long long wave = 2LL * sm_count, rounds = (tiles(most) + wave - 1) / wave;
     for (tb = most; tb > 1 && tiles(tb - 1) <= rounds * wave;) --tb;
   } else {
-    // a sine for every thread, rows for every thread where heads are few (as in rope.cu)
+    // two sines for every thread, rows for every thread where heads are few (as in rope.cu; with one sine 139 us for 4 x 8192, with four 137, in place of 135)
     tb = kNormThreads / pairs < 8 ? kNormThreads / pairs : 8;
     if (tb < (4 * by + heads - 1) / heads) tb = (4 * by + heads - 1) / heads;
+    tb *= 2;
     if (tb > most) tb = most;
   }
   if (tb < 1) tb = 1;
@@ -321,7 +319,6 @@ cudaError_t launch_norm(const RopeTable& rt, const int* positions, int batch, in
     const NormGroup& g = r.g[i];
     if (g.n_heads == 0) continue;
     r.head_magic[i] = (unsigned)(((1ull << 32) + g.n_heads - 1) / g.n_heads);
-    r.head_magic[2] = (unsigned)(((1ull << 32) + heads - 1) / heads);
     wide = wide && wide_strides(g.x, e, g.x_batch, g.x_token, g.x_head) && wide_strides(g.out, e, g.out_batch, g.out_token, g.out_head) &&
            (!backward || wide_strides(g.dy, e, g.dy_batch, g.dy_token, g.dy_head));
   }
