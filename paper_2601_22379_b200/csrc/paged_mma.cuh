@@ -686,11 +686,13 @@ __global__ void __launch_bounds__(kPmThreads, 1)
             tmem_ld128(tS, r);
           }
           // 8-bit pages: a score of block c is r 2^(eq + ek), times the scale; a value stands for its fp16 times 2^ev, which goes into the weight:
-          // y = r c_c + ev, weight 2^(y - m).  (Under a cap, or with a distance: the scores first, ev behind those.)
+          // y = r c_c + ev, weight 2^(y - m).  (Under a cap the scores come first, the scale and ev behind that.)
+          const bool capped = MODS && a.softcap > 0.f;
           if constexpr (BYTES) {
+            const float more = capped ? up : sc2 * up;
 #pragma unroll
             for (int c = 0; c < KEYS / 16; ++c) {
-              const float f = fminf(fmaxf(MODS ? scales[c].x * up : scales[c].x * sc2 * up, 1e-37f), 3e38f), add = MODS ? 0.f : scales[c].y;
+              const float f = fminf(fmaxf(scales[c].x * more, 1e-37f), 3e38f), add = capped ? 0.f : scales[c].y;
 #pragma unroll
               for (int x = 16 * c; x < 16 * c + 16; x += 2) {
                 const float2 v = __ffma2_rn(make_float2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), make_float2(f, f), make_float2(add, add));
@@ -730,7 +732,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
                   r[x + 1] = __float_as_uint(fabsf(v.y) * to_u >= kCapNear ? copysignf(t1 * c2, v.y) : y.y);
                 }
               }
-            } else {
+            } else if (!BYTES) {
 #pragma unroll
               for (int x = 0; x < KEYS; ++x) r[x] = __float_as_uint(__uint_as_float(r[x]) * sc2);
             }
@@ -739,7 +741,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
 #pragma unroll
               for (int x = 0; x < KEYS; ++x) r[x] = __float_as_uint(fmaf(-slope2, fabsf(d0 + (float)x), __uint_as_float(r[x])));
             }
-            if constexpr (BYTES) {
+            if (BYTES && capped) {
 #pragma unroll
               for (int c = 0; c < KEYS / 16; ++c) {
                 const float add = scales[c].y;
