@@ -38,7 +38,10 @@ struct PfSeg {
 
 template <int D>
 struct PfSmem {
-  static constexpr int kTile = kPfKeys * D, NS = D == 128 ? 4 : 7;   // K and V of a stage: 2 kTile
+  // (An even number of stages: with R8 two sets of warps take the tiles in turn, and a stage has to be one set's alone.  A set that is ahead would take the
+  // phase before, which is the other's, for the one that it waits for.)
+  static constexpr int kTile = kPfKeys * D, NS = D == 128 ? 4 : 8;   // K and V of a stage: 2 kTile
+  static_assert(NS % 2 == 0, "a stage is one set's");
   static constexpr int kRing = 0, kMerge = NS * 2 * kTile;           // float [8 warps][16 rows][D], or of 16 warps 8 rows
   static constexpr int kQ = kMerge + kPfBlocks * kPfRows * D * 4;    // bf16 [kPfSegs][16][D]
   static constexpr int kScales = kQ + kPfSegs * kPfRows * D * 2;     // int [NS][16]: exponents of K's blocks, of V's
