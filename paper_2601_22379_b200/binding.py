@@ -726,6 +726,8 @@ class PagedCache:
         """Attention of the new tokens' queries q [total, H_q, d] over the cache, which holds their keys already; max_new and max_len
         bound the new tokens and the length of any sequence.  Returns out [total, H_q, d] and lse fp32 [total, H_q].  See
         spla_paged_mask_t for the mask; `sinks` first tokens stay visible beside a window (`spla_paged_attend_sinks`)."""
+        if sinks > 0x7fffffff:
+            raise ValueError("paged cache: sinks is an int32")
         total, hq, dev = q.shape[0], self.n_q_heads, self.device
         qs = self._rows(q, total, hq, self.q_torch_dtype, "q")
         if out is None:

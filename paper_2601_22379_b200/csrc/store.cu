@@ -214,6 +214,7 @@ __global__ void __launch_bounds__(kStoreThreads, 2) store_kernel(const __grid_co
           scale_at = (GI == 1 ? r.k_scales : r.v_scales) + (crow >> 4);
           if (off > 0) e_old = held_exponent(scale_at);
         }
+        __syncwarp();                                      // (all lanes have read the byte before one writes it)
       }
       const float2* tab = table + (t0 + first) * pairs;
       T* out = GI == 0 ? reinterpret_cast<T*>(r.q_out) + (tok0 + t0 + first) * r.q_out_stride + (long long)h * D

@@ -4,7 +4,7 @@ import torch
 
 from paper_2601_22379_b200 import binding
 from tests import paged_bytes_reference as ref8
-from tests.test_gpu_paged import Batch, kinds
+from tests.test_gpu_paged import TYPES, Batch, kinds
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +55,42 @@ def test_sinks_with_documents_are_refused():
     assert e.value.status == binding.SPLA_ERR_UNSUPPORTED
     with pytest.raises(binding.SplaError):
         b.attend(window=10, sinks=-1)
+    with pytest.raises(ValueError):
+        b.attend(window=10, sinks=2 ** 32)
+
+
+def test_as_many_sinks_as_there_are():
+    """The largest number: every key is visible, as without a window."""
+    b = Batch([1, 40], [300, 100])
+    out, lse = b.attend(window=3, sinks=2 ** 31 - 1)
+    assert b.cache.sync_status() == 0
+    check(b, out, lse)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "f32"])
+def test_over_an_spla_cache(kv):
+    """Its pages read back are what was appended, and sinks beside a window are those of the same tokens in pages of their own."""
+    B, hq, hkv, d, T = 3, 8, 2, 128, 300
+    cfg = binding.make_config(batch=B, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, block_size=64, top_k=8, max_context=512, kv_dtype=kv, flags=binding.SPLA_NO_RLA)
+    cache = binding.SplaCache(cfg, "cuda:0")
+    t = TYPES[kv]
+    g = torch.Generator(device="cuda:0").manual_seed(2)
+    k, v = (torch.randn(B, hkv, T, d, device="cuda:0", generator=g).to(t) for _ in range(2))
+    q = torch.randn(B, hq, d, device="cuda:0", generator=g).to(t)
+    lens = [300, 1, 129]
+    cache.append_tokens(k, v, torch.tensor(lens, dtype=torch.int32, device="cuda:0"))
+    pages = binding.PagedCache.of(cache)
+    cu = torch.tensor([0, 300, 301, 430], dtype=torch.int32, device="cuda:0")
+    kr, vr = pages.read(cu, cache.bufs.seq_lens, pages.table(), 430)
+    rows = lambda x: torch.cat([x[b, :, :n].transpose(0, 1) for b, n in enumerate(lens)])  # noqa: E731
+    assert torch.equal(kr, rows(k)) and torch.equal(vr, rows(v))
+
+    b = Batch([1, 1, 1], [n - 1 for n in lens], hq=hq, hkv=hkv, d=d, P=64, kv=kv, q=kv)
+    own = torch.arange(3, dtype=torch.int32, device="cuda:0")
+    b.cache.append(rows(k), rows(v), cu, b.lens_t, b.table)
+    kw = dict(window=30, sinks=5)
+    cu1 = torch.arange(B + 1, dtype=torch.int32, device="cuda:0")
+    got = pages.attend(q, cu1, cache.bufs.seq_lens, pages.table(), 1, 300, **kw)
+    want = b.cache.attend(q, cu1, b.lens_t, b.table, 1, 300, **kw)
+    assert pages.sync_status() == 0 and b.cache.sync_status() == 0
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
