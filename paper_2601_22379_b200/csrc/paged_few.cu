@@ -9,7 +9,7 @@
 // segment.  (tcgen05 would want the values widened in shared memory: four times the traffic there, and 128 rows for 16.)  Which channel is which of a
 // product's k, and which of its columns, is free: a lane takes 32 neighbouring bytes of a token of K, 16 of a token of V.
 // The scales never touch the values: K's multiply a warp's 16 scores, V's are exponents and go into that of the weights, so that the
-// weights of a row are all at most 2^15 whatever the blocks' scales are, and fp16 holds them to 2^-12 of themselves and 2^-40 of the largest.  Queries are
+// weights of a row are at most 2^15, the largest at least 2^14, whatever the blocks' scales are, and fp16 holds them to 2^-11 of themselves and 2^-39 of the largest.  Queries are
 // scaled by a power of two to below 2^15: fp16 holds bf16's eight bits down to 2^-28 of a row's largest channel.  Products are exact, sums fp32: each
 // tile's are started anew and added to O in fp32 (the tensor core truncates when it adds into an accumulator).
 //
@@ -382,35 +382,77 @@ __global__ void __launch_bounds__(kPfThreads<R8>, 1)
             }
           }
           // ---- weights
-          float f[2];
+          float f[2], top[2], up[2];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) up[x] = power_of_two(min(max(qe[x] + ek, -126), 127));
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int y = 0; y < TOKENS; ++y) p[x][y] = p[x][y] * up[x] * sc2;
+          if constexpr (MODS) {
+            if (cap > 0.f) {                       // cap tanh(z / cap), in base 2 (see paged_mma.cuh)
+              float most = 0.f;
+#pragma unroll
+              for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int y = 0; y < TOKENS; ++y) most = fmaxf(most, fabsf(p[x][y]));
+              const bool far = __any_sync(0xffffffffu, most * to_u >= kCapNear);
+#pragma unroll
+              for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int y = 0; y < TOKENS; y += 2) {
+                  const float2 z = make_float2(p[x][y], p[x][y + 1]), u = __fmul2_rn(z, make_float2(to_u, to_u)), u2 = __fmul2_rn(u, u);
+                  float2 c = __ffma2_rn(u2, make_float2(-0.048268907f, -0.048268907f), make_float2(0.13284431f, 0.13284431f));
+                  c = __ffma2_rn(u2, c, make_float2(-0.33331972f, -0.33331972f));
+                  c = __fmul2_rn(z, __ffma2_rn(u2, c, make_float2(0.99999994f, 0.99999994f)));
+                  p[x][y] = c.x;
+                  p[x][y + 1] = c.y;
+                  if (far) {
+                    auto other = [&](float& to, float v) {
+                      if (fabsf(v) >= kCapNear) to = copysignf(fmaf(-2.f, rcp_approx(1.f + ex2(fabsf(v) * (2.f * kLog2e))), 1.f), v) * (cap * kLog2e);
+                    };
+                    other(p[x][y], u.x);
+                    other(p[x][y + 1], u.y);
+                  }
+                }
+            }
+            if (a.slopes)
+#pragma unroll
+              for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int y = 0; y < TOKENS; ++y) p[x][y] = fmaf(-slope2[x], fabsf((float)(key0 - pos[x] + token_of(y))), p[x][y]);
+          }
+          if (part)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+              for (int y = 0; y < TOKENS; ++y) {
+                const int j = key0 + token_of(y);
+                if (!((j >= see[x].lo || j < a.sinks) && j < see[x].hi)) p[x][y] = -INFINITY;
+              }
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const float up = power_of_two(min(max(qe[x] + ek, -126), 127));
-            float top = -INFINITY;
+            top[x] = -INFINITY;
 #pragma unroll
-            for (int y = 0; y < TOKENS; ++y) {
-              float z = p[x][y] * up * sc2;
-              if constexpr (MODS) {
-                if (cap > 0.f) {                   // cap tanh(z / cap), in base 2 (see paged_mma.cuh)
-                  const float u = z * to_u, u2 = u * u;
-                  const float near = fmaf(u2, fmaf(u2, fmaf(u2, -0.048268907f, 0.13284431f), -0.33331972f), 0.99999994f) * u;
-                  const float far = copysignf(fmaf(-2.f, rcp_approx(1.f + ex2(fabsf(u) * (2.f * kLog2e))), 1.f), u);
-                  z = (fabsf(u) >= kCapNear ? far : near) * (cap * kLog2e);
-                }
-                if (a.slopes) z = fmaf(-slope2[x], fabsf((float)(key0 - pos[x] + token_of(y))), z);
+            for (int y = 0; y < TOKENS; ++y) top[x] = fmaxf(top[x], p[x][y]);
+            top[x] += (float)(ev - 15);
+            f[x] = 1.f;
+          }
+          // The first tokens that a row sees set its maximum, one above what their weights need; later ones only move it when a weight would exceed 2^15.
+          if (__any_sync(0xffffffffu, top[0] > m[0] || top[1] > m[1])) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+#pragma unroll
+              for (int w = R8 ? 4 : 1; w < (R8 ? 32 : 4); w <<= 1) top[x] = fmaxf(top[x], __shfl_xor_sync(0xffffffffu, top[x], w));
+              if (top[x] > m[x]) {
+                f[x] = ex2(m[x] - (top[x] + 1.f));
+                m[x] = top[x] + 1.f;
               }
-              if (part) {
-                const int j = key0 + token_of(y);
-                if (!((j >= see[x].lo || j < a.sinks) && j < see[x].hi)) z = -INFINITY;
-              }
-              p[x][y] = z;
-              top = fmaxf(top, z);
             }
+          }
 #pragma unroll
-            for (int w = R8 ? 4 : 1; w < (R8 ? 32 : 4); w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-            const float mn = fmaxf(m[x], top + (float)(ev - 15));           // (the largest weight is 2^15)
-            f[x] = m[x] == mn ? 1.f : ex2(m[x] - mn);
-            m[x] = mn;
+          for (int x = 0; x < 2; ++x) {
+            const float mn = m[x];
             const float nm = mn == -INFINITY ? 0.f : (float)ev - mn;
             float sum = 0.f;
 #pragma unroll

@@ -61,7 +61,7 @@ def attend(q, k, v, cu, lens, table, kernel, exps, sm_scale=None, softcap=0.0, w
     anywhere (for the weights that fp16 cannot hold).  Returns out, lse and bounds as paged_reference.attend, whose terms hold here too; besides:
 
     few: queries in fp16 below 2^15 of the row's largest channel are off by 2^-39 of it at most; chunk: what e4m3 and e5m2 leave is at most 2^-21 of it.
-    Weights are rounded to fp16, half a step, 2^-11; those it cannot hold are off by 2^-25 of a scale where the largest is 2^15 (few) or at least 2^11 (chunk).
+    Weights are rounded to fp16, half a step, 2^-11; those it cannot hold are off by 2^-25 of a scale where the largest is at least 2^14 (few) or 2^11 (chunk).
     chunk: the tensor core cuts off less than 2^-23 of a sum at each addition of 16 tokens, over 128 tiles at most."""
     total, hq, d = q.shape
     hkv = k.shape[1]
@@ -113,7 +113,7 @@ def attend(q, k, v, cu, lens, table, kernel, exps, sm_scale=None, softcap=0.0, w
                 e = e + 2.0 ** -20 + 2.0 ** -23 * (s.abs().nan_to_num(posinf=0.0, neginf=0.0, nan=0.0) + 90) + e * e
                 mass, lse_e = w @ va, (w * e).sum(-1)
                 rel = {"general": 0.0, "few": 2.0 ** -11, "chunk": 2.0 ** -11 + min(L / 16 + 8, 1024) * 2.0 ** -23}[how]
-                least = {"general": 0.0, "few": 2.0 ** -40, "chunk": 2.0 ** -36}[how] * L * 448 * 2.0 ** exps * w.amax(-1, keepdim=True)
+                least = {"general": 0.0, "few": 2.0 ** -39, "chunk": 2.0 ** -36}[how] * L * 448 * 2.0 ** exps * w.amax(-1, keepdim=True)
                 out[r0:r1, m] = o
                 lse[r0:r1, m] = torch.where(z[:, 0] == 0, torch.full_like(top[:, 0], -math.inf), top[:, 0] + torch.log(z[:, 0]))
                 out_b[r0:r1, m] = (w * e) @ va + lse_e[:, None] * mass + rel * mass + least

@@ -188,6 +188,15 @@ def test_score_scales(q, flags, scale):
     Batch([1, 2, 40], [100, 300, 90], d=64, q=q, flags=flags, sm_scale=scale, size=0.2).run()
 
 
+@pytest.mark.parametrize("cap", [1e30, 3e38])
+def test_a_cap_that_is_none(cap):
+    """Up to the end of fp32: scores far below it stay what they are."""
+    b = Batch([1, 2, 40], [100, 300, 90], d=64)
+    out, lse = b.attend(softcap=cap)
+    assert b.cache.sync_status() == 0
+    b.check(out, lse)
+
+
 @kinds
 def test_what_a_row_does_not_see_does_not_touch_it(q, flags):
     """NaN among keys and values that some rows see and others do not: the former are NaN (one channel, for a value), the latter as ever."""
