@@ -45,7 +45,9 @@ namespace spla {
 
 namespace {
 
-constexpr int kPmThreads = 384;
+// (four warps more widen the values of 8-bit pages for launches of few rows, which are bound by that otherwise: 8 new tokens on 32768 x8 246 -> 168 us.
+// Elsewhere they would cost the softmax registers: prompt of 8192 721 -> 733.)
+template <bool FEW, bool BYTES> constexpr int kPmThreads = FEW && BYTES ? 512 : 384;
 constexpr int kPmScales = 8;                       // tiles whose scales are kept: more than are between their copies and the softmax (NK + 2)
 constexpr int kPmKeys = 128;                       // keys per tile
 constexpr int kPmDrain = 128;                      // tiles that are added up in O before it is drained: 1024 truncations, each of less than 2^-23: 2^-13 at most
@@ -207,12 +209,14 @@ __device__ __forceinline__ float pm_undrain(uint32_t tO, float* drain, int slot,
 
 // LONG: caches of more than kPmDrain tiles (the others go without what drains O: 106 us for a mixed batch in place of 108).
 template <int D, bool MODS, bool FEW, bool LONG, bool BYTES>
-__global__ void __launch_bounds__(kPmThreads, 1)
+__global__ void __launch_bounds__(kPmThreads<FEW, BYTES>, 1)
     paged_mma_kernel(const PagedAttend a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                      const __grid_constant__ CUtensorMap map_q) {
   using SM = PmSmem<D, FEW, BYTES>;
   static_assert(!BYTES || SM::NK + 2 <= kPmScales, "scales of tiles on their way");
   constexpr int H = SM::H, NK = SM::NK, NV = SM::NV;
+  constexpr bool MORE = FEW && BYTES;                             // warps 12 to 15 widen values, otherwise warp 2
+  constexpr int WIDENERS = MORE ? 4 : 1;
   extern __shared__ __align__(1024) unsigned char smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + SM::kBars);
   uint64_t *k_full = bars, *k_empty = k_full + NK, *v_full = k_empty + NK, *v_empty = v_full + NV, *q_full = v_empty + NV, *q_empty = q_full + 1,
@@ -229,7 +233,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
 
   if (tid == 0) {
     for (int s = 0; s < NK; ++s) { mbar_init(&k_full[s], 1);  mbar_init(&k_empty[s], 1); }
-    for (int s = 0; s < NV; ++s) { mbar_init(&v_full[s], 1);  mbar_init(&v_empty[s], 1); }
+    for (int s = 0; s < NV; ++s) { mbar_init(&v_full[s], WIDENERS);  mbar_init(&v_empty[s], 1); }
     mbar_init(q_full, 1);
     mbar_init(q_empty, 1);
     for (int s = 0; s < 2; ++s) {
@@ -243,10 +247,10 @@ __global__ void __launch_bounds__(kPmThreads, 1)
     mbar_init(quarters, 4);
     mbar_init(done, 1);
     if (BYTES) {
-      for (int s = 0; s < SM::NR; ++s) { mbar_init(&r_full[s], 1);  mbar_init(&r_empty[s], 1); }
+      for (int s = 0; s < SM::NR; ++s) { mbar_init(&r_full[s], 1);  mbar_init(&r_empty[s], WIDENERS); }
       for (int s = 0; s < kPmScales; ++s) mbar_init(&sc_full[s], 1);
     }
-    for (int s = 0; s < kPmSegs; ++s) { mbar_init(&seg_full[s], 1);  mbar_init(&seg_empty[s], 11); }   // K, V, MMA and eight softmax warps
+    for (int s = 0; s < kPmSegs; ++s) { mbar_init(&seg_full[s], 1);  mbar_init(&seg_empty[s], 10 + WIDENERS); }   // K, V, MMA and eight softmax warps
     mbar_init_done();
     *abort_flag = 0;
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
@@ -257,7 +261,7 @@ __global__ void __launch_bounds__(kPmThreads, 1)
   pdl_wait();
   pdl_launch_dependents();
   tc_fence_before();
-  const long long share = paged_share(a.w, paged_fill_seqs(a, seqs, tid, kPmThreads));   // (ends with a barrier)
+  const long long share = paged_share(a.w, paged_fill_seqs(a, seqs, tid, kPmThreads<FEW, BYTES>));   // (ends with a barrier)
   tc_fence_after();
   const uint32_t tmem = *tmem_base_s;
   const uint32_t sbase = smem_u32(smem);
@@ -286,8 +290,48 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         tma_load_q(sbase + SM::kQ + s * (FEW ? 32 * 128 : SM::kTile) + x * SM::kHalf, &map_q, x, sg.h * G, sg.row0 + sg.first + (FEW ? 0 : s * ppos), q_full);
   };
 
+  // 8-bit pages: V as fp16, in which e4m3 is exact (its scales stay out of the products: see the softmax).  A lane takes 16 bytes of every fourth (or eighth)
+  // token; two rows x four pieces of one array are stored side by side: no bank twice.  `who`: which of the WIDENERS.
+  auto widen_values = [&](int who) {
+    constexpr int PIECES = D / 16, ROWS = 32 / PIECES;        // of a row; rows at a time
+    const int piece = D == 128 ? (lane & 3) + (lane >> 1 & 4) : lane & 3, r0 = D == 128 ? (lane >> 2 & 1) + (lane >> 3 & 2) : lane >> 2;
+    const int c0 = 2 * (piece & 3);
+    int kt = 0;
+    bool ok = true;
+    each_segment(ok, [&](const PmSeg& sg) {
+      const int A = sg.pl.A, E = sg.pl.E;
+#pragma unroll 1
+      for (int t = A; t < E; ++t, ++kt) {
+        const int st = kt % NV, sr = kt % SM::NR;
+        if (!pm_wait(&r_full[sr], (kt / SM::NR) & 1, lim, abort_flag)) return false;
+        if (kt >= NV && !pm_wait(&v_empty[st], ((kt / NV) - 1) & 1, lim, abort_flag)) return false;
+        const unsigned char* raw = smem + SM::kR + sr * SM::kRaw + r0 * D;
+        unsigned char* tile = smem + SM::kV + st * SM::kTile + (piece >> 2) * SM::kHalf + r0 * 128;
+#pragma unroll 8
+        for (int x = 0; x < kPmKeys / ROWS / WIDENERS; ++x) {
+          const int at = ROWS * (x * WIDENERS + who), row = at + r0;
+          const uint4 w = *reinterpret_cast<const uint4*>(raw + at * D + ((D == 128 ? piece ^ (row & 7) : piece ^ (row >> 1 & 3)) << 4));
+          uint4 y0, y1;
+          widen(w.x, y0.x, y0.y);
+          widen(w.y, y0.z, y0.w);
+          widen(w.z, y1.x, y1.y);
+          widen(w.w, y1.z, y1.w);
+          *reinterpret_cast<uint4*>(tile + at * 128 + ((c0 ^ (row & 7)) << 4)) = y0;
+          *reinterpret_cast<uint4*>(tile + at * 128 + (((c0 + 1) ^ (row & 7)) << 4)) = y1;
+        }
+        proxy_fence();                                        // (tile written -> tensor core)
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive1(&v_full[st]);
+          mbar_arrive1(&r_empty[sr]);
+        }
+      }
+      return true;
+    });
+    if (!ok) *abort_flag = 1;
+  };
   if (wg == 0) {
-    warpgroup_reg_dec<120>();                                     // (120 + 2 x 192 = 3 x 168, what the CTA is launched with)
+    warpgroup_reg_dec<MORE ? 96 : 120>();                         // (120 + 2 x 192 = 3 x 168, 2 x 96 + 2 x 160 = 4 x 128: what the CTA is launched with)
     if (BYTES && (warp == 0 || warp == 2)) {
       if (warp == 0) {
         // ---------------------------------------------------------- 8-bit pages: TMA of K and V, scales ---------------------
@@ -348,46 +392,8 @@ __global__ void __launch_bounds__(kPmThreads, 1)
         for (int x = max(0, kt + k_more - NK); x < kt + k_more; ++x) warp_waits(&k_full[x % NK], (x / NK) & 1, lim);
         for (int x = max(0, kt - SM::NR); x < kt; ++x) warp_waits(&r_full[x % SM::NR], (x / SM::NR) & 1, lim);
         if (seg > 0) warp_waits(q_full, (seg - 1) & 1, lim);
-      } else {
-        // ---------------------------------------------------------- 8-bit pages: V as fp16, in which e4m3 is exact -----------
-        // (its scales stay out of the products: see the softmax.)  A lane takes 16 bytes of every fourth (or eighth) token; two rows x four pieces of one
-        // array are stored side by side: no bank twice.
-        constexpr int PIECES = D / 16, ROWS = 32 / PIECES;        // of a row; rows at a time
-        const int piece = D == 128 ? (lane & 3) + (lane >> 1 & 4) : lane & 3, r0 = D == 128 ? (lane >> 2 & 1) + (lane >> 3 & 2) : lane >> 2;
-        const int c0 = 2 * (piece & 3);
-        int kt = 0;
-        bool ok = true;
-        each_segment(ok, [&](const PmSeg& sg) {
-          const int A = sg.pl.A, E = sg.pl.E;
-#pragma unroll 1
-          for (int t = A; t < E; ++t, ++kt) {
-            const int st = kt % NV, sr = kt % SM::NR;
-            if (!pm_wait(&r_full[sr], (kt / SM::NR) & 1, lim, abort_flag)) return false;
-            if (kt >= NV && !pm_wait(&v_empty[st], ((kt / NV) - 1) & 1, lim, abort_flag)) return false;
-            const unsigned char* raw = smem + SM::kR + sr * SM::kRaw + r0 * D;
-            unsigned char* tile = smem + SM::kV + st * SM::kTile + (piece >> 2) * SM::kHalf + r0 * 128;
-#pragma unroll 8
-            for (int x = 0; x < kPmKeys / ROWS; ++x) {
-              const int at = ROWS * x, row = at + r0;
-              const uint4 w = *reinterpret_cast<const uint4*>(raw + at * D + ((D == 128 ? piece ^ (row & 7) : piece ^ (row >> 1 & 3)) << 4));
-              uint4 y0, y1;
-              widen(w.x, y0.x, y0.y);
-              widen(w.y, y0.z, y0.w);
-              widen(w.z, y1.x, y1.y);
-              widen(w.w, y1.z, y1.w);
-              *reinterpret_cast<uint4*>(tile + at * 128 + ((c0 ^ (row & 7)) << 4)) = y0;
-              *reinterpret_cast<uint4*>(tile + at * 128 + (((c0 + 1) ^ (row & 7)) << 4)) = y1;
-            }
-            proxy_fence();                                        // (tile written -> tensor core)
-            __syncwarp();
-            if (lane == 0) {
-              mbar_arrive1(&v_full[st]);
-              mbar_arrive1(&r_empty[sr]);
-            }
-          }
-          return true;
-        });
-        if (!ok) *abort_flag = 1;
+      } else if (!MORE) {
+        widen_values(0);
       }
     } else if (warp == 0 || warp == 2) {
       // ------------------------------------------------------------ TMA: queries and K, or V ----------------------------
@@ -555,9 +561,12 @@ __global__ void __launch_bounds__(kPmThreads, 1)
       }
       if (a.w.cuts && lane == 0) a.w.cuts[blockIdx.x] = cut;
     }
+  } else if (MORE && wg == 3) {
+    warpgroup_reg_dec<96>();
+    widen_values(warp & 3);
   } else {
     // -------------------------------------------------------------- softmax and epilogue: one row per thread -------------
-    warpgroup_reg_inc<192>();
+    warpgroup_reg_inc<MORE ? 160 : 192>();
     const int slot = wg - 1, thr = tid - 128 * wg, row = FEW ? lane : thr, pi = row / G, g = row % G;
     constexpr int KEYS = FEW ? 32 : kPmKeys;                      // keys of a tile that a thread takes
     const int kb = FEW ? 32 * (warp & 3) : 0;                     // the first of them
@@ -1089,7 +1098,7 @@ cudaError_t mma_variant(const PagedAttend& a, const PagedMaps& maps, cudaStream_
   static unsigned long long allowed = 0;
   cudaError_t e = allow_smem_once(kern, bytes, allowed);
   if (e != cudaSuccess) return e;
-  return launch_ex(kern, dim3(a.w.n_cta), dim3(kPmThreads), bytes, s, 0, true, a, *reinterpret_cast<const CUtensorMap*>(maps.k),
+  return launch_ex(kern, dim3(a.w.n_cta), dim3(kPmThreads<FEW, BYTES>), bytes, s, 0, true, a, *reinterpret_cast<const CUtensorMap*>(maps.k),
                    *reinterpret_cast<const CUtensorMap*>(maps.v), *reinterpret_cast<const CUtensorMap*>(maps.q));
 }
 template <int D, bool MODS, bool FEW, bool BYTES>
