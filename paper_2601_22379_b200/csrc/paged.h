@@ -483,6 +483,17 @@ cudaError_t launch_paged_few(const PagedAttend& a, const PagedMaps& maps, cudaSt
 // paged_split.cu: bf16 queries as two parts of 8 bits, [token][head][part][d], and the exponents of the rows' scales [token][head]
 size_t paged_split_bytes(const PagedLayout& pl, int total_new, size_t* exps);
 cudaError_t launch_paged_split(const PagedLayout& pl, const void* q, long long q_stride, int total_new, unsigned char* parts, signed char* exps, cudaStream_t s);
+// ... or the cached tokens as bf16 pages of kWidePage tokens: their layout, and the places of the values and of the page table behind the keys
+constexpr int kWidePage = 128;
+struct PagedWide {
+  PagedLayout pl;
+  int cols;                             // pages of a sequence
+  size_t v_at, table_at, bytes;
+  bool fits;                            // (rows that a TMA coordinate can name)
+};
+PagedWide paged_wide(const PagedLayout& pl, const PagedBatch& pb);
+cudaError_t launch_paged_widen(const PagedBatch& pb, const PagedLayout& pl, const PagedPages& pages, const PagedWide& w, int from_new, int window, int sinks, void* to,
+                               cudaStream_t s);
 // paged_mma.cu: bf16 on tcgen05
 size_t paged_mma_drain_bytes(const PagedWork& w, const PagedBatch& pb, const PagedLayout& pl);
 int paged_mma_positions(const PagedBatch& pb, const PagedLayout& pl);   // new tokens of a row tile: the query boxes' size

@@ -290,14 +290,16 @@ extern "C" int spla_paged_read(spla_paged_t* p, const spla_paged_batch_t* batch,
   return e == cudaSuccess ? SPLA_OK : cuda_fail(e, "spla_paged_read");
 }
 
-// Which kernel a launch is: fp32 arithmetic, bf16 on the tensor cores, 8-bit pages with few rows, 8-bit pages on the tensor cores.
-enum PagedKernel { kGeneral, kTensor, kFew, kTensorBytes };
+// Which kernel a launch is: fp32 arithmetic, bf16 on the tensor cores, 8-bit pages with few rows, 8-bit pages on the tensor cores, the same widened to bf16 before.
+enum PagedKernel { kGeneral, kTensor, kFew, kTensorBytes, kTensorWide };
 
 // The plan of one launch (a batch of at most kPagedMaxBatch sequences), the bytes of its partial results and of the sums of long walks,
 // and their places in the workspace, where there is one (no cuts: whole units only).
-// (8-bit pages: where a sequence may have more rows than the kernel for few takes, the queries' parts lie in front, the same for all launches of a call.)
+// (8-bit pages: where a sequence may have more rows than the kernel for few takes, the queries' parts lie in front, the same for all launches of a call; or in
+// their place, where they take no more than that, the widened tokens.)
 static size_t plan_attend(const spla_paged* p, PagedBatch pb, PagedKernel kernel, PagedWork* w, void* workspace) {
-  const bool tensor = kernel == kTensor || kernel == kTensorBytes, parts = (kernel == kFew || kernel == kTensorBytes) && pb.max_new > paged_few_positions(p->pl);
+  const bool tensor = kernel == kTensor || kernel == kTensorBytes || kernel == kTensorWide;
+  const bool parts = kernel != kGeneral && kernel != kTensor && pb.max_new > paged_few_positions(p->pl);
   if (kernel == kFew && pb.max_new > paged_few_positions(p->pl)) pb.max_new = paged_few_positions(p->pl);   // (the others are another launch's)
   if (tensor) paged_plan_mma(w, pb, p->pl, p->sm_count);
   else if (kernel == kFew) paged_plan_few(w, pb, p->pl, p->sm_count);
@@ -406,8 +408,19 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
   PagedMaps maps;
   const bool rows16 = aligned(q, 16) && q_stride % 8 == 0, few = p->few && rows16;
   const bool parts = few && pb.max_new > paged_few_positions(p->pl);               // some sequences may have more rows: their queries in two parts
-  const bool tensor = (p->tensor || parts) && rows16 && cap_fits(p->cfg.sm_scale, mask->softcap) &&
-                      make_q_map(maps.q, parts ? workspace : q, p->pl, parts ? q_row : q_stride, pb);
+  const bool tensor_fits = (p->tensor || parts) && rows16 && cap_fits(p->cfg.sm_scale, mask->softcap);
+  // More rows than few: where there are many for each key, the keys and values are widened to bf16 in a pass of their own, once for all rows (a prompt of 8192
+  // @wide).  The measure is that they take no more of the workspace than the queries' parts, @wide2.  (Documents: which
+  // keys are looked at is not known before.)
+  const PagedWide w = paged_wide(p->pl, pb);
+  size_t exps = 0;
+  char* front = reinterpret_cast<char*>(workspace);
+  PagedMaps wide_maps;
+  const bool wide = tensor_fits && parts && !mask->first_key && w.fits && w.bytes <= paged_split_bytes(p->pl, pb.total_new, &exps) &&
+                    make_kv_map(wide_maps.k, front, p->pl.d, kWidePage, (unsigned long long)w.pl.n_pages * w.pl.page_stride) &&
+                    make_kv_map(wide_maps.v, front + w.v_at, p->pl.d, kWidePage, (unsigned long long)w.pl.n_pages * w.pl.page_stride) &&
+                    make_q_map(wide_maps.q, q, p->pl, q_stride, pb);
+  const bool tensor = !wide && tensor_fits && make_q_map(maps.q, parts ? workspace : q, p->pl, parts ? q_row : q_stride, pb);
   if (tensor || few) {
     memcpy(maps.k, p->maps.k, sizeof(maps.k));
     memcpy(maps.v, p->maps.v, sizeof(maps.v));
@@ -421,13 +434,22 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
     switch (kernel) {
       case kTensor: e = launch_paged_mma(a, maps, s); break;
       case kFew: e = launch_paged_few(a, maps, s); break;
+      case kTensorWide: {
+        PagedAttend b = a;
+        b.pl = w.pl;
+        b.pb.table = reinterpret_cast<const int*>(front + w.table_at) + (long long)a.pb.first * w.cols;
+        b.pb.table_stride = w.cols;
+        e = launch_paged_mma(b, wide_maps, s);
+        break;
+      }
       case kTensorBytes: e = p->pl.d == 128 ? launch_paged_mma_bytes128(a, maps, s) : launch_paged_mma_bytes64(a, maps, s); break;
       default: e = launch_paged_general(a, p->pages, q16, s);
     }
     if (e == cudaSuccess) e = launch_paged_join(a, q16, s);
   };
-  if (parts && tensor) {
-    size_t exps;
+  if (wide) {
+    e = launch_paged_widen(pb, p->pl, p->pages, w, paged_few_positions(p->pl) + 1, a.window, a.sinks, front, s);
+  } else if (parts && tensor) {
     paged_split_bytes(p->pl, pb.total_new, &exps);
     unsigned char* at = reinterpret_cast<unsigned char*>(workspace);
     a.q_exp = reinterpret_cast<signed char*>(at + exps);
@@ -439,7 +461,7 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
     if (few) {                                                                     // two launches where a sequence may have more rows
       const int most = paged_few_positions(p->pl);
       launch(kFew, 0, most);
-      if (parts) launch(tensor ? kTensorBytes : kGeneral, most + 1, 0x7fffffff);
+      if (parts) launch(wide ? kTensorWide : tensor ? kTensorBytes : kGeneral, most + 1, 0x7fffffff);
     } else {
       launch(tensor ? kTensor : kGeneral, 0, 0);
     }

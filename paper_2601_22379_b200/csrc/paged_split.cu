@@ -72,7 +72,92 @@ __global__ void __launch_bounds__(kSplitThreads) paged_split_kernel(const __nv_b
   }
 }
 
+
+// Cached tokens as bf16 pages of 128 tokens, for sequences of from_new new tokens and more: page `col` of sequence b is number b cols + col.
+// Block (page, head).  Those that no row walks stay as they are (and their pages' numbers unread), as do the rows behind the end.
+template <int D>
+__global__ void __launch_bounds__(kSplitThreads) paged_widen_kernel(const __grid_constant__ PagedBatch pb, const __grid_constant__ PagedLayout pl,
+                                                                    const __grid_constant__ PagedPages pages, int cols, int from_new, int window, int sinks,
+                                                                    __nv_bfloat16* k, __nv_bfloat16* v, int* table) {
+  constexpr int PIECES = D / 16, EACH = kWidePage * PIECES / kSplitThreads;       // of a row; of a thread
+  __shared__ long long rows[kWidePage / 16];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int tid = threadIdx.x, b = blockIdx.x / cols, col = blockIdx.x - b * cols, h = blockIdx.y, tok0 = col * kWidePage;
+  const PagedSeq s = paged_seq(pb, pl.status, b);
+  if (tid == 0 && h == 0) table[blockIdx.x] = blockIdx.x;
+  if (s.n < from_new || tok0 >= s.L) return;
+  if (window > 0 && tok0 >= sinks && tok0 + kWidePage <= s.L - s.n - window + 1) return;
+  if (tid < kWidePage >> pl.log_p && tok0 + (tid << pl.log_p) < s.L) rows[tid] = paged_row(pb, pl, b, h, (tok0 >> pl.log_p) + tid);
+  __syncthreads();
+  uint4 w[2][EACH];
+  float mul[2][EACH];
+#pragma unroll
+  for (int x = 0; x < EACH; ++x) {
+    const int piece = tid + x * kSplitThreads, r = piece / PIECES, c = piece % PIECES * 16;
+    long long row = tok0 + r < s.L ? rows[r >> pl.log_p] : -1;
+    if (row >= 0) row += r & (pl.P - 1);
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      w[y][x] = make_uint4(0u, 0u, 0u, 0u);                                        // (a page number outside the pool: zeros)
+      mul[y][x] = 1.f;
+      if (row >= 0) {
+        w[y][x] = *reinterpret_cast<const uint4*>(reinterpret_cast<const unsigned char*>(y ? pages.v : pages.k) + row * D + c);
+        mul[y][x] = paged_scale(y ? pages.v_scales : pages.k_scales, row);
+      }
+    }
+  }
+  const long long row0 = ((long long)blockIdx.x * pl.Hkv + h) * kWidePage;
+#pragma unroll
+  for (int x = 0; x < EACH; ++x) {
+    const int piece = tid + x * kSplitThreads, r = piece / PIECES, c = piece % PIECES * 16;
+    if (tok0 + r >= s.L) continue;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const uint32_t from[4] = {w[y][x].x, w[y][x].y, w[y][x].z, w[y][x].w};
+      uint32_t to[8];
+#pragma unroll
+      for (int z = 0; z < 4; ++z) {
+        uint32_t lo, hi;
+        widen(from[z], lo, hi);
+        const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), e = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+        to[2 * z] = pack_bf16(a.x * mul[y][x], a.y * mul[y][x]);
+        to[2 * z + 1] = pack_bf16(e.x * mul[y][x], e.y * mul[y][x]);
+      }
+      uint4* at = reinterpret_cast<uint4*>((y ? v : k) + (row0 + r) * D + c);
+      at[0] = make_uint4(to[0], to[1], to[2], to[3]);
+      at[1] = make_uint4(to[4], to[5], to[6], to[7]);
+    }
+  }
+}
+
 }  // namespace
+
+PagedWide paged_wide(const PagedLayout& pl, const PagedBatch& pb) {
+  PagedWide w = {};
+  w.cols = (pb.max_len + kWidePage - 1) / kWidePage;
+  const long long pages = (long long)pb.batch * w.cols;
+  const size_t tokens = (size_t)pages * pl.Hkv * kWidePage;
+  w.pl = pl;
+  w.pl.P = kWidePage;
+  w.pl.log_p = 7;
+  static_assert(kWidePage == 1 << 7, "tokens of a page");
+  w.pl.n_pages = (int)pages;
+  w.pl.page_stride = (long long)pl.Hkv * kWidePage;
+  w.pl.head_stride = kWidePage;
+  w.v_at = tokens * pl.d * 2;
+  w.table_at = 2 * w.v_at;
+  w.bytes = w.table_at + (size_t)pages * 4;
+  w.fits = tokens < (1ull << 31) - 256;
+  return w;
+}
+
+cudaError_t launch_paged_widen(const PagedBatch& pb, const PagedLayout& pl, const PagedPages& pages, const PagedWide& w, int from_new, int window, int sinks, void* to,
+                               cudaStream_t s) {
+  unsigned char* at = reinterpret_cast<unsigned char*>(to);
+  return launch_ex(pl.d == 128 ? paged_widen_kernel<128> : paged_widen_kernel<64>, dim3((unsigned)w.pl.n_pages, (unsigned)pl.Hkv), dim3(kSplitThreads), 0, s, 0, true, pb, pl,
+                   pages, w.cols, from_new, window, sinks, (__nv_bfloat16*)at, (__nv_bfloat16*)(at + w.v_at), (int*)(at + w.table_at));
+}
 
 size_t paged_split_bytes(const PagedLayout& pl, int total_new, size_t* exps) {
   const size_t rows = (size_t)total_new * pl.Hq;

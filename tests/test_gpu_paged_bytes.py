@@ -63,6 +63,7 @@ class Batch:
         self.cu_cpu = torch.tensor([0] + torch.tensor(new).cumsum(0).tolist(), dtype=torch.int32)
         self.cu, self.lens_t, self.table = self.cu_cpu.to(DEV), ints(self.lens), table.to(DEV)
         self.max_new, self.max_len = max(max(new), 1), max(max(self.lens), 1)
+        self.wide = self.widened(self.max_new, self.max_len)
         self.put()
 
     def put(self):
@@ -74,11 +75,17 @@ class Batch:
                                         k_scales=self.ks, v_scales=self.vs, sm_scale=self.sm_scale)
 
     def kernel(self, n):
-        return "general" if self.flags or self.q_t == torch.float32 else "few" if n * (self.hq // self.hkv) <= 16 else "chunk"
+        return "general" if self.flags or self.q_t == torch.float32 else "few" if n * (self.hq // self.hkv) <= 16 else "wide" if self.wide else "chunk"
+
+    def widened(self, max_new, max_len, first_key=None):
+        """Whether keys and values are widened to bf16: where they take no more memory so than the queries in two parts of 8 bits."""
+        pages = len(self.new) * -(-max_len // 128)
+        return first_key is None and 2 * pages * self.hkv * 128 * self.d * 2 + 4 * pages <= self.rows * self.hq * (2 * self.d + 1)
 
     def attend(self, q=None, **kw):
         put = {x: kw.pop(x).to(DEV) for x in ("slopes", "first_key", "prefix_lens") if kw.get(x) is not None}
         max_new, max_len = kw.pop("max_new", self.max_new), kw.pop("max_len", self.max_len)
+        self.wide = self.widened(max_new, max_len, kw.get("first_key"))
         return self.cache.attend(self.qd if q is None else q, self.cu, self.lens_t, self.table, max_new, max_len, **put, **kw)
 
     def check(self, out, lse, seqs=None, none=False, kernel=None, **kw):
@@ -130,6 +137,32 @@ def test_masks(q, flags, mask, few, d):
              "documents": dict(first_key=first), "prefix": dict(prefix_lens=torch.tensor([0, 340, 5, 10000, 100], dtype=torch.int32)),
              "all": dict(softcap=8.0, slopes=slopes, window=90, first_key=first, prefix_lens=prefix),
              "all-sinks": dict(softcap=8.0, slopes=slopes, window=90, sinks=5, prefix_lens=prefix)}[mask])
+
+
+@pytest.mark.parametrize("mask", ["none", "cap", "slopes", "window", "window-1", "window-sinks", "sinks-far", "prefix", "all"])
+@pytest.mark.parametrize("d,P", [(128, 64), (64, 16), (128, 16), (64, 128)])
+@pytest.mark.parametrize("new,old", [([300, 7, 1, 150], [0, 30, 90, 0]), ([129], [0]), ([700, 690], [20, 0])], ids=["ragged", "one", "two"])
+def test_prompts(mask, d, P, new, old):
+    """Many rows for each key: keys and values are widened before.  Pages that no row's window reaches have no number."""
+    b = Batch(new, old, hq=8, hkv=1, d=d, P=P, extra_cols=2, extra_rows=1)
+    kw = {"none": {}, "cap": dict(softcap=5.0), "slopes": dict(slopes=torch.tensor([0.5, 0.0, 0.01, 2.0, 0.25, 0.125, 0.0, 1.0])), "window": dict(window=37), "window-1": dict(window=1),
+          "window-sinks": dict(window=37, sinks=4), "sinks-far": dict(window=20, sinks=141), "prefix": dict(prefix_lens=torch.tensor([0, 20, 10000, 100][:len(new)], dtype=torch.int32)),
+          "all": dict(softcap=8.0, slopes=torch.tensor([0.25, 0.125, 0.0, 1.0] * 2), window=90, sinks=5, prefix_lens=torch.tensor([290, 5, 0, 60][:len(new)], dtype=torch.int32))}[mask]
+    b.run(**kw)
+    assert b.wide
+
+
+@pytest.mark.parametrize("sinks", [0, 100, 129])
+def test_prompts_whose_first_pages_are_gone(sinks):
+    """Pages before the window may have no number, or any, as long as no tile of 128 tokens that a row sees is in them."""
+    b = Batch([300, 280], [700, 40], hq=8, hkv=1, d=64, P=32)
+    b.table_cpu[0, -(-sinks // 128) * 4:16] = torch.tensor([-1, 1 << 30] * 8, dtype=torch.int32)[:16 - -(-sinks // 128) * 4]   # (token 700 sees from 601 on, tile 4)
+    kept = b.table.clone()
+    b.table = b.table_cpu.to(DEV)
+    out, lse = b.attend(window=100, sinks=sinks)
+    assert b.wide and b.cache.sync_status() == 0
+    b.table_cpu = kept.cpu()
+    b.check(out, lse, window=100, sinks=sinks)
 
 
 @kinds
@@ -354,7 +387,10 @@ def test_two_threads():
 
 @kinds
 def test_many_sequences(q, flags):
-    """More sequences than a launch's table holds; chunks among them."""
+    """More sequences than a launch's table holds; chunks among them; prompts only."""
+    b = Batch(torch.randint(20, 60, (400,), generator=torch.Generator().manual_seed(4)).tolist(), [0] * 400, hq=8, hkv=1, d=64, P=16, q=q, flags=flags)
+    b.run()
+    assert b.wide
     n = 900
     g = torch.Generator().manual_seed(3)
     new = torch.randint(0, 3, (n,), generator=g).tolist()
