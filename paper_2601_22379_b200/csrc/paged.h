@@ -492,8 +492,7 @@ struct PagedWide {
   bool fits;                            // (rows that a TMA coordinate can name)
 };
 PagedWide paged_wide(const PagedLayout& pl, const PagedBatch& pb);
-cudaError_t launch_paged_widen(const PagedBatch& pb, const PagedLayout& pl, const PagedPages& pages, const PagedWide& w, int from_new, int window, int sinks, void* to,
-                               cudaStream_t s);
+cudaError_t launch_paged_widen(const PagedBatch& pb, const PagedLayout& pl, const PagedPages& pages, const PagedWide& w, int window, int sinks, void* to, cudaStream_t s);
 // paged_mma.cu: bf16 on tcgen05
 size_t paged_mma_drain_bytes(const PagedWork& w, const PagedBatch& pb, const PagedLayout& pl);
 int paged_mma_positions(const PagedBatch& pb, const PagedLayout& pl);   // new tokens of a row tile: the query boxes' size

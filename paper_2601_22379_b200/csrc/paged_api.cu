@@ -293,19 +293,34 @@ extern "C" int spla_paged_read(spla_paged_t* p, const spla_paged_batch_t* batch,
 // Which kernel a launch is: fp32 arithmetic, bf16 on the tensor cores, 8-bit pages with few rows, 8-bit pages on the tensor cores, the same widened to bf16 before.
 enum PagedKernel { kGeneral, kTensor, kFew, kTensorBytes, kTensorWide };
 
+// 8-bit pages, sequences of more rows than few: where there are half as many rows as keys (of sequences as long as max_len) and more, the keys and values
+// are widened to bf16 in a pass of their own, once for all rows, and the kernel for bf16 pages does the rest.
+// (Graphs, us, this way and over the 8-bit pages: a prompt of 8192 tokens 557 and 717, of 1000 43 and 55, of 64 31 and 41; ragged ones of up to 2000 x16 330 and 447; 4000 on
+// 4000 with a window of 512 127 and 168; 512 on 3500 x4, near the bound, 195 and 215.  A key costs about 0.14 ns / head to widen and 256 rows gain 0.04.)
+// The measure is the workspace: up to four times the queries' parts.  (Documents: which keys are looked at is not known before; they go without.)
+constexpr size_t kWideMost = 4;
+// Bytes of the workspace's front, the same for all launches of a call: the queries' parts, or the widened tokens.
+static size_t front_bytes(const spla_paged* p, const PagedBatch& pb) {
+  if (!p->few || pb.max_new <= paged_few_positions(p->pl)) return 0;
+  size_t exps;
+  const size_t parts = paged_split_bytes(p->pl, pb.total_new, &exps);
+  const PagedWide w = paged_wide(p->pl, pb);
+  return w.fits && w.bytes > parts && w.bytes <= kWideMost * parts ? w.bytes : parts;
+}
+
 // The plan of one launch (a batch of at most kPagedMaxBatch sequences), the bytes of its partial results and of the sums of long walks,
 // and their places in the workspace, where there is one (no cuts: whole units only).
 // (8-bit pages: where a sequence may have more rows than the kernel for few takes, the queries' parts lie in front, the same for all launches of a call; or in
 // their place, where they take no more than that, the widened tokens.)
-static size_t plan_attend(const spla_paged* p, PagedBatch pb, PagedKernel kernel, PagedWork* w, void* workspace) {
+static size_t plan_attend(const spla_paged* p, PagedBatch pb, PagedKernel kernel, size_t front, PagedWork* w, void* workspace) {
   const bool tensor = kernel == kTensor || kernel == kTensorBytes || kernel == kTensorWide;
   const bool parts = kernel != kGeneral && kernel != kTensor && pb.max_new > paged_few_positions(p->pl);
   if (kernel == kFew && pb.max_new > paged_few_positions(p->pl)) pb.max_new = paged_few_positions(p->pl);   // (the others are another launch's)
   if (tensor) paged_plan_mma(w, pb, p->pl, p->sm_count);
   else if (kernel == kFew) paged_plan_few(w, pb, p->pl, p->sm_count);
   else paged_plan_general(w, pb, p->pl, p->sm_count);
-  size_t used = 0, exps;
-  if (parts) used = align_up(paged_split_bytes(p->pl, pb.total_new, &exps), 256);
+  size_t used = 0;
+  if (parts) used = align_up(front, 256);
   auto take = [&](size_t bytes) {
     char* at = workspace ? reinterpret_cast<char*>(workspace) + used : nullptr;
     used += align_up(bytes, 256);
@@ -348,6 +363,7 @@ extern "C" int spla_paged_query_workspace(const spla_paged_t* p, const spla_page
   if (rc != SPLA_OK) return rc;
   if (!bytes_out) return SPLA_ERR_INVALID_ARG;
   const PagedBatch pb = device_batch(batch);
+  const size_t front = front_bytes(p, pb);
   size_t most = 0;
   for (int first = 0; first < batch->batch; first += kPagedMaxBatch) {
     PagedBatch part = pb;
@@ -355,7 +371,7 @@ extern "C" int spla_paged_query_workspace(const spla_paged_t* p, const spla_page
     for (PagedKernel kernel : {kGeneral, kTensor, kFew, kTensorBytes}) {   // (queries that TMA does not take go to the general kernel)
       if ((kernel == kTensor && !p->tensor) || ((kernel == kFew || kernel == kTensorBytes) && !p->few)) continue;
       PagedWork w = {};
-      const size_t n = plan_attend(p, part, kernel, &w, nullptr);
+      const size_t n = plan_attend(p, part, kernel, front, &w, nullptr);
       if (n > most) most = n;
     }
   }
@@ -409,14 +425,12 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
   const bool rows16 = aligned(q, 16) && q_stride % 8 == 0, few = p->few && rows16;
   const bool parts = few && pb.max_new > paged_few_positions(p->pl);               // some sequences may have more rows: their queries in two parts
   const bool tensor_fits = (p->tensor || parts) && rows16 && cap_fits(p->cfg.sm_scale, mask->softcap);
-  // More rows than few: where there are many for each key, the keys and values are widened to bf16 in a pass of their own, once for all rows (a prompt of 8192
-  // @wide).  The measure is that they take no more of the workspace than the queries' parts, @wide2.  (Documents: which
-  // keys are looked at is not known before.)
   const PagedWide w = paged_wide(p->pl, pb);
+  const size_t front_size = front_bytes(p, pb);
   size_t exps = 0;
   char* front = reinterpret_cast<char*>(workspace);
   PagedMaps wide_maps;
-  const bool wide = tensor_fits && parts && !mask->first_key && w.fits && w.bytes <= paged_split_bytes(p->pl, pb.total_new, &exps) &&
+  const bool wide = tensor_fits && parts && !mask->first_key && w.fits && w.bytes <= kWideMost * paged_split_bytes(p->pl, pb.total_new, &exps) &&
                     make_kv_map(wide_maps.k, front, p->pl.d, kWidePage, (unsigned long long)w.pl.n_pages * w.pl.page_stride) &&
                     make_kv_map(wide_maps.v, front + w.v_at, p->pl.d, kWidePage, (unsigned long long)w.pl.n_pages * w.pl.page_stride) &&
                     make_q_map(wide_maps.q, q, p->pl, q_stride, pb);
@@ -430,7 +444,7 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
     a.from_new = from_new;
     a.to_new = to_new;
     a.w = PagedWork{};
-    plan_attend(p, a.pb, kernel, &a.w, workspace);
+    plan_attend(p, a.pb, kernel, front_size, &a.w, workspace);
     switch (kernel) {
       case kTensor: e = launch_paged_mma(a, maps, s); break;
       case kFew: e = launch_paged_few(a, maps, s); break;
@@ -448,7 +462,7 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
     if (e == cudaSuccess) e = launch_paged_join(a, q16, s);
   };
   if (wide) {
-    e = launch_paged_widen(pb, p->pl, p->pages, w, paged_few_positions(p->pl) + 1, a.window, a.sinks, front, s);
+    e = launch_paged_widen(pb, p->pl, p->pages, w, a.window, a.sinks, front, s);
   } else if (parts && tensor) {
     paged_split_bytes(p->pl, pb.total_new, &exps);
     unsigned char* at = reinterpret_cast<unsigned char*>(workspace);
@@ -458,10 +472,12 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
   for (int first = 0; first < batch->batch && e == cudaSuccess; first += kPagedMaxBatch) {
     a.pb = part_of(pb, first);
     a.prefix = mask->prefix_lens ? mask->prefix_lens + first : nullptr;
-    if (few) {                                                                     // two launches where a sequence may have more rows
+    if (wide) {                                                                    // (sequences of few rows too: one launch less)
+      launch(kTensorWide, 0, 0);
+    } else if (few) {                                                              // two launches where a sequence may have more rows
       const int most = paged_few_positions(p->pl);
       launch(kFew, 0, most);
-      if (parts) launch(wide ? kTensorWide : tensor ? kTensorBytes : kGeneral, most + 1, 0x7fffffff);
+      if (parts) launch(tensor ? kTensorBytes : kGeneral, most + 1, 0x7fffffff);
     } else {
       launch(tensor ? kTensor : kGeneral, 0, 0);
     }

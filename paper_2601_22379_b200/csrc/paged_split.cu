@@ -73,11 +73,11 @@ __global__ void __launch_bounds__(kSplitThreads) paged_split_kernel(const __nv_b
 }
 
 
-// Cached tokens as bf16 pages of 128 tokens, for sequences of from_new new tokens and more: page `col` of sequence b is number b cols + col.
+// Cached tokens of the sequences that have new ones, as bf16 pages of 128 tokens: page `col` of sequence b is number b cols + col.
 // Block (page, head).  Those that no row walks stay as they are (and their pages' numbers unread), as do the rows behind the end.
 template <int D>
 __global__ void __launch_bounds__(kSplitThreads) paged_widen_kernel(const __grid_constant__ PagedBatch pb, const __grid_constant__ PagedLayout pl,
-                                                                    const __grid_constant__ PagedPages pages, int cols, int from_new, int window, int sinks,
+                                                                    const __grid_constant__ PagedPages pages, int cols, int window, int sinks,
                                                                     __nv_bfloat16* k, __nv_bfloat16* v, int* table) {
   constexpr int PIECES = D / 16, EACH = kWidePage * PIECES / kSplitThreads;       // of a row; of a thread
   __shared__ long long rows[kWidePage / 16];
@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(kSplitThreads) paged_widen_kernel(const __grid
   const int tid = threadIdx.x, b = blockIdx.x / cols, col = blockIdx.x - b * cols, h = blockIdx.y, tok0 = col * kWidePage;
   const PagedSeq s = paged_seq(pb, pl.status, b);
   if (tid == 0 && h == 0) table[blockIdx.x] = blockIdx.x;
-  if (s.n < from_new || tok0 >= s.L) return;
+  if (s.n == 0 || tok0 >= s.L) return;
   if (window > 0 && tok0 >= sinks && tok0 + kWidePage <= s.L - s.n - window + 1) return;
   if (tid < kWidePage >> pl.log_p && tok0 + (tid << pl.log_p) < s.L) rows[tid] = paged_row(pb, pl, b, h, (tok0 >> pl.log_p) + tid);
   __syncthreads();
@@ -152,11 +152,11 @@ PagedWide paged_wide(const PagedLayout& pl, const PagedBatch& pb) {
   return w;
 }
 
-cudaError_t launch_paged_widen(const PagedBatch& pb, const PagedLayout& pl, const PagedPages& pages, const PagedWide& w, int from_new, int window, int sinks, void* to,
+cudaError_t launch_paged_widen(const PagedBatch& pb, const PagedLayout& pl, const PagedPages& pages, const PagedWide& w, int window, int sinks, void* to,
                                cudaStream_t s) {
   unsigned char* at = reinterpret_cast<unsigned char*>(to);
   return launch_ex(pl.d == 128 ? paged_widen_kernel<128> : paged_widen_kernel<64>, dim3((unsigned)w.pl.n_pages, (unsigned)pl.Hkv), dim3(kSplitThreads), 0, s, 0, true, pb, pl,
-                   pages, w.cols, from_new, window, sinks, (__nv_bfloat16*)at, (__nv_bfloat16*)(at + w.v_at), (int*)(at + w.table_at));
+                   pages, w.cols, window, sinks, (__nv_bfloat16*)at, (__nv_bfloat16*)(at + w.v_at), (int*)(at + w.table_at));
 }
 
 size_t paged_split_bytes(const PagedLayout& pl, int total_new, size_t* exps) {

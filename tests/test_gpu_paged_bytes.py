@@ -26,6 +26,12 @@ def on_device(pages, scales):
     return pages.to(DEV).view(torch.float8_e4m3fn), scales.to(DEV).view(torch.float8_e8m0fnu)
 
 
+def widened(batch, total, hq, hkv, d, max_new, max_len, first_key=None):
+    """Whether keys and values are widened to bf16: where they take at most four times the memory of the queries in two parts of 8 bits."""
+    pages = batch * -(-max_len // 128)
+    return max_new * (hq // hkv) > 16 and first_key is None and 2 * pages * hkv * 128 * d * 2 + 4 * pages <= 4 * total * hq * (2 * d + 1)
+
+
 class Batch:
     """Sequences with `new` tokens each on top of `old` ones, pages anywhere in the pool, blocks of different scales.  Memory that belongs to no sequence
     holds NaN, and the scales of such blocks 2^128."""
@@ -63,7 +69,7 @@ class Batch:
         self.cu_cpu = torch.tensor([0] + torch.tensor(new).cumsum(0).tolist(), dtype=torch.int32)
         self.cu, self.lens_t, self.table = self.cu_cpu.to(DEV), ints(self.lens), table.to(DEV)
         self.max_new, self.max_len = max(max(new), 1), max(max(self.lens), 1)
-        self.wide = self.widened(self.max_new, self.max_len)
+        self.wide = widened(B, self.rows, hq, hkv, d, self.max_new, self.max_len)
         self.put()
 
     def put(self):
@@ -75,17 +81,12 @@ class Batch:
                                         k_scales=self.ks, v_scales=self.vs, sm_scale=self.sm_scale)
 
     def kernel(self, n):
-        return "general" if self.flags or self.q_t == torch.float32 else "few" if n * (self.hq // self.hkv) <= 16 else "wide" if self.wide else "chunk"
-
-    def widened(self, max_new, max_len, first_key=None):
-        """Whether keys and values are widened to bf16: where they take no more memory so than the queries in two parts of 8 bits."""
-        pages = len(self.new) * -(-max_len // 128)
-        return first_key is None and 2 * pages * self.hkv * 128 * self.d * 2 + 4 * pages <= self.rows * self.hq * (2 * self.d + 1)
+        return "general" if self.flags or self.q_t == torch.float32 else "wide" if self.wide else "few" if n * (self.hq // self.hkv) <= 16 else "chunk"
 
     def attend(self, q=None, **kw):
         put = {x: kw.pop(x).to(DEV) for x in ("slopes", "first_key", "prefix_lens") if kw.get(x) is not None}
         max_new, max_len = kw.pop("max_new", self.max_new), kw.pop("max_len", self.max_len)
-        self.wide = self.widened(max_new, max_len, kw.get("first_key"))
+        self.wide = widened(len(self.new), self.rows, self.hq, self.hkv, self.d, max_new, max_len, kw.get("first_key"))
         return self.cache.attend(self.qd if q is None else q, self.cu, self.lens_t, self.table, max_new, max_len, **put, **kw)
 
     def check(self, out, lse, seqs=None, none=False, kernel=None, **kw):
@@ -711,7 +712,8 @@ def test_a_layer():
         out, lse = cache.attend(q, cu, ln, table.to(DEV), max(new), max(lens), window=64, sinks=3)
         assert cache.sync_status() == 0
         k, v = (ref8.values(t[x + "_pages"].view(torch.uint8).cpu(), t[x + "_scales"].view(torch.uint8).cpu()) for x in "kv")
-        o, l, ob, lb = ref8.attend(q.cpu(), k, v, cu.cpu(), lens, table, lambda n: "few" if n * 4 <= 16 else "chunk", 4, window=64, sinks=3)
+        wide = widened(3, total, hq, hkv, d, max(new), max(lens))
+        o, l, ob, lb = ref8.attend(q.cpu(), k, v, cu.cpu(), lens, table, lambda n: "wide" if wide else "few" if n * 4 <= 16 else "chunk", 4, window=64, sinks=3)
         ref8.check(lse, l, lb, what="lse")
         ref8.check(out, o, ob, torch.bfloat16, "out")
 
