@@ -342,7 +342,8 @@ int spla_rope_apply(const spla_rope_t *rope, const int32_t *positions, int32_t b
 
 /*
  * Norms of queries and keys, head by head, and their rotation in the same pass: y = R n, n_c = x_c r w_c, r = 1 / sqrt(mean_c x_c^2 + eps) over the
- * head's channels (all of them, whatever part is rotated), R the rotation of spla_rope_apply; fp32, rounded once.
+ * head's channels (all of them, whatever part is rotated), R the rotation of spla_rope_apply; fp32, rounded once (so r is 0 where the mean leaves fp32's range,
+ * from magnitudes of 10^19 on).
  */
 typedef struct {
   const float *q_weight, *k_weight;  /* DEVICE fp32 [head_dim]: w of queries and of keys, shared by their heads */
@@ -473,7 +474,8 @@ int spla_paged_query_workspace(const spla_paged_t *paged, const spla_paged_batch
  *   out:  DEVICE [total_new][H_q][d] q_dtype.  lse: DEVICE fp32 [total_new][H_q] or NULL: ln of the sum of exp(s).
  *   workspace: DEVICE, 256-byte aligned, as spla_paged_query_workspace says; NULL where that is 0.  Calls that may overlap need
  *         one each.
- * bf16 caches and queries run on the tensor cores (probabilities rounded to bf16, sums in fp32); the others, scales far
+ * bf16 caches and queries run on the tensor cores (probabilities rounded to bf16, sums in fp32), and so do 8-bit pages with bf16 queries (probabilities in fp16;
+ * in bf16 where there are many rows for each key, whose keys and values are then widened in the workspace); the others, scales far
  * above the cap (10^5 times and more), and SPLA_GENERAL_KERNELS, in fp32.  Results do not depend on max_new, max_len or the rows of other sequences beyond rounding.
  */
 int spla_paged_attend(spla_paged_t *paged, const spla_paged_batch_t *batch, const void *q, int64_t q_stride,
@@ -489,7 +491,7 @@ int spla_paged_attend_sinks(spla_paged_t *paged, const spla_paged_batch_t *batch
 /* As spla_sync_status, for the status word of `paged`. */
 int spla_paged_sync_status(spla_paged_t *paged, void *stream);
 
-/* As spla_debug_wait_hook, for the tensor-core kernel of spla_paged_attend. */
+/* As spla_debug_wait_hook, for the tensor-core kernels of spla_paged_attend. */
 int spla_paged_debug_wait_hook(spla_paged_t *paged, int32_t max_wait_polls, int32_t extra_expected_bytes);
 
 /* Static, NUL-terminated description of a status code. */

@@ -474,7 +474,7 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
     a.prefix = mask->prefix_lens ? mask->prefix_lens + first : nullptr;
     if (wide) {                                                                    // (sequences of few rows too: one launch less)
       launch(kTensorWide, 0, 0);
-    } else if (few) {                                                              // two launches where a sequence may have more rows
+    } else if (few) {                                                              // two launches where a sequence may have more rows (see paged_few_positions)
       const int most = paged_few_positions(p->pl);
       launch(kFew, 0, most);
       if (parts) launch(tensor ? kTensorBytes : kGeneral, most + 1, 0x7fffffff);

@@ -1,4 +1,4 @@
-// Attention of new tokens over a paged cache on the 5th-generation tensor cores: bf16 cache and queries.
+// Attention of new tokens over a paged cache on the 5th-generation tensor cores: bf16 queries, pages of bf16 or of 8 bits (BYTES).
 //
 //   S = Q K^T,  P = 2^(S scale log2 e - m),  O += P V,  l += sum P    over tiles of 128 keys; lse = ln 2 (m + log2 l), out = O / l
 //
@@ -30,6 +30,15 @@
 // Keys outside a row's mask: their scores are replaced before the maximum, whatever they are.  Values are looked over in tiles that
 // some row sees only in part: behind the sequence's end they are zeroed, and where one that is not finite is inside, the tile's product
 // with V is formed by the softmax warps, visible keys only (0 x infinity is no 0).
+//
+// 8-bit pages.  Scores are formed from the keys' bytes as they are (kind::f8f6f4), with the queries in two parts of 8 bits (paged_split.cu): eight products of 32 channels for the
+// eight of 16 that bf16 takes, and half the bytes.  Values are widened to fp16, in which e4m3 is exact, from a ring that TMA fills (a product takes both operands from one type's
+// family, and P needs more than 8 bits).  Scales touch neither: K's multiplies its 16 scores, V's is an exponent that is added to theirs, so that weights stay below 2^15 whatever the blocks'
+// scales are (kPmHead, kPmGrow), and l sums w 2^-ev.  P is fp16, half a step of 2^-11.  Warp 0 brings K, V, queries and scales, warp 2 (of FEW warps 12 to 15) widens V.
+// Of a prompt's 717 us the widening cost 51, the scales 36 and the queries' second part 37 (each taken out in turn; bf16 pages 543): calls of many rows for each key widen K and V before
+// instead (paged_api.cu).  Here remain chunks on a long cache (graphs, us, bf16 pages beside: 512 on 32768 x2 710 and 590, 33 on 32768 x8 358 and 285), documents, and 17 to 32
+// rows, which read half the bytes (8 on 32768 x8 170 and 195).  Not kept: K and V widened by four warps from registers (prompt 1014), queries split by the softmax warps (848),
+// a factor for every block instead of a pass over the scores (spills, 759), widening by four warps for all (733).
 //
 // Every wait is bounded; on expiry the CTA's roles leave their loops, copies and products in flight are waited for, tensor memory is
 // released and the time-out status latched.  No multicast.

@@ -1,8 +1,12 @@
-// Queries for the tensor-core attention over 8-bit pages: bf16 rows as two parts of 8 bits, whose products with e4m3 keys are the row's own.
+// What comes before the tensor-core attention over 8-bit pages: queries as two parts of 8 bits, or keys and values in bf16.
+//
+// Queries: bf16 rows as two parts of 8 bits, whose products with e4m3 keys are the row's own.
 //
 // A row is scaled by a power of two, so that its largest magnitude is in [128, 256); the first part is each channel rounded to e4m3, which takes the first four
 // of bf16's eight bits, the second what that leaves, as e5m2: three bits and a sign, all there is left down to 2^-14 of the row's largest channel,
-// within 2^-21 of it below.  Bound by memory: 4 bytes in and out per channel (a prompt of 8192 tokens, 32 heads of 128: @split).
+// within 2^-21 of it below.  Bound by memory: 4 bytes in and out per channel (8192 tokens, 32 heads of 128: 134 MB).
+// Keys and values: e4m3 times a power of two is exact in bf16.  Three bytes a value, 0.14 ns for a token and KV head of 128.  Where a call has many rows for each key this is little
+// beside what the kernel for bf16 pages does faster: no widening on the way, no scales in the softmax, one product of queries and keys for two.
 #include <cuda_fp8.h>
 
 #include "paged_tiles.cuh"

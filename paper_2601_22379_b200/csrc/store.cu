@@ -9,7 +9,11 @@
 // head (or a single new token of several heads), holds it in registers, norms and turns it, finds the largest magnitude by shuffles and
 // stores.  Queries go the same way without the scale.  New values are read once, written once; a block's earlier tokens are touched only when
 // its scale grows.
-// @figures
+//
+// What bounds it: the first loads of a CTA come behind a search for its sequences and the page table's entries, which are dependent loads; then memory.  A prompt of 32768 tokens of 32 + 8 + 8
+// heads of 128 in bf16: 166 us in a graph (112 at a copy's rate), 16384 in fp32, pages of 16: 43 (27), turns of 50 to 700 tokens x 16 74 (23), a token for each of 64
+// sequences 14 (launch 8).  Steps: a body for each kind of head, so that rows without norm or turn skip them, and packed arithmetic 242 -> 164 us (prompt).
+// Reading back: 131072 tokens, 8 heads of 128: 154 us (123), in pages of 16 54 (30).
 #include <type_traits>
 
 #include "rope_device.cuh"
