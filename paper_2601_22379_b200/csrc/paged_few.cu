@@ -650,7 +650,7 @@ cudaError_t few_dim(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s)
 
 }  // namespace
 
-// (32768 x8, 32 heads in 8 groups of 128, graphs: 16 rows take 123 us here, and the 20 to 32 of the tensor-core kernel 170, which would take fewer no less.)
+// (32768 x8, 32 heads in 8 groups of 128, graphs: 16 rows take 123 us here, and the 20 to 32 of the tensor-core kernel 166, which would take fewer no less.)
 int paged_few_positions(const PagedLayout& pl) { return kPfRows / pl.G; }
 
 void paged_plan_few(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int sm_count) {

@@ -36,8 +36,8 @@
 // family, and P needs more than 8 bits).  Scales touch neither: K's multiplies its 16 scores, V's is an exponent that is added to theirs, so that weights stay below 2^15 whatever the blocks'
 // scales are (kPmHead, kPmGrow), and l sums w 2^-ev.  P is fp16, half a step of 2^-11.  Warp 0 brings K, V, queries and scales, warp 2 (of FEW warps 12 to 15) widens V.
 // Of a prompt's 717 us the widening cost 51, the scales 36 and the queries' second part 37 (each taken out in turn; bf16 pages 543): calls of many rows for each key widen K and V before
-// instead (paged_api.cu).  Here remain chunks on a long cache (graphs, us, bf16 pages beside: 512 on 32768 x2 710 and 590, 33 on 32768 x8 358 and 285), documents, and 17 to 32
-// rows, which read half the bytes (8 on 32768 x8 170 and 195).  Not kept: K and V widened by four warps from registers (prompt 1014), queries split by the softmax warps (848),
+// instead (paged_api.cu).  Here remain chunks on a long cache (graphs, us, bf16 pages beside: 512 on 32768 x2 678 and 576, 33 on 32768 x8 348 and 279), documents, and 17 to 32
+// rows, which read half the bytes (8 on 32768 x8 166 and 199).  Not kept: K and V widened by four warps from registers (prompt 1014), queries split by the softmax warps (848),
 // a factor for every block instead of a pass over the scores (spills, 759), widening by four warps for all (733).
 //
 // Every wait is bounded; on expiry the CTA's roles leave their loops, copies and products in flight are waited for, tensor memory is
@@ -57,6 +57,7 @@ namespace {
 // (four warps more widen the values of 8-bit pages for launches of few rows, which are bound by that otherwise: 8 new tokens on 32768 x8 246 -> 168 us.
 // Elsewhere they would cost the softmax registers: prompt of 8192 721 -> 733.)
 template <bool FEW, bool BYTES> constexpr int kPmThreads = FEW && BYTES ? 512 : 384;
+enum { kPmPlain, kPmSinks, kPmMods };
 constexpr int kPmScales = 8;                       // tiles whose scales are kept: more than are between their copies and the softmax (NK + 2)
 constexpr int kPmKeys = 128;                       // keys per tile
 constexpr int kPmDrain = 128;                      // tiles that are added up in O before it is drained: 1024 truncations, each of less than 2^-23: 2^-13 at most
@@ -216,14 +217,16 @@ __device__ __forceinline__ float pm_undrain(uint32_t tO, float* drain, int slot,
   return fmaf(*place_l, f, l);
 }
 
+// MODE: plain scores, with sinks (without the code for them 512 on 32768 x2 is 2 % faster over bf16 pages and 6 % over 8-bit ones, 8 on 32768 x8 11 %), with cap, distances and sinks.
 // LONG: caches of more than kPmDrain tiles (the others go without what drains O: 106 us for a mixed batch in place of 108).
-template <int D, bool MODS, bool FEW, bool LONG, bool BYTES>
+template <int D, int MODE, bool FEW, bool LONG, bool BYTES>
 __global__ void __launch_bounds__(kPmThreads<FEW, BYTES>, 1)
     paged_mma_kernel(const PagedAttend a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                      const __grid_constant__ CUtensorMap map_q) {
   using SM = PmSmem<D, FEW, BYTES>;
   static_assert(!BYTES || SM::NK + 2 <= kPmScales, "scales of tiles on their way");
   constexpr int H = SM::H, NK = SM::NK, NV = SM::NV;
+  constexpr bool MODS = MODE == kPmMods, SINKS = MODE != kPmPlain;
   constexpr bool MORE = FEW && BYTES;                             // warps 12 to 15 widen values, otherwise warp 2
   constexpr int WIDENERS = MORE ? 4 : 1;
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -277,6 +280,8 @@ __global__ void __launch_bounds__(kPmThreads<FEW, BYTES>, 1)
   const int lim = a.wait_limit;
   const int ppos = a.w.ppos, G = a.pl.G;
   PmSeg* segs = reinterpret_cast<PmSeg*>(smem + SM::kSegs);
+  const int sinks = SINKS ? a.sinks : 0;
+  auto key_tile = [](int t, int ns, int skip) { return !SINKS || t < ns ? t : t + skip; };   // see PagedSpan
   // The CTA's segments, one after the other: the body returns false to give up.
   auto each_segment = [&](bool& ok, auto body) {
 #pragma unroll 1
@@ -361,7 +366,7 @@ __global__ void __launch_bounds__(kPmThreads<FEW, BYTES>, 1)
           if (lane == 0) copy_q(sg);
           ++seg;
           auto find = [&](int t0) {                               // cache row of this lane's block of the group from t0 on, -1: none
-            const int t = t0 + (lane >> 3), tok = (t < sg.ns ? t : t + sg.skip) * kPmKeys + 16 * i8;
+            const int t = t0 + (lane >> 3), tok = key_tile(t, sg.ns, sg.skip) * kPmKeys + 16 * i8;
             if (t >= E || tok >= sg.L) return -1;
             const long long r = paged_row(a.pb, a.pl, sg.b, sg.h, tok >> a.pl.log_p);
             return r < 0 ? -1 : (int)(r + (tok & (P - 1)));
@@ -421,7 +426,7 @@ __global__ void __launch_bounds__(kPmThreads<FEW, BYTES>, 1)
         const int L = sg.L, b = sg.b, h = sg.h, ns = sg.ns, skip = sg.skip;
         // row of this lane's box in tile t; loaded a tile ahead
         auto box_row = [&](int t) {
-          const int index = (t < ns ? t : t + skip) * npg + pg;
+          const int index = key_tile(t, ns, skip) * npg + pg;
           long long r = -1;
           if (lane < boxes && t < pl.E && index * P < L) r = paged_row(a.pb, a.pl, b, h, index);
           return r < 0 ? n_rows : (int)r;
@@ -628,7 +633,7 @@ __global__ void __launch_bounds__(kPmThreads<FEW, BYTES>, 1)
       int done_items = 0;
 #pragma unroll 1
       for (; t < t_end; t += t_step) {
-        const int tok0 = (t < sg.ns ? t : t + sg.skip) * kPmKeys, st = (uint32_t)(k_base + t) % NV;
+        const int tok0 = key_tile(t, sg.ns, sg.skip) * kPmKeys, st = (uint32_t)(k_base + t) % NV;
         const bool look = t < la || t >= le;
         bool simt = false;
         if (!pm_wait(&s_full[slot], n & 1, lim, abort_flag)) return false;
@@ -650,7 +655,7 @@ __global__ void __launch_bounds__(kPmThreads<FEW, BYTES>, 1)
           if (alike) {
             const int from = lo_most - tok0, to = hi_least - tok0;
             for (int j = thr >> 3; j < kPmKeys; j += 16)           // a row of 128 bytes by eight threads
-              if ((j < from && tok0 + j >= a.sinks) || j >= to) {
+              if ((j < from && tok0 + j >= sinks) || j >= to) {
 #pragma unroll
                 for (int x = 0; x < H; ++x) *reinterpret_cast<uint4*>(vt + x * SM::kHalf + j * 128 + (thr & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
               }
@@ -772,7 +777,8 @@ __global__ void __launch_bounds__(kPmThreads<FEW, BYTES>, 1)
 #pragma unroll
             for (int c = 0; c < KEYS / 32; ++c) {
               const int c0 = key0 + 32 * c;
-              const uint32_t bits = bits_between(see.lo - c0, see.hi - c0) | bits_between(-c0, min(a.sinks, see.hi) - c0);
+              uint32_t bits = bits_between(see.lo - c0, see.hi - c0);
+              if (tok0 < sinks) bits |= bits_between(-c0, min(sinks, see.hi) - c0);
 #pragma unroll
               for (int x = 0; x < 32; ++x)
                 if (!(bits & (1u << x))) r[32 * c + x] = 0xff800000u;
@@ -865,7 +871,8 @@ __global__ void __launch_bounds__(kPmThreads<FEW, BYTES>, 1)
               tmem_ld16_async(tS + 16 * w, pw);
               tmem_ld_wait16(pw);
               const int c0 = tok0 + 32 * w;
-              const uint32_t bits = valid ? bits_between(see.lo - c0, see.hi - c0) | bits_between(-c0, min(a.sinks, see.hi) - c0) : 0u;
+              uint32_t bits = valid ? bits_between(see.lo - c0, see.hi - c0) : 0u;
+              if (valid && tok0 < sinks) bits |= bits_between(-c0, min(sinks, see.hi) - c0);
 #pragma unroll
               for (int y = 0; y < 32; ++y) {
                 if (!(bits & (1u << y))) continue;
@@ -1100,9 +1107,9 @@ __global__ void __launch_bounds__(kPmThreads<FEW, BYTES>, 1)
   }
 }
 
-template <int D, bool MODS, bool FEW, bool LONG, bool BYTES>
+template <int D, int MODE, bool FEW, bool LONG, bool BYTES>
 cudaError_t mma_variant(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
-  auto kern = paged_mma_kernel<D, MODS, FEW, LONG, BYTES>;
+  auto kern = paged_mma_kernel<D, MODE, FEW, LONG, BYTES>;
   constexpr int bytes = PmSmem<D, FEW, BYTES>::kBytes;
   static unsigned long long allowed = 0;
   cudaError_t e = allow_smem_once(kern, bytes, allowed);
@@ -1110,15 +1117,16 @@ cudaError_t mma_variant(const PagedAttend& a, const PagedMaps& maps, cudaStream_
   return launch_ex(kern, dim3(a.w.n_cta), dim3(kPmThreads<FEW, BYTES>), bytes, s, 0, true, a, *reinterpret_cast<const CUtensorMap*>(maps.k),
                    *reinterpret_cast<const CUtensorMap*>(maps.v), *reinterpret_cast<const CUtensorMap*>(maps.q));
 }
-template <int D, bool MODS, bool FEW, bool BYTES>
+template <int D, int MODE, bool FEW, bool BYTES>
 cudaError_t mma_launch(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
-  return a.w.drain ? mma_variant<D, MODS, FEW, true, BYTES>(a, maps, s) : mma_variant<D, MODS, FEW, false, BYTES>(a, maps, s);
+  return a.w.drain ? mma_variant<D, MODE, FEW, true, BYTES>(a, maps, s) : mma_variant<D, MODE, FEW, false, BYTES>(a, maps, s);
 }
 template <int D, bool BYTES>
 cudaError_t mma_d(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
-  const bool mods = a.softcap > 0.f || a.slopes, few = a.w.ppos * a.pl.G <= 32;
-  if (few) return mods ? mma_launch<D, true, true, BYTES>(a, maps, s) : mma_launch<D, false, true, BYTES>(a, maps, s);
-  return mods ? mma_launch<D, true, false, BYTES>(a, maps, s) : mma_launch<D, false, false, BYTES>(a, maps, s);
+  const bool few = a.w.ppos * a.pl.G <= 32;
+  if (a.softcap > 0.f || a.slopes) return few ? mma_launch<D, kPmMods, true, BYTES>(a, maps, s) : mma_launch<D, kPmMods, false, BYTES>(a, maps, s);
+  if (a.sinks > 0) return few ? mma_launch<D, kPmSinks, true, BYTES>(a, maps, s) : mma_launch<D, kPmSinks, false, BYTES>(a, maps, s);
+  return few ? mma_launch<D, kPmPlain, true, BYTES>(a, maps, s) : mma_launch<D, kPmPlain, false, BYTES>(a, maps, s);
 }
 
 }  // namespace
