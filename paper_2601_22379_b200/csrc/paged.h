@@ -487,12 +487,12 @@ cudaError_t launch_paged_split(const PagedLayout& pl, const void* q, long long q
 constexpr int kWidePage = 128;
 struct PagedWide {
   PagedLayout pl;
-  int cols;                             // pages of a sequence
+  int cols, slots, first;               // tiles of a sequence, pages it has (fewer with a window), those of the sinks
   size_t v_at, table_at, bytes;
   bool fits;                            // (rows that a TMA coordinate can name)
 };
-PagedWide paged_wide(const PagedLayout& pl, const PagedBatch& pb);
-cudaError_t launch_paged_widen(const PagedBatch& pb, const PagedLayout& pl, const PagedPages& pages, const PagedWide& w, int window, int sinks, void* to, cudaStream_t s);
+PagedWide paged_wide(const PagedLayout& pl, const PagedBatch& pb, int window, int sinks);
+cudaError_t launch_paged_widen(const PagedBatch& pb, const PagedLayout& pl, const PagedPages& pages, const PagedWide& w, int window, void* to, cudaStream_t s);
 // paged_mma.cu: bf16 on tcgen05
 size_t paged_mma_drain_bytes(const PagedWork& w, const PagedBatch& pb, const PagedLayout& pl);
 int paged_mma_positions(const PagedBatch& pb, const PagedLayout& pl);   // new tokens of a row tile: the query boxes' size

@@ -293,19 +293,26 @@ extern "C" int spla_paged_read(spla_paged_t* p, const spla_paged_batch_t* batch,
 // Which kernel a launch is: fp32 arithmetic, bf16 on the tensor cores, 8-bit pages with few rows, 8-bit pages on the tensor cores, the same widened to bf16 before.
 enum PagedKernel { kGeneral, kTensor, kFew, kTensorBytes, kTensorWide };
 
-// 8-bit pages, sequences of more rows than few: where there are half as many rows as keys (of sequences as long as max_len) and more, the keys and values
-// are widened to bf16 in a pass of their own, once for all rows, and the kernel for bf16 pages does the rest.
-// (Graphs, us, this way and over the 8-bit pages: a prompt of 8192 tokens 557 and 717, of 1000 43 and 55, of 64 31 and 41; ragged ones of up to 2000 x16 330 and 447; 4000 on
-// 4000 with a window of 512 127 and 168; 512 on 3500 x4, near the bound, 195 and 215.  A key costs about 0.14 ns / head to widen and 256 rows gain 0.04.)
-// The measure is the workspace: up to four times the queries' parts.  (Documents: which keys are looked at is not known before; they go without.)
-constexpr size_t kWideMost = 4;
+// 8-bit pages, sequences of more rows than few: where there are enough rows for each key, the keys and values (with a window, its and the sinks') are widened to
+// bf16 in a pass of their own, once for all rows, and the kernel for bf16 pages does the rest.  Graphs, us, this way and over the 8-bit pages: a prompt of 8192 tokens 567 and
+// 690, of 1000 43 and 55, of 64 31 and 45; ragged ones of up to 2000 x16 320 and 438; 4000 on 4000 with a window of 512 125 and 164; 1 to 600 on 100 to 9000 x24 with a window of
+// 2048 184 and 221; 512 on 3500 x4 197 and 213, on 7000 x2 184 and 193.  A key costs about 0.14 ns / head to widen, 256 rows gain 0.04.
+// The measure is the workspace: up to four times the queries' parts, or eight where the sequences have 512 rows on average (200 on 2800 x8 176 and 180).
+// (Documents: which keys are looked at is not known before; they go without.)
+constexpr size_t kWideMost = 8;
+static bool wide_fits(const spla_paged* p, const PagedBatch& pb, const PagedWide& w) {
+  size_t exps;
+  const size_t parts = paged_split_bytes(p->pl, pb.total_new, &exps);
+  return w.fits && w.bytes <= ((long long)pb.total_new * p->pl.G >= 512ll * pb.batch ? kWideMost : kWideMost / 2) * parts;
+}
 // Bytes of the workspace's front, the same for all launches of a call: the queries' parts, or the widened tokens.
 static size_t front_bytes(const spla_paged* p, const PagedBatch& pb) {
   if (!p->few || pb.max_new <= paged_few_positions(p->pl)) return 0;
   size_t exps;
   const size_t parts = paged_split_bytes(p->pl, pb.total_new, &exps);
-  const PagedWide w = paged_wide(p->pl, pb);
-  return w.fits && w.bytes > parts && w.bytes <= kWideMost * parts ? w.bytes : parts;
+  const PagedWide w = paged_wide(p->pl, pb, 0, 0);                                 // (less with a window, which is not known here)
+  const size_t most = w.fits && w.bytes < kWideMost * parts ? w.bytes : kWideMost * parts;
+  return most > parts ? most : parts;
 }
 
 // The plan of one launch (a batch of at most kPagedMaxBatch sequences), the bytes of its partial results and of the sums of long walks,
@@ -425,12 +432,12 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
   const bool rows16 = aligned(q, 16) && q_stride % 8 == 0, few = p->few && rows16;
   const bool parts = few && pb.max_new > paged_few_positions(p->pl);               // some sequences may have more rows: their queries in two parts
   const bool tensor_fits = (p->tensor || parts) && rows16 && cap_fits(p->cfg.sm_scale, mask->softcap);
-  const PagedWide w = paged_wide(p->pl, pb);
+  const PagedWide w = paged_wide(p->pl, pb, a.window, a.sinks);
   const size_t front_size = front_bytes(p, pb);
   size_t exps = 0;
   char* front = reinterpret_cast<char*>(workspace);
   PagedMaps wide_maps;
-  const bool wide = tensor_fits && parts && !mask->first_key && w.fits && w.bytes <= kWideMost * paged_split_bytes(p->pl, pb.total_new, &exps) &&
+  const bool wide = tensor_fits && parts && !mask->first_key && wide_fits(p, pb, w) &&
                     make_kv_map(wide_maps.k, front, p->pl.d, kWidePage, (unsigned long long)w.pl.n_pages * w.pl.page_stride) &&
                     make_kv_map(wide_maps.v, front + w.v_at, p->pl.d, kWidePage, (unsigned long long)w.pl.n_pages * w.pl.page_stride) &&
                     make_q_map(wide_maps.q, q, p->pl, q_stride, pb);
@@ -462,7 +469,7 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
     if (e == cudaSuccess) e = launch_paged_join(a, q16, s);
   };
   if (wide) {
-    e = launch_paged_widen(pb, p->pl, p->pages, w, a.window, a.sinks, front, s);
+    e = launch_paged_widen(pb, p->pl, p->pages, w, a.window, front, s);
   } else if (parts && tensor) {
     paged_split_bytes(p->pl, pb.total_new, &exps);
     unsigned char* at = reinterpret_cast<unsigned char*>(workspace);

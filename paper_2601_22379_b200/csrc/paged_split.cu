@@ -77,21 +77,23 @@ __global__ void __launch_bounds__(kSplitThreads) paged_split_kernel(const __nv_b
 }
 
 
-// Cached tokens of the sequences that have new ones, as bf16 pages of 128 tokens: page `col` of sequence b is number b cols + col.
-// Block (page, head).  Those that no row walks stay as they are (and their pages' numbers unread), as do the rows behind the end.
+// Cached tokens of the sequences that have new ones, as bf16 pages of 128 tokens and their page table.  With a window: the tiles of the sinks (`first` of
+// them) and those from the first token's window on, which is all that any row walks.  Block (page, head).  The rows behind the end stay as they are.
 template <int D>
 __global__ void __launch_bounds__(kSplitThreads) paged_widen_kernel(const __grid_constant__ PagedBatch pb, const __grid_constant__ PagedLayout pl,
-                                                                    const __grid_constant__ PagedPages pages, int cols, int window, int sinks,
+                                                                    const __grid_constant__ PagedPages pages, int cols, int slots, int first, int window,
                                                                     __nv_bfloat16* k, __nv_bfloat16* v, int* table) {
   constexpr int PIECES = D / 16, EACH = kWidePage * PIECES / kSplitThreads;       // of a row; of a thread
   __shared__ long long rows[kWidePage / 16];
   pdl_wait();
   pdl_launch_dependents();
-  const int tid = threadIdx.x, b = blockIdx.x / cols, col = blockIdx.x - b * cols, h = blockIdx.y, tok0 = col * kWidePage;
+  const int tid = threadIdx.x, b = blockIdx.x / slots, slot = blockIdx.x - b * slots, h = blockIdx.y;
   const PagedSeq s = paged_seq(pb, pl.status, b);
-  if (tid == 0 && h == 0) table[blockIdx.x] = blockIdx.x;
-  if (s.n == 0 || tok0 >= s.L) return;
-  if (window > 0 && tok0 >= sinks && tok0 + kWidePage <= s.L - s.n - window + 1) return;
+  if (s.n == 0) return;
+  const int from = window > 0 ? max(0, s.L - s.n - window + 1) / kWidePage : 0;    // the first tile of a window
+  const int tile = slot < first ? slot : max(from, first) + slot - first, tok0 = tile * kWidePage;
+  if (tok0 >= s.L) return;
+  if (tid == 0 && h == 0) table[(long long)b * cols + tile] = blockIdx.x;
   if (tid < kWidePage >> pl.log_p && tok0 + (tid << pl.log_p) < s.L) rows[tid] = paged_row(pb, pl, b, h, (tok0 >> pl.log_p) + tid);
   __syncthreads();
   uint4 w[2][EACH];
@@ -137,10 +139,13 @@ __global__ void __launch_bounds__(kSplitThreads) paged_widen_kernel(const __grid
 
 }  // namespace
 
-PagedWide paged_wide(const PagedLayout& pl, const PagedBatch& pb) {
+PagedWide paged_wide(const PagedLayout& pl, const PagedBatch& pb, int window, int sinks) {
   PagedWide w = {};
   w.cols = (pb.max_len + kWidePage - 1) / kWidePage;
-  const long long pages = (long long)pb.batch * w.cols;
+  w.first = window > 0 ? (int)(((long long)sinks + kWidePage - 1) / kWidePage) : 0;
+  const long long reach = w.first + ((long long)pb.max_new + window - 1 + kWidePage - 1) / kWidePage + 1;   // tiles of the sinks, of the window of all new tokens
+  w.slots = window > 0 && reach < w.cols ? (int)reach : w.cols;
+  const long long pages = (long long)pb.batch * w.slots;
   const size_t tokens = (size_t)pages * pl.Hkv * kWidePage;
   w.pl = pl;
   w.pl.P = kWidePage;
@@ -151,16 +156,15 @@ PagedWide paged_wide(const PagedLayout& pl, const PagedBatch& pb) {
   w.pl.head_stride = kWidePage;
   w.v_at = tokens * pl.d * 2;
   w.table_at = 2 * w.v_at;
-  w.bytes = w.table_at + (size_t)pages * 4;
-  w.fits = tokens < (1ull << 31) - 256;
+  w.bytes = w.table_at + (size_t)pb.batch * w.cols * 4;
+  w.fits = (double)pages * pl.Hkv * kWidePage < 2147483392.0;                      // (2^31 - 256)
   return w;
 }
 
-cudaError_t launch_paged_widen(const PagedBatch& pb, const PagedLayout& pl, const PagedPages& pages, const PagedWide& w, int window, int sinks, void* to,
-                               cudaStream_t s) {
+cudaError_t launch_paged_widen(const PagedBatch& pb, const PagedLayout& pl, const PagedPages& pages, const PagedWide& w, int window, void* to, cudaStream_t s) {
   unsigned char* at = reinterpret_cast<unsigned char*>(to);
   return launch_ex(pl.d == 128 ? paged_widen_kernel<128> : paged_widen_kernel<64>, dim3((unsigned)w.pl.n_pages, (unsigned)pl.Hkv), dim3(kSplitThreads), 0, s, 0, true, pb, pl,
-                   pages, w.cols, window, sinks, (__nv_bfloat16*)at, (__nv_bfloat16*)(at + w.v_at), (int*)(at + w.table_at));
+                   pages, w.cols, w.slots, w.first, window, (__nv_bfloat16*)at, (__nv_bfloat16*)(at + w.v_at), (int*)(at + w.table_at));
 }
 
 size_t paged_split_bytes(const PagedLayout& pl, int total_new, size_t* exps) {

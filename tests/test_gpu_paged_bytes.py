@@ -26,10 +26,13 @@ def on_device(pages, scales):
     return pages.to(DEV).view(torch.float8_e4m3fn), scales.to(DEV).view(torch.float8_e8m0fnu)
 
 
-def widened(batch, total, hq, hkv, d, max_new, max_len, first_key=None):
-    """Whether keys and values are widened to bf16: where they take at most four times the memory of the queries in two parts of 8 bits."""
-    pages = batch * -(-max_len // 128)
-    return max_new * (hq // hkv) > 16 and first_key is None and 2 * pages * hkv * 128 * d * 2 + 4 * pages <= 4 * total * hq * (2 * d + 1)
+def widened(batch, total, hq, hkv, d, max_new, max_len, first_key=None, window=0, sinks=0):
+    """Whether keys and values are widened to bf16: where they take at most four times the memory of the queries in two parts of 8 bits, or eight where there are
+    512 rows a sequence; with a window its tiles only."""
+    max_new, cols = min(max_new, total), -(-max_len // 128)
+    slots = min(cols, -(-sinks // 128) + -(-(max_new + window - 1) // 128) + 1) if window else cols
+    most = 8 if total * (hq // hkv) >= 512 * batch else 4
+    return max_new * (hq // hkv) > 16 and first_key is None and 2 * batch * slots * hkv * 128 * d * 2 + 4 * batch * cols <= most * total * hq * (2 * d + 1)
 
 
 class Batch:
@@ -86,7 +89,7 @@ class Batch:
     def attend(self, q=None, **kw):
         put = {x: kw.pop(x).to(DEV) for x in ("slopes", "first_key", "prefix_lens") if kw.get(x) is not None}
         max_new, max_len = kw.pop("max_new", self.max_new), kw.pop("max_len", self.max_len)
-        self.wide = widened(len(self.new), self.rows, self.hq, self.hkv, self.d, max_new, max_len, kw.get("first_key"))
+        self.wide = widened(len(self.new), self.rows, self.hq, self.hkv, self.d, max_new, max_len, kw.get("first_key"), kw.get("window", 0), kw.get("sinks", 0))
         return self.cache.attend(self.qd if q is None else q, self.cu, self.lens_t, self.table, max_new, max_len, **put, **kw)
 
     def check(self, out, lse, seqs=None, none=False, kernel=None, **kw):
@@ -142,7 +145,7 @@ def test_masks(q, flags, mask, few, d):
 
 @pytest.mark.parametrize("mask", ["none", "cap", "slopes", "window", "window-1", "window-sinks", "sinks-far", "prefix", "all"])
 @pytest.mark.parametrize("d,P", [(128, 64), (64, 16), (128, 16), (64, 128)])
-@pytest.mark.parametrize("new,old", [([300, 7, 1, 150], [0, 30, 90, 0]), ([129], [0]), ([700, 690], [20, 0])], ids=["ragged", "one", "two"])
+@pytest.mark.parametrize("new,old", [([300, 7, 1, 150], [0, 30, 90, 0]), ([129], [0]), ([700, 690], [20, 0]), ([4, 3, 1], [0, 9, 2])], ids=["ragged", "one", "two", "short"])
 def test_prompts(mask, d, P, new, old):
     """Many rows for each key: keys and values are widened before.  Pages that no row's window reaches have no number."""
     b = Batch(new, old, hq=8, hkv=1, d=d, P=P, extra_cols=2, extra_rows=1)
@@ -150,7 +153,42 @@ def test_prompts(mask, d, P, new, old):
           "window-sinks": dict(window=37, sinks=4), "sinks-far": dict(window=20, sinks=141), "prefix": dict(prefix_lens=torch.tensor([0, 20, 10000, 100][:len(new)], dtype=torch.int32)),
           "all": dict(softcap=8.0, slopes=torch.tensor([0.25, 0.125, 0.0, 1.0] * 2), window=90, sinks=5, prefix_lens=torch.tensor([290, 5, 0, 60][:len(new)], dtype=torch.int32))}[mask]
     b.run(**kw)
-    assert b.wide
+    assert b.wide == (sum(new) > 8)                                           # (eight tokens have too few rows)
+
+
+def test_prompts_in_graphs_and_streams():
+    """Captured calls hold their widened copies themselves: two graphs and an eager call on another stream at once, replayed with other tokens."""
+    b = [Batch([300, 20 + 100 * x], [40, 0], hq=8, hkv=1, d=64, P=32, seed=x) for x in range(2)]
+    want = [x.run() for x in b]
+    assert all(x.wide for x in b)
+    streams, graphs, outs = [torch.cuda.Stream() for _ in range(3)], [], []
+    for x, s in zip(b, streams):
+        with torch.cuda.stream(s):
+            x.attend()
+            s.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=s):
+                outs.append(x.attend())
+            graphs.append(g)
+    for _ in range(3):
+        for x, s, g in zip(b, streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        with torch.cuda.stream(streams[2]):
+            third = b[0].attend()
+        torch.cuda.synchronize()
+        for got, w in zip([*outs, third], [*want, want[0]]):
+            assert all(torch.equal(p, r) for p, r in zip(got, w))
+    for x in b:                                                               # other tokens in the same places
+        x.kd.view(torch.uint8).copy_(x.kd.view(torch.uint8).flip(-1))
+    for s, g in zip(streams, graphs):
+        with torch.cuda.stream(s):
+            g.replay()
+    torch.cuda.synchronize()
+    for x, got in zip(b, outs):
+        x.bytes["k"] = x.kd.view(torch.uint8).cpu()
+        x.check(*got)
+        assert x.cache.sync_status() == 0
 
 
 @pytest.mark.parametrize("sinks", [0, 100, 129])
@@ -712,7 +750,7 @@ def test_a_layer():
         out, lse = cache.attend(q, cu, ln, table.to(DEV), max(new), max(lens), window=64, sinks=3)
         assert cache.sync_status() == 0
         k, v = (ref8.values(t[x + "_pages"].view(torch.uint8).cpu(), t[x + "_scales"].view(torch.uint8).cpu()) for x in "kv")
-        wide = widened(3, total, hq, hkv, d, max(new), max(lens))
+        wide = widened(3, total, hq, hkv, d, max(new), max(lens), window=64, sinks=3)
         o, l, ob, lb = ref8.attend(q.cpu(), k, v, cu.cpu(), lens, table, lambda n: "wide" if wide else "few" if n * 4 <= 16 else "chunk", 4, window=64, sinks=3)
         ref8.check(lse, l, lb, what="lse")
         ref8.check(out, o, ob, torch.bfloat16, "out")
