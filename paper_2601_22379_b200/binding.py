@@ -432,6 +432,7 @@ class Rope:
             raise ValueError(f"rope: scaling must be one of {sorted(self.SCALING)}")
         self.lib = load()
         self.head_dim = head_dim
+        self._norm_bytes = (None, 0)
         cfg = SplaRopeConfig(head_dim, rot_dim, int(interleaved), self.SCALING[scaling], base, factor, original_len, ramp[0], ramp[1], amplitude)
         self.handle = C.c_void_p()
         _check(self.lib.spla_rope_create(C.byref(cfg), C.byref(self.handle)), "spla_rope_create")
@@ -522,17 +523,21 @@ class Rope:
             wk = _norm_weight(k_weight, self.head_dim, device)
         norm = _pack_norm(_norm_weight(q_weight, self.head_dim, device), wk, eps)
         if n and batch:
-            nbytes = C.c_size_t()
-            rc = _on(device.index, lambda *a: self.lib.spla_rope_norm_query_workspace(*a[:-1]), self.handle, batch, n, heads, C.byref(nbytes))
-            if rc != SPLA_OK:
-                raise SplaError(rc, "spla_rope_norm_query_workspace")
+            sizes, nbytes = self._norm_bytes                                 # (of the last call: a training loop asks for the same again and again)
+            if sizes != (batch, n, heads, device.index):
+                out = C.c_size_t()
+                rc = _on(device.index, lambda *a: self.lib.spla_rope_norm_query_workspace(*a[:-1]), self.handle, batch, n, heads, C.byref(out))
+                if rc != SPLA_OK:
+                    raise SplaError(rc, "spla_rope_norm_query_workspace")
+                nbytes = out.value
+                self._norm_bytes = (batch, n, heads, device.index), nbytes
             # the weights' gradients and the call's own scratch, from the stream's pool
             dq_weight = torch.empty(self.head_dim, dtype=torch.float32, device=device)
             if k is not None:
                 dk_weight = torch.empty(self.head_dim, dtype=torch.float32, device=device)
-            ws = torch.empty(nbytes.value, dtype=torch.uint8, device=device)
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
             rc = _on(device.index, self.lib.spla_rope_norm_backward, self.handle, positions.data_ptr(), batch, n, tq, xq, tk, xk, _TYPE_CODE[dtype], norm,
-                     dq_weight.data_ptr(), _ptr(dk_weight), ws.data_ptr(), nbytes.value)
+                     dq_weight.data_ptr(), _ptr(dk_weight), ws.data_ptr(), nbytes)
             if rc != SPLA_OK:
                 raise SplaError(rc, "spla_rope_norm_backward")
         else:
