@@ -11,10 +11,10 @@
 // rows meet in shared memory, and a second kernel adds the CTAs' sums in their order: no atomics, the same bits every time.
 // All arithmetic in fp32, one rounding at the end.
 //
-// What bounds it: memory, read and write once.  Forward, 4 x 8192 tokens of 32 + 8 heads of 128 in bf16: 135 us in a graph (102 at a copy's rate; issue slots 61 % busy), fp32 16 + 4 heads
+// What bounds it: memory, read and write once.  Forward, 4 x 8192 tokens of 32 + 8 heads of 128 in bf16: 125 us in a graph (102 at a copy's rate), fp32 16 + 4 heads
 // of 64 20.5 (12.8).  Gradients 200 us (153): two reads for a write, 128 registers, two CTAs an SM.  Few tokens: launches (eight tokens 8 us, what a graph of one
 // small kernel takes here; the second kernel of the gradients takes 7 by itself when it is cold).  Steps: groups known to the compiler, four CTAs an SM and one row a thread 158 -> 135 us (two rows under way and three
-// CTAs 156; five and six CTAs were slower too); gradients with tiles as large as the table allows and two values at a time 281 -> 197.
+// CTAs 156; five and six CTAs were slower too), the next row asked for as soon as this one's values are out of its registers 134 -> 125 (three CTAs 131, fp32 20.5 -> 24.6); gradients with tiles as large as the table allows and two values at a time 281 -> 197.
 #include <type_traits>
 
 #include "rope_device.cuh"
@@ -78,26 +78,22 @@ __global__ void __launch_bounds__(kNormThreads, BWD ? 2 : 4)
     const int* pos = r.positions + (long long)b * r.tokens + tok0;
     fill_turns<ROW>(rt, table, nt, tid, kNormThreads, BWD, [&](int t) { return __ldg(pos + t); });
   };
-  // Up to N rows of a thread on their way: row x0 + k by + ty of the group.  (Which group is known to the compiler: its strides are constants then.)
-  constexpr int N = 1;                                             // (two: 156 us in place of 135)
-  int tk[N];                                                       // token of the tile, -1: none
-  T* out[N];
-  uint32_t raw[N][WORDS] = {}, raw_g[N][BWD ? WORDS : 1] = {};
+  // A thread's row on its way: row x0 + ty of the group.  (Which group is known to the compiler: its strides are constants then.)
+  int tk;                                                          // its token of the tile, -1: none
+  T* out;
+  uint32_t raw[WORDS] = {}, raw_g[BWD ? WORDS : 1] = {};
   auto fetch = [&](auto group_c, int x0) {
     constexpr int GI = decltype(group_c)::value;
     const NormGroup& g = r.g[GI];
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const int x = x0 + k * by + ty;
-      tk[k] = -1;
-      if (x >= to[GI] || !row.here) continue;
-      const int t = g.n_heads == 1 ? x : (int)__umulhi((unsigned)x, r.head_magic[GI]), h = x - t * g.n_heads;
-      const long long tok = tok0 + t;
-      tk[k] = t;
-      out[k] = reinterpret_cast<T*>(g.out) + b * g.out_batch + tok * g.out_token + h * g.out_head;
-      row.load(reinterpret_cast<const T*>(g.x) + b * g.x_batch + tok * g.x_token + h * g.x_head, raw[k]);
-      if constexpr (BWD) row.load(reinterpret_cast<const T*>(g.dy) + b * g.dy_batch + tok * g.dy_token + h * g.dy_head, raw_g[k]);
-    }
+    const int x = x0 + ty;
+    tk = -1;
+    if (x >= to[GI] || !row.here) return;
+    const int t = g.n_heads == 1 ? x : (int)__umulhi((unsigned)x, r.head_magic[GI]), h = x - t * g.n_heads;
+    const long long tok = tok0 + t;
+    tk = t;
+    out = reinterpret_cast<T*>(g.out) + b * g.out_batch + tok * g.out_token + h * g.out_head;
+    row.load(reinterpret_cast<const T*>(g.x) + b * g.x_batch + tok * g.x_token + h * g.x_head, raw);
+    if constexpr (BWD) row.load(reinterpret_cast<const T*>(g.dy) + b * g.dy_batch + tok * g.dy_token + h * g.dy_head, raw_g);
   };
   auto fetch_first = [&]() {
     if (from[0] < to[0]) fetch(queries, from[0]); else fetch(keys, from[1]);
@@ -105,7 +101,7 @@ __global__ void __launch_bounds__(kNormThreads, BWD ? 2 : 4)
   // (what comes behind the rows from x0 on)
   auto fetch_next = [&](auto group_c, int x0) {
     constexpr int GI = decltype(group_c)::value;
-    if (GI == 0 && x0 + N * by >= to[0]) fetch(keys, from[1]); else fetch(group_c, x0 + N * by);
+    if (GI == 0 && x0 + by >= to[0]) fetch(keys, from[1]); else fetch(group_c, x0 + by);
   };
   float acc[2][BWD ? CH : 1];
 
@@ -119,21 +115,20 @@ __global__ void __launch_bounds__(kNormThreads, BWD ? 2 : 4)
     auto group = [&](auto group_c) {
       constexpr int GI = decltype(group_c)::value;
 #pragma unroll 1
-      for (int x0 = from[GI]; x0 < to[GI]; x0 += N * by) {         // (whole warps: a row's lanes meet in shuffles)
+      for (int x0 = from[GI]; x0 < to[GI]; x0 += by) {             // (whole warps: a row's lanes meet in shuffles)
+        float x[CH], w[CH];
+        const int t = tk;
+        T* const to_row = out;
+        row.values(raw, x);                                     // (of no row: whatever, and not stored)
+        fetch_next(group_c, x0);                                   // (its registers are free)
+        if (!loose && !row.here)                                   // (lanes beside a row's: nothing to its sum)
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-          float x[CH], w[CH];
-          row.values(raw[k], x);                                   // (of no row: whatever, and not stored)
-          if (!loose && !row.here)                                 // (lanes beside a row's: nothing to its sum)
-#pragma unroll
-            for (int i = 0; i < CH; ++i) x[i] = 0.f;
-          const float rms = row_rms(x, width, r.per_channel, r.eps);
-          row.weights(w_s[GI], w);
-          row_scale(x, rms, w);
-          row.turn(x, table + max(tk[k], 0) * pairs, own_row);
-          if (tk[k] >= 0) row.store(out[k], x);
-        }
-        fetch_next(group_c, x0);
+          for (int i = 0; i < CH; ++i) x[i] = 0.f;
+        const float rms = row_rms(x, width, r.per_channel, r.eps);
+        row.weights(w_s[GI], w);
+        row_scale(x, rms, w);
+        row.turn(x, table + max(t, 0) * pairs, own_row);
+        if (t >= 0) row.store(to_row, x);
       }
     };
     group(queries);
@@ -149,10 +144,10 @@ __global__ void __launch_bounds__(kNormThreads, BWD ? 2 : 4)
 #pragma unroll 1
       for (int x0 = from[GI]; x0 < to[GI]; x0 += by) {
         float x[CH], u[CH];
-        const int t = tk[0];
-        T* const to_row = out[0];
-        row.values(raw[0], x);
-        row.values(raw_g[0], u);
+        const int t = tk;
+        T* const to_row = out;
+        row.values(raw, x);
+        row.values(raw_g, u);
         fetch_next(group_c, x0);                                   // (its registers are free)
         if (t < 0) {
 #pragma unroll
