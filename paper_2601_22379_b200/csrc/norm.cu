@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(kNormThreads, BWD ? 2 : 4)
 }
 
 // Sums of `n` CTAs for 32 channels of one weight, in their order: every warp a run of the CTAs, then the runs.
-constexpr int kNormSumWarps = 16;
+constexpr int kNormSumWarps = 32, kNormSumRows = 10;        // (two CTAs an SM: all rows of a warp under way at once)
 __global__ void __launch_bounds__(32 * kNormSumWarps) norm_sum_kernel(const float* part, int n, int dim, float* dq, float* dk) {
   __shared__ float runs[kNormSumWarps][32];
   pdl_wait();
@@ -218,8 +218,13 @@ __global__ void __launch_bounds__(32 * kNormSumWarps) norm_sum_kernel(const floa
   const int from = (int)((long long)n * warp / kNormSumWarps), to = (int)((long long)n * (warp + 1) / kNormSumWarps);
   float s = 0.f;
   if (c < dim)
-#pragma unroll 8
-    for (int x = from; x < to; ++x) s += part[((long long)x * 2 + g) * dim + c];
+    for (int x0 = from; x0 < to; x0 += kNormSumRows) {
+      float v[kNormSumRows];
+#pragma unroll
+      for (int x = 0; x < kNormSumRows; ++x) v[x] = x0 + x < to ? part[((long long)(x0 + x) * 2 + g) * dim + c] : 0.f;
+#pragma unroll
+      for (int x = 0; x < kNormSumRows; ++x) s += v[x];
+    }
   runs[warp][lane] = s;
   __syncthreads();
   if (warp == 0 && c < dim) {
