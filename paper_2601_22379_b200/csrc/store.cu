@@ -11,7 +11,7 @@
 // its scale grows.
 //
 // What bounds it: the first loads of a CTA come behind a search for its sequences and the page table's entries, which are dependent loads; then memory.  A prompt of 32768 tokens of 32 + 8 + 8
-// heads of 128 in bf16: 166 us in a graph (112 at a copy's rate), 16384 in fp32, pages of 16: 43 (27), turns of 50 to 700 tokens x 16 74 (23), a token for each of 64
+// heads of 128 in bf16: 166 us in a graph (112 at a copy's rate), 16384 in fp32, pages of 16: 43 (27), turns of 50 to 700 tokens x 16 61 (23), a token for each of 64
 // sequences 14 (launch 8).  Steps: a body for each kind of head, so that rows without norm or turn skip them, and packed arithmetic 242 -> 164 us (prompt).
 // Reading back: 131072 tokens, 8 heads of 128: 154 us (123), in pages of 16 54 (30).
 #include <type_traits>
@@ -363,13 +363,14 @@ __global__ void __launch_bounds__(kStoreThreads) read_kernel(const __grid_consta
 template <typename T, class ROW, bool E8, int D>
 cudaError_t store_launch(StoreLaunch r, const RopeTable& rt, cudaStream_t s) {
   const int heads = r.n_q + 2 * r.n_kv, sm = device_sm_count();
-  // rows of a CTA: 16, fewer where SMs would idle, then the heads are shared out
+  // rows of a CTA: 16, fewer where SMs would idle; then, up to two rounds of CTAs, the heads are shared out to four (turns of 50 to 700 x 16 74 -> 61 us; from more
+  // rounds on the sines of a token, which every CTA forms again, cost more than they bring: 16384 tokens in fp32 43 -> 49)
   int tb = kStoreTokens;
   while (tb > 1 && (r.pb.total_new + tb - 1) / tb < 2 * sm) tb /= 2;
   const int blocks = (r.pb.total_new + tb - 1) / tb;
   int ys = 1;
-  if (blocks < 2 * sm) {
-    ys = (4 * sm + blocks - 1) / blocks;
+  if (blocks < 4 * sm) {
+    ys = (8 * sm + blocks - 1) / blocks;
     const int most = (heads + 7) / 8;                      // a head for every warp
     if (ys > most) ys = most;
   }
