@@ -460,7 +460,8 @@ typedef struct {
   const int32_t *prefix_lens;  /* DEVICE int32 [batch] or NULL: so many first tokens are visible from every position */
 } spla_paged_mask_t;
 
-/* Scratch that spla_paged_attend needs for these sizes (HOST; may be 0).  Only host values of `batch` are used. */
+/* Scratch that spla_paged_attend needs for these sizes (HOST; may be 0).  Only host values of `batch` are used.  (8-bit pages, bf16 queries, more than 16 rows of new
+ * tokens x G: besides the rest 2 to 17 bytes for each channel of the queries, or what keys and values of `batch` sequences of max_len tokens take in bf16, if that is less.) */
 int spla_paged_query_workspace(const spla_paged_t *paged, const spla_paged_batch_t *batch, size_t *bytes_out);
 
 /*
