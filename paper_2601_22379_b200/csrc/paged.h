@@ -476,10 +476,10 @@ cudaError_t launch_norm(const RopeTable& rt, const int* positions, int batch, in
 void paged_plan_general(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int sm_count);
 cudaError_t launch_paged_general(const PagedAttend& a, const PagedPages& pages, int q_bf16, cudaStream_t s);
 cudaError_t launch_paged_join(const PagedAttend& a, int out_bf16, cudaStream_t s);
-// paged_few.cu: 8-bit pages, bf16 queries, at most 16 rows per sequence and KV head
+// paged_few.cu: 8-bit pages, at most 16 rows per sequence and KV head
 int paged_few_positions(const PagedLayout& pl);   // new tokens of a sequence that it takes, at most
 void paged_plan_few(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, int sm_count);
-cudaError_t launch_paged_few(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s);
+cudaError_t launch_paged_few(const PagedAttend& a, const PagedMaps& maps, int f32, cudaStream_t s);   // f32: queries and outputs
 // paged_split.cu: bf16 queries as two parts of 8 bits, [token][head][part][d], and the exponents of the rows' scales [token][head]
 size_t paged_split_bytes(const PagedLayout& pl, int total_new, size_t* exps);
 cudaError_t launch_paged_split(const PagedLayout& pl, const void* q, long long q_stride, int total_new, unsigned char* parts, signed char* exps, cudaStream_t s);

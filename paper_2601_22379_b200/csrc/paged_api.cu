@@ -21,6 +21,7 @@ struct spla_paged {
   PagedMaps maps;
   bool tensor;                          // bf16 cache and queries, tensor maps made: the tensor-core kernel serves it
   bool few;                             // 8-bit pages and bf16 queries, maps made: paged_few.cu serves sequences of few rows, the tensor-core kernel the others
+  bool few32;                           // fp32 queries: paged_few.cu serves sequences of few rows, the fp32 kernel the others
   int sm_count;
   int wait_limit, dbg_tx_extra;
 };
@@ -200,8 +201,10 @@ static int create_paged(const spla_paged_config_t* c, void* k_pages, void* v_pag
   p->tensor = !k_scales && c->kv_dtype == SPLA_BF16 && c->q_dtype == SPLA_BF16 && !(c->flags & SPLA_GENERAL_KERNELS) && rows < (1ll << 31) - 256 &&
               make_kv_map(p->maps.k, k_pages, c->head_dim, P, rows) && make_kv_map(p->maps.v, v_pages, c->head_dim, P, rows);
   // (scales of 2^60 and more would leave the range that its exponents are kept in)
-  p->few = k_scales && c->q_dtype == SPLA_BF16 && !(c->flags & SPLA_GENERAL_KERNELS) && rows < (1ll << 31) - 256 && p->cfg.sm_scale < 1.15e18f &&
+  const bool bytes = k_scales && !(c->flags & SPLA_GENERAL_KERNELS) && rows < (1ll << 31) - 256 && p->cfg.sm_scale < 1.15e18f &&
            make_byte_map(p->maps.k, k_pages, c->head_dim, P, rows) && make_byte_map(p->maps.v, v_pages, c->head_dim, P, rows);
+  p->few = bytes && c->q_dtype == SPLA_BF16;
+  p->few32 = bytes && c->q_dtype == SPLA_F32;
   *paged_out = p;
   return SPLA_OK;
 }
@@ -376,7 +379,7 @@ extern "C" int spla_paged_query_workspace(const spla_paged_t* p, const spla_page
     PagedBatch part = pb;
     part.batch = pb.batch - first < kPagedMaxBatch ? pb.batch - first : kPagedMaxBatch;
     for (PagedKernel kernel : {kGeneral, kTensor, kFew, kTensorBytes}) {   // (queries that TMA does not take go to the general kernel)
-      if ((kernel == kTensor && !p->tensor) || ((kernel == kFew || kernel == kTensorBytes) && !p->few)) continue;
+      if ((kernel == kTensor && !p->tensor) || (kernel == kFew && !p->few && !p->few32) || (kernel == kTensorBytes && !p->few)) continue;
       PagedWork w = {};
       const size_t n = plan_attend(p, part, kernel, front, &w, nullptr);
       if (n > most) most = n;
@@ -429,7 +432,7 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
   cudaStream_t s = (cudaStream_t)stream;
   cudaError_t e = cudaSuccess;
   PagedMaps maps;
-  const bool rows16 = aligned(q, 16) && q_stride % 8 == 0, few = p->few && rows16;
+  const bool rows16 = aligned(q, 16) && q_stride % 8 == 0, few = p->few && rows16, few32 = p->few32 && aligned(q, 16) && q_stride % 4 == 0;
   const bool parts = few && pb.max_new > paged_few_positions(p->pl);               // some sequences may have more rows: their queries in two parts
   const bool tensor_fits = (p->tensor || parts) && rows16 && cap_fits(p->cfg.sm_scale, mask->softcap);
   const PagedWide w = paged_wide(p->pl, pb, a.window, a.sinks);
@@ -442,7 +445,7 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
                     make_kv_map(wide_maps.v, front + w.v_at, p->pl.d, kWidePage, (unsigned long long)w.pl.n_pages * w.pl.page_stride) &&
                     make_q_map(wide_maps.q, q, p->pl, q_stride, pb);
   const bool tensor = !wide && tensor_fits && make_q_map(maps.q, parts ? workspace : q, p->pl, parts ? q_row : q_stride, pb);
-  if (tensor || few) {
+  if (tensor || few || few32) {
     memcpy(maps.k, p->maps.k, sizeof(maps.k));
     memcpy(maps.v, p->maps.v, sizeof(maps.v));
   }
@@ -454,7 +457,7 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
     plan_attend(p, a.pb, kernel, front_size, &a.w, workspace);
     switch (kernel) {
       case kTensor: e = launch_paged_mma(a, maps, s); break;
-      case kFew: e = launch_paged_few(a, maps, s); break;
+      case kFew: e = launch_paged_few(a, maps, !q16, s); break;
       case kTensorWide: {
         PagedAttend b = a;
         b.pl = w.pl;
@@ -481,10 +484,10 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
     a.prefix = mask->prefix_lens ? mask->prefix_lens + first : nullptr;
     if (wide) {                                                                    // (sequences of few rows too: one launch less)
       launch(kTensorWide, 0, 0);
-    } else if (few) {                                                              // two launches where a sequence may have more rows (see paged_few_positions)
+    } else if (few || few32) {                                                           // two launches where a sequence may have more rows (see paged_few_positions)
       const int most = paged_few_positions(p->pl);
       launch(kFew, 0, most);
-      if (parts) launch(tensor ? kTensorBytes : kGeneral, most + 1, 0x7fffffff);
+      if (pb.max_new > most) launch(tensor ? kTensorBytes : kGeneral, most + 1, 0x7fffffff);
     } else {
       launch(tensor ? kTensor : kGeneral, 0, 0);
     }

@@ -75,6 +75,13 @@ __device__ __forceinline__ uint32_t nan8_to_zero(uint32_t w) {
 template <int D>
 __device__ __forceinline__ int piece_at(int row, int c) { return row * D + ((D == 128 ? c ^ (row & 7) : c ^ ((row >> 1) & 3)) << 4); }
 
+// Two fp32 values as fp16 and what that leaves, as fp16 again (of an infinity nothing).
+__device__ __forceinline__ void two_parts(float x, float y, uint32_t& first, uint32_t& rest) {
+  first = pack_f16(x, y);
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&first));
+  rest = pack_f16(fabsf(x) < INFINITY ? x - f.x : 0.f, fabsf(y) < INFINITY ? y - f.y : 0.f);
+}
+
 // 8 x 8 values of 16 bits, two neighbours of a row in each lane: its transpose.
 __device__ __forceinline__ uint32_t transposed(uint32_t v) {
   uint32_t y;
@@ -84,7 +91,8 @@ __device__ __forceinline__ uint32_t transposed(uint32_t v) {
 
 // R8: at most 8 rows.  Tokens and channels are the products' 16 rows then, the queries their 8 columns: half the products and half the registers, so
 // that sixteen warps work, eight on a tile and eight on the next.
-template <int D, bool MODS, bool R8>
+// F32: fp32 queries and outputs.  Queries and weights are two parts of fp16, 22 bits, each times the same fragments: 2^-24 of a row's largest channel, of its largest weight.
+template <int D, bool MODS, bool R8, bool F32>
 __global__ void __launch_bounds__(kPfThreads<R8>, 1)
     paged_few_kernel(const __grid_constant__ PagedAttend a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   using SM = PfSmem<D>;
@@ -164,9 +172,9 @@ __global__ void __launch_bounds__(kPfThreads<R8>, 1)
       if (!pm_wait(&seg_full[slot], (i / kPfSegs) & 1, lim, abort_flag)) { ok = false; break; }
       const PfSeg sg = segs[slot];
       if (sg.end) break;
-      if (lane == 0) mbar_expect_tx(&q_full[slot], sg.n * G * D * 2 + (uint32_t)a.dbg_tx_extra);
+      if (!F32 && lane == 0) mbar_expect_tx(&q_full[slot], sg.n * G * D * 2 + (uint32_t)a.dbg_tx_extra);
       __syncwarp();
-      if (lane < sg.n)
+      if (!F32 && lane < sg.n)                       // (fp32 queries: straight from memory, there is no place for them)
         bulk_g2s(smem + SM::kQ + (slot * kPfRows + lane * G) * D * 2,
                  reinterpret_cast<const __nv_bfloat16*>(a.q) + (sg.row0 + lane) * a.q_stride + (long long)sg.h * G * D, G * D * 2, &q_full[slot]);
 #pragma unroll 1
@@ -193,7 +201,7 @@ __global__ void __launch_bounds__(kPfThreads<R8>, 1)
     if (!ok) *abort_flag = 1;
     // every copy has landed before the CTA leaves, whatever the other roles do
     for (int x = max(0, kt - NS); x < kt; ++x) warp_waits(&full[x % NS], (x / NS) & 1, lim);
-    for (int x = max(0, i - kPfSegs); x < i; ++x) warp_waits(&q_full[x % kPfSegs], (x / kPfSegs) & 1, lim);
+    for (int x = max(0, i - kPfSegs); x < i && !F32; ++x) warp_waits(&q_full[x % kPfSegs], (x / kPfSegs) & 1, lim);
   } else if (warp == WARPS + 2) {
     // -------------------------------------------------------------- where tiles lie, and their scales: eight tiles at a time --------
     // (a byte of a scale comes from memory like anything else, behind the page's number: a microsecond, which one tile would not hide)
@@ -284,12 +292,34 @@ __global__ void __launch_bounds__(kPfThreads<R8>, 1)
       hi_least = __reduce_min_sync(0xffffffffu, hi_least);
       hi_most = __reduce_max_sync(0xffffffffu, hi_most);
       // queries as fragments: k-step j takes bytes 4 j .. of the lane's 32 (16) channels; rows g (and g + 8)
-      uint32_t qf[D / 16][R8 ? 2 : 4];
+      uint32_t qf[D / 16][R8 ? 2 : 4], ql[F32 ? D / 16 : 1][4];
       int qe[2];
-      if (!pm_wait(&q_full[slot], (i / kPfSegs) & 1, lim, abort_flag)) { ok = false; break; }
+      if (!F32 && !pm_wait(&q_full[slot], (i / kPfSegs) & 1, lim, abort_flag)) { ok = false; break; }
 #pragma unroll
       for (int x = 0; x < (R8 ? 1 : 2); ++x) {
         const int r = g + 8 * x;
+        if constexpr (F32) {
+          float w[D / 4];
+          const float4* from = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.q) + (sg.row0 + r / G) * a.q_stride + ((long long)sg.h * G + r % G) * D + t4 * (D / 4));
+#pragma unroll
+          for (int y = 0; y < D / 16; ++y) {
+            const float4 v = r < rows ? from[y] : make_float4(0.f, 0.f, 0.f, 0.f);
+            w[4 * y] = v.x; w[4 * y + 1] = v.y; w[4 * y + 2] = v.z; w[4 * y + 3] = v.w;
+          }
+          float top = 0.f;
+#pragma unroll
+          for (int y = 0; y < D / 4; ++y)
+            if (fabsf(w[y]) < INFINITY) top = fmaxf(top, fabsf(w[y]));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          qe[x] = top > 0.f ? max((__float_as_int(top) >> 23) - 127 - 14, -100) : 0;
+          const float mul = power_of_two(-qe[x]);
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) two_parts(w[4 * j + 2 * y] * mul, w[4 * j + 2 * y + 1] * mul, qf[j][2 * y + x], ql[j][2 * y + x]);
+          continue;
+        }
         uint32_t w[D / 8];
         if (r < rows) {
           const uint4* from = reinterpret_cast<const uint4*>(smem + SM::kQ + (slot * kPfRows + r) * D * 2 + t4 * (D / 2));
@@ -364,6 +394,10 @@ __global__ void __launch_bounds__(kPfThreads<R8>, 1)
               } else {
                 mma_f16(s[0][j & 1], qf[j], b[0][0], b[0][1]);
                 mma_f16(s[1][j & 1], qf[j], b[1][0], b[1][1]);
+                if constexpr (F32) {
+                  mma_f16(s[0][j & 1], ql[j], b[0][0], b[0][1]);
+                  mma_f16(s[1][j & 1], ql[j], b[1][0], b[1][1]);
+                }
               }
             }
 #pragma unroll
@@ -468,10 +502,15 @@ __global__ void __launch_bounds__(kPfThreads<R8>, 1)
             }
             l[x] = fmaf(l[x], f[x], sum * power_of_two(-ev));
           }
-          uint32_t pf[R8 ? 2 : 4];
+          uint32_t pf[R8 ? 2 : 4], pl[4];
           if constexpr (R8) {
             pf[0] = transposed(pack_f16(p[0][0], p[1][0]));
             pf[1] = transposed(pack_f16(p[0][1], p[1][1]));
+          } else if constexpr (F32) {
+            two_parts(p[0][0], p[0][1], pf[0], pl[0]);
+            two_parts(p[1][0], p[1][1], pf[1], pl[1]);
+            two_parts(p[0][2], p[0][3], pf[2], pl[2]);
+            two_parts(p[1][2], p[1][3], pf[3], pl[3]);
           } else {
             pf[0] = pack_f16(p[0][0], p[0][1]);
             pf[1] = pack_f16(p[1][0], p[1][1]);
@@ -524,6 +563,7 @@ __global__ void __launch_bounds__(kPfThreads<R8>, 1)
               for (int x = 0; x < 4; ++x) {
                 float c[4] = {0.f, 0.f, 0.f, 0.f};
                 mma_f16(c, pf, b[0][x], b[1][x]);
+                if constexpr (F32) mma_f16(c, pl, b[0][x], b[1][x]);
                 add(o[4 * y + x], c);
               }
             }
@@ -611,8 +651,11 @@ __global__ void __launch_bounds__(kPfThreads<R8>, 1)
         const long long out_row = (long long)(sg.row0 + pi) * a.pl.Hq + sg.h * G + r - pi * G;
         if (whole) {
           const float inv = sum == 0.f ? 0.f : 1.f / sum;
-          *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.out) + out_row * D + 4 * q4) =
-              make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
+          if constexpr (F32)
+            *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + out_row * D + 4 * q4) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+          else
+            *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.out) + out_row * D + 4 * q4) =
+                make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
           if (q4 == 0 && a.lse) a.lse[out_row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
         } else {
           *reinterpret_cast<float4*>(a.w.part_o + (part0 + r) * D + 4 * q4) = v;
@@ -632,9 +675,9 @@ __global__ void __launch_bounds__(kPfThreads<R8>, 1)
   if (*abort_flag && tid == 0) atomicExch(a.pl.status, kStatusTimeout);
 }
 
-template <int D, bool MODS, bool R8>
+template <int D, bool MODS, bool R8, bool F32>
 cudaError_t few_launch(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
-  auto kern = paged_few_kernel<D, MODS, R8>;
+  auto kern = paged_few_kernel<D, MODS, R8, F32>;
   static unsigned long long allowed = 0;
   cudaError_t e = allow_smem_once(kern, PfSmem<D>::kBytes, allowed);
   if (e != cudaSuccess) return e;
@@ -642,10 +685,11 @@ cudaError_t few_launch(const PagedAttend& a, const PagedMaps& maps, cudaStream_t
                    *reinterpret_cast<const CUtensorMap*>(maps.v));
 }
 template <int D>
-cudaError_t few_dim(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
+cudaError_t few_dim(const PagedAttend& a, const PagedMaps& maps, int f32, cudaStream_t s) {
   const bool mods = a.softcap > 0.f || a.slopes;
-  if (a.w.rows <= 8) return mods ? few_launch<D, true, true>(a, maps, s) : few_launch<D, false, true>(a, maps, s);
-  return mods ? few_launch<D, true, false>(a, maps, s) : few_launch<D, false, false>(a, maps, s);
+  if (f32) return mods ? few_launch<D, true, false, true>(a, maps, s) : few_launch<D, false, false, true>(a, maps, s);   // (two parts fill the registers of eight warps)
+  if (a.w.rows <= 8) return mods ? few_launch<D, true, true, false>(a, maps, s) : few_launch<D, false, true, false>(a, maps, s);
+  return mods ? few_launch<D, true, false, false>(a, maps, s) : few_launch<D, false, false, false>(a, maps, s);
 }
 
 }  // namespace
@@ -667,8 +711,8 @@ void paged_plan_few(PagedWork* w, const PagedBatch& pb, const PagedLayout& pl, i
   w->rows = (pb.max_new < w->upos ? pb.max_new : w->upos) * pl.G;
 }
 
-cudaError_t launch_paged_few(const PagedAttend& a, const PagedMaps& maps, cudaStream_t s) {
-  return a.pl.d == 128 ? few_dim<128>(a, maps, s) : few_dim<64>(a, maps, s);
+cudaError_t launch_paged_few(const PagedAttend& a, const PagedMaps& maps, int f32, cudaStream_t s) {
+  return a.pl.d == 128 ? few_dim<128>(a, maps, f32, s) : few_dim<64>(a, maps, f32, s);
 }
 
 }  // namespace spla

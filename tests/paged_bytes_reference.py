@@ -57,11 +57,13 @@ def store(pages, scales, x, new, old, table, P):
 
 
 def attend(q, k, v, cu, lens, table, kernel, exps, sm_scale=None, softcap=0.0, window=0, slopes=None, first_key=None, prefix=None, sinks=0, seqs=None):
-    """k, v: float64 pages (values).  kernel(n): "general", "few", "chunk" or "wide", what serves a sequence of n new tokens.  exps: largest exponent of a block of V
+    """k, v: float64 pages (values).  kernel(n): "general", "few", "few32", "chunk" or "wide", what serves a sequence of n new tokens.  exps: largest exponent of a block of V
     anywhere (for the weights that fp16 cannot hold).  Returns out, lse and bounds as paged_reference.attend, whose terms hold here too; besides:
 
     few: queries in fp16 below 2^15 of the row's largest channel are off by 2^-39 of it at most; chunk: what e4m3 and e5m2 leave is at most 2^-21 of it.
     Weights are rounded to fp16, half a step, 2^-11; those it cannot hold are off by 2^-25 of a scale where the largest is at least 2^14 (few) or 2^11 (chunk).
+    few32: queries below 2^15 in two parts of fp16 are off by 2^-9 where the largest channel is 2^14 at least; weights in two parts by 2^-22 of themselves or 2^-25 of
+    that scale, and the tensor core cuts off less than 2^-23 of a sum at each of the four additions of 16 tokens (of two parts each).
     wide: keys and values in bf16, which is exact; weights rounded to bf16, half a step, 2^-8.
     chunk, wide: the tensor core cuts off less than 2^-23 of a sum at each addition of 16 tokens, over 128 tiles at most."""
     total, hq, d = q.shape
@@ -95,7 +97,7 @@ def attend(q, k, v, cu, lens, table, kernel, exps, sm_scale=None, softcap=0.0, w
                 s = sc * (x @ kk.T)
                 sums = sc * kk.abs().nan_to_num(nan=0.0).sum(-1)[None]
                 e = sc * (xa @ kk.abs().nan_to_num(nan=0.0).T) * (d + 8) * 2.0 ** -24
-                e = e + {"general": 0.0, "few": 2.0 ** -39, "chunk": 2.0 ** -21, "wide": 0.0}[how] * top_q * sums
+                e = e + {"general": 0.0, "few": 2.0 ** -39, "few32": 2.0 ** -23, "chunk": 2.0 ** -21, "wide": 0.0}[how] * top_q * sums
                 if softcap:
                     s = torch.where(torch.isnan(s), s, softcap * torch.tanh(s / softcap))
                     e = e + softcap * 2.0 ** -21
@@ -114,8 +116,8 @@ def attend(q, k, v, cu, lens, table, kernel, exps, sm_scale=None, softcap=0.0, w
                 e = e + 2.0 ** -20 + 2.0 ** -23 * (s.abs().nan_to_num(posinf=0.0, neginf=0.0, nan=0.0) + 90) + e * e
                 mass, lse_e = w @ va, (w * e).sum(-1)
                 cut = min(L / 16 + 8, 1024) * 2.0 ** -23
-                rel = {"general": 0.0, "few": 2.0 ** -11, "chunk": 2.0 ** -11 + cut, "wide": 2.0 ** -8 + cut}[how]
-                least = {"general": 0.0, "few": 2.0 ** -39, "chunk": 2.0 ** -36, "wide": 0.0}[how] * L * 448 * 2.0 ** exps * w.amax(-1, keepdim=True)
+                rel = {"general": 0.0, "few": 2.0 ** -11, "few32": 2.0 ** -22 + 2.0 ** -21, "chunk": 2.0 ** -11 + cut, "wide": 2.0 ** -8 + cut}[how]
+                least = {"general": 0.0, "few": 2.0 ** -39, "few32": 2.0 ** -39, "chunk": 2.0 ** -36, "wide": 0.0}[how] * L * 448 * 2.0 ** exps * w.amax(-1, keepdim=True)
                 out[r0:r1, m] = o
                 lse[r0:r1, m] = torch.where(z[:, 0] == 0, torch.full_like(top[:, 0], -math.inf), top[:, 0] + torch.log(z[:, 0]))
                 out_b[r0:r1, m] = (w * e) @ va + lse_e[:, None] * mass + rel * mass + least

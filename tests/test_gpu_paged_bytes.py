@@ -84,7 +84,10 @@ class Batch:
                                         k_scales=self.ks, v_scales=self.vs, sm_scale=self.sm_scale)
 
     def kernel(self, n):
-        return "general" if self.flags or self.q_t == torch.float32 else "wide" if self.wide else "few" if n * (self.hq // self.hkv) <= 16 else "chunk"
+        few = n * (self.hq // self.hkv) <= 16
+        if self.flags or self.q_t == torch.float32:
+            return "few32" if few and not self.flags else "general"
+        return "wide" if self.wide else "few" if few else "chunk"
 
     def attend(self, q=None, **kw):
         put = {x: kw.pop(x).to(DEV) for x in ("slopes", "first_key", "prefix_lens") if kw.get(x) is not None}
