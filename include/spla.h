@@ -476,7 +476,8 @@ int spla_paged_query_workspace(const spla_paged_t *paged, const spla_paged_batch
  *   workspace: DEVICE, 256-byte aligned, as spla_paged_query_workspace says; NULL where that is 0.  Calls that may overlap need
  *         one each.
  * bf16 caches and queries run on the tensor cores (probabilities rounded to bf16, sums in fp32), and so do 8-bit pages with bf16 queries (probabilities in fp16;
- * in bf16 where there are many rows for each key, whose keys and values are then widened in the workspace); the others, scales far
+ * in bf16 where there are many rows for each key, whose keys and values are then widened in the workspace) and, up to 16 rows of new tokens x G, with fp32 queries
+ * (queries and probabilities in two parts of fp16: 22 bits); the others, scales far
  * above the cap (10^5 times and more), and SPLA_GENERAL_KERNELS, in fp32.  Results do not depend on max_new, max_len or the rows of other sequences beyond rounding.
  */
 int spla_paged_attend(spla_paged_t *paged, const spla_paged_batch_t *batch, const void *q, int64_t q_stride,
