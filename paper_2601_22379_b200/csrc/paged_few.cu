@@ -18,8 +18,8 @@
 // What bounds it: reading the pages.  32 heads in 8 groups of 128, graphs: one token on 32768 x8 115 us (82 at a copy's rate; bf16 pages 189), x8 heads of 64 75 (41), 17000 x64 375 (340; bf16 660), of
 // 2000 to 32000 x64 under a cap, 40 heads, 393 to 400 (299; bf16 656), 300 x64 31 (6: segments of three tiles, each with its merge), four new tokens on 32768 x8 123.  About 8 us of each are the launch, 12 the ramp and
 // the join.  Inside, of a small case (16384 x8): issue slots 46 %, tensor pipe 16 %, conversions the longest pipe (32 words of a warp's block, 8 cycles each).
-// fp32 queries (two parts, twice the products): one token on 32768 x8 180 us, 300 x64 41, ragged under a cap 895 (the fp32 kernel: 1266, 123, 5235); D = 128 spills 40 to 45 registers
-// a thread there once a segment or tile.
+// fp32 queries (two parts, twice the products): one token on 32768 x8 180 us, 300 x64 41, ragged under a cap 895 (the fp32 kernel: 1266, 123, 5235; heads of 128
+// spill 37 to 45 registers a thread).
 // Steps (32768 x8, which takes 117 now): eight warps of 16 rows each 133, places and scales looked up eight tiles ahead and the rows as columns (R8) 117; capped scores two at a time
 // with the far form only where a score needs it 459 -> 400 (ragged).  Not kept: handing a stage back once its values are in registers (ragged 459 -> 490: the warps fall out of step and
 // the stage waits for the last of them anyway), rings of K and V apart and the merge in halves (459 -> 543), four warps that widen to shared memory.
