@@ -153,7 +153,8 @@ __global__ void __launch_bounds__(kNormThreads, BWD ? 2 : 4)
 #pragma unroll
           for (int i = 0; i < CH; ++i) x[i] = u[i] = 0.f;
         }
-        const float rms = row_rms(x, width, r.per_channel, r.eps);
+        float rms = row_rms(x, width, r.per_channel, r.eps);
+        if (t < 0) rms = 0.f;                                      // (of no row: nothing to the sums, infinite or not)
         row.turn(u, table + max(t, 0) * pairs, own_row);
         float w[CH];
         row.weights(w_s[GI], w);
