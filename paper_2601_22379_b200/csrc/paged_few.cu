@@ -481,6 +481,8 @@ __global__ void __launch_bounds__(kPfThreads<R8>, 1)
             f[x] = 1.f;
           }
           // The first tokens that a row sees set its maximum, one above what their weights need; later ones only move it when a weight would exceed 2^15.
+          // (From scores of 2^24 on fp32 counts in steps of 2 and more, and the largest weight may come out up to a step above 2^15, which fp16 would not hold, or below 2^14,
+          // but never below 1: the weights are held to 2^15, for O and l alike, which is less than the score's own rounding does.)
           if (__any_sync(0xffffffffu, top[0] > m[0] || top[1] > m[1])) {
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
@@ -499,7 +501,7 @@ __global__ void __launch_bounds__(kPfThreads<R8>, 1)
             float sum = 0.f;
 #pragma unroll
             for (int y = 0; y < TOKENS; ++y) {
-              p[x][y] = ex2(p[x][y] + nm);
+              p[x][y] = ex2(min_or_nan(p[x][y] + nm, 15.f));
               sum += p[x][y];
             }
             l[x] = fmaf(l[x], f[x], sum * power_of_two(-ev));
