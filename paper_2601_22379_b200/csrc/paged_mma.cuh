@@ -787,10 +787,19 @@ __global__ void __launch_bounds__(kPmThreads<FEW, BYTES>, 1)
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
           for (int x = 0; x < KEYS; x += 2) mx[x / 2 & 3] = fmaxf(mx[x / 2 & 3], fmaxf(__uint_as_float(r[x]), __uint_as_float(r[x + 1])));
-          const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * (BYTES ? 1.f : mul) - (BYTES ? kPmHead : 0.f);
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * (BYTES ? 1.f : mul);
           // The first visible keys of a row set its maximum (its row of O is zero so far); later ones only move it when it would
-          // let a probability exceed 2^8.
-          const bool grow = mt > m + (BYTES ? kPmGrow : 8.f) && m > -INFINITY;
+          // let a probability exceed 2^8.  (8-bit pages: 2^15, of the difference as it is rounded for the weights.  From scores of 2^24 on fp32 counts in steps of 2 and more,
+          // and 11 may come out as 16, which fp16 would not hold: the maximum is the score itself then.)
+          float mt = top;
+          bool grow;
+          if constexpr (BYTES) {
+            mt = top - kPmHead;
+            if (top - mt > kPmHead + kPmGrow) mt = top;
+            grow = top - m > kPmHead + kPmGrow && m > -INFINITY;
+          } else {
+            grow = mt > m + 8.f && m > -INFINITY;
+          }
           if (m == -INFINITY) m = mt;
           if (__any_sync(0xffffffffu, grow)) {
             if (!pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) return false;   // every product with P so far

@@ -53,7 +53,7 @@ def visible_mean(b, fall=0.0):
     return torch.stack(rows).repeat_interleave(G, 1), torch.tensor(counts).double(), torch.stack(most).repeat_interleave(G, 1)
 
 
-SHAPES = {"one": ([1, 1], [0, 500]), "few": ([3, 2, 1], [700, 30, 0])}
+SHAPES = {"one": ([1, 1], [0, 500]), "few": ([3, 2, 1], [700, 30, 0]), "chunk": ([40, 1], [600, 90])}
 
 
 @kinds
@@ -114,7 +114,7 @@ def test_large_scores_over_scales_of_all_sizes(q, flags, shape, power):
 @pytest.mark.parametrize("q", ["bf16", "f32"])
 def test_a_largest_score_that_is_not_finite(what, q):
     """NaN and infinity among the scores of a row make the row NaN, beside rows with large scores that stay finite."""
-    for new, old in (([2], [40]), ([2, 3], [40, 700])):
+    for new, old in (([2], [40]), ([2, 3], [40, 700]), ([40, 1], [600, 90])):
         b = one_channel(new, old, q, 0, 2.0 ** 26, [0], 64)
         b.q[1, 2, 0] = math.inf if what == "inf" else math.nan
         b.put()
