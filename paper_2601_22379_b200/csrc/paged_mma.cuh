@@ -801,24 +801,36 @@ __global__ void __launch_bounds__(kPmThreads<FEW, BYTES>, 1)
             grow = mt > m + 8.f && m > -INFINITY;
           }
           if (m == -INFINITY) m = mt;
-          if (__any_sync(0xffffffffu, grow)) {
-            if (!pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) return false;   // every product with P so far
-            tc_fence_after();
-            const float m_new = grow ? mt : m, f = grow ? ex2(m - m_new) : 1.f;
-            m = m_new;
-            l *= f;
-            if (LONG) fd *= f;
+          // Plain scores: the weights' products with the scale are not rounded by themselves, the maximum's is; from 2^31 on half its step is more than an exponent has
+          // room for.  There the products are rounded too, and what they are above the maximum takes the scores' place.
+          bool huge = false;
+          if constexpr (!BYTES && !MODS) huge = fabsf(mt) >= 0x1p29f && fabsf(mt) < INFINITY;
+          if (__any_sync(0xffffffffu, grow || huge)) {
+            if (__any_sync(0xffffffffu, grow)) {
+              if (!pm_wait(&pv_done[slot], (n - 1) & 1, lim, abort_flag)) return false;   // every product with P so far
+              tc_fence_after();
+              const float m_new = grow ? mt : m, f = grow ? ex2(m - m_new) : 1.f;
+              m = m_new;
+              l *= f;
+              if (LONG) fd *= f;
 #pragma unroll 1
-            for (int c = 0; c < D; c += 16) {
-              uint32_t o[16];
-              tmem_ld16_async(tO + c, o);
-              tmem_ld_wait16(o);
+              for (int c = 0; c < D; c += 16) {
+                uint32_t o[16];
+                tmem_ld16_async(tO + c, o);
+                tmem_ld_wait16(o);
 #pragma unroll
-              for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
-              tmem_st16(tO + c, o);
+                for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+                tmem_st16(tO + c, o);
+              }
+            }
+            if (!BYTES && !MODS && __any_sync(0xffffffffu, huge)) {
+              const float inv = 1.f / sc2;
+#pragma unroll
+              for (int x = 0; x < KEYS; ++x)
+                if (huge) r[x] = __float_as_uint(__fadd_rn(__fmul_rn(__uint_as_float(r[x]), sc2), -m) * inv);
             }
           }
-          const float nm = m == -INFINITY ? 0.f : -m;
+          const float nm = m == -INFINITY || huge ? 0.f : -m;
           if constexpr (BYTES) {
 #pragma unroll
             for (int c = 0; c < KEYS / 32; ++c) {
