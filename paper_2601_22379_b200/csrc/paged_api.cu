@@ -302,19 +302,17 @@ enum PagedKernel { kGeneral, kTensor, kFew, kTensorBytes, kTensorWide };
 // 2048 184 and 221; 512 on 3500 x4 197 and 213, on 7000 x2 184 and 193.  A key costs about 0.14 ns / head to widen, 256 rows gain 0.04.
 // The measure is the workspace: up to four times the queries' parts, or eight where the sequences have 512 rows on average (200 on 2800 x8 176 and 180).
 // (Documents: which keys are looked at is not known before; they go without.)
-constexpr size_t kWideMost = 8;
-static bool wide_fits(const spla_paged* p, const PagedBatch& pb, const PagedWide& w) {
+static size_t wide_most(const spla_paged* p, const PagedBatch& pb) {
   size_t exps;
-  const size_t parts = paged_split_bytes(p->pl, pb.total_new, &exps);
-  return w.fits && w.bytes <= ((long long)pb.total_new * p->pl.G >= 512ll * pb.batch ? kWideMost : kWideMost / 2) * parts;
+  return ((long long)pb.total_new * p->pl.G >= 512ll * pb.batch ? 8 : 4) * paged_split_bytes(p->pl, pb.total_new, &exps);
 }
-// Bytes of the workspace's front, the same for all launches of a call: the queries' parts, or the widened tokens.
+// Bytes of the workspace's front, the same for all launches of a call: the queries' parts, or the widened tokens as far as they may be widened.
 static size_t front_bytes(const spla_paged* p, const PagedBatch& pb) {
   if (!p->few || pb.max_new <= paged_few_positions(p->pl)) return 0;
   size_t exps;
-  const size_t parts = paged_split_bytes(p->pl, pb.total_new, &exps);
+  const size_t parts = paged_split_bytes(p->pl, pb.total_new, &exps), limit = wide_most(p, pb);
   const PagedWide w = paged_wide(p->pl, pb, 0, 0);                                 // (less with a window, which is not known here)
-  const size_t most = w.fits && w.bytes < kWideMost * parts ? w.bytes : kWideMost * parts;
+  const size_t most = w.fits && w.bytes < limit ? w.bytes : limit;
   return most > parts ? most : parts;
 }
 
@@ -440,7 +438,7 @@ extern "C" int spla_paged_attend_sinks(spla_paged_t* p, const spla_paged_batch_t
   size_t exps = 0;
   char* front = reinterpret_cast<char*>(workspace);
   PagedMaps wide_maps;
-  const bool wide = tensor_fits && parts && !mask->first_key && wide_fits(p, pb, w) &&
+  const bool wide = tensor_fits && parts && !mask->first_key && w.fits && w.bytes <= wide_most(p, pb) &&
                     make_kv_map(wide_maps.k, front, p->pl.d, kWidePage, (unsigned long long)w.pl.n_pages * w.pl.page_stride) &&
                     make_kv_map(wide_maps.v, front + w.v_at, p->pl.d, kWidePage, (unsigned long long)w.pl.n_pages * w.pl.page_stride) &&
                     make_q_map(wide_maps.q, q, p->pl, q_stride, pb);
