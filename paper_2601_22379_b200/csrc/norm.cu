@@ -240,12 +240,13 @@ struct NormPlan {
   int tb, tiles_per_batch, ys, rows_per_y, grid_x;
   long long tiles;
 };
-// tokens and heads alone decide it: the sums that the weights' gradients take are the same for any addresses
+// (sizes alone decide it, not addresses: the workspace is asked for without them)
 NormPlan plan_norm(const RopeTable& rt, int batch, int tokens, int heads, bool backward, int sm_count) {
   NormPlan p;
   const int pairs = rt.rot / 2;
   constexpr int by = 32;
-  auto tiles = [&](int x) { return (long long)((tokens + x - 1) / x) * batch; };
+  auto per_batch = [&](int x) { return (int)(((long long)tokens + x - 1) / x); };
+  auto tiles = [&](int x) { return (long long)per_batch(x) * batch; };
   int tb, most = kNormTable / pairs < 64 ? kNormTable / pairs : 64;
   if (backward) {
     // two CTAs an SM, each as many tiles as the next, as large as the table of sines allows: what comes before a tile's first row is rarely paid
@@ -263,7 +264,7 @@ NormPlan plan_norm(const RopeTable& rt, int batch, int tokens, int heads, bool b
   while (tb > 1 && tiles(tb) < (backward ? 1LL : 2LL) * sm_count) tb /= 2;
   if (tb > tokens) tb = tokens;
   p.tb = tb;
-  p.tiles_per_batch = (tokens + tb - 1) / tb;
+  p.tiles_per_batch = per_batch(tb);
   p.tiles = tiles(tb);
   const int rows = tb * heads;
   p.ys = 1;
