@@ -400,7 +400,8 @@ int spla_paged_destroy(spla_paged_t *paged);   /* NULL is allowed */
  * Appending: the scale of a block of 16 tokens is the least 2^e, e in [-40, 40], with every magnitude of the block at most 448 2^e; values are
  * rounded to the nearest e4m3 (beyond 448 2^40: 448 2^40; NaN and infinities: NaN, without part in the scale).  A block whose first token is among the
  * new ones starts anew, whatever its bytes were; one that was begun before keeps its scale where that is large enough, or else
- * its tokens before the new ones are rounded again to the larger one (exact, but for values that come below 2^-6 of it).
+ * its tokens before the new ones are rounded again to the larger one (exact, but for values that come below 2^-6 of it).  So a block that is begun
+ * belongs to one sequence that appends to it; others that read its first tokens see them rounded again.
  */
 int spla_paged_create_scaled(const spla_paged_config_t *config, void *k_pages, void *v_pages, uint8_t *k_scales, uint8_t *v_scales, int32_t *status,
                            spla_paged_t **paged_out);
@@ -476,9 +477,10 @@ int spla_paged_query_workspace(const spla_paged_t *paged, const spla_paged_batch
  *   workspace: DEVICE, 256-byte aligned, as spla_paged_query_workspace says; NULL where that is 0.  Calls that may overlap need
  *         one each.
  * bf16 caches and queries run on the tensor cores (probabilities rounded to bf16, sums in fp32), and so do 8-bit pages with bf16 queries (probabilities in fp16;
- * in bf16 where there are many rows for each key, whose keys and values are then widened in the workspace) and, up to 16 rows of new tokens x G, with fp32 queries
+ * in bf16, for all sequences of a call, where by its sizes there are many rows for each key, whose keys and values are then widened in the workspace) and, up to 16 rows of new tokens x G, with fp32 queries
  * (queries and probabilities in two parts of fp16: 22 bits); the others, scales far
  * above the cap (10^5 times and more), and SPLA_GENERAL_KERNELS, in fp32.  Results do not depend on max_new, max_len or the rows of other sequences beyond rounding.
+ * (Which for 8-bit pages takes in that the exponent of a value's scale, up to 40, is added to its score in base 2, in fp32: what a score of 2^20 or more is in steps of an eighth or more.)
  */
 int spla_paged_attend(spla_paged_t *paged, const spla_paged_batch_t *batch, const void *q, int64_t q_stride,
                       const spla_paged_mask_t *mask, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);

@@ -11,8 +11,8 @@
 // rows meet in shared memory, and a second kernel adds the CTAs' sums in their order: no atomics, the same bits every time.
 // All arithmetic in fp32, one rounding at the end.
 //
-// What bounds it: memory, read and write once.  Forward, 4 x 8192 tokens of 32 + 8 heads of 128 in bf16: 125 us in a graph (102 at a copy's rate), fp32 16 + 4 heads
-// of 64 20.5 (12.8).  Gradients 200 us (153): two reads for a write, 128 registers, two CTAs an SM.  Few tokens: launches (eight tokens 8 us, what a graph of one
+// What bounds it: memory, read and write once.  Forward, 4 x 8192 tokens of 32 + 8 heads of 128 in bf16: 125 us in a graph (102 at a copy's rate), in fp32 217 (204), 3 x 2731
+// of 16 + 4 heads of 64 in fp32 22 (12.8).  Gradients 197 us (153), in fp32 357 (307), the smaller one 39 (19): two reads for a write, 128 registers, two CTAs an SM.  Few tokens: launches (eight tokens 8 us, what a graph of one
 // small kernel takes here; the second kernel of the gradients takes 7 by itself when it is cold).  Steps: groups known to the compiler, four CTAs an SM and one row a thread 158 -> 135 us (two rows under way and three
 // CTAs 156; five and six CTAs were slower too), the next row asked for as soon as this one's values are out of its registers 134 -> 125 (three CTAs 131, fp32 20.5 -> 24.6); gradients with tiles as large as the table allows and two values at a time 281 -> 197.
 #include <type_traits>

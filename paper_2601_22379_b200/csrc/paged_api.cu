@@ -297,11 +297,15 @@ extern "C" int spla_paged_read(spla_paged_t* p, const spla_paged_batch_t* batch,
 enum PagedKernel { kGeneral, kTensor, kFew, kTensorBytes, kTensorWide };
 
 // 8-bit pages, sequences of more rows than few: where there are enough rows for each key, the keys and values (with a window, its and the sinks') are widened to
-// bf16 in a pass of their own, once for all rows, and the kernel for bf16 pages does the rest.  Graphs, us, this way and over the 8-bit pages: a prompt of 8192 tokens 567 and
-// 690, of 1000 43 and 55, of 64 31 and 45; ragged ones of up to 2000 x16 320 and 438; 4000 on 4000 with a window of 512 125 and 164; 1 to 600 on 100 to 9000 x24 with a window of
-// 2048 184 and 221; 512 on 3500 x4 197 and 213, on 7000 x2 184 and 193.  A key costs about 0.14 ns / head to widen, 256 rows gain 0.04.
-// The measure is the workspace: up to four times the queries' parts, or eight where the sequences have 512 rows on average (200 on 2800 x8 176 and 180).
-// (Documents: which keys are looked at is not known before; they go without.)
+// bf16 in a pass of their own, once for all rows, and the kernel for bf16 pages does the rest.  Graphs, us, this way and over the 8-bit pages: a prompt of 8192 tokens 539 and
+// 688, of 1000 43 and 55, of 64 31 and 41; ragged ones of up to 2000 x16 307 and 436; 4000 on 4000 with a window of 512 119 and 162; 1 to 600 on 100 to 9000 x24 with a window of
+// 2048 182 and 217; 512 on 3500 x4 186 and 207, on 7000 x2 174 and 186.
+// It pays from 1000 to 1500 rows of queries for each key on (32 heads in 8 groups of 128: 512 tokens, 2048 rows, on 8000 117 and 127, on 32768 x4 1243 and 1299, 2048 tokens there 4507 and
+// 5256; 128 tokens on 8000 x4 150 and 127, on 32768 x4 473 and 363), and on caches of no more than 2000 with any number, where it is a launch less, or two (33 tokens on none 27 and 39, on
+// 2000 41 and 47).  What is looked at here instead is memory: up to four times the queries' parts, or eight where the sequences have 512 rows on average (200 on 2800 x8 170 and 177), so that
+// the longest caches are left to the slower way (512 on 32768 360 in place of 330, 2048 on 32768 x4 5174 of 4507).  (Documents: which keys are looked at is not known before; they go without.)
+// Weights are rounded to bf16 this way, 2^-8, to fp16 the other, 2^-11: the error of out against float64 (2-norm) is 2.0e-3 in place of 1.7e-3, which is what the rounding of
+// out takes alone.  It goes by the call's sizes, so a sequence may be served the one way in one batch and the other in the next.
 static size_t wide_most(const spla_paged* p, const PagedBatch& pb) {
   size_t exps;
   return ((long long)pb.total_new * p->pl.G >= 512ll * pb.batch ? 8 : 4) * paged_split_bytes(p->pl, pb.total_new, &exps);

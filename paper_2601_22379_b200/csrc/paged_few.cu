@@ -93,7 +93,8 @@ __device__ __forceinline__ uint32_t transposed(uint32_t v) {
 
 // R8: at most 8 rows.  Tokens and channels are the products' 16 rows then, the queries their 8 columns: half the products and half the registers, so
 // that sixteen warps work, eight on a tile and eight on the next.
-// F32: fp32 queries and outputs.  Queries and weights are two parts of fp16, 22 bits, each times the same fragments: 2^-24 of a row's largest channel, of its largest weight.
+// F32: fp32 queries and outputs.  Queries and weights are two parts of fp16, 22 bits, each times the same fragments: channels are off by 2^-23 of a row's largest at most (its second part
+// is up to 8 where the largest is 2^14, rounded to steps of 2^-8), weights by 2^-22 of themselves, or 2^-25 where the row's largest is 2^14 at least.
 template <int D, bool MODS, bool R8, bool F32>
 __global__ void __launch_bounds__(kPfThreads<R8>, 1)
     paged_few_kernel(const __grid_constant__ PagedAttend a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {

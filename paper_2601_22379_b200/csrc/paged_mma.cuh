@@ -35,9 +35,9 @@
 // eight of 16 that bf16 takes, and half the bytes.  Values are widened to fp16, in which e4m3 is exact, from a ring that TMA fills (a product takes both operands from one type's
 // family, and P needs more than 8 bits).  Scales touch neither: K's multiplies its 16 scores, V's is an exponent that is added to theirs, so that weights stay below 2^15 whatever the blocks'
 // scales are (kPmHead, kPmGrow), and l sums w 2^-ev.  P is fp16, half a step of 2^-11.  Warp 0 brings K, V, queries and scales, warp 2 (of FEW warps 12 to 15) widens V.
-// Of a prompt's 717 us (690 now) the widening cost 51, the scales 36 and the queries' second part 37 (each taken out in turn; bf16 pages 543): calls of many rows for each key widen K and V
-// before instead (paged_api.cu).  Here remain chunks on a long cache (graphs, us, bf16 pages beside: 512 on 32768 x2 678 and 576, 33 on 32768 x8 348 and 279), documents, and 17 to 32
-// rows, which read half the bytes (8 on 32768 x8 166 and 199).  Not kept: K and V widened by four warps from registers (prompt 1014), queries split by the softmax warps (848),
+// Of a prompt's 717 us (688 now) the widening cost 51, the scales 36 and the queries' second part 37 (each taken out in turn; bf16 pages 543, 528 now): calls of many rows for each key widen K
+// and V before instead (paged_api.cu).  Here remain chunks on a long cache (graphs, us, bf16 pages beside: 512 on 32768 x2 676 and 553, 33 on 32768 x8 342 and 270), documents, and 17 to 32
+// rows, which read half the bytes (8 on 32768 x8 164 and 195).  Not kept: K and V widened by four warps from registers (prompt 1014), queries split by the softmax warps (848),
 // a factor for every block instead of a pass over the scores (spills, 759), widening by four warps for all (733).
 //
 // Every wait is bounded; on expiry the CTA's roles leave their loops, copies and products in flight are waited for, tensor memory is

@@ -3,7 +3,7 @@
 // 8-bit pages hold e4m3 values and a power-of-two scale 2^e for every 16 tokens of a head (a block):  e is the least integer with
 // max |x| <= 448 2^e over the block's tokens, between -40 and 40.  Powers of two cost no accuracy (a floating format's steps are relative), a
 // value times its scale is exact in bf16, and a block that is begun in one call and grown in the next is rescaled exactly but for values
-// below 2^-14 of its largest, which lose bits at the format's end: e only grows, so that any cutting of the tokens into calls ends with the same scale.
+// below 2^-6 of the new scale, which lose bits at the format's end: e only grows, so that any cutting of the tokens into calls ends with the same scale.
 //
 // A run is the new tokens of one block: at most 16 rows of one sequence.  A CTA takes the runs that start in its rows; a warp takes a run of one
 // head (or a single new token of several heads), holds it in registers, norms and turns it, finds the largest magnitude by shuffles and
@@ -13,7 +13,8 @@
 // What bounds it: the first loads of a CTA come behind a search for its sequences and the page table's entries, which are dependent loads; then memory.  A prompt of 32768 tokens of 32 + 8 + 8
 // heads of 128 in bf16: 166 us in a graph (112 at a copy's rate), 16384 in fp32, pages of 16: 43 (27), turns of 50 to 700 tokens x 16 61 (23), a token for each of 64
 // sequences 14 (launch 8).  Steps: a body for each kind of head, so that rows without norm or turn skip them, and packed arithmetic 242 -> 164 us (prompt).
-// Reading back: 131072 tokens, 8 heads of 128: 154 us (123), in pages of 16 54 (30).
+// Reading back: 131072 tokens, 8 heads of 128: 154 us (123), 32000 tokens in pages of 16 54 (30).  Norms on the way into pages of 16 and 32 bits (without them rope.cu's times, in
+// brackets, then the floor): a prompt of 32768 in bf16 156 (141; 123), turns 53 (37; 23), in fp32 72 (66; 47), 16384 in fp32 in pages of 16 47 (43; 31).
 #include <type_traits>
 
 #include "rope_device.cuh"
