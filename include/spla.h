@@ -347,7 +347,7 @@ int spla_rope_apply(const spla_rope_t *rope, const int32_t *positions, int32_t b
  */
 typedef struct {
   const float *q_weight, *k_weight;  /* DEVICE fp32 [head_dim]: w of queries and of keys, shared by their heads */
-  float eps;                         /* >= 0.  With 0 a row whose squares are all 0 in fp32 (magnitudes below 10^-23) is NaN, as are its gradients and its weight's */
+  float eps;                         /* >= 0.  With 0 a row whose squares are all 0 in fp32 (magnitudes below 10^-23) does not come out finite, nor do its gradients and its weight's */
 } spla_head_norm_t;
 
 /* As spla_rope_apply, without `transpose`.  Both weights are given (k_weight with k only). */

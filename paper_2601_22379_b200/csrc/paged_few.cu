@@ -445,9 +445,9 @@ __global__ void __launch_bounds__(kPfThreads<R8>, 1)
 #pragma unroll
                 for (int y = 0; y < TOKENS; y += 2) {
                   const float2 z = make_float2(p[x][y], p[x][y + 1]), u = __fmul2_rn(z, make_float2(to_u, to_u)), u2 = __fmul2_rn(u, u);
-                  float2 c = __ffma2_rn(u2, make_float2(-0.048268907f, -0.048268907f), make_float2(0.13284431f, 0.13284431f));
-                  c = __ffma2_rn(u2, c, make_float2(-0.33331972f, -0.33331972f));
-                  c = __fmul2_rn(z, __ffma2_rn(u2, c, make_float2(0.99999994f, 0.99999994f)));
+                  float2 c = __ffma2_rn(u2, make_float2(kTanh3, kTanh3), make_float2(kTanh2, kTanh2));
+                  c = __ffma2_rn(u2, c, make_float2(kTanh1, kTanh1));
+                  c = __fmul2_rn(z, __ffma2_rn(u2, c, make_float2(kTanh0, kTanh0)));
                   p[x][y] = c.x;
                   p[x][y + 1] = c.y;
                   if (far) {

@@ -588,8 +588,8 @@ __global__ void __launch_bounds__(kPmThreads<FEW, BYTES>, 1)
     const uint32_t tS = tmem + slot * 128 + lane_off, tO = tmem + 256 + slot * 128 + lane_off;
     const float sc2 = a.sm_scale * kLog2e;
     const float to_u = MODS && a.softcap > 0.f ? a.sm_scale / a.softcap : 0.f, sq_u = to_u * to_u;
-    const float cap0 = 0.99999994f * sc2, cap1 = -0.33331972f * sc2 * sq_u, cap2 = 0.13284431f * sc2 * sq_u * sq_u,
-                cap3 = -0.048268907f * sc2 * sq_u * sq_u * sq_u;   // (a score of 1 is sc2 in base 2)
+    const float cap0 = kTanh0 * sc2, cap1 = kTanh1 * sc2 * sq_u, cap2 = kTanh2 * sc2 * sq_u * sq_u,
+                cap3 = kTanh3 * sc2 * sq_u * sq_u * sq_u;   // (a score of 1 is sc2 in base 2)
     auto not_finite = [](uint32_t w) { return BYTES ? pair_not_finite_f16(w) : pair_not_finite(w); };
     auto val_lo = [](uint32_t w) { return BYTES ? f16_lo(w) : bf16_lo(w); };
     auto val_hi = [](uint32_t w) { return BYTES ? f16_hi(w) : bf16_hi(w); };
@@ -726,7 +726,7 @@ __global__ void __launch_bounds__(kPmThreads<FEW, BYTES>, 1)
           }
           if constexpr (MODS) {
             if (a.softcap > 0.f) {
-              // cap tanh(u), u = x / cap, in base 2.  Up to |u| = 3/8 an odd polynomial (interpolated at Chebyshev nodes, 6e-8 off), its coefficients
+              // cap tanh(u), u = x / cap, in base 2.  Up to |u| = 3/8 an odd polynomial (kTanh0 ..), its coefficients
               // scaled to the raw scores; where a row of the warp has more, 1 - 2 / (1 + e^(2 |u|)) there, which alone would be off by
               // 2^-22 of the cap, however small the score, and takes two of the exponential unit's turns per key.
               float most = 0.f;

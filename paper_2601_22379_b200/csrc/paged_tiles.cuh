@@ -22,7 +22,8 @@ __device__ __forceinline__ bool pm_wait(uint64_t* bar, uint32_t parity, int limi
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, 1)) || pm_wait_slow(bar, parity, limit, abort_flag);
 }
 
-constexpr float kCapNear = 0.375f;                 // up to here tanh goes by a polynomial
+constexpr float kCapNear = 0.375f;                 // up to here tanh goes by a polynomial: u (c0 + c1 u^2 + c2 u^4 + c3 u^6), interpolated at Chebyshev nodes, 6e-8 off
+constexpr float kTanh0 = 0.99999994f, kTanh1 = -0.33331972f, kTanh2 = 0.13284431f, kTanh3 = -0.048268907f;
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float y;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
